@@ -52,6 +52,8 @@ extern "C" {
 #define SALT_MAX_GROUP 8             /* projections per grouped apply */
 #define SALT_MAX_GAMMA_BINS 16       /* gamma bins of one segments build */
 #define SALT_MAX_ALIGN_RANK 128      /* r + rc of one alignment pair */
+#define SALT_MAX_KV_PAGE 128         /* tokens per cache page (a power of two, at least 16) */
+#define SALT_MAX_VOCAB (1 << 20)     /* tokens of a vocabulary salt_verify_drafts draws from */
 #define SALT_BLOB_HEADER_BYTES 256
 #define SALT_BLOB_MAGIC 0x3153455254414C53ULL /* "SALTRES1" little-endian */
 
@@ -89,7 +91,9 @@ typedef enum salt_status {
 #define SALT_DEVERR_RANK 0x10u
 #define SALT_DEVERR_TIMEOUT 0x20u        /* a bounded in-kernel wait gave up (results of that call invalid) */
 #define SALT_DEVERR_GAMMA_RANGE 0x40u
-#define SALT_DEVERR_BATCH 0x80u          /* a captured salt_lora_apply_with_base was replayed on a larger batch */
+#define SALT_DEVERR_BATCH 0x80u          /* a captured call was replayed on a larger batch (salt_lora_apply_with_base, salt_attn_run) */
+#define SALT_DEVERR_KV_SLOT 0x100u       /* a cache slot outside the cache (salt_kv_write, salt_kv_read) */
+#define SALT_DEVERR_DRAFT 0x200u         /* draft pointers out of order or a drafted token outside the vocabulary */
 
 /*
  * Context configuration.  d_in / d_out are host arrays of n_layers entries,
@@ -539,6 +543,168 @@ typedef struct salt_align_pair {
 } salt_align_pair;
 salt_status salt_align_loss(int32_t n, const salt_align_pair *pairs, float eps, float *loss,
                             float *cosine, salt_stream_t stream);
+
+/*
+ * A paged key/value cache of 8-bit floats, for the attention between the
+ * adapted q/k/v and o projections.  (The paper leaves attention to its
+ * serving engine; with it a domain's requests can share their prompt's
+ * cache as they share the domain's centroid.)  The memory is the caller's:
+ * device arrays, 16-byte aligned,
+ *     k, v:         e4m3 codes [n_layers][n_pages][n_kv_heads][page_tokens][head_dim]
+ *     k_exp, v_exp: bytes      [n_layers][n_pages][n_kv_heads][page_tokens]
+ * A row (one token, one head) x is stored as codes c and one exponent byte
+ * e and stands for c * 2^(e - 127): with a = max |x| and k the smallest
+ * integer with a <= 448 * 2^k, but at least -126, c = x / 2^k rounded once to
+ * e4m3 (round to nearest even) and e = k + 127.  A power of two, not
+ * a / 448, so that scaling itself never rounds and a stored value is exact in
+ * bf16; it costs at most one of the code's 15 binades.  A row of
+ * zeros has e = 0; a row with an infinity or a NaN is stored as e = 255 and
+ * zero codes and stands for NaN throughout.  A slot is page * page_tokens +
+ * offset in the page.  head_dim is 64 or 128, page_tokens 16, 32, 64 or 128;
+ * n_layers * n_pages * n_kv_heads * page_tokens < 2^31.
+ */
+typedef struct salt_kv salt_kv;
+typedef struct salt_kv_config {
+    int32_t n_layers;
+    int32_t n_pages;
+    int32_t n_kv_heads;
+    int32_t page_tokens;
+    int32_t head_dim;
+    void *k, *v;
+    void *k_exp, *v_exp;
+} salt_kv_config;
+
+/* A handle on the caller's cache memory, which must outlive it (nothing is
+ * initialised).  Destroy it, and the plans made from it, before the context.
+ * Host only. */
+salt_status salt_kv_create(salt_ctx *ctx, const salt_kv_config *config, salt_kv **out);
+/* NULL is a no-op.  The calls enqueued on the cache may still be running. */
+void salt_kv_destroy(salt_kv *kv);
+
+/*
+ * Quantise and store new tokens: row t of k and v ([n_tokens] rows of
+ * [n_kv_heads][head_dim] bf16, k_stride / v_stride elements apart, multiples of
+ * 8, so slices of a fused projection's rows need no copy) goes to slot
+ * slots[t] of `layer`.  slots is device int32[n_tokens]; -1 skips the token,
+ * any other slot outside the cache is skipped too and raises
+ * SALT_DEVERR_KV_SLOT.  Slots of one call must be distinct.  k, v are 16-byte
+ * aligned.  One kernel; asynchronous on `stream`.
+ */
+salt_status salt_kv_write(salt_kv *kv, int32_t layer, int32_t n_tokens, const void *k, int64_t k_stride,
+                          const void *v, int64_t v_stride, const int32_t *slots, salt_stream_t stream);
+
+/*
+ * The cached rows of slots[0..n_tokens) back as bf16, laid out as in
+ * salt_kv_write: exact, but for results below the normal range of bf16 (rounded)
+ * and above the range (infinite).  A slot of -1 gives zeros, and so does one
+ * outside the cache, which raises SALT_DEVERR_KV_SLOT.  Asynchronous on
+ * `stream`.
+ */
+salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int32_t *slots, void *k,
+                         int64_t k_stride, void *v, int64_t v_stride, salt_stream_t stream);
+
+/*
+ * Attention of a batch over the cache, the requests of a group (a domain,
+ * say) sharing a prompt that is read once for all of them.  A plan is made
+ * for a cache and the limits of the batches, built once a step from the
+ * batch's lengths and pages, and run for every layer.
+ */
+typedef struct salt_attn salt_attn;
+typedef struct salt_attn_config {
+    int32_t n_heads;     /* query heads, a multiple of the cache's n_kv_heads (at most 64 times) */
+    int32_t max_seqs;    /* requests of a batch, at most SALT_MAX_TOKENS */
+    int32_t max_tokens;  /* query tokens of a batch, at most SALT_MAX_TOKENS */
+    int32_t max_pages;   /* entries of a batch's page lists, the groups' and the requests' together */
+    int32_t max_groups;  /* groups of a batch, at most SALT_MAX_TOKENS */
+} salt_attn_config;
+
+/*
+ * A batch, in host arrays (read during the build only).  Request b has
+ * q_len[b] >= 0 query tokens, which follow those of request b - 1, and
+ * kv_len[b] >= 0 cached tokens of its own, the query tokens among them (so
+ * they are written before the run): token j lies in page
+ * pages[page_ptr[b] + j / page_tokens], offset j % page_tokens.  group[b] is
+ * its group or -1; group g has a prompt of group_len[g] >= 0 cached tokens in
+ * pages group_pages[group_page_ptr[g] + ...].  A page list may be longer than
+ * its tokens need.  With n_groups == 0 the group arrays may be NULL.
+ */
+typedef struct salt_attn_batch {
+    int32_t n_seqs;
+    const int32_t *q_len;           /* [n_seqs] */
+    const int32_t *kv_len;          /* [n_seqs] */
+    const int32_t *page_ptr;        /* [n_seqs + 1] */
+    const int32_t *pages;           /* [page_ptr[n_seqs]] */
+    const int32_t *group;           /* [n_seqs] */
+    int32_t n_groups;
+    const int32_t *group_len;       /* [n_groups] */
+    const int32_t *group_page_ptr;  /* [n_groups + 1] */
+    const int32_t *group_pages;     /* [group_page_ptr[n_groups]] */
+} salt_attn_batch;
+
+/* Allocates the plan's device tables and workspace.  The plan keeps kv, which
+ * must outlive it.  Synchronous. */
+salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *config, salt_attn **out);
+/* Waits for the device, then frees the plan.  NULL is a no-op. */
+void salt_attn_destroy(salt_attn *plan);
+
+/*
+ * Plan a batch: every length and page is checked on the host (an error leaves
+ * the plan not built) and the work is divided over the SMs.  Asynchronous on
+ * `stream`, after the runs enqueued on the previous build; not to be captured
+ * (SALT_ERR_INVALID_ARG), but a captured run may be replayed after the plan
+ * was built again.
+ */
+salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_stream_t stream);
+
+/*
+ * Row i (0 <= i < q_len[b]) of request b sees its group's whole prompt and its
+ * own tokens [0, kv_len[b] - q_len[b] + i]; query head h reads key/value head
+ * h / (n_heads / n_kv_heads):
+ *     out = sum_j softmax_j(scale * q k_j) v_j,   lse = log sum_j exp(scale * q k_j)
+ * over the tokens j it sees.  A row that sees none gives zeros and a log-sum of
+ * minus infinity; what lies in pages past a length is never used.  q and
+ * out are rows of [n_heads][head_dim] bf16, q_stride / out_stride elements apart
+ * (multiples of 8), 16-byte aligned; out must not overlap q.  lse is float
+ * [tokens][n_heads] or NULL.  Scores, running maxima, sums and partial results
+ * are held in fp32 and out is rounded once.  The query and the probabilities
+ * meet the 8-bit cache as sums of two e4m3 terms each (about 8 bits, as
+ * bf16).  A row with an infinity or a NaN in its query, or that sees a cached
+ * row standing for NaN, is NaN.  Results do not depend on timing.
+ * Asynchronous on `stream`; runs of one plan share its workspace and are
+ * ordered one after the other.  A captured run may be replayed after the
+ * plan was built again with at most as many query tokens as it had at the capture; on a larger
+ * batch it computes and writes nothing and raises SALT_DEVERR_BATCH.
+ */
+salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, float scale,
+                          void *out, int64_t out_stride, float *lse, salt_stream_t stream);
+
+/*
+ * Hold drafted tokens against the target model's probabilities (speculative
+ * decoding's rejection step; no counterpart in the paper).  Request b
+ * has the drafted tokens draft_tokens[draft_ptr[b] .. draft_ptr[b + 1]), each
+ * drawn from its row of draft_p ([n_drafts] rows of n_vocab floats,
+ * draft_stride elements apart), and one more row of target_p ([n_drafts +
+ * n_seqs] rows, request b's first at draft_ptr[b] + b).  Draft j, token t, is
+ * accepted while
+ *     accept_u[j] * draft_p[j][t] < target_p[j + b][t]   (one fp32 product);
+ * at the first that is not, the next token is drawn from max(p - q, 0) of that row
+ * (from p where that is zero throughout); when all are accepted, from p of the row
+ * after the last.  Drawn by inverting the running sum: with W[v] the weight (at
+ * most 1, NaN and below zero count as 0) in whole units of 2^-40, W their sum and
+ * U = floor(sample_u[b] * 2^24), the first v with W[0] + .. + W[v] > floor(U * W /
+ * 2^24), computed in 64-bit integers, so the result depends on no order of
+ * summation.  accepted[b] gets the drafts accepted, next_token[b] the token
+ * (-1 when the row has no weight).  sample_u in [0, 1).  Every pointer is
+ * device memory; int32 but for the floats.  A request whose draft_ptr is
+ * out of order or range gets 0 and -1, and a drafted token outside the vocabulary is
+ * not accepted; both raise SALT_DEVERR_DRAFT.  n_vocab <= SALT_MAX_VOCAB.
+ * One kernel, asynchronous on `stream`.
+ */
+salt_status salt_verify_drafts(salt_ctx *ctx, int32_t n_seqs, int32_t n_drafts, int32_t n_vocab,
+                               const int32_t *draft_ptr, const int32_t *draft_tokens, const float *target_p,
+                               int64_t target_stride, const float *draft_p, int64_t draft_stride,
+                               const float *accept_u, const float *sample_u, int32_t *accepted,
+                               int32_t *next_token, salt_stream_t stream);
 
 /*
  * Self-test of the failure path.  Enqueues on `stream` one thread that

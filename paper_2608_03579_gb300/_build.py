@@ -19,7 +19,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsalt.so")
 SOURCES = ["salt_runtime.cu", "salt_segments.cu", "salt_apply.cu", "salt_base.cu", "salt_fold.cu", "salt_align.cu",
-           "salt_swap.cu"]
+           "salt_swap.cu", "salt_kv.cu", "salt_attn.cu", "salt_verify.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

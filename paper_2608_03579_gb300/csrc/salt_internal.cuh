@@ -268,4 +268,16 @@ constexpr int STATIC_PART_CAP = 256;
 // device with cudaGetSymbolAddress); blk_cap = STATIC_APPLY_BLOCKS.
 cudaError_t apply_static_workspace(ApplyWork *out);
 
+// Device view of a key/value cache (one layer's arrays start at layer * n_pages pages).
+struct KvDev {
+    uint8_t *k, *v, *k_exp, *v_exp;
+    int32_t n_pages, heads, page, page_log2, dim;
+};
+
 }  // namespace salt
+
+struct salt_kv {
+    salt_ctx *ctx;
+    int n_layers;
+    salt::KvDev dev;
+};

@@ -20,8 +20,7 @@
 
 #include <sys/mman.h>
 
-#include <nvtx3/nvToolsExt.h>
-
+#include "salt_host.cuh"
 #include "salt_internal.cuh"
 
 using namespace salt;
@@ -105,28 +104,7 @@ struct salt_host_pipe {
 
 namespace {
 
-// A named NVTX range around a library call on the host (what a timeline
-// tool shows next to the kernels the call enqueues); free when no tool is
-// attached.
-struct NvtxRange {
-    explicit NvtxRange(const char *name) { nvtxRangePushA(name); }
-    ~NvtxRange() { nvtxRangePop(); }
-    NvtxRange(const NvtxRange &) = delete;
-    NvtxRange &operator=(const NvtxRange &) = delete;
-};
-
-salt_status fail(salt_ctx *ctx, salt_status s, const char *fmt, ...)
-{
-    if (ctx) {
-        char buf[512];
-        va_list ap;
-        va_start(ap, fmt);
-        vsnprintf(buf, sizeof buf, fmt, ap);
-        va_end(ap);
-        ctx->last_error = buf;
-    }
-    return s;
-}
+salt_status (*const fail)(salt_ctx *, salt_status, const char *, ...) = ctx_fail;
 
 #define CUDA_OR_FAIL(ctx, call)                                                                    \
     do {                                                                                           \
@@ -472,6 +450,25 @@ salt_status enqueue_loads(salt_ctx *ctx, int32_t n, const int32_t *slots, const 
     return SALT_OK;
 }
 }  // namespace
+
+namespace salt {
+salt_status ctx_fail(salt_ctx *ctx, salt_status s, const char *fmt, ...)
+{
+    if (ctx) {
+        char buf[512];
+        va_list ap;
+        va_start(ap, fmt);
+        vsnprintf(buf, sizeof buf, fmt, ap);
+        va_end(ap);
+        ctx->last_error = buf;
+    }
+    return s;
+}
+bool ctx_select_device(salt_ctx *ctx) { return set_device(ctx); }
+int ctx_device(const salt_ctx *ctx) { return ctx->device; }
+uint32_t *ctx_error_word(salt_ctx *ctx) { return ctx->err_dev; }
+bool on_device(const void *p) { return is_device_pointer(p); }
+}  // namespace salt
 
 extern "C" {
 

@@ -71,6 +71,22 @@ class salt_base_shape(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("cta_group", "tile_cols", "k_splits", "shrink_ctas", "units", "clusters")]
 
 
+class _kv_config(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("n_layers", "n_pages", "n_kv_heads", "page_tokens", "head_dim")]
+                + [(k, ctypes.c_void_p) for k in ("k", "v", "k_exp", "v_exp")])
+
+
+class _attn_config(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("n_heads", "max_seqs", "max_tokens", "max_pages", "max_groups")]
+
+
+class _attn_batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("q_len", ctypes.c_void_p), ("kv_len", ctypes.c_void_p),
+                ("page_ptr", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("group", ctypes.c_void_p),
+                ("n_groups", ctypes.c_int32), ("group_len", ctypes.c_void_p), ("group_page_ptr", ctypes.c_void_p),
+                ("group_pages", ctypes.c_void_p)]
+
+
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _SIGS = {
     "salt_abi_version": (_i32, []),
@@ -111,6 +127,16 @@ _SIGS = {
     "salt_fold_plan_create": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i32, ctypes.POINTER(_vp)]),
     "salt_fold_plan_run": (ctypes.c_int, [_vp, _f32, _vp]),
     "salt_fold_plan_destroy": (None, [_vp]),
+    "salt_kv_create": (ctypes.c_int, [_vp, ctypes.POINTER(_kv_config), ctypes.POINTER(_vp)]),
+    "salt_kv_destroy": (None, [_vp]),
+    "salt_kv_write": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "salt_kv_read": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "salt_attn_create": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_config), ctypes.POINTER(_vp)]),
+    "salt_attn_destroy": (None, [_vp]),
+    "salt_attn_build": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_batch), _vp]),
+    "salt_attn_run": (ctypes.c_int, [_vp, _i32, _vp, _i64, _f32, _vp, _i64, _vp, _vp]),
+    "salt_verify_drafts": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp,
+                                          _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -437,6 +463,187 @@ def salt_lora_apply_host(pipe, seg, layers, x_hosts, y_hosts, stream=None) -> No
 
 def salt_host_pipe_wait(pipe, stream=None) -> None:
     _check(_lib.salt_host_pipe_wait(pipe.ptr, _stream(stream)), pipe.ctx)
+
+
+class KvCache:
+    """A salt_kv handle on the caller's cache tensors (kept alive with it)."""
+
+    def __init__(self, ctx, k, v, k_exp, v_exp):
+        if k.dim() != 5 or tuple(v.shape) != tuple(k.shape):
+            raise ValueError("k and v are [layers, pages, kv heads, page tokens, head dim]")
+        if tuple(k_exp.shape) != tuple(k.shape[:4]) or tuple(v_exp.shape) != tuple(k.shape[:4]):
+            raise ValueError("k_exp and v_exp are [layers, pages, kv heads, page tokens]")
+        for t in (k, v, k_exp, v_exp):
+            if t.element_size() != 1:
+                raise TypeError("the cache's tensors hold bytes (uint8 or float8_e4m3fn)")
+            _device_tensor(t)
+        out = _vp()
+        cfg = _kv_config(*(int(n) for n in k.shape), _ptr(k), _ptr(v), _ptr(k_exp), _ptr(v_exp))
+        _check(_lib.salt_kv_create(ctx, ctypes.byref(cfg), ctypes.byref(out)), ctx)
+        self.ctx, self.handle, self._tensors = ctx, out.value, (k, v, k_exp, v_exp)
+        self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = (int(n) for n in k.shape)
+
+    def close(self):
+        if self.handle:
+            _lib.salt_kv_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _device_tensor(t):
+    if not t.is_cuda:
+        raise TypeError("not a CUDA tensor")
+    return t
+
+
+def _head_rows(t, heads: int, dim: int):
+    """(pointer, elements from row to row) of a CUDA bf16 tensor
+    [tokens, heads, dim] whose heads are contiguous within a row."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.element_size() != 2 or not t.is_cuda:
+        raise ValueError(f"not a CUDA bf16 tensor [tokens, {heads}, {dim}]")
+    s = t.stride()
+    if s[2] != 1 or (s[1] != dim and heads > 1):
+        raise ValueError("the heads of a row are not contiguous")
+    return t.data_ptr(), s[0] if t.shape[0] > 1 else max(s[0], heads * dim)
+
+
+def _int32s(t, n: int | None = None):
+    """Pointer of a contiguous CUDA int32 tensor of n elements."""
+    if not t.is_cuda or t.is_floating_point() or t.element_size() != 4 or not t.is_contiguous():
+        raise ValueError("not a contiguous CUDA int32 tensor")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{t.numel()} entries, {n} expected")
+    return t.data_ptr()
+
+
+def salt_kv_create(ctx, k, v, k_exp, v_exp) -> KvCache:
+    """A handle on cache memory: k, v [layers, pages, kv heads, page tokens,
+    head dim] and k_exp, v_exp [layers, pages, kv heads, page tokens], CUDA
+    tensors of bytes."""
+    return KvCache(ctx, k, v, k_exp, v_exp)
+
+
+def salt_kv_destroy(kv: KvCache) -> None:
+    if kv is not None:
+        kv.close()
+
+
+def salt_kv_write(kv: KvCache, layer: int, k, v, slots, stream=None) -> None:
+    """Quantise rows k, v (CUDA bf16 [tokens, kv heads, head dim], heads
+    contiguous within a row) into slots (CUDA int32 [tokens], -1: skip)."""
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError("k and v have different numbers of tokens")
+    kp, ks = _head_rows(k, kv.n_kv_heads, kv.head_dim)
+    vp, vs = _head_rows(v, kv.n_kv_heads, kv.head_dim)
+    _check(_lib.salt_kv_write(kv.handle, layer, n, kp, ks, vp, vs, _int32s(slots, n), _stream(stream)), kv.ctx)
+
+
+def salt_kv_read(kv: KvCache, layer: int, slots, k, v, stream=None) -> None:
+    """The cached rows of slots into k, v (CUDA bf16 [tokens, kv heads, head dim])."""
+    n = k.shape[0]
+    if v.shape[0] != n:
+        raise ValueError("k and v have different numbers of tokens")
+    kp, ks = _head_rows(k, kv.n_kv_heads, kv.head_dim)
+    vp, vs = _head_rows(v, kv.n_kv_heads, kv.head_dim)
+    _check(_lib.salt_kv_read(kv.handle, layer, n, _int32s(slots, n), kp, ks, vp, vs, _stream(stream)), kv.ctx)
+
+
+class AttnPlan:
+    """A salt_attn handle with the cache it reads."""
+
+    def __init__(self, kv: KvCache, n_heads: int, max_seqs: int, max_tokens: int, max_pages: int, max_groups: int):
+        out = _vp()
+        cfg = _attn_config(n_heads, max_seqs, max_tokens, max_pages, max_groups)
+        _check(_lib.salt_attn_create(kv.handle, ctypes.byref(cfg), ctypes.byref(out)), kv.ctx)
+        self.kv, self.ctx, self.handle, self.n_heads = kv, kv.ctx, out.value, n_heads
+        self.n_tokens = 0
+
+    def close(self):
+        if self.handle:
+            _lib.salt_attn_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def salt_attn_create(kv: KvCache, n_heads: int, max_seqs: int, max_tokens: int, max_pages: int,
+                     max_groups: int = 0) -> AttnPlan:
+    return AttnPlan(kv, int(n_heads), int(max_seqs), int(max_tokens), int(max_pages), int(max_groups))
+
+
+def salt_attn_destroy(plan: AttnPlan) -> None:
+    if plan is not None:
+        plan.close()
+
+
+def salt_attn_batch(q_len, kv_len, page_ptr, pages, group=None, group_len=(), group_page_ptr=(0,), group_pages=()):
+    """A salt_attn_batch of host sequences (with the arrays it points to)."""
+    a = [np.ascontiguousarray(x, dtype=np.int32) for x in
+         (q_len, kv_len, page_ptr, pages, [-1] * len(q_len) if group is None else group, group_len, group_page_ptr,
+          group_pages)]
+    n, g = len(a[0]), len(a[5])
+    if len(a[1]) != n or len(a[2]) != n + 1 or len(a[4]) != n or len(a[6]) != g + 1:
+        raise ValueError("a batch's arrays do not match")
+    if a[2][-1] > len(a[3]) or a[6][-1] > len(a[7]):
+        raise ValueError("a page list runs past its array")
+    p = [x.ctypes.data for x in a]
+    b = _attn_batch(n, p[0], p[1], p[2], p[3], p[4], g, p[5], p[6], p[7])
+    b._keep, b._tokens = a, int(a[0].sum()) if n else 0
+    return b
+
+
+def salt_attn_build(plan: AttnPlan, batch, stream=None) -> None:
+    """Plan a batch (salt_attn_batch)."""
+    _check(_lib.salt_attn_build(plan.handle, ctypes.byref(batch), _stream(stream)), plan.ctx)
+    plan.n_tokens = batch._tokens
+
+
+def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, stream=None) -> None:
+    """Attention of the built batch: q, out CUDA bf16 [tokens, heads, head dim]
+    (heads contiguous within a row), lse CUDA float32 [tokens, heads] or None."""
+    qp, qs = _head_rows(q, plan.n_heads, plan.kv.head_dim)
+    op, os_ = _head_rows(out, plan.n_heads, plan.kv.head_dim)
+    if q.shape[0] < plan.n_tokens or out.shape[0] < plan.n_tokens:
+        raise ValueError(f"q or out has fewer rows than the batch's {plan.n_tokens} query tokens")
+    if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or lse.element_size() != 4 or not lse.is_cuda):
+        raise ValueError("lse is not a CUDA float32 tensor of the batch's rows")
+    _check(_lib.salt_attn_run(plan.handle, layer, qp, qs, scale, op, os_, _ptr(lse), _stream(stream)), plan.ctx)
+
+
+def _prob_rows(t, rows: int):
+    if t.dim() != 2 or t.shape[0] != rows or t.element_size() != 4 or not t.is_cuda or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"not a CUDA float32 tensor of {rows} rows")
+    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+
+
+def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u, sample_u, accepted, next_token,
+                       stream=None) -> None:
+    """Accept drafted tokens and draw the next one.  CUDA tensors: draft_ptr
+    int32 [requests + 1], draft_tokens int32 [drafts], target_p float32
+    [drafts + requests, vocab], draft_p float32 [drafts, vocab], accept_u
+    float32 [drafts], sample_u float32 [requests]; results accepted and
+    next_token, int32 [requests]."""
+    n, d, vocab = sample_u.numel(), draft_tokens.numel(), target_p.shape[1]
+    tp, ts = _prob_rows(target_p, d + n)
+    dp, ds = _prob_rows(draft_p, d)
+    if d and draft_p.shape[1] != vocab:
+        raise ValueError("target_p and draft_p have different vocabularies")
+    for t, m in ((accept_u, d), (sample_u, n)):
+        if not t.is_cuda or t.element_size() != 4 or not t.is_contiguous() or t.numel() != m:
+            raise ValueError(f"not a contiguous CUDA float32 tensor of {m} entries")
+    _check(_lib.salt_verify_drafts(ctx, n, d, vocab, _int32s(draft_ptr, n + 1), _int32s(draft_tokens), tp, ts, dp, ds,
+                                   accept_u.data_ptr(), sample_u.data_ptr(), _int32s(accepted, n),
+                                   _int32s(next_token, n), _stream(stream)), ctx)
 
 
 def salt_guard_check(ctx, seg=None) -> int:
