@@ -1,10 +1,26 @@
 // Attention of a batch over the paged 8-bit cache, requests of a group
 // sharing their prompt.
 //
-// attn_row_kernel: one warp per (query token, head).  Lanes hold D / 32
-// dimensions of q and of the output; each visible token costs a dot product
-// over the warp and one step of the running softmax
-//     m' = max(m, s),  l' = l 2^(m - m') + 2^(s - m'),  o' = o 2^(m - m') + 2^(s - m') v.
+// The work is cut into items: up to R rows (query token x query heads of one
+// key/value head) against a range of cached tokens, either a group's prompt
+// (rows of all its requests) or a request's own tokens.  An item walks its
+// range in tiles of 128 tokens, on the tensor cores with the cache as the
+// 128-row operand A, so that few query rows waste little:
+//     S^T[token][row] = K[token][:] . Q[row][:]            (M = 128, N = R)
+//     O^T[dim][row]  += V[token][dim] P[token][row]        (M = D, K = tokens)
+// The e4m3 codes go from the cache to the MMA as they are; the exponents of a
+// token's row multiply its scores (K) and its probabilities (V), both exact.
+// Q and P meet them as two e4m3 terms each, hi + lo, which holds 8 bits: a bf16
+// query is split exactly (its 8 bits are 4 and 4; elements below 2^-9 of the
+// row's largest to within 2^-17 of that), a probability to within 2^-9 and lo
+// kept at 16 times its size in columns of its own, so that small ones next to
+// a large one stay exact to 2^-21 of it.
+//
+// Softmax: thread = token, registers = rows.  The reference m of a row moves
+// only when a score passes it by more than the codes' headroom (a vote a
+// tile), so the usual tile needs no reduction over tokens: p = 2^(s - m), l += p,
+// P = p 2^e_v in codes.  Items of one row meet in the combine kernel through their
+// (o / l, m + log2 l).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -15,26 +31,46 @@
 #include "salt_async.cuh"
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
+#include "salt_pipe.cuh"
+#include "salt_tcgen05.cuh"
 
 namespace salt {
 namespace {
 
-// The plan's device tables: int32 words at these places of one block, written
-// by the host into a staging area and copied by a kernel.
-constexpr int HEAD_WORDS = 8;      // [0]: query tokens
-constexpr int TOK_WORDS = 4;       // per query token: first entry of its own page list, own tokens it sees, first entry
-                                   // of its group's page list, the prompt's tokens
+// The plan's device tables: int32 words of one block, written by the host
+// into a staging area and copied by a kernel.
+constexpr int HEAD_WORDS = 8;   // HD_* below
+constexpr int HD_TOKENS = 0, HD_RECS = 1, HD_PARTIAL = 2;
+constexpr int TOK_WORDS = 8;    // per query token: where its partial rows are, see TK_*
+constexpr int TK_OWN = 0, TK_OWN_ROWS = 1, TK_OWN_N = 2, TK_PRE = 3, TK_PRE_ROWS = 4, TK_PRE_N = 5, TK_DIRECT = 6;
+constexpr int REC_WORDS = 8;    // per item, shared by the key/value heads
+// flags (class, RF_*), first entry in the token order, tokens, first entry in the page lists, first and last + 1 cached
+// token, tokens the first query token sees, first partial row
+constexpr int RC_FLAGS = 0, RC_TOK = 1, RC_NTOK = 2, RC_PAGES = 3, RC_T0 = 4, RC_T1 = 5, RC_LIM = 6, RC_PART = 7;
+constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
+
+constexpr int TT = 128;          // cached tokens a tile
+constexpr int R_MAX = 128;       // rows an item
+constexpr int ATTN_THREADS = 384;
+constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
+constexpr float P_TOP = 7.5f;    // a new reference puts the row's largest P at 2^7.5
+constexpr float P_MOST = 8.8f;   // and is due when one passes 2^8.8 (e4m3 ends at 448 = 2^8.807)
+constexpr float M_NONE = -1e30f; // the reference before the first token
 
 struct AttnParams {
-    const int32_t *plan;           // header, token records, page lists
+    alignas(64) CUtensorMap kmap;  // the codes of every layer as rows of D bytes, box of one page
+    alignas(64) CUtensorMap vmap;
+    const int32_t *plan;           // header, token records, token order, items, page lists
     KvDev kv;
     int64_t layer;
     const uint16_t *q;
     uint16_t *out;
     float *lse;
+    float *part_o;                 // [partial rows][D]
+    float *part_l;                 // [partial rows] log2 of the sum
     int64_t q_stride, out_stride;
     int32_t n_heads, max_tok;
-    int32_t tok_at, pages_at;      // word offsets in plan
+    int32_t tok_at, order_at, rec_at, pages_at;  // word offsets in plan
     float scale_log2;              // scale * log2(e)
     uint32_t *err;
 };
@@ -44,73 +80,744 @@ __global__ void plan_copy_kernel(const uint4 *src, uint4 *dst, int n)
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) dst[i] = src[i];
 }
 
+// ---------------------------------------------------------------- shared memory
+template <int D>
+struct Layout {
+    static constexpr int STAGES = D == 128 ? 3 : 6;
+    static constexpr uint32_t SIDE = TT * D;              // codes of K or V of a tile
+    static constexpr uint32_t P_BUF = TT * 2 * R_MAX;     // P of a tile, hi and lo
+    static constexpr uint32_t KV = 0;
+    static constexpr uint32_t P = KV + STAGES * 2 * SIDE;
+    static constexpr uint32_t Q = P + 2 * P_BUF;
+    static constexpr uint32_t EXPS = Q + 2 * R_MAX * D;   // per stage: 128 of K, 128 of V
+    static constexpr uint32_t INFO = EXPS + STAGES * 2 * TT;
+    static constexpr uint32_t FAC = INFO + 2 * R_MAX * 16;
+    static constexpr uint32_t WMAX = FAC + R_MAX * 4;     // [2][4][R_MAX / 2] floats
+    static constexpr uint32_t BARS = WMAX + 4 * R_MAX * 4;
+    static constexpr uint32_t N_BARS = 3 * STAGES + 12;
+    static constexpr uint32_t MISC = BARS + N_BARS * 8;   // TMEM address, failure flag, [2][2] largest value exponents
+    static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
+};
+
+// A column's constants: factor of its scores (query row scale, scale, log2 e), reference m, tokens it
+// sees, (query token << 8 | head in the group).
+struct ColInfo {
+    float a, m;
+    int32_t lim, row;
+};
+
+__device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ __half2 half2_of_e4m3x2(uint16_t c)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(c));
+    return *reinterpret_cast<__half2 *>(&r);
+}
+__device__ __forceinline__ uint16_t e4m3x2_of_half2(__half2 h)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;\n" : "=h"(r) : "r"(*reinterpret_cast<uint32_t *>(&h)));
+    return r;
+}
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+    return r;
+}
+// 2^k, 0 below the normal range (k <= 127)
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float(k < -126 ? 0u : (uint32_t)(k + 127) << 23); }
+// 2^(e - 127) of an exponent byte; 0 for a row of zeros, NaN for a row that stands for NaN
 __device__ __forceinline__ float row_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
 
-template <int E>
-__device__ __forceinline__ void load_codes(const uint8_t *p, float (&f)[E])
+// hi and lo * 16 of two values as codes: v = hi + lo to 2^-9
+__device__ __forceinline__ void split_pair(float v0, float v1, uint16_t &hi, uint16_t &lo)
 {
-    uint32_t c = E == 4 ? __ldg(reinterpret_cast<const uint32_t *>(p)) : __ldg(reinterpret_cast<const uint16_t *>(p));
-#pragma unroll
-    for (int i = 0; i < E; i += 2) {
-        uint32_t h;
-        asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(h) : "h"((uint16_t)(c >> (8 * i))));
-        const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&h));
-        f[i] = v.x;
-        f[i + 1] = v.y;
-    }
+    hi = e4m3x2(v0, v1);
+    const __half2 rest = __hsub2(__floats2half2_rn(v0, v1), half2_of_e4m3x2(hi));
+    lo = e4m3x2_of_half2(__hmul2(rest, __floats2half2_rn(16.f, 16.f)));
 }
 
-constexpr int ROW_WARPS = 4;
-
-template <int D>
-__global__ void __launch_bounds__(32 * ROW_WARPS) attn_row_kernel(AttnParams p)
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts16(uint32_t a, uint16_t v) { asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(a), "h"(v) : "memory"); }
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
-    constexpr int E = D / 32;
-    const int T = p.plan[0], H = p.n_heads, G = H / p.kv.heads, lane = threadIdx.x & 31;
-    if (T > p.max_tok) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
-        return;
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+struct Item {
+    int flags, tok, ntok, pages, t0, t1, lim, part, kh;
+    int tiles, rows, half;  // half: rows of the first warpgroup's columns
+};
+
+// The CTA's r-th item of n: the records are in falling order of cost, handed
+// out forwards and backwards in turn.
+__device__ __forceinline__ int item_index(int r) { return r * (int)gridDim.x + ((r & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); }
+
+__device__ __forceinline__ Item load_item(const AttnParams &p, int idx, int G)
+{
+    const int rec = idx / p.kv.heads;
+    const int4 *w = reinterpret_cast<const int4 *>(p.plan + p.rec_at + rec * REC_WORDS);
+    const int4 a = __ldg(w), b = __ldg(w + 1);
+    Item it;
+    it.flags = a.x;
+    it.tok = a.y;
+    it.ntok = a.z;
+    it.pages = a.w;
+    it.t0 = b.x;
+    it.t1 = b.y;
+    it.lim = b.z;
+    it.kh = idx - rec * p.kv.heads;
+    it.rows = it.ntok * G;
+    it.part = b.w + it.kh * it.rows;
+    it.half = (it.rows + 1) >> 1;
+    it.tiles = (it.t1 - it.t0 + TT - 1) / TT;
+    return it;
+}
+
+// A bounded wait that also gives up when another role has.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, const volatile int *dead)
+{
+    for (int i = 0; i < (1 << 20); ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 255) == 255 && *dead) return false;
     }
-    for (int64_t row = (int64_t)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); row < (int64_t)T * H; row += (int64_t)gridDim.x * ROW_WARPS) {
-        const int t = (int)(row / H), h = (int)(row - (int64_t)t * H), kh = h / G;
-        const int4 rec = *reinterpret_cast<const int4 *>(p.plan + p.tok_at + t * TOK_WORDS);
-        float q[E], o[E], m = -INFINITY, l = 0.f;
-        const uint16_t *qr = p.q + t * p.q_stride + h * D + lane * E;
+    return false;
+}
+
+// Adds up each of N values over the warp's lanes: lane's sum is that of value
+// returned in `col` (32 / N lanes hold the same one).
+template <int N>
+__device__ __forceinline__ float sum_columns(const float *v, int lane, int &col)
+{
+    float t[N];
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            q[i] = bf16_to_f(qr[i]) * p.scale_log2;
-            o[i] = 0.f;
+    for (int i = 0; i < N; ++i) t[i] = v[i];
+    col = 0;
+    int n = N;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        if (n > 1) {
+            n >>= 1;
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                if (i < n) {
+                    const bool up = lane & o;
+                    const float send = up ? t[i] : t[i + n];
+                    t[i] = (up ? t[i + n] : t[i]) + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            }
+            if (lane & o) col += n;
+        } else {
+            t[0] += __shfl_xor_sync(0xffffffffu, t[0], o);
         }
-        bool nan = false;
-        for (int part = 0; part < 2; ++part) {
-            const int32_t *list = p.plan + p.pages_at + (part ? rec.x : rec.z);
-            const int n = part ? rec.y : rec.w;
-            for (int j = 0; j < n; ++j) {
-                const int64_t at = ((p.layer * p.kv.n_pages + list[j >> p.kv.page_log2]) * p.kv.heads + kh) * p.kv.page + (j & (p.kv.page - 1));
-                float k[E], v[E];
-                load_codes<E>(p.kv.k + at * D + lane * E, k);
-                load_codes<E>(p.kv.v + at * D + lane * E, v);
-                float s = 0.f;
+    }
+    return t[0];
+}
+
+// What the softmax warpgroups share across their functions.
+struct Soft {
+    uint8_t *sm;
+    uint32_t base, tmem;
+    volatile int *dead;
+    int wg, tid, lane, quarter;
+    uint32_t g;                    // tiles done by this CTA
+    uint32_t stage, stage_phase;
+    bool ok;
+};
+
+// A wait of a softmax warp: all of its lanes get the same answer.
+__device__ __forceinline__ void soft_wait(Soft &s, uint32_t bar, uint32_t parity)
+{
+    bool r = s.ok;
+    if (r) r = wait_bar(bar, parity, s.dead);
+    s.ok = __all_sync(0xffffffffu, r);
+}
+
+// One item of the class with CW columns a warpgroup.  False: gave up (the
+// whole warpgroup together).
+template <int D, int CW>
+__device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const Item &it, int n_item)
+{
+    using L = Layout<D>;
+    constexpr int CH = CW < 32 ? CW : 32;    // columns in registers at a time
+    constexpr int PITCH = CW == 64 ? 128 : 4 * CW;
+    const uint32_t bars = s.base + L::BARS;
+    const uint32_t kfull = bars, vfull = bars + 8 * L::STAGES;
+    const uint32_t s_full = bars + 8 * (3 * L::STAGES), p_full = s_full + 16, pv_done = s_full + 32, o_free = s_full + 64;
+    ColInfo *info = reinterpret_cast<ColInfo *>(s.sm + L::INFO) + (n_item & 1) * R_MAX + s.wg * CW;
+    float *fac = reinterpret_cast<float *>(s.sm + L::FAC) + s.wg * (R_MAX / 2);
+    float *wmax = reinterpret_cast<float *>(s.sm + L::WMAX) + s.wg * 4 * (R_MAX / 2);
+    const int ncol = s.wg ? it.rows - it.half : it.half;
+    const uint32_t lanes = (uint32_t)(s.quarter * 32) << 16;
+    const uint32_t o_at = s.tmem + lanes + 256 + s.wg * 2 * CW;
+    const int nb = 1 + s.wg;
+    // values count in units of the largest exponent of the range
+    const volatile int *vt = reinterpret_cast<const volatile int *>(s.sm + L::MISC + 8) + 2 * (n_item & 1);
+    const int vtop = max(vt[0], vt[1]) > 0 ? max(vt[0], vt[1]) : 127;
+    float l[CW];
 #pragma unroll
-                for (int i = 0; i < E; ++i) s = fmaf(q[i], k[i], s);
+    for (int c = 0; c < CW; ++c) l[c] = 0.f;
+    for (int j = 0; j < it.tiles; ++j) {
+        const uint32_t b = s.g & 1;
+        const int tok = it.t0 + j * TT + s.tid;
+        // every row sees the whole tile: no column masks (the first query token sees least)
+        const bool mask = it.t0 + (j + 1) * TT > min(it.t1, it.lim);
+        soft_wait(s, kfull + 8 * s.stage, s.stage_phase);
+        soft_wait(s, s_full + 8 * b, (s.g >> 1) & 1);
+        tc_fence_after();
+        const uint32_t ke = s.sm[L::EXPS + s.stage * 2 * TT + s.tid], ve = s.sm[L::EXPS + s.stage * 2 * TT + TT + s.tid];
+        const float kf = row_scale(ke), vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - vtop);
+        // what P is to p in log2, held so that p stays in range (a value 2^100 below the largest may lose bits)
+        const float vref = ve == 255u ? 0.f : (float)max((int)ve - vtop, -100);
+        const uint32_t s_at = s.tmem + lanes + b * 128 + s.wg * CW;
 #pragma unroll
-                for (int w = 16; w > 0; w >>= 1) s += __shfl_xor_sync(0xffffffffu, s, w);
-                s *= row_scale(p.kv.k_exp[at]);
-                const float vs = row_scale(p.kv.v_exp[at]);
-                nan |= !(fabsf(s) < INFINITY);
-                const float m2 = fmaxf(m, s), c = exp2f(m - m2), w = exp2f(s - m2);
-                l = l * c + w;
+        for (int ch = 0; ch < CW / CH; ++ch) {
+            float x[CH];
+            float mx = -INFINITY;
+            auto load = [&] {
 #pragma unroll
-                for (int i = 0; i < E; ++i) o[i] = o[i] * c + w * vs * v[i];
-                m = m2;
+                for (int c = 0; c < CH; c += 8) tmem_ld8(s_at + ch * CH + c, reinterpret_cast<uint32_t *>(x) + c);
+                tmem_ld_wait();
+            };
+            load();
+            auto args = [&] {  // s - m; -inf where the row does not see the token
+                mx = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    if (ch * CH + c < ncol) {
+                        const ColInfo ci = info[ch * CH + c];
+                        x[c] = fmaf(x[c], kf * ci.a, -ci.m);
+                        if (mask && tok >= ci.lim) x[c] = -INFINITY;
+                        mx = fmaxf(mx, x[c]);
+                    }
+                }
+                mx += vref;
+            };
+            args();
+            if (!named_sync_and(nb, WG, s.ok && !(mx > P_MOST))) {
+                // some row's reference has to move
+                if (!named_sync_and(nb, WG, s.ok)) return false;
+                load();
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    if (ch * CH + c < ncol) {
+                        const ColInfo ci = info[ch * CH + c];
+                        float v = fmaf(x[c], kf * ci.a, vref);
+                        if ((mask && tok >= ci.lim) || !(v == v)) v = -INFINITY;
+#pragma unroll
+                        for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                        if (s.lane == 0) wmax[s.quarter * (R_MAX / 2) + c] = v;
+                    }
+                }
+                named_sync(nb, WG);
+                if (s.tid < CH && ch * CH + s.tid < ncol) {
+                    float v = wmax[s.tid];
+                    for (int w = 1; w < 4; ++w) v = fmaxf(v, wmax[w * (R_MAX / 2) + s.tid]);
+                    ColInfo &ci = info[ch * CH + s.tid];
+                    float f = 1.f;
+                    if (v - ci.m > P_MOST) {
+                        const float m = v - P_TOP;
+                        f = ex2(ci.m - m);
+                        ci.m = m;
+                    }
+                    fac[s.tid] = f;
+                }
+                named_sync(nb, WG);
+                if (j > 0) {
+                    const uint32_t last = s.g - 1;
+                    soft_wait(s, pv_done + 8 * (last & 1), (last >> 1) & 1);
+                    tc_fence_after();
+#pragma unroll
+                    for (int c = 0; c < CH; c += 8) {
+                        if (ch * CH + c < ncol) {
+                            uint32_t o[16];
+                            const uint32_t at = o_at + ch * CH + c;
+                            tmem_ld8(at, o);
+                            tmem_ld8(at + CW, o + 8);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float f = ch * CH + c + i < ncol ? fac[c + i] : 1.f;
+                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                o[i + 8] = __float_as_uint(__uint_as_float(o[i + 8]) * f);
+                            }
+                            tmem_st8(at, o);
+                            tmem_st8(at + CW, o + 8);
+                        }
+                    }
+                    tmem_st_wait();
+#pragma unroll
+                    for (int c = 0; c < CH; ++c)
+                        if (ch * CH + c < ncol) l[ch * CH + c] *= fac[c];
+                }
+                load();
+                args();
+                named_sync(nb, WG);  // fac and wmax are free again
+            }
+            // the P buffer is free once the product two tiles back is done
+            if (ch == 0 && s.g >= 2) soft_wait(s, pv_done + 8 * b, ((s.g >> 1) - 1) & 1);
+            const uint32_t p_at = s.base + L::P + b * L::P_BUF + (CW == 64 ? s.wg * (TT * 128) : 0);
+            const uint32_t row_at = s.tid * PITCH + (CW == 64 ? 0 : s.wg * 2 * CW);
+            uint32_t hi[CH / 4], lo[CH / 4];
+#pragma unroll
+            for (int c = 0; c < CH; c += 2) {
+                uint16_t h = 0, w = 0;
+                if (ch * CH + c < ncol) {
+                    float v[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const float e = ex2(x[c + i]);
+                        v[i] = e * vf;
+                        if (ch * CH + c + i < ncol) {
+                            l[ch * CH + c + i] += e;
+                            if (mask && x[c + i] == -INFINITY) v[i] = 0.f;  // not 0 * NaN
+                        }
+                    }
+                    split_pair(v[0], v[1], h, w);
+                }
+                if (c % 4 == 0) {
+                    hi[c / 4] = h;
+                    lo[c / 4] = w;
+                } else {
+                    hi[c / 4] |= (uint32_t)h << 16;
+                    lo[c / 4] |= (uint32_t)w << 16;
+                }
+            }
+            if constexpr (CW == 8) {
+                sts128(p_at + swz_rows<PITCH>(row_at), hi[0], hi[1], lo[0], lo[1]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < CH; c += 16) {
+                    sts128(p_at + swz_rows<PITCH>(row_at + ch * CH + c), hi[c / 4], hi[c / 4 + 1], hi[c / 4 + 2], hi[c / 4 + 3]);
+                    sts128(p_at + swz_rows<PITCH>(row_at + CW + ch * CH + c), lo[c / 4], lo[c / 4 + 1], lo[c / 4 + 2], lo[c / 4 + 3]);
+                }
             }
         }
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        uint16_t *orow = p.out + t * p.out_stride + h * D + lane * E;
+        // past the range a stage holds other tokens' values, or none: 0 * NaN must not arise
+        if (s.wg == 0 && it.t0 + (j + 1) * TT > it.t1) {
+            soft_wait(s, vfull + 8 * s.stage, s.stage_phase);
+            if (tok >= it.t1) {
+                const uint32_t v_at = s.base + L::KV + s.stage * 2 * L::SIDE + L::SIDE + s.tid * D;
 #pragma unroll
-        for (int i = 0; i < E; ++i) orow[i] = f_to_bf16(nan ? __uint_as_float(0x7fc00000u) : o[i] * inv);
-        if (p.lse && lane == 0)
-            p.lse[(int64_t)t * H + h] = nan ? __uint_as_float(0x7fc00000u) : l > 0.f ? (m + log2f(l)) * 0.69314718056f : -INFINITY;
+                for (int c = 0; c < D; c += 16) sts128(v_at + c, 0, 0, 0, 0);
+            }
+        }
+        tc_fence_before();
+        fence_async_smem();
+        mbar_arrive_release(p_full + 8 * b);
+        ++s.g;
+        if (++s.stage == L::STAGES) {
+            s.stage = 0;
+            s.stage_phase ^= 1;
+        }
+    }
+    // ------------------------------------------------ the item's rows
+    const uint32_t last = s.g - 1;
+    soft_wait(s, pv_done + 8 * (last & 1), (last >> 1) & 1);
+    tc_fence_after();
+#pragma unroll
+    for (int c0 = 0; c0 < CW; c0 += CH) {
+        int col;
+        const float t = sum_columns<CH>(l + c0, s.lane, col);
+        wmax[s.quarter * (R_MAX / 2) + c0 + col] = t;
+    }
+    if (!named_sync_and(nb, WG, s.ok)) return false;
+    const int G = p.n_heads / p.kv.heads;
+    const bool direct = it.flags & RF_DIRECT;
+    const int row0 = s.wg ? it.half : 0;
+    const int dim = D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
+    const bool live = D == 128 || s.lane < 16;
+    const float unit = pow2(vtop - 127);
+    auto total = [&](int c) { return wmax[c] + wmax[R_MAX / 2 + c] + wmax[R_MAX + c] + wmax[R_MAX + R_MAX / 2 + c]; };
+    if (s.tid < ncol) {
+        const float t = total(s.tid);
+        const ColInfo ci = info[s.tid];
+        const float lse2 = t > 0.f ? ci.m + log2f(t) : t == t ? -INFINITY : t;
+        if (!direct) p.part_l[it.part + row0 + s.tid] = lse2;
+        else if (p.lse) p.lse[(int64_t)(ci.row >> 8) * p.n_heads + it.kh * G + (ci.row & 255)] = lse2 * 0.693147180559945f;
+    }
+#pragma unroll
+    for (int c0 = 0; c0 < CW; c0 += 8) {
+        if (c0 < ncol) {
+            float o[16];
+            tmem_ld8(o_at + c0, reinterpret_cast<uint32_t *>(o));
+            tmem_ld8(o_at + CW + c0, reinterpret_cast<uint32_t *>(o) + 8);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int c = c0 + i;
+                if (c < ncol && live) {
+                    const float t = total(c);
+                    const float v = t > 0.f ? fmaf(o[i + 8], 0.0625f, o[i]) / t * unit : t == t ? 0.f : t;
+                    if (direct) {
+                        const int row = info[c].row;
+                        p.out[(row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * D + dim] = f_to_bf16(v);
+                    } else {
+                        p.part_o[(int64_t)(it.part + row0 + c) * D + dim] = v;
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    mbar_arrive_release(o_free + 8 * (n_item & 1));
+    named_sync(nb, WG);  // wmax is free again
+    return true;
+}
+
+template <int D>
+__global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid_constant__ AttnParams p)
+{
+    using L = Layout<D>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int KV = p.kv.heads, G = p.n_heads / KV;
+    if (p.plan[HD_TOKENS] > p.max_tok) {
+        if (blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
+        return;
+    }
+    const int n_items = p.plan[HD_RECS] * KV;
+    if ((int)blockIdx.x >= n_items) return;
+    const uint32_t bars = base + L::BARS;
+    const uint32_t kfull = bars, vfull = bars + 8 * L::STAGES, kv_free = bars + 16 * L::STAGES;
+    const uint32_t s_full = bars + 24 * L::STAGES, p_full = s_full + 16, pv_done = s_full + 32, q_full = s_full + 48,
+                   o_free = s_full + 64, q_free = s_full + 80, drain = s_full + 88;
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + L::MISC);
+    volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
+    if (tid == 0) {
+        for (int i = 0; i < L::STAGES; ++i) {
+            mbar_init(kfull + 8 * i, 1);
+            mbar_init(vfull + 8 * i, 1);
+            mbar_init(kv_free + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(s_full + 8 * i, 1);
+            mbar_init(p_full + 8 * i, 2 * WG);
+            mbar_init(pv_done + 8 * i, 1);
+            mbar_init(o_free + 8 * i, 2 * WG);
+            mbar_init(q_full + 8 * i, 64);
+        }
+        mbar_init(q_free, 1);
+        mbar_init(drain, 1);
+        *dead = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(base + L::MISC, 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+
+    if (warp == 0) {
+        // ------------------------------------------------ loads: a lane per page of a tile
+        uint32_t st = 0, phase = 0, used = 0;
+        for (int r = 0; ok; ++r) {
+            const int idx = item_index(r);
+            if (idx >= n_items) break;
+            const Item it = load_item(p, idx, G);
+            const int32_t *list = p.plan + p.pages_at + it.pages;
+            const int per = TT >> p.kv.page_log2;
+            for (int j = 0; j < it.tiles && ok; ++j) {
+                const int t = it.t0 + j * TT;
+                const int first = t >> p.kv.page_log2;
+                const int n = min(per, ((it.t1 - 1) >> p.kv.page_log2) - first + 1);
+                int page = 0;
+                if (lane < n) page = __ldg(list + first + lane);
+                if (used >= (uint32_t)L::STAGES) ok = wait_bar(kv_free + 8 * st, phase ^ 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t bytes = (uint32_t)n * p.kv.page;
+                if (lane == 0) {
+                    mbar_expect_tx(kfull + 8 * st, bytes * (D + 2));
+                    mbar_expect_tx(vfull + 8 * st, bytes * D);
+                }
+                __syncwarp();
+                if (lane < n) {
+                    const int64_t row = ((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2;
+                    const uint32_t at = base + L::KV + st * 2 * L::SIDE + lane * p.kv.page * D;
+                    const uint32_t ex = base + L::EXPS + st * 2 * TT + lane * p.kv.page;
+                    tma_load_2d(at, &p.kmap, 0, (int)row, kfull + 8 * st);
+                    bulk_load(ex, p.kv.k_exp + row, p.kv.page, kfull + 8 * st);
+                    bulk_load(ex + TT, p.kv.v_exp + row, p.kv.page, kfull + 8 * st);
+                    tma_load_2d(at + L::SIDE, &p.vmap, 0, (int)row, vfull + 8 * st);
+                }
+                ++used;
+                if (++st == (uint32_t)L::STAGES) {
+                    st = 0;
+                    phase ^= 1;
+                }
+            }
+        }
+        if (!ok) {  // copies in flight land before the CTA ends
+            if (lane == 0) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+            }
+            const uint32_t n = min(used, (uint32_t)L::STAGES);
+            for (uint32_t i = 0; i < n; ++i) {
+                const uint32_t k = (used - 1 - i) % L::STAGES, ph = ((used - 1 - i) / L::STAGES) & 1;
+                mbar_wait(kfull + 8 * k, ph);
+                mbar_wait(vfull + 8 * k, ph);
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issue
+        if (lane == 0) {
+            uint32_t g = 0, qk_st = 0, qk_ph = 0, pv_st = 0, pv_ph = 0;
+            for (int r = 0; ok; ++r) {
+                const int idx = item_index(r);
+                if (idx >= n_items) break;
+                const Item it = load_item(p, idx, G);
+                const int cw = 8 << (it.flags & 3), R = 2 * cw;
+                const uint32_t q_at = base + L::Q;
+                const uint32_t id_s = idesc_e4m3_f32(128, R, 0), id_o = idesc_e4m3_f32(D, 2 * R, 3);
+                auto scores = [&](uint32_t n) {
+                    if (!(ok = ok && wait_bar(kfull + 8 * qk_st, qk_ph, dead))) return;
+                    const uint32_t k_at = base + L::KV + qk_st * 2 * L::SIDE;
+                    const uint64_t kd = sdesc_rows(k_at, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+#pragma unroll
+                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(tmem + (n & 1) * 128, kd + 2 * ks, qh + 2 * ks, id_s, ks > 0);
+#pragma unroll
+                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(tmem + (n & 1) * 128, kd + 2 * ks, ql + 2 * ks, id_s, 1);
+                    umma_commit(s_full + 8 * (n & 1));
+                    if (++qk_st == (uint32_t)L::STAGES) {
+                        qk_st = 0;
+                        qk_ph ^= 1;
+                    }
+                };
+                if (!(ok = wait_bar(q_full + 8 * (r & 1), (r >> 1) & 1, dead))) break;
+                tc_fence_after();
+                scores(g);
+                for (int j = 0; j < it.tiles && ok; ++j, ++g) {
+                    if (j + 1 < it.tiles) scores(g + 1);
+                    else umma_commit(q_free);
+                    const uint32_t b = g & 1;
+                    ok = ok && wait_bar(p_full + 8 * b, (g >> 1) & 1, dead) && wait_bar(vfull + 8 * pv_st, pv_ph, dead);
+                    if (j == 0 && r > 0) ok = ok && wait_bar(o_free + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const int pitch = cw == 64 ? 128 : 4 * cw;
+                    const uint64_t vd = sdesc_rows(base + L::KV + pv_st * 2 * L::SIDE + L::SIDE, D, 0);
+                    const uint64_t pd = sdesc_rows(base + L::P + b * L::P_BUF, pitch, TT * 128);
+                    const int steps = min(TT, it.t1 - it.t0 - j * TT + 31) / 32;
+                    for (int ks = 0; ks < steps; ++ks)
+                        umma_e4m3(tmem + 256, vd + ks * (32 * D / 16), pd + ks * (32 * pitch / 16), id_o, j > 0 || ks > 0);
+                    umma_commit(kv_free + 8 * pv_st);
+                    umma_commit(pv_done + 8 * b);
+                    if (++pv_st == (uint32_t)L::STAGES) {
+                        pv_st = 0;
+                        pv_ph ^= 1;
+                    }
+                }
+            }
+            if (!ok) {  // the products issued so far end before the CTA does
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+                umma_commit(drain);
+                mbar_wait(drain, 0);
+            }
+        }
+        __syncwarp();
+    } else if (warp < 4) {
+        // ------------------------------------------------ queries: rows scaled by a power of two and split in hi + lo
+        const int w = warp - 2;
+        for (int r = 0; ok; ++r) {
+            const int idx = item_index(r);
+            if (idx >= n_items) break;
+            const Item it = load_item(p, idx, G);
+            const int cw = 8 << (it.flags & 3), R = 2 * cw;
+            const int32_t *order = p.plan + p.order_at + it.tok;
+            if (r > 0) ok = wait_bar(q_free, (r - 1) & 1, dead);
+            if (r > 1) ok = ok && wait_bar(o_free + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            ColInfo *info = reinterpret_cast<ColInfo *>(sm + L::INFO) + (r & 1) * R_MAX;
+            // the largest exponent of the range's values: 16 tokens a lane
+            uint32_t top = 0;
+            for (int t = it.t0 + (tid - 64) * 16; t < it.t1; t += 64 * 16) {
+                const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
+                const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
+                const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
+                const uint32_t x[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
+                    const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+                    top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
+                }
+            }
+            top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
+            top = __reduce_max_sync(0xffffffffu, top);
+            if (lane == 0) reinterpret_cast<volatile int *>(sm + L::MISC + 8)[2 * (r & 1) + w] = (int)top;
+            constexpr int E = D / 32;   // elements a lane
+            constexpr int AT_ONCE = 8;  // rows whose loads are under way together
+            for (int row0 = w; row0 < it.rows; row0 += 2 * AT_ONCE) {
+                uint32_t u[AT_ONCE][2];
+                int tok[AT_ONCE];
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) tok[k] = row0 + 2 * k < it.rows ? __ldg(order + (row0 + 2 * k) / G) : 0;
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int row = row0 + 2 * k;
+                    u[k][0] = u[k][1] = 0;
+                    if (row < it.rows) {
+                        const uint16_t *src = p.q + tok[k] * p.q_stride + (it.kh * G + row % G) * D + lane * E;
+                        if constexpr (E == 4) {
+                            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
+                            u[k][0] = v.x;
+                            u[k][1] = v.y;
+                        } else {
+                            u[k][0] = __ldg(reinterpret_cast<const uint32_t *>(src));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int row = row0 + 2 * k;
+                    if (row >= it.rows) break;
+                    uint32_t a = max(max((u[k][0] << 16) & 0x7fffffffu, u[k][0] & 0x7fff0000u),
+                                     max((u[k][1] << 16) & 0x7fffffffu, u[k][1] & 0x7fff0000u));
+                    a = __reduce_max_sync(0xffffffffu, a);
+                    // the row's largest element to [2^7, 2^8)
+                    const int qe = max((int)(a >> 23) - 127 - 7, -120);
+                    const bool bad = (a >> 23) == 255;
+                    const float inv = __uint_as_float((uint32_t)(127 - qe) << 23);
+                    uint32_t hi = 0, lo = 0;
+#pragma unroll
+                    for (int e = 0; e < E / 2; ++e) {
+                        const float v0 = __uint_as_float(u[k][e] << 16) * inv, v1 = __uint_as_float(u[k][e] & 0xffff0000u) * inv;
+                        const uint16_t h = e4m3x2(v0, v1);
+                        const float2 hf = __half22float2(half2_of_e4m3x2(h));
+                        hi |= (uint32_t)h << (16 * e);
+                        lo |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * e);
+                    }
+                    if (bad) hi = lo = 0x7f7f7f7fu;
+                    const int col = row < it.half ? row : cw + row - it.half;
+                    const uint32_t at = base + L::Q + swz_rows<D>(col * D + lane * E);
+                    const uint32_t at_lo = base + L::Q + swz_rows<D>((R + col) * D + lane * E);
+                    if constexpr (E == 4) {
+                        sts32(at, hi);
+                        sts32(at_lo, lo);
+                    } else {
+                        sts16(at, (uint16_t)hi);
+                        sts16(at_lo, (uint16_t)lo);
+                    }
+                    if (lane == 0) {
+                        const int i = row / G;
+                        ColInfo c;
+                        c.a = bad ? 1.f : __uint_as_float((uint32_t)(127 + qe) << 23) * p.scale_log2;
+                        c.m = M_NONE;
+                        c.lim = it.lim + ((it.flags & RF_CAUSAL) ? i : 0);
+                        c.row = (tok[k] << 8) | (row - i * G);
+                        info[col] = c;
+                    }
+                }
+            }
+            fence_async_smem();
+            mbar_arrive_release(q_full + 8 * (r & 1));
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    } else {
+        // ------------------------------------------------ softmax and results
+        Soft s;
+        s.sm = sm;
+        s.base = base;
+        s.tmem = tmem;
+        s.dead = dead;
+        s.wg = warp >= 8;
+        s.tid = tid & (WG - 1);
+        s.lane = lane;
+        s.quarter = warp & 3;
+        s.g = s.stage = s.stage_phase = 0;
+        s.ok = true;
+        for (int r = 0; ok; ++r) {
+            const int idx = item_index(r);
+            if (idx >= n_items) break;
+            const Item it = load_item(p, idx, G);
+            // (the columns' constants are there before the first scores are)
+            soft_wait(s, q_full + 8 * (r & 1), (r >> 1) & 1);
+            switch (it.flags & 3) {
+            case 0: ok = soft_item<D, 8>(p, s, it, r); break;
+            case 1: ok = soft_item<D, 16>(p, s, it, r); break;
+            case 2: ok = soft_item<D, 32>(p, s, it, r); break;
+            default: ok = soft_item<D, 64>(p, s, it, r); break;
+            }
+        }
+        if (!ok && s.tid == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, 512);
+}
+
+// The rows that several items share (and those no item has): a warp per row,
+//     out = sum_i 2^(l_i - L) o_i,   L = log2 sum_i 2^(l_i).
+constexpr int COMBINE_WARPS = 4;
+
+template <int D>
+__global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const __grid_constant__ AttnParams p)
+{
+    constexpr int E = D / 32;
+    const int T = p.plan[HD_TOKENS], H = p.n_heads, G = H / p.kv.heads, lane = threadIdx.x & 31;
+    if (T > p.max_tok || !p.plan[HD_PARTIAL]) return;
+    for (int64_t row = (int64_t)blockIdx.x * COMBINE_WARPS + (threadIdx.x >> 5); row < (int64_t)T * H; row += (int64_t)gridDim.x * COMBINE_WARPS) {
+        const int t = (int)(row / H), h = (int)(row - (int64_t)t * H), kh = h / G, g = h - kh * G;
+        const int4 *rec = reinterpret_cast<const int4 *>(p.plan + p.tok_at + t * TOK_WORDS);
+        const int4 a = __ldg(rec), b = __ldg(rec + 1);
+        if (b.z) continue;  // written by its only item
+        const int own = a.x, own_rows = a.y, own_n = a.z, pre = a.w, pre_rows = b.x, n = own_n + b.y;
+        auto place = [&](int i) -> int64_t {  // the row's i-th partial
+            return i < own_n ? own + (int64_t)(i * p.kv.heads + kh) * own_rows + g
+                             : pre + (int64_t)((i - own_n) * p.kv.heads + kh) * pre_rows + g;
+        };
+        float top = -INFINITY;
+        bool nan = false;
+        for (int i = lane; i < n; i += 32) {
+            const float l = p.part_l[place(i)];
+            top = fmaxf(top, l);
+            nan |= !(l == l);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        nan = __any_sync(0xffffffffu, nan);
+        float sum = 0.f, o[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+        if (top > -INFINITY) {
+            for (int i = 0; i < n; ++i) {
+                const int64_t at = place(i);
+                const float w = ex2(p.part_l[at] - top);
+                const float *src = p.part_o + at * D + lane * E;
+                sum += w;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = fmaf(w, src[e], o[e]);
+            }
+        }
+        const float bad = __uint_as_float(0x7fc00000u), inv = nan ? bad : sum > 0.f ? 1.f / sum : 0.f;
+        uint16_t *dst = p.out + t * p.out_stride + h * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) dst[e] = f_to_bf16(o[e] * inv);
+        if (p.lse && lane == 0) p.lse[row] = nan ? bad : sum > 0.f ? (top + log2f(sum)) * 0.693147180559945f : -INFINITY;
     }
 }
 
@@ -122,14 +829,19 @@ using namespace salt;
 struct salt_attn {
     salt_kv *kv = nullptr;
     salt_attn_config cfg{};
+    int device = 0, n_sm = 1;
+    CUtensorMap kmap, vmap;
     int32_t *plan = nullptr;                   // device tables
-    int tok_at = 0, pages_at = 0;
+    int tok_at = 0, order_at = 0, rec_at = 0, rec_cap = 0, pages_at = 0;
     size_t plan_words = 0;
+    float *part_o = nullptr, *part_l = nullptr;
+    int64_t part_cap = 0;                      // partial rows
     int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies of the tables
     cudaEvent_t staging_ev[2] = {nullptr, nullptr};
     bool staging_used[2] = {false, false};
     int staging_next = 0;
     bool built = false;
+    bool partial = false;                      // some row needs the combine
     int T = 0;
     std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since
     cudaEvent_t tmp_ev = nullptr;
@@ -201,28 +913,174 @@ salt_status check_batch(const salt_attn *a, const salt_attn_batch *b, int *token
     return SALT_OK;
 }
 
-// Writes the tables of a checked batch; returns the words used.
-size_t fill_plan(const salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
+// Rows of query tokens that go through the cache together.
+struct RowTile {
+    int tok, ntok;      // in the token order
+    int pages;          // first entry of the page list
+    int len;            // cached tokens it walks
+    int lim;            // tokens the first query token sees
+    bool causal, alone; // alone: no row of it has another tile
+    int cls;            // columns a warpgroup: 8 << cls
+};
+
+// The time of an item in units of 128-token tiles of the smallest class, from
+// measurements of single items: a tile of each class, and what an item takes besides.
+constexpr float TILE_COST[4] = {1.f, 1.1f, 1.6f, 2.8f};
+constexpr float ITEM_COST = 2.f;
+
+// Plans a checked batch into the tables at w; returns the words used.
+size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
 {
+    const KvDev &kv = a->kv->dev;
+    const int G = a->cfg.n_heads / kv.heads, KV = kv.heads;
+    const int per = std::max(1, R_MAX / G);  // whole query tokens a tile
     std::memset(w, 0, HEAD_WORDS * 4);
-    w[0] = T;
+    w[HD_TOKENS] = T;
     const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
     const int grp_pages = b->n_groups > 0 ? b->group_page_ptr[b->n_groups] : 0;
-    int32_t *tok = w + a->tok_at;
-    for (int i = 0; i < b->n_seqs; ++i) {
-        const int g = b->group && b->n_groups > 0 ? b->group[i] : -1;
-        for (int j = 0; j < b->q_len[i]; ++j, tok += TOK_WORDS) {
-            const int64_t see = (int64_t)b->kv_len[i] - b->q_len[i] + j + 1;
-            tok[0] = b->page_ptr[i];
-            tok[1] = see > 0 ? (int32_t)see : 0;
-            tok[2] = g >= 0 ? own_pages + b->group_page_ptr[g] : 0;
-            tok[3] = g >= 0 ? b->group_len[g] : 0;
+    int32_t *order = w + a->order_at, *tok = w + a->tok_at;
+    std::memset(tok, 0, (size_t)T * TOK_WORDS * 4);
+    for (int t = 0; t < T; ++t) order[t] = t;
+    const bool grouped = b->group && b->n_groups > 0;
+    auto prompt = [&](int i) { return grouped && b->group[i] >= 0 ? b->group_len[b->group[i]] : 0; };
+    auto class_of = [&](int ntok) {
+        const int half = (ntok * G + 1) / 2;
+        return half <= 8 ? 0 : half <= 16 ? 1 : half <= 32 ? 2 : 3;
+    };
+    std::vector<RowTile> tiles;
+    // own tokens: `per` query tokens of a request at a time
+    int t0 = 0;
+    for (int i = 0; i < b->n_seqs; t0 += b->q_len[i], ++i) {
+        const int n = b->q_len[i], kvl = b->kv_len[i];
+        for (int j = 0; j < n; j += per) {
+            const int m = std::min(per, n - j);
+            const int64_t len = (int64_t)kvl - n + j + m;  // what the last of them sees
+            if (len <= 0) continue;
+            tiles.push_back({t0 + j, m, b->page_ptr[i], (int)len, (int)((int64_t)kvl - n + j + 1), true, prompt(i) == 0, class_of(m)});
         }
     }
+    // prompts: the query tokens of a group's requests, in the second part of the order
+    if (grouped) {
+        std::vector<int> at(b->n_groups + 1, 0);
+        for (int i = 0; i < b->n_seqs; ++i)
+            if (b->group[i] >= 0) at[b->group[i] + 1] += b->q_len[i];
+        for (int g = 0; g < b->n_groups; ++g) at[g + 1] += at[g];
+        std::vector<int> next(at.begin(), at.end() - 1);
+        std::vector<uint8_t> own(T, 0);
+        for (const RowTile &x : tiles)
+            for (int k = 0; k < x.ntok; ++k) own[x.tok + k] = 1;
+        t0 = 0;
+        for (int i = 0; i < b->n_seqs; t0 += b->q_len[i], ++i)
+            if (b->group[i] >= 0)
+                for (int j = 0; j < b->q_len[i]; ++j) order[T + next[b->group[i]]++] = t0 + j;
+        for (int g = 0; g < b->n_groups; ++g) {
+            if (b->group_len[g] == 0) continue;
+            for (int j = at[g]; j < at[g + 1]; j += per) {
+                const int m = std::min(per, at[g + 1] - j);
+                bool alone = true;
+                for (int k = 0; k < m; ++k) alone = alone && !own[order[T + j + k]];
+                tiles.push_back({T + j, m, own_pages + b->group_page_ptr[g], b->group_len[g], b->group_len[g], false, alone, class_of(m)});
+            }
+        }
+    }
+    // How long an item may get: the shortest estimated run among some lengths,
+    // where a run is its items spread over the SMs plus half of the longest one.
+    double whole = 0;
+    for (const RowTile &x : tiles) whole += KV * (TILE_COST[x.cls] * ((x.len + TT - 1) / TT));
+    const double even = std::max(1.0, whole / a->n_sm);
+    double best = 1e300, limit = 0;
+    for (double part : {0.0, 2.0, 1.0, 0.66, 0.5, 0.33, 0.25, 0.125}) {  // 0: no splits
+        const double most = part == 0.0 ? 1e300 : std::max(1.0, even * part);
+        double sum = 0, longest = 0;
+        int64_t recs = 0, rows = 0;
+        for (const RowTile &x : tiles) {
+            const int n = (x.len + TT - 1) / TT;
+            const int per_item = (int)std::min<double>(n, std::max(1.0, std::floor(most / TILE_COST[x.cls])));
+            const int items = (n + per_item - 1) / per_item;
+            recs += items;
+            rows += (int64_t)items * KV * x.ntok * G;
+            sum += KV * (n * TILE_COST[x.cls] + items * ITEM_COST);
+            longest = std::max(longest, (double)per_item * TILE_COST[x.cls] + ITEM_COST);
+        }
+        const double est = std::max(longest, sum / a->n_sm + 0.5 * longest);
+        if (part != 0.0 && (recs > a->rec_cap || rows > a->part_cap)) continue;
+        if (est < best) {
+            best = est;
+            limit = most;
+        }
+    }
+    struct Rec {
+        float cost;
+        int tile, t0, t1, part;
+        bool direct;
+    };
+    std::vector<Rec> recs;
+    int64_t part = 0;
+    bool partial = false;
+    std::vector<uint8_t> seen(T, 0);
+    for (size_t k = 0; k < tiles.size(); ++k) {
+        const RowTile &x = tiles[k];
+        const int n = (x.len + TT - 1) / TT, rows = x.ntok * G;
+        const int per_item = (int)std::min<double>(n, std::max(1.0, std::floor(limit / TILE_COST[x.cls])));
+        const int items = (n + per_item - 1) / per_item;
+        const bool direct = items == 1 && x.alone;
+        for (int i = 0; i < items; ++i) {
+            // splits of equal length but for rounding
+            const int a0 = (int)((int64_t)n * i / items), a1 = (int)((int64_t)n * (i + 1) / items);
+            recs.push_back({TILE_COST[x.cls] * (a1 - a0), (int)k, a0 * TT, std::min(x.len, a1 * TT),
+                            direct ? 0 : (int)(part + (int64_t)i * KV * rows), direct});
+        }
+        for (int i = 0; i < x.ntok; ++i) {
+            const int t = order[x.tok + i];
+            int32_t *r = tok + (size_t)t * TOK_WORDS;
+            seen[t] = 1;
+            if (direct) {
+                r[TK_DIRECT] = 1;
+                continue;
+            }
+            r[x.causal ? TK_OWN : TK_PRE] = (int)(part + i * G);
+            r[x.causal ? TK_OWN_ROWS : TK_PRE_ROWS] = rows;
+            r[x.causal ? TK_OWN_N : TK_PRE_N] = items;
+        }
+        if (!direct) {
+            part += (int64_t)items * KV * rows;
+            partial = true;
+        }
+    }
+    for (int t = 0; t < T && !partial; ++t) partial = !seen[t];  // a row that sees nothing is the combine's too
+    std::stable_sort(recs.begin(), recs.end(), [](const Rec &x, const Rec &y) { return x.cost > y.cost; });
+    int32_t *rw = w + a->rec_at;
+    for (const Rec &r : recs) {
+        const RowTile &x = tiles[r.tile];
+        rw[RC_FLAGS] = x.cls | (r.direct ? RF_DIRECT : 0) | (x.causal ? RF_CAUSAL : 0);
+        rw[RC_TOK] = x.tok;
+        rw[RC_NTOK] = x.ntok;
+        rw[RC_PAGES] = x.pages;
+        rw[RC_T0] = r.t0;
+        rw[RC_T1] = r.t1;
+        rw[RC_LIM] = x.lim;
+        rw[RC_PART] = r.part;
+        rw += REC_WORDS;
+    }
+    w[HD_RECS] = (int)recs.size();
+    w[HD_PARTIAL] = partial ? 1 : 0;
+    a->partial = partial;
     int32_t *pg = w + a->pages_at;
     if (own_pages > 0) std::memcpy(pg, b->pages, (size_t)own_pages * 4);
     if (grp_pages > 0) std::memcpy(pg + own_pages, b->group_pages, (size_t)grp_pages * 4);
-    return a->pages_at + own_pages + grp_pages;
+    return (size_t)a->pages_at + own_pages + grp_pages;
+}
+
+template <int D>
+cudaError_t launch_attn(const AttnParams &p, int n_sm, bool combine, cudaStream_t stream)
+{
+    attn_tile_kernel<D><<<n_sm, ATTN_THREADS, Layout<D>::BYTES, stream>>>(p);
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess || !combine) return e;
+    const int64_t rows = (int64_t)p.max_tok * p.n_heads;
+    const int64_t blocks = std::min<int64_t>((rows + COMBINE_WARPS - 1) / COMBINE_WARPS, 16 * (int64_t)n_sm);
+    attn_combine_kernel<D><<<(unsigned)blocks, 32 * COMBINE_WARPS, 0, stream>>>(p);
+    return cudaGetLastError();
 }
 
 }  // namespace
@@ -235,8 +1093,9 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
     *out = nullptr;
     if (!kv || !c) return SALT_ERR_INVALID_ARG;
     salt_ctx *ctx = kv->ctx;
-    if (c->n_heads < 1 || c->n_heads % kv->dev.heads || c->n_heads / kv->dev.heads > 64)
-        return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%d query heads over %d key/value heads", c->n_heads, kv->dev.heads);
+    const KvDev &d = kv->dev;
+    if (c->n_heads < 1 || c->n_heads % d.heads || c->n_heads / d.heads > 64)
+        return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%d query heads over %d key/value heads", c->n_heads, d.heads);
     if (c->max_seqs < 1 || c->max_seqs > SALT_MAX_TOKENS || c->max_groups < 0 || c->max_groups > SALT_MAX_TOKENS)
         return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "max_seqs %d, max_groups %d", c->max_seqs, c->max_groups);
     if (c->max_tokens < 1 || c->max_tokens > SALT_MAX_TOKENS)
@@ -247,19 +1106,41 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
     if (!a) return ctx_fail(ctx, SALT_ERR_OOM, "no host memory");
     a->kv = kv;
     a->cfg = *c;
+    a->device = ctx_device(ctx);
+    auto fail_with = [&](salt_status st, const char *what) {
+        cudaGetLastError();
+        salt_attn_destroy(a);
+        return ctx_fail(ctx, st, "%s", what);
+    };
+    if (cudaDeviceGetAttribute(&a->n_sm, cudaDevAttrMultiProcessorCount, ctx_device(ctx)) != cudaSuccess ||
+        cudaFuncSetAttribute(attn_tile_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<64>::BYTES) != cudaSuccess ||
+        cudaFuncSetAttribute(attn_tile_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<128>::BYTES) != cudaSuccess)
+        return fail_with(SALT_ERR_CUDA, "cannot prepare the attention kernel");
+    // codes as rows of D / 2 two-byte elements
+    const int64_t rows = (int64_t)kv->n_layers * d.n_pages * d.heads * d.page;
+    if (encode_map_2d(&a->kmap, reinterpret_cast<const uint16_t *>(d.k), d.dim / 2, rows, d.dim / 2, d.page) != cudaSuccess ||
+        encode_map_2d(&a->vmap, reinterpret_cast<const uint16_t *>(d.v), d.dim / 2, rows, d.dim / 2, d.page) != cudaSuccess)
+        return fail_with(SALT_ERR_CUDA, "cannot map the cache");
+    // Items: without splits at most one per request's and per group's row
+    // tile; with them the plan keeps within the rest.  Partial rows: two per
+    // row without splits.
+    const int G = c->n_heads / d.heads, per = std::max(1, R_MAX / G);
+    a->rec_cap = c->max_seqs + c->max_groups + 2 * (c->max_tokens / per + 1) + 16 * a->n_sm;
+    a->part_cap = 2ll * c->max_tokens * c->n_heads + 512ll * a->n_sm;
+    if (a->part_cap >= (1ll << 31)) return fail_with(SALT_ERR_INVALID_ARG, "max_tokens times n_heads is too large");
     a->tok_at = HEAD_WORDS;
-    a->pages_at = a->tok_at + c->max_tokens * TOK_WORDS;
+    a->order_at = a->tok_at + c->max_tokens * TOK_WORDS;
+    a->rec_at = (a->order_at + 2 * c->max_tokens + 3) / 4 * 4;
+    a->pages_at = a->rec_at + a->rec_cap * REC_WORDS;
     a->plan_words = ((size_t)a->pages_at + c->max_pages + 3) / 4 * 4;
-    bool ok = cudaMalloc(&a->plan, a->plan_words * 4) == cudaSuccess;
+    bool ok = cudaMalloc(&a->plan, a->plan_words * 4) == cudaSuccess &&
+              cudaMalloc(&a->part_o, (size_t)a->part_cap * d.dim * 4) == cudaSuccess &&
+              cudaMalloc(&a->part_l, (size_t)a->part_cap * 4) == cudaSuccess;
     for (int i = 0; i < 2 && ok; ++i)
         ok = cudaHostAlloc(reinterpret_cast<void **>(&a->staging[i]), a->plan_words * 4, cudaHostAllocMapped) == cudaSuccess &&
              cudaEventCreateWithFlags(&a->staging_ev[i], cudaEventDisableTiming) == cudaSuccess;
     ok = ok && cudaEventCreateWithFlags(&a->tmp_ev, cudaEventDisableTiming) == cudaSuccess;
-    if (!ok) {
-        cudaGetLastError();
-        salt_attn_destroy(a);
-        return ctx_fail(ctx, SALT_ERR_OOM, "no memory for the plan's tables (%zu bytes)", a->plan_words * 4);
-    }
+    if (!ok) return fail_with(SALT_ERR_OOM, "no memory for the plan's tables and partial results");
     *out = a;
     return SALT_OK;
 }
@@ -267,9 +1148,11 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
 void salt_attn_destroy(salt_attn *a)
 {
     if (!a) return;
-    ctx_select_device(a->kv->ctx);
+    cudaSetDevice(a->device);  // (the cache and the context may be gone already)
     cudaDeviceSynchronize();
     cudaFree(a->plan);
+    cudaFree(a->part_o);
+    cudaFree(a->part_l);
     for (int i = 0; i < 2; ++i) {
         if (a->staging[i]) cudaFreeHost(a->staging[i]);
         if (a->staging_ev[i]) cudaEventDestroy(a->staging_ev[i]);
@@ -280,7 +1163,7 @@ void salt_attn_destroy(salt_attn *a)
 }
 
 salt_status salt_attn_build(salt_attn *a, const salt_attn_batch *b, salt_stream_t stream_)
-{
+try {
     NvtxRange nvtx_range("salt_attn_build");
     if (!a) return SALT_ERR_INVALID_ARG;
     salt_ctx *ctx = a->kv->ctx;
@@ -306,14 +1189,16 @@ salt_status salt_attn_build(salt_attn *a, const salt_attn_batch *b, salt_stream_
     SALT_CUDA_OR_FAIL(ctx, cudaEventRecord(a->staging_ev[k], stream));
     a->staging_used[k] = true;
     a->T = T;
-    a->built = true;
     a->use_streams.assign(1, stream);
+    a->built = true;
     return SALT_OK;
+} catch (const std::bad_alloc &) {
+    return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
 }
 
 salt_status salt_attn_run(salt_attn *a, int32_t layer, const void *q, int64_t q_stride, float scale, void *out,
                           int64_t out_stride, float *lse, salt_stream_t stream_)
-{
+try {
     NvtxRange nvtx_range("salt_attn_run");
     if (!a) return SALT_ERR_INVALID_ARG;
     salt_ctx *ctx = a->kv->ctx;
@@ -338,26 +1223,35 @@ salt_status salt_attn_run(salt_attn *a, int32_t layer, const void *q, int64_t q_
         if (std::find(a->use_streams.begin(), a->use_streams.end(), stream) == a->use_streams.end())
             a->use_streams.push_back(stream);
     }
+    // a captured run may be replayed for a plan that needs the combine
+    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+    if (!a->partial) SALT_CUDA_OR_FAIL(ctx, cudaStreamIsCapturing(stream, &cap));
     AttnParams p;
+    p.kmap = a->kmap;
+    p.vmap = a->vmap;
     p.plan = a->plan;
     p.kv = kv;
     p.layer = layer;
     p.q = static_cast<const uint16_t *>(q);
     p.out = static_cast<uint16_t *>(out);
     p.lse = lse;
+    p.part_o = a->part_o;
+    p.part_l = a->part_l;
     p.q_stride = q_stride;
     p.out_stride = out_stride;
     p.n_heads = a->cfg.n_heads;
     p.max_tok = a->T;
     p.tok_at = a->tok_at;
+    p.order_at = a->order_at;
+    p.rec_at = a->rec_at;
     p.pages_at = a->pages_at;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.err = ctx_error_word(ctx);
-    const int64_t blocks = ((int64_t)a->T * a->cfg.n_heads + ROW_WARPS - 1) / ROW_WARPS;
-    auto kernel = kv.dim == 128 ? attn_row_kernel<128> : attn_row_kernel<64>;
-    kernel<<<(unsigned)blocks, 32 * ROW_WARPS, 0, stream>>>(p);
-    SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+    const bool combine = a->partial || cap != cudaStreamCaptureStatusNone;
+    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_attn<128>(p, a->n_sm, combine, stream) : launch_attn<64>(p, a->n_sm, combine, stream));
     return SALT_OK;
+} catch (const std::bad_alloc &) {
+    return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
 }
 
 }  // extern "C"

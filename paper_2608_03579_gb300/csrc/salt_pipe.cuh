@@ -41,6 +41,14 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
         "l"(map), "r"(x), "r"(y), "r"(bar)
         : "memory");
 }
+// `bytes` (a multiple of 16, both addresses 16-byte aligned) from global to
+// shared memory, completing on bar by bytes
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(bar)
+                 : "memory");
+}
 // The same into this CTA's shared memory; with CG = 2 the barrier may be the
 // peer's (a cluster address).
 template <int CG>

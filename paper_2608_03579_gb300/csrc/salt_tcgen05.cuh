@@ -307,4 +307,52 @@ __device__ __forceinline__ void umma_commit_cg(uint32_t bar)
     }
 }
 
+// ---------------------------------------------------------------- 8-bit operands
+// kind::f8f6f4, e4m3 x e4m3 -> fp32; a set bit of `mn` (1: A, 2: B) makes that
+// operand MN-major.  One MMA is 32 deep.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, uint32_t mn)
+{
+    return (1u << 4)                     // D format: f32 (A and B formats 0: e4m3)
+           | (mn << 15)                  // transposed operands
+           | ((uint32_t)(N >> 3) << 17)  // N / 8
+           | ((uint32_t)(M >> 4) << 24); // M / 16
+}
+// Descriptor of an operand whose rows (K-major: one row's K; MN-major: one K
+// index's MN extent) are `pitch` = 32, 64 or 128 bytes, swizzled as wide as they
+// are; 8-row groups follow each other.  An MN extent past the pitch continues
+// `lbo` bytes further (MN-major).
+__device__ __forceinline__ uint64_t sdesc_rows(uint32_t saddr, uint32_t pitch, uint32_t lbo)
+{
+    const uint64_t layout = pitch == 128 ? 2 : pitch == 64 ? 4 : 6;
+    return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
+           ((uint64_t)((8 * pitch) >> 4) << 32) | ((uint64_t)1 << 46) | (layout << 61);
+}
+// the swizzle of such rows: where byte `at` of the tile lies
+template <int PITCH>
+__device__ __forceinline__ uint32_t swz_rows(uint32_t at)
+{
+    constexpr uint32_t mask = PITCH == 128 ? 7u : PITCH == 64 ? 3u : 1u;
+    return at ^ (((at >> 7) & mask) << 4);
+}
+__device__ __forceinline__ void umma_e4m3(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n" ::"r"(
+            d_tmem),
+        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate));
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];\n"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};\n" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;\n" ::: "memory"); }
+
 }  // namespace salt
