@@ -6,21 +6,19 @@
 // (rows of all its requests) or a request's own tokens.  An item walks its
 // range in tiles of 128 tokens, on the tensor cores with the cache as the
 // 128-row operand A, so that few query rows waste little:
-//     S^T[token][row] = K[token][:] . Q[row][:]            (M = 128, N = R)
-//     O^T[dim][row]  += V[token][dim] P[token][row]        (M = D, K = tokens)
-// The e4m3 codes go from the cache to the MMA as they are; the exponents of a
-// token's row multiply its scores (K) and its probabilities (V), both exact.
-// Q and P meet them as two e4m3 terms each, hi + lo, which holds 8 bits: a bf16
-// query is split exactly (its 8 bits are 4 and 4; elements below 2^-9 of the
-// row's largest to within 2^-17 of that), a probability to within 2^-9 and lo
-// kept at 16 times its size in columns of its own, so that small ones next to
-// a large one stay exact to 2^-21 of it.
+//     S^T[token][row] = K[token][:] . Q[row][:]            (M = 128, N = R, e4m3)
+//     O^T[dim][row]  += V[token][dim] P[token][row]        (M = D, K = tokens, f16)
+// The e4m3 codes of K go from the cache to the MMA as they are, those of V
+// are widened to f16 on the way (both exact); the exponents of a token's row
+// multiply its scores (K) and its probabilities (V), exact too.  Q meets K as
+// two e4m3 terms, hi + lo: the 8 bits of a bf16 are 4 and 4 (elements below 2^-9 of
+// the row's largest are off by up to 2^-17 of that).  P is f16: 2^-12 relative,
+// and 2^-27 of the row's largest where that is more.
 //
 // Softmax: thread = token, registers = rows.  The reference m of a row moves
-// only when a score passes it by more than the codes' headroom (a vote a
-// tile), so the usual tile needs no reduction over tokens: p = 2^(s - m), l += p,
-// P = p 2^e_v in codes.  Items of one row meet in the combine kernel through their
-// (o / l, m + log2 l).
+// only when a probability passes f16's range (a vote a tile), so the usual tile
+// needs no reduction over tokens: p = 2^(s - m), l += p, P = p 2^e_v.  Items of one
+// row meet in the combine kernel through their (o / l, m + log2 l).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -51,10 +49,12 @@ constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
 
 constexpr int TT = 128;          // cached tokens a tile
 constexpr int R_MAX = 128;       // rows an item
-constexpr int ATTN_THREADS = 384;
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
-constexpr float P_TOP = 7.5f;    // a new reference puts the row's largest P at 2^7.5
-constexpr float P_MOST = 8.8f;   // and is due when one passes 2^8.8 (e4m3 ends at 448 = 2^8.807)
+constexpr int NWG = 4;           // softmax warpgroups, each with its share of the rows
+constexpr int ATTN_THREADS = 128 + NWG * WG;
+constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
+constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
+constexpr int CW_MAX = R_MAX / NWG;  // columns of a warpgroup
 constexpr float M_NONE = -1e30f; // the reference before the first token
 
 struct AttnParams {
@@ -83,26 +83,41 @@ __global__ void plan_copy_kernel(const uint4 *src, uint4 *dst, int n)
 // ---------------------------------------------------------------- shared memory
 template <int D>
 struct Layout {
-    static constexpr int STAGES = D == 128 ? 3 : 6;
+    static constexpr int STAGES = D == 128 ? 3 : 6;       // of K and of V
     static constexpr uint32_t SIDE = TT * D;              // codes of K or V of a tile
-    static constexpr uint32_t P_BUF = TT * 2 * R_MAX;     // P of a tile, hi and lo
-    static constexpr uint32_t KV = 0;
-    static constexpr uint32_t P = KV + STAGES * 2 * SIDE;
-    static constexpr uint32_t Q = P + 2 * P_BUF;
-    static constexpr uint32_t EXPS = Q + 2 * R_MAX * D;   // per stage: 128 of K, 128 of V
+    static constexpr uint32_t K = 0;
+    static constexpr uint32_t V = K + STAGES * SIDE;
+    static constexpr uint32_t VH = V + STAGES * SIDE;     // V of a tile in f16
+    static constexpr uint32_t P = VH + 2 * SIDE;          // P of a tile in f16
+    static constexpr uint32_t Q = P + TT * 2 * R_MAX;
+    static constexpr uint32_t EXPS = Q + 2 * R_MAX * D;   // per stage of V: 128 of K, 128 of V
     static constexpr uint32_t INFO = EXPS + STAGES * 2 * TT;
-    static constexpr uint32_t FAC = INFO + 2 * R_MAX * 16;
-    static constexpr uint32_t WMAX = FAC + R_MAX * 4;     // [2][4][R_MAX / 2] floats
-    static constexpr uint32_t BARS = WMAX + 4 * R_MAX * 4;
-    static constexpr uint32_t N_BARS = 3 * STAGES + 12;
-    static constexpr uint32_t MISC = BARS + N_BARS * 8;   // TMEM address, failure flag, [2][2] largest value exponents
+    static constexpr uint32_t FAC = INFO + 2 * R_MAX * 16;  // (INFO: per item ColAM[R_MAX], ColLR[R_MAX])
+    static constexpr uint32_t WMAX = FAC + R_MAX * 4;     // [NWG][4][CW_MAX] floats
+    // barriers: K full, K free, V full, V free (a stage each), scores full [2], P full, product done, Q full [2], item
+    // done [2], Q free, drain
+    static constexpr uint32_t K_FULL = WMAX + 4 * R_MAX * 4;
+    static constexpr uint32_t K_FREE = K_FULL + 8 * STAGES;
+    static constexpr uint32_t V_FULL = K_FREE + 8 * STAGES;
+    static constexpr uint32_t V_FREE = V_FULL + 8 * STAGES;
+    static constexpr uint32_t S_FULL = V_FREE + 8 * STAGES;
+    static constexpr uint32_t P_FULL = S_FULL + 16;
+    static constexpr uint32_t PV_DONE = P_FULL + 8;
+    static constexpr uint32_t Q_FULL = PV_DONE + 8;
+    static constexpr uint32_t O_FREE = Q_FULL + 16;
+    static constexpr uint32_t Q_FREE = O_FREE + 16;
+    static constexpr uint32_t DRAIN = Q_FREE + 8;
+    static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents
     static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
 };
+constexpr uint32_t TM_S = 0, TM_O = 256;  // tensor memory columns: two buffers of R_MAX scores, the output
 
-// A column's constants: factor of its scores (query row scale, scale, log2 e), reference m, tokens it
-// sees, (query token << 8 | head in the group).
-struct ColInfo {
+// A column's constants: the factor of its scores (query row's power of two, scale,
+// log2 e) and the reference m; the tokens it sees and (query token << 8 | head in the group).
+struct ColAM {
     float a, m;
+};
+struct ColLR {
     int32_t lim, row;
 };
 
@@ -112,16 +127,10 @@ __device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ __half2 half2_of_e4m3x2(uint16_t c)
+__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c)
 {
     uint32_t r;
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(c));
-    return *reinterpret_cast<__half2 *>(&r);
-}
-__device__ __forceinline__ uint16_t e4m3x2_of_half2(__half2 h)
-{
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;\n" : "=h"(r) : "r"(*reinterpret_cast<uint32_t *>(&h)));
     return r;
 }
 __device__ __forceinline__ float ex2(float x)
@@ -135,24 +144,22 @@ __device__ __forceinline__ float pow2(int k) { return __uint_as_float(k < -126 ?
 // 2^(e - 127) of an exponent byte; 0 for a row of zeros, NaN for a row that stands for NaN
 __device__ __forceinline__ float row_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
 
-// hi and lo * 16 of two values as codes: v = hi + lo to 2^-9
-__device__ __forceinline__ void split_pair(float v0, float v1, uint16_t &hi, uint16_t &lo)
-{
-    hi = e4m3x2(v0, v1);
-    const __half2 rest = __hsub2(__floats2half2_rn(v0, v1), half2_of_e4m3x2(hi));
-    lo = e4m3x2_of_half2(__hmul2(rest, __floats2half2_rn(16.f, 16.f)));
-}
-
-__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
-__device__ __forceinline__ void sts16(uint32_t a, uint16_t v) { asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(a), "h"(v) : "memory"); }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(a), "r"(x), "r"(y) : "memory"); }
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
 
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
 struct Item {
     int flags, tok, ntok, pages, t0, t1, lim, part, kh;
-    int tiles, rows, half;  // half: rows of the first warpgroup's columns
+    int tiles, rows, per;  // per: rows a warpgroup takes
 };
 
 // The CTA's r-th item of n: the records are in falling order of cost, handed
@@ -175,7 +182,7 @@ __device__ __forceinline__ Item load_item(const AttnParams &p, int idx, int G)
     it.kh = idx - rec * p.kv.heads;
     it.rows = it.ntok * G;
     it.part = b.w + it.kh * it.rows;
-    it.half = (it.rows + 1) >> 1;
+    it.per = (it.rows + NWG - 1) / NWG;
     it.tiles = (it.t1 - it.t0 + TT - 1) / TT;
     return it;
 }
@@ -190,31 +197,29 @@ __device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, const vo
     return false;
 }
 
-// Adds up each of N values over the warp's lanes: lane's sum is that of value
-// returned in `col` (32 / N lanes hold the same one).
-template <int N>
-__device__ __forceinline__ float sum_columns(const float *v, int lane, int &col)
+// Reduces each of N values over the warp's lanes (N a power of two up to
+// 32) by halving: a lane ends up with that of value `col`, 32 / N lanes with
+// the same one.
+template <int N, class Op>
+__device__ __forceinline__ float reduce_columns(float *t, int lane, int &col, Op op)
 {
-    float t[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) t[i] = v[i];
     col = 0;
     int n = N;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
         if (n > 1) {
             n >>= 1;
+            const bool up = lane & o;
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
                 if (i < n) {
-                    const bool up = lane & o;
                     const float send = up ? t[i] : t[i + n];
-                    t[i] = (up ? t[i + n] : t[i]) + __shfl_xor_sync(0xffffffffu, send, o);
+                    t[i] = op(up ? t[i + n] : t[i], __shfl_xor_sync(0xffffffffu, send, o));
                 }
             }
-            if (lane & o) col += n;
+            if (up) col += n;
         } else {
-            t[0] += __shfl_xor_sync(0xffffffffu, t[0], o);
+            t[0] = op(t[0], __shfl_xor_sync(0xffffffffu, t[0], o));
         }
     }
     return t[0];
@@ -239,178 +244,211 @@ __device__ __forceinline__ void soft_wait(Soft &s, uint32_t bar, uint32_t parity
     s.ok = __all_sync(0xffffffffu, r);
 }
 
+// Addresses and constants of an item for a softmax warpgroup.
+struct SoftItem {
+    ColAM *am;
+    ColLR *lr;
+    float *fac, *wmax;
+    int ncol, vtop, nb, j;
+    uint32_t lanes, o_at;
+};
+
+// Scores of CH columns (from column c0 of the warpgroup) less their references, in log2;
+// with MASK minus infinity where the row does not see the token.  Returns the
+// largest.  Columns are dealt with eight at a time.
+template <int CH, bool MASK>
+__device__ __forceinline__ float soft_args(float (&x)[CH], const SoftItem &w, uint32_t s_at, int c0, float kf, int tok)
+{
+#pragma unroll
+    for (int c = 0; c < CH; c += 8)
+        if (c0 + c < w.ncol) tmem_ld8(s_at + c0 + c, reinterpret_cast<uint32_t *>(x) + c);
+    tmem_ld_wait();
+    float mx = -INFINITY;
+#pragma unroll
+    for (int c = 0; c < CH; c += 8) {
+        if (c0 + c < w.ncol) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const float4 k = *reinterpret_cast<const float4 *>(w.am + c0 + c + i);
+                x[c + i] = fmaf(x[c + i], kf * k.x, -k.y);
+                x[c + i + 1] = fmaf(x[c + i + 1], kf * k.z, -k.w);
+                if (MASK) {
+                    const int4 v = *reinterpret_cast<const int4 *>(w.lr + c0 + c + i);
+                    if (tok >= v.x) x[c + i] = -INFINITY;
+                    if (tok >= v.z) x[c + i + 1] = -INFINITY;
+                }
+                mx = fmaxf(mx, fmaxf(x[c + i], x[c + i + 1]));
+            }
+        }
+    }
+    return mx;
+}
+
+// A tile of an item of the class with CW columns a warpgroup.  False: gave up
+// (the whole warpgroup together).
+template <int D, int CW, bool MASK>
+__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float (&l)[CW], int tok, uint32_t ke, uint32_t ve)
+{
+    using L = Layout<D>;
+    constexpr int CH = CW < 16 ? CW : 16;    // columns in registers at a time
+    constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
+    const float kf = row_scale(ke), vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - w.vtop);
+    // what P is to p in log2, held so that p stays in range (a value 2^100 below the largest may lose bits)
+    const float vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
+    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
+    uint32_t ph[CW / 2];
+#pragma unroll
+    for (int c0 = 0; c0 < CW; c0 += CH) {
+        if (c0 >= w.ncol) break;
+        float x[CH];
+        float mx = soft_args<CH, MASK>(x, w, s_at, c0, kf, tok) + vref;
+        if (!named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST))) {
+            // some row's reference has to move
+            if (!named_sync_and(w.nb, WG, s.ok)) return false;
+            int col;
+#pragma unroll
+            for (int c = 0; c < CH; c += 8)  // m + (s - m) is not s: take the scores anew
+                if (c0 + c < w.ncol) tmem_ld8(s_at + c0 + c, reinterpret_cast<uint32_t *>(x) + c);
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const ColAM k = w.am[c0 + c];
+                x[c] = fmaf(x[c], kf * k.a, vref);
+                if ((MASK && tok >= w.lr[c0 + c].lim) || !(x[c] == x[c]) || c0 + c >= w.ncol) x[c] = -INFINITY;
+            }
+            const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
+            w.wmax[s.quarter * CW_MAX + col] = v;
+            named_sync(w.nb, WG);
+            if (s.tid < CH) {
+                float t = w.wmax[s.tid];
+                for (int q = 1; q < 4; ++q) t = fmaxf(t, w.wmax[q * CW_MAX + s.tid]);
+                const float m = w.am[c0 + s.tid].m;
+                const bool move = t - m > P_MOST && c0 + s.tid < w.ncol;
+                w.fac[s.tid] = move ? ex2(m - (t - P_TOP)) : 1.f;
+                if (move) w.am[c0 + s.tid].m = t - P_TOP;
+            }
+            named_sync(w.nb, WG);
+            if (w.j > 0) {
+                soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < CH; c += 8) {
+                    if (c0 + c < w.ncol) {
+                        float o[8];
+                        tmem_ld8(w.o_at + c0 + c, reinterpret_cast<uint32_t *>(o));
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float f = w.fac[c + i];
+                            o[i] *= f;
+                            l[c0 + c + i] *= f;
+                        }
+                        tmem_st8(w.o_at + c0 + c, reinterpret_cast<const uint32_t *>(o));
+                    }
+                }
+                tmem_st_wait();
+            }
+            soft_args<CH, MASK>(x, w, s_at, c0, kf, tok);
+            named_sync(w.nb, WG);  // fac and wmax are free again
+        }
+#pragma unroll
+        for (int c = 0; c < CH; c += 8) {
+            if (c0 + c < w.ncol) {
+#pragma unroll
+                for (int i = c; i < c + 8; i += 2) {
+                    const float e0 = ex2(x[i]), e1 = ex2(x[i + 1]);
+                    float v0 = e0 * vf, v1 = e1 * vf;
+                    l[c0 + i] += e0;
+                    l[c0 + i + 1] += e1;
+                    if (MASK) {  // not 0 * NaN
+                        if (x[i] == -INFINITY) v0 = 0.f;
+                        if (x[i + 1] == -INFINITY) v1 = 0.f;
+                    }
+                    const __half2 h = __floats2half2_rn(v0, v1);
+                    ph[(c0 + i) / 2] = *reinterpret_cast<const uint32_t *>(&h);
+                }
+            }
+        }
+    }
+    // P and the widened V take the place of the last tile's once its product is done
+    if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+    const uint32_t p_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128);
+    const uint32_t row_at = s.tid * PITCH + s.wg * 2 * CW % 128;
+#pragma unroll
+    for (int c = 0; c < CW; c += 8)
+        if (c < w.ncol) sts128(p_at + swz_rows<PITCH>(row_at + 2 * c), ph[c / 2], ph[c / 2 + 1], ph[c / 2 + 2], ph[c / 2 + 3]);
+    return true;
+}
+
+// The warpgroups' share of a tile's values in f16; zeros from row `valid` on
+// (past the range a stage holds other tokens' values, or none: 0 * NaN must
+// not arise).
+template <int D>
+__device__ __forceinline__ void widen_values(const Soft &s, int valid)
+{
+    using L = Layout<D>;
+    constexpr int CPR = D / 16;  // 16-byte pieces of a row's codes
+    const uint32_t from = s.base + L::V + s.stage * L::SIDE, to = s.base + L::VH;
+#pragma unroll
+    for (int k = 0; k < TT * CPR / (NWG * WG); ++k) {
+        const int q = k * (NWG * WG) + s.wg * WG + s.tid;
+        const int row = q / CPR, ch = q % CPR;
+        const uint4 c = lds128(from + swz_rows<D>(row * D + ch * 16));
+        const uint32_t x[4] = {c.x, c.y, c.z, c.w};
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            h[2 * i] = f16x2_of_e4m3x2((uint16_t)x[i]);
+            h[2 * i + 1] = f16x2_of_e4m3x2((uint16_t)(x[i] >> 16));
+        }
+        if (row >= valid) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] = 0;
+        }
+        const uint32_t at = to + (ch / 4) * (TT * 128), off = row * 128 + (ch % 4) * 32;
+        sts128(at + swz_rows<128>(off), h[0], h[1], h[2], h[3]);
+        sts128(at + swz_rows<128>(off + 16), h[4], h[5], h[6], h[7]);
+    }
+}
+
 // One item of the class with CW columns a warpgroup.  False: gave up (the
 // whole warpgroup together).
 template <int D, int CW>
 __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const Item &it, int n_item)
 {
     using L = Layout<D>;
-    constexpr int CH = CW < 32 ? CW : 32;    // columns in registers at a time
-    constexpr int PITCH = CW == 64 ? 128 : 4 * CW;
-    const uint32_t bars = s.base + L::BARS;
-    const uint32_t kfull = bars, vfull = bars + 8 * L::STAGES;
-    const uint32_t s_full = bars + 8 * (3 * L::STAGES), p_full = s_full + 16, pv_done = s_full + 32, o_free = s_full + 64;
-    ColInfo *info = reinterpret_cast<ColInfo *>(s.sm + L::INFO) + (n_item & 1) * R_MAX + s.wg * CW;
-    float *fac = reinterpret_cast<float *>(s.sm + L::FAC) + s.wg * (R_MAX / 2);
-    float *wmax = reinterpret_cast<float *>(s.sm + L::WMAX) + s.wg * 4 * (R_MAX / 2);
-    const int ncol = s.wg ? it.rows - it.half : it.half;
-    const uint32_t lanes = (uint32_t)(s.quarter * 32) << 16;
-    const uint32_t o_at = s.tmem + lanes + 256 + s.wg * 2 * CW;
-    const int nb = 1 + s.wg;
+    constexpr int CH = CW < 16 ? CW : 16;
+    SoftItem w;
+    w.am = reinterpret_cast<ColAM *>(s.sm + L::INFO + (n_item & 1) * R_MAX * 16) + s.wg * CW;
+    w.lr = reinterpret_cast<ColLR *>(s.sm + L::INFO + (n_item & 1) * R_MAX * 16 + R_MAX * 8) + s.wg * CW;
+    w.fac = reinterpret_cast<float *>(s.sm + L::FAC) + s.wg * CW_MAX;
+    w.wmax = reinterpret_cast<float *>(s.sm + L::WMAX) + s.wg * 4 * CW_MAX;
+    w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
+    w.lanes = (uint32_t)(s.quarter * 32) << 16;
+    w.o_at = s.tmem + w.lanes + TM_O + s.wg * CW;
+    w.nb = 1 + s.wg;
     // values count in units of the largest exponent of the range
     const volatile int *vt = reinterpret_cast<const volatile int *>(s.sm + L::MISC + 8) + 2 * (n_item & 1);
-    const int vtop = max(vt[0], vt[1]) > 0 ? max(vt[0], vt[1]) : 127;
+    w.vtop = max(vt[0], vt[1]) > 0 ? max(vt[0], vt[1]) : 127;
     float l[CW];
 #pragma unroll
     for (int c = 0; c < CW; ++c) l[c] = 0.f;
-    for (int j = 0; j < it.tiles; ++j) {
-        const uint32_t b = s.g & 1;
-        const int tok = it.t0 + j * TT + s.tid;
-        // every row sees the whole tile: no column masks (the first query token sees least)
-        const bool mask = it.t0 + (j + 1) * TT > min(it.t1, it.lim);
-        soft_wait(s, kfull + 8 * s.stage, s.stage_phase);
-        soft_wait(s, s_full + 8 * b, (s.g >> 1) & 1);
+    for (w.j = 0; w.j < it.tiles; ++w.j) {
+        const int tok = it.t0 + w.j * TT + s.tid;
+        const int end = it.t0 + (w.j + 1) * TT;
+        soft_wait(s, s.base + L::V_FULL + 8 * s.stage, s.stage_phase);
+        soft_wait(s, s.base + L::S_FULL + 8 * (s.g & 1), (s.g >> 1) & 1);
         tc_fence_after();
         const uint32_t ke = s.sm[L::EXPS + s.stage * 2 * TT + s.tid], ve = s.sm[L::EXPS + s.stage * 2 * TT + TT + s.tid];
-        const float kf = row_scale(ke), vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - vtop);
-        // what P is to p in log2, held so that p stays in range (a value 2^100 below the largest may lose bits)
-        const float vref = ve == 255u ? 0.f : (float)max((int)ve - vtop, -100);
-        const uint32_t s_at = s.tmem + lanes + b * 128 + s.wg * CW;
-#pragma unroll
-        for (int ch = 0; ch < CW / CH; ++ch) {
-            float x[CH];
-            float mx = -INFINITY;
-            auto load = [&] {
-#pragma unroll
-                for (int c = 0; c < CH; c += 8) tmem_ld8(s_at + ch * CH + c, reinterpret_cast<uint32_t *>(x) + c);
-                tmem_ld_wait();
-            };
-            load();
-            auto args = [&] {  // s - m; -inf where the row does not see the token
-                mx = -INFINITY;
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    if (ch * CH + c < ncol) {
-                        const ColInfo ci = info[ch * CH + c];
-                        x[c] = fmaf(x[c], kf * ci.a, -ci.m);
-                        if (mask && tok >= ci.lim) x[c] = -INFINITY;
-                        mx = fmaxf(mx, x[c]);
-                    }
-                }
-                mx += vref;
-            };
-            args();
-            if (!named_sync_and(nb, WG, s.ok && !(mx > P_MOST))) {
-                // some row's reference has to move
-                if (!named_sync_and(nb, WG, s.ok)) return false;
-                load();
-#pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    if (ch * CH + c < ncol) {
-                        const ColInfo ci = info[ch * CH + c];
-                        float v = fmaf(x[c], kf * ci.a, vref);
-                        if ((mask && tok >= ci.lim) || !(v == v)) v = -INFINITY;
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-                        if (s.lane == 0) wmax[s.quarter * (R_MAX / 2) + c] = v;
-                    }
-                }
-                named_sync(nb, WG);
-                if (s.tid < CH && ch * CH + s.tid < ncol) {
-                    float v = wmax[s.tid];
-                    for (int w = 1; w < 4; ++w) v = fmaxf(v, wmax[w * (R_MAX / 2) + s.tid]);
-                    ColInfo &ci = info[ch * CH + s.tid];
-                    float f = 1.f;
-                    if (v - ci.m > P_MOST) {
-                        const float m = v - P_TOP;
-                        f = ex2(ci.m - m);
-                        ci.m = m;
-                    }
-                    fac[s.tid] = f;
-                }
-                named_sync(nb, WG);
-                if (j > 0) {
-                    const uint32_t last = s.g - 1;
-                    soft_wait(s, pv_done + 8 * (last & 1), (last >> 1) & 1);
-                    tc_fence_after();
-#pragma unroll
-                    for (int c = 0; c < CH; c += 8) {
-                        if (ch * CH + c < ncol) {
-                            uint32_t o[16];
-                            const uint32_t at = o_at + ch * CH + c;
-                            tmem_ld8(at, o);
-                            tmem_ld8(at + CW, o + 8);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float f = ch * CH + c + i < ncol ? fac[c + i] : 1.f;
-                                o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                                o[i + 8] = __float_as_uint(__uint_as_float(o[i + 8]) * f);
-                            }
-                            tmem_st8(at, o);
-                            tmem_st8(at + CW, o + 8);
-                        }
-                    }
-                    tmem_st_wait();
-#pragma unroll
-                    for (int c = 0; c < CH; ++c)
-                        if (ch * CH + c < ncol) l[ch * CH + c] *= fac[c];
-                }
-                load();
-                args();
-                named_sync(nb, WG);  // fac and wmax are free again
-            }
-            // the P buffer is free once the product two tiles back is done
-            if (ch == 0 && s.g >= 2) soft_wait(s, pv_done + 8 * b, ((s.g >> 1) - 1) & 1);
-            const uint32_t p_at = s.base + L::P + b * L::P_BUF + (CW == 64 ? s.wg * (TT * 128) : 0);
-            const uint32_t row_at = s.tid * PITCH + (CW == 64 ? 0 : s.wg * 2 * CW);
-            uint32_t hi[CH / 4], lo[CH / 4];
-#pragma unroll
-            for (int c = 0; c < CH; c += 2) {
-                uint16_t h = 0, w = 0;
-                if (ch * CH + c < ncol) {
-                    float v[2];
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const float e = ex2(x[c + i]);
-                        v[i] = e * vf;
-                        if (ch * CH + c + i < ncol) {
-                            l[ch * CH + c + i] += e;
-                            if (mask && x[c + i] == -INFINITY) v[i] = 0.f;  // not 0 * NaN
-                        }
-                    }
-                    split_pair(v[0], v[1], h, w);
-                }
-                if (c % 4 == 0) {
-                    hi[c / 4] = h;
-                    lo[c / 4] = w;
-                } else {
-                    hi[c / 4] |= (uint32_t)h << 16;
-                    lo[c / 4] |= (uint32_t)w << 16;
-                }
-            }
-            if constexpr (CW == 8) {
-                sts128(p_at + swz_rows<PITCH>(row_at), hi[0], hi[1], lo[0], lo[1]);
-            } else {
-#pragma unroll
-                for (int c = 0; c < CH; c += 16) {
-                    sts128(p_at + swz_rows<PITCH>(row_at + ch * CH + c), hi[c / 4], hi[c / 4 + 1], hi[c / 4 + 2], hi[c / 4 + 3]);
-                    sts128(p_at + swz_rows<PITCH>(row_at + CW + ch * CH + c), lo[c / 4], lo[c / 4 + 1], lo[c / 4 + 2], lo[c / 4 + 3]);
-                }
-            }
-        }
-        // past the range a stage holds other tokens' values, or none: 0 * NaN must not arise
-        if (s.wg == 0 && it.t0 + (j + 1) * TT > it.t1) {
-            soft_wait(s, vfull + 8 * s.stage, s.stage_phase);
-            if (tok >= it.t1) {
-                const uint32_t v_at = s.base + L::KV + s.stage * 2 * L::SIDE + L::SIDE + s.tid * D;
-#pragma unroll
-                for (int c = 0; c < D; c += 16) sts128(v_at + c, 0, 0, 0, 0);
-            }
-        }
+        // column masks only where a row does not see the whole tile (the first query token sees least)
+        const bool go = end > min(it.t1, it.lim) ? soft_tile<D, CW, true>(s, w, l, tok, ke, ve)
+                                                 : soft_tile<D, CW, false>(s, w, l, tok, ke, ve);
+        if (!go) return false;
+        widen_values<D>(s, it.t1 - (end - TT));
         tc_fence_before();
         fence_async_smem();
-        mbar_arrive_release(p_full + 8 * b);
+        mbar_arrive_release(s.base + L::P_FULL);
+        mbar_arrive_release(s.base + L::V_FREE + 8 * s.stage);
         ++s.g;
         if (++s.stage == L::STAGES) {
             s.stage = 0;
@@ -418,56 +456,57 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         }
     }
     // ------------------------------------------------ the item's rows
-    const uint32_t last = s.g - 1;
-    soft_wait(s, pv_done + 8 * (last & 1), (last >> 1) & 1);
-    tc_fence_after();
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += CH) {
         int col;
-        const float t = sum_columns<CH>(l + c0, s.lane, col);
-        wmax[s.quarter * (R_MAX / 2) + c0 + col] = t;
+        const float t = reduce_columns<CH>(l + c0, s.lane, col, [](float p, float q) { return p + q; });
+        w.wmax[s.quarter * CW_MAX + c0 + col] = t;
     }
-    if (!named_sync_and(nb, WG, s.ok)) return false;
+    if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int G = p.n_heads / p.kv.heads;
     const bool direct = it.flags & RF_DIRECT;
-    const int row0 = s.wg ? it.half : 0;
+    if (s.tid < w.ncol) {
+        const float t = w.wmax[s.tid] + w.wmax[CW_MAX + s.tid] + w.wmax[2 * CW_MAX + s.tid] + w.wmax[3 * CW_MAX + s.tid];
+        const int row = w.lr[s.tid].row;
+        const float lse2 = t > 0.f ? w.am[s.tid].m + log2f(t) : t == t ? -INFINITY : t;
+        int64_t at;  // the row's first element
+        if (direct) {
+            at = (row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * D;
+            if (p.lse) p.lse[(int64_t)(row >> 8) * p.n_heads + it.kh * G + (row & 255)] = lse2 * 0.693147180559945f;
+        } else {
+            const int part = it.part + s.wg * it.per + s.tid;
+            at = (int64_t)part * D;
+            p.part_l[part] = lse2;
+        }
+        // the column's constants make way for its factors and its place
+        w.am[s.tid] = ColAM{t > 0.f ? 1.f / t : t == t ? 0.f : t, pow2(w.vtop - 127)};
+        reinterpret_cast<int64_t *>(w.lr)[s.tid] = at;
+    }
+    soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+    tc_fence_after();
+    if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int dim = D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
     const bool live = D == 128 || s.lane < 16;
-    const float unit = pow2(vtop - 127);
-    auto total = [&](int c) { return wmax[c] + wmax[R_MAX / 2 + c] + wmax[R_MAX + c] + wmax[R_MAX + R_MAX / 2 + c]; };
-    if (s.tid < ncol) {
-        const float t = total(s.tid);
-        const ColInfo ci = info[s.tid];
-        const float lse2 = t > 0.f ? ci.m + log2f(t) : t == t ? -INFINITY : t;
-        if (!direct) p.part_l[it.part + row0 + s.tid] = lse2;
-        else if (p.lse) p.lse[(int64_t)(ci.row >> 8) * p.n_heads + it.kh * G + (ci.row & 255)] = lse2 * 0.693147180559945f;
-    }
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += 8) {
-        if (c0 < ncol) {
-            float o[16];
-            tmem_ld8(o_at + c0, reinterpret_cast<uint32_t *>(o));
-            tmem_ld8(o_at + CW + c0, reinterpret_cast<uint32_t *>(o) + 8);
+        if (c0 < w.ncol) {
+            float o[8];
+            tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int c = c0 + i;
-                if (c < ncol && live) {
-                    const float t = total(c);
-                    const float v = t > 0.f ? fmaf(o[i + 8], 0.0625f, o[i]) / t * unit : t == t ? 0.f : t;
-                    if (direct) {
-                        const int row = info[c].row;
-                        p.out[(row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * D + dim] = f_to_bf16(v);
-                    } else {
-                        p.part_o[(int64_t)(it.part + row0 + c) * D + dim] = v;
-                    }
+                const ColAM k = w.am[c0 + i];
+                const int64_t at = reinterpret_cast<const int64_t *>(w.lr)[c0 + i] + dim;
+                const float v = o[i] * k.a * k.m;
+                if (c0 + i < w.ncol && live) {
+                    if (direct) p.out[at] = f_to_bf16(v);
+                    else p.part_o[at] = v;
                 }
             }
         }
     }
     tc_fence_before();
-    mbar_arrive_release(o_free + 8 * (n_item & 1));
-    named_sync(nb, WG);  // wmax is free again
+    mbar_arrive_release(s.base + L::O_FREE + 8 * (n_item & 1));
     return true;
 }
 
@@ -486,27 +525,24 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     }
     const int n_items = p.plan[HD_RECS] * KV;
     if ((int)blockIdx.x >= n_items) return;
-    const uint32_t bars = base + L::BARS;
-    const uint32_t kfull = bars, vfull = bars + 8 * L::STAGES, kv_free = bars + 16 * L::STAGES;
-    const uint32_t s_full = bars + 24 * L::STAGES, p_full = s_full + 16, pv_done = s_full + 32, q_full = s_full + 48,
-                   o_free = s_full + 64, q_free = s_full + 80, drain = s_full + 88;
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + L::MISC);
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
         for (int i = 0; i < L::STAGES; ++i) {
-            mbar_init(kfull + 8 * i, 1);
-            mbar_init(vfull + 8 * i, 1);
-            mbar_init(kv_free + 8 * i, 1);
+            mbar_init(base + L::K_FULL + 8 * i, 1);
+            mbar_init(base + L::K_FREE + 8 * i, 1);
+            mbar_init(base + L::V_FULL + 8 * i, 1);
+            mbar_init(base + L::V_FREE + 8 * i, NWG * WG);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(s_full + 8 * i, 1);
-            mbar_init(p_full + 8 * i, 2 * WG);
-            mbar_init(pv_done + 8 * i, 1);
-            mbar_init(o_free + 8 * i, 2 * WG);
-            mbar_init(q_full + 8 * i, 64);
+            mbar_init(base + L::S_FULL + 8 * i, 1);
+            mbar_init(base + L::Q_FULL + 8 * i, 64);
+            mbar_init(base + L::O_FREE + 8 * i, NWG * WG);
         }
-        mbar_init(q_free, 1);
-        mbar_init(drain, 1);
+        mbar_init(base + L::P_FULL, NWG * WG);
+        mbar_init(base + L::PV_DONE, 1);
+        mbar_init(base + L::Q_FREE, 1);
+        mbar_init(base + L::DRAIN, 1);
         *dead = 0;
         mbar_fence_init();
     }
@@ -522,7 +558,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
 
     if (warp == 0) {
         // ------------------------------------------------ loads: a lane per page of a tile
-        uint32_t st = 0, phase = 0, used = 0;
+        uint32_t st = 0, phase = 0, used = 0, k_used = 0;
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
@@ -535,23 +571,27 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 const int n = min(per, ((it.t1 - 1) >> p.kv.page_log2) - first + 1);
                 int page = 0;
                 if (lane < n) page = __ldg(list + first + lane);
-                if (used >= (uint32_t)L::STAGES) ok = wait_bar(kv_free + 8 * st, phase ^ 1, dead);
+                const uint32_t bytes = (uint32_t)n * p.kv.page;
+                const int64_t row = ((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2;
+                const uint32_t at = st * L::SIDE + lane * p.kv.page * D;
+                const uint32_t k_full = base + L::K_FULL + 8 * st, v_full = base + L::V_FULL + 8 * st;
+                if (used >= (uint32_t)L::STAGES) ok = wait_bar(base + L::K_FREE + 8 * st, phase ^ 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t bytes = (uint32_t)n * p.kv.page;
-                if (lane == 0) {
-                    mbar_expect_tx(kfull + 8 * st, bytes * (D + 2));
-                    mbar_expect_tx(vfull + 8 * st, bytes * D);
-                }
+                if (lane == 0) mbar_expect_tx(k_full, bytes * D);
+                __syncwarp();
+                if (lane < n) tma_load_2d(base + L::K + at, &p.kmap, 0, (int)row, k_full);
+                ++k_used;
+                if (used >= (uint32_t)L::STAGES) ok = wait_bar(base + L::V_FREE + 8 * st, phase ^ 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (lane == 0) mbar_expect_tx(v_full, bytes * (D + 2));
                 __syncwarp();
                 if (lane < n) {
-                    const int64_t row = ((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2;
-                    const uint32_t at = base + L::KV + st * 2 * L::SIDE + lane * p.kv.page * D;
                     const uint32_t ex = base + L::EXPS + st * 2 * TT + lane * p.kv.page;
-                    tma_load_2d(at, &p.kmap, 0, (int)row, kfull + 8 * st);
-                    bulk_load(ex, p.kv.k_exp + row, p.kv.page, kfull + 8 * st);
-                    bulk_load(ex + TT, p.kv.v_exp + row, p.kv.page, kfull + 8 * st);
-                    tma_load_2d(at + L::SIDE, &p.vmap, 0, (int)row, vfull + 8 * st);
+                    tma_load_2d(base + L::V + at, &p.vmap, 0, (int)row, v_full);
+                    bulk_load(ex, p.kv.k_exp + row, p.kv.page, v_full);
+                    bulk_load(ex + TT, p.kv.v_exp + row, p.kv.page, v_full);
                 }
                 ++used;
                 if (++st == (uint32_t)L::STAGES) {
@@ -565,85 +605,80 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 *dead = 1;
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
             }
-            const uint32_t n = min(used, (uint32_t)L::STAGES);
-            for (uint32_t i = 0; i < n; ++i) {
-                const uint32_t k = (used - 1 - i) % L::STAGES, ph = ((used - 1 - i) / L::STAGES) & 1;
-                mbar_wait(kfull + 8 * k, ph);
-                mbar_wait(vfull + 8 * k, ph);
+            for (uint32_t i = 0; i < (uint32_t)L::STAGES; ++i) {
+                if (i < k_used) mbar_wait(base + L::K_FULL + 8 * ((k_used - 1 - i) % L::STAGES), ((k_used - 1 - i) / L::STAGES) & 1);
+                if (i < used) mbar_wait(base + L::V_FULL + 8 * ((used - 1 - i) % L::STAGES), ((used - 1 - i) / L::STAGES) & 1);
             }
         }
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issue
         if (lane == 0) {
-            uint32_t g = 0, qk_st = 0, qk_ph = 0, pv_st = 0, pv_ph = 0;
+            uint32_t g = 0, st = 0, ph = 0;
             for (int r = 0; ok; ++r) {
                 const int idx = item_index(r);
                 if (idx >= n_items) break;
                 const Item it = load_item(p, idx, G);
-                const int cw = 8 << (it.flags & 3), R = 2 * cw;
+                const int cw = 8 << (it.flags & 3), R = NWG * cw;
                 const uint32_t q_at = base + L::Q;
-                const uint32_t id_s = idesc_e4m3_f32(128, R, 0), id_o = idesc_e4m3_f32(D, 2 * R, 3);
+                const uint32_t id_s = idesc_e4m3_f32(128, R), id_o = idesc_f16_f32_mn(D, R);
+                const uint64_t qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+                const int pitch = min(2 * R, 128);
+                const uint64_t vd = sdesc_rows(base + L::VH, 128, TT * 128), pd = sdesc_rows(base + L::P, pitch, TT * 128);
                 auto scores = [&](uint32_t n) {
-                    if (!(ok = ok && wait_bar(kfull + 8 * qk_st, qk_ph, dead))) return;
-                    const uint32_t k_at = base + L::KV + qk_st * 2 * L::SIDE;
-                    const uint64_t kd = sdesc_rows(k_at, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+                    if (!(ok = ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead))) return;
+                    const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0);
+                    const uint32_t to = tmem + TM_S + (n & 1) * R_MAX;
 #pragma unroll
-                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(tmem + (n & 1) * 128, kd + 2 * ks, qh + 2 * ks, id_s, ks > 0);
+                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id_s, ks > 0);
 #pragma unroll
-                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(tmem + (n & 1) * 128, kd + 2 * ks, ql + 2 * ks, id_s, 1);
-                    umma_commit(s_full + 8 * (n & 1));
-                    if (++qk_st == (uint32_t)L::STAGES) {
-                        qk_st = 0;
-                        qk_ph ^= 1;
+                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id_s, 1);
+                    umma_commit(base + L::S_FULL + 8 * (n & 1));
+                    umma_commit(base + L::K_FREE + 8 * st);
+                    if (++st == (uint32_t)L::STAGES) {
+                        st = 0;
+                        ph ^= 1;
                     }
                 };
-                if (!(ok = wait_bar(q_full + 8 * (r & 1), (r >> 1) & 1, dead))) break;
+                if (!(ok = wait_bar(base + L::Q_FULL + 8 * (r & 1), (r >> 1) & 1, dead))) break;
                 tc_fence_after();
                 scores(g);
                 for (int j = 0; j < it.tiles && ok; ++j, ++g) {
                     if (j + 1 < it.tiles) scores(g + 1);
-                    else umma_commit(q_free);
-                    const uint32_t b = g & 1;
-                    ok = ok && wait_bar(p_full + 8 * b, (g >> 1) & 1, dead) && wait_bar(vfull + 8 * pv_st, pv_ph, dead);
-                    if (j == 0 && r > 0) ok = ok && wait_bar(o_free + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
+                    else umma_commit(base + L::Q_FREE);
+                    ok = ok && wait_bar(base + L::P_FULL, g & 1, dead);
+                    if (j == 0 && r > 0) ok = ok && wait_bar(base + L::O_FREE + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
                     if (!ok) break;
                     tc_fence_after();
-                    const int pitch = cw == 64 ? 128 : 4 * cw;
-                    const uint64_t vd = sdesc_rows(base + L::KV + pv_st * 2 * L::SIDE + L::SIDE, D, 0);
-                    const uint64_t pd = sdesc_rows(base + L::P + b * L::P_BUF, pitch, TT * 128);
-                    const int steps = min(TT, it.t1 - it.t0 - j * TT + 31) / 32;
+                    const int steps = min(TT, it.t1 - it.t0 - j * TT + 15) / 16;
                     for (int ks = 0; ks < steps; ++ks)
-                        umma_e4m3(tmem + 256, vd + ks * (32 * D / 16), pd + ks * (32 * pitch / 16), id_o, j > 0 || ks > 0);
-                    umma_commit(kv_free + 8 * pv_st);
-                    umma_commit(pv_done + 8 * b);
-                    if (++pv_st == (uint32_t)L::STAGES) {
-                        pv_st = 0;
-                        pv_ph ^= 1;
-                    }
+                        umma_bf16(tmem + TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id_o, j > 0 || ks > 0);
+                    umma_commit(base + L::PV_DONE);
                 }
             }
             if (!ok) {  // the products issued so far end before the CTA does
                 *dead = 1;
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
-                umma_commit(drain);
-                mbar_wait(drain, 0);
+                umma_commit(base + L::DRAIN);
+                mbar_wait(base + L::DRAIN, 0);
             }
         }
         __syncwarp();
     } else if (warp < 4) {
         // ------------------------------------------------ queries: rows scaled by a power of two and split in hi + lo
         const int w = warp - 2;
+        const int g_inv = (65535 + G) / G;  // row / G by a product: rows are below 128, G at most 64
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
             const Item it = load_item(p, idx, G);
-            const int cw = 8 << (it.flags & 3), R = 2 * cw;
+            const int cw = 8 << (it.flags & 3), R = NWG * cw;
             const int32_t *order = p.plan + p.order_at + it.tok;
-            if (r > 0) ok = wait_bar(q_free, (r - 1) & 1, dead);
-            if (r > 1) ok = ok && wait_bar(o_free + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
+            if (r > 0) ok = wait_bar(base + L::Q_FREE, (r - 1) & 1, dead);
+            if (r > 1) ok = ok && wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            ColInfo *info = reinterpret_cast<ColInfo *>(sm + L::INFO) + (r & 1) * R_MAX;
+            ColAM *am = reinterpret_cast<ColAM *>(sm + L::INFO + (r & 1) * R_MAX * 16);
+            ColLR *lr = reinterpret_cast<ColLR *>(sm + L::INFO + (r & 1) * R_MAX * 16 + R_MAX * 8);
             // the largest exponent of the range's values: 16 tokens a lane
             uint32_t top = 0;
             for (int t = it.t0 + (tid - 64) * 16; t < it.t1; t += 64 * 16) {
@@ -661,72 +696,72 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
             top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
             top = __reduce_max_sync(0xffffffffu, top);
             if (lane == 0) reinterpret_cast<volatile int *>(sm + L::MISC + 8)[2 * (r & 1) + w] = (int)top;
-            constexpr int E = D / 32;   // elements a lane
-            constexpr int AT_ONCE = 8;  // rows whose loads are under way together
-            for (int row0 = w; row0 < it.rows; row0 += 2 * AT_ONCE) {
-                uint32_t u[AT_ONCE][2];
-                int tok[AT_ONCE];
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) tok[k] = row0 + 2 * k < it.rows ? __ldg(order + (row0 + 2 * k) / G) : 0;
+            const int per_inv = (65535 + it.per) / it.per;
+            constexpr int LPR = D / 8;           // lanes a row, eight elements each
+            constexpr int RPW = 32 / LPR;        // rows a warp deals with at a time
+            constexpr int AT_ONCE = 4;           // loads of a lane under way together
+            const int part = lane % LPR;
+            for (int row0 = w * RPW + lane / LPR; row0 < it.rows + lane / LPR; row0 += 2 * RPW * AT_ONCE) {
+                uint4 u[AT_ONCE];
+                int id[AT_ONCE];
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * k;
-                    u[k][0] = u[k][1] = 0;
-                    if (row < it.rows) {
-                        const uint16_t *src = p.q + tok[k] * p.q_stride + (it.kh * G + row % G) * D + lane * E;
-                        if constexpr (E == 4) {
-                            const uint2 v = __ldg(reinterpret_cast<const uint2 *>(src));
-                            u[k][0] = v.x;
-                            u[k][1] = v.y;
-                        } else {
-                            u[k][0] = __ldg(reinterpret_cast<const uint32_t *>(src));
-                        }
-                    }
+                    const int row = row0 + 2 * RPW * k, i = row * g_inv >> 16;
+                    id[k] = 0;
+                    if (row < it.rows) id[k] = (((it.flags & RF_CAUSAL) ? it.tok + i : __ldg(order + i)) << 8) | (row - i * G);
                 }
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * k;
-                    if (row >= it.rows) break;
-                    uint32_t a = max(max((u[k][0] << 16) & 0x7fffffffu, u[k][0] & 0x7fff0000u),
-                                     max((u[k][1] << 16) & 0x7fffffffu, u[k][1] & 0x7fff0000u));
-                    a = __reduce_max_sync(0xffffffffu, a);
+                    const int row = row0 + 2 * RPW * k;
+                    u[k] = make_uint4(0, 0, 0, 0);
+                    if (row < it.rows)
+                        u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * D + part * 8));
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int row = row0 + 2 * RPW * k;
+                    const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+                    uint32_t a = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) a = max(a, max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
+#pragma unroll
+                    for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
                     // the row's largest element to [2^7, 2^8)
                     const int qe = max((int)(a >> 23) - 127 - 7, -120);
                     const bool bad = (a >> 23) == 255;
-                    const float inv = __uint_as_float((uint32_t)(127 - qe) << 23);
-                    uint32_t hi = 0, lo = 0;
+                    const float inv = pow2(-qe);
+                    uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
 #pragma unroll
-                    for (int e = 0; e < E / 2; ++e) {
-                        const float v0 = __uint_as_float(u[k][e] << 16) * inv, v1 = __uint_as_float(u[k][e] & 0xffff0000u) * inv;
+                    for (int e = 0; e < 4; ++e) {
+                        const float v0 = __uint_as_float(x[e] << 16) * inv, v1 = __uint_as_float(x[e] & 0xffff0000u) * inv;
                         const uint16_t h = e4m3x2(v0, v1);
-                        const float2 hf = __half22float2(half2_of_e4m3x2(h));
-                        hi |= (uint32_t)h << (16 * e);
-                        lo |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * e);
+                        const uint32_t back = f16x2_of_e4m3x2(h);
+                        const float2 hf = __half22float2(*reinterpret_cast<const __half2 *>(&back));
+                        hi[e / 2] |= (uint32_t)h << (16 * (e & 1));
+                        lo[e / 2] |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * (e & 1));
                     }
-                    if (bad) hi = lo = 0x7f7f7f7fu;
-                    const int col = row < it.half ? row : cw + row - it.half;
-                    const uint32_t at = base + L::Q + swz_rows<D>(col * D + lane * E);
-                    const uint32_t at_lo = base + L::Q + swz_rows<D>((R + col) * D + lane * E);
-                    if constexpr (E == 4) {
-                        sts32(at, hi);
-                        sts32(at_lo, lo);
-                    } else {
-                        sts16(at, (uint16_t)hi);
-                        sts16(at_lo, (uint16_t)lo);
-                    }
-                    if (lane == 0) {
-                        const int i = row / G;
-                        ColInfo c;
-                        c.a = bad ? 1.f : __uint_as_float((uint32_t)(127 + qe) << 23) * p.scale_log2;
-                        c.m = M_NONE;
-                        c.lim = it.lim + ((it.flags & RF_CAUSAL) ? i : 0);
-                        c.row = (tok[k] << 8) | (row - i * G);
-                        info[col] = c;
+                    if (bad) hi[0] = hi[1] = lo[0] = lo[1] = 0x7f7f7f7fu;
+                    if (row < it.rows) {
+                        const int wg = row * per_inv >> 16, col = wg * cw + row - wg * it.per;
+                        sts64(base + L::Q + swz_rows<D>(col * D + part * 8), hi[0], hi[1]);
+                        sts64(base + L::Q + swz_rows<D>((R + col) * D + part * 8), lo[0], lo[1]);
+                        if (part == 0) {
+                            am[col] = ColAM{bad ? 1.f : pow2(qe) * p.scale_log2, M_NONE};
+                            lr[col] = ColLR{it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]};
+                        }
                     }
                 }
             }
+            // columns that fill up a warpgroup's last eight: they take part, unused
+            for (int g = w; g < NWG; g += 2) {
+                const int ncol = min(max(it.rows - g * it.per, 0), it.per);
+                if (ncol + lane < ((ncol + 7) & ~7)) {
+                    am[g * cw + ncol + lane] = ColAM{0.f, 0.f};
+                    lr[g * cw + ncol + lane] = ColLR{0x7fffffff, 0};
+                }
+            }
             fence_async_smem();
-            mbar_arrive_release(q_full + 8 * (r & 1));
+            mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
         }
         if (!ok && lane == 0) {
             *dead = 1;
@@ -739,7 +774,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         s.base = base;
         s.tmem = tmem;
         s.dead = dead;
-        s.wg = warp >= 8;
+        s.wg = (warp - 4) >> 2;
         s.tid = tid & (WG - 1);
         s.lane = lane;
         s.quarter = warp & 3;
@@ -750,12 +785,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
             if (idx >= n_items) break;
             const Item it = load_item(p, idx, G);
             // (the columns' constants are there before the first scores are)
-            soft_wait(s, q_full + 8 * (r & 1), (r >> 1) & 1);
+            soft_wait(s, base + L::Q_FULL + 8 * (r & 1), (r >> 1) & 1);
             switch (it.flags & 3) {
             case 0: ok = soft_item<D, 8>(p, s, it, r); break;
             case 1: ok = soft_item<D, 16>(p, s, it, r); break;
-            case 2: ok = soft_item<D, 32>(p, s, it, r); break;
-            default: ok = soft_item<D, 64>(p, s, it, r); break;
+            default: ok = soft_item<D, 32>(p, s, it, r); break;
             }
         }
         if (!ok && s.tid == 0) {
@@ -925,7 +959,7 @@ struct RowTile {
 
 // The time of an item in units of 128-token tiles of the smallest class, from
 // measurements of single items: a tile of each class, and what an item takes besides.
-constexpr float TILE_COST[4] = {1.f, 1.1f, 1.6f, 2.8f};
+constexpr float TILE_COST[3] = {1.f, 1.2f, 1.8f};
 constexpr float ITEM_COST = 2.f;
 
 // Plans a checked batch into the tables at w; returns the words used.
@@ -944,8 +978,8 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     const bool grouped = b->group && b->n_groups > 0;
     auto prompt = [&](int i) { return grouped && b->group[i] >= 0 ? b->group_len[b->group[i]] : 0; };
     auto class_of = [&](int ntok) {
-        const int half = (ntok * G + 1) / 2;
-        return half <= 8 ? 0 : half <= 16 ? 1 : half <= 32 ? 2 : 3;
+        const int cw = (ntok * G + NWG - 1) / NWG;
+        return cw <= 8 ? 0 : cw <= 16 ? 1 : 2;
     };
     std::vector<RowTile> tiles;
     // own tokens: `per` query tokens of a request at a time

@@ -308,14 +308,17 @@ __device__ __forceinline__ void umma_commit_cg(uint32_t bar)
 }
 
 // ---------------------------------------------------------------- 8-bit operands
-// kind::f8f6f4, e4m3 x e4m3 -> fp32; a set bit of `mn` (1: A, 2: B) makes that
-// operand MN-major.  One MMA is 32 deep.
-__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N, uint32_t mn)
+// kind::f8f6f4, e4m3 x e4m3 -> fp32, both operands K-major.  One MMA is 32 deep.
+__host__ __device__ constexpr uint32_t idesc_e4m3_f32(int M, int N)
 {
     return (1u << 4)                     // D format: f32 (A and B formats 0: e4m3)
-           | (mn << 15)                  // transposed operands
            | ((uint32_t)(N >> 3) << 17)  // N / 8
            | ((uint32_t)(M >> 4) << 24); // M / 16
+}
+// kind::f16, f16 x f16 -> fp32, both operands MN-major
+__host__ __device__ constexpr uint32_t idesc_f16_f32_mn(int M, int N)
+{
+    return (1u << 4) | (3u << 15) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // Descriptor of an operand whose rows (K-major: one row's K; MN-major: one K
 // index's MN extent) are `pitch` = 32, 64 or 128 bytes, swizzled as wide as they
