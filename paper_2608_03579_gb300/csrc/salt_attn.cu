@@ -83,43 +83,43 @@ __global__ void plan_copy_kernel(const uint4 *src, uint4 *dst, int n)
 // ---------------------------------------------------------------- shared memory
 template <int D>
 struct Layout {
-    static constexpr int STAGES = D == 128 ? 3 : 6;       // of K and of V
+    static constexpr int KST = D == 128 ? 3 : 6;          // stages of K and of V
+    static constexpr int VST = D == 128 ? 2 : 4;
     static constexpr uint32_t SIDE = TT * D;              // codes of K or V of a tile
     static constexpr uint32_t K = 0;
-    static constexpr uint32_t V = K + STAGES * SIDE;
-    static constexpr uint32_t VH = V + STAGES * SIDE;     // V of a tile in f16
+    static constexpr uint32_t V = K + KST * SIDE;
+    static constexpr uint32_t VH = V + VST * SIDE;        // V of a tile in f16
     static constexpr uint32_t P = VH + 2 * SIDE;          // P of a tile in f16
-    static constexpr uint32_t Q = P + TT * 2 * R_MAX;
-    static constexpr uint32_t EXPS = Q + 2 * R_MAX * D;   // per stage of V: 128 of K, 128 of V
-    static constexpr uint32_t INFO = EXPS + STAGES * 2 * TT;
-    static constexpr uint32_t FAC = INFO + 2 * R_MAX * 16;  // (INFO: per item ColAM[R_MAX], ColLR[R_MAX])
+    static constexpr uint32_t Q_BUF = 2 * R_MAX * D;
+    static constexpr uint32_t Q = P + TT * 2 * R_MAX;     // two items' queries
+    static constexpr uint32_t EXPS = Q + 2 * Q_BUF;       // per stage of V: 128 of K, 128 of V
+    static constexpr uint32_t INFO = EXPS + VST * 2 * TT;  // two items' constants of the columns, see IN_*
+    static constexpr uint32_t INFO_BUF = R_MAX * 16;
+    static constexpr uint32_t FAC = INFO + 2 * INFO_BUF;
     static constexpr uint32_t WMAX = FAC + R_MAX * 4;     // [NWG][4][CW_MAX] floats
-    // barriers: K full, K free, V full, V free (a stage each), scores full [2], P full, product done, Q full [2], item
-    // done [2], Q free, drain
+    // barriers: K full, K free, V full, V free (a stage each), scores full [2], P full, product done, Q full [2], Q free
+    // [2], item done [2], drain
     static constexpr uint32_t K_FULL = WMAX + 4 * R_MAX * 4;
-    static constexpr uint32_t K_FREE = K_FULL + 8 * STAGES;
-    static constexpr uint32_t V_FULL = K_FREE + 8 * STAGES;
-    static constexpr uint32_t V_FREE = V_FULL + 8 * STAGES;
-    static constexpr uint32_t S_FULL = V_FREE + 8 * STAGES;
+    static constexpr uint32_t K_FREE = K_FULL + 8 * KST;
+    static constexpr uint32_t V_FULL = K_FREE + 8 * KST;
+    static constexpr uint32_t V_FREE = V_FULL + 8 * VST;
+    static constexpr uint32_t S_FULL = V_FREE + 8 * VST;
     static constexpr uint32_t P_FULL = S_FULL + 16;
     static constexpr uint32_t PV_DONE = P_FULL + 8;
     static constexpr uint32_t Q_FULL = PV_DONE + 8;
     static constexpr uint32_t O_FREE = Q_FULL + 16;
     static constexpr uint32_t Q_FREE = O_FREE + 16;
-    static constexpr uint32_t DRAIN = Q_FREE + 8;
+    static constexpr uint32_t DRAIN = Q_FREE + 16;
     static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents
     static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
 };
 constexpr uint32_t TM_S = 0, TM_O = 256;  // tensor memory columns: two buffers of R_MAX scores, the output
 
-// A column's constants: the factor of its scores (query row's power of two, scale,
-// log2 e) and the reference m; the tokens it sees and (query token << 8 | head in the group).
-struct ColAM {
-    float a, m;
-};
-struct ColLR {
-    int32_t lim, row;
-};
+// A column's constants, arrays of R_MAX words: the factor a of its scores (query row's
+// power of two, scale, log2 e), its reference -m, the tokens it sees and (query
+// token << 8 | head in the group).  In the end a and -m make way for the
+// factor of its output, the other two for the place of its row.
+constexpr uint32_t IN_A = 0, IN_M = R_MAX * 4, IN_LIM = R_MAX * 8, IN_ROW = R_MAX * 12;
 
 __device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
 {
@@ -144,7 +144,10 @@ __device__ __forceinline__ float pow2(int k) { return __uint_as_float(k < -126 ?
 // 2^(e - 127) of an exponent byte; 0 for a row of zeros, NaN for a row that stands for NaN
 __device__ __forceinline__ float row_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
 
-__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(a), "r"(x), "r"(y) : "memory"); }
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y)
+{
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(a), "r"(x), "r"(y) : "memory");
+}
 __device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
@@ -155,6 +158,59 @@ __device__ __forceinline__ uint4 lds128(uint32_t a)
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
     return v;
+}
+
+__device__ __forceinline__ float4 lds4f(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ldsf(uint32_t a)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void stsf(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(a), "f"(v) : "memory"); }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
+
+// two floats at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
 }
 
 struct Item {
@@ -227,7 +283,6 @@ __device__ __forceinline__ float reduce_columns(float *t, int lane, int &col, Op
 
 // What the softmax warpgroups share across their functions.
 struct Soft {
-    uint8_t *sm;
     uint32_t base, tmem;
     volatile int *dead;
     int wg, tid, lane, quarter;
@@ -246,11 +301,9 @@ __device__ __forceinline__ void soft_wait(Soft &s, uint32_t bar, uint32_t parity
 
 // Addresses and constants of an item for a softmax warpgroup.
 struct SoftItem {
-    ColAM *am;
-    ColLR *lr;
-    float *fac, *wmax;
+    uint32_t info, fac, wmax;      // shared memory: constants of the warpgroup's columns (IN_*), scratch
     int ncol, vtop, nb, j;
-    uint32_t lanes, o_at;
+    uint32_t lanes, o_at;          // tensor memory
 };
 
 // Scores of CH columns (from column c0 of the warpgroup) less their references, in log2;
@@ -264,120 +317,155 @@ __device__ __forceinline__ float soft_args(float (&x)[CH], const SoftItem &w, ui
         if (c0 + c < w.ncol) tmem_ld8(s_at + c0 + c, reinterpret_cast<uint32_t *>(x) + c);
     tmem_ld_wait();
     float mx = -INFINITY;
+    const float2 kf2 = make_float2(kf, kf);
 #pragma unroll
     for (int c = 0; c < CH; c += 8) {
         if (c0 + c < w.ncol) {
 #pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                const float4 k = *reinterpret_cast<const float4 *>(w.am + c0 + c + i);
-                x[c + i] = fmaf(x[c + i], kf * k.x, -k.y);
-                x[c + i + 1] = fmaf(x[c + i + 1], kf * k.z, -k.w);
+            for (int i = c; i < c + 8; i += 4) {
+                const float4 a = lds4f(w.info + IN_A + 4 * (c0 + i)), m = lds4f(w.info + IN_M + 4 * (c0 + i));
+                const float2 u = fma2(make_float2(x[i], x[i + 1]), mul2(make_float2(a.x, a.y), kf2), make_float2(m.x, m.y));
+                const float2 v = fma2(make_float2(x[i + 2], x[i + 3]), mul2(make_float2(a.z, a.w), kf2), make_float2(m.z, m.w));
+                x[i] = u.x;
+                x[i + 1] = u.y;
+                x[i + 2] = v.x;
+                x[i + 3] = v.y;
                 if (MASK) {
-                    const int4 v = *reinterpret_cast<const int4 *>(w.lr + c0 + c + i);
-                    if (tok >= v.x) x[c + i] = -INFINITY;
-                    if (tok >= v.z) x[c + i + 1] = -INFINITY;
+                    const uint4 n = lds128(w.info + IN_LIM + 4 * (c0 + i));
+                    if (tok >= (int)n.x) x[i] = -INFINITY;
+                    if (tok >= (int)n.y) x[i + 1] = -INFINITY;
+                    if (tok >= (int)n.z) x[i + 2] = -INFINITY;
+                    if (tok >= (int)n.w) x[i + 3] = -INFINITY;
                 }
-                mx = fmaxf(mx, fmaxf(x[c + i], x[c + i + 1]));
+                mx = fmaxf(fmaxf(mx, fmaxf(x[i], x[i + 1])), fmaxf(x[i + 2], x[i + 3]));
             }
         }
     }
     return mx;
 }
 
-// A tile of an item of the class with CW columns a warpgroup.  False: gave up
-// (the whole warpgroup together).
+// A token's part of a tile: factors of its scores and of its probabilities, and what
+// P is to p in log2, held so that p stays in range (a value 2^100 below the
+// largest may lose bits).
+struct Token {
+    int at;
+    float kf, vf, vref;
+};
+
+// P of a tile into shared memory, the probabilities to the sums l.  Returns
+// the largest log2 P of the token.  References that lie too low may make P and
+// l infinite: move_refs then mends both.
 template <int D, int CW, bool MASK>
-__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float (&l)[CW], int tok, uint32_t ke, uint32_t ve)
+__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
 {
     using L = Layout<D>;
     constexpr int CH = CW < 16 ? CW : 16;    // columns in registers at a time
     constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
-    const float kf = row_scale(ke), vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - w.vtop);
-    // what P is to p in log2, held so that p stays in range (a value 2^100 below the largest may lose bits)
-    const float vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
-    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
-    uint32_t ph[CW / 2];
+    const uint32_t p_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128);
+    const uint32_t row_at = s.tid * PITCH + s.wg * 2 * CW % 128;
+    float mx = -INFINITY;
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += CH) {
         if (c0 >= w.ncol) break;
         float x[CH];
-        float mx = soft_args<CH, MASK>(x, w, s_at, c0, kf, tok) + vref;
-        if (!named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST))) {
-            // some row's reference has to move
-            if (!named_sync_and(w.nb, WG, s.ok)) return false;
-            int col;
+        mx = fmaxf(mx, soft_args<CH, MASK>(x, w, s_at, c0, t.kf, t.at));
+        uint32_t h[CH / 2];
 #pragma unroll
-            for (int c = 0; c < CH; c += 8)  // m + (s - m) is not s: take the scores anew
-                if (c0 + c < w.ncol) tmem_ld8(s_at + c0 + c, reinterpret_cast<uint32_t *>(x) + c);
-            tmem_ld_wait();
+        for (int c = 0; c < CH; c += 2) {
+            const float2 e = make_float2(ex2(x[c]), ex2(x[c + 1]));
+            float2 v = mul2(e, make_float2(t.vf, t.vf));
+            l[(c0 + c) / 2] = add2(l[(c0 + c) / 2], e);
+            if (MASK) {  // not 0 * NaN
+                if (x[c] == -INFINITY) v.x = 0.f;
+                if (x[c + 1] == -INFINITY) v.y = 0.f;
+            }
+            const __half2 p = __floats2half2_rn(v.x, v.y);
+            h[c / 2] = *reinterpret_cast<const uint32_t *>(&p);
+        }
+        // P takes the place of the last tile's once its product is done
+        if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+#pragma unroll
+        for (int c = 0; c < CH; c += 8)
+            sts128(p_at + swz_rows<PITCH>(row_at + 2 * (c0 + c)), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+    }
+    return mx + t.vref;
+}
+
+// Moves the references that a score of this tile passes by too much (all of
+// them where there is none yet), and with them what the output and the
+// sums hold already; after an item's first tile the sums hold this tile's
+// probabilities too, which are taken out again.  The whole warpgroup; needs the product
+// before this tile's to be done.
+template <int CW>
+__device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
+{
+    constexpr int CH = 8;
+#pragma unroll
+    for (int c0 = 0; c0 < CW; c0 += CH) {
+        if (c0 >= w.ncol) break;
+        float x[CH];
+        tmem_ld8(s_at + c0, reinterpret_cast<uint32_t *>(x));
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            x[c] = fmaf(x[c], t.kf * ldsf(w.info + IN_A + 4 * (c0 + c)), t.vref);
+            if (t.at >= (int)lds32(w.info + IN_LIM + 4 * (c0 + c)) || !(x[c] == x[c])) x[c] = -INFINITY;
+        }
+        int col;
+        const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
+        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), v);
+    }
+    named_sync(w.nb, WG);
+    if (s.tid < w.ncol) {
+        float v = ldsf(w.wmax + 4 * s.tid);
+        for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * CW_MAX + s.tid)));
+        const uint32_t nm = w.info + IN_M + 4 * s.tid;
+        const float m = -ldsf(nm);
+        const bool move = v - m > P_MOST;
+        stsf(w.fac + 4 * s.tid, move ? v - P_TOP - m : 0.f);
+        if (move) stsf(nm, P_TOP - v);
+    }
+    named_sync(w.nb, WG);
+    if (w.j > 0) {
+#pragma unroll
+        for (int c0 = 0; c0 < CW; c0 += CH) {
+            if (c0 >= w.ncol) break;
+            float o[CH], x[CH];
+            tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
+            soft_args<CH, true>(x, w, s_at, c0, t.kf, t.at);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
-                const ColAM k = w.am[c0 + c];
-                x[c] = fmaf(x[c], kf * k.a, vref);
-                if ((MASK && tok >= w.lr[c0 + c].lim) || !(x[c] == x[c]) || c0 + c >= w.ncol) x[c] = -INFINITY;
+                const float up = c0 + c < w.ncol ? ldsf(w.fac + 4 * (c0 + c)) : 0.f, f = ex2(-up);
+                o[c] *= f;
+                // (next to a probability that went out of range the sum was nothing)
+                float &lc = c & 1 ? l[(c0 + c) / 2].y : l[(c0 + c) / 2].x;
+                lc = x[c] + up > 100.f ? 0.f : lc * f - ex2(x[c]);
             }
-            const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
-            w.wmax[s.quarter * CW_MAX + col] = v;
-            named_sync(w.nb, WG);
-            if (s.tid < CH) {
-                float t = w.wmax[s.tid];
-                for (int q = 1; q < 4; ++q) t = fmaxf(t, w.wmax[q * CW_MAX + s.tid]);
-                const float m = w.am[c0 + s.tid].m;
-                const bool move = t - m > P_MOST && c0 + s.tid < w.ncol;
-                w.fac[s.tid] = move ? ex2(m - (t - P_TOP)) : 1.f;
-                if (move) w.am[c0 + s.tid].m = t - P_TOP;
-            }
-            named_sync(w.nb, WG);
-            if (w.j > 0) {
-                soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-                tc_fence_after();
-#pragma unroll
-                for (int c = 0; c < CH; c += 8) {
-                    if (c0 + c < w.ncol) {
-                        float o[8];
-                        tmem_ld8(w.o_at + c0 + c, reinterpret_cast<uint32_t *>(o));
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float f = w.fac[c + i];
-                            o[i] *= f;
-                            l[c0 + c + i] *= f;
-                        }
-                        tmem_st8(w.o_at + c0 + c, reinterpret_cast<const uint32_t *>(o));
-                    }
-                }
-                tmem_st_wait();
-            }
-            soft_args<CH, MASK>(x, w, s_at, c0, kf, tok);
-            named_sync(w.nb, WG);  // fac and wmax are free again
+            tmem_st8(w.o_at + c0, reinterpret_cast<const uint32_t *>(o));
         }
-#pragma unroll
-        for (int c = 0; c < CH; c += 8) {
-            if (c0 + c < w.ncol) {
-#pragma unroll
-                for (int i = c; i < c + 8; i += 2) {
-                    const float e0 = ex2(x[i]), e1 = ex2(x[i + 1]);
-                    float v0 = e0 * vf, v1 = e1 * vf;
-                    l[c0 + i] += e0;
-                    l[c0 + i + 1] += e1;
-                    if (MASK) {  // not 0 * NaN
-                        if (x[i] == -INFINITY) v0 = 0.f;
-                        if (x[i + 1] == -INFINITY) v1 = 0.f;
-                    }
-                    const __half2 h = __floats2half2_rn(v0, v1);
-                    ph[(c0 + i) / 2] = *reinterpret_cast<const uint32_t *>(&h);
-                }
-            }
-        }
+        tmem_st_wait();
     }
-    // P and the widened V take the place of the last tile's once its product is done
-    if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-    const uint32_t p_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128);
-    const uint32_t row_at = s.tid * PITCH + s.wg * 2 * CW % 128;
-#pragma unroll
-    for (int c = 0; c < CW; c += 8)
-        if (c < w.ncol) sts128(p_at + swz_rows<PITCH>(row_at + 2 * c), ph[c / 2], ph[c / 2 + 1], ph[c / 2 + 2], ph[c / 2 + 3]);
-    return true;
+}
+
+// A tile of an item of the class with CW columns a warpgroup.  False: gave up
+// (the whole warpgroup together).
+template <int D, int CW>
+__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, bool mask)
+{
+    using L = Layout<D>;
+    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
+    if (w.ncol == 0) {
+        if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+        return true;
+    }
+    // (a second time the references fit, but for scores so large that fp32 rounds them by more than P_MOST)
+    for (int round = 0;; ++round) {
+        if (round > 0 || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
+        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at) : soft_probs<D, CW, false>(s, w, l, t, s_at);
+        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && round == 0))) return true;
+        if (!named_sync_and(w.nb, WG, s.ok)) return false;
+        tc_fence_after();
+    }
 }
 
 // The warpgroups' share of a tile's values in f16; zeros from row `valid` on
@@ -419,38 +507,41 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     using L = Layout<D>;
     constexpr int CH = CW < 16 ? CW : 16;
     SoftItem w;
-    w.am = reinterpret_cast<ColAM *>(s.sm + L::INFO + (n_item & 1) * R_MAX * 16) + s.wg * CW;
-    w.lr = reinterpret_cast<ColLR *>(s.sm + L::INFO + (n_item & 1) * R_MAX * 16 + R_MAX * 8) + s.wg * CW;
-    w.fac = reinterpret_cast<float *>(s.sm + L::FAC) + s.wg * CW_MAX;
-    w.wmax = reinterpret_cast<float *>(s.sm + L::WMAX) + s.wg * 4 * CW_MAX;
+    w.info = s.base + L::INFO + (n_item & 1) * L::INFO_BUF + s.wg * CW * 4;
+    w.fac = s.base + L::FAC + s.wg * CW_MAX * 4;
+    w.wmax = s.base + L::WMAX + s.wg * 4 * CW_MAX * 4;
     w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
     w.lanes = (uint32_t)(s.quarter * 32) << 16;
     w.o_at = s.tmem + w.lanes + TM_O + s.wg * CW;
     w.nb = 1 + s.wg;
     // values count in units of the largest exponent of the range
-    const volatile int *vt = reinterpret_cast<const volatile int *>(s.sm + L::MISC + 8) + 2 * (n_item & 1);
-    w.vtop = max(vt[0], vt[1]) > 0 ? max(vt[0], vt[1]) : 127;
-    float l[CW];
+    w.vtop = max((int)lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), (int)lds32(s.base + L::MISC + 12 + 8 * (n_item & 1)));
+    if (w.vtop == 0) w.vtop = 127;
+    float2 l[CW / 2];
 #pragma unroll
-    for (int c = 0; c < CW; ++c) l[c] = 0.f;
+    for (int c = 0; c < CW / 2; ++c) l[c] = make_float2(0.f, 0.f);
     for (w.j = 0; w.j < it.tiles; ++w.j) {
         const int tok = it.t0 + w.j * TT + s.tid;
         const int end = it.t0 + (w.j + 1) * TT;
         soft_wait(s, s.base + L::V_FULL + 8 * s.stage, s.stage_phase);
         soft_wait(s, s.base + L::S_FULL + 8 * (s.g & 1), (s.g >> 1) & 1);
         tc_fence_after();
-        const uint32_t ke = s.sm[L::EXPS + s.stage * 2 * TT + s.tid], ve = s.sm[L::EXPS + s.stage * 2 * TT + TT + s.tid];
+        const uint32_t ex = s.base + L::EXPS + s.stage * 2 * TT + s.tid;
+        const uint32_t ke = lds8(ex), ve = lds8(ex + TT);
+        Token t;
+        t.at = tok;
+        t.kf = row_scale(ke);
+        t.vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - w.vtop);
+        t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
         // column masks only where a row does not see the whole tile (the first query token sees least)
-        const bool go = end > min(it.t1, it.lim) ? soft_tile<D, CW, true>(s, w, l, tok, ke, ve)
-                                                 : soft_tile<D, CW, false>(s, w, l, tok, ke, ve);
-        if (!go) return false;
+        if (!soft_tile<D, CW>(s, w, l, t, end > min(it.t1, it.lim))) return false;
         widen_values<D>(s, it.t1 - (end - TT));
         tc_fence_before();
         fence_async_smem();
         mbar_arrive_release(s.base + L::P_FULL);
         mbar_arrive_release(s.base + L::V_FREE + 8 * s.stage);
         ++s.g;
-        if (++s.stage == L::STAGES) {
+        if (++s.stage == L::VST) {
             s.stage = 0;
             s.stage_phase ^= 1;
         }
@@ -459,16 +550,20 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += CH) {
         int col;
-        const float t = reduce_columns<CH>(l + c0, s.lane, col, [](float p, float q) { return p + q; });
-        w.wmax[s.quarter * CW_MAX + c0 + col] = t;
+        float v[CH];
+#pragma unroll
+        for (int c = 0; c < CH; ++c) v[c] = c & 1 ? l[(c0 + c) / 2].y : l[(c0 + c) / 2].x;
+        const float t = reduce_columns<CH>(v, s.lane, col, [](float p, float q) { return p + q; });
+        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), t);
     }
     if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int G = p.n_heads / p.kv.heads;
     const bool direct = it.flags & RF_DIRECT;
     if (s.tid < w.ncol) {
-        const float t = w.wmax[s.tid] + w.wmax[CW_MAX + s.tid] + w.wmax[2 * CW_MAX + s.tid] + w.wmax[3 * CW_MAX + s.tid];
-        const int row = w.lr[s.tid].row;
-        const float lse2 = t > 0.f ? w.am[s.tid].m + log2f(t) : t == t ? -INFINITY : t;
+        const uint32_t at_w = w.wmax + 4 * s.tid, at_i = w.info + 4 * s.tid;
+        const float t = (ldsf(at_w) + ldsf(at_w + 4 * CW_MAX)) + (ldsf(at_w + 8 * CW_MAX) + ldsf(at_w + 12 * CW_MAX));
+        const int row = (int)lds32(at_i + IN_ROW);
+        const float lse2 = t > 0.f ? log2f(t) - ldsf(at_i + IN_M) : t == t ? -INFINITY : t;
         int64_t at;  // the row's first element
         if (direct) {
             at = (row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * D;
@@ -478,15 +573,16 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
             at = (int64_t)part * D;
             p.part_l[part] = lse2;
         }
-        // the column's constants make way for its factors and its place
-        w.am[s.tid] = ColAM{t > 0.f ? 1.f / t : t == t ? 0.f : t, pow2(w.vtop - 127)};
-        reinterpret_cast<int64_t *>(w.lr)[s.tid] = at;
+        stsf(at_i + IN_A, t > 0.f ? 1.f / t : t == t ? 0.f : t);
+        sts32(at_i + IN_LIM, (uint32_t)at);
+        sts32(at_i + IN_ROW, (uint32_t)(at >> 32));
     }
     soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
     tc_fence_after();
     if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int dim = D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
     const bool live = D == 128 || s.lane < 16;
+    const float unit = pow2(w.vtop - 127);
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += 8) {
         if (c0 < w.ncol) {
@@ -495,9 +591,9 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const ColAM k = w.am[c0 + i];
-                const int64_t at = reinterpret_cast<const int64_t *>(w.lr)[c0 + i] + dim;
-                const float v = o[i] * k.a * k.m;
+                const uint32_t at_i = w.info + 4 * (c0 + i);
+                const int64_t at = (int64_t)((uint64_t)lds32(at_i + IN_ROW) << 32 | lds32(at_i + IN_LIM)) + dim;
+                const float v = o[i] * ldsf(at_i + IN_A) * unit;
                 if (c0 + i < w.ncol && live) {
                     if (direct) p.out[at] = f_to_bf16(v);
                     else p.part_o[at] = v;
@@ -528,20 +624,22 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + L::MISC);
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
-        for (int i = 0; i < L::STAGES; ++i) {
+        for (int i = 0; i < L::KST; ++i) {
             mbar_init(base + L::K_FULL + 8 * i, 1);
             mbar_init(base + L::K_FREE + 8 * i, 1);
+        }
+        for (int i = 0; i < L::VST; ++i) {
             mbar_init(base + L::V_FULL + 8 * i, 1);
             mbar_init(base + L::V_FREE + 8 * i, NWG * WG);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(base + L::S_FULL + 8 * i, 1);
             mbar_init(base + L::Q_FULL + 8 * i, 64);
+            mbar_init(base + L::Q_FREE + 8 * i, 1);
             mbar_init(base + L::O_FREE + 8 * i, NWG * WG);
         }
         mbar_init(base + L::P_FULL, NWG * WG);
         mbar_init(base + L::PV_DONE, 1);
-        mbar_init(base + L::Q_FREE, 1);
         mbar_init(base + L::DRAIN, 1);
         *dead = 0;
         mbar_fence_init();
@@ -558,7 +656,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
 
     if (warp == 0) {
         // ------------------------------------------------ loads: a lane per page of a tile
-        uint32_t st = 0, phase = 0, used = 0, k_used = 0;
+        uint32_t ks = 0, kph = 0, vs = 0, vph = 0, k_used = 0, v_used = 0;
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
@@ -573,30 +671,34 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 if (lane < n) page = __ldg(list + first + lane);
                 const uint32_t bytes = (uint32_t)n * p.kv.page;
                 const int64_t row = ((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2;
-                const uint32_t at = st * L::SIDE + lane * p.kv.page * D;
-                const uint32_t k_full = base + L::K_FULL + 8 * st, v_full = base + L::V_FULL + 8 * st;
-                if (used >= (uint32_t)L::STAGES) ok = wait_bar(base + L::K_FREE + 8 * st, phase ^ 1, dead);
+                const uint32_t at = lane * p.kv.page * D;
+                const uint32_t k_full = base + L::K_FULL + 8 * ks, v_full = base + L::V_FULL + 8 * vs;
+                if (k_used >= (uint32_t)L::KST) ok = wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (lane == 0) mbar_expect_tx(k_full, bytes * D);
                 __syncwarp();
-                if (lane < n) tma_load_2d(base + L::K + at, &p.kmap, 0, (int)row, k_full);
+                if (lane < n) tma_load_2d(base + L::K + ks * L::SIDE + at, &p.kmap, 0, (int)row, k_full);
                 ++k_used;
-                if (used >= (uint32_t)L::STAGES) ok = wait_bar(base + L::V_FREE + 8 * st, phase ^ 1, dead);
+                if (++ks == (uint32_t)L::KST) {
+                    ks = 0;
+                    kph ^= 1;
+                }
+                if (v_used >= (uint32_t)L::VST) ok = wait_bar(base + L::V_FREE + 8 * vs, vph ^ 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (lane == 0) mbar_expect_tx(v_full, bytes * (D + 2));
                 __syncwarp();
                 if (lane < n) {
-                    const uint32_t ex = base + L::EXPS + st * 2 * TT + lane * p.kv.page;
-                    tma_load_2d(base + L::V + at, &p.vmap, 0, (int)row, v_full);
+                    const uint32_t ex = base + L::EXPS + vs * 2 * TT + lane * p.kv.page;
+                    tma_load_2d(base + L::V + vs * L::SIDE + at, &p.vmap, 0, (int)row, v_full);
                     bulk_load(ex, p.kv.k_exp + row, p.kv.page, v_full);
                     bulk_load(ex + TT, p.kv.v_exp + row, p.kv.page, v_full);
                 }
-                ++used;
-                if (++st == (uint32_t)L::STAGES) {
-                    st = 0;
-                    phase ^= 1;
+                ++v_used;
+                if (++vs == (uint32_t)L::VST) {
+                    vs = 0;
+                    vph ^= 1;
                 }
             }
         }
@@ -605,53 +707,73 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 *dead = 1;
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
             }
-            for (uint32_t i = 0; i < (uint32_t)L::STAGES; ++i) {
-                if (i < k_used) mbar_wait(base + L::K_FULL + 8 * ((k_used - 1 - i) % L::STAGES), ((k_used - 1 - i) / L::STAGES) & 1);
-                if (i < used) mbar_wait(base + L::V_FULL + 8 * ((used - 1 - i) % L::STAGES), ((used - 1 - i) / L::STAGES) & 1);
-            }
+            for (uint32_t i = 0; i < min(k_used, (uint32_t)L::KST); ++i)
+                mbar_wait(base + L::K_FULL + 8 * ((k_used - 1 - i) % L::KST), ((k_used - 1 - i) / L::KST) & 1);
+            for (uint32_t i = 0; i < min(v_used, (uint32_t)L::VST); ++i)
+                mbar_wait(base + L::V_FULL + 8 * ((v_used - 1 - i) % L::VST), ((v_used - 1 - i) / L::VST) & 1);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issue
         if (lane == 0) {
-            uint32_t g = 0, st = 0, ph = 0;
+            // the scores run one tile ahead of the products, into the next item where its queries are there
+            uint32_t g = 0, n = 0, st = 0, ph = 0;
+            int sr = 0, sj = 0;  // the scores' next tile: item and tile in it
+            Item si;
+            auto scores_item = [&]() -> bool {
+                const int idx = item_index(sr);
+                if (idx >= n_items) return false;
+                si = load_item(p, idx, G);
+                return true;
+            };
+            bool more = scores_item();
+            auto scores = [&](bool wait) {
+                if (!ok || !more) return;
+                if (sj == 0) {
+                    const uint32_t bar = base + L::Q_FULL + 8 * (sr & 1);
+                    if (!wait && !mbar_try_wait(bar, (sr >> 1) & 1)) return;
+                    ok = wait_bar(bar, (sr >> 1) & 1, dead);
+                }
+                ok = ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead);
+                if (!ok) return;
+                tc_fence_after();
+                const int R = NWG * (8 << (si.flags & 3));
+                const uint32_t id = idesc_e4m3_f32(128, R), to = tmem + TM_S + (n & 1) * R_MAX, q_at = base + L::Q + (sr & 1) * L::Q_BUF;
+                const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+#pragma unroll
+                for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id, ks > 0);
+#pragma unroll
+                for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id, 1);
+                umma_commit(base + L::S_FULL + 8 * (n & 1));
+                umma_commit(base + L::K_FREE + 8 * st);
+                if (++st == (uint32_t)L::KST) {
+                    st = 0;
+                    ph ^= 1;
+                }
+                ++n;
+                if (++sj == si.tiles) {
+                    umma_commit(base + L::Q_FREE + 8 * (sr & 1));
+                    sj = 0;
+                    ++sr;
+                    more = scores_item();
+                }
+            };
             for (int r = 0; ok; ++r) {
                 const int idx = item_index(r);
                 if (idx >= n_items) break;
                 const Item it = load_item(p, idx, G);
-                const int cw = 8 << (it.flags & 3), R = NWG * cw;
-                const uint32_t q_at = base + L::Q;
-                const uint32_t id_s = idesc_e4m3_f32(128, R), id_o = idesc_f16_f32_mn(D, R);
-                const uint64_t qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
-                const int pitch = min(2 * R, 128);
+                const int R = NWG * (8 << (it.flags & 3)), pitch = min(2 * R, 128);
+                const uint32_t id = idesc_f16_f32_mn(D, R);
                 const uint64_t vd = sdesc_rows(base + L::VH, 128, TT * 128), pd = sdesc_rows(base + L::P, pitch, TT * 128);
-                auto scores = [&](uint32_t n) {
-                    if (!(ok = ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead))) return;
-                    const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0);
-                    const uint32_t to = tmem + TM_S + (n & 1) * R_MAX;
-#pragma unroll
-                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id_s, ks > 0);
-#pragma unroll
-                    for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id_s, 1);
-                    umma_commit(base + L::S_FULL + 8 * (n & 1));
-                    umma_commit(base + L::K_FREE + 8 * st);
-                    if (++st == (uint32_t)L::STAGES) {
-                        st = 0;
-                        ph ^= 1;
-                    }
-                };
-                if (!(ok = wait_bar(base + L::Q_FULL + 8 * (r & 1), (r >> 1) & 1, dead))) break;
-                tc_fence_after();
-                scores(g);
                 for (int j = 0; j < it.tiles && ok; ++j, ++g) {
-                    if (j + 1 < it.tiles) scores(g + 1);
-                    else umma_commit(base + L::Q_FREE);
+                    if (n == g) scores(true);
+                    if (n == g + 1) scores(false);
                     ok = ok && wait_bar(base + L::P_FULL, g & 1, dead);
                     if (j == 0 && r > 0) ok = ok && wait_bar(base + L::O_FREE + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
                     if (!ok) break;
                     tc_fence_after();
                     const int steps = min(TT, it.t1 - it.t0 - j * TT + 15) / 16;
                     for (int ks = 0; ks < steps; ++ks)
-                        umma_bf16(tmem + TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id_o, j > 0 || ks > 0);
+                        umma_bf16(tmem + TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id, j > 0 || ks > 0);
                     umma_commit(base + L::PV_DONE);
                 }
             }
@@ -673,12 +795,18 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
             const Item it = load_item(p, idx, G);
             const int cw = 8 << (it.flags & 3), R = NWG * cw;
             const int32_t *order = p.plan + p.order_at + it.tok;
-            if (r > 0) ok = wait_bar(base + L::Q_FREE, (r - 1) & 1, dead);
+            if (r > 1) ok = wait_bar(base + L::Q_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             if (r > 1) ok = ok && wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            ColAM *am = reinterpret_cast<ColAM *>(sm + L::INFO + (r & 1) * R_MAX * 16);
-            ColLR *lr = reinterpret_cast<ColLR *>(sm + L::INFO + (r & 1) * R_MAX * 16 + R_MAX * 8);
+            uint8_t *info = sm + L::INFO + (r & 1) * L::INFO_BUF;
+            auto set_column = [&](int col, float a, float nm, int lim, int row) {
+                reinterpret_cast<float *>(info + IN_A)[col] = a;
+                reinterpret_cast<float *>(info + IN_M)[col] = nm;
+                reinterpret_cast<int32_t *>(info + IN_LIM)[col] = lim;
+                reinterpret_cast<int32_t *>(info + IN_ROW)[col] = row;
+            };
+            const uint32_t q_at = base + L::Q + (r & 1) * L::Q_BUF;
             // the largest exponent of the range's values: 16 tokens a lane
             uint32_t top = 0;
             for (int t = it.t0 + (tid - 64) * 16; t < it.t1; t += 64 * 16) {
@@ -717,48 +845,55 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                     if (row < it.rows)
                         u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * D + part * 8));
                 }
+                uint32_t a[AT_ONCE], hi[AT_ONCE][2], lo[AT_ONCE][2];
+                int qe[AT_ONCE];
 #pragma unroll
                 for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * RPW * k;
                     const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-                    uint32_t a = 0;
+                    a[k] = 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) a = max(a, max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
+                    for (int e = 0; e < 4; ++e) a[k] = max(a[k], max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
+                }
 #pragma unroll
-                    for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+                for (int o = LPR / 2; o > 0; o >>= 1)
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) a[k] = max(a[k], __shfl_xor_sync(0xffffffffu, a[k], o));
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
                     // the row's largest element to [2^7, 2^8)
-                    const int qe = max((int)(a >> 23) - 127 - 7, -120);
-                    const bool bad = (a >> 23) == 255;
-                    const float inv = pow2(-qe);
-                    uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+                    const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+                    qe[k] = max((int)(a[k] >> 23) - 127 - 7, -120);
+                    const float inv = pow2(-qe[k]);
+                    hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const float v0 = __uint_as_float(x[e] << 16) * inv, v1 = __uint_as_float(x[e] & 0xffff0000u) * inv;
                         const uint16_t h = e4m3x2(v0, v1);
                         const uint32_t back = f16x2_of_e4m3x2(h);
                         const float2 hf = __half22float2(*reinterpret_cast<const __half2 *>(&back));
-                        hi[e / 2] |= (uint32_t)h << (16 * (e & 1));
-                        lo[e / 2] |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * (e & 1));
+                        hi[k][e / 2] |= (uint32_t)h << (16 * (e & 1));
+                        lo[k][e / 2] |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * (e & 1));
                     }
-                    if (bad) hi[0] = hi[1] = lo[0] = lo[1] = 0x7f7f7f7fu;
+                }
+#pragma unroll
+                for (int k = 0; k < AT_ONCE; ++k) {
+                    const int row = row0 + 2 * RPW * k;
                     if (row < it.rows) {
+                        const bool bad = (a[k] >> 23) == 255;
+                        if (bad) hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0x7f7f7f7fu;
                         const int wg = row * per_inv >> 16, col = wg * cw + row - wg * it.per;
-                        sts64(base + L::Q + swz_rows<D>(col * D + part * 8), hi[0], hi[1]);
-                        sts64(base + L::Q + swz_rows<D>((R + col) * D + part * 8), lo[0], lo[1]);
-                        if (part == 0) {
-                            am[col] = ColAM{bad ? 1.f : pow2(qe) * p.scale_log2, M_NONE};
-                            lr[col] = ColLR{it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]};
-                        }
+                        sts64(q_at + swz_rows<D>(col * D + part * 8), hi[k][0], hi[k][1]);
+                        sts64(q_at + swz_rows<D>((R + col) * D + part * 8), lo[k][0], lo[k][1]);
+                        if (part == 0)
+                            set_column(col, bad ? 1.f : pow2(qe[k]) * p.scale_log2, -M_NONE,
+                                       it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]);
                     }
                 }
             }
-            // columns that fill up a warpgroup's last eight: they take part, unused
+            // columns that fill up a warpgroup's last eight take part, unused; they see nothing
             for (int g = w; g < NWG; g += 2) {
                 const int ncol = min(max(it.rows - g * it.per, 0), it.per);
-                if (ncol + lane < ((ncol + 7) & ~7)) {
-                    am[g * cw + ncol + lane] = ColAM{0.f, 0.f};
-                    lr[g * cw + ncol + lane] = ColLR{0x7fffffff, 0};
-                }
+                if (ncol + lane < ((ncol + 7) & ~7)) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
             }
             fence_async_smem();
             mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
@@ -770,7 +905,6 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     } else {
         // ------------------------------------------------ softmax and results
         Soft s;
-        s.sm = sm;
         s.base = base;
         s.tmem = tmem;
         s.dead = dead;
