@@ -50,7 +50,7 @@ constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
 constexpr int TT = 128;          // cached tokens a tile
 constexpr int R_MAX = 128;       // rows an item
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
-constexpr int NWG = 4;           // softmax warpgroups, each with its share of the rows
+constexpr int NWG = 2;           // softmax warpgroups, each with its share of the rows
 constexpr int ATTN_THREADS = 128 + NWG * WG;
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
@@ -352,17 +352,18 @@ struct Token {
     float kf, vf, vref;
 };
 
-// P of a tile into shared memory, the probabilities to the sums l.  Returns
-// the largest log2 P of the token.  References that lie too low may make P and
-// l infinite: move_refs then mends both.
+// P of a tile into shared memory, the probabilities times `sign` to the sums
+// l.  Returns the largest log2 P of the token.
 template <int D, int CW, bool MASK>
-__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
+__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at, float sign)
 {
     using L = Layout<D>;
     constexpr int CH = CW < 16 ? CW : 16;    // columns in registers at a time
     constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
-    const uint32_t p_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128);
-    const uint32_t row_at = s.tid * PITCH + s.wg * 2 * CW % 128;
+    // the token's row; a piece's place in it is XORed with a constant of the row, see swz_rows
+    constexpr uint32_t SWZ = PITCH == 128 ? 7 : PITCH == 64 ? 3 : 1;
+    const uint32_t row_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128) + s.tid * PITCH;
+    const uint32_t mix = (s.wg * 2 * CW % 128) ^ ((((uint32_t)s.tid * PITCH >> 7) & SWZ) << 4);
     float mx = -INFINITY;
 #pragma unroll
     for (int c0 = 0; c0 < CW; c0 += CH) {
@@ -374,7 +375,7 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
         for (int c = 0; c < CH; c += 2) {
             const float2 e = make_float2(ex2(x[c]), ex2(x[c + 1]));
             float2 v = mul2(e, make_float2(t.vf, t.vf));
-            l[(c0 + c) / 2] = add2(l[(c0 + c) / 2], e);
+            l[(c0 + c) / 2] = fma2(e, make_float2(sign, sign), l[(c0 + c) / 2]);
             if (MASK) {  // not 0 * NaN
                 if (x[c] == -INFINITY) v.x = 0.f;
                 if (x[c + 1] == -INFINITY) v.y = 0.f;
@@ -386,23 +387,21 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
         if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
 #pragma unroll
         for (int c = 0; c < CH; c += 8)
-            sts128(p_at + swz_rows<PITCH>(row_at + 2 * (c0 + c)), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+            sts128(row_at + (mix ^ (2 * (c0 + c))), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
     }
     return mx + t.vref;
 }
 
 // Moves the references that a score of this tile passes by too much (all of
 // them where there is none yet), and with them what the output and the
-// sums hold already; after an item's first tile the sums hold this tile's
-// probabilities too, which are taken out again.  The whole warpgroup; needs the product
-// before this tile's to be done.
+// sums of earlier tiles hold.  The whole warpgroup; needs the product before this
+// tile's to be done.
 template <int CW>
 __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
 {
     constexpr int CH = 8;
-#pragma unroll
-    for (int c0 = 0; c0 < CW; c0 += CH) {
-        if (c0 >= w.ncol) break;
+#pragma unroll 1
+    for (int c0 = 0; c0 < w.ncol; c0 += CH) {
         float x[CH];
         tmem_ld8(s_at + c0, reinterpret_cast<uint32_t *>(x));
         tmem_ld_wait();
@@ -416,34 +415,36 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
         stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), v);
     }
     named_sync(w.nb, WG);
-    if (s.tid < w.ncol) {
+    if (s.tid < CW) {
         float v = ldsf(w.wmax + 4 * s.tid);
         for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * CW_MAX + s.tid)));
         const uint32_t nm = w.info + IN_M + 4 * s.tid;
         const float m = -ldsf(nm);
-        const bool move = v - m > P_MOST;
-        stsf(w.fac + 4 * s.tid, move ? v - P_TOP - m : 0.f);
+        const bool move = s.tid < w.ncol && v - m > P_MOST;
+        stsf(w.fac + 4 * s.tid, move ? ex2(m - (v - P_TOP)) : 1.f);
         if (move) stsf(nm, P_TOP - v);
     }
     named_sync(w.nb, WG);
     if (w.j > 0) {
-#pragma unroll
-        for (int c0 = 0; c0 < CW; c0 += CH) {
-            if (c0 >= w.ncol) break;
-            float o[CH], x[CH];
+#pragma unroll 1
+        for (int c0 = 0; c0 < w.ncol; c0 += CH) {
+            float o[CH];
             tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
-            soft_args<CH, true>(x, w, s_at, c0, t.kf, t.at);
+            tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < CH; ++c) {
-                const float up = c0 + c < w.ncol ? ldsf(w.fac + 4 * (c0 + c)) : 0.f, f = ex2(-up);
-                o[c] *= f;
-                // (next to a probability that went out of range the sum was nothing)
-                float &lc = c & 1 ? l[(c0 + c) / 2].y : l[(c0 + c) / 2].x;
-                lc = x[c] + up > 100.f ? 0.f : lc * f - ex2(x[c]);
-            }
+            for (int c = 0; c < CH; ++c) o[c] *= ldsf(w.fac + 4 * (c0 + c));
             tmem_st8(w.o_at + c0, reinterpret_cast<const uint32_t *>(o));
         }
         tmem_st_wait();
+#pragma unroll
+        for (int c = 0; c < CW; c += 4) {
+            // (a sum is nothing next to a score 2^100 above, and may have been put out of range by it)
+            const float4 f = lds4f(w.fac + 4 * c);
+            l[c / 2].x = f.x < 0x1p-100f ? 0.f : l[c / 2].x * f.x;
+            l[c / 2].y = f.y < 0x1p-100f ? 0.f : l[c / 2].y * f.y;
+            l[c / 2 + 1].x = f.z < 0x1p-100f ? 0.f : l[c / 2 + 1].x * f.z;
+            l[c / 2 + 1].y = f.w < 0x1p-100f ? 0.f : l[c / 2 + 1].y * f.w;
+        }
     }
 }
 
@@ -458,12 +459,18 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
         if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
         return true;
     }
-    // (a second time the references fit, but for scores so large that fp32 rounds them by more than P_MOST)
-    for (int round = 0;; ++round) {
-        if (round > 0 || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
-        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at) : soft_probs<D, CW, false>(s, w, l, t, s_at);
-        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && round == 0))) return true;
-        if (!named_sync_and(w.nb, WG, s.ok)) return false;
+    // References are set before an item's first tile; where a later one passes
+    // them by too much its probabilities are taken out of the sums again, the
+    // references moved and the tile done anew.  (Then they fit, but for scores so large
+    // that fp32 rounds them by more than P_MOST.)
+    enum { FIRST, TAKE_OUT, AGAIN };
+    for (int pass = FIRST;; ++pass) {
+        if (pass == AGAIN || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
+        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
+        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at, sign) : soft_probs<D, CW, false>(s, w, l, t, s_at, sign);
+        if (pass == TAKE_OUT) continue;
+        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
+        if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;
         tc_fence_after();
     }
 }
@@ -475,13 +482,15 @@ template <int D>
 __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 {
     using L = Layout<D>;
-    constexpr int CPR = D / 16;  // 16-byte pieces of a row's codes
-    const uint32_t from = s.base + L::V + s.stage * L::SIDE, to = s.base + L::VH;
+    constexpr int CPR = D / 16;                    // 16-byte pieces of a row's codes
+    constexpr int ROWS = NWG * WG / CPR;           // rows a pass; a multiple of 8, so a thread's swizzle stays
+    const int me = s.wg * WG + s.tid, row0 = me / CPR, ch = me % CPR;
+    const uint32_t from = s.base + L::V + s.stage * L::SIDE + swz_rows<D>(row0 * D + ch * 16);
+    const uint32_t to = s.base + L::VH + (ch / 4) * (TT * 128);
+    const uint32_t to0 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32), to1 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32 + 16);
 #pragma unroll
-    for (int k = 0; k < TT * CPR / (NWG * WG); ++k) {
-        const int q = k * (NWG * WG) + s.wg * WG + s.tid;
-        const int row = q / CPR, ch = q % CPR;
-        const uint4 c = lds128(from + swz_rows<D>(row * D + ch * 16));
+    for (int k = 0; k < TT / ROWS; ++k) {
+        const uint4 c = lds128(from + k * ROWS * D);
         const uint32_t x[4] = {c.x, c.y, c.z, c.w};
         uint32_t h[8];
 #pragma unroll
@@ -489,13 +498,12 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
             h[2 * i] = f16x2_of_e4m3x2((uint16_t)x[i]);
             h[2 * i + 1] = f16x2_of_e4m3x2((uint16_t)(x[i] >> 16));
         }
-        if (row >= valid) {
+        if (valid < TT && row0 + k * ROWS >= valid) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) h[i] = 0;
         }
-        const uint32_t at = to + (ch / 4) * (TT * 128), off = row * 128 + (ch % 4) * 32;
-        sts128(at + swz_rows<128>(off), h[0], h[1], h[2], h[3]);
-        sts128(at + swz_rows<128>(off + 16), h[4], h[5], h[6], h[7]);
+        sts128(to0 + k * ROWS * 128, h[0], h[1], h[2], h[3]);
+        sts128(to1 + k * ROWS * 128, h[4], h[5], h[6], h[7]);
     }
 }
 
@@ -923,7 +931,8 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
             switch (it.flags & 3) {
             case 0: ok = soft_item<D, 8>(p, s, it, r); break;
             case 1: ok = soft_item<D, 16>(p, s, it, r); break;
-            default: ok = soft_item<D, 32>(p, s, it, r); break;
+            case 2: ok = soft_item<D, 32>(p, s, it, r); break;
+            default: ok = soft_item<D, CW_MAX>(p, s, it, r); break;
             }
         }
         if (!ok && s.tid == 0) {
@@ -1093,7 +1102,7 @@ struct RowTile {
 
 // The time of an item in units of 128-token tiles of the smallest class, from
 // measurements of single items: a tile of each class, and what an item takes besides.
-constexpr float TILE_COST[3] = {1.f, 1.2f, 1.8f};
+constexpr float TILE_COST[4] = {1.f, 1.1f, 1.4f, 2.2f};
 constexpr float ITEM_COST = 2.f;
 
 // Plans a checked batch into the tables at w; returns the words used.
@@ -1113,7 +1122,7 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     auto prompt = [&](int i) { return grouped && b->group[i] >= 0 ? b->group_len[b->group[i]] : 0; };
     auto class_of = [&](int ntok) {
         const int cw = (ntok * G + NWG - 1) / NWG;
-        return cw <= 8 ? 0 : cw <= 16 ? 1 : 2;
+        return cw <= 8 ? 0 : cw <= 16 ? 1 : cw <= 32 ? 2 : 3;
     };
     std::vector<RowTile> tiles;
     // own tokens: `per` query tokens of a request at a time
