@@ -96,7 +96,8 @@ struct Layout {
     static constexpr uint32_t INFO = EXPS + VST * 2 * TT;  // two items' constants of the columns, see IN_*
     static constexpr uint32_t INFO_BUF = R_MAX * 16;
     static constexpr uint32_t FAC = INFO + 2 * INFO_BUF;
-    static constexpr uint32_t WMAX = FAC + R_MAX * 4;     // [NWG][4][CW_MAX] floats
+    static constexpr uint32_t PLACE = FAC + R_MAX * 4;    // where the rows go, 64 bits each
+    static constexpr uint32_t WMAX = PLACE + R_MAX * 8;   // [NWG][4][CW_MAX] floats
     // barriers: K full, K free, V full, V free (a stage each), scores full [2], P full, product done, Q full [2], Q free
     // [2], item done [2], drain
     static constexpr uint32_t K_FULL = WMAX + 4 * R_MAX * 4;
@@ -117,8 +118,7 @@ constexpr uint32_t TM_S = 0, TM_O = 256;  // tensor memory columns: two buffers 
 
 // A column's constants, arrays of R_MAX words: the factor a of its scores (query row's
 // power of two, scale, log2 e), its reference -m, the tokens it sees and (query
-// token << 8 | head in the group).  In the end a and -m make way for the
-// factor of its output, the other two for the place of its row.
+// token << 8 | head in the group).
 constexpr uint32_t IN_A = 0, IN_M = R_MAX * 4, IN_LIM = R_MAX * 8, IN_ROW = R_MAX * 12;
 
 __device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
@@ -301,21 +301,27 @@ __device__ __forceinline__ void soft_wait(Soft &s, uint32_t bar, uint32_t parity
 
 // Addresses and constants of an item for a softmax warpgroup.
 struct SoftItem {
-    uint32_t info, fac, wmax;      // shared memory: constants of the warpgroup's columns (IN_*), scratch
+    uint32_t info, fac, place, wmax;  // shared memory: constants of the warpgroup's columns (IN_*), scratch
     int ncol, vtop, nb, j;
     uint32_t lanes, o_at;          // tensor memory
 };
 
-// Scores of CH columns (from column c0 of the warpgroup) less their references, in log2;
-// with MASK minus infinity where the row does not see the token.  Returns the
-// largest.  Columns are dealt with eight at a time.
-template <int CH, bool MASK>
-__device__ __forceinline__ float soft_args(float (&x)[CH], const SoftItem &w, uint32_t s_at, int c0, float kf, int tok)
+// CH columns of tensor memory, this warp's lanes
+template <int CH>
+__device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
 {
-#pragma unroll
-    for (int c = 0; c < CH; c += 8)
-        if (c0 + c < w.ncol) tmem_ld8(s_at + c0 + c, reinterpret_cast<uint32_t *>(x) + c);
-    tmem_ld_wait();
+    uint32_t *r = reinterpret_cast<uint32_t *>(x);
+    if constexpr (CH == 8) tmem_ld8(at, r);
+    else if constexpr (CH == 16) tmem_ld16(at, *reinterpret_cast<uint32_t(*)[16]>(r));
+    else tmem_ld32(at, r);
+}
+
+// Turns scores of CH columns (from column c0 of the warpgroup) into what they are above their
+// references, in log2; with MASK minus infinity where the row does not see the
+// token.  Returns the largest.  Columns are dealt with eight at a time.
+template <int CH, bool MASK>
+__device__ __forceinline__ float soft_args(float (&x)[CH], const SoftItem &w, int c0, float kf, int tok)
+{
     float mx = -INFINITY;
     const float2 kf2 = make_float2(kf, kf);
 #pragma unroll
@@ -352,129 +358,6 @@ struct Token {
     float kf, vf, vref;
 };
 
-// P of a tile into shared memory, the probabilities times `sign` to the sums
-// l.  Returns the largest log2 P of the token.
-template <int D, int CW, bool MASK>
-__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at, float sign)
-{
-    using L = Layout<D>;
-    constexpr int CH = CW < 16 ? CW : 16;    // columns in registers at a time
-    constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
-    // the token's row; a piece's place in it is XORed with a constant of the row, see swz_rows
-    constexpr uint32_t SWZ = PITCH == 128 ? 7 : PITCH == 64 ? 3 : 1;
-    const uint32_t row_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128) + s.tid * PITCH;
-    const uint32_t mix = (s.wg * 2 * CW % 128) ^ ((((uint32_t)s.tid * PITCH >> 7) & SWZ) << 4);
-    float mx = -INFINITY;
-#pragma unroll
-    for (int c0 = 0; c0 < CW; c0 += CH) {
-        if (c0 >= w.ncol) break;
-        float x[CH];
-        mx = fmaxf(mx, soft_args<CH, MASK>(x, w, s_at, c0, t.kf, t.at));
-        uint32_t h[CH / 2];
-#pragma unroll
-        for (int c = 0; c < CH; c += 2) {
-            const float2 e = make_float2(ex2(x[c]), ex2(x[c + 1]));
-            float2 v = mul2(e, make_float2(t.vf, t.vf));
-            l[(c0 + c) / 2] = fma2(e, make_float2(sign, sign), l[(c0 + c) / 2]);
-            if (MASK) {  // not 0 * NaN
-                if (x[c] == -INFINITY) v.x = 0.f;
-                if (x[c + 1] == -INFINITY) v.y = 0.f;
-            }
-            const __half2 p = __floats2half2_rn(v.x, v.y);
-            h[c / 2] = *reinterpret_cast<const uint32_t *>(&p);
-        }
-        // P takes the place of the last tile's once its product is done
-        if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-#pragma unroll
-        for (int c = 0; c < CH; c += 8)
-            sts128(row_at + (mix ^ (2 * (c0 + c))), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
-    }
-    return mx + t.vref;
-}
-
-// Moves the references that a score of this tile passes by too much (all of
-// them where there is none yet), and with them what the output and the
-// sums of earlier tiles hold.  The whole warpgroup; needs the product before this
-// tile's to be done.
-template <int CW>
-__device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
-{
-    constexpr int CH = 8;
-#pragma unroll 1
-    for (int c0 = 0; c0 < w.ncol; c0 += CH) {
-        float x[CH];
-        tmem_ld8(s_at + c0, reinterpret_cast<uint32_t *>(x));
-        tmem_ld_wait();
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            x[c] = fmaf(x[c], t.kf * ldsf(w.info + IN_A + 4 * (c0 + c)), t.vref);
-            if (t.at >= (int)lds32(w.info + IN_LIM + 4 * (c0 + c)) || !(x[c] == x[c])) x[c] = -INFINITY;
-        }
-        int col;
-        const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
-        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), v);
-    }
-    named_sync(w.nb, WG);
-    if (s.tid < CW) {
-        float v = ldsf(w.wmax + 4 * s.tid);
-        for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * CW_MAX + s.tid)));
-        const uint32_t nm = w.info + IN_M + 4 * s.tid;
-        const float m = -ldsf(nm);
-        const bool move = s.tid < w.ncol && v - m > P_MOST;
-        stsf(w.fac + 4 * s.tid, move ? ex2(m - (v - P_TOP)) : 1.f);
-        if (move) stsf(nm, P_TOP - v);
-    }
-    named_sync(w.nb, WG);
-    if (w.j > 0) {
-#pragma unroll 1
-        for (int c0 = 0; c0 < w.ncol; c0 += CH) {
-            float o[CH];
-            tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
-            tmem_ld_wait();
-#pragma unroll
-            for (int c = 0; c < CH; ++c) o[c] *= ldsf(w.fac + 4 * (c0 + c));
-            tmem_st8(w.o_at + c0, reinterpret_cast<const uint32_t *>(o));
-        }
-        tmem_st_wait();
-#pragma unroll
-        for (int c = 0; c < CW; c += 4) {
-            // (a sum is nothing next to a score 2^100 above, and may have been put out of range by it)
-            const float4 f = lds4f(w.fac + 4 * c);
-            l[c / 2].x = f.x < 0x1p-100f ? 0.f : l[c / 2].x * f.x;
-            l[c / 2].y = f.y < 0x1p-100f ? 0.f : l[c / 2].y * f.y;
-            l[c / 2 + 1].x = f.z < 0x1p-100f ? 0.f : l[c / 2 + 1].x * f.z;
-            l[c / 2 + 1].y = f.w < 0x1p-100f ? 0.f : l[c / 2 + 1].y * f.w;
-        }
-    }
-}
-
-// A tile of an item of the class with CW columns a warpgroup.  False: gave up
-// (the whole warpgroup together).
-template <int D, int CW>
-__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, bool mask)
-{
-    using L = Layout<D>;
-    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
-    if (w.ncol == 0) {
-        if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-        return true;
-    }
-    // References are set before an item's first tile; where a later one passes
-    // them by too much its probabilities are taken out of the sums again, the
-    // references moved and the tile done anew.  (Then they fit, but for scores so large
-    // that fp32 rounds them by more than P_MOST.)
-    enum { FIRST, TAKE_OUT, AGAIN };
-    for (int pass = FIRST;; ++pass) {
-        if (pass == AGAIN || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
-        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
-        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at, sign) : soft_probs<D, CW, false>(s, w, l, t, s_at, sign);
-        if (pass == TAKE_OUT) continue;
-        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
-        if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;
-        tc_fence_after();
-    }
-}
-
 // The warpgroups' share of a tile's values in f16; zeros from row `valid` on
 // (past the range a stage holds other tokens' values, or none: 0 * NaN must
 // not arise).
@@ -507,6 +390,145 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
     }
 }
 
+// P of a tile and the warpgroup's share of its widened values into shared
+// memory, the probabilities times `sign` to the sums l.  Returns the largest log2 P
+// of the token.
+template <int D, int CW, bool MASK>
+__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at, float sign,
+                                            int valid)
+{
+    using L = Layout<D>;
+    constexpr int CH = CW < 16 ? CW : 16;    // columns at a time; the next ones' scores are on their way
+    constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
+    // the token's row; a piece's place in it is XORed with a constant of the row, see swz_rows
+    constexpr uint32_t SWZ = PITCH == 128 ? 7 : PITCH == 64 ? 3 : 1;
+    const uint32_t row_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128) + s.tid * PITCH;
+    const uint32_t mix = (s.wg * 2 * CW % 128) ^ ((((uint32_t)s.tid * PITCH >> 7) & SWZ) << 4);
+    float mx = -INFINITY;
+    float x[2][CH];
+    load_columns<CH>(x[0], s_at);
+#pragma unroll
+    for (int c0 = 0; c0 < CW; c0 += CH) {
+        if (c0 >= w.ncol) break;
+        float (&y)[CH] = x[(c0 / CH) & 1];
+        tmem_ld_wait();
+        if (c0 + CH < CW) load_columns<CH>(x[(c0 / CH + 1) & 1], s_at + c0 + CH);
+        mx = fmaxf(mx, soft_args<CH, MASK>(y, w, c0, t.kf, t.at));
+        uint32_t h[CH / 2];
+#pragma unroll
+        for (int c = 0; c < CH; c += 2) {
+            const float2 e = make_float2(ex2(y[c]), ex2(y[c + 1]));
+            float2 v = mul2(e, make_float2(t.vf, t.vf));
+            l[(c0 + c) / 2] = fma2(e, make_float2(sign, sign), l[(c0 + c) / 2]);
+            if (MASK) {  // not 0 * NaN
+                if (y[c] == -INFINITY) v.x = 0.f;
+                if (y[c + 1] == -INFINITY) v.y = 0.f;
+            }
+            const __half2 p = __floats2half2_rn(v.x, v.y);
+            h[c / 2] = *reinterpret_cast<const uint32_t *>(&p);
+        }
+        if (c0 == 0) {  // P and the values take the place of the last tile's once its product is done
+            if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+            widen_values<D>(s, valid);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; c += 8)
+            sts128(row_at + (mix ^ (2 * (c0 + c))), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+    }
+    return mx + t.vref;
+}
+
+// Moves the references that a score of this tile passes by too much (all of
+// them where there is none yet), and with them what the output and the
+// sums of earlier tiles hold.  The whole warpgroup; needs the product before this
+// tile's to be done.
+template <int CW>
+__device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
+{
+    constexpr int CH = CW < 32 ? CW : 32;
+#pragma unroll 1
+    for (int c0 = 0; c0 < w.ncol; c0 += CH) {
+        float x[CH];
+        load_columns<CH>(x, s_at + c0);
+        tmem_ld_wait();
+#pragma unroll
+        for (int c = 0; c < CH; c += 4) {
+            const float4 a = lds4f(w.info + IN_A + 4 * (c0 + c));
+            const uint4 n = lds128(w.info + IN_LIM + 4 * (c0 + c));
+            const float k[4] = {a.x, a.y, a.z, a.w};
+            const int lim[4] = {(int)n.x, (int)n.y, (int)n.z, (int)n.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[c + i] = fmaf(x[c + i], t.kf * k[i], t.vref);
+                if (t.at >= lim[i] || !(x[c + i] == x[c + i]) || c0 + c + i >= w.ncol) x[c + i] = -INFINITY;
+            }
+        }
+        int col;
+        const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
+        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), v);
+    }
+    named_sync(w.nb, WG);
+    if (s.tid < CW) {
+        float v = ldsf(w.wmax + 4 * s.tid);
+        for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * CW_MAX + s.tid)));
+        const uint32_t nm = w.info + IN_M + 4 * s.tid;
+        const float m = -ldsf(nm);
+        const bool move = s.tid < w.ncol && v - m > P_MOST;
+        stsf(w.fac + 4 * s.tid, move ? ex2(m - (v - P_TOP)) : 1.f);
+        if (move) stsf(nm, P_TOP - v);
+    }
+    named_sync(w.nb, WG);
+    if (w.j > 0) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < w.ncol; c0 += 8) {
+            float o[8];
+            tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
+            tmem_ld_wait();
+#pragma unroll
+            for (int c = 0; c < 8; ++c) o[c] *= ldsf(w.fac + 4 * (c0 + c));
+            tmem_st8(w.o_at + c0, reinterpret_cast<const uint32_t *>(o));
+        }
+        tmem_st_wait();
+#pragma unroll
+        for (int c = 0; c < CW; c += 4) {
+            // (a sum is nothing next to a score 2^100 above, and may have been put out of range by it)
+            const float4 f = lds4f(w.fac + 4 * c);
+            l[c / 2].x = f.x < 0x1p-100f ? 0.f : l[c / 2].x * f.x;
+            l[c / 2].y = f.y < 0x1p-100f ? 0.f : l[c / 2].y * f.y;
+            l[c / 2 + 1].x = f.z < 0x1p-100f ? 0.f : l[c / 2 + 1].x * f.z;
+            l[c / 2 + 1].y = f.w < 0x1p-100f ? 0.f : l[c / 2 + 1].y * f.w;
+        }
+    }
+}
+
+// A tile of an item of the class with CW columns a warpgroup.  False: gave up
+// (the whole warpgroup together).
+template <int D, int CW>
+__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, bool mask, int valid)
+{
+    using L = Layout<D>;
+    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
+    if (w.ncol == 0) {
+        if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+        widen_values<D>(s, valid);
+        return true;
+    }
+    // References are set before an item's first tile; where a later one passes
+    // them by too much its probabilities are taken out of the sums again, the
+    // references moved and the tile done anew.  (Then they fit, but for scores so large
+    // that fp32 rounds them by more than P_MOST.)
+    enum { FIRST, TAKE_OUT, AGAIN };
+    for (int pass = FIRST;; ++pass) {
+        if (pass == AGAIN || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
+        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
+        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at, sign, valid) : soft_probs<D, CW, false>(s, w, l, t, s_at, sign, valid);
+        if (pass == TAKE_OUT) continue;
+        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
+        if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;
+        tc_fence_after();
+    }
+}
+
 // One item of the class with CW columns a warpgroup.  False: gave up (the
 // whole warpgroup together).
 template <int D, int CW>
@@ -517,6 +539,7 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     SoftItem w;
     w.info = s.base + L::INFO + (n_item & 1) * L::INFO_BUF + s.wg * CW * 4;
     w.fac = s.base + L::FAC + s.wg * CW_MAX * 4;
+    w.place = s.base + L::PLACE + s.wg * CW_MAX * 8;
     w.wmax = s.base + L::WMAX + s.wg * 4 * CW_MAX * 4;
     w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
     w.lanes = (uint32_t)(s.quarter * 32) << 16;
@@ -542,8 +565,7 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         t.vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - w.vtop);
         t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
         // column masks only where a row does not see the whole tile (the first query token sees least)
-        if (!soft_tile<D, CW>(s, w, l, t, end > min(it.t1, it.lim))) return false;
-        widen_values<D>(s, it.t1 - (end - TT));
+        if (!soft_tile<D, CW>(s, w, l, t, end > min(it.t1, it.lim), it.t1 - (end - TT))) return false;
         tc_fence_before();
         fence_async_smem();
         mbar_arrive_release(s.base + L::P_FULL);
@@ -581,9 +603,8 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
             at = (int64_t)part * D;
             p.part_l[part] = lse2;
         }
-        stsf(at_i + IN_A, t > 0.f ? 1.f / t : t == t ? 0.f : t);
-        sts32(at_i + IN_LIM, (uint32_t)at);
-        sts32(at_i + IN_ROW, (uint32_t)(at >> 32));
+        stsf(w.fac + 4 * s.tid, t > 0.f ? 1.f / t : t == t ? 0.f : t);
+        sts64(w.place + 8 * s.tid, (uint32_t)at, (uint32_t)(at >> 32));
     }
     soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
     tc_fence_after();
@@ -591,27 +612,139 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     const int dim = D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
     const bool live = D == 128 || s.lane < 16;
     const float unit = pow2(w.vtop - 127);
-#pragma unroll
-    for (int c0 = 0; c0 < CW; c0 += 8) {
-        if (c0 < w.ncol) {
-            float o[8];
-            tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
+    auto rows_out = [&](auto *to, auto of) {
+        constexpr int CO = CW < 16 ? CW : 16;
+#pragma unroll 1
+        for (int c0 = 0; c0 < w.ncol; c0 += CO) {
+            float o[CO];
+            load_columns<CO>(o, w.o_at + c0);
             tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t at_i = w.info + 4 * (c0 + i);
-                const int64_t at = (int64_t)((uint64_t)lds32(at_i + IN_ROW) << 32 | lds32(at_i + IN_LIM)) + dim;
-                const float v = o[i] * ldsf(at_i + IN_A) * unit;
-                if (c0 + i < w.ncol && live) {
-                    if (direct) p.out[at] = f_to_bf16(v);
-                    else p.part_o[at] = v;
-                }
+            for (int c = 0; c < CO; c += 4) {
+                const float4 f = lds4f(w.fac + 4 * (c0 + c));
+                const uint4 p0 = lds128(w.place + 8 * (c0 + c)), p1 = lds128(w.place + 8 * (c0 + c) + 16);
+                const float k[4] = {f.x, f.y, f.z, f.w};
+                const uint32_t lo[4] = {p0.x, p0.z, p1.x, p1.z}, hi[4] = {p0.y, p0.w, p1.y, p1.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (c0 + c + i < w.ncol && live) to[(int64_t)((uint64_t)hi[i] << 32 | lo[i]) + dim] = of(o[c + i] * k[i] * unit);
             }
         }
-    }
+    };
+    if (direct) rows_out(p.out, [](float v) { return f_to_bf16(v); });
+    else rows_out(p.part_o, [](float v) { return v; });
     tc_fence_before();
     mbar_arrive_release(s.base + L::O_FREE + 8 * (n_item & 1));
     return true;
+}
+
+// An item's queries: rows scaled by a power of two and split in hi + lo, the
+// constants of its columns, the largest exponent of its values.  W warps, this
+// one the w-th.
+template <int D, int W>
+__device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base, const Item &it, int n_item, int w, int lane)
+{
+    using L = Layout<D>;
+    const int KV = p.kv.heads, G = p.n_heads / KV;
+    const int cw = 8 << (it.flags & 3), R = NWG * cw;
+    const int g_inv = (65535 + G) / G, per_inv = (65535 + it.per) / it.per;  // quotients by products: rows are below 129, divisors at most 64
+    const int32_t *order = p.plan + p.order_at + it.tok;
+    const uint32_t info = base + L::INFO + (n_item & 1) * L::INFO_BUF, q_at = base + L::Q + (n_item & 1) * L::Q_BUF;
+    auto set_column = [&](int col, float a, float nm, int lim, int row) {
+        stsf(info + IN_A + 4 * col, a);
+        stsf(info + IN_M + 4 * col, nm);
+        sts32(info + IN_LIM + 4 * col, (uint32_t)lim);
+        sts32(info + IN_ROW + 4 * col, (uint32_t)row);
+    };
+    constexpr int LPR = D / 8;           // lanes a row, eight elements each
+    constexpr int RPW = 32 / LPR;        // rows a warp deals with at a time
+    constexpr int AT_ONCE = 4;           // loads of a lane under way together
+    const int part = lane % LPR;
+    for (int row0 = w * RPW + lane / LPR; row0 < it.rows + lane / LPR; row0 += W * RPW * AT_ONCE) {
+        uint4 u[AT_ONCE];
+        int id[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int row = row0 + W * RPW * k, i = row * g_inv >> 16;
+            id[k] = 0;
+            if (row < it.rows) id[k] = (((it.flags & RF_CAUSAL) ? it.tok + i : __ldg(order + i)) << 8) | (row - i * G);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            u[k] = make_uint4(0, 0, 0, 0);
+            if (row0 + W * RPW * k < it.rows)
+                u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * D + part * 8));
+        }
+        uint32_t a[AT_ONCE], hi[AT_ONCE][2], lo[AT_ONCE][2];
+        int qe[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+            a[k] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) a[k] = max(a[k], max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
+        }
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int k = 0; k < AT_ONCE; ++k) a[k] = max(a[k], __shfl_xor_sync(0xffffffffu, a[k], o));
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            // the row's largest element to [2^7, 2^8)
+            const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+            qe[k] = max((int)(a[k] >> 23) - 127 - 7, -120);
+            const float inv = pow2(-qe[k]);
+            hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float v0 = __uint_as_float(x[e] << 16) * inv, v1 = __uint_as_float(x[e] & 0xffff0000u) * inv;
+                const uint16_t h = e4m3x2(v0, v1);
+                const uint32_t back = f16x2_of_e4m3x2(h);
+                const float2 hf = __half22float2(*reinterpret_cast<const __half2 *>(&back));
+                hi[k][e / 2] |= (uint32_t)h << (16 * (e & 1));
+                lo[k][e / 2] |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * (e & 1));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int row = row0 + W * RPW * k;
+            if (row < it.rows) {
+                const bool bad = (a[k] >> 23) == 255;
+                if (bad) hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0x7f7f7f7fu;
+                const int wg = row * per_inv >> 16, col = wg * cw + row - wg * it.per;
+                sts64(q_at + swz_rows<D>(col * D + part * 8), hi[k][0], hi[k][1]);
+                sts64(q_at + swz_rows<D>((R + col) * D + part * 8), lo[k][0], lo[k][1]);
+                if (part == 0)
+                    set_column(col, bad ? 1.f : pow2(qe[k]) * p.scale_log2, -M_NONE,
+                               it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]);
+            }
+        }
+    }
+    // columns that fill up a warpgroup's last eight take part, unused; they see nothing
+    for (int g = w; g < NWG; g += W) {
+        const int ncol = min(max(it.rows - g * it.per, 0), it.per);
+        if (ncol + lane < ((ncol + 7) & ~7)) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
+    }
+    // the largest exponent of the range's values, by two of the warps: 16 tokens a lane
+    if (w < 2) {
+        uint32_t top = 0;
+        for (int t = it.t0 + (w * 32 + lane) * 16; t < it.t1; t += 64 * 16) {
+            const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
+            const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
+            const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
+            const uint32_t x[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
+                const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+                top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
+            }
+        }
+        top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
+        top = __reduce_max_sync(0xffffffffu, top);
+        if (lane == 0) sts32(base + L::MISC + 8 + 8 * (n_item & 1) + 4 * w, top);
+    }
+    fence_async_smem();
 }
 
 template <int D>
@@ -661,6 +794,11 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
+    constexpr int OTHERS = ATTN_THREADS - 32;
+    if (warp > 0) {  // the first item's queries by every warp but the one that starts its loads
+        stage_queries<D, OTHERS / 32>(p, base, load_item(p, blockIdx.x, G), 0, warp - 1, lane);
+        named_sync(1 + NWG, OTHERS);
+    }
 
     if (warp == 0) {
         // ------------------------------------------------ loads: a lane per page of a tile
@@ -796,114 +934,15 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     } else if (warp < 4) {
         // ------------------------------------------------ queries: rows scaled by a power of two and split in hi + lo
         const int w = warp - 2;
-        const int g_inv = (65535 + G) / G;  // row / G by a product: rows are below 128, G at most 64
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
             const Item it = load_item(p, idx, G);
-            const int cw = 8 << (it.flags & 3), R = NWG * cw;
-            const int32_t *order = p.plan + p.order_at + it.tok;
             if (r > 1) ok = wait_bar(base + L::Q_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             if (r > 1) ok = ok && wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            uint8_t *info = sm + L::INFO + (r & 1) * L::INFO_BUF;
-            auto set_column = [&](int col, float a, float nm, int lim, int row) {
-                reinterpret_cast<float *>(info + IN_A)[col] = a;
-                reinterpret_cast<float *>(info + IN_M)[col] = nm;
-                reinterpret_cast<int32_t *>(info + IN_LIM)[col] = lim;
-                reinterpret_cast<int32_t *>(info + IN_ROW)[col] = row;
-            };
-            const uint32_t q_at = base + L::Q + (r & 1) * L::Q_BUF;
-            // the largest exponent of the range's values: 16 tokens a lane
-            uint32_t top = 0;
-            for (int t = it.t0 + (tid - 64) * 16; t < it.t1; t += 64 * 16) {
-                const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
-                const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
-                const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
-                const uint32_t x[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
-                    const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
-                    top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
-                }
-            }
-            top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
-            top = __reduce_max_sync(0xffffffffu, top);
-            if (lane == 0) reinterpret_cast<volatile int *>(sm + L::MISC + 8)[2 * (r & 1) + w] = (int)top;
-            const int per_inv = (65535 + it.per) / it.per;
-            constexpr int LPR = D / 8;           // lanes a row, eight elements each
-            constexpr int RPW = 32 / LPR;        // rows a warp deals with at a time
-            constexpr int AT_ONCE = 4;           // loads of a lane under way together
-            const int part = lane % LPR;
-            for (int row0 = w * RPW + lane / LPR; row0 < it.rows + lane / LPR; row0 += 2 * RPW * AT_ONCE) {
-                uint4 u[AT_ONCE];
-                int id[AT_ONCE];
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * RPW * k, i = row * g_inv >> 16;
-                    id[k] = 0;
-                    if (row < it.rows) id[k] = (((it.flags & RF_CAUSAL) ? it.tok + i : __ldg(order + i)) << 8) | (row - i * G);
-                }
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * RPW * k;
-                    u[k] = make_uint4(0, 0, 0, 0);
-                    if (row < it.rows)
-                        u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * D + part * 8));
-                }
-                uint32_t a[AT_ONCE], hi[AT_ONCE][2], lo[AT_ONCE][2];
-                int qe[AT_ONCE];
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-                    a[k] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) a[k] = max(a[k], max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
-                }
-#pragma unroll
-                for (int o = LPR / 2; o > 0; o >>= 1)
-#pragma unroll
-                    for (int k = 0; k < AT_ONCE; ++k) a[k] = max(a[k], __shfl_xor_sync(0xffffffffu, a[k], o));
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    // the row's largest element to [2^7, 2^8)
-                    const uint32_t x[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
-                    qe[k] = max((int)(a[k] >> 23) - 127 - 7, -120);
-                    const float inv = pow2(-qe[k]);
-                    hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float v0 = __uint_as_float(x[e] << 16) * inv, v1 = __uint_as_float(x[e] & 0xffff0000u) * inv;
-                        const uint16_t h = e4m3x2(v0, v1);
-                        const uint32_t back = f16x2_of_e4m3x2(h);
-                        const float2 hf = __half22float2(*reinterpret_cast<const __half2 *>(&back));
-                        hi[k][e / 2] |= (uint32_t)h << (16 * (e & 1));
-                        lo[k][e / 2] |= (uint32_t)e4m3x2(v0 - hf.x, v1 - hf.y) << (16 * (e & 1));
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k < AT_ONCE; ++k) {
-                    const int row = row0 + 2 * RPW * k;
-                    if (row < it.rows) {
-                        const bool bad = (a[k] >> 23) == 255;
-                        if (bad) hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0x7f7f7f7fu;
-                        const int wg = row * per_inv >> 16, col = wg * cw + row - wg * it.per;
-                        sts64(q_at + swz_rows<D>(col * D + part * 8), hi[k][0], hi[k][1]);
-                        sts64(q_at + swz_rows<D>((R + col) * D + part * 8), lo[k][0], lo[k][1]);
-                        if (part == 0)
-                            set_column(col, bad ? 1.f : pow2(qe[k]) * p.scale_log2, -M_NONE,
-                                       it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]);
-                    }
-                }
-            }
-            // columns that fill up a warpgroup's last eight take part, unused; they see nothing
-            for (int g = w; g < NWG; g += 2) {
-                const int ncol = min(max(it.rows - g * it.per, 0), it.per);
-                if (ncol + lane < ((ncol + 7) & ~7)) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
-            }
-            fence_async_smem();
+            if (r > 0) stage_queries<D, 2>(p, base, it, r, w, lane);
             mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
         }
         if (!ok && lane == 0) {
