@@ -371,10 +371,12 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
     const uint32_t from = s.base + L::V + s.stage * L::SIDE + swz_rows<D>(row0 * D + ch * 16);
     const uint32_t to = s.base + L::VH + (ch / 4) * (TT * 128);
     const uint32_t to0 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32), to1 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32 + 16);
+    uint4 c[TT / ROWS];
+#pragma unroll
+    for (int k = 0; k < TT / ROWS; ++k) c[k] = lds128(from + k * ROWS * D);
 #pragma unroll
     for (int k = 0; k < TT / ROWS; ++k) {
-        const uint4 c = lds128(from + k * ROWS * D);
-        const uint32_t x[4] = {c.x, c.y, c.z, c.w};
+        const uint32_t x[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
         uint32_t h[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -859,78 +861,84 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 mbar_wait(base + L::V_FULL + 8 * ((v_used - 1 - i) % L::VST), ((v_used - 1 - i) / L::VST) & 1);
         }
     } else if (warp == 1) {
-        // ------------------------------------------------ MMA issue
-        if (lane == 0) {
-            // the scores run one tile ahead of the products, into the next item where its queries are there
-            uint32_t g = 0, n = 0, st = 0, ph = 0;
-            int sr = 0, sj = 0;  // the scores' next tile: item and tile in it
-            Item si;
-            auto scores_item = [&]() -> bool {
-                const int idx = item_index(sr);
-                if (idx >= n_items) return false;
-                si = load_item(p, idx, G);
-                return true;
-            };
-            bool more = scores_item();
-            auto scores = [&](bool wait) {
-                if (!ok || !more) return;
-                if (sj == 0) {
-                    const uint32_t bar = base + L::Q_FULL + 8 * (sr & 1);
-                    if (!wait && !mbar_try_wait(bar, (sr >> 1) & 1)) return;
-                    ok = wait_bar(bar, (sr >> 1) & 1, dead);
-                }
-                ok = ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead);
-                if (!ok) return;
-                tc_fence_after();
-                const int R = NWG * (8 << (si.flags & 3));
-                const uint32_t id = idesc_e4m3_f32(128, R), to = tmem + TM_S + (n & 1) * R_MAX, q_at = base + L::Q + (sr & 1) * L::Q_BUF;
-                const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+        // ------------------------------------------------ MMA issue: the whole warp goes along, one lane issues (so that the
+        // descriptors stay in uniform registers).  The scores run one tile ahead of the products, into the next
+        // item where its queries are there.
+        const bool lead = elect_one();
+        uint32_t g = 0, n = 0, st = 0, ph = 0;
+        int sr = 0, sj = 0;  // the scores' next tile: item and tile in it
+        bool more = true;
+        Item si = load_item(p, blockIdx.x, G);
+        auto scores = [&](bool wait) {
+            if (!ok || !more) return;
+            if (sj == 0) {
+                const uint32_t bar = base + L::Q_FULL + 8 * (sr & 1);
+                if (!wait && !__all_sync(0xffffffffu, mbar_try_wait(bar, (sr >> 1) & 1))) return;
+                ok = wait_bar(bar, (sr >> 1) & 1, dead);
+            }
+            ok = __all_sync(0xffffffffu, ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead));
+            if (!ok) return;
+            tc_fence_after();
+            const int R = NWG * (8 << (si.flags & 3));
+            const uint32_t id = idesc_e4m3_f32(128, R), to = tmem + TM_S + (n & 1) * R_MAX, q_at = base + L::Q + (sr & 1) * L::Q_BUF;
+            const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+            const bool last = sj + 1 == si.tiles;
+            if (lead) {
 #pragma unroll
                 for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id, ks > 0);
 #pragma unroll
                 for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id, 1);
                 umma_commit(base + L::S_FULL + 8 * (n & 1));
                 umma_commit(base + L::K_FREE + 8 * st);
-                if (++st == (uint32_t)L::KST) {
-                    st = 0;
-                    ph ^= 1;
-                }
-                ++n;
-                if (++sj == si.tiles) {
-                    umma_commit(base + L::Q_FREE + 8 * (sr & 1));
-                    sj = 0;
-                    ++sr;
-                    more = scores_item();
-                }
-            };
-            for (int r = 0; ok; ++r) {
-                const int idx = item_index(r);
-                if (idx >= n_items) break;
-                const Item it = load_item(p, idx, G);
-                const int R = NWG * (8 << (it.flags & 3)), pitch = min(2 * R, 128);
-                const uint32_t id = idesc_f16_f32_mn(D, R);
-                const uint64_t vd = sdesc_rows(base + L::VH, 128, TT * 128), pd = sdesc_rows(base + L::P, pitch, TT * 128);
-                for (int j = 0; j < it.tiles && ok; ++j, ++g) {
-                    if (n == g) scores(true);
-                    if (n == g + 1) scores(false);
-                    ok = ok && wait_bar(base + L::P_FULL, g & 1, dead);
-                    if (j == 0 && r > 0) ok = ok && wait_bar(base + L::O_FREE + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const int steps = min(TT, it.t1 - it.t0 - j * TT + 15) / 16;
+                if (last) umma_commit(base + L::Q_FREE + 8 * (sr & 1));
+            }
+            __syncwarp();
+            if (++st == (uint32_t)L::KST) {
+                st = 0;
+                ph ^= 1;
+            }
+            ++n;
+            if (++sj == si.tiles) {
+                sj = 0;
+                ++sr;
+                const int idx = item_index(sr);
+                more = idx < n_items;
+                if (more) si = load_item(p, idx, G);
+            }
+        };
+        for (int r = 0; ok; ++r) {
+            const int idx = item_index(r);
+            if (idx >= n_items) break;
+            const Item it = load_item(p, idx, G);
+            const int R = NWG * (8 << (it.flags & 3)), pitch = min(2 * R, 128);
+            const uint32_t id = idesc_f16_f32_mn(D, R);
+            const uint64_t vd = sdesc_rows(base + L::VH, 128, TT * 128), pd = sdesc_rows(base + L::P, pitch, TT * 128);
+            for (int j = 0; j < it.tiles && ok; ++j, ++g) {
+                if (n == g) scores(true);
+                if (n == g + 1) scores(false);
+                ok = ok && wait_bar(base + L::P_FULL, g & 1, dead);
+                if (j == 0 && r > 0) ok = ok && wait_bar(base + L::O_FREE + 8 * ((r - 1) & 1), ((r - 1) >> 1) & 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                tc_fence_after();
+                const int steps = min(TT, it.t1 - it.t0 - j * TT + 15) / 16;
+                if (lead) {
                     for (int ks = 0; ks < steps; ++ks)
                         umma_bf16(tmem + TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id, j > 0 || ks > 0);
                     umma_commit(base + L::PV_DONE);
                 }
+                __syncwarp();
             }
-            if (!ok) {  // the products issued so far end before the CTA does
+        }
+        if (!ok) {  // the products issued so far end before the CTA does
+            if (lead) {
                 *dead = 1;
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
                 umma_commit(base + L::DRAIN);
                 mbar_wait(base + L::DRAIN, 0);
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else if (warp < 4) {
         // ------------------------------------------------ queries: rows scaled by a power of two and split in hi + lo
         const int w = warp - 2;
