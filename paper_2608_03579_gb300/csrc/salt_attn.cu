@@ -38,7 +38,7 @@ namespace {
 // The plan's device tables: int32 words of one block, written by the host
 // into a staging area and copied by a kernel.
 constexpr int HEAD_WORDS = 8;   // HD_* below
-constexpr int HD_TOKENS = 0, HD_RECS = 1, HD_PARTIAL = 2;
+constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // query tokens, records of either kind, whether rows need the combine
 constexpr int TOK_WORDS = 8;    // per query token: where its partial rows are, see TK_*
 constexpr int TK_OWN = 0, TK_OWN_ROWS = 1, TK_OWN_N = 2, TK_PRE = 3, TK_PRE_ROWS = 4, TK_PRE_N = 5, TK_DIRECT = 6;
 constexpr int REC_WORDS = 8;    // per item, shared by the key/value heads
@@ -48,13 +48,10 @@ constexpr int RC_FLAGS = 0, RC_TOK = 1, RC_NTOK = 2, RC_PAGES = 3, RC_T0 = 4, RC
 constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
 
 constexpr int TT = 128;          // cached tokens a tile
-constexpr int R_MAX = 128;       // rows an item
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
-constexpr int NWG = 2;           // softmax warpgroups, each with its share of the rows
-constexpr int ATTN_THREADS = 128 + NWG * WG;
+constexpr int CH = 16;           // columns a softmax thread has in hand at a time
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
-constexpr int CW_MAX = R_MAX / NWG;  // columns of a warpgroup
 constexpr float M_NONE = -1e30f; // the reference before the first token
 
 struct AttnParams {
@@ -81,10 +78,23 @@ __global__ void plan_copy_kernel(const uint4 *src, uint4 *dst, int n)
 }
 
 // ---------------------------------------------------------------- shared memory
-template <int D>
-struct Layout {
-    static constexpr int KST = D == 128 ? 3 : 6;          // stages of K and of V
-    static constexpr int VST = D == 128 ? 2 : 4;
+// The two kernels.  WIDE: up to 128 rows an item, their columns shared by two softmax
+// warpgroups, one CTA an SM.  Narrow: few rows (single query tokens and drafts), bound by the
+// latency of a tile's steps and by memory: one warpgroup, two CTAs an SM.
+template <int D_, bool WIDE_>
+struct Shape {
+    static constexpr int D = D_;
+    static constexpr bool WIDE = WIDE_;
+    static constexpr int NWG = WIDE ? 2 : 1;              // softmax warpgroups
+    static constexpr int R_MAX = WIDE ? 128 : D == 128 ? 16 : 32;  // rows an item
+    static constexpr int CW_MAX = R_MAX / NWG;            // columns of a warpgroup
+    static constexpr int THREADS = 128 + NWG * WG;
+    static constexpr int CTAS = WIDE ? 1 : 2;             // an SM
+    // tensor memory columns: two buffers of R_MAX scores, the output
+    static constexpr uint32_t TM_S = 0, TM_O = 2 * R_MAX, TM_COLS = WIDE ? 512 : D == 128 ? 64 : 128;
+    // shared memory
+    static constexpr int KST = WIDE ? (D == 128 ? 3 : 6) : (D == 128 ? 2 : 4);  // stages of K and of V
+    static constexpr int VST = WIDE ? (D == 128 ? 2 : 4) : (D == 128 ? 2 : 4);
     static constexpr uint32_t SIDE = TT * D;              // codes of K or V of a tile
     static constexpr uint32_t K = 0;
     static constexpr uint32_t V = K + KST * SIDE;
@@ -93,8 +103,12 @@ struct Layout {
     static constexpr uint32_t Q_BUF = 2 * R_MAX * D;
     static constexpr uint32_t Q = P + TT * 2 * R_MAX;     // two items' queries
     static constexpr uint32_t EXPS = Q + 2 * Q_BUF;       // per stage of V: 128 of K, 128 of V
-    static constexpr uint32_t INFO = EXPS + VST * 2 * TT;  // two items' constants of the columns, see IN_*
+    // Two items' constants of the columns, arrays of R_MAX words: the factor a of a column's scores (query
+    // row's power of two, scale, log2 e), its reference -m, the tokens it sees and (query token << 8 | head in
+    // the group).
+    static constexpr uint32_t INFO = EXPS + VST * 2 * TT;
     static constexpr uint32_t INFO_BUF = R_MAX * 16;
+    static constexpr uint32_t IN_A = 0, IN_M = R_MAX * 4, IN_LIM = R_MAX * 8, IN_ROW = R_MAX * 12;
     static constexpr uint32_t FAC = INFO + 2 * INFO_BUF;
     static constexpr uint32_t PLACE = FAC + R_MAX * 4;    // where the rows go, 64 bits each
     static constexpr uint32_t WMAX = PLACE + R_MAX * 8;   // [NWG][4][CW_MAX] floats
@@ -113,13 +127,12 @@ struct Layout {
     static constexpr uint32_t DRAIN = Q_FREE + 16;
     static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents
     static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
+    static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
+    static_assert(TM_O + R_MAX <= TM_COLS, "tensor memory");
 };
-constexpr uint32_t TM_S = 0, TM_O = 256;  // tensor memory columns: two buffers of R_MAX scores, the output
-
-// A column's constants, arrays of R_MAX words: the factor a of its scores (query row's
-// power of two, scale, log2 e), its reference -m, the tokens it sees and (query
-// token << 8 | head in the group).
-constexpr uint32_t IN_A = 0, IN_M = R_MAX * 4, IN_LIM = R_MAX * 8, IN_ROW = R_MAX * 12;
+// Rows up to which an item is narrow, and at most.
+constexpr int narrow_rows(int D) { return D == 128 ? Shape<128, false>::R_MAX : Shape<64, false>::R_MAX; }
+constexpr int WIDE_ROWS = Shape<128, true>::R_MAX;
 
 __device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
 {
@@ -222,10 +235,12 @@ struct Item {
 // out forwards and backwards in turn.
 __device__ __forceinline__ int item_index(int r) { return r * (int)gridDim.x + ((r & 1) ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); }
 
+template <class L>
 __device__ __forceinline__ Item load_item(const AttnParams &p, int idx, int G)
 {
     const int rec = idx / p.kv.heads;
-    const int4 *w = reinterpret_cast<const int4 *>(p.plan + p.rec_at + rec * REC_WORDS);
+    // (the wide items' records come first)
+    const int4 *w = reinterpret_cast<const int4 *>(p.plan + p.rec_at + ((L::WIDE ? 0 : __ldg(p.plan + HD_WIDE)) + rec) * REC_WORDS);
     const int4 a = __ldg(w), b = __ldg(w + 1);
     Item it;
     it.flags = a.x;
@@ -238,7 +253,7 @@ __device__ __forceinline__ Item load_item(const AttnParams &p, int idx, int G)
     it.kh = idx - rec * p.kv.heads;
     it.rows = it.ntok * G;
     it.part = b.w + it.kh * it.rows;
-    it.per = (it.rows + NWG - 1) / NWG;
+    it.per = (it.rows + L::NWG - 1) / L::NWG;
     it.tiles = (it.t1 - it.t0 + TT - 1) / TT;
     return it;
 }
@@ -302,8 +317,9 @@ __device__ __forceinline__ void soft_wait(Soft &s, uint32_t bar, uint32_t parity
 // Addresses and constants of an item for a softmax warpgroup.
 struct SoftItem {
     uint32_t info, fac, place, wmax;  // shared memory: constants of the warpgroup's columns (IN_*), scratch
+    uint32_t p_row, p_mix;            // this token's row of P; a piece's place in it is XORed with p_mix (the swizzle)
+    uint32_t s_at, o_at;              // tensor memory: the first buffer of the scores, the output
     int ncol, vtop, nb, j;
-    uint32_t lanes, o_at;          // tensor memory
 };
 
 // CH columns of tensor memory, this warp's lanes
@@ -316,76 +332,48 @@ __device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
     else tmem_ld32(at, r);
 }
 
-// Turns scores of CH columns (from column c0 of the warpgroup) into what they are above their
-// references, in log2; with MASK minus infinity where the row does not see the
-// token.  Returns the largest.  Columns are dealt with eight at a time.
-template <int CH, bool MASK>
-__device__ __forceinline__ float soft_args(float (&x)[CH], const SoftItem &w, int c0, float kf, int tok)
-{
-    float mx = -INFINITY;
-    const float2 kf2 = make_float2(kf, kf);
-#pragma unroll
-    for (int c = 0; c < CH; c += 8) {
-        if (c0 + c < w.ncol) {
-#pragma unroll
-            for (int i = c; i < c + 8; i += 4) {
-                const float4 a = lds4f(w.info + IN_A + 4 * (c0 + i)), m = lds4f(w.info + IN_M + 4 * (c0 + i));
-                const float2 u = fma2(make_float2(x[i], x[i + 1]), mul2(make_float2(a.x, a.y), kf2), make_float2(m.x, m.y));
-                const float2 v = fma2(make_float2(x[i + 2], x[i + 3]), mul2(make_float2(a.z, a.w), kf2), make_float2(m.z, m.w));
-                x[i] = u.x;
-                x[i + 1] = u.y;
-                x[i + 2] = v.x;
-                x[i + 3] = v.y;
-                if (MASK) {
-                    const uint4 n = lds128(w.info + IN_LIM + 4 * (c0 + i));
-                    if (tok >= (int)n.x) x[i] = -INFINITY;
-                    if (tok >= (int)n.y) x[i + 1] = -INFINITY;
-                    if (tok >= (int)n.z) x[i + 2] = -INFINITY;
-                    if (tok >= (int)n.w) x[i + 3] = -INFINITY;
-                }
-                mx = fmaxf(fmaxf(mx, fmaxf(x[i], x[i + 1])), fmaxf(x[i + 2], x[i + 3]));
-            }
-        }
-    }
-    return mx;
-}
-
 // A token's part of a tile: factors of its scores and of its probabilities, and what
 // P is to p in log2, held so that p stays in range (a value 2^100 below the
 // largest may lose bits).
 struct Token {
     int at;
     float kf, vf, vref;
+    bool mask;                        // some row does not see the whole tile
 };
 
-// The warpgroups' share of a tile's values in f16; zeros from row `valid` on
-// (past the range a stage holds other tokens' values, or none: 0 * NaN must
-// not arise).
-template <int D>
+// The warpgroups' share of a tile's values in f16; zeros for rows that stand
+// for NaN and from row `valid` on (past the range a stage holds other tokens'
+// values, or none): 0 * NaN must not arise.
+template <class L>
 __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 {
-    using L = Layout<D>;
-    constexpr int CPR = D / 16;                    // 16-byte pieces of a row's codes
-    constexpr int ROWS = NWG * WG / CPR;           // rows a pass; a multiple of 8, so a thread's swizzle stays
-    const int me = s.wg * WG + s.tid, row0 = me / CPR, ch = me % CPR;
-    const uint32_t from = s.base + L::V + s.stage * L::SIDE + swz_rows<D>(row0 * D + ch * 16);
+    constexpr int CPR = L::D / 16;                 // 16-byte pieces of a row's codes
+    constexpr int ROWS = L::NWG * WG / CPR;        // rows a pass; a multiple of 8, so a thread's swizzle stays
+    // Eight threads in a row deal with halves of rows r and r ^ 5: their pieces lie in different banks both where
+    // they are read and (twice as wide, every other piece) where they are written.
+    const int me = s.wg * WG + s.tid;
+    const int pair = (me >> 3) & 3, up = (me >> 2) & 1, rest = me >> 5;
+    const int ch = (me & 3) + 4 * (CPR == 8 ? rest & 1 : 0), row0 = 8 * (CPR == 8 ? rest >> 1 : rest) + (up ? pair ^ 5 : pair);
+    const uint32_t from = s.base + L::V + s.stage * L::SIDE + swz_rows<L::D>(row0 * L::D + ch * 16);
+    const uint32_t exps = s.base + L::EXPS + s.stage * 2 * TT + TT + row0;
     const uint32_t to = s.base + L::VH + (ch / 4) * (TT * 128);
     const uint32_t to0 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32), to1 = to + swz_rows<128>(row0 * 128 + (ch % 4) * 32 + 16);
     uint4 c[TT / ROWS];
+    uint32_t ve[TT / ROWS];
 #pragma unroll
-    for (int k = 0; k < TT / ROWS; ++k) c[k] = lds128(from + k * ROWS * D);
+    for (int k = 0; k < TT / ROWS; ++k) {
+        c[k] = lds128(from + k * ROWS * L::D);
+        ve[k] = lds8(exps + k * ROWS);
+    }
 #pragma unroll
     for (int k = 0; k < TT / ROWS; ++k) {
         const uint32_t x[4] = {c[k].x, c[k].y, c[k].z, c[k].w};
+        const uint32_t keep = row0 + k * ROWS < valid && ve[k] != 255u ? 0xffffffffu : 0u;
         uint32_t h[8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[2 * i] = f16x2_of_e4m3x2((uint16_t)x[i]);
-            h[2 * i + 1] = f16x2_of_e4m3x2((uint16_t)(x[i] >> 16));
-        }
-        if (valid < TT && row0 + k * ROWS >= valid) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[i] = 0;
+            h[2 * i] = f16x2_of_e4m3x2((uint16_t)(x[i] & keep));
+            h[2 * i + 1] = f16x2_of_e4m3x2((uint16_t)((x[i] & keep) >> 16));
         }
         sts128(to0 + k * ROWS * 128, h[0], h[1], h[2], h[3]);
         sts128(to1 + k * ROWS * 128, h[4], h[5], h[6], h[7]);
@@ -394,49 +382,61 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 
 // P of a tile and the warpgroup's share of its widened values into shared
 // memory, the probabilities times `sign` to the sums l.  Returns the largest log2 P
-// of the token.
-template <int D, int CW, bool MASK>
-__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at, float sign,
-                                            int valid)
+// of the token.  Columns go by sixteens (the last ones are filled up), the next ones'
+// scores under way.  (One copy of this code for every number of
+// rows: with one for each, and one for masked tiles, the kernel had 223 KB of code and
+// an item's first tile waited 6,000 cycles for instructions.)
+template <class L>
+__device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
+                                            float sign, int valid)
 {
-    using L = Layout<D>;
-    constexpr int CH = CW < 16 ? CW : 16;    // columns at a time; the next ones' scores are on their way
-    constexpr int PITCH = 2 * NWG * CW < 128 ? 2 * NWG * CW : 128;
-    // the token's row; a piece's place in it is XORed with a constant of the row, see swz_rows
-    constexpr uint32_t SWZ = PITCH == 128 ? 7 : PITCH == 64 ? 3 : 1;
-    const uint32_t row_at = s.base + L::P + (s.wg * 2 * CW / 128) * (TT * 128) + s.tid * PITCH;
-    const uint32_t mix = (s.wg * 2 * CW % 128) ^ ((((uint32_t)s.tid * PITCH >> 7) & SWZ) << 4);
+    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
     float mx = -INFINITY;
     float x[2][CH];
-    load_columns<CH>(x[0], s_at);
+    if (w.ncol > 0) load_columns<CH>(x[0], s_at);
 #pragma unroll
-    for (int c0 = 0; c0 < CW; c0 += CH) {
+    for (int c0 = 0; c0 < L::CW_MAX; c0 += CH) {
         if (c0 >= w.ncol) break;
         float (&y)[CH] = x[(c0 / CH) & 1];
         tmem_ld_wait();
-        if (c0 + CH < CW) load_columns<CH>(x[(c0 / CH + 1) & 1], s_at + c0 + CH);
-        mx = fmaxf(mx, soft_args<CH, MASK>(y, w, c0, t.kf, t.at));
+        if (c0 + CH < L::CW_MAX && c0 + CH < w.ncol) load_columns<CH>(x[(c0 / CH + 1) & 1], s_at + c0 + CH);
+        const uint32_t at = w.info + 4 * c0;
+#pragma unroll
+        for (int i = 0; i < CH; i += 4) {
+            const float4 a = lds4f(at + L::IN_A + 4 * i), m = lds4f(at + L::IN_M + 4 * i);
+            const float2 u = fma2(make_float2(y[i], y[i + 1]), mul2(make_float2(a.x, a.y), kf2), make_float2(m.x, m.y));
+            const float2 v = fma2(make_float2(y[i + 2], y[i + 3]), mul2(make_float2(a.z, a.w), kf2), make_float2(m.z, m.w));
+            y[i] = u.x;
+            y[i + 1] = u.y;
+            y[i + 2] = v.x;
+            y[i + 3] = v.y;
+        }
+        if (t.mask) {
+#pragma unroll
+            for (int i = 0; i < CH; i += 4) {
+                const uint4 n = lds128(at + L::IN_LIM + 4 * i);
+                if (t.at >= (int)n.x) y[i] = -INFINITY;
+                if (t.at >= (int)n.y) y[i + 1] = -INFINITY;
+                if (t.at >= (int)n.z) y[i + 2] = -INFINITY;
+                if (t.at >= (int)n.w) y[i + 3] = -INFINITY;
+            }
+        }
         uint32_t h[CH / 2];
 #pragma unroll
-        for (int c = 0; c < CH; c += 2) {
-            const float2 e = make_float2(ex2(y[c]), ex2(y[c + 1]));
-            float2 v = mul2(e, make_float2(t.vf, t.vf));
-            l[(c0 + c) / 2] = fma2(e, make_float2(sign, sign), l[(c0 + c) / 2]);
-            if (MASK) {  // not 0 * NaN
-                if (y[c] == -INFINITY) v.x = 0.f;
-                if (y[c + 1] == -INFINITY) v.y = 0.f;
-            }
-            const __half2 p = __floats2half2_rn(v.x, v.y);
-            h[c / 2] = *reinterpret_cast<const uint32_t *>(&p);
+        for (int i = 0; i < CH; i += 2) {
+            mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
+            const float2 e = make_float2(ex2(y[i]), ex2(y[i + 1])), v = mul2(e, vf2);
+            l[(c0 + i) / 2] = fma2(e, sign2, l[(c0 + i) / 2]);
+            const __half2 q = __floats2half2_rn(v.x, v.y);
+            h[i / 2] = *reinterpret_cast<const uint32_t *>(&q);
         }
-        if (c0 == 0) {  // P and the values take the place of the last tile's once its product is done
-            if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-            widen_values<D>(s, valid);
-        }
-#pragma unroll
-        for (int c = 0; c < CH; c += 8)
-            sts128(row_at + (mix ^ (2 * (c0 + c))), h[c / 2], h[c / 2 + 1], h[c / 2 + 2], h[c / 2 + 3]);
+        // P and the values take the place of the last tile's once its product is done
+        if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+        sts128(w.p_row + (w.p_mix ^ (2 * c0)), h[0], h[1], h[2], h[3]);
+        sts128(w.p_row + (w.p_mix ^ (2 * c0 + 16)), h[4], h[5], h[6], h[7]);
     }
+    if (w.ncol == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+    widen_values<L>(s, valid);
     return mx + t.vref;
 }
 
@@ -444,10 +444,9 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
 // them where there is none yet), and with them what the output and the
 // sums of earlier tiles hold.  The whole warpgroup; needs the product before this
 // tile's to be done.
-template <int CW>
-__device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, uint32_t s_at)
+template <class L>
+__device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at)
 {
-    constexpr int CH = CW < 32 ? CW : 32;
 #pragma unroll 1
     for (int c0 = 0; c0 < w.ncol; c0 += CH) {
         float x[CH];
@@ -455,29 +454,32 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
         tmem_ld_wait();
 #pragma unroll
         for (int c = 0; c < CH; c += 4) {
-            const float4 a = lds4f(w.info + IN_A + 4 * (c0 + c));
-            const uint4 n = lds128(w.info + IN_LIM + 4 * (c0 + c));
+            const float4 a = lds4f(w.info + L::IN_A + 4 * (c0 + c));
+            const uint4 n = lds128(w.info + L::IN_LIM + 4 * (c0 + c));
             const float k[4] = {a.x, a.y, a.z, a.w};
             const int lim[4] = {(int)n.x, (int)n.y, (int)n.z, (int)n.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[c + i] = fmaf(x[c + i], t.kf * k[i], t.vref);
-                if (t.at >= lim[i] || !(x[c + i] == x[c + i]) || c0 + c + i >= w.ncol) x[c + i] = -INFINITY;
+                if (t.at >= lim[i] || !(x[c + i] == x[c + i])) x[c + i] = -INFINITY;
             }
         }
         int col;
         const float v = reduce_columns<CH>(x, s.lane, col, [](float p, float q) { return fmaxf(p, q); });
-        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), v);
+        stsf(w.wmax + 4 * (s.quarter * L::CW_MAX + c0 + col), v);
     }
     named_sync(w.nb, WG);
-    if (s.tid < CW) {
+    if (s.tid < L::CW_MAX) {
         float v = ldsf(w.wmax + 4 * s.tid);
-        for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * CW_MAX + s.tid)));
-        const uint32_t nm = w.info + IN_M + 4 * s.tid;
-        const float m = -ldsf(nm);
-        const bool move = s.tid < w.ncol && v - m > P_MOST;
+        for (int q = 1; q < 4; ++q) v = fmaxf(v, ldsf(w.wmax + 4 * (q * L::CW_MAX + s.tid)));
+        bool move = false;
+        float m = 0.f;
+        if (s.tid < w.ncol) {
+            m = -ldsf(w.info + L::IN_M + 4 * s.tid);
+            move = v - m > P_MOST;
+        }
         stsf(w.fac + 4 * s.tid, move ? ex2(m - (v - P_TOP)) : 1.f);
-        if (move) stsf(nm, P_TOP - v);
+        if (move) stsf(w.info + L::IN_M + 4 * s.tid, P_TOP - v);
     }
     named_sync(w.nb, WG);
     if (w.j > 0) {
@@ -492,7 +494,7 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
         }
         tmem_st_wait();
 #pragma unroll
-        for (int c = 0; c < CW; c += 4) {
+        for (int c = 0; c < L::CW_MAX; c += 4) {
             // (a sum is nothing next to a score 2^100 above, and may have been put out of range by it)
             const float4 f = lds4f(w.fac + 4 * c);
             l[c / 2].x = f.x < 0x1p-100f ? 0.f : l[c / 2].x * f.x;
@@ -503,27 +505,20 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
     }
 }
 
-// A tile of an item of the class with CW columns a warpgroup.  False: gave up
-// (the whole warpgroup together).
-template <int D, int CW>
-__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l)[CW / 2], const Token &t, bool mask, int valid)
+// A tile of an item.  False: gave up (the whole warpgroup together).
+template <class L>
+__device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, int valid)
 {
-    using L = Layout<D>;
-    const uint32_t s_at = s.tmem + w.lanes + TM_S + (s.g & 1) * R_MAX + s.wg * CW;
-    if (w.ncol == 0) {
-        if (s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-        widen_values<D>(s, valid);
-        return true;
-    }
+    const uint32_t s_at = w.s_at + (s.g & 1) * L::R_MAX;
     // References are set before an item's first tile; where a later one passes
     // them by too much its probabilities are taken out of the sums again, the
     // references moved and the tile done anew.  (Then they fit, but for scores so large
     // that fp32 rounds them by more than P_MOST.)
     enum { FIRST, TAKE_OUT, AGAIN };
+#pragma unroll 1
     for (int pass = FIRST;; ++pass) {
-        if (pass == AGAIN || w.j == 0) move_refs<CW>(s, w, l, t, s_at);
-        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
-        const float mx = mask ? soft_probs<D, CW, true>(s, w, l, t, s_at, sign, valid) : soft_probs<D, CW, false>(s, w, l, t, s_at, sign, valid);
+        if ((pass == AGAIN || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
+        const float mx = soft_probs<L>(s, w, l, t, s_at, pass == TAKE_OUT ? -1.f : 1.f, valid);
         if (pass == TAKE_OUT) continue;
         if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
         if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;
@@ -531,30 +526,31 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
     }
 }
 
-// One item of the class with CW columns a warpgroup.  False: gave up (the
-// whole warpgroup together).
-template <int D, int CW>
+// One item.  False: gave up (the whole warpgroup together).
+template <class L>
 __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const Item &it, int n_item)
 {
-    using L = Layout<D>;
-    constexpr int CH = CW < 16 ? CW : 16;
+    const int cw = 16 << (it.flags & 3), pitch = min(2 * L::NWG * cw, 128), at = s.wg * 2 * cw;  // columns a warpgroup; bytes of P
+    const uint32_t lanes = (uint32_t)(s.quarter * 32) << 16;
     SoftItem w;
-    w.info = s.base + L::INFO + (n_item & 1) * L::INFO_BUF + s.wg * CW * 4;
-    w.fac = s.base + L::FAC + s.wg * CW_MAX * 4;
-    w.place = s.base + L::PLACE + s.wg * CW_MAX * 8;
-    w.wmax = s.base + L::WMAX + s.wg * 4 * CW_MAX * 4;
+    w.info = s.base + L::INFO + (n_item & 1) * L::INFO_BUF + s.wg * cw * 4;
+    w.fac = s.base + L::FAC + s.wg * L::CW_MAX * 4;
+    w.place = s.base + L::PLACE + s.wg * L::CW_MAX * 8;
+    w.wmax = s.base + L::WMAX + s.wg * 4 * L::CW_MAX * 4;
+    w.p_row = s.base + L::P + at / 128 * (TT * 128) + s.tid * pitch;
+    w.p_mix = at % 128 ^ (((uint32_t)(s.tid * pitch) >> 7 & (pitch / 16 - 1)) << 4);
+    w.s_at = s.tmem + lanes + L::TM_S + s.wg * cw;
+    w.o_at = s.tmem + lanes + L::TM_O + s.wg * cw;
     w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
-    w.lanes = (uint32_t)(s.quarter * 32) << 16;
-    w.o_at = s.tmem + w.lanes + TM_O + s.wg * CW;
     w.nb = 1 + s.wg;
     // values count in units of the largest exponent of the range
     w.vtop = max((int)lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), (int)lds32(s.base + L::MISC + 12 + 8 * (n_item & 1)));
     if (w.vtop == 0) w.vtop = 127;
-    float2 l[CW / 2];
+    float2 l[L::CW_MAX / 2];
 #pragma unroll
-    for (int c = 0; c < CW / 2; ++c) l[c] = make_float2(0.f, 0.f);
+    for (int c = 0; c < L::CW_MAX / 2; ++c) l[c] = make_float2(0.f, 0.f);
+#pragma unroll 1
     for (w.j = 0; w.j < it.tiles; ++w.j) {
-        const int tok = it.t0 + w.j * TT + s.tid;
         const int end = it.t0 + (w.j + 1) * TT;
         soft_wait(s, s.base + L::V_FULL + 8 * s.stage, s.stage_phase);
         soft_wait(s, s.base + L::S_FULL + 8 * (s.g & 1), (s.g >> 1) & 1);
@@ -562,16 +558,21 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         const uint32_t ex = s.base + L::EXPS + s.stage * 2 * TT + s.tid;
         const uint32_t ke = lds8(ex), ve = lds8(ex + TT);
         Token t;
-        t.at = tok;
+        t.at = end - TT + s.tid;
         t.kf = row_scale(ke);
-        t.vf = ve == 255u ? __uint_as_float(0x7fc00000u) : pow2((int)ve - w.vtop);
+        // A NaN row's values are zero codes: an infinite P makes the rows that see the token NaN, and where P is
+        // 0, as where they do not see it, it adds nothing.
+        t.vf = t.at >= it.t1 ? 0.f : ve == 255u ? 0x1p127f : pow2((int)ve - w.vtop);
         t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
-        // column masks only where a row does not see the whole tile (the first query token sees least)
-        if (!soft_tile<D, CW>(s, w, l, t, end > min(it.t1, it.lim), it.t1 - (end - TT))) return false;
+        t.mask = end > min(it.t1, it.lim);  // (the first query token sees least)
+        if (!soft_tile<L>(s, w, l, t, it.t1 - (end - TT))) return false;
         tc_fence_before();
         fence_async_smem();
-        mbar_arrive_release(s.base + L::P_FULL);
-        mbar_arrive_release(s.base + L::V_FREE + 8 * s.stage);
+        __syncwarp();
+        if (s.lane == 0) {
+            mbar_arrive_release(s.base + L::P_FULL);
+            mbar_arrive_release(s.base + L::V_FREE + 8 * s.stage);
+        }
         ++s.g;
         if (++s.stage == L::VST) {
             s.stage = 0;
@@ -580,87 +581,90 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     }
     // ------------------------------------------------ the item's rows
 #pragma unroll
-    for (int c0 = 0; c0 < CW; c0 += CH) {
+    for (int c0 = 0; c0 < L::CW_MAX; c0 += CH) {
+        if (c0 >= w.ncol) break;
         int col;
         float v[CH];
 #pragma unroll
         for (int c = 0; c < CH; ++c) v[c] = c & 1 ? l[(c0 + c) / 2].y : l[(c0 + c) / 2].x;
         const float t = reduce_columns<CH>(v, s.lane, col, [](float p, float q) { return p + q; });
-        stsf(w.wmax + 4 * (s.quarter * CW_MAX + c0 + col), t);
+        stsf(w.wmax + 4 * (s.quarter * L::CW_MAX + c0 + col), t);
     }
     if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int G = p.n_heads / p.kv.heads;
     const bool direct = it.flags & RF_DIRECT;
     if (s.tid < w.ncol) {
         const uint32_t at_w = w.wmax + 4 * s.tid, at_i = w.info + 4 * s.tid;
-        const float t = (ldsf(at_w) + ldsf(at_w + 4 * CW_MAX)) + (ldsf(at_w + 8 * CW_MAX) + ldsf(at_w + 12 * CW_MAX));
-        const int row = (int)lds32(at_i + IN_ROW);
-        const float lse2 = t > 0.f ? log2f(t) - ldsf(at_i + IN_M) : t == t ? -INFINITY : t;
-        int64_t at;  // the row's first element
+        const float t = (ldsf(at_w) + ldsf(at_w + 4 * L::CW_MAX)) + (ldsf(at_w + 8 * L::CW_MAX) + ldsf(at_w + 12 * L::CW_MAX));
+        const int row = (int)lds32(at_i + L::IN_ROW);
+        const float lse2 = t > 0.f ? log2f(t) - ldsf(at_i + L::IN_M) : t == t ? -INFINITY : t;
+        int64_t to;  // the row's first element
         if (direct) {
-            at = (row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * D;
+            to = (row >> 8) * p.out_stride + (it.kh * G + (row & 255)) * L::D;
             if (p.lse) p.lse[(int64_t)(row >> 8) * p.n_heads + it.kh * G + (row & 255)] = lse2 * 0.693147180559945f;
         } else {
             const int part = it.part + s.wg * it.per + s.tid;
-            at = (int64_t)part * D;
+            to = (int64_t)part * L::D;
             p.part_l[part] = lse2;
         }
         stsf(w.fac + 4 * s.tid, t > 0.f ? 1.f / t : t == t ? 0.f : t);
-        sts64(w.place + 8 * s.tid, (uint32_t)at, (uint32_t)(at >> 32));
+        sts64(w.place + 8 * s.tid, (uint32_t)to, (uint32_t)(to >> 32));
     }
     soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
     tc_fence_after();
     if (!named_sync_and(w.nb, WG, s.ok)) return false;
-    const int dim = D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
-    const bool live = D == 128 || s.lane < 16;
+    const int dim = L::D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
+    const bool live = L::D == 128 || s.lane < 16;
     const float unit = pow2(w.vtop - 127);
-    auto rows_out = [&](auto *to, auto of) {
-        constexpr int CO = CW < 16 ? CW : 16;
 #pragma unroll 1
-        for (int c0 = 0; c0 < w.ncol; c0 += CO) {
-            float o[CO];
-            load_columns<CO>(o, w.o_at + c0);
-            tmem_ld_wait();
+    for (int c0 = 0; c0 < w.ncol; c0 += CH) {
+        float o[CH];
+        load_columns<CH>(o, w.o_at + c0);
+        tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < CO; c += 4) {
-                const float4 f = lds4f(w.fac + 4 * (c0 + c));
-                const uint4 p0 = lds128(w.place + 8 * (c0 + c)), p1 = lds128(w.place + 8 * (c0 + c) + 16);
-                const float k[4] = {f.x, f.y, f.z, f.w};
-                const uint32_t lo[4] = {p0.x, p0.z, p1.x, p1.z}, hi[4] = {p0.y, p0.w, p1.y, p1.w};
+        for (int c = 0; c < CH; c += 4) {
+            const float4 f = lds4f(w.fac + 4 * (c0 + c));
+            const uint4 p0 = lds128(w.place + 8 * (c0 + c)), p1 = lds128(w.place + 8 * (c0 + c) + 16);
+            const float k[4] = {f.x, f.y, f.z, f.w};
+            const uint32_t lo[4] = {p0.x, p0.z, p1.x, p1.z}, hi[4] = {p0.y, p0.w, p1.y, p1.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (c0 + c + i < w.ncol && live) to[(int64_t)((uint64_t)hi[i] << 32 | lo[i]) + dim] = of(o[c + i] * k[i] * unit);
+            for (int i = 0; i < 4; ++i) {
+                const int64_t to = (int64_t)((uint64_t)hi[i] << 32 | lo[i]) + dim;
+                const float v = o[c + i] * k[i] * unit;
+                if (c0 + c + i < w.ncol && live) {
+                    if (direct) p.out[to] = f_to_bf16(v);
+                    else p.part_o[to] = v;
+                }
             }
         }
-    };
-    if (direct) rows_out(p.out, [](float v) { return f_to_bf16(v); });
-    else rows_out(p.part_o, [](float v) { return v; });
+    }
     tc_fence_before();
-    mbar_arrive_release(s.base + L::O_FREE + 8 * (n_item & 1));
+    __syncwarp();
+    if (s.lane == 0) mbar_arrive_release(s.base + L::O_FREE + 8 * (n_item & 1));
     return true;
 }
 
 // An item's queries: rows scaled by a power of two and split in hi + lo, the
 // constants of its columns, the largest exponent of its values.  W warps, this
 // one the w-th.
-template <int D, int W>
-__device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base, const Item &it, int n_item, int w, int lane)
+template <class L>
+__device__ __noinline__ void stage_queries(const AttnParams &p, uint32_t base, int idx, int n_item, int w, int W)
 {
-    using L = Layout<D>;
-    const int KV = p.kv.heads, G = p.n_heads / KV;
-    const int cw = 8 << (it.flags & 3), R = NWG * cw;
+    const int KV = p.kv.heads, G = p.n_heads / KV, lane = threadIdx.x & 31;
+    const Item it = load_item<L>(p, idx, G);
+    const int cw = 16 << (it.flags & 3), R = L::NWG * cw;
     const int g_inv = (65535 + G) / G, per_inv = (65535 + it.per) / it.per;  // quotients by products: rows are below 129, divisors at most 64
     const int32_t *order = p.plan + p.order_at + it.tok;
     const uint32_t info = base + L::INFO + (n_item & 1) * L::INFO_BUF, q_at = base + L::Q + (n_item & 1) * L::Q_BUF;
     auto set_column = [&](int col, float a, float nm, int lim, int row) {
-        stsf(info + IN_A + 4 * col, a);
-        stsf(info + IN_M + 4 * col, nm);
-        sts32(info + IN_LIM + 4 * col, (uint32_t)lim);
-        sts32(info + IN_ROW + 4 * col, (uint32_t)row);
+        stsf(info + L::IN_A + 4 * col, a);
+        stsf(info + L::IN_M + 4 * col, nm);
+        sts32(info + L::IN_LIM + 4 * col, (uint32_t)lim);
+        sts32(info + L::IN_ROW + 4 * col, (uint32_t)row);
     };
-    constexpr int LPR = D / 8;           // lanes a row, eight elements each
+    constexpr int LPR = L::D / 8;           // lanes a row, eight elements each
     constexpr int RPW = 32 / LPR;        // rows a warp deals with at a time
-    constexpr int AT_ONCE = 4;           // loads of a lane under way together
+    constexpr int AT_ONCE = L::WIDE ? 4 : 2;  // loads of a lane under way together
     const int part = lane % LPR;
     for (int row0 = w * RPW + lane / LPR; row0 < it.rows + lane / LPR; row0 += W * RPW * AT_ONCE) {
         uint4 u[AT_ONCE];
@@ -675,7 +679,7 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
         for (int k = 0; k < AT_ONCE; ++k) {
             u[k] = make_uint4(0, 0, 0, 0);
             if (row0 + W * RPW * k < it.rows)
-                u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * D + part * 8));
+                u[k] = __ldg(reinterpret_cast<const uint4 *>(p.q + (id[k] >> 8) * p.q_stride + (it.kh * G + (id[k] & 255)) * L::D + part * 8));
         }
         uint32_t a[AT_ONCE], hi[AT_ONCE][2], lo[AT_ONCE][2];
         int qe[AT_ONCE];
@@ -714,56 +718,62 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
                 const bool bad = (a[k] >> 23) == 255;
                 if (bad) hi[k][0] = hi[k][1] = lo[k][0] = lo[k][1] = 0x7f7f7f7fu;
                 const int wg = row * per_inv >> 16, col = wg * cw + row - wg * it.per;
-                sts64(q_at + swz_rows<D>(col * D + part * 8), hi[k][0], hi[k][1]);
-                sts64(q_at + swz_rows<D>((R + col) * D + part * 8), lo[k][0], lo[k][1]);
+                sts64(q_at + swz_rows<L::D>(col * L::D + part * 8), hi[k][0], hi[k][1]);
+                sts64(q_at + swz_rows<L::D>((R + col) * L::D + part * 8), lo[k][0], lo[k][1]);
                 if (part == 0)
                     set_column(col, bad ? 1.f : pow2(qe[k]) * p.scale_log2, -M_NONE,
                                it.lim + ((it.flags & RF_CAUSAL) ? (row * g_inv >> 16) : 0), id[k]);
             }
         }
     }
-    // columns that fill up a warpgroup's last eight take part, unused; they see nothing
-    for (int g = w; g < NWG; g += W) {
+    // columns that fill up a warpgroup's last sixteen take part, unused; they see nothing
+    for (int g = w; g < L::NWG; g += W) {
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
-        if (ncol + lane < ((ncol + 7) & ~7)) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
+        if (ncol + lane < ((ncol + CH - 1) & ~(CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
     }
-    // the largest exponent of the range's values, by two of the warps: 16 tokens a lane
-    if (w < 2) {
-        uint32_t top = 0;
-        for (int t = it.t0 + (w * 32 + lane) * 16; t < it.t1; t += 64 * 16) {
-            const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
-            const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
-            const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
-            const uint32_t x[4] = {e.x, e.y, e.z, e.w};
+    // the largest exponent of the range's values, 16 tokens a lane
+    uint32_t top = 0;
+    for (int t = it.t0 + (w * 32 + lane) * 16; t < it.t1; t += W * 32 * 16) {
+        const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
+        const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
+        const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
+        const uint32_t x[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
-                const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
-                top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
-            }
+        for (int i = 0; i < 4; ++i) {
+            const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
+            const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
+            top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
         }
-        top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
-        top = __reduce_max_sync(0xffffffffu, top);
-        if (lane == 0) sts32(base + L::MISC + 8 + 8 * (n_item & 1) + 4 * w, top);
+    }
+    top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
+    top = __reduce_max_sync(0xffffffffu, top);
+    const uint32_t slot = base + L::MISC + 8 + 8 * (n_item & 1) + 4 * (w & 1);
+    if (lane == 0) {
+        if (n_item == 0) asm volatile("red.shared.max.u32 [%0], %1;\n" ::"r"(slot), "r"(top) : "memory");
+        else sts32(slot, top);  // (two warps)
     }
     fence_async_smem();
 }
 
-template <int D>
-__global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid_constant__ AttnParams p)
+template <class L>
+__global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __grid_constant__ AttnParams p)
 {
-    using L = Layout<D>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int KV = p.kv.heads, G = p.n_heads / KV;
+    if (L::WIDE) pdl_launch_dependents();  // the narrow items need nothing of the wide ones
     if (p.plan[HD_TOKENS] > p.max_tok) {
         if (blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
+        if (!L::WIDE) pdl_wait();
         return;
     }
-    const int n_items = p.plan[HD_RECS] * KV;
-    if ((int)blockIdx.x >= n_items) return;
+    const int n_items = p.plan[L::WIDE ? HD_WIDE : HD_NARROW] * KV;
+    if ((int)blockIdx.x >= n_items) {
+        if (!L::WIDE) pdl_wait();
+        return;
+    }
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + L::MISC);
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
@@ -773,22 +783,23 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         }
         for (int i = 0; i < L::VST; ++i) {
             mbar_init(base + L::V_FULL + 8 * i, 1);
-            mbar_init(base + L::V_FREE + 8 * i, NWG * WG);
+            mbar_init(base + L::V_FREE + 8 * i, L::NWG * WG / 32);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(base + L::S_FULL + 8 * i, 1);
-            mbar_init(base + L::Q_FULL + 8 * i, 64);
+            mbar_init(base + L::Q_FULL + 8 * i, 2);
             mbar_init(base + L::Q_FREE + 8 * i, 1);
-            mbar_init(base + L::O_FREE + 8 * i, NWG * WG);
+            mbar_init(base + L::O_FREE + 8 * i, L::NWG * WG / 32);
         }
-        mbar_init(base + L::P_FULL, NWG * WG);
+        mbar_init(base + L::P_FULL, L::NWG * WG / 32);
         mbar_init(base + L::PV_DONE, 1);
         mbar_init(base + L::DRAIN, 1);
         *dead = 0;
+        sts64(base + L::MISC + 8, 0, 0);
         mbar_fence_init();
     }
     if (warp == 1) {
-        tmem_alloc(base + L::MISC, 512);
+        tmem_alloc(base + L::MISC, L::TM_COLS);
         tmem_relinquish();
     }
     tc_fence_before();
@@ -796,10 +807,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    constexpr int OTHERS = ATTN_THREADS - 32;
+    constexpr int OTHERS = L::THREADS - 32;
     if (warp > 0) {  // the first item's queries by every warp but the one that starts its loads
-        stage_queries<D, OTHERS / 32>(p, base, load_item(p, blockIdx.x, G), 0, warp - 1, lane);
-        named_sync(1 + NWG, OTHERS);
+        stage_queries<L>(p, base, blockIdx.x, 0, warp - 1, OTHERS / 32);
+        named_sync(1 + L::NWG, OTHERS);
     }
 
     if (warp == 0) {
@@ -808,7 +819,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
-            const Item it = load_item(p, idx, G);
+            const Item it = load_item<L>(p, idx, G);
             const int32_t *list = p.plan + p.pages_at + it.pages;
             const int per = TT >> p.kv.page_log2;
             for (int j = 0; j < it.tiles && ok; ++j) {
@@ -819,12 +830,12 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 if (lane < n) page = __ldg(list + first + lane);
                 const uint32_t bytes = (uint32_t)n * p.kv.page;
                 const int64_t row = ((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2;
-                const uint32_t at = lane * p.kv.page * D;
+                const uint32_t at = lane * p.kv.page * L::D;
                 const uint32_t k_full = base + L::K_FULL + 8 * ks, v_full = base + L::V_FULL + 8 * vs;
                 if (k_used >= (uint32_t)L::KST) ok = wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx(k_full, bytes * D);
+                if (lane == 0) mbar_expect_tx(k_full, bytes * L::D);
                 __syncwarp();
                 if (lane < n) tma_load_2d(base + L::K + ks * L::SIDE + at, &p.kmap, 0, (int)row, k_full);
                 ++k_used;
@@ -835,7 +846,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 if (v_used >= (uint32_t)L::VST) ok = wait_bar(base + L::V_FREE + 8 * vs, vph ^ 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                if (lane == 0) mbar_expect_tx(v_full, bytes * (D + 2));
+                if (lane == 0) mbar_expect_tx(v_full, bytes * (L::D + 2));
                 __syncwarp();
                 if (lane < n) {
                     const uint32_t ex = base + L::EXPS + vs * 2 * TT + lane * p.kv.page;
@@ -868,7 +879,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         uint32_t g = 0, n = 0, st = 0, ph = 0;
         int sr = 0, sj = 0;  // the scores' next tile: item and tile in it
         bool more = true;
-        Item si = load_item(p, blockIdx.x, G);
+        Item si = load_item<L>(p, blockIdx.x, G);
         auto scores = [&](bool wait) {
             if (!ok || !more) return;
             if (sj == 0) {
@@ -879,15 +890,15 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
             ok = __all_sync(0xffffffffu, ok && wait_bar(base + L::K_FULL + 8 * st, ph, dead));
             if (!ok) return;
             tc_fence_after();
-            const int R = NWG * (8 << (si.flags & 3));
-            const uint32_t id = idesc_e4m3_f32(128, R), to = tmem + TM_S + (n & 1) * R_MAX, q_at = base + L::Q + (sr & 1) * L::Q_BUF;
-            const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, D, 0), qh = sdesc_rows(q_at, D, 0), ql = sdesc_rows(q_at + R * D, D, 0);
+            const int R = L::NWG * (16 << (si.flags & 3));
+            const uint32_t id = idesc_e4m3_f32(128, R), to = tmem + L::TM_S + (n & 1) * L::R_MAX, q_at = base + L::Q + (sr & 1) * L::Q_BUF;
+            const uint64_t kd = sdesc_rows(base + L::K + st * L::SIDE, L::D, 0), qh = sdesc_rows(q_at, L::D, 0), ql = sdesc_rows(q_at + R * L::D, L::D, 0);
             const bool last = sj + 1 == si.tiles;
             if (lead) {
 #pragma unroll
-                for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id, ks > 0);
+                for (int ks = 0; ks < L::D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, qh + 2 * ks, id, ks > 0);
 #pragma unroll
-                for (int ks = 0; ks < D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id, 1);
+                for (int ks = 0; ks < L::D / 32; ++ks) umma_e4m3(to, kd + 2 * ks, ql + 2 * ks, id, 1);
                 umma_commit(base + L::S_FULL + 8 * (n & 1));
                 umma_commit(base + L::K_FREE + 8 * st);
                 if (last) umma_commit(base + L::Q_FREE + 8 * (sr & 1));
@@ -903,15 +914,15 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 ++sr;
                 const int idx = item_index(sr);
                 more = idx < n_items;
-                if (more) si = load_item(p, idx, G);
+                if (more) si = load_item<L>(p, idx, G);
             }
         };
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
-            const Item it = load_item(p, idx, G);
-            const int R = NWG * (8 << (it.flags & 3)), pitch = min(2 * R, 128);
-            const uint32_t id = idesc_f16_f32_mn(D, R);
+            const Item it = load_item<L>(p, idx, G);
+            const int R = L::NWG * (16 << (it.flags & 3)), pitch = min(2 * R, 128);
+            const uint32_t id = idesc_f16_f32_mn(L::D, R);
             const uint64_t vd = sdesc_rows(base + L::VH, 128, TT * 128), pd = sdesc_rows(base + L::P, pitch, TT * 128);
             for (int j = 0; j < it.tiles && ok; ++j, ++g) {
                 if (n == g) scores(true);
@@ -924,7 +935,7 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
                 const int steps = min(TT, it.t1 - it.t0 - j * TT + 15) / 16;
                 if (lead) {
                     for (int ks = 0; ks < steps; ++ks)
-                        umma_bf16(tmem + TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id, j > 0 || ks > 0);
+                        umma_bf16(tmem + L::TM_O, vd + ks * (16 * 128 / 16), pd + ks * (16 * pitch / 16), id, j > 0 || ks > 0);
                     umma_commit(base + L::PV_DONE);
                 }
                 __syncwarp();
@@ -945,13 +956,13 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
-            const Item it = load_item(p, idx, G);
             if (r > 1) ok = wait_bar(base + L::Q_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             if (r > 1) ok = ok && wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            if (r > 0) stage_queries<D, 2>(p, base, it, r, w, lane);
-            mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
+            if (r > 0) stage_queries<L>(p, base, idx, r, w, 2);
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
         }
         if (!ok && lane == 0) {
             *dead = 1;
@@ -972,15 +983,10 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
         for (int r = 0; ok; ++r) {
             const int idx = item_index(r);
             if (idx >= n_items) break;
-            const Item it = load_item(p, idx, G);
+            const Item it = load_item<L>(p, idx, G);
             // (the columns' constants are there before the first scores are)
             soft_wait(s, base + L::Q_FULL + 8 * (r & 1), (r >> 1) & 1);
-            switch (it.flags & 3) {
-            case 0: ok = soft_item<D, 8>(p, s, it, r); break;
-            case 1: ok = soft_item<D, 16>(p, s, it, r); break;
-            case 2: ok = soft_item<D, 32>(p, s, it, r); break;
-            default: ok = soft_item<D, CW_MAX>(p, s, it, r); break;
-            }
+            ok = soft_item<L>(p, s, it, r);
         }
         if (!ok && s.tid == 0) {
             *dead = 1;
@@ -991,7 +997,8 @@ __global__ void __launch_bounds__(ATTN_THREADS, 1) attn_tile_kernel(const __grid
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 1) tmem_dealloc(tmem, 512);
+    if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
+    if (!L::WIDE) pdl_wait();  // so that what follows this kernel follows the wide one too
 }
 
 // The rows that several items share (and those no item has): a warp per row,
@@ -1065,6 +1072,7 @@ struct salt_attn {
     bool staging_used[2] = {false, false};
     int staging_next = 0;
     bool built = false;
+    bool wide = false, narrow = false;         // there are items of this kind
     bool partial = false;                      // some row needs the combine
     int T = 0;
     std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since
@@ -1144,20 +1152,69 @@ struct RowTile {
     int len;            // cached tokens it walks
     int lim;            // tokens the first query token sees
     bool causal, alone; // alone: no row of it has another tile
-    int cls;            // columns a warpgroup: 8 << cls
+    int cls;            // columns a warpgroup: 16 << cls
+    bool wide;
 };
 
-// The time of an item in units of 128-token tiles of the smallest class, from
-// measurements of single items: a tile of each class, and what an item takes besides.
-constexpr float TILE_COST[4] = {1.f, 1.1f, 1.4f, 2.2f};
-constexpr float ITEM_COST = 2.f;
+// The time of an item in units of a narrow item's tile of 128 tokens, from measurements: a
+// tile of each class of wide items, and what an item takes besides.
+constexpr float NARROW_TILE = 1.f, NARROW_ITEM = 2.f;
+constexpr float WIDE_TILE[3] = {1.1f, 1.4f, 2.2f};
+constexpr float WIDE_ITEM = 4.f;
+
+float tile_cost(const RowTile &x) { return x.wide ? WIDE_TILE[x.cls] : NARROW_TILE; }
+int items_of(const RowTile &x, double most, int *per_item)
+{
+    const int n = (x.len + TT - 1) / TT;
+    *per_item = (int)std::min<double>(n, std::max(1.0, std::floor(most / tile_cost(x))));
+    return (n + *per_item - 1) / *per_item;
+}
+
+// How long an item of the wide (or of the narrow) tiles may get: the shortest estimated run among some lengths,
+// where a run is its items spread over the CTAs plus half of the longest one.  Keeps
+// to the records and partial rows that are left, if it splits at all.
+double split_limit(const std::vector<RowTile> &tiles, bool wide, int KV, int G, int ctas, int64_t *recs_left, int64_t *rows_left)
+{
+    double whole = 0;
+    for (const RowTile &x : tiles)
+        if (x.wide == wide) whole += KV * (tile_cost(x) * ((x.len + TT - 1) / TT));
+    const double even = std::max(1.0, whole / ctas);
+    double best = 1e300, limit = 1e300;
+    int64_t best_recs = 0, best_rows = 0;
+    for (double part : {0.0, 2.0, 1.0, 0.66, 0.5, 0.33, 0.25, 0.125}) {  // 0: no splits
+        const double most = part == 0.0 ? 1e300 : std::max(1.0, even * part);
+        double sum = 0, longest = 0;
+        int64_t recs = 0, rows = 0;
+        for (const RowTile &x : tiles) {
+            if (x.wide != wide) continue;
+            const float cost = tile_cost(x), fixed = wide ? WIDE_ITEM : NARROW_ITEM;
+            int per_item;
+            const int items = items_of(x, most, &per_item);
+            recs += items;
+            rows += (int64_t)items * KV * x.ntok * G;
+            sum += KV * ((x.len + TT - 1) / TT * cost + items * fixed);
+            longest = std::max(longest, (double)per_item * cost + fixed);
+        }
+        const double est = std::max(longest, sum / ctas + 0.5 * longest);
+        if (part != 0.0 && (recs > *recs_left || rows > *rows_left)) continue;
+        if (est < best) {
+            best = est;
+            limit = most;
+            best_recs = recs;
+            best_rows = rows;
+        }
+    }
+    *recs_left -= best_recs;
+    *rows_left -= best_rows;
+    return limit;
+}
 
 // Plans a checked batch into the tables at w; returns the words used.
 size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
 {
     const KvDev &kv = a->kv->dev;
     const int G = a->cfg.n_heads / kv.heads, KV = kv.heads;
-    const int per = std::max(1, R_MAX / G);  // whole query tokens a tile
+    const int per = std::max(1, WIDE_ROWS / G);  // whole query tokens a tile
     std::memset(w, 0, HEAD_WORDS * 4);
     w[HD_TOKENS] = T;
     const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
@@ -1167,9 +1224,11 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     for (int t = 0; t < T; ++t) order[t] = t;
     const bool grouped = b->group && b->n_groups > 0;
     auto prompt = [&](int i) { return grouped && b->group[i] >= 0 ? b->group_len[b->group[i]] : 0; };
-    auto class_of = [&](int ntok) {
-        const int cw = (ntok * G + NWG - 1) / NWG;
-        return cw <= 8 ? 0 : cw <= 16 ? 1 : cw <= 32 ? 2 : 3;
+    auto add = [&](std::vector<RowTile> &to, int tok, int ntok, int pages, int64_t len, int64_t lim, bool causal, bool alone) {
+        const int rows = ntok * G;
+        const bool wide = rows > narrow_rows(kv.dim);
+        const int cw = wide ? (rows + 1) / 2 : rows;
+        to.push_back({tok, ntok, pages, (int)len, (int)lim, causal, alone, cw <= 16 ? 0 : cw <= 32 ? 1 : 2, wide});
     };
     std::vector<RowTile> tiles;
     // own tokens: `per` query tokens of a request at a time
@@ -1180,7 +1239,7 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
             const int m = std::min(per, n - j);
             const int64_t len = (int64_t)kvl - n + j + m;  // what the last of them sees
             if (len <= 0) continue;
-            tiles.push_back({t0 + j, m, b->page_ptr[i], (int)len, (int)((int64_t)kvl - n + j + 1), true, prompt(i) == 0, class_of(m)});
+            add(tiles, t0 + j, m, b->page_ptr[i], len, (int64_t)kvl - n + j + 1, true, prompt(i) == 0);
         }
     }
     // prompts: the query tokens of a group's requests, in the second part of the order
@@ -1203,56 +1262,46 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
                 const int m = std::min(per, at[g + 1] - j);
                 bool alone = true;
                 for (int k = 0; k < m; ++k) alone = alone && !own[order[T + j + k]];
-                tiles.push_back({T + j, m, own_pages + b->group_page_ptr[g], b->group_len[g], b->group_len[g], false, alone, class_of(m)});
+                add(tiles, T + j, m, own_pages + b->group_page_ptr[g], b->group_len[g], b->group_len[g], false, alone);
             }
         }
     }
-    // How long an item may get: the shortest estimated run among some lengths,
-    // where a run is its items spread over the SMs plus half of the longest one.
-    double whole = 0;
-    for (const RowTile &x : tiles) whole += KV * (TILE_COST[x.cls] * ((x.len + TT - 1) / TT));
-    const double even = std::max(1.0, whole / a->n_sm);
-    double best = 1e300, limit = 0;
-    for (double part : {0.0, 2.0, 1.0, 0.66, 0.5, 0.33, 0.25, 0.125}) {  // 0: no splits
-        const double most = part == 0.0 ? 1e300 : std::max(1.0, even * part);
-        double sum = 0, longest = 0;
-        int64_t recs = 0, rows = 0;
-        for (const RowTile &x : tiles) {
-            const int n = (x.len + TT - 1) / TT;
-            const int per_item = (int)std::min<double>(n, std::max(1.0, std::floor(most / TILE_COST[x.cls])));
-            const int items = (n + per_item - 1) / per_item;
-            recs += items;
-            rows += (int64_t)items * KV * x.ntok * G;
-            sum += KV * (n * TILE_COST[x.cls] + items * ITEM_COST);
-            longest = std::max(longest, (double)per_item * TILE_COST[x.cls] + ITEM_COST);
+    // (without splits every list fits: its share of the records and rows is set aside first)
+    int64_t recs_left = a->rec_cap, rows_left = a->part_cap;
+    for (const RowTile &x : tiles)
+        if (!x.wide) {
+            recs_left -= 1;
+            rows_left -= (int64_t)KV * x.ntok * G;
         }
-        const double est = std::max(longest, sum / a->n_sm + 0.5 * longest);
-        if (part != 0.0 && (recs > a->rec_cap || rows > a->part_cap)) continue;
-        if (est < best) {
-            best = est;
-            limit = most;
+    const double wide_limit = split_limit(tiles, true, KV, G, a->n_sm * Shape<128, true>::CTAS, &recs_left, &rows_left);
+    for (const RowTile &x : tiles)
+        if (!x.wide) {
+            recs_left += 1;
+            rows_left += (int64_t)KV * x.ntok * G;
         }
-    }
+    const double narrow_limit = split_limit(tiles, false, KV, G, a->n_sm * Shape<128, false>::CTAS, &recs_left, &rows_left);
     struct Rec {
         float cost;
         int tile, t0, t1, part;
-        bool direct;
+        bool direct, wide;
     };
     std::vector<Rec> recs;
+    int n_wide = 0;
     int64_t part = 0;
     bool partial = false;
     std::vector<uint8_t> seen(T, 0);
     for (size_t k = 0; k < tiles.size(); ++k) {
         const RowTile &x = tiles[k];
         const int n = (x.len + TT - 1) / TT, rows = x.ntok * G;
-        const int per_item = (int)std::min<double>(n, std::max(1.0, std::floor(limit / TILE_COST[x.cls])));
-        const int items = (n + per_item - 1) / per_item;
+        int per_item;
+        const int items = items_of(x, x.wide ? wide_limit : narrow_limit, &per_item);
         const bool direct = items == 1 && x.alone;
         for (int i = 0; i < items; ++i) {
             // splits of equal length but for rounding
             const int a0 = (int)((int64_t)n * i / items), a1 = (int)((int64_t)n * (i + 1) / items);
-            recs.push_back({TILE_COST[x.cls] * (a1 - a0), (int)k, a0 * TT, std::min(x.len, a1 * TT),
-                            direct ? 0 : (int)(part + (int64_t)i * KV * rows), direct});
+            recs.push_back({tile_cost(x) * (a1 - a0), (int)k, a0 * TT, std::min(x.len, a1 * TT),
+                            direct ? 0 : (int)(part + (int64_t)i * KV * rows), direct, x.wide});
+            n_wide += x.wide;
         }
         for (int i = 0; i < x.ntok; ++i) {
             const int t = order[x.tok + i];
@@ -1272,7 +1321,7 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
         }
     }
     for (int t = 0; t < T && !partial; ++t) partial = !seen[t];  // a row that sees nothing is the combine's too
-    std::stable_sort(recs.begin(), recs.end(), [](const Rec &x, const Rec &y) { return x.cost > y.cost; });
+    std::stable_sort(recs.begin(), recs.end(), [](const Rec &x, const Rec &y) { return x.wide != y.wide ? x.wide : x.cost > y.cost; });
     int32_t *rw = w + a->rec_at;
     for (const Rec &r : recs) {
         const RowTile &x = tiles[r.tile];
@@ -1286,7 +1335,10 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
         rw[RC_PART] = r.part;
         rw += REC_WORDS;
     }
-    w[HD_RECS] = (int)recs.size();
+    w[HD_WIDE] = n_wide;
+    w[HD_NARROW] = (int)recs.size() - n_wide;
+    a->wide = n_wide > 0;
+    a->narrow = (int)recs.size() > n_wide;
     w[HD_PARTIAL] = partial ? 1 : 0;
     a->partial = partial;
     int32_t *pg = w + a->pages_at;
@@ -1295,12 +1347,42 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     return (size_t)a->pages_at + own_pages + grp_pages;
 }
 
-template <int D>
-cudaError_t launch_attn(const AttnParams &p, int n_sm, bool combine, cudaStream_t stream)
+template <class L>
+cudaError_t prepare_tiles()
 {
-    attn_tile_kernel<D><<<n_sm, ATTN_THREADS, Layout<D>::BYTES, stream>>>(p);
-    cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess || !combine) return e;
+    return cudaFuncSetAttribute(attn_tile_kernel<L>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::BYTES);
+}
+
+template <class L>
+cudaError_t launch_tiles(const AttnParams &p, int n_sm, bool after_wide, cudaStream_t stream)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(n_sm * L::CTAS, 1, 1);
+    cfg.blockDim = dim3(L::THREADS, 1, 1);
+    cfg.dynamicSmemBytes = L::BYTES;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = after_wide ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, attn_tile_kernel<L>, p);
+}
+
+// The wide items, the narrow ones (which fill the SMs as the wide ones
+// end) and the rows they share.
+template <int D>
+cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, bool combine, cudaStream_t stream)
+{
+    if (wide) {
+        const cudaError_t e = launch_tiles<Shape<D, true>>(p, n_sm, false, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (narrow) {
+        const cudaError_t e = launch_tiles<Shape<D, false>>(p, n_sm, wide, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (!combine) return cudaSuccess;
     const int64_t rows = (int64_t)p.max_tok * p.n_heads;
     const int64_t blocks = std::min<int64_t>((rows + COMBINE_WARPS - 1) / COMBINE_WARPS, 16 * (int64_t)n_sm);
     attn_combine_kernel<D><<<(unsigned)blocks, 32 * COMBINE_WARPS, 0, stream>>>(p);
@@ -1337,8 +1419,8 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
         return ctx_fail(ctx, st, "%s", what);
     };
     if (cudaDeviceGetAttribute(&a->n_sm, cudaDevAttrMultiProcessorCount, ctx_device(ctx)) != cudaSuccess ||
-        cudaFuncSetAttribute(attn_tile_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<64>::BYTES) != cudaSuccess ||
-        cudaFuncSetAttribute(attn_tile_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, Layout<128>::BYTES) != cudaSuccess)
+        prepare_tiles<Shape<64, true>>() != cudaSuccess || prepare_tiles<Shape<64, false>>() != cudaSuccess ||
+        prepare_tiles<Shape<128, true>>() != cudaSuccess || prepare_tiles<Shape<128, false>>() != cudaSuccess)
         return fail_with(SALT_ERR_CUDA, "cannot prepare the attention kernel");
     // codes as rows of D / 2 two-byte elements
     const int64_t rows = (int64_t)kv->n_layers * d.n_pages * d.heads * d.page;
@@ -1348,7 +1430,7 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
     // Items: without splits at most one per request's and per group's row
     // tile; with them the plan keeps within the rest.  Partial rows: two per
     // row without splits.
-    const int G = c->n_heads / d.heads, per = std::max(1, R_MAX / G);
+    const int G = c->n_heads / d.heads, per = std::max(1, WIDE_ROWS / G);
     a->rec_cap = c->max_seqs + c->max_groups + 2 * (c->max_tokens / per + 1) + 16 * a->n_sm;
     a->part_cap = 2ll * c->max_tokens * c->n_heads + 512ll * a->n_sm;
     if (a->part_cap >= (1ll << 31)) return fail_with(SALT_ERR_INVALID_ARG, "max_tokens times n_heads is too large");
@@ -1447,9 +1529,9 @@ try {
         if (std::find(a->use_streams.begin(), a->use_streams.end(), stream) == a->use_streams.end())
             a->use_streams.push_back(stream);
     }
-    // a captured run may be replayed for a plan that needs the combine
+    // a captured run may be replayed for a plan that needs other launches
     cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    if (!a->partial) SALT_CUDA_OR_FAIL(ctx, cudaStreamIsCapturing(stream, &cap));
+    if (!(a->wide && a->narrow && a->partial)) SALT_CUDA_OR_FAIL(ctx, cudaStreamIsCapturing(stream, &cap));
     AttnParams p;
     p.kmap = a->kmap;
     p.vmap = a->vmap;
@@ -1471,8 +1553,9 @@ try {
     p.pages_at = a->pages_at;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.err = ctx_error_word(ctx);
-    const bool combine = a->partial || cap != cudaStreamCaptureStatusNone;
-    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_attn<128>(p, a->n_sm, combine, stream) : launch_attn<64>(p, a->n_sm, combine, stream));
+    const bool all = cap != cudaStreamCaptureStatusNone, wide = a->wide || all, narrow = a->narrow || all, combine = a->partial || all;
+    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_attn<128>(p, a->n_sm, wide, narrow, combine, stream)
+                                         : launch_attn<64>(p, a->n_sm, wide, narrow, combine, stream));
     return SALT_OK;
 } catch (const std::bad_alloc &) {
     return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
