@@ -648,10 +648,9 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
 // constants of its columns, the largest exponent of its values.  W warps, this
 // one the w-th.
 template <class L>
-__device__ __noinline__ void stage_queries(const AttnParams &p, uint32_t base, int idx, int n_item, int w, int W)
+__device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base, const Item &it, int n_item, int w, int W)
 {
     const int KV = p.kv.heads, G = p.n_heads / KV, lane = threadIdx.x & 31;
-    const Item it = load_item<L>(p, idx, G);
     const int cw = 16 << (it.flags & 3), R = L::NWG * cw;
     const int g_inv = (65535 + G) / G, per_inv = (65535 + it.per) / it.per;  // quotients by products: rows are below 129, divisors at most 64
     const int32_t *order = p.plan + p.order_at + it.tok;
@@ -662,6 +661,10 @@ __device__ __noinline__ void stage_queries(const AttnParams &p, uint32_t base, i
         sts32(info + L::IN_LIM + 4 * col, (uint32_t)lim);
         sts32(info + L::IN_ROW + 4 * col, (uint32_t)row);
     };
+    // exponents of 16 values a lane (their pages' numbers are on their way while the queries are)
+    const int t_first = it.t0 + (w * 32 + lane) * 16, t_step = W * 32 * 16;
+    const int32_t *pages = p.plan + p.pages_at + it.pages;
+    int page = t_first < it.t1 ? __ldg(pages + (t_first >> p.kv.page_log2)) : 0;
     constexpr int LPR = L::D / 8;           // lanes a row, eight elements each
     constexpr int RPW = 32 / LPR;        // rows a warp deals with at a time
     constexpr int AT_ONCE = L::WIDE ? 4 : 2;  // loads of a lane under way together
@@ -731,12 +734,12 @@ __device__ __noinline__ void stage_queries(const AttnParams &p, uint32_t base, i
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
         if (ncol + lane < ((ncol + CH - 1) & ~(CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
     }
-    // the largest exponent of the range's values, 16 tokens a lane
+    // the largest exponent of the range's values
     uint32_t top = 0;
-    for (int t = it.t0 + (w * 32 + lane) * 16; t < it.t1; t += W * 32 * 16) {
-        const int page = __ldg(p.plan + p.pages_at + it.pages + (t >> p.kv.page_log2));
+    for (int t = t_first; t < it.t1; t += t_step) {
         const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
         const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
+        if (t + t_step < it.t1) page = __ldg(pages + ((t + t_step) >> p.kv.page_log2));
         const uint32_t x[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -763,7 +766,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     const uint32_t base = smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int KV = p.kv.heads, G = p.n_heads / KV;
-    if (L::WIDE) pdl_launch_dependents();  // the narrow items need nothing of the wide ones
+    pdl_launch_dependents();  // (the narrow items need nothing of the wide ones, the combine waits)
     if (p.plan[HD_TOKENS] > p.max_tok) {
         if (blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
         if (!L::WIDE) pdl_wait();
@@ -807,10 +810,32 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool ok = true;
-    constexpr int OTHERS = L::THREADS - 32;
-    if (warp > 0) {  // the first item's queries by every warp but the one that starts its loads
-        stage_queries<L>(p, base, blockIdx.x, 0, warp - 1, OTHERS / 32);
-        named_sync(1 + L::NWG, OTHERS);
+    if (warp > 0) {
+        // ------------------------------------------------ queries: the first item's by every warp but the one that starts its
+        // loads, the later ones' by warps 2 and 3 alongside the items before them
+        constexpr int OTHERS = L::THREADS - 32;
+        const bool stays = warp == 2 || warp == 3;
+        for (int r = 0; ok; ++r) {
+            const int idx = item_index(r);
+            if (idx >= n_items) break;
+            if (r > 1) {
+                ok = wait_bar(base + L::Q_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead) &&
+                     wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+            }
+            stage_queries<L>(p, base, load_item<L>(p, idx, G), r, r == 0 ? warp - 1 : warp - 2, r == 0 ? OTHERS / 32 : 2);
+            if (r == 0) {
+                named_sync(1 + L::NWG, OTHERS);
+                if (!stays) break;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
     }
 
     if (warp == 0) {
@@ -950,25 +975,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
             }
             __syncwarp();
         }
-    } else if (warp < 4) {
-        // ------------------------------------------------ queries: rows scaled by a power of two and split in hi + lo
-        const int w = warp - 2;
-        for (int r = 0; ok; ++r) {
-            const int idx = item_index(r);
-            if (idx >= n_items) break;
-            if (r > 1) ok = wait_bar(base + L::Q_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
-            if (r > 1) ok = ok && wait_bar(base + L::O_FREE + 8 * (r & 1), ((r - 2) >> 1) & 1, dead);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) break;
-            if (r > 0) stage_queries<L>(p, base, idx, r, w, 2);
-            __syncwarp();
-            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * (r & 1));
-        }
-        if (!ok && lane == 0) {
-            *dead = 1;
-            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
-        }
-    } else {
+    } else if (warp >= 4) {
         // ------------------------------------------------ softmax and results
         Soft s;
         s.base = base;
@@ -1002,54 +1009,87 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
 }
 
 // The rows that several items share (and those no item has): a warp per row,
-//     out = sum_i 2^(l_i - L) o_i,   L = log2 sum_i 2^(l_i).
+//     out = sum_i 2^(l_i - L) o_i,   L = log2 sum_i 2^(l_i),
+// the logarithms of 32 items at a time over the lanes, their rows four at a time.
 constexpr int COMBINE_WARPS = 4;
 
 template <int D>
 __global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const __grid_constant__ AttnParams p)
 {
     constexpr int E = D / 32;
-    const int T = p.plan[HD_TOKENS], H = p.n_heads, G = H / p.kv.heads, lane = threadIdx.x & 31;
-    if (T > p.max_tok || !p.plan[HD_PARTIAL]) return;
-    for (int64_t row = (int64_t)blockIdx.x * COMBINE_WARPS + (threadIdx.x >> 5); row < (int64_t)T * H; row += (int64_t)gridDim.x * COMBINE_WARPS) {
-        const int t = (int)(row / H), h = (int)(row - (int64_t)t * H), kh = h / G, g = h - kh * G;
+    const int T = __ldg(p.plan + HD_TOKENS), H = p.n_heads, KV = p.kv.heads, G = H / KV, lane = threadIdx.x & 31;
+    const int partial = __ldg(p.plan + HD_PARTIAL);
+    const int row = blockIdx.x * COMBINE_WARPS + (threadIdx.x >> 5), t = row / H, h = row - t * H, kh = h / G, g = h - kh * G;
+    const bool live = T <= p.max_tok && partial && t < T;
+    int4 a = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 1, 0);
+    if (live) {
         const int4 *rec = reinterpret_cast<const int4 *>(p.plan + p.tok_at + t * TOK_WORDS);
-        const int4 a = __ldg(rec), b = __ldg(rec + 1);
-        if (b.z) continue;  // written by its only item
-        const int own = a.x, own_rows = a.y, own_n = a.z, pre = a.w, pre_rows = b.x, n = own_n + b.y;
-        auto place = [&](int i) -> int64_t {  // the row's i-th partial
-            return i < own_n ? own + (int64_t)(i * p.kv.heads + kh) * own_rows + g
-                             : pre + (int64_t)((i - own_n) * p.kv.heads + kh) * pre_rows + g;
-        };
-        float top = -INFINITY;
-        bool nan = false;
-        for (int i = lane; i < n; i += 32) {
-            const float l = p.part_l[place(i)];
-            top = fmaxf(top, l);
-            nan |= !(l == l);
-        }
+        a = __ldg(rec);
+        b = __ldg(rec + 1);
+    }
+    pdl_wait();    // (the plan is older than the items' kernels)
+    if (b.z) return;  // no such row, or written by its only item
+    const int own_n = a.z, n = own_n + b.y;
+    auto place = [&](int i) -> int {  // the row's i-th partial
+        return i < own_n ? a.x + (i * KV + kh) * a.y + g : a.w + ((i - own_n) * KV + kh) * b.x + g;
+    };
+    float top = -INFINITY, sum = 0.f, o[E];
+    bool nan = false;
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        nan = __any_sync(0xffffffffu, nan);
-        float sum = 0.f, o[E];
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        const int mine = i0 + lane < n ? place(i0 + lane) : 0;
+        const float l = i0 + lane < n ? __ldcg(p.part_l + mine) : -INFINITY;
+        nan |= !(l == l);
+        float m = fmaxf(top, l);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = 0.f;
-        if (top > -INFINITY) {
-            for (int i = 0; i < n; ++i) {
-                const int64_t at = place(i);
-                const float w = ex2(p.part_l[at] - top);
-                const float *src = p.part_o + at * D + lane * E;
-                sum += w;
+        for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+        if (m == -INFINITY) continue;
+        const float keep = ex2(top - m), w = ex2(l - m);
+        top = m;
+        sum *= keep;
 #pragma unroll
-                for (int e = 0; e < E; ++e) o[e] = fmaf(w, src[e], o[e]);
+        for (int e = 0; e < E; ++e) o[e] *= keep;
+        const int k = min(32, n - i0);
+        for (int i = 0; i < k; i += 4) {
+            float f[4], v[4][E];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int at = __shfl_sync(0xffffffffu, mine, min(i + u, k - 1));
+                f[u] = i + u < k ? __shfl_sync(0xffffffffu, w, i + u) : 0.f;
+                if constexpr (E == 4) {
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.part_o + (int64_t)at * D + lane * E));
+                    v[u][0] = x.x;
+                    v[u][1] = x.y;
+                    v[u][2] = x.z;
+                    v[u][3] = x.w;
+                } else {
+                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(p.part_o + (int64_t)at * D + lane * E));
+                    v[u][0] = x.x;
+                    v[u][1] = x.y;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                sum += f[u];
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (i + u < k) o[e] = fmaf(f[u], v[u][e], o[e]);
             }
         }
-        const float bad = __uint_as_float(0x7fc00000u), inv = nan ? bad : sum > 0.f ? 1.f / sum : 0.f;
-        uint16_t *dst = p.out + t * p.out_stride + h * D + lane * E;
-#pragma unroll
-        for (int e = 0; e < E; ++e) dst[e] = f_to_bf16(o[e] * inv);
-        if (p.lse && lane == 0) p.lse[row] = nan ? bad : sum > 0.f ? (top + log2f(sum)) * 0.693147180559945f : -INFINITY;
     }
+    nan = __any_sync(0xffffffffu, nan);
+    const float bad = __uint_as_float(0x7fc00000u), inv = nan ? bad : sum > 0.f ? 1.f / sum : 0.f;
+    uint32_t out[E / 2];
+#pragma unroll
+    for (int e = 0; e < E; e += 2) {
+        const __nv_bfloat162 r = __floats2bfloat162_rn(o[e] * inv, o[e + 1] * inv);
+        out[e / 2] = *reinterpret_cast<const uint32_t *>(&r);
+    }
+    uint16_t *dst = p.out + t * p.out_stride + h * D + lane * E;
+    if constexpr (E == 4) *reinterpret_cast<uint2 *>(dst) = make_uint2(out[0], out[1]);
+    else *reinterpret_cast<uint32_t *>(dst) = out[0];
+    if (p.lse && lane == 0) p.lse[row] = nan ? bad : sum > 0.f ? (top + log2f(sum)) * 0.693147180559945f : -INFINITY;
 }
 
 }  // namespace
@@ -1383,10 +1423,17 @@ cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, b
         if (e != cudaSuccess) return e;
     }
     if (!combine) return cudaSuccess;
-    const int64_t rows = (int64_t)p.max_tok * p.n_heads;
-    const int64_t blocks = std::min<int64_t>((rows + COMBINE_WARPS - 1) / COMBINE_WARPS, 16 * (int64_t)n_sm);
-    attn_combine_kernel<D><<<(unsigned)blocks, 32 * COMBINE_WARPS, 0, stream>>>(p);
-    return cudaGetLastError();
+    // (rows in all are below 2^31: partial rows, twice as many, are)
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3((p.max_tok * p.n_heads + COMBINE_WARPS - 1) / COMBINE_WARPS, 1, 1);
+    cfg.blockDim = dim3(32 * COMBINE_WARPS, 1, 1);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, attn_combine_kernel<D>, p);
 }
 
 }  // namespace
