@@ -561,6 +561,7 @@ salt_status salt_align_loss(int32_t n, const salt_align_pair *pairs, float eps, 
  * zeros has e = 0; a row with an infinity or a NaN is stored as e = 255 and
  * zero codes and stands for NaN throughout.  A slot is page * page_tokens +
  * offset in the page.  head_dim is 64 or 128, page_tokens 16, 32, 64 or 128;
+ * n_kv_heads <= 1024 and
  * n_layers * n_pages * n_kv_heads * page_tokens < 2^31.
  */
 typedef struct salt_kv salt_kv;

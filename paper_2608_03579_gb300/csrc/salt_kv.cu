@@ -6,6 +6,7 @@
 // 2^8 gives the smallest k with a <= 448 * 2^k: E - 8 where f <= 1.75, else E - 7,
 // all read off the bits of a.  2^-k is a normal float for every k in [-126, 121],
 // so x * 2^-k is exact and the conversion to e4m3 is the only rounding.
+#include <algorithm>
 #include <new>
 
 #include <cuda_fp16.h>
@@ -18,6 +19,7 @@ namespace salt {
 namespace {
 
 constexpr int KV_THREADS = 256;
+constexpr int ROWS = 4;  // rows a thread
 
 __device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
 {
@@ -42,89 +44,126 @@ __device__ __forceinline__ uint32_t row_exp(uint32_t a)
     return (uint32_t)max(e, 1);
 }
 
-// One row per D / 8 lanes, a lane 8 elements; rows are (token, k or v, head).
+// Rows are (token, k or v, head), one per D / 8 lanes of 8 elements each.  Both
+// kernels only move bytes: a thread deals with ROWS rows so that enough of
+// them are under way (KV_THREADS / (D / 8) apart), and reads and writes past the L2 what it
+// will not meet again.  Measured at 128-wide heads (GB/s of bytes read and written), see ROWS.
+struct KvRow {
+    int t, h;
+    bool live, is_v;
+};
+
 template <int D>
-__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvDev c, int64_t layer, int n_tokens, const uint16_t *k,
-                                                              int64_t k_stride, const uint16_t *v, int64_t v_stride,
-                                                              const int32_t *slots, uint32_t *err)
+__device__ __forceinline__ KvRow kv_row(const KvDev &c, int n_tokens, uint32_t heads2_inv, int k)
 {
-    constexpr int LPR = D / 8;
-    const int64_t rows = (int64_t)n_tokens * 2 * c.heads;
-    const int64_t row = ((int64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LPR;
-    const int part = threadIdx.x % LPR;
-    const bool live = row < rows;  // every lane stays for the shuffles
-    const int t = live ? (int)(row / (2 * c.heads)) : 0;
-    const int kh = live ? (int)(row - (int64_t)t * 2 * c.heads) : 0;
-    const bool is_v = kh >= c.heads;
-    const int h = is_v ? kh - c.heads : kh;
-    uint4 x = make_uint4(0, 0, 0, 0);
-    int slot = -1;
-    if (live) {
-        const uint16_t *src = (is_v ? v + (int64_t)t * v_stride : k + (int64_t)t * k_stride) + (int64_t)h * D + part * 8;
-        x = __ldcs(reinterpret_cast<const uint4 *>(src));
-        slot = __ldg(slots + t);
-    }
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    uint32_t a = 0;  // magnitudes of bf16 order like their bits
-#pragma unroll
-    for (int i = 0; i < 4; ++i) a = max(a, max((w[i] << 16) & 0x7fffffffu, w[i] & 0x7fff0000u));
-#pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
-    const int page = slot >> c.page_log2;
-    if (slot < 0 || page >= c.n_pages) {
-        if (live && slot != -1 && part == 0) atomicOr(err, SALT_DEVERR_KV_SLOT);
-        return;
-    }
-    const uint32_t e = row_exp(a);
-    const float inv = __uint_as_float(e == 255u ? 0u : (254u - max(e, 1u)) << 23);
-    uint32_t codes[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t p = w[2 * i], q = w[2 * i + 1];
-        codes[i] = (uint32_t)e4m3x2(__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv) |
-                   (uint32_t)e4m3x2(__uint_as_float(q << 16) * inv, __uint_as_float(q & 0xffff0000u) * inv) << 16;
-    }
-    if (e == 255u) codes[0] = codes[1] = 0;
-    const int64_t at = ((layer * c.n_pages + page) * c.heads + h) * c.page + (slot & (c.page - 1));
-    *reinterpret_cast<uint2 *>((is_v ? c.v : c.k) + at * D + part * 8) = make_uint2(codes[0], codes[1]);
-    if (part == 0) (is_v ? c.v_exp : c.k_exp)[at] = (uint8_t)e;
+    constexpr int PER = KV_THREADS / (D / 8);  // rows a block deals with at a time
+    const uint32_t row = blockIdx.x * (uint32_t)(PER * ROWS) + k * PER + threadIdx.x / (D / 8);
+    const uint32_t n = 2 * c.heads;
+    const uint32_t t = __umulhi(row, heads2_inv);  // row / (2 heads)
+    const int kh = (int)(row - t * n);
+    KvRow r;
+    r.live = t < (uint32_t)n_tokens;
+    r.t = r.live ? (int)t : 0;
+    r.is_v = kh >= c.heads;
+    r.h = r.is_v ? kh - c.heads : kh;
+    return r;
 }
 
 template <int D>
-__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvDev c, int64_t layer, int n_tokens, const int32_t *slots,
-                                                             uint16_t *k, int64_t k_stride, uint16_t *v,
+__global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvDev c, int64_t layer, int n_tokens, uint32_t heads2_inv,
+                                                              const uint16_t *k, int64_t k_stride, const uint16_t *v,
+                                                              int64_t v_stride, const int32_t *slots, uint32_t *err)
+{
+    constexpr int LPR = D / 8;
+    const int part = threadIdx.x % LPR;
+    KvRow r[ROWS];
+    uint4 x[ROWS];
+    int slot[ROWS];
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        r[i] = kv_row<D>(c, n_tokens, heads2_inv, i);
+        x[i] = make_uint4(0, 0, 0, 0);
+        slot[i] = -1;
+        if (r[i].live) {  // every lane stays for the shuffles
+            const uint16_t *src = (r[i].is_v ? v + r[i].t * v_stride : k + r[i].t * k_stride) + r[i].h * D + part * 8;
+            x[i] = __ldcs(reinterpret_cast<const uint4 *>(src));
+            slot[i] = __ldg(slots + r[i].t);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t a = 0;  // magnitudes of bf16 order like their bits
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a = max(a, max((w[e] << 16) & 0x7fffffffu, w[e] & 0x7fff0000u));
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const int page = slot[i] >> c.page_log2;
+        if (slot[i] < 0 || page >= c.n_pages) {
+            if (slot[i] != -1 && part == 0) atomicOr(err, SALT_DEVERR_KV_SLOT);
+            continue;
+        }
+        const uint32_t e = row_exp(a);
+        const float inv = __uint_as_float(e == 255u ? 0u : (254u - max(e, 1u)) << 23);
+        uint32_t codes[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t p = w[2 * h], q = w[2 * h + 1];
+            codes[h] = (uint32_t)e4m3x2(__uint_as_float(p << 16) * inv, __uint_as_float(p & 0xffff0000u) * inv) |
+                       (uint32_t)e4m3x2(__uint_as_float(q << 16) * inv, __uint_as_float(q & 0xffff0000u) * inv) << 16;
+        }
+        if (e == 255u) codes[0] = codes[1] = 0;
+        const int64_t at = ((layer * c.n_pages + page) * c.heads + r[i].h) * c.page + (slot[i] & (c.page - 1));
+        *reinterpret_cast<uint2 *>((r[i].is_v ? c.v : c.k) + at * D + part * 8) = make_uint2(codes[0], codes[1]);
+        if (part == 0) (r[i].is_v ? c.v_exp : c.k_exp)[at] = (uint8_t)e;
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvDev c, int64_t layer, int n_tokens, uint32_t heads2_inv,
+                                                             const int32_t *slots, uint16_t *k, int64_t k_stride, uint16_t *v,
                                                              int64_t v_stride, uint32_t *err)
 {
     constexpr int LPR = D / 8;
-    const int64_t rows = (int64_t)n_tokens * 2 * c.heads;
-    const int64_t row = ((int64_t)blockIdx.x * KV_THREADS + threadIdx.x) / LPR;
     const int part = threadIdx.x % LPR;
-    if (row >= rows) return;
-    const int t = (int)(row / (2 * c.heads));
-    const int kh = (int)(row - (int64_t)t * 2 * c.heads);
-    const bool is_v = kh >= c.heads;
-    const int h = is_v ? kh - c.heads : kh;
-    const int slot = __ldg(slots + t);
-    const int page = slot >> c.page_log2;
-    uint32_t out[4] = {0, 0, 0, 0};
-    if (slot >= 0 && page < c.n_pages) {
-        const int64_t at = ((layer * c.n_pages + page) * c.heads + h) * c.page + (slot & (c.page - 1));
-        const uint2 codes = __ldcs(reinterpret_cast<const uint2 *>((is_v ? c.v : c.k) + at * D + part * 8));
-        const uint32_t e = (is_v ? c.v_exp : c.k_exp)[at];
-        const float scale = __uint_as_float(e == 255u ? 0x7fc00000u : e << 23);
-        const uint32_t two[2] = {codes.x, codes.y};
+    KvRow r[ROWS];
+    int slot[ROWS];
+    uint2 codes[ROWS];
+    uint32_t e[ROWS];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t h2 = f16x2_of_e4m3x2((uint16_t)(two[i >> 1] >> (16 * (i & 1))));
+    for (int i = 0; i < ROWS; ++i) {
+        r[i] = kv_row<D>(c, n_tokens, heads2_inv, i);
+        slot[i] = r[i].live ? __ldg(slots + r[i].t) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int page = slot[i] >> c.page_log2;
+        codes[i] = make_uint2(0, 0);
+        e[i] = 0;
+        if (slot[i] >= 0 && page < c.n_pages) {
+            const int64_t at = ((layer * c.n_pages + page) * c.heads + r[i].h) * c.page + (slot[i] & (c.page - 1));
+            codes[i] = __ldcs(reinterpret_cast<const uint2 *>((r[i].is_v ? c.v : c.k) + at * D + part * 8));
+            e[i] = (r[i].is_v ? c.v_exp : c.k_exp)[at];
+        } else if (slot[i] != -1 && part == 0) {
+            atomicOr(err, SALT_DEVERR_KV_SLOT);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        if (!r[i].live) continue;
+        const float scale = __uint_as_float(e[i] == 255u ? 0x7fc00000u : e[i] << 23);
+        const uint32_t two[2] = {codes[i].x, codes[i].y};
+        uint32_t out[4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+            const uint32_t h2 = f16x2_of_e4m3x2((uint16_t)(two[h >> 1] >> (16 * (h & 1))));
             const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h2));
             const __nv_bfloat162 b = __floats2bfloat162_rn(f.x * scale, f.y * scale);
-            out[i] = *reinterpret_cast<const uint32_t *>(&b);
+            out[h] = *reinterpret_cast<const uint32_t *>(&b);
         }
-    } else if (slot != -1 && part == 0) {
-        atomicOr(err, SALT_DEVERR_KV_SLOT);
+        uint16_t *dst = (r[i].is_v ? v + r[i].t * v_stride : k + r[i].t * k_stride) + r[i].h * D + part * 8;
+        __stcs(reinterpret_cast<uint4 *>(dst), make_uint4(out[0], out[1], out[2], out[3]));
     }
-    uint16_t *dst = (is_v ? v + (int64_t)t * v_stride : k + (int64_t)t * k_stride) + (int64_t)h * D + part * 8;
-    __stcs(reinterpret_cast<uint4 *>(dst), make_uint4(out[0], out[1], out[2], out[3]));
 }
 
 salt_status check_rows(salt_kv *kv, int32_t layer, int32_t n_tokens, const void *k, int64_t k_stride, const void *v,
@@ -146,10 +185,18 @@ salt_status check_rows(salt_kv *kv, int32_t layer, int32_t n_tokens, const void 
     return SALT_OK;
 }
 
-int64_t row_blocks(const salt_kv *kv, int32_t n_tokens)
+// Tokens that one launch may take: a row's number times 2 heads stays below 2^32, so that its quotient by 2
+// heads is the high half of its product with floor(2^32 / (2 heads)) + 1.
+int32_t launch_tokens(const salt_kv *kv)
 {
-    const int64_t threads = (int64_t)n_tokens * 2 * kv->dev.heads * (kv->dev.dim / 8);
-    return (threads + KV_THREADS - 1) / KV_THREADS;
+    const int64_t n = 2ll * kv->dev.heads, slack = (int64_t)KV_THREADS * ROWS;
+    return (int32_t)std::max<int64_t>(1, ((1ll << 32) / n - slack) / n);
+}
+uint32_t heads2_inv(const salt_kv *kv) { return (uint32_t)((1ull << 32) / (2ull * kv->dev.heads) + 1); }
+unsigned row_blocks(const salt_kv *kv, int32_t n_tokens)
+{
+    const int64_t per = (int64_t)KV_THREADS / (kv->dev.dim / 8) * ROWS;
+    return (unsigned)((2ll * n_tokens * kv->dev.heads + per - 1) / per);
 }
 
 }  // namespace
@@ -171,6 +218,7 @@ salt_status salt_kv_create(salt_ctx *ctx, const salt_kv_config *c, salt_kv **out
         return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "head_dim %d is not 64 or 128", c->head_dim);
     if (c->page_tokens < 16 || c->page_tokens > SALT_MAX_KV_PAGE || (c->page_tokens & (c->page_tokens - 1)))
         return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "page_tokens %d is not 16, 32, 64 or 128", c->page_tokens);
+    if (c->n_kv_heads > 1024) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%d key/value heads, at most 1024", c->n_kv_heads);
     // rows are numbered in 32 bits (each factor is below 2^31, so the products below cannot overflow unseen)
     int64_t rows = (int64_t)c->n_layers * c->n_pages;
     if (rows < (1ll << 31)) rows *= c->n_kv_heads;
@@ -208,13 +256,15 @@ salt_status salt_kv_write(salt_kv *kv, int32_t layer, int32_t n_tokens, const vo
     salt_status st = check_rows(kv, layer, n_tokens, k, k_stride, v, v_stride, slots);
     if (st != SALT_OK || n_tokens == 0) return st;
     if (!ctx_select_device(kv->ctx)) return ctx_fail(kv->ctx, SALT_ERR_CUDA, "cannot select the device");
-    const int64_t blocks = row_blocks(kv, n_tokens);
-    if (blocks > 0x7fffffff) return ctx_fail(kv->ctx, SALT_ERR_TOO_MANY_TOKENS, "%d tokens in one call", n_tokens);
     auto kernel = kv->dev.dim == 128 ? kv_write_kernel<128> : kv_write_kernel<64>;
-    kernel<<<(unsigned)blocks, KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
-        kv->dev, layer, n_tokens, static_cast<const uint16_t *>(k), k_stride, static_cast<const uint16_t *>(v), v_stride, slots,
-        ctx_error_word(kv->ctx));
-    SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+    const int32_t most = launch_tokens(kv);
+    for (int32_t t = 0; t < n_tokens; t += most) {
+        const int32_t n = std::min(most, n_tokens - t);
+        kernel<<<row_blocks(kv, n), KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+            kv->dev, layer, n, heads2_inv(kv), static_cast<const uint16_t *>(k) + t * k_stride, k_stride,
+            static_cast<const uint16_t *>(v) + t * v_stride, v_stride, slots + t, ctx_error_word(kv->ctx));
+        SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+    }
     return SALT_OK;
 }
 
@@ -226,13 +276,15 @@ salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int
     salt_status st = check_rows(kv, layer, n_tokens, k, k_stride, v, v_stride, slots);
     if (st != SALT_OK || n_tokens == 0) return st;
     if (!ctx_select_device(kv->ctx)) return ctx_fail(kv->ctx, SALT_ERR_CUDA, "cannot select the device");
-    const int64_t blocks = row_blocks(kv, n_tokens);
-    if (blocks > 0x7fffffff) return ctx_fail(kv->ctx, SALT_ERR_TOO_MANY_TOKENS, "%d tokens in one call", n_tokens);
     auto kernel = kv->dev.dim == 128 ? kv_read_kernel<128> : kv_read_kernel<64>;
-    kernel<<<(unsigned)blocks, KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
-        kv->dev, layer, n_tokens, slots, static_cast<uint16_t *>(k), k_stride, static_cast<uint16_t *>(v), v_stride,
-        ctx_error_word(kv->ctx));
-    SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+    const int32_t most = launch_tokens(kv);
+    for (int32_t t = 0; t < n_tokens; t += most) {
+        const int32_t n = std::min(most, n_tokens - t);
+        kernel<<<row_blocks(kv, n), KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+            kv->dev, layer, n, heads2_inv(kv), slots + t, static_cast<uint16_t *>(k) + t * k_stride, k_stride,
+            static_cast<uint16_t *>(v) + t * v_stride, v_stride, ctx_error_word(kv->ctx));
+        SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+    }
     return SALT_OK;
 }
 

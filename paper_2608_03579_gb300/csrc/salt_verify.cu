@@ -5,14 +5,23 @@
 // are taken in whole units of 2^-40 (a weight is at most 1 and a vocabulary at
 // most 2^20, so 64 bits hold every sum), which makes the sums exact: any split
 // of the row over threads gives the same token.
+//
+// A request's work is reading one row of p and one of q (1 MB for 131,072
+// tokens), so it is spread over a cluster of CTAs: each sums its share, the
+// sums meet in shared memory, and the one warp whose share holds the drawn
+// place goes over that share again.
+#include <cooperative_groups.h>
+
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
 
 namespace salt {
 namespace {
 
-constexpr int VF_THREADS = 1024;
+constexpr int VF_THREADS = 512;
 constexpr int VF_WARPS = VF_THREADS / 32;
+constexpr int VF_CLUSTER = 8;         // CTAs a request at most
+constexpr int VF_SHARE = 2048;        // tokens that are worth another CTA
 
 struct VerifyParams {
     const int32_t *ptr, *tok;
@@ -26,14 +35,58 @@ struct VerifyParams {
 // a weight in units of 2^-40; NaN and what is not above zero count as 0
 __device__ __forceinline__ int64_t units(float w) { return w > 0.f ? __float2ll_rz(fminf(w, 1.f) * 1099511627776.f) : 0ll; }
 
+// Four weights from v on (those below end), p and q (or none) read as one
+// 16-byte piece where VEC says that rows lie on such boundaries.
+template <bool VEC>
+__device__ __forceinline__ void weights4(const float *p, const float *q, int v, int end, float (&w)[4])
+{
+    float a[4] = {0.f, 0.f, 0.f, 0.f}, b[4] = {0.f, 0.f, 0.f, 0.f};
+    if (VEC && v + 4 <= end) {
+        const float4 x = __ldg(reinterpret_cast<const float4 *>(p + v));
+        a[0] = x.x, a[1] = x.y, a[2] = x.z, a[3] = x.w;
+        if (q) {
+            const float4 y = __ldg(reinterpret_cast<const float4 *>(q + v));
+            b[0] = y.x, b[1] = y.y, b[2] = y.z, b[3] = y.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (v + i < end) {
+                a[i] = __ldg(p + v + i);
+                if (q) b[i] = __ldg(q + v + i);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = q ? __fsub_rn(a[i], b[i]) : a[i];
+}
+
+template <bool VEC>
+__device__ __forceinline__ int64_t sum_share(const float *p, const float *q, int v0, int v1, int lane)
+{
+    int64_t sum = 0;
+#pragma unroll 4
+    for (int v = v0 + 4 * lane; v < v1; v += 128) {
+        float w[4];
+        weights4<VEC>(p, q, v, v1, w);
+        sum += (units(w[0]) + units(w[1])) + (units(w[2]) + units(w[3]));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    return sum;
+}
+
+template <bool VEC>
 __global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyParams a)
 {
-    const int b = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int b = blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __shared__ int s_stop;
-    __shared__ int64_t s_sum[VF_WARPS];
+    __shared__ int64_t s_sum[VF_WARPS], s_all[2][VF_CLUSTER];
     const int lo = __ldg(a.ptr + b), hi = __ldg(a.ptr + b + 1);
-    if (lo < 0 || hi < lo || hi > a.n_drafts) {
-        if (tid == 0) {
+    if (lo < 0 || hi < lo || hi > a.n_drafts) {  // (the whole cluster)
+        if (tid == 0 && rank == 0) {
             atomicOr(a.err, SALT_DEVERR_DRAFT);
             a.accepted[b] = 0;
             a.next[b] = -1;
@@ -54,48 +107,59 @@ __global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyParams a)
     const int stop = s_stop;
     const float *p = a.p + (int64_t)(lo + b + stop) * a.p_stride;
     const float *q = stop < n ? a.q + (int64_t)(lo + stop) * a.q_stride : nullptr;
-    const int chunk = (V + VF_WARPS - 1) / VF_WARPS;
-    const int v0 = min(V, warp * chunk), v1 = min(V, v0 + chunk);
-    auto weight = [&](int v) { return units(q ? __fsub_rn(__ldg(p + v), __ldg(q + v)) : __ldg(p + v)); };
-    int64_t total = 0, before = 0;
+    // this warp's share of the row
+    const int share = (V + C * VF_WARPS * 4 - 1) / (C * VF_WARPS * 4) * 4;
+    const int v0 = min(V, (rank * VF_WARPS + warp) * share), v1 = min(V, v0 + share);
+    int64_t total = 0, before = 0, mine = 0;
     for (int pass = 0; pass < 2; ++pass) {
-        int64_t sum = 0;
-        for (int v = v0 + lane; v < v1; v += 32) sum += weight(v);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) s_sum[warp] = sum;
+        mine = sum_share<VEC>(p, q, v0, v1, lane);
+        if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
-        total = before = 0;
-        for (int w = 0; w < VF_WARPS; ++w) {
-            if (w < warp) before += s_sum[w];
-            total += s_sum[w];
+        if (warp == 0) {  // the CTA's sum to every CTA of the cluster
+            int64_t s = lane < VF_WARPS ? s_sum[lane] : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+            if (lane < C) *cluster.map_shared_rank(&s_all[pass][rank], lane) = s;
         }
+        cluster.sync();
+        total = before = 0;
+        for (int c = 0; c < C; ++c) {
+            if (c < rank) before += s_all[pass][c];
+            total += s_all[pass][c];
+        }
+        for (int w = 0; w < warp; ++w) before += s_sum[w];
         if (total > 0 || !q) break;
         q = nullptr;  // p is nowhere above q: p itself
         __syncthreads();
     }
-    if (tid == 0) {
+    if (tid == 0 && rank == 0) {
         a.accepted[b] = stop;
         if (total <= 0) a.next[b] = -1;
     }
     if (total <= 0) return;
     const int64_t U = __float2ll_rz(fminf(fmaxf(__ldg(a.su + b), 0.f), 0.99999994f) * 16777216.f);
     const int64_t at = U * (total >> 24) + ((U * (total & 0xffffff)) >> 24);
-    if (at < before || at >= before + s_sum[warp]) return;
+    if (at < before || at >= before + mine) return;
     // the one warp whose share of the running sum holds `at`
-    for (int v = v0; v < v1; v += 32) {
-        int64_t w = v + lane < v1 ? weight(v + lane) : 0;
+    for (int v = v0; v < v1; v += 128) {
+        float w[4];
+        weights4<VEC>(p, q, v + 4 * lane, v1, w);
+        const int64_t u0 = units(w[0]), u1 = u0 + units(w[1]), u2 = u1 + units(w[2]), u3 = u2 + units(w[3]);
+        int64_t run = u3;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t up = __shfl_up_sync(0xffffffffu, w, o);
-            if (lane >= o) w += up;
+            const int64_t up = __shfl_up_sync(0xffffffffu, run, o);
+            if (lane >= o) run += up;
         }
-        const uint32_t past = __ballot_sync(0xffffffffu, before + w > at);
+        const uint32_t past = __ballot_sync(0xffffffffu, before + run > at);
         if (past) {
-            if (lane == 0) a.next[b] = v + __ffs(past) - 1;
+            if (lane == __ffs(past) - 1) {
+                const int64_t from = before + run - u3;
+                a.next[b] = v + 4 * lane + (from + u0 > at ? 0 : from + u1 > at ? 1 : from + u2 > at ? 2 : 3);
+            }
             return;
         }
-        before += __shfl_sync(0xffffffffu, w, 31);
+        before += __shfl_sync(0xffffffffu, run, 31);
     }
 }
 
@@ -128,7 +192,22 @@ extern "C" salt_status salt_verify_drafts(salt_ctx *ctx, int32_t n_seqs, int32_t
     if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
     const VerifyParams a{draft_ptr, draft_tokens, target_p, draft_p, accept_u, sample_u, target_stride, draft_stride,
                          n_drafts, n_vocab, accepted, next_token, ctx_error_word(ctx)};
-    verify_kernel<<<n_seqs, VF_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+    // One CTA for each VF_SHARE tokens, up to VF_CLUSTER (a power of two).
+    int ctas = 1;
+    while (ctas < VF_CLUSTER && ctas * VF_SHARE < n_vocab) ctas *= 2;
+    if ((int64_t)n_seqs * ctas > 0x7fffffff) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%d requests in one call", n_seqs);
+    const bool vec = ((reinterpret_cast<uintptr_t>(target_p) | (n_drafts > 0 ? reinterpret_cast<uintptr_t>(draft_p) : 0)) & 15) == 0 &&
+                     target_stride % 4 == 0 && (n_drafts == 0 || draft_stride % 4 == 0);
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(n_seqs * ctas), 1, 1);
+    cfg.blockDim = dim3(VF_THREADS, 1, 1);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    SALT_CUDA_OR_FAIL(ctx, cudaLaunchKernelEx(&cfg, vec ? verify_kernel<true> : verify_kernel<false>, a));
     return SALT_OK;
 }
