@@ -440,6 +440,65 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
     return mx + t.vref;
 }
 
+// soft_probs where every column of the warpgroup is a row and every row sees every token: no
+// branches, and each sixteen columns' exponentials run beside the next ones' loads and products.
+// (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
+// loads, a tile of 128 rows took 2,100 cycles here.)
+template <class L>
+__device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
+                                                 float sign, int valid)
+{
+    constexpr int N = L::CW_MAX / CH;
+    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
+    float mx = -INFINITY;
+    float x[2][CH];
+    float4 a[CH / 4], m[CH / 4];
+    auto fetch = [&](int c) {
+        load_columns<CH>(x[c & 1], s_at + c * CH);
+#pragma unroll
+        for (int i = 0; i < CH / 4; ++i) {
+            a[i] = lds4f(w.info + 4 * c * CH + L::IN_A + 16 * i);
+            m[i] = lds4f(w.info + 4 * c * CH + L::IN_M + 16 * i);
+        }
+    };
+    auto args = [&](int c) {
+        float (&y)[CH] = x[c & 1];
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < CH; i += 4) {
+            const float2 u = fma2(make_float2(y[i], y[i + 1]), mul2(make_float2(a[i / 4].x, a[i / 4].y), kf2), make_float2(m[i / 4].x, m[i / 4].y));
+            const float2 v = fma2(make_float2(y[i + 2], y[i + 3]), mul2(make_float2(a[i / 4].z, a[i / 4].w), kf2), make_float2(m[i / 4].z, m[i / 4].w));
+            y[i] = u.x;
+            y[i + 1] = u.y;
+            y[i + 2] = v.x;
+            y[i + 3] = v.y;
+        }
+    };
+    fetch(0);
+    args(0);
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        float (&y)[CH] = x[c & 1];
+        if (c + 1 < N) fetch(c + 1);
+        uint32_t h[CH / 2];
+#pragma unroll
+        for (int i = 0; i < CH; i += 2) {
+            mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
+            const float2 e = make_float2(ex2(y[i]), ex2(y[i + 1])), v = mul2(e, vf2);
+            l[(c * CH + i) / 2] = fma2(e, sign2, l[(c * CH + i) / 2]);
+            const __half2 q = __floats2half2_rn(v.x, v.y);
+            h[i / 2] = *reinterpret_cast<const uint32_t *>(&q);
+        }
+        if (c + 1 < N) args(c + 1);
+        // P and the values take the place of the last tile's once its product is done
+        if (c == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+        sts128(w.p_row + (w.p_mix ^ (2 * c * CH)), h[0], h[1], h[2], h[3]);
+        sts128(w.p_row + (w.p_mix ^ (2 * c * CH + 16)), h[4], h[5], h[6], h[7]);
+    }
+    widen_values<L>(s, valid);
+    return mx + t.vref;
+}
+
 // Moves the references that a score of this tile passes by too much (all of
 // them where there is none yet), and with them what the output and the
 // sums of earlier tiles hold.  The whole warpgroup; needs the product before this
@@ -518,7 +577,9 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
 #pragma unroll 1
     for (int pass = FIRST;; ++pass) {
         if ((pass == AGAIN || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
-        const float mx = soft_probs<L>(s, w, l, t, s_at, pass == TAKE_OUT ? -1.f : 1.f, valid);
+        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
+        const float mx = L::WIDE && w.ncol == L::CW_MAX && !t.mask ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
+                                                                   : soft_probs<L>(s, w, l, t, s_at, sign, valid);
         if (pass == TAKE_OUT) continue;
         if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
         if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;

@@ -32,8 +32,16 @@ struct VerifyParams {
     uint32_t *err;
 };
 
-// a weight in units of 2^-40; NaN and what is not above zero count as 0
-__device__ __forceinline__ int64_t units(float w) { return w > 0.f ? __float2ll_rz(fminf(w, 1.f) * 1099511627776.f) : 0ll; }
+// A weight in units of 2^-40; NaN and what is not above zero count as 0.  w = M 2^(E - 150) with a
+// whole M below 2^24, so this is M shifted by E - 110 places (a conversion to 64-bit integers runs at a
+// small part of the rate of these).
+__device__ __forceinline__ int64_t units(float w)
+{
+    const uint32_t b = __float_as_uint(fminf(w, 1.f)), M = (b & 0x7fffffu) | 0x800000u;
+    const int s = (int)(b >> 23) - 110;  // at most 17; weights below the normal range come to 0
+    const uint32_t lo = s >= 0 ? M << s : M >> min(-s, 31), hi = (M >> 1) >> (31 - max(s, 0));
+    return w > 0.f ? (int64_t)((uint64_t)hi << 32 | lo) : 0ll;
+}
 
 // Four weights from v on (those below end), p and q (or none) read as one
 // 16-byte piece where VEC says that rows lie on such boundaries.
