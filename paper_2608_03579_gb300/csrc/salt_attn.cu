@@ -382,8 +382,8 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 
 // P of a tile and the warpgroup's share of its widened values into shared
 // memory, the probabilities times `sign` to the sums l.  Returns the largest log2 P
-// of the token.  Columns go by sixteens (the last ones are filled up), the next ones'
-// scores under way.  (One copy of this code for every number of
+// of the token.  Columns go by sixteens (the last ones are filled up; fetching the next ones'
+// scores ahead took 3% longer, in registers).  (One copy of this code for every number of
 // rows: with one for each, and one for masked tiles, the kernel had 223 KB of code and
 // an item's first tile waited 6,000 cycles for instructions.)
 template <class L>
@@ -392,14 +392,12 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
 {
     const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
     float mx = -INFINITY;
-    float x[2][CH];
-    if (w.ncol > 0) load_columns<CH>(x[0], s_at);
 #pragma unroll
     for (int c0 = 0; c0 < L::CW_MAX; c0 += CH) {
         if (c0 >= w.ncol) break;
-        float (&y)[CH] = x[(c0 / CH) & 1];
+        float y[CH];
+        load_columns<CH>(y, s_at + c0);
         tmem_ld_wait();
-        if (c0 + CH < L::CW_MAX && c0 + CH < w.ncol) load_columns<CH>(x[(c0 / CH + 1) & 1], s_at + c0 + CH);
         const uint32_t at = w.info + 4 * c0;
 #pragma unroll
         for (int i = 0; i < CH; i += 4) {
@@ -1261,7 +1259,7 @@ struct RowTile {
 // tile of each class of wide items, and what an item takes besides.
 constexpr float NARROW_TILE = 1.f, NARROW_ITEM = 2.f;
 constexpr float WIDE_TILE[3] = {1.1f, 1.4f, 2.2f};
-constexpr float WIDE_ITEM = 4.f;
+constexpr float WIDE_ITEM = 6.f;
 
 float tile_cost(const RowTile &x) { return x.wide ? WIDE_TILE[x.cls] : NARROW_TILE; }
 int items_of(const RowTile &x, double most, int *per_item)
