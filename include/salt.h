@@ -667,10 +667,12 @@ salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_
  * out are rows of [n_heads][head_dim] bf16, q_stride / out_stride elements apart
  * (multiples of 8), 16-byte aligned; out must not overlap q.  lse is float
  * [tokens][n_heads] or NULL.  Scores, running maxima, sums and partial results
- * are held in fp32 and out is rounded once.  The query and the probabilities
- * meet the 8-bit cache as sums of two e4m3 terms each (about 8 bits, as
- * bf16).  A row with an infinity or a NaN in its query, or that sees a cached
- * row standing for NaN, is NaN.  Results do not depend on timing.
+ * are held in fp32 and out is rounded once.  The query meets the cached keys
+ * as the sum of two e4m3 terms (about 8 bits, as bf16), the probabilities meet
+ * the cached values, widened exactly, in f16 (11 bits).  A row with an infinity or a NaN
+ * in its query, or that sees a cached key standing for NaN, is NaN; so is one that sees a
+ * cached value standing for NaN with a probability within fp32's range.  Results do not depend on
+ * timing.
  * Asynchronous on `stream`; runs of one plan share its workspace and are
  * ordered one after the other.  A captured run may be replayed after the
  * plan was built again with at most as many query tokens as it had at the capture; on a larger
