@@ -1067,18 +1067,21 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     if (!L::WIDE) pdl_wait();  // so that what follows this kernel follows the wide one too
 }
 
-// The rows that several items share (and those no item has): a warp per row,
-//     out = sum_i 2^(l_i - L) o_i,   L = log2 sum_i 2^(l_i),
-// the logarithms of 32 items at a time over the lanes, their rows four at a time.
-constexpr int COMBINE_WARPS = 4;
+// The rows that several items share (and those no item has),
+//     out = sum_i 2^(l_i - L) o_i,   L = log2 sum_i 2^(l_i).
+// A CTA's warps take a row each, or (SPLIT) a part of one row's items each and meet in shared memory, where
+// rows are so few that the time is that of a row's loads one behind the other.  A
+// warp has the logarithms of 32 items over its lanes, and four items' rows under way.
+constexpr int COMBINE_WARPS = 4, COMBINE_SPLIT = 16;
+constexpr int COMBINE_FEW = 4;  // rows an SM up to which they are split: the CTAs of COMBINE_SPLIT warps that it holds
 
-template <int D>
-__global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const __grid_constant__ AttnParams p)
+template <int D, int SPLIT>
+__global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : COMBINE_WARPS)) attn_combine_kernel(const __grid_constant__ AttnParams p)
 {
-    constexpr int E = D / 32;
-    const int T = __ldg(p.plan + HD_TOKENS), H = p.n_heads, KV = p.kv.heads, G = H / KV, lane = threadIdx.x & 31;
+    constexpr int E = D / 32, AT_ONCE = 4;
+    const int T = __ldg(p.plan + HD_TOKENS), H = p.n_heads, KV = p.kv.heads, G = H / KV, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int partial = __ldg(p.plan + HD_PARTIAL);
-    const int row = blockIdx.x * COMBINE_WARPS + (threadIdx.x >> 5), t = row / H, h = row - t * H, kh = h / G, g = h - kh * G;
+    const int row = SPLIT == 1 ? blockIdx.x * COMBINE_WARPS + warp : blockIdx.x, t = row / H, h = row - t * H, kh = h / G, g = h - kh * G;
     const bool live = T <= p.max_tok && partial && t < T;
     int4 a = make_int4(0, 0, 0, 0), b = make_int4(0, 0, 1, 0);
     if (live) {
@@ -1088,7 +1091,8 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const 
     }
     pdl_wait();    // (the plan is older than the items' kernels)
     if (b.z) return;  // no such row, or written by its only item
-    const int own_n = a.z, n = own_n + b.y;
+    const int own_n = a.z, all = own_n + b.y;
+    const int part = SPLIT == 1 ? 0 : warp, from = all * part / SPLIT, n = all * (part + 1) / SPLIT;
     auto place = [&](int i) -> int {  // the row's i-th partial
         return i < own_n ? a.x + (i * KV + kh) * a.y + g : a.w + ((i - own_n) * KV + kh) * b.x + g;
     };
@@ -1096,9 +1100,30 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const 
     bool nan = false;
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        const int mine = i0 + lane < n ? place(i0 + lane) : 0;
-        const float l = i0 + lane < n ? __ldcg(p.part_l + mine) : -INFINITY;
+    for (int i0 = from; i0 < n; i0 += 32) {
+        const int k = min(32, n - i0), mine = place(i0 + min(lane, k - 1));
+        const float l = lane < k ? __ldcg(p.part_l + mine) : -INFINITY;
+        float v[AT_ONCE][E];
+        auto load = [&](int i) {
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int at = __shfl_sync(0xffffffffu, mine, min(i + u, 31));
+                const float *src = p.part_o + (int64_t)at * D + lane * E;
+                if (i + u >= k) continue;
+                if constexpr (E == 4) {
+                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(src));
+                    v[u][0] = x.x;
+                    v[u][1] = x.y;
+                    v[u][2] = x.z;
+                    v[u][3] = x.w;
+                } else {
+                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(src));
+                    v[u][0] = x.x;
+                    v[u][1] = x.y;
+                }
+            }
+        };
+        load(0);
         nan |= !(l == l);
         float m = fmaxf(top, l);
 #pragma unroll
@@ -1109,35 +1134,45 @@ __global__ void __launch_bounds__(32 * COMBINE_WARPS) attn_combine_kernel(const 
         sum *= keep;
 #pragma unroll
         for (int e = 0; e < E; ++e) o[e] *= keep;
-        const int k = min(32, n - i0);
-        for (int i = 0; i < k; i += 4) {
-            float f[4], v[4][E];
+        for (int i = 0; i < k; i += AT_ONCE) {
+            if (i > 0) load(i);
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int at = __shfl_sync(0xffffffffu, mine, min(i + u, k - 1));
-                f[u] = i + u < k ? __shfl_sync(0xffffffffu, w, i + u) : 0.f;
-                if constexpr (E == 4) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4 *>(p.part_o + (int64_t)at * D + lane * E));
-                    v[u][0] = x.x;
-                    v[u][1] = x.y;
-                    v[u][2] = x.z;
-                    v[u][3] = x.w;
-                } else {
-                    const float2 x = __ldcg(reinterpret_cast<const float2 *>(p.part_o + (int64_t)at * D + lane * E));
-                    v[u][0] = x.x;
-                    v[u][1] = x.y;
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const float f = __shfl_sync(0xffffffffu, w, min(i + u, 31));
+                if (i + u < k) {
+                    sum += f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[e] = fmaf(f, v[u][e], o[e]);
                 }
-            }
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                sum += f[u];
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (i + u < k) o[e] = fmaf(f[u], v[u][e], o[e]);
             }
         }
     }
     nan = __any_sync(0xffffffffu, nan);
+    if constexpr (SPLIT > 1) {  // (the whole CTA has one row)
+        __shared__ float s_o[SPLIT][D], s_top[SPLIT], s_sum[SPLIT];
+#pragma unroll
+        for (int e = 0; e < E; ++e) s_o[part][lane * E + e] = o[e];
+        if (lane == 0) {
+            s_top[part] = top;
+            s_sum[part] = nan ? __uint_as_float(0x7fc00000u) : sum;
+        }
+        __syncthreads();
+        if (warp > 0) return;
+        top = s_top[0];
+#pragma unroll
+        for (int q = 1; q < SPLIT; ++q) top = fmaxf(top, s_top[q]);
+        sum = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int q = 0; q < SPLIT; ++q) {
+            const float f = s_top[q] == -INFINITY ? 0.f : ex2(s_top[q] - top);
+            nan |= !(s_sum[q] == s_sum[q]);
+            sum = fmaf(s_sum[q], f, sum);
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = fmaf(s_o[q][lane * E + e], f, o[e]);
+        }
+    }
     const float bad = __uint_as_float(0x7fc00000u), inv = nan ? bad : sum > 0.f ? 1.f / sum : 0.f;
     uint32_t out[E / 2];
 #pragma unroll
@@ -1487,12 +1522,14 @@ cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, b
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3((p.max_tok * p.n_heads + COMBINE_WARPS - 1) / COMBINE_WARPS, 1, 1);
-    cfg.blockDim = dim3(32 * COMBINE_WARPS, 1, 1);
+    const int rows = p.max_tok * p.n_heads;
+    const bool few = rows <= n_sm * COMBINE_FEW;
+    cfg.gridDim = dim3(few ? rows : (rows + COMBINE_WARPS - 1) / COMBINE_WARPS, 1, 1);
+    cfg.blockDim = dim3(32 * (few ? COMBINE_SPLIT : COMBINE_WARPS), 1, 1);
     cfg.stream = stream;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_combine_kernel<D>, p);
+    return cudaLaunchKernelEx(&cfg, few ? attn_combine_kernel<D, COMBINE_SPLIT> : attn_combine_kernel<D, 1>, p);
 }
 
 }  // namespace
