@@ -67,6 +67,7 @@ struct AttnParams {
     float *part_l;                 // [partial rows] log2 of the sum
     int64_t q_stride, out_stride;
     int32_t n_heads, max_tok;
+    int32_t behind;                // whether the wide items' kernel is the one before
     int32_t tok_at, order_at, rec_at, pages_at;  // word offsets in plan
     float scale_log2;              // scale * log2(e)
     uint32_t *err;
@@ -825,17 +826,6 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     const uint32_t base = smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int KV = p.kv.heads, G = p.n_heads / KV;
-    pdl_launch_dependents();  // (the narrow items need nothing of the wide ones, the combine waits)
-    if (p.plan[HD_TOKENS] > p.max_tok) {
-        if (blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
-        if (!L::WIDE) pdl_wait();
-        return;
-    }
-    const int n_items = p.plan[L::WIDE ? HD_WIDE : HD_NARROW] * KV;
-    if ((int)blockIdx.x >= n_items) {
-        if (!L::WIDE) pdl_wait();
-        return;
-    }
     uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(sm + L::MISC);
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
@@ -868,6 +858,18 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    // A run's first kernel gets this far beside the end of what came before it in the stream; the narrow
+    // items' behind the wide ones' needs nothing of that one, which itself lets it begin after its own wait.
+    if (!p.behind) pdl_wait();
+    pdl_launch_dependents();  // (the combine waits)
+    const bool fits = p.plan[HD_TOKENS] <= p.max_tok;
+    if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
+    const int n_items = fits ? p.plan[L::WIDE ? HD_WIDE : HD_NARROW] * KV : 0;
+    if ((int)blockIdx.x >= n_items) {
+        if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
+        if (!L::WIDE) pdl_wait();
+        return;
+    }
     bool ok = true;
     if (warp > 0) {
         // ------------------------------------------------ queries: the first item's by every warp but the one that starts its
@@ -1488,8 +1490,10 @@ cudaError_t prepare_tiles()
 }
 
 template <class L>
-cudaError_t launch_tiles(const AttnParams &p, int n_sm, bool after_wide, cudaStream_t stream)
+cudaError_t launch_tiles(const AttnParams &params, int n_sm, bool behind, cudaStream_t stream)
 {
+    AttnParams p = params;
+    p.behind = behind;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1499,7 +1503,7 @@ cudaError_t launch_tiles(const AttnParams &p, int n_sm, bool after_wide, cudaStr
     cfg.dynamicSmemBytes = L::BYTES;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = after_wide ? 1 : 0;
+    cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, attn_tile_kernel<L>, p);
 }
 
@@ -1528,7 +1532,7 @@ cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, b
     cfg.blockDim = dim3(32 * (few ? COMBINE_SPLIT : COMBINE_WARPS), 1, 1);
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = wide || narrow ? 1 : 0;  // (the plan is there when an items' kernel is past its wait)
     return cudaLaunchKernelEx(&cfg, few ? attn_combine_kernel<D, COMBINE_SPLIT> : attn_combine_kernel<D, 1>, p);
 }
 
