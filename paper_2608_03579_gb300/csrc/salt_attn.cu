@@ -862,9 +862,10 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
     // items' behind the wide ones' needs nothing of that one, which itself lets it begin after its own wait.
     if (!p.behind) pdl_wait();
     pdl_launch_dependents();  // (the combine waits)
-    const bool fits = p.plan[HD_TOKENS] <= p.max_tok;
+    const int32_t *plan = after_pdl_wait(p.plan);
+    const bool fits = plan[HD_TOKENS] <= p.max_tok;
     if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
-    const int n_items = fits ? p.plan[L::WIDE ? HD_WIDE : HD_NARROW] * KV : 0;
+    const int n_items = fits ? plan[L::WIDE ? HD_WIDE : HD_NARROW] * KV : 0;
     if ((int)blockIdx.x >= n_items) {
         if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
         if (!L::WIDE) pdl_wait();

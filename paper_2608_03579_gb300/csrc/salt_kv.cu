@@ -14,6 +14,7 @@
 #include "salt_async.cuh"
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
+#include "salt_pipe.cuh"
 
 namespace salt {
 namespace {
@@ -86,6 +87,11 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvDev c, uint32_t 
 {
     constexpr int LPR = D / 16, ROWS = WRITE_ROWS;
     const int part = threadIdx.x % LPR;
+    pdl_wait();  // (launched beside the end of what came before)
+    pdl_launch_dependents();
+    k = after_pdl_wait(k);
+    v = after_pdl_wait(v);
+    slots = after_pdl_wait(slots);
     KvRow r[ROWS];
     uint4 x[ROWS][2];
     int slot[ROWS];
@@ -141,6 +147,9 @@ __global__ void __launch_bounds__(KV_THREADS) kv_read_kernel(KvDev c, uint32_t f
 {
     constexpr int LPR = D / 16, ROWS = READ_ROWS;
     const int part = threadIdx.x % LPR;
+    pdl_wait();  // (launched beside the end of what came before)
+    pdl_launch_dependents();
+    slots = after_pdl_wait(slots);
     KvRow r[ROWS];
     int slot[ROWS];
     uint2 codes[ROWS][2];
@@ -219,6 +228,22 @@ unsigned row_blocks(const salt_kv *kv, int32_t n_tokens, int rows)
     return (unsigned)((2ll * n_tokens * kv->dev.heads + per - 1) / per);
 }
 
+// A launch that may begin while the stream's last kernel ends (the kernel waits for that one itself).
+template <class... P, class... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), unsigned blocks, unsigned threads, cudaStream_t stream, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(blocks, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 }  // namespace
 }  // namespace salt
 
@@ -280,10 +305,9 @@ salt_status salt_kv_write(salt_kv *kv, int32_t layer, int32_t n_tokens, const vo
     const int32_t most = launch_tokens(kv);
     for (int64_t t = 0; t < n_tokens; t += most) {
         const int32_t n = (int32_t)std::min<int64_t>(most, n_tokens - t);
-        kernel<<<row_blocks(kv, n, WRITE_ROWS), KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, WRITE_ROWS), KV_THREADS, static_cast<cudaStream_t>(stream),
             kv->dev, (uint32_t)layer * kv->dev.n_pages, n, heads2_inv(kv), static_cast<const uint16_t *>(k) + t * k_stride, k_stride,
-            static_cast<const uint16_t *>(v) + t * v_stride, v_stride, slots + t, ctx_error_word(kv->ctx));
-        SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+            static_cast<const uint16_t *>(v) + t * v_stride, v_stride, slots + t, ctx_error_word(kv->ctx)));
     }
     return SALT_OK;
 }
@@ -300,10 +324,9 @@ salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int
     const int32_t most = launch_tokens(kv);
     for (int64_t t = 0; t < n_tokens; t += most) {
         const int32_t n = (int32_t)std::min<int64_t>(most, n_tokens - t);
-        kernel<<<row_blocks(kv, n, READ_ROWS), KV_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(
+        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, READ_ROWS), KV_THREADS, static_cast<cudaStream_t>(stream),
             kv->dev, (uint32_t)layer * kv->dev.n_pages, n, heads2_inv(kv), slots + t, static_cast<uint16_t *>(k) + t * k_stride, k_stride,
-            static_cast<uint16_t *>(v) + t * v_stride, v_stride, ctx_error_word(kv->ctx));
-        SALT_CUDA_OR_FAIL(kv->ctx, cudaGetLastError());
+            static_cast<uint16_t *>(v) + t * v_stride, v_stride, ctx_error_word(kv->ctx)));
     }
     return SALT_OK;
 }

@@ -82,5 +82,13 @@ __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence
 
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;\n" ::); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;\n" ::: "memory"); }
+// p as known after a pdl_wait only: loads through it cannot be moved before the wait, not even those
+// that the compiler takes for loads of constants (__ldg)
+template <class T>
+__device__ __forceinline__ T *after_pdl_wait(T *p)
+{
+    asm volatile("" : "+l"(p)::"memory");
+    return p;
+}
 
 }  // namespace salt

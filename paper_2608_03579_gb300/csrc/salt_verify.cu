@@ -14,6 +14,7 @@
 
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
+#include "salt_pipe.cuh"
 
 namespace salt {
 namespace {
@@ -92,6 +93,10 @@ __global__ void __launch_bounds__(VF_THREADS) verify_kernel(VerifyParams a)
     const int b = blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __shared__ int s_stop;
     __shared__ int64_t s_sum[VF_WARPS], s_all[2][VF_CLUSTER];
+    pdl_wait();  // (launched beside the end of what came before)
+    pdl_launch_dependents();
+    a.ptr = after_pdl_wait(a.ptr);
+    a.su = after_pdl_wait(a.su);
     const int lo = __ldg(a.ptr + b), hi = __ldg(a.ptr + b + 1);
     if (lo < 0 || hi < lo || hi > a.n_drafts) {  // (the whole cluster)
         if (tid == 0 && rank == 0) {
@@ -207,15 +212,17 @@ extern "C" salt_status salt_verify_drafts(salt_ctx *ctx, int32_t n_seqs, int32_t
     const bool vec = ((reinterpret_cast<uintptr_t>(target_p) | (n_drafts > 0 ? reinterpret_cast<uintptr_t>(draft_p) : 0)) & 15) == 0 &&
                      target_stride % 4 == 0 && (n_drafts == 0 || draft_stride % 4 == 0);
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.gridDim = dim3((unsigned)(n_seqs * ctas), 1, 1);
     cfg.blockDim = dim3(VF_THREADS, 1, 1);
     cfg.stream = static_cast<cudaStream_t>(stream);
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     SALT_CUDA_OR_FAIL(ctx, cudaLaunchKernelEx(&cfg, vec ? verify_kernel<true> : verify_kernel<false>, a));
     return SALT_OK;
 }
