@@ -514,26 +514,22 @@ def _device_tensor(t):
     return t
 
 
-_bf16 = None
+_bf16 = _f32 = _i32 = None
 
 
-def _is_bf16(t) -> bool:
-    global _bf16
-    if _bf16 is None:
-        import torch
-        _bf16 = torch.bfloat16
-    return t.dtype is _bf16
-
-
-def _is_f32(t) -> bool:
-    return t.is_cuda and t.is_floating_point() and t.element_size() == 4
+def _load_types():
+    global _bf16, _f32, _i32
+    import torch
+    _bf16, _f32, _i32 = torch.bfloat16, torch.float32, torch.int32
 
 
 def _head_rows(t, heads: int, dim: int):
     """(tokens, pointer, elements from row to row) of a CUDA bf16 tensor
     [tokens, heads, dim] whose heads are contiguous within a row."""
+    if _bf16 is None:
+        _load_types()
     shape, s = t.shape, t.stride()
-    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or not _is_bf16(t) or not t.is_cuda:
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not _bf16 or not t.is_cuda:
         raise ValueError(f"not a CUDA bf16 tensor [tokens, {heads}, {dim}]")
     if s[2] != 1 or (s[1] != dim and heads > 1):
         raise ValueError("the heads of a row are not contiguous")
@@ -543,7 +539,9 @@ def _head_rows(t, heads: int, dim: int):
 
 def _int32s(t, n: int | None = None):
     """Pointer of a contiguous CUDA int32 tensor of n elements."""
-    if not t.is_cuda or t.is_floating_point() or t.element_size() != 4 or not t.is_contiguous():
+    if _i32 is None:
+        _load_types()
+    if t.dtype is not _i32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError("not a contiguous CUDA int32 tensor")
     if n is not None and t.numel() != n:
         raise ValueError(f"{t.numel()} entries, {n} expected")
@@ -642,15 +640,17 @@ def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, st
     m, op, os_ = _head_rows(out, plan.n_heads, plan.head_dim)
     if n < plan.n_tokens or m < plan.n_tokens:
         raise ValueError(f"q or out has fewer rows than the batch's {plan.n_tokens} query tokens")
-    if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or not _is_f32(lse)):
+    if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or lse.dtype is not _f32 or not lse.is_cuda):
         raise ValueError("lse is not a CUDA float32 tensor of the batch's rows")
     _check(_lib.salt_attn_run(plan.handle, layer, qp, qs, scale, op, os_, _ptr(lse), _stream(stream)), plan.ctx)
 
 
 def _prob_rows(t, rows: int):
-    if t.dim() != 2 or t.shape[0] != rows or not _is_f32(t) or (t.shape[1] > 1 and t.stride(1) != 1):
+    """(pointer, elements from row to row, columns) of a CUDA float32 matrix of `rows` rows."""
+    shape, s = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != rows or t.dtype is not _f32 or not t.is_cuda or (s[1] != 1 and shape[1] > 1):
         raise ValueError(f"not a CUDA float32 tensor of {rows} rows")
-    return t.data_ptr(), t.stride(0) if rows > 1 else max(t.stride(0), t.shape[1])
+    return t.data_ptr(), s[0] if rows > 1 else max(s[0], shape[1]), shape[1]
 
 
 def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u, sample_u, accepted, next_token,
@@ -660,13 +660,15 @@ def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u
     [drafts + requests, vocab], draft_p float32 [drafts, vocab], accept_u
     float32 [drafts], sample_u float32 [requests]; results accepted and
     next_token, int32 [requests]."""
-    n, d, vocab = sample_u.numel(), draft_tokens.numel(), target_p.shape[1]
-    tp, ts = _prob_rows(target_p, d + n)
-    dp, ds = _prob_rows(draft_p, d)
-    if d and draft_p.shape[1] != vocab:
+    if _f32 is None:
+        _load_types()
+    n, d = sample_u.numel(), draft_tokens.numel()
+    tp, ts, vocab = _prob_rows(target_p, d + n)
+    dp, ds, draft_vocab = _prob_rows(draft_p, d)
+    if d and draft_vocab != vocab:
         raise ValueError("target_p and draft_p have different vocabularies")
     for t, m in ((accept_u, d), (sample_u, n)):
-        if not _is_f32(t) or not t.is_contiguous() or t.numel() != m:
+        if t.dtype is not _f32 or not t.is_cuda or not t.is_contiguous() or t.numel() != m:
             raise ValueError(f"not a contiguous CUDA float32 tensor of {m} entries")
     _check(_lib.salt_verify_drafts(ctx, n, d, vocab, _int32s(draft_ptr, n + 1), _int32s(draft_tokens), tp, ts, dp, ds,
                                    accept_u.data_ptr(), sample_u.data_ptr(), _int32s(accepted, n),
