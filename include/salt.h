@@ -700,7 +700,8 @@ salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t
  * (-1 when the row has no weight).  sample_u in [0, 1).  Every pointer is
  * device memory; int32 but for the floats.  A request whose draft_ptr is
  * out of order or range gets 0 and -1, and a drafted token outside the vocabulary is
- * not accepted; both raise SALT_DEVERR_DRAFT.  n_vocab <= SALT_MAX_VOCAB.
+ * not accepted; both raise SALT_DEVERR_DRAFT.  ctx may be NULL: the current
+ * device is used then, and no error word.  n_vocab <= SALT_MAX_VOCAB.
  * One kernel, asynchronous on `stream`.
  */
 salt_status salt_verify_drafts(salt_ctx *ctx, int32_t n_seqs, int32_t n_drafts, int32_t n_vocab,

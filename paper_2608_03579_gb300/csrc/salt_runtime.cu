@@ -460,7 +460,10 @@ salt_status ctx_fail(salt_ctx *ctx, salt_status s, const char *fmt, ...)
         va_start(ap, fmt);
         vsnprintf(buf, sizeof buf, fmt, ap);
         va_end(ap);
-        ctx->last_error = buf;
+        try {
+            ctx->last_error = buf;
+        } catch (...) {  // no memory for the message: the status still tells
+        }
     }
     return s;
 }

@@ -659,7 +659,7 @@ def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u
     int32 [requests + 1], draft_tokens int32 [drafts], target_p float32
     [drafts + requests, vocab], draft_p float32 [drafts, vocab], accept_u
     float32 [drafts], sample_u float32 [requests]; results accepted and
-    next_token, int32 [requests]."""
+    next_token, int32 [requests].  ctx may be None (the current device)."""
     if _f32 is None:
         _load_types()
     n, d = sample_u.numel(), draft_tokens.numel()

@@ -103,3 +103,16 @@ def test_other_types_are_refused(salt_lib, drafted):
             salt_lib.salt_verify_drafts(*args(p.int(), p[0, :1].contiguous()))
         with pytest.raises(ValueError):
             salt_lib.salt_verify_drafts(*args(p, ints[:1]))
+
+
+def test_verification_without_a_context(salt_lib):
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    p = torch.tensor([[0.5, 0.25, 0.25, 0.0], [0.0, 0.0, 1.0, 0.0]], device="cuda")
+    q = torch.tensor([[0.25, 0.75, 0.0, 0.0]], device="cuda")
+    u, su = torch.tensor([0.5], device="cuda"), torch.tensor([0.0], device="cuda")
+    a, b = i32([9]), i32([9])
+    for token, accepted, following in ((0, 1, 2), (1, 0, 0), (7, 0, 0)):  # 7: outside the vocabulary
+        salt_lib.salt_verify_drafts(None, i32([0, 1]), i32([token]), p, q, u, su, a, b)
+        assert (a.item(), b.item()) == (accepted, following)
+    with pytest.raises(salt_lib.SaltError):
+        salt_lib.salt_verify_drafts(None, i32([0, 0]), i32([]), torch.zeros((1, (1 << 20) + 4), device="cuda"), q[:0], u[:0], su, a, b)
