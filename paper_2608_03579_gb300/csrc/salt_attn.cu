@@ -19,6 +19,13 @@
 // only when a probability passes f16's range (a vote a tile), so the usual tile
 // needs no reduction over tokens: p = 2^(s - m), l += p, P = p 2^e_v.  Items of one
 // row meet in the combine kernel through their (o / l, m + log2 l).
+//
+// What bounds it: neither memory nor the tensor cores but the steps of a tile one behind the
+// other (scores out of tensor memory, exponentials, P and V into shared memory, vote, product).  With 128
+// rows of 128 elements a tile takes about 4,300 cycles, 1,024 of them exponentials at the SM's rate and
+// 512 products: four prompt chunks of 900 to 2,048 tokens behind 4,096 take 1.2 ms (520 TFLOP/s).  With four
+// rows it is 2,400 cycles, two CTAs of an SM side by side: two requests of 200,000 tokens and more with
+// heads of 64 take 128 us (3.5 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
