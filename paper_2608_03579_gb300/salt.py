@@ -514,22 +514,22 @@ def _device_tensor(t):
     return t
 
 
-_bf16 = _f32 = _i32 = None
+_torch_bf16 = _torch_f32 = _torch_i32 = None
 
 
 def _load_types():
-    global _bf16, _f32, _i32
+    global _torch_bf16, _torch_f32, _torch_i32
     import torch
-    _bf16, _f32, _i32 = torch.bfloat16, torch.float32, torch.int32
+    _torch_bf16, _torch_f32, _torch_i32 = torch.bfloat16, torch.float32, torch.int32
 
 
 def _head_rows(t, heads: int, dim: int):
     """(tokens, pointer, elements from row to row) of a CUDA bf16 tensor
     [tokens, heads, dim] whose heads are contiguous within a row."""
-    if _bf16 is None:
+    if _torch_bf16 is None:
         _load_types()
     shape, s = t.shape, t.stride()
-    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not _bf16 or not t.is_cuda:
+    if len(shape) != 3 or shape[1] != heads or shape[2] != dim or t.dtype is not _torch_bf16 or not t.is_cuda:
         raise ValueError(f"not a CUDA bf16 tensor [tokens, {heads}, {dim}]")
     if s[2] != 1 or (s[1] != dim and heads > 1):
         raise ValueError("the heads of a row are not contiguous")
@@ -539,9 +539,9 @@ def _head_rows(t, heads: int, dim: int):
 
 def _int32s(t, n: int | None = None):
     """Pointer of a contiguous CUDA int32 tensor of n elements."""
-    if _i32 is None:
+    if _torch_i32 is None:
         _load_types()
-    if t.dtype is not _i32 or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not _torch_i32 or not t.is_cuda or not t.is_contiguous():
         raise ValueError("not a contiguous CUDA int32 tensor")
     if n is not None and t.numel() != n:
         raise ValueError(f"{t.numel()} entries, {n} expected")
@@ -640,7 +640,7 @@ def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, st
     m, op, os_ = _head_rows(out, plan.n_heads, plan.head_dim)
     if n < plan.n_tokens or m < plan.n_tokens:
         raise ValueError(f"q or out has fewer rows than the batch's {plan.n_tokens} query tokens")
-    if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or lse.dtype is not _f32 or not lse.is_cuda):
+    if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or lse.dtype is not _torch_f32 or not lse.is_cuda):
         raise ValueError("lse is not a CUDA float32 tensor of the batch's rows")
     _check(_lib.salt_attn_run(plan.handle, layer, qp, qs, scale, op, os_, _ptr(lse), _stream(stream)), plan.ctx)
 
@@ -648,7 +648,7 @@ def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, st
 def _prob_rows(t, rows: int):
     """(pointer, elements from row to row, columns) of a CUDA float32 matrix of `rows` rows."""
     shape, s = t.shape, t.stride()
-    if len(shape) != 2 or shape[0] != rows or t.dtype is not _f32 or not t.is_cuda or (s[1] != 1 and shape[1] > 1):
+    if len(shape) != 2 or shape[0] != rows or t.dtype is not _torch_f32 or not t.is_cuda or (s[1] != 1 and shape[1] > 1):
         raise ValueError(f"not a CUDA float32 tensor of {rows} rows")
     return t.data_ptr(), s[0] if rows > 1 else max(s[0], shape[1]), shape[1]
 
@@ -660,7 +660,7 @@ def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u
     [drafts + requests, vocab], draft_p float32 [drafts, vocab], accept_u
     float32 [drafts], sample_u float32 [requests]; results accepted and
     next_token, int32 [requests].  ctx may be None (the current device)."""
-    if _f32 is None:
+    if _torch_f32 is None:
         _load_types()
     n, d = sample_u.numel(), draft_tokens.numel()
     tp, ts, vocab = _prob_rows(target_p, d + n)
@@ -668,7 +668,7 @@ def salt_verify_drafts(ctx, draft_ptr, draft_tokens, target_p, draft_p, accept_u
     if d and draft_vocab != vocab:
         raise ValueError("target_p and draft_p have different vocabularies")
     for t, m in ((accept_u, d), (sample_u, n)):
-        if t.dtype is not _f32 or not t.is_cuda or not t.is_contiguous() or t.numel() != m:
+        if t.dtype is not _torch_f32 or not t.is_cuda or not t.is_contiguous() or t.numel() != m:
             raise ValueError(f"not a contiguous CUDA float32 tensor of {m} entries")
     _check(_lib.salt_verify_drafts(ctx, n, d, vocab, _int32s(draft_ptr, n + 1), _int32s(draft_tokens), tp, ts, dp, ds,
                                    accept_u.data_ptr(), sample_u.data_ptr(), _int32s(accepted, n),
