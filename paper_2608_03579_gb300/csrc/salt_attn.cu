@@ -1491,6 +1491,25 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     return (size_t)a->pages_at + own_pages + grp_pages;
 }
 
+// A cache's codes as rows of D bytes, a box a page's rows of one head, swizzled over a row's width.
+cudaError_t encode_codes_map(CUtensorMap *out, uint8_t *codes, int dim, int64_t rows, int page)
+{
+    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
+                                const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
+                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+    if (e != cudaSuccess || q != cudaDriverEntryPointSuccess || !fn) return e != cudaSuccess ? e : cudaErrorNotSupported;
+    const cuuint64_t dims[2] = {(cuuint64_t)dim, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)dim};
+    const cuuint32_t box[2] = {(cuuint32_t)dim, (cuuint32_t)page}, es[2] = {1, 1};
+    const CUresult r = reinterpret_cast<Encode>(fn)(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, codes, dims, strides, box, es,
+                                                    CU_TENSOR_MAP_INTERLEAVE_NONE,
+                                                    dim == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <class L>
 cudaError_t prepare_tiles()
 {
@@ -1577,10 +1596,9 @@ salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *c, salt_attn *
         prepare_tiles<Shape<64, true>>() != cudaSuccess || prepare_tiles<Shape<64, false>>() != cudaSuccess ||
         prepare_tiles<Shape<128, true>>() != cudaSuccess || prepare_tiles<Shape<128, false>>() != cudaSuccess)
         return fail_with(SALT_ERR_CUDA, "cannot prepare the attention kernel");
-    // codes as rows of D / 2 two-byte elements
     const int64_t rows = (int64_t)kv->n_layers * d.n_pages * d.heads * d.page;
-    if (encode_map_2d(&a->kmap, reinterpret_cast<const uint16_t *>(d.k), d.dim / 2, rows, d.dim / 2, d.page) != cudaSuccess ||
-        encode_map_2d(&a->vmap, reinterpret_cast<const uint16_t *>(d.v), d.dim / 2, rows, d.dim / 2, d.page) != cudaSuccess)
+    if (encode_codes_map(&a->kmap, d.k, d.dim, rows, d.page) != cudaSuccess ||
+        encode_codes_map(&a->vmap, d.v, d.dim, rows, d.page) != cudaSuccess)
         return fail_with(SALT_ERR_CUDA, "cannot map the cache");
     // Items: without splits at most one per request's and per group's row
     // tile; with them the plan keeps within the rest.  Partial rows: two per

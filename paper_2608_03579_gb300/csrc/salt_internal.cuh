@@ -207,8 +207,7 @@ cudaError_t launch_base(BaseParams &p, const uint16_t *W, int n_blk, cudaStream_
 int base_shrink_ctas(int T, int d_in, int d_out, int n_blk);
 // The shape launch_base would use on the current device; false when it is not prepared.
 bool base_launch_shape(int T, int d_in, int d_out, int n_blk, salt_base_shape *out);
-// A row-major bf16 tensor [rows][cols] as a 2-D TMA map; the swizzle is as wide
-// as the box, 128 bytes (box_cols 64) or 64 (32) (host).
+// A row-major bf16 tensor [rows][cols] as a 2-D TMA map, 128-byte swizzle (host).
 cudaError_t encode_map_2d(CUtensorMap *out, const uint16_t *base, int64_t cols, int64_t rows, uint32_t box_cols,
                           uint32_t box_rows);
 
