@@ -56,7 +56,6 @@ constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
 
 constexpr int TT = 128;          // cached tokens a tile
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
-constexpr int CH = 16;           // columns a softmax thread has in hand at a time
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
 constexpr float M_NONE = -1e30f; // the reference before the first token
@@ -96,6 +95,7 @@ struct Shape {
     static constexpr int NWG = WIDE ? 2 : 1;              // softmax warpgroups
     static constexpr int R_MAX = WIDE ? 128 : D == 128 ? 16 : 32;  // rows an item
     static constexpr int CW_MAX = R_MAX / NWG;            // columns of a warpgroup
+    static constexpr int CH = WIDE ? 16 : 8;              // columns a softmax thread has in hand at a time
     static constexpr int THREADS = 128 + NWG * WG;
     static constexpr int CTAS = WIDE ? 1 : 2;             // an SM
     // tensor memory columns: two buffers of R_MAX scores, the output
@@ -398,6 +398,7 @@ template <class L>
 __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
                                             float sign, int valid)
 {
+    constexpr int CH = L::CH;
     const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
     float mx = -INFINITY;
 #pragma unroll
@@ -438,8 +439,8 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
         }
         // P and the values take the place of the last tile's once its product is done
         if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
-        sts128(w.p_row + (w.p_mix ^ (2 * c0)), h[0], h[1], h[2], h[3]);
-        sts128(w.p_row + (w.p_mix ^ (2 * c0 + 16)), h[4], h[5], h[6], h[7]);
+#pragma unroll
+        for (int i = 0; i < CH / 2; i += 4) sts128(w.p_row + (w.p_mix ^ (2 * c0 + 4 * i)), h[i], h[i + 1], h[i + 2], h[i + 3]);
     }
     if (w.ncol == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
     widen_values<L>(s, valid);
@@ -454,7 +455,7 @@ template <class L>
 __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
                                                  float sign, int valid)
 {
-    constexpr int N = L::CW_MAX / CH;
+    constexpr int CH = L::CH, N = L::CW_MAX / CH;
     const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
     float mx = -INFINITY;
     float x[2][CH];
@@ -512,6 +513,7 @@ __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, flo
 template <class L>
 __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at)
 {
+    constexpr int CH = L::CH;
 #pragma unroll 1
     for (int c0 = 0; c0 < w.ncol; c0 += CH) {
         float x[CH];
@@ -597,6 +599,7 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
 template <class L>
 __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const Item &it, int n_item)
 {
+    constexpr int CH = L::CH;
     const int cw = 16 << (it.flags & 3), pitch = min(2 * L::NWG * cw, 128), at = s.wg * 2 * cw;  // columns a warpgroup; bytes of P
     const uint32_t lanes = (uint32_t)(s.quarter * 32) << 16;
     SoftItem w;
@@ -796,10 +799,10 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
             }
         }
     }
-    // columns that fill up a warpgroup's last sixteen take part, unused; they see nothing
+    // columns that fill up a warpgroup's last CH take part, unused; they see nothing
     for (int g = w; g < L::NWG; g += W) {
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
-        if (ncol + lane < ((ncol + CH - 1) & ~(CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
+        if (ncol + lane < ((ncol + L::CH - 1) & ~(L::CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
     }
     // the largest exponent of the range's values
     uint32_t top = 0;
