@@ -95,7 +95,7 @@ struct Shape {
     static constexpr int NWG = WIDE ? 2 : 1;              // softmax warpgroups
     static constexpr int R_MAX = WIDE ? 128 : D == 128 ? 16 : 32;  // rows an item
     static constexpr int CW_MAX = R_MAX / NWG;            // columns of a warpgroup
-    static constexpr int CH = WIDE ? 16 : 8;              // columns a softmax thread has in hand at a time
+    static constexpr int CH = WIDE ? 16 : 4;              // columns a softmax thread has in hand at a time
     static constexpr int THREADS = 128 + NWG * WG;
     static constexpr int CTAS = WIDE ? 1 : 2;             // an SM
     // tensor memory columns: two buffers of R_MAX scores, the output
@@ -335,7 +335,8 @@ template <int CH>
 __device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
 {
     uint32_t *r = reinterpret_cast<uint32_t *>(x);
-    if constexpr (CH == 8) tmem_ld8(at, r);
+    if constexpr (CH == 4) tmem_ld4(at, r);
+    else if constexpr (CH == 8) tmem_ld8(at, r);
     else if constexpr (CH == 16) tmem_ld16(at, *reinterpret_cast<uint32_t(*)[16]>(r));
     else tmem_ld32(at, r);
 }
@@ -439,8 +440,9 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
         }
         // P and the values take the place of the last tile's once its product is done
         if (c0 == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
+        if constexpr (CH == 4) sts64(w.p_row + (w.p_mix ^ (2 * c0)), h[0], h[1]);
 #pragma unroll
-        for (int i = 0; i < CH / 2; i += 4) sts128(w.p_row + (w.p_mix ^ (2 * c0 + 4 * i)), h[i], h[i + 1], h[i + 2], h[i + 3]);
+        for (int i = 0; i + 4 <= CH / 2; i += 4) sts128(w.p_row + (w.p_mix ^ (2 * c0 + 4 * i)), h[i], h[i + 1], h[i + 2], h[i + 3]);
     }
     if (w.ncol == 0 && s.g > 0) soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
     widen_values<L>(s, valid);
