@@ -1319,40 +1319,83 @@ int items_of(const RowTile &x, double most, int *per_item)
     return (n + *per_item - 1) / *per_item;
 }
 
-// How long an item of the wide (or of the narrow) tiles may get: the shortest estimated run among some lengths,
-// where a run is its items spread over the CTAs plus half of the longest one.  Keeps
-// to the records and partial rows that are left, if it splits at all.
+// Items of one cost.
+struct Same {
+    float cost;
+    int64_t items;
+};
+
+// How long the CTAs take for items handed out in falling order of cost, forwards and backwards in turn: of
+// every two rounds, the longer of a CTA's at the ends of a round and at its middle.
+double run_length(std::vector<Same> &v, int ctas)
+{
+    std::sort(v.begin(), v.end(), [](const Same &x, const Same &y) { return x.cost > y.cost; });
+    int64_t all = 0;
+    for (Same &x : v) x.items = all += x.items;  // (now up to and with these)
+    auto cost = [&](int64_t rank) {
+        const auto it = std::upper_bound(v.begin(), v.end(), rank, [](int64_t r, const Same &x) { return r < x.items; });
+        return it == v.end() ? 0.0 : (double)it->cost;
+    };
+    double sum = 0;
+    for (int64_t r = 0; r < all; r += 2 * (int64_t)ctas)
+        sum += std::max(cost(r) + cost(r + 2 * ctas - 1), cost(r + ctas - 1) + cost(r + ctas));
+    return sum;
+}
+
+// How long an item of the wide (or of the narrow) tiles may get: the shortest estimated run among some lengths.
+// With few tiles (long ranges, many items each) the run is what its rounds of items take, which is why
+// lengths a little above a whole part of a CTA's share are among them: with the share's fourth itself some
+// CTAs got a fifth item (two requests of 200,000 tokens took 116 us, now 99 us).  With many it is their items spread over
+// the CTAs plus half of the longest one.  Keeps to the records and partial rows that are left, if it
+// splits at all.
 double split_limit(const std::vector<RowTile> &tiles, bool wide, int KV, int G, int ctas, int64_t *recs_left, int64_t *rows_left)
 {
+    constexpr int FEW = 64;
     double whole = 0;
+    int kind = 0;
     for (const RowTile &x : tiles)
-        if (x.wide == wide) whole += KV * (tile_cost(x) * ((x.len + TT - 1) / TT));
+        if (x.wide == wide) {
+            whole += KV * (tile_cost(x) * ((x.len + TT - 1) / TT));
+            ++kind;
+        }
     const double even = std::max(1.0, whole / ctas);
     double best = 1e300, limit = 1e300;
     int64_t best_recs = 0, best_rows = 0;
-    for (double part : {0.0, 2.0, 1.0, 0.66, 0.5, 0.33, 0.25, 0.125}) {  // 0: no splits
+    std::vector<Same> same;
+    auto consider = [&](double part) {  // 0: no splits
         const double most = part == 0.0 ? 1e300 : std::max(1.0, even * part);
+        const float fixed = wide ? WIDE_ITEM : NARROW_ITEM;
         double sum = 0, longest = 0;
         int64_t recs = 0, rows = 0;
+        same.clear();
         for (const RowTile &x : tiles) {
             if (x.wide != wide) continue;
-            const float cost = tile_cost(x), fixed = wide ? WIDE_ITEM : NARROW_ITEM;
+            const float cost = tile_cost(x);
             int per_item;
-            const int items = items_of(x, most, &per_item);
+            const int n = (x.len + TT - 1) / TT, items = items_of(x, most, &per_item);
             recs += items;
             rows += (int64_t)items * KV * x.ntok * G;
-            sum += KV * ((x.len + TT - 1) / TT * cost + items * fixed);
+            sum += KV * (n * cost + items * fixed);
             longest = std::max(longest, (double)per_item * cost + fixed);
+            if (kind <= FEW) {
+                const int less = n / items, more = n - less * items;  // `more` items have a tile more
+                if (more > 0) same.push_back({(less + 1) * cost + fixed, (int64_t)more * KV});
+                same.push_back({less * cost + fixed, (int64_t)(items - more) * KV});
+            }
         }
-        const double est = std::max(longest, sum / ctas + 0.5 * longest);
-        if (part != 0.0 && (recs > *recs_left || rows > *rows_left)) continue;
+        if (part != 0.0 && (recs > *recs_left || rows > *rows_left)) return;
+        const double est = kind <= FEW ? run_length(same, ctas) : std::max(longest, sum / ctas + 0.5 * longest);
         if (est < best) {
             best = est;
             limit = most;
             best_recs = recs;
             best_rows = rows;
         }
-    }
+    };
+    for (double part : {0.0, 2.0, 1.0, 0.66, 0.5, 0.33, 0.25, 0.125}) consider(part);
+    if (kind <= FEW)
+        for (int k : {1, 2, 3, 4, 6, 8})
+            for (double more : {1.03, 1.06, 1.1}) consider(more / k);
     *recs_left -= best_recs;
     *rows_left -= best_rows;
     return limit;
