@@ -24,8 +24,8 @@
 // other (scores out of tensor memory, exponentials, P and V into shared memory, vote, product).  With 128
 // rows of 128 elements a tile takes about 4,300 cycles, 1,024 of them exponentials at the SM's rate and
 // 512 products: four prompt chunks of 900 to 2,048 tokens behind 4,096 take 1.2 ms (520 TFLOP/s).  With four
-// rows it is 2,400 cycles, two CTAs of an SM side by side: two requests of 200,000 tokens and more with
-// heads of 64 take 128 us (3.5 TB/s).
+// rows it is 2,100 cycles, two CTAs of an SM side by side: two requests of 200,000 tokens and more with
+// heads of 64 take 99 us (4.5 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -391,8 +391,8 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 
 // P of a tile and the warpgroup's share of its widened values into shared
 // memory, the probabilities times `sign` to the sums l.  Returns the largest log2 P
-// of the token.  Columns go by sixteens (the last ones are filled up; fetching the next ones'
-// scores ahead took 3% longer, in registers).  (One copy of this code for every number of
+// of the token.  Columns go by sixteens, where rows are few by fours (the last ones are filled up; fetching the next ones'
+// scores ahead took 3% longer, in registers; sixteens for four rows took 10% longer).  (One copy of this code for every number of
 // rows: with one for each, and one for masked tiles, the kernel had 223 KB of code and
 // an item's first tile waited 6,000 cycles for instructions.)
 template <class L>
@@ -1088,7 +1088,9 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
 // rows are so few that the time is that of a row's loads one behind the other.  A
 // warp has the logarithms of 32 items over its lanes, and four items' rows under way.
 constexpr int COMBINE_WARPS = 4, COMBINE_SPLIT = 16;
-constexpr int COMBINE_FEW = 4;  // rows an SM up to which they are split: the CTAs of COMBINE_SPLIT warps that it holds
+// Rows an SM up to which they are split: the CTAs of COMBINE_SPLIT warps that it holds.  64 rows of 80 items each took
+// 21 us with a warp a row and 7 us split; 2,048 rows of few items gain nothing (64 us a run with a warp a row, 66 split).
+constexpr int COMBINE_FEW = 4;
 
 template <int D, int SPLIT>
 __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : COMBINE_WARPS)) attn_combine_kernel(const __grid_constant__ AttnParams p)
@@ -1306,7 +1308,8 @@ struct RowTile {
 };
 
 // The time of an item in units of a narrow item's tile of 128 tokens, from measurements: a
-// tile of each class of wide items, and what an item takes besides.
+// tile of each class of wide items, and what an item takes besides.  (3, 6 and 8 for a wide item and 1.5 to 4 for
+// a narrow one move the batches measured by 2% at most, 1 for a narrow one costs up to 9%.)
 constexpr float NARROW_TILE = 1.f, NARROW_ITEM = 2.f;
 constexpr float WIDE_TILE[3] = {1.1f, 1.4f, 2.2f};
 constexpr float WIDE_ITEM = 6.f;
