@@ -138,7 +138,8 @@ struct Shape {
     static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
     static_assert(TM_O + R_MAX <= TM_COLS, "tensor memory");
 };
-// Rows up to which an item is narrow, and at most.
+// Rows up to which an item is narrow, and at most.  (With the wide kernel for all of them, two requests of 200,000 tokens
+// took 183 us where the narrow one took 159, and a step of 256 requests 527 and 503.)
 constexpr int narrow_rows(int D) { return D == 128 ? Shape<128, false>::R_MAX : Shape<64, false>::R_MAX; }
 constexpr int WIDE_ROWS = Shape<128, true>::R_MAX;
 
