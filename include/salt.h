@@ -669,10 +669,10 @@ salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_
  * [tokens][n_heads] or NULL.  Scores, running maxima, sums and partial results
  * are held in fp32 and out is rounded once.  The query meets the cached keys
  * as the sum of two e4m3 terms (about 8 bits, as bf16), the probabilities meet
- * the cached values, widened exactly, in f16 (11 bits).  A row with an infinity or a NaN
- * in its query, or that sees a cached key standing for NaN, is NaN; so is one that sees a
- * cached value standing for NaN with a probability within fp32's range.  Results do not depend on
- * timing.
+ * the cached values, widened exactly, in f16 (11 bits).  A row that sees a token is NaN if there is
+ * an infinity or a NaN in its query or it sees a cached key standing for NaN; if it sees a
+ * cached value standing for NaN, out is, whatever that token's probability.  Results do not
+ * depend on timing.
  * Asynchronous on `stream`; runs of one plan share its workspace and are
  * ordered one after the other.  A captured run may be replayed after the
  * plan was built again with at most as many query tokens as it had at the capture; on a larger

@@ -58,6 +58,8 @@ constexpr int TT = 128;          // cached tokens a tile
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
+constexpr float VF_NAN = 0x1p127f; // the factor of a token's P where its value stands for NaN
+constexpr uint32_t TOP_NAN = 256; // beside a range's largest value exponent: a value stands for NaN
 constexpr float M_NONE = -1e30f; // the reference before the first token
 
 struct AttnParams {
@@ -133,7 +135,7 @@ struct Shape {
     static constexpr uint32_t O_FREE = Q_FULL + 16;
     static constexpr uint32_t Q_FREE = O_FREE + 16;
     static constexpr uint32_t DRAIN = Q_FREE + 16;
-    static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents
+    static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents, whether the first item has a NaN value
     static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
     static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
     static_assert(TM_O + R_MAX <= TM_COLS, "tensor memory");
@@ -159,6 +161,13 @@ __device__ __forceinline__ float ex2(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+    return r;
+}
+// the larger one, NaN if either is
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 // 2^k, 0 below the normal range (k <= 127)
@@ -348,7 +357,7 @@ __device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
 struct Token {
     int at;
     float kf, vf, vref;
-    bool mask;                        // some row does not see the whole tile
+    bool all;                         // every row sees the whole tile, and no value of the item stands for NaN
 };
 
 // The warpgroups' share of a tile's values in f16; zeros for rows that stand
@@ -420,10 +429,13 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
             y[i + 2] = v.x;
             y[i + 3] = v.y;
         }
-        if (t.mask) {
+        if (!t.all) {
+            const float least = t.vf == VF_NAN ? -100.f : -INFINITY;
 #pragma unroll
             for (int i = 0; i < CH; i += 4) {
                 const uint4 n = lds128(at + L::IN_LIM + 4 * i);
+#pragma unroll
+                for (int k = i; k < i + 4; ++k) y[k] = max_nan(y[k], least);
                 if (t.at >= (int)n.x) y[i] = -INFINITY;
                 if (t.at >= (int)n.y) y[i + 1] = -INFINITY;
                 if (t.at >= (int)n.z) y[i + 2] = -INFINITY;
@@ -450,9 +462,9 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
     return mx + t.vref;
 }
 
-// soft_probs where every column of the warpgroup is a row and every row sees every token: no
-// branches, and each sixteen columns' exponentials run beside the next ones' loads and products.
-// (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
+// soft_probs where every column of the warpgroup is a row, every row sees every token and no value stands for NaN: no
+// branches (with one for such values prompt chunks took 22% longer, with a vote on a tile's 5%), and each sixteen columns'
+// exponentials run beside the next ones' loads and products.  (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
 // loads, a tile of 128 rows took 2,100 cycles here.)
 template <class L>
 __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
@@ -589,7 +601,7 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
     for (int pass = FIRST;; ++pass) {
         if ((pass == AGAIN || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
         const float sign = pass == TAKE_OUT ? -1.f : 1.f;
-        const float mx = L::WIDE && w.ncol == L::CW_MAX && !t.mask ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
+        const float mx = L::WIDE && w.ncol == L::CW_MAX && t.all ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
                                                                    : soft_probs<L>(s, w, l, t, s_at, sign, valid);
         if (pass == TAKE_OUT) continue;
         if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
@@ -617,7 +629,10 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
     w.nb = 1 + s.wg;
     // values count in units of the largest exponent of the range
-    w.vtop = max((int)lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), (int)lds32(s.base + L::MISC + 12 + 8 * (n_item & 1)));
+    const uint32_t top0 = lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), top1 = lds32(s.base + L::MISC + 12 + 8 * (n_item & 1));
+    w.vtop = (int)max(top0 & 255u, top1 & 255u);
+    const bool nan = ((top0 | top1) & TOP_NAN) || (n_item == 0 && lds32(s.base + L::MISC + 24));
+    const int all_to = nan ? 0 : min(it.t1, it.lim);  // (the first query token sees least)
     if (w.vtop == 0) w.vtop = 127;
     float2 l[L::CW_MAX / 2];
 #pragma unroll
@@ -633,11 +648,12 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         Token t;
         t.at = end - TT + s.tid;
         t.kf = row_scale(ke);
-        // A NaN row's values are zero codes: an infinite P makes the rows that see the token NaN, and where P is
-        // 0, as where they do not see it, it adds nothing.
-        t.vf = t.at >= it.t1 ? 0.f : ve == 255u ? 0x1p127f : pow2((int)ve - w.vtop);
+        // The values of a row that stands for NaN are zero codes: an infinite P makes the rows that see the token NaN, and
+        // where they do not see it P is 0 and adds nothing.  So that every row that sees it gets the infinity, its p
+        // is 2^-100 at least, which the sums do not notice.
+        t.vf = t.at >= it.t1 ? 0.f : ve == 255u ? VF_NAN : pow2((int)ve - w.vtop);
         t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
-        t.mask = end > min(it.t1, it.lim);  // (the first query token sees least)
+        t.all = end <= all_to;
         if (!soft_tile<L>(s, w, l, t, it.t1 - (end - TT))) return false;
         tc_fence_before();
         fence_async_smem();
@@ -807,8 +823,8 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
         if (ncol + lane < ((ncol + L::CH - 1) & ~(L::CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
     }
-    // the largest exponent of the range's values
-    uint32_t top = 0;
+    // the largest exponent of the range's values, and whether one stands for NaN
+    uint32_t top = 0, nans = 0;
     for (int t = t_first; t < it.t1; t += t_step) {
         const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
         const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
@@ -818,15 +834,22 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
         for (int i = 0; i < 4; ++i) {
             const int n = min(max(it.t1 - t - 4 * i, 0), 4);  // bytes of tokens in the range
             const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
-            top = __vmaxu4(top, x[i] & in & ~__vcmpeq4(x[i], 0xffffffffu));
+            const uint32_t nan = __vcmpeq4(x[i], 0xffffffffu) & in;
+            top = __vmaxu4(top, x[i] & in & ~nan);
+            nans |= nan;
         }
     }
     top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
     top = __reduce_max_sync(0xffffffffu, top);
+    nans = __any_sync(0xffffffffu, nans != 0) ? TOP_NAN : 0u;
     const uint32_t slot = base + L::MISC + 8 + 8 * (n_item & 1) + 4 * (w & 1);
     if (lane == 0) {
-        if (n_item == 0) asm volatile("red.shared.max.u32 [%0], %1;\n" ::"r"(slot), "r"(top) : "memory");
-        else sts32(slot, top);  // (two warps)
+        if (n_item == 0) {
+            asm volatile("red.shared.max.u32 [%0], %1;\n" ::"r"(slot), "r"(top) : "memory");
+            if (nans) sts32(base + L::MISC + 24, nans);
+        } else {
+            sts32(slot, top | nans);  // (two warps)
+        }
     }
     fence_async_smem();
 }
@@ -861,6 +884,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
         mbar_init(base + L::DRAIN, 1);
         *dead = 0;
         sts64(base + L::MISC + 8, 0, 0);
+        sts32(base + L::MISC + 24, 0);
         mbar_fence_init();
     }
     if (warp == 1) {
