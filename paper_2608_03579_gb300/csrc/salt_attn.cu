@@ -58,8 +58,7 @@ constexpr int TT = 128;          // cached tokens a tile
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
-constexpr float VF_NAN = 0x1p127f; // the factor of a token's P where its value stands for NaN
-constexpr uint32_t TOP_NAN = 256; // beside a range's largest value exponent: a value stands for NaN
+constexpr int NEVER = 0x7fffffff; // the place of a range's first value that stands for NaN where there is none
 constexpr float M_NONE = -1e30f; // the reference before the first token
 
 struct AttnParams {
@@ -135,8 +134,8 @@ struct Shape {
     static constexpr uint32_t O_FREE = Q_FULL + 16;
     static constexpr uint32_t Q_FREE = O_FREE + 16;
     static constexpr uint32_t DRAIN = Q_FREE + 16;
-    static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents, whether the first item has a NaN value
-    static constexpr uint32_t BYTES = MISC + 32 + 1024;   // slack for the 1024-byte alignment
+    static constexpr uint32_t MISC = DRAIN + 8;           // TMEM address, failure flag, [2][2] largest value exponents, [2][2] first NaN values
+    static constexpr uint32_t BYTES = MISC + 48 + 1024;   // slack for the 1024-byte alignment
     static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
     static_assert(TM_O + R_MAX <= TM_COLS, "tensor memory");
 };
@@ -161,13 +160,6 @@ __device__ __forceinline__ float ex2(float x)
 {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-    return r;
-}
-// the larger one, NaN if either is
-__device__ __forceinline__ float max_nan(float a, float b)
-{
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;\n" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 // 2^k, 0 below the normal range (k <= 127)
@@ -357,7 +349,7 @@ __device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
 struct Token {
     int at;
     float kf, vf, vref;
-    bool all;                         // every row sees the whole tile, and no value of the item stands for NaN
+    bool mask;                        // some row does not see the whole tile
 };
 
 // The warpgroups' share of a tile's values in f16; zeros for rows that stand
@@ -429,13 +421,10 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
             y[i + 2] = v.x;
             y[i + 3] = v.y;
         }
-        if (!t.all) {
-            const float least = t.vf == VF_NAN ? -100.f : -INFINITY;
+        if (t.mask) {
 #pragma unroll
             for (int i = 0; i < CH; i += 4) {
                 const uint4 n = lds128(at + L::IN_LIM + 4 * i);
-#pragma unroll
-                for (int k = i; k < i + 4; ++k) y[k] = max_nan(y[k], least);
                 if (t.at >= (int)n.x) y[i] = -INFINITY;
                 if (t.at >= (int)n.y) y[i + 1] = -INFINITY;
                 if (t.at >= (int)n.z) y[i + 2] = -INFINITY;
@@ -462,9 +451,9 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
     return mx + t.vref;
 }
 
-// soft_probs where every column of the warpgroup is a row, every row sees every token and no value stands for NaN: no
-// branches (with one for such values prompt chunks took 22% longer, with a vote on a tile's 5%), and each sixteen columns'
-// exponentials run beside the next ones' loads and products.  (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
+// soft_probs where every column of the warpgroup is a row and every row sees every token: no
+// branches, and each sixteen columns' exponentials run beside the next ones' loads and products.
+// (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
 // loads, a tile of 128 rows took 2,100 cycles here.)
 template <class L>
 __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
@@ -601,7 +590,7 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
     for (int pass = FIRST;; ++pass) {
         if ((pass == AGAIN || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
         const float sign = pass == TAKE_OUT ? -1.f : 1.f;
-        const float mx = L::WIDE && w.ncol == L::CW_MAX && t.all ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
+        const float mx = L::WIDE && w.ncol == L::CW_MAX && !t.mask ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
                                                                    : soft_probs<L>(s, w, l, t, s_at, sign, valid);
         if (pass == TAKE_OUT) continue;
         if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
@@ -629,10 +618,7 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     w.ncol = min(max(it.rows - s.wg * it.per, 0), it.per);
     w.nb = 1 + s.wg;
     // values count in units of the largest exponent of the range
-    const uint32_t top0 = lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), top1 = lds32(s.base + L::MISC + 12 + 8 * (n_item & 1));
-    w.vtop = (int)max(top0 & 255u, top1 & 255u);
-    const bool nan = ((top0 | top1) & TOP_NAN) || (n_item == 0 && lds32(s.base + L::MISC + 24));
-    const int all_to = nan ? 0 : min(it.t1, it.lim);  // (the first query token sees least)
+    w.vtop = max((int)lds32(s.base + L::MISC + 8 + 8 * (n_item & 1)), (int)lds32(s.base + L::MISC + 12 + 8 * (n_item & 1)));
     if (w.vtop == 0) w.vtop = 127;
     float2 l[L::CW_MAX / 2];
 #pragma unroll
@@ -648,12 +634,10 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         Token t;
         t.at = end - TT + s.tid;
         t.kf = row_scale(ke);
-        // The values of a row that stands for NaN are zero codes: an infinite P makes the rows that see the token NaN, and
-        // where they do not see it P is 0 and adds nothing.  So that every row that sees it gets the infinity, its p
-        // is 2^-100 at least, which the sums do not notice.
-        t.vf = t.at >= it.t1 ? 0.f : ve == 255u ? VF_NAN : pow2((int)ve - w.vtop);
+        // (a value that stands for NaN adds nothing; the rows that see it are known at the end)
+        t.vf = t.at >= it.t1 || ve == 255u ? 0.f : pow2((int)ve - w.vtop);
         t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
-        t.all = end <= all_to;
+        t.mask = end > min(it.t1, it.lim);  // (the first query token sees least)
         if (!soft_tile<L>(s, w, l, t, it.t1 - (end - TT))) return false;
         tc_fence_before();
         fence_async_smem();
@@ -696,7 +680,10 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
             to = (int64_t)part * L::D;
             p.part_l[part] = lse2;
         }
-        stsf(w.fac + 4 * s.tid, t > 0.f ? 1.f / t : t == t ? 0.f : t);
+        // a row that sees a value that stands for NaN is NaN, but for its log-sum
+        const int first_nan = min((int)lds32(s.base + L::MISC + 24 + 8 * (n_item & 1)), (int)lds32(s.base + L::MISC + 28 + 8 * (n_item & 1)));
+        const bool spoiled = (int)lds32(at_i + L::IN_LIM) > first_nan;
+        stsf(w.fac + 4 * s.tid, spoiled ? __uint_as_float(0x7fc00000u) : t > 0.f ? 1.f / t : t == t ? 0.f : t);
         sts64(w.place + 8 * s.tid, (uint32_t)to, (uint32_t)(to >> 32));
     }
     soft_wait(s, s.base + L::PV_DONE, (s.g - 1) & 1);
@@ -734,7 +721,7 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
 }
 
 // An item's queries: rows scaled by a power of two and split in hi + lo, the
-// constants of its columns, the largest exponent of its values.  W warps, this
+// constants of its columns, the largest exponent of its values and the first of them that stands for NaN.  W warps, this
 // one the w-th.
 template <class L>
 __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base, const Item &it, int n_item, int w, int W)
@@ -823,8 +810,9 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
         if (ncol + lane < ((ncol + L::CH - 1) & ~(L::CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
     }
-    // the largest exponent of the range's values, and whether one stands for NaN
-    uint32_t top = 0, nans = 0;
+    // the largest exponent of the range's values, the first one that stands for NaN
+    uint32_t top = 0;
+    int first_nan = NEVER;
     for (int t = t_first; t < it.t1; t += t_step) {
         const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + it.kh) << p.kv.page_log2) + (t & (p.kv.page - 1));
         const uint4 e = __ldg(reinterpret_cast<const uint4 *>(p.kv.v_exp + at));
@@ -836,19 +824,20 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
             const uint32_t in = n == 4 ? 0xffffffffu : (1u << (8 * n)) - 1u;
             const uint32_t nan = __vcmpeq4(x[i], 0xffffffffu) & in;
             top = __vmaxu4(top, x[i] & in & ~nan);
-            nans |= nan;
+            if (nan) first_nan = min(first_nan, t + 4 * i + (__ffs(nan) - 1) / 8);
         }
     }
     top = max(max(top & 255u, (top >> 8) & 255u), max((top >> 16) & 255u, top >> 24));
     top = __reduce_max_sync(0xffffffffu, top);
-    nans = __any_sync(0xffffffffu, nans != 0) ? TOP_NAN : 0u;
+    first_nan = __reduce_min_sync(0xffffffffu, first_nan);
     const uint32_t slot = base + L::MISC + 8 + 8 * (n_item & 1) + 4 * (w & 1);
     if (lane == 0) {
         if (n_item == 0) {
             asm volatile("red.shared.max.u32 [%0], %1;\n" ::"r"(slot), "r"(top) : "memory");
-            if (nans) sts32(base + L::MISC + 24, nans);
-        } else {
-            sts32(slot, top | nans);  // (two warps)
+            asm volatile("red.shared.min.s32 [%0], %1;\n" ::"r"(slot + 16), "r"(first_nan) : "memory");
+        } else {  // (two warps)
+            sts32(slot, top);
+            sts32(slot + 16, (uint32_t)first_nan);
         }
     }
     fence_async_smem();
@@ -884,7 +873,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) attn_tile_kernel(const __
         mbar_init(base + L::DRAIN, 1);
         *dead = 0;
         sts64(base + L::MISC + 8, 0, 0);
-        sts32(base + L::MISC + 24, 0);
+        sts64(base + L::MISC + 24, NEVER, NEVER);
         mbar_fence_init();
     }
     if (warp == 1) {
