@@ -17,8 +17,9 @@
 //
 // Softmax: thread = token, registers = rows.  The reference m of a row moves
 // only when a probability passes f16's range (a vote a tile), so the usual tile
-// needs no reduction over tokens: p = 2^(s - m), l += p, P = p 2^e_v.  Items of one
-// row meet in the combine kernel through their (o / l, m + log2 l).
+// needs no reduction over tokens: p = 2^(s - m), l += p, P = p 2^(e_v + P_UP), e_v the exponent of the token's value
+// under the range's largest.  m follows the largest P; where values are small or zero p is far above it, so l
+// counts p in units that leave room.  Items of one row meet in the combine kernel through their (o / l, m + log2 l).
 //
 // What bounds it: neither memory nor the tensor cores but the steps of a tile one behind the
 // other (scores out of tensor memory, exponentials, P and V into shared memory, vote, product).  With 128
@@ -56,6 +57,11 @@ constexpr int RF_DIRECT = 8, RF_CAUSAL = 16;
 
 constexpr int TT = 128;          // cached tokens a tile
 constexpr int WG = 128;          // threads of a softmax warpgroup (one per token of a tile)
+// The largest P is in [2^2, 2^16), a p in units of 2^-P_UP and where the value is small up to 2^P_LOW above that: the sum of 2^26
+// tokens is in fp32's range, and where a p above 2^128 makes a sum infinite what it held before was nothing
+// next to it.  A row's P lose bits where one of 2^-P_LOW of its values or less (or zero) has 2^(P_LOW + 16) times their probability.
+constexpr int P_UP = 40, P_LOW = 125;
+constexpr float P_HOT = 120.f;   // log2 of a p that sums may not hold
 constexpr float P_TOP = 2.f;     // a new reference puts the row's largest P at 2^2
 constexpr float P_MOST = 15.9f;  // and is due when one passes 2^15.9 (f16 ends at 65504)
 constexpr int NEVER = 0x7fffffff; // the place of a range's first value that stands for NaN where there is none
@@ -392,17 +398,17 @@ __device__ __forceinline__ void widen_values(const Soft &s, int valid)
 }
 
 // P of a tile and the warpgroup's share of its widened values into shared
-// memory, the probabilities times `sign` to the sums l.  Returns the largest log2 P
+// memory, the probabilities times `add` to the sums l.  Returns the largest log2 P
 // of the token.  Columns go by sixteens, where rows are few by fours (the last ones are filled up; fetching the next ones'
 // scores ahead took 3% longer, in registers; sixteens for four rows took 10% longer).  (One copy of this code for every number of
 // rows: with one for each, and one for masked tiles, the kernel had 223 KB of code and
 // an item's first tile waited 6,000 cycles for instructions.)
 template <class L>
 __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
-                                            float sign, int valid)
+                                            float add, int valid)
 {
     constexpr int CH = L::CH;
-    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
+    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), add1 = make_float2(add, add);
     float mx = -INFINITY;
 #pragma unroll
     for (int c0 = 0; c0 < L::CW_MAX; c0 += CH) {
@@ -436,7 +442,7 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
         for (int i = 0; i < CH; i += 2) {
             mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
             const float2 e = make_float2(ex2(y[i]), ex2(y[i + 1])), v = mul2(e, vf2);
-            l[(c0 + i) / 2] = fma2(e, sign2, l[(c0 + i) / 2]);
+            l[(c0 + i) / 2] = fma2(e, add1, l[(c0 + i) / 2]);
             const __half2 q = __floats2half2_rn(v.x, v.y);
             h[i / 2] = *reinterpret_cast<const uint32_t *>(&q);
         }
@@ -457,10 +463,10 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
 // loads, a tile of 128 rows took 2,100 cycles here.)
 template <class L>
 __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,
-                                                 float sign, int valid)
+                                                 float add, int valid)
 {
     constexpr int CH = L::CH, N = L::CW_MAX / CH;
-    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), sign2 = make_float2(sign, sign);
+    const float2 kf2 = make_float2(t.kf, t.kf), vf2 = make_float2(t.vf, t.vf), add1 = make_float2(add, add);
     float mx = -INFINITY;
     float x[2][CH];
     float4 a[CH / 4], m[CH / 4];
@@ -496,7 +502,7 @@ __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, flo
         for (int i = 0; i < CH; i += 2) {
             mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
             const float2 e = make_float2(ex2(y[i]), ex2(y[i + 1])), v = mul2(e, vf2);
-            l[(c * CH + i) / 2] = fma2(e, sign2, l[(c * CH + i) / 2]);
+            l[(c * CH + i) / 2] = fma2(e, add1, l[(c * CH + i) / 2]);
             const __half2 q = __floats2half2_rn(v.x, v.y);
             h[i / 2] = *reinterpret_cast<const uint32_t *>(&q);
         }
@@ -508,6 +514,32 @@ __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, flo
     }
     widen_values<L>(s, valid);
     return mx + t.vref;
+}
+
+// Takes a tile's probabilities out of the sums of a thread that has very large ones.  What an infinite sum held before
+// was nothing next to what made it so (a NaN stays).  The whole warp; by way of local memory, as this hardly ever runs and the
+// sums' registers are better left alone.
+template <class L>
+__device__ __forceinline__ void take_out(const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at, bool mine)
+{
+    float sums[L::CW_MAX];
+#pragma unroll
+    for (int c = 0; c < L::CW_MAX; ++c) sums[c] = c & 1 ? l[c / 2].y : l[c / 2].x;
+#pragma unroll 1
+    for (int c0 = 0; c0 < w.ncol; c0 += 4) {
+        float y[4];
+        load_columns<4>(y, s_at + c0);
+        tmem_ld_wait();
+#pragma unroll 1
+        for (int c = c0; c < min(c0 + 4, w.ncol); ++c) {
+            const uint32_t at = w.info + 4 * c;
+            const float x = fmaf(y[0], ldsf(at + L::IN_A) * t.kf, ldsf(at + L::IN_M));
+            y[0] = y[1], y[1] = y[2], y[2] = y[3];
+            if (mine && t.at < (int)lds32(at + L::IN_LIM)) sums[c] = sums[c] == INFINITY ? 0.f : sums[c] - ex2(x);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < L::CW_MAX; ++c) (c & 1 ? l[c / 2].y : l[c / 2].x) = sums[c];
 }
 
 // Moves the references that a score of this tile passes by too much (all of
@@ -549,7 +581,7 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
             m = -ldsf(w.info + L::IN_M + 4 * s.tid);
             move = v - m > P_MOST;
         }
-        stsf(w.fac + 4 * s.tid, move ? ex2(m - (v - P_TOP)) : 1.f);
+        stsf(w.fac + 4 * s.tid, move ? ex2(0.5f * (m - (v - P_TOP))) : 1.f);  // (applied twice: 2^-160 is no float)
         if (move) stsf(w.info + L::IN_M + 4 * s.tid, P_TOP - v);
     }
     named_sync(w.nb, WG);
@@ -560,18 +592,18 @@ __device__ __forceinline__ void move_refs(const Soft &s, const SoftItem &w, floa
             tmem_ld8(w.o_at + c0, reinterpret_cast<uint32_t *>(o));
             tmem_ld_wait();
 #pragma unroll
-            for (int c = 0; c < 8; ++c) o[c] *= ldsf(w.fac + 4 * (c0 + c));
+            for (int c = 0; c < 8; ++c) {
+                const float f = ldsf(w.fac + 4 * (c0 + c));
+                o[c] = o[c] * f * f;
+            }
             tmem_st8(w.o_at + c0, reinterpret_cast<const uint32_t *>(o));
         }
         tmem_st_wait();
 #pragma unroll
         for (int c = 0; c < L::CW_MAX; c += 4) {
-            // (a sum is nothing next to a score 2^100 above, and may have been put out of range by it)
             const float4 f = lds4f(w.fac + 4 * c);
-            l[c / 2].x = f.x < 0x1p-100f ? 0.f : l[c / 2].x * f.x;
-            l[c / 2].y = f.y < 0x1p-100f ? 0.f : l[c / 2].y * f.y;
-            l[c / 2 + 1].x = f.z < 0x1p-100f ? 0.f : l[c / 2 + 1].x * f.z;
-            l[c / 2 + 1].y = f.w < 0x1p-100f ? 0.f : l[c / 2 + 1].y * f.w;
+            l[c / 2] = mul2(mul2(l[c / 2], make_float2(f.x, f.y)), make_float2(f.x, f.y));
+            l[c / 2 + 1] = mul2(mul2(l[c / 2 + 1], make_float2(f.z, f.w)), make_float2(f.z, f.w));
         }
     }
 }
@@ -582,19 +614,19 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
 {
     const uint32_t s_at = w.s_at + (s.g & 1) * L::R_MAX;
     // References are set before an item's first tile; where a later one passes
-    // them by too much its probabilities are taken out of the sums again, the
-    // references moved and the tile done anew.  (Then they fit, but for scores so large
-    // that fp32 rounds them by more than P_MOST.)
-    enum { FIRST, TAKE_OUT, AGAIN };
+    // them by too much they are moved and the tile's P made anew.  Its probabilities are in the sums already and
+    // are scaled with them, but for those of a thread whose sums may have left fp32's range.  (Then P fits, but
+    // for scores so large that fp32 rounds them by more than P_MOST.)
+    float add = 1.f;
 #pragma unroll 1
-    for (int pass = FIRST;; ++pass) {
-        if ((pass == AGAIN || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
-        const float sign = pass == TAKE_OUT ? -1.f : 1.f;
-        const float mx = L::WIDE && w.ncol == L::CW_MAX && !t.mask ? soft_probs_full<L>(s, w, l, t, s_at, sign, valid)
-                                                                   : soft_probs<L>(s, w, l, t, s_at, sign, valid);
-        if (pass == TAKE_OUT) continue;
-        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && pass == FIRST && w.j > 0))) return true;
-        if (pass == AGAIN || !named_sync_and(w.nb, WG, s.ok)) return false;
+    for (bool again = false;; again = true) {
+        if (again && __any_sync(0xffffffffu, add != 0.f)) take_out<L>(w, l, t, s_at, add != 0.f);
+        if ((again || w.j == 0) && w.ncol > 0) move_refs<L>(s, w, l, t, s_at);
+        const float mx = L::WIDE && w.ncol == L::CW_MAX && !t.mask ? soft_probs_full<L>(s, w, l, t, s_at, add, valid)
+                                                                   : soft_probs<L>(s, w, l, t, s_at, add, valid);
+        if (named_sync_and(w.nb, WG, s.ok && !(mx > P_MOST && !again && w.j > 0))) return true;
+        if (again || !named_sync_and(w.nb, WG, s.ok)) return false;
+        add = mx - t.vref >= P_HOT ? 1.f : 0.f;
         tc_fence_after();
     }
 }
@@ -635,8 +667,8 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
         t.at = end - TT + s.tid;
         t.kf = row_scale(ke);
         // (a value that stands for NaN adds nothing; the rows that see it are known at the end)
-        t.vf = t.at >= it.t1 || ve == 255u ? 0.f : pow2((int)ve - w.vtop);
-        t.vref = ve == 255u ? 0.f : (float)max((int)ve - w.vtop, -100);
+        t.vf = t.at >= it.t1 || ve == 255u ? 0.f : pow2((int)ve - w.vtop + P_UP);
+        t.vref = (float)(P_UP + (ve == 255u ? -P_LOW : max((int)ve - w.vtop, -P_LOW)));
         t.mask = end > min(it.t1, it.lim);  // (the first query token sees least)
         if (!soft_tile<L>(s, w, l, t, it.t1 - (end - TT))) return false;
         tc_fence_before();
@@ -691,7 +723,9 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
     if (!named_sync_and(w.nb, WG, s.ok)) return false;
     const int dim = L::D == 128 ? s.tid : s.quarter * 16 + s.lane;   // M = 64 uses 16 lanes of each quarter
     const bool live = L::D == 128 || s.lane < 16;
-    const float unit = pow2(w.vtop - 127);
+    // 2^(vtop - 127 - P_UP) in two factors
+    const int e_unit = w.vtop - 127 - P_UP;
+    const float unit = pow2(max(e_unit, -126)), rest = pow2(min(e_unit + 126, 0));
 #pragma unroll 1
     for (int c0 = 0; c0 < w.ncol; c0 += CH) {
         float o[CH];
@@ -706,7 +740,7 @@ __device__ __forceinline__ bool soft_item(const AttnParams &p, Soft &s, const It
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int64_t to = (int64_t)((uint64_t)hi[i] << 32 | lo[i]) + dim;
-                const float v = o[c + i] * k[i] * unit;
+                const float v = o[c + i] * k[i] * unit * rest;
                 if (c0 + c + i < w.ncol && live) {
                     if (direct) p.out[to] = f_to_bf16(v);
                     else p.part_o[to] = v;
@@ -808,7 +842,7 @@ __device__ __forceinline__ void stage_queries(const AttnParams &p, uint32_t base
     // columns that fill up a warpgroup's last CH take part, unused; they see nothing
     for (int g = w; g < L::NWG; g += W) {
         const int ncol = min(max(it.rows - g * it.per, 0), it.per);
-        if (ncol + lane < ((ncol + L::CH - 1) & ~(L::CH - 1))) set_column(g * cw + ncol + lane, 0.f, 0.f, 0, 0);
+        if (ncol + lane < ((ncol + L::CH - 1) & ~(L::CH - 1))) set_column(g * cw + ncol + lane, 0.f, -INFINITY, 0, 0);
     }
     // the largest exponent of the range's values, the first one that stands for NaN
     uint32_t top = 0;
