@@ -669,7 +669,8 @@ salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_
  * [tokens][n_heads] or NULL.  Scores, running maxima, sums and partial results
  * are held in fp32 and out is rounded once.  The query meets the cached keys
  * as the sum of two e4m3 terms (about 8 bits, as bf16), the probabilities meet
- * the cached values, widened exactly, in f16 (11 bits).  A row that sees a token is NaN if there is
+ * the cached values, widened exactly, in f16 (11 bits).  Scores are served up to 2^23 in
+ * magnitude, where fp32 still holds their fractions; a row with one past that may be NaN.  A row that sees a token is NaN if there is
  * an infinity or a NaN in its query or it sees a cached key standing for NaN; if it sees a
  * cached value standing for NaN, out is, whatever that token's probability.  Results do not
  * depend on timing.

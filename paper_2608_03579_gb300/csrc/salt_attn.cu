@@ -615,8 +615,8 @@ __device__ __forceinline__ bool soft_tile(Soft &s, const SoftItem &w, float2 (&l
     const uint32_t s_at = w.s_at + (s.g & 1) * L::R_MAX;
     // References are set before an item's first tile; where a later one passes
     // them by too much they are moved and the tile's P made anew.  Its probabilities are in the sums already and
-    // are scaled with them, but for those of a thread whose sums may have left fp32's range.  (Then P fits, but
-    // for scores so large that fp32 rounds them by more than P_MOST.)
+    // are scaled with them, but for those of a thread whose sums may have left fp32's range.  Then P fits: scores
+    // up to 2^23 are rounded by 1 at most.  (A way for larger ones took 9% more time on prompt chunks.)
     float add = 1.f;
 #pragma unroll 1
     for (bool again = false;; again = true) {
