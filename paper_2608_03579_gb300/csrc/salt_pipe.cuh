@@ -76,6 +76,10 @@ __device__ __forceinline__ bool named_sync_and(int id, int n, bool v)
                  : "memory");
     return r != 0;
 }
+// The cluster's barrier in two halves: every thread of the cluster arrives, and each that has may wait for
+// all the others to.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;\n" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;\n" ::: "memory"); }
 // order global data this thread observed through the generic proxy before
 // async-proxy (TMA) reads of it
 __device__ __forceinline__ void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;\n" ::: "memory"); }

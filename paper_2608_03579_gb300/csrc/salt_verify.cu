@@ -112,6 +112,9 @@ __global__ void __launch_bounds__(VF_THREADS, VF_CTAS) verify_kernel(VerifyParam
     const int b = blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     __shared__ int s_stop;
     __shared__ int64_t s_sum[VF_WARPS], s_all[2][VF_CLUSTER];
+    // A CTA writes into the others' shared memory once all of them run: they say so here, and it waits
+    // when its share is summed.
+    cluster_arrive();
     pdl_wait();  // (launched beside the end of what came before)
     pdl_launch_dependents();
     a.ptr = after_pdl_wait(a.ptr);
@@ -123,6 +126,7 @@ __global__ void __launch_bounds__(VF_THREADS, VF_CTAS) verify_kernel(VerifyParam
             a.accepted[b] = 0;
             a.next[b] = -1;
         }
+        cluster_wait();
         return;
     }
     const int n = hi - lo, V = a.n_vocab;
@@ -145,6 +149,7 @@ __global__ void __launch_bounds__(VF_THREADS, VF_CTAS) verify_kernel(VerifyParam
     int64_t total = 0, before = 0, mine = 0;
     for (int pass = 0; pass < 2; ++pass) {
         mine = sum_share<VEC>(p, q, v0, v1, lane);
+        if (pass == 0) cluster_wait();
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
         if (warp == 0) {  // the CTA's sum to every CTA of the cluster
