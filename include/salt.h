@@ -653,7 +653,8 @@ void salt_attn_destroy(salt_attn *plan);
  * the plan not built) and the work is divided over the SMs.  Asynchronous on
  * `stream`, after the runs enqueued on the previous build; not to be captured
  * (SALT_ERR_INVALID_ARG), but a captured run may be replayed after the plan
- * was built again.
+ * was built again.  While a stream that the plan was built or run on is being
+ * captured, builds and runs on other streams are refused (SALT_ERR_INVALID_ARG).
  */
 salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_stream_t stream);
 
@@ -675,9 +676,12 @@ salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_
  * cached value standing for NaN, out is, whatever that token's probability.  Results do not
  * depend on timing.
  * Asynchronous on `stream`; runs of one plan share its workspace and are
- * ordered one after the other.  A captured run may be replayed after the
+ * ordered one after the other, on whatever streams.  A captured run (on any stream; it
+ * waits for nothing outside its capture) may be replayed after the
  * plan was built again with at most as many query tokens as it had at the capture; on a larger
- * batch it computes and writes nothing and raises SALT_DEVERR_BATCH.
+ * batch it computes and writes nothing and raises SALT_DEVERR_BATCH.  The plan
+ * does not know of replays: order them after the build, after and before the plan's
+ * other runs and before its next build, by one stream or by events.
  */
 salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, float scale,
                           void *out, int64_t out_stride, float *lse, salt_stream_t stream);

@@ -1274,22 +1274,53 @@ struct salt_attn {
     bool wide = false, narrow = false;         // there are items of this kind
     bool partial = false;                      // some row needs the combine
     int T = 0;
-    std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since
+    std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since, but for captured ones
+    unsigned long long capture = 0;            // the capture that the last captured run belongs to
+    std::vector<cudaStream_t> capture_streams; // and its runs' streams
     cudaEvent_t tmp_ev = nullptr;
 };
 
 namespace {
 
-// Makes `stream` wait for what the plan's other streams were given so far.
-cudaError_t order_after_uses(salt_attn *a, cudaStream_t stream)
+// The capture that the stream takes part in, 0 for none.
+cudaError_t capture_of(cudaStream_t stream, unsigned long long *id)
 {
-    for (cudaStream_t s : a->use_streams) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    *id = 0;
+    const cudaError_t e = cudaStreamGetCaptureInfo(stream, &status, id);
+    if (e == cudaSuccess && status == cudaStreamCaptureStatusNone) *id = 0;
+    return e;
+}
+
+// Makes `stream` wait for what the others were given so far.
+cudaError_t order_after(salt_attn *a, const std::vector<cudaStream_t> &others, cudaStream_t stream)
+{
+    for (cudaStream_t s : others) {
         if (s == stream) continue;
         cudaError_t e = cudaEventRecord(a->tmp_ev, s);
         if (e == cudaSuccess) e = cudaStreamWaitEvent(stream, a->tmp_ev, 0);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
+}
+
+// The same for a stream that is not captured and the plan's uses.  One whose stream is being captured by now cannot be waited
+// for: that is refused, as a wait would draw `stream` into the capture.
+salt_status order_after_uses(salt_attn *a, cudaStream_t stream)
+{
+    salt_ctx *ctx = a->kv->ctx;
+    for (cudaStream_t s : a->use_streams) {
+        unsigned long long id = 0;
+        if (s != stream) SALT_CUDA_OR_FAIL(ctx, capture_of(s, &id));
+        if (id) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "a stream that the plan was used on is being captured");
+    }
+    SALT_CUDA_OR_FAIL(ctx, order_after(a, a->use_streams, stream));
+    return SALT_OK;
+}
+
+void add_stream(std::vector<cudaStream_t> &v, cudaStream_t stream)
+{
+    if (std::find(v.begin(), v.end(), stream) == v.end()) v.push_back(stream);
 }
 
 salt_status check_batch(const salt_attn *a, const salt_attn_batch *b, int *tokens)
@@ -1748,18 +1779,19 @@ try {
     if (!b) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null batch");
     if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    cudaStreamCaptureStatus cap;
-    SALT_CUDA_OR_FAIL(ctx, cudaStreamIsCapturing(stream, &cap));
-    if (cap != cudaStreamCaptureStatusNone) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "a build cannot be captured");
+    unsigned long long capture;
+    SALT_CUDA_OR_FAIL(ctx, capture_of(stream, &capture));
+    if (capture) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "a build cannot be captured");
     a->built = false;
     int T = 0;
-    const salt_status st = check_batch(a, b, &T);
+    salt_status st = check_batch(a, b, &T);
     if (st != SALT_OK) return st;
     const int k = a->staging_next;
     if (a->staging_used[k]) SALT_CUDA_OR_FAIL(ctx, cudaEventSynchronize(a->staging_ev[k]));
     a->staging_next ^= 1;
     const size_t words = fill_plan(a, b, T, a->staging[k]);
-    SALT_CUDA_OR_FAIL(ctx, order_after_uses(a, stream));
+    st = order_after_uses(a, stream);
+    if (st != SALT_OK) return st;
     const int n16 = (int)((words + 3) / 4);
     plan_copy_kernel<<<std::min(64, (n16 + 255) / 256), 256, 0, stream>>>(reinterpret_cast<const uint4 *>(a->staging[k]),
                                                                           reinterpret_cast<uint4 *>(a->plan), n16);
@@ -1785,25 +1817,31 @@ try {
     if (layer < 0 || layer >= a->kv->n_layers)
         return ctx_fail(ctx, SALT_ERR_LAYER_RANGE, "layer %d outside [0, %d)", layer, a->kv->n_layers);
     if (!std::isfinite(scale)) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "scale is not finite");
-    if (a->T == 0) return SALT_OK;
-    if (!q || !out) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null q or out");
-    const int64_t row = (int64_t)a->cfg.n_heads * kv.dim;
-    if (q_stride < row || out_stride < row)
-        return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "rows of %lld elements %lld and %lld apart", (long long)row,
-                        (long long)q_stride, (long long)out_stride);
-    if ((q_stride | out_stride) % 8 || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) ||
-        (reinterpret_cast<uintptr_t>(lse) & 3))
-        return ctx_fail(ctx, SALT_ERR_ALIGN, "rows of q or out not on 16-byte boundaries, or lse not on a 4-byte one");
     if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
-    if (a->use_streams.size() != 1 || a->use_streams[0] != stream) {
-        SALT_CUDA_OR_FAIL(ctx, order_after_uses(a, stream));
-        if (std::find(a->use_streams.begin(), a->use_streams.end(), stream) == a->use_streams.end())
-            a->use_streams.push_back(stream);
+    unsigned long long capture;
+    SALT_CUDA_OR_FAIL(ctx, capture_of(stream, &capture));
+    if (a->T == 0 && !capture) return SALT_OK;
+    if (a->T > 0) {
+        if (!q || !out) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null q or out");
+        const int64_t row = (int64_t)a->cfg.n_heads * kv.dim;
+        if (q_stride < row || out_stride < row)
+            return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "rows of %lld elements %lld and %lld apart", (long long)row,
+                            (long long)q_stride, (long long)out_stride);
+        if ((q_stride | out_stride) % 8 || ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) & 15) ||
+            (reinterpret_cast<uintptr_t>(lse) & 3))
+            return ctx_fail(ctx, SALT_ERR_ALIGN, "rows of q or out not on 16-byte boundaries, or lse not on a 4-byte one");
     }
-    // a captured run may be replayed for a plan that needs other launches
-    cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-    if (!(a->wide && a->narrow && a->partial)) SALT_CUDA_OR_FAIL(ctx, cudaStreamIsCapturing(stream, &cap));
+    if (capture) {  // in the order of its capture's other runs; what its replays come after is the caller's to say
+        if (a->capture != capture) a->capture_streams.clear();
+        a->capture = capture;
+        SALT_CUDA_OR_FAIL(ctx, order_after(a, a->capture_streams, stream));
+        add_stream(a->capture_streams, stream);
+    } else if (a->use_streams.size() != 1 || a->use_streams[0] != stream) {
+        const salt_status st = order_after_uses(a, stream);
+        if (st != SALT_OK) return st;
+        add_stream(a->use_streams, stream);
+    }
     AttnParams p;
     p.kmap = a->kmap;
     p.vmap = a->vmap;
@@ -1825,7 +1863,8 @@ try {
     p.pages_at = a->pages_at;
     p.scale_log2 = scale * 1.4426950408889634f;
     p.err = ctx_error_word(ctx);
-    const bool all = cap != cudaStreamCaptureStatusNone, wide = a->wide || all, narrow = a->narrow || all, combine = a->partial || all;
+    // a captured run may be replayed for a plan that needs other launches
+    const bool all = capture != 0, wide = a->wide || all, narrow = a->narrow || all, combine = (a->partial || all) && a->T > 0;
     SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_attn<128>(p, a->n_sm, wide, narrow, combine, stream)
                                          : launch_attn<64>(p, a->n_sm, wide, narrow, combine, stream));
     return SALT_OK;

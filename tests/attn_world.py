@@ -57,6 +57,8 @@ class Shared:
     def run(self, stream=None):
         out = torch.full((self.T, self.heads, self.dim), 7.0, dtype=torch.bfloat16, device="cuda")
         lse = torch.full((self.T, self.heads), 7.0, device="cuda")
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())
         self.salt.salt_attn_run(self.plan, 0, self.q, out, self.scale, lse, stream)
         torch.cuda.synchronize()
         assert self.salt.salt_get_device_error(self.ctx) == 0
