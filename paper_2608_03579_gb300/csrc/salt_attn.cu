@@ -1342,11 +1342,13 @@ salt_status check_batch(const salt_attn *a, const salt_attn_batch *b, int *token
     auto check_lists = [&](const char *what, int n, const int32_t *len, const int32_t *ptr, const int32_t *pages, int64_t used) -> salt_status {
         if (n == 0) return SALT_OK;
         if (ptr[0] != 0) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "the %ss' page lists start at %d", what, ptr[0]);
-        for (int i = 0; i < n; ++i) {
-            if (len[i] < 0) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d has %d tokens", what, i, len[i]);
+        // (all pointers first: only then is the last one the number of pages that may be read)
+        for (int i = 0; i < n; ++i)
             if (ptr[i + 1] < ptr[i] || used + ptr[i + 1] > c.max_pages)
                 return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d: page list [%d, %d) out of order or past max_pages", what, i,
                                 ptr[i], ptr[i + 1]);
+        for (int i = 0; i < n; ++i) {
+            if (len[i] < 0) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d has %d tokens", what, i, len[i]);
             const int need = (int)(((int64_t)len[i] + kv.page - 1) >> kv.page_log2);
             if (need > ptr[i + 1] - ptr[i])
                 return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d: %d tokens need %d pages, its list has %d", what, i, len[i], need,
