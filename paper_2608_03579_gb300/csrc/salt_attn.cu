@@ -1347,13 +1347,13 @@ salt_status check_batch(const salt_attn *a, const salt_attn_batch *b, int *token
             if (ptr[i + 1] < ptr[i] || used + ptr[i + 1] > c.max_pages)
                 return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d: page list [%d, %d) out of order or past max_pages", what, i,
                                 ptr[i], ptr[i + 1]);
+        if (ptr[n] > 0 && !pages) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null page list");
         for (int i = 0; i < n; ++i) {
             if (len[i] < 0) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d has %d tokens", what, i, len[i]);
             const int need = (int)(((int64_t)len[i] + kv.page - 1) >> kv.page_log2);
             if (need > ptr[i + 1] - ptr[i])
                 return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "%s %d: %d tokens need %d pages, its list has %d", what, i, len[i], need,
                                 ptr[i + 1] - ptr[i]);
-            if (need > 0 && !pages) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null page list");
             for (int j = ptr[i]; j < ptr[i] + need; ++j)
                 if (pages[j] < 0 || pages[j] >= kv.n_pages)
                     return ctx_fail(ctx, SALT_ERR_SLOT_RANGE, "%s %d: page %d outside [0, %d)", what, i, pages[j], kv.n_pages);
