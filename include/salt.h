@@ -642,7 +642,8 @@ typedef struct salt_attn_batch {
     const int32_t *group_pages;     /* [group_page_ptr[n_groups]] */
 } salt_attn_batch;
 
-/* Allocates the plan's device tables and workspace.  The plan keeps kv, which
+/* Allocates the plan's device tables and workspace (salt_attn_get_shape tells their size, which is
+ * mostly two fp32 rows for each of max_tokens * n_heads query rows).  The plan keeps kv, which
  * must outlive it.  Synchronous. */
 salt_status salt_attn_create(salt_kv *kv, const salt_attn_config *config, salt_attn **out);
 /* Waits for the device, then frees the plan.  NULL is a no-op. */
@@ -658,6 +659,20 @@ void salt_attn_destroy(salt_attn *plan);
  */
 salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_stream_t stream);
 
+/* How a run of the built batch is divided (diagnostics; no device work; no items before the first
+ * build).  An item is the query rows that go through a range of the cache together. */
+typedef struct salt_attn_shape {
+    int32_t wide_items;       /* items of many rows, over all key/value heads */
+    int32_t wide_tiles;       /* 128-token tiles of the longest of them */
+    int32_t wide_ctas;        /* CTAs that they are spread over */
+    int32_t narrow_items;     /* the same of few rows */
+    int32_t narrow_tiles;
+    int32_t narrow_ctas;
+    int32_t combined;         /* whether rows of several items are joined by a further kernel */
+    int64_t workspace_bytes;  /* device memory of the plan */
+} salt_attn_shape;
+salt_status salt_attn_get_shape(const salt_attn *plan, salt_attn_shape *shape);
+
 /*
  * Row i (0 <= i < q_len[b]) of request b sees its group's whole prompt and its
  * own tokens [0, kv_len[b] - q_len[b] + i]; query head h reads key/value head
@@ -670,7 +685,8 @@ salt_status salt_attn_build(salt_attn *plan, const salt_attn_batch *batch, salt_
  * [tokens][n_heads] or NULL.  Scores, running maxima, sums and partial results
  * are held in fp32 and out is rounded once.  The query meets the cached keys
  * as the sum of two e4m3 terms (about 8 bits, as bf16), the probabilities meet
- * the cached values, widened exactly, in f16 (11 bits).  Scores are served up to 2^23 in
+ * the cached values, widened exactly, in f16: times their value's power of two they are rounded
+ * to 11 bits, or by up to 2^-27 of the row's largest such product where that is more.  Scores are served up to 2^23 in
  * magnitude, where fp32 still holds their fractions; a row with one past that may be NaN.  A row that sees a token is NaN if there is
  * an infinity or a NaN in its query or it sees a cached key standing for NaN; if it sees a
  * cached value standing for NaN, out is, whatever that token's probability.  Results do not

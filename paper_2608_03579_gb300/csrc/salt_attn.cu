@@ -1273,6 +1273,7 @@ struct salt_attn {
     bool built = false;
     bool wide = false, narrow = false;         // there are items of this kind
     bool partial = false;                      // some row needs the combine
+    int n_items[2] = {0, 0}, most_tiles[2] = {0, 0};  // narrow and wide items of all heads, tiles of the longest
     int T = 0;
     std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since, but for captured ones
     unsigned long long capture = 0;            // the capture that the last captured run belongs to
@@ -1563,6 +1564,7 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     };
     std::vector<Rec> recs;
     int n_wide = 0;
+    a->most_tiles[0] = a->most_tiles[1] = 0;
     int64_t part = 0;
     bool partial = false;
     std::vector<uint8_t> seen(T, 0);
@@ -1578,6 +1580,7 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
             recs.push_back({tile_cost(x) * (a1 - a0), (int)k, a0 * TT, std::min(x.len, a1 * TT),
                             direct ? 0 : (int)(part + (int64_t)i * KV * rows), direct, x.wide});
             n_wide += x.wide;
+            a->most_tiles[x.wide] = std::max(a->most_tiles[x.wide], a1 - a0);
         }
         for (int i = 0; i < x.ntok; ++i) {
             const int t = order[x.tok + i];
@@ -1615,6 +1618,8 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     w[HD_NARROW] = (int)recs.size() - n_wide;
     a->wide = n_wide > 0;
     a->narrow = (int)recs.size() > n_wide;
+    a->n_items[1] = n_wide * KV;
+    a->n_items[0] = ((int)recs.size() - n_wide) * KV;
     w[HD_PARTIAL] = partial ? 1 : 0;
     a->partial = partial;
     int32_t *pg = w + a->pages_at;
@@ -1806,6 +1811,22 @@ try {
     return SALT_OK;
 } catch (const std::bad_alloc &) {
     return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
+}
+
+salt_status salt_attn_get_shape(const salt_attn *a, salt_attn_shape *out)
+{
+    if (!a || !out) return SALT_ERR_INVALID_ARG;
+    *out = salt_attn_shape{};
+    out->workspace_bytes = (int64_t)a->plan_words * 4 + a->part_cap * (a->kv->dev.dim + 1) * 4;
+    out->wide_ctas = a->n_sm * Shape<128, true>::CTAS;
+    out->narrow_ctas = a->n_sm * Shape<128, false>::CTAS;
+    if (!a->built) return SALT_OK;
+    out->wide_items = a->n_items[1];
+    out->wide_tiles = a->most_tiles[1];
+    out->narrow_items = a->n_items[0];
+    out->narrow_tiles = a->most_tiles[0];
+    out->combined = a->partial;
+    return SALT_OK;
 }
 
 salt_status salt_attn_run(salt_attn *a, int32_t layer, const void *q, int64_t q_stride, float scale, void *out,

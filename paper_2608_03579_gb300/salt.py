@@ -87,6 +87,11 @@ class _attn_batch(ctypes.Structure):
                 ("group_pages", ctypes.c_void_p)]
 
 
+class _attn_shape(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("wide_items", "wide_tiles", "wide_ctas", "narrow_items", "narrow_tiles",
+                                               "narrow_ctas", "combined")] + [("workspace_bytes", ctypes.c_int64)])
+
+
 _vp, _i32, _i64, _f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
 _SIGS = {
     "salt_abi_version": (_i32, []),
@@ -134,6 +139,7 @@ _SIGS = {
     "salt_attn_create": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_config), ctypes.POINTER(_vp)]),
     "salt_attn_destroy": (None, [_vp]),
     "salt_attn_build": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_batch), _vp]),
+    "salt_attn_get_shape": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_shape)]),
     "salt_attn_run": (ctypes.c_int, [_vp, _i32, _vp, _i64, _f32, _vp, _i64, _vp, _vp]),
     "salt_verify_drafts": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp,
                                           _vp]),
@@ -631,6 +637,13 @@ def salt_attn_build(plan: AttnPlan, batch, stream=None) -> None:
     """Plan a batch (salt_attn_batch)."""
     _check(_lib.salt_attn_build(plan.handle, ctypes.byref(batch), _stream(stream)), plan.ctx)
     plan.n_tokens = batch._tokens
+
+
+def salt_attn_get_shape(plan: AttnPlan) -> dict:
+    """How a run of the built batch is divided, and the plan's device memory."""
+    s = _attn_shape()
+    _check(_lib.salt_attn_get_shape(plan.handle, ctypes.byref(s)), plan.ctx)
+    return {k: getattr(s, k) for (k, _) in _attn_shape._fields_}
 
 
 def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, stream=None) -> None:

@@ -40,6 +40,7 @@ class Shared:
             e[0, pages, :, offset] = qe.to(torch.uint8)
             self.codes[name], self.exps[name] = c.cuda(), e.cuda()
             self.values[name] = value(c[0, pages, :, offset], e[0, pages, :, offset]).cuda()
+        self.unit = torch.where(qe == 255, torch.zeros(()), torch.exp2(qe.double() - 127)).cuda()   # of the values' codes [n, KV]
         g = torch.Generator().manual_seed(seed + 1)
         self.q = torch.randn((self.T, heads, dim), generator=g).bfloat16().cuda()
         self.scale = dim ** -0.5 if scale is None else scale
@@ -75,13 +76,17 @@ class Shared:
             at += n
 
     def reference(self):
-        """out, lse and their tolerances: those of attn_reference.attention, row by row."""
+        """out, lse and their tolerances: those of attn_reference.attention, row by row, and for out
+        the end of f16's range, in which probabilities times their value's power of two meet the
+        values' codes: the largest of a row is at least 2^2 and all are rounded by 2^-25 at least."""
         G, D = self.heads // self.kv_heads, self.dim
         f64 = dict(dtype=torch.float64, device="cuda")
         out, tol = torch.zeros((self.T, self.heads, D), **f64), torch.zeros((self.T, self.heads, D), **f64)
         lse, ltol = torch.full((self.T, self.heads), -math.inf, **f64), torch.zeros((self.T, self.heads), **f64)
         for at, K, V, see in self.requests():
-            n = see.shape[0]
+            n, keep = see.shape
+            if keep == 0:
+                continue
             x = self.q[at].double().view(n, self.kv_heads, G, D)
             hide = ~see[:, None, None]
             s = torch.einsum("nkgd,tkd->nkgt", x, K) * self.scale
@@ -94,8 +99,11 @@ class Shared:
             ds = abs(self.scale) * (most(ksum.expand_as(s)) * x.abs().amax(-1) * 2.0 ** -17
                                     + most(torch.einsum("nkgd,tkd->nkgt", x.abs(), K.abs())) * D * 2.0 ** -23)
             ds = ds + most(s.abs()) * 2.0 ** -20 + 2.0 ** -20
+            unit = self.unit[:keep]
+            codes = (V.abs() / torch.where(unit > 0, unit, torch.ones_like(unit))[..., None]).nan_to_num(0.0).sum(0)   # [KV, D]
+            least = (p * unit.T[None, :, None]).amax(-1)[..., None] * codes[None, :, None] * 2.0 ** -27
             out[at], lse[at] = o.reshape(n, -1, D), ls.reshape(n, -1)
-            tol[at] = (o.abs() * 2.0 ** -9 + A * (2.0 ** -8 + 2.0 * ds)[..., None] + 2.0 ** -130).reshape(n, -1, D)
+            tol[at] = (o.abs() * 2.0 ** -9 + A * (2.0 ** -8 + 2.0 * ds)[..., None] + least + 2.0 ** -130).reshape(n, -1, D)
             ltol[at] = (ds + 2.0 ** -18 * (1.0 + ls.abs())).reshape(n, -1)
         return out, lse, tol, ltol
 
