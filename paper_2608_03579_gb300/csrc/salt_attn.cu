@@ -233,15 +233,6 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    float2 r;
-    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-
 struct Item {
     int flags, tok, ntok, pages, t0, t1, lim, part, kh;
     int tiles, rows, per;  // per: rows a warpgroup takes
@@ -343,10 +334,9 @@ template <int CH>
 __device__ __forceinline__ void load_columns(float (&x)[CH], uint32_t at)
 {
     uint32_t *r = reinterpret_cast<uint32_t *>(x);
+    static_assert(CH == 4 || CH == 16, "the columns a softmax thread has in hand");
     if constexpr (CH == 4) tmem_ld4(at, r);
-    else if constexpr (CH == 8) tmem_ld8(at, r);
-    else if constexpr (CH == 16) tmem_ld16(at, *reinterpret_cast<uint32_t(*)[16]>(r));
-    else tmem_ld32(at, r);
+    else tmem_ld16(at, *reinterpret_cast<uint32_t(*)[16]>(r));
 }
 
 // A token's part of a tile: factors of its scores and of its probabilities, and what
