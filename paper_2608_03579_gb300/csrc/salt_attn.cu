@@ -150,18 +150,6 @@ struct Shape {
 constexpr int narrow_rows(int D) { return D == 128 ? Shape<128, false>::R_MAX : Shape<64, false>::R_MAX; }
 constexpr int WIDE_ROWS = Shape<128, true>::R_MAX;
 
-__device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
-{
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(c));
-    return r;
-}
 __device__ __forceinline__ float ex2(float x)
 {
     float r;
@@ -233,6 +221,7 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
+
 struct Item {
     int flags, tok, ntok, pages, t0, t1, lim, part, kh;
     int tiles, rows, per;  // per: rows a warpgroup takes
@@ -1648,17 +1637,7 @@ cudaError_t launch_tiles(const AttnParams &params, int n_sm, bool behind, cudaSt
 {
     AttnParams p = params;
     p.behind = behind;
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(n_sm * L::CTAS, 1, 1);
-    cfg.blockDim = dim3(L::THREADS, 1, 1);
-    cfg.dynamicSmemBytes = L::BYTES;
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attn_tile_kernel<L>, p);
+    return launch_overlapped(attn_tile_kernel<L>, n_sm * L::CTAS, L::THREADS, L::BYTES, stream, p);
 }
 
 // The wide items, the narrow ones (which fill the SMs as the wide ones
@@ -1676,18 +1655,14 @@ cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, b
     }
     if (!combine) return cudaSuccess;
     // (rows in all are below 2^31: partial rows, twice as many, are)
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
     const int rows = p.max_tok * p.n_heads;
     const bool few = rows <= n_sm * COMBINE_FEW;
-    cfg.gridDim = dim3(few ? rows : (rows + COMBINE_WARPS - 1) / COMBINE_WARPS, 1, 1);
-    cfg.blockDim = dim3(32 * (few ? COMBINE_SPLIT : COMBINE_WARPS), 1, 1);
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = wide || narrow ? 1 : 0;  // (the plan is there when an items' kernel is past its wait)
-    return cudaLaunchKernelEx(&cfg, few ? attn_combine_kernel<D, COMBINE_SPLIT> : attn_combine_kernel<D, 1>, p);
+    const auto kernel = few ? attn_combine_kernel<D, COMBINE_SPLIT> : attn_combine_kernel<D, 1>;
+    const unsigned blocks = few ? rows : (rows + COMBINE_WARPS - 1) / COMBINE_WARPS, threads = 32 * (few ? COMBINE_SPLIT : COMBINE_WARPS);
+    // (it reads the plan before its wait: the plan is there when an items' kernel is past its own)
+    if (wide || narrow) return launch_overlapped(kernel, blocks, threads, 0, stream, p);
+    kernel<<<blocks, threads, 0, stream>>>(p);
+    return cudaGetLastError();
 }
 
 }  // namespace

@@ -42,4 +42,21 @@ bool on_device(const void *p);
         }                                                                                                           \
     } while (0)
 
+// Launches a kernel that may begin while the stream's last one ends (it waits for that one itself).
+template <class... P, class... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), unsigned blocks, unsigned threads, size_t shared_bytes, cudaStream_t stream, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(blocks, 1, 1);
+    cfg.blockDim = dim3(threads, 1, 1);
+    cfg.dynamicSmemBytes = shared_bytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
 }  // namespace salt

@@ -268,6 +268,20 @@ constexpr int STATIC_PART_CAP = 256;
 // device with cudaGetSymbolAddress); blk_cap = STATIC_APPLY_BLOCKS.
 cudaError_t apply_static_workspace(ApplyWork *out);
 
+// two floats as e4m3 codes (rounded to nearest even), and two codes as f16
+__device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
+{
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(c));
+    return r;
+}
+
 // Device view of a key/value cache (one layer's arrays start at layer * n_pages pages).
 struct KvDev {
     uint8_t *k, *v, *k_exp, *v_exp;

@@ -22,19 +22,6 @@ namespace {
 constexpr int KV_THREADS = 256;
 constexpr int WRITE_ROWS = 2, READ_ROWS = 4;  // rows a thread
 
-__device__ __forceinline__ uint16_t e4m3x2(float lo, float hi)
-{
-    uint16_t r;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;\n" : "=h"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ uint32_t f16x2_of_e4m3x2(uint16_t c)
-{
-    uint32_t r;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;\n" : "=r"(r) : "h"(c));
-    return r;
-}
-
 // Exponent byte of a row whose largest magnitude has the float bits `a`.
 __device__ __forceinline__ uint32_t row_exp(uint32_t a)
 {
@@ -228,22 +215,6 @@ unsigned row_blocks(const salt_kv *kv, int32_t n_tokens, int rows)
     return (unsigned)((2ll * n_tokens * kv->dev.heads + per - 1) / per);
 }
 
-// A launch that may begin while the stream's last kernel ends (the kernel waits for that one itself).
-template <class... P, class... A>
-cudaError_t launch_overlapped(void (*kernel)(P...), unsigned blocks, unsigned threads, cudaStream_t stream, A... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = dim3(blocks, 1, 1);
-    cfg.blockDim = dim3(threads, 1, 1);
-    cfg.stream = stream;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
-}
-
 }  // namespace
 }  // namespace salt
 
@@ -305,7 +276,7 @@ salt_status salt_kv_write(salt_kv *kv, int32_t layer, int32_t n_tokens, const vo
     const int32_t most = launch_tokens(kv);
     for (int64_t t = 0; t < n_tokens; t += most) {
         const int32_t n = (int32_t)std::min<int64_t>(most, n_tokens - t);
-        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, WRITE_ROWS), KV_THREADS, static_cast<cudaStream_t>(stream),
+        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, WRITE_ROWS), KV_THREADS, 0, static_cast<cudaStream_t>(stream),
             kv->dev, (uint32_t)layer * kv->dev.n_pages, n, heads2_inv(kv), static_cast<const uint16_t *>(k) + t * k_stride, k_stride,
             static_cast<const uint16_t *>(v) + t * v_stride, v_stride, slots + t, ctx_error_word(kv->ctx)));
     }
@@ -324,7 +295,7 @@ salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int
     const int32_t most = launch_tokens(kv);
     for (int64_t t = 0; t < n_tokens; t += most) {
         const int32_t n = (int32_t)std::min<int64_t>(most, n_tokens - t);
-        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, READ_ROWS), KV_THREADS, static_cast<cudaStream_t>(stream),
+        SALT_CUDA_OR_FAIL(kv->ctx, launch_overlapped(kernel, row_blocks(kv, n, READ_ROWS), KV_THREADS, 0, static_cast<cudaStream_t>(stream),
             kv->dev, (uint32_t)layer * kv->dev.n_pages, n, heads2_inv(kv), slots + t, static_cast<uint16_t *>(k) + t * k_stride, k_stride,
             static_cast<uint16_t *>(v) + t * v_stride, v_stride, ctx_error_word(kv->ctx)));
     }
