@@ -23,10 +23,10 @@
 //
 // What bounds it: neither memory nor the tensor cores but the steps of a tile one behind the
 // other (scores out of tensor memory, exponentials, P and V into shared memory, vote, product).  With 128
-// rows of 128 elements a tile takes about 4,300 cycles, 1,024 of them exponentials at the SM's rate and
-// 512 products: four prompt chunks of 900 to 2,048 tokens behind 4,096 take 1.2 ms (520 TFLOP/s).  With four
-// rows it is 2,100 cycles, two CTAs of an SM side by side: two requests of 200,000 tokens and more with
-// heads of 64 take 99 us (4.5 TB/s).
+// rows of 128 elements a tile takes about 4,300 cycles, of which exponentials would take 512 at the SM's rate (32 a
+// cycle, measured) and the products 512: four prompt chunks of 900 to 2,048 tokens behind 4,096 take 1.22 ms
+// (515 TFLOP/s).  With four rows it is 2,100 cycles, two CTAs of an SM side by side: two requests of 200,000
+// tokens and more with heads of 64 take 95.5 us (4.7 TB/s).
 #include <algorithm>
 #include <cmath>
 #include <cstring>
@@ -438,7 +438,7 @@ __device__ __forceinline__ float soft_probs(Soft &s, const SoftItem &w, float2 (
 
 // soft_probs where every column of the warpgroup is a row and every row sees every token: no
 // branches, and each sixteen columns' exponentials run beside the next ones' loads and products.
-// (16 exponentials of each of an SM quarter's two warps take 256 cycles; behind one another with the
+// (16 exponentials of each of an SM quarter's two warps take 128 cycles; behind one another with the
 // loads, a tile of 128 rows took 2,100 cycles here.)
 template <class L>
 __device__ __forceinline__ float soft_probs_full(Soft &s, const SoftItem &w, float2 (&l)[L::CW_MAX / 2], const Token &t, uint32_t s_at,

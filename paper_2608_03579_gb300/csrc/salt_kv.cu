@@ -37,9 +37,9 @@ __device__ __forceinline__ uint32_t row_exp(uint32_t a)
 // the maximum's exchange, its exponent) is shared by 16 of them.  A thread deals with ROWS rows,
 // KV_THREADS / (D / 16) apart, so that enough bytes are under way, and reads and writes past
 // the L2 what it will not meet again.  Both kernels move bytes: 16,384 tokens of 8 heads of 128 are written in
-// 20 us (5.1 TB/s of bytes read and written; 1 row a thread 20, 4 rows 20.5; with 8 elements a
-// lane the kernel was short of instruction slots and took 25), 100,003 are read in 95 us (6.5 TB/s; 1
-// row 98, 2 rows 96; with 8 elements a lane 112).
+// 17.6 us (5.7 TB/s of bytes read and written), 100,003 are read in 93 us (6.6 TB/s).  Before the launches overlapped with
+// what came before them these were 20 and 95, with 1 row a thread 20 and 98, with 4 and 2 rows 20.5 and 96; with 8 elements
+// a lane the kernels were short of instruction slots and took 25 and 112.
 struct KvRow {
     int t, h;
     bool live, is_v;

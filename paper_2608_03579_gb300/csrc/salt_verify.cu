@@ -19,10 +19,11 @@
 namespace salt {
 namespace {
 
-// 256 requests over 131,072 tokens take 52 us (5.2 TB/s) with 256 threads, four pieces of each row under
-// way and five CTAs an SM.  With 512 threads and two CTAs 64 us, three and two pieces 60, four and two pieces 56; 256
-// threads, three CTAs and eight pieces 61; 128 threads, ten CTAs 62.  What is left over the bytes (40 us) is what a CTA does before
-// its rows are known: three dependent reads, then the cluster's meeting at the end.
+// 256 requests over 131,072 tokens, about half of which read p alone (198 MB), take 54 us (3.7 TB/s, 54% of a copy's rate)
+// with 256 threads, four pieces of each row under way and five CTAs an SM.  Measured at 52 us of that kernel: with 512 threads and two CTAs 64 us, three and two pieces 60, four and two pieces 56; 256
+// threads, three CTAs and eight pieces 61; 128 threads, ten CTAs 62.  What is left over the bytes (29 us) is what a CTA does before
+// its rows are known, three dependent reads that its cluster's eight CTAs repeat, and the cluster's meeting at the end, in 2.7
+// rounds of resident CTAs.
 constexpr int VF_THREADS = 256;
 constexpr int VF_WARPS = VF_THREADS / 32;
 constexpr int VF_CTAS = 5;            // CTAs an SM
