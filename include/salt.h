@@ -92,7 +92,7 @@ typedef enum salt_status {
 #define SALT_DEVERR_TIMEOUT 0x20u        /* a bounded in-kernel wait gave up (results of that call invalid) */
 #define SALT_DEVERR_GAMMA_RANGE 0x40u
 #define SALT_DEVERR_BATCH 0x80u          /* a captured call was replayed on a larger batch (salt_lora_apply_with_base, salt_attn_run) */
-#define SALT_DEVERR_KV_SLOT 0x100u       /* a cache slot outside the cache (salt_kv_write, salt_kv_read) */
+#define SALT_DEVERR_KV_SLOT 0x100u       /* a cache slot outside the cache (salt_kv_write, salt_kv_read, salt_rope_write) */
 #define SALT_DEVERR_DRAFT 0x200u         /* draft pointers out of order or a drafted token outside the vocabulary */
 
 /*
@@ -603,6 +603,58 @@ salt_status salt_kv_write(salt_kv *kv, int32_t layer, int32_t n_tokens, const vo
  */
 salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int32_t *slots, void *k,
                          int64_t k_stride, void *v, int64_t v_stride, salt_stream_t stream);
+
+/*
+ * Norms of queries and keys, head by head, and their rotation to the tokens'
+ * positions, in one pass.  A head x of head_dim elements becomes
+ *     y = x * (mean(x^2) + eps)^(-1/2) * (w + norm_offset)
+ * (y = x without norm weights w), and of its first rot_dim elements each pair
+ * (a, b) becomes scale * (a cos t - b sin t, b cos t + a sin t), t = position *
+ * inv_freq[pair]; the others stay y.  Pair i is elements (i, i + rot_dim / 2), or
+ * (2i, 2i + 1) where interleaved.  Angles are exact to 2^-24 of a half turn at
+ * any position (int32, below zero too); everything else is fp32, rounded once.  An infinity
+ * or a NaN among a head's elements spoils that head alone.
+ */
+typedef struct salt_rope salt_rope;
+typedef struct salt_rope_config {
+    int32_t head_dim;        /* 64 or 128 */
+    int32_t rot_dim;         /* a multiple of 16 up to head_dim; 0: no rotation */
+    int32_t interleaved;
+    const double *inv_freq;  /* host array of rot_dim / 2: radians a position, at most a turn */
+    float scale;             /* of the rotated elements (1; other models' stretched rotations) */
+    float eps;               /* a positive normal float */
+    float norm_offset;       /* added to the norm weights (0 or 1) */
+} salt_rope_config;
+/* Host only; inv_freq is copied. */
+salt_status salt_rope_create(salt_ctx *ctx, const salt_rope_config *config, salt_rope **out);
+/* NULL is a no-op.  The calls enqueued with it may still be running. */
+void salt_rope_destroy(salt_rope *rope);
+
+/*
+ * Rows of queries ([n_tokens] rows of [n_heads][head_dim] bf16, q_stride
+ * elements apart, a multiple of 8, 16-byte aligned) into q_out, rows of keys
+ * ([n_kv_heads][head_dim]) into k_out, both bf16.  Either may have no heads (its pointers
+ * are then not looked at).  q_norm and k_norm are device bf16[head_dim],
+ * 16-byte aligned, each NULL for no norm of its side.  positions is device int32[n_tokens].
+ * q_out may be q itself, with the same stride, and k_out k; they may not overlap otherwise.
+ * n_heads <= 65536, n_kv_heads <= 1024.  One kernel, asynchronous on `stream`.
+ */
+salt_status salt_rope_apply(salt_rope *rope, int32_t n_tokens, const void *q, int64_t q_stride, int32_t n_heads,
+                            const void *k, int64_t k_stride, int32_t n_kv_heads, const void *q_norm,
+                            const void *k_norm, const int32_t *positions, void *q_out, int64_t q_out_stride,
+                            void *k_out, int64_t k_out_stride, salt_stream_t stream);
+
+/*
+ * salt_rope_apply for the queries, and salt_kv_write of the keys so treated
+ * (without a rounding to bf16 between) and of the values as they are, in one
+ * pass over a fused projection's rows.  A token whose slot is -1 has its query
+ * treated and nothing cached; so has one whose slot is outside the cache, which raises
+ * SALT_DEVERR_KV_SLOT.  Slots of one call must be distinct.  One kernel, asynchronous on `stream`.
+ */
+salt_status salt_rope_write(salt_rope *rope, salt_kv *kv, int32_t layer, int32_t n_tokens, const void *q,
+                            int64_t q_stride, int32_t n_heads, const void *k, int64_t k_stride, const void *v,
+                            int64_t v_stride, const void *q_norm, const void *k_norm, const int32_t *positions,
+                            const int32_t *slots, void *q_out, int64_t q_out_stride, salt_stream_t stream);
 
 /*
  * Attention of a batch over the cache, the requests of a group (a domain,

@@ -14,6 +14,7 @@
 #include "salt_async.cuh"
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
+#include "salt_kvrow.cuh"
 #include "salt_pipe.cuh"
 
 namespace salt {
@@ -21,16 +22,6 @@ namespace {
 
 constexpr int KV_THREADS = 256;
 constexpr int WRITE_ROWS = 2, READ_ROWS = 4;  // rows a thread
-
-// Exponent byte of a row whose largest magnitude has the float bits `a`.
-__device__ __forceinline__ uint32_t row_exp(uint32_t a)
-{
-    const int E = (int)(a >> 23);
-    if (E == 255) return 255u;
-    if (a == 0) return 0u;
-    const int e = E - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);
-    return (uint32_t)max(e, 1);
-}
 
 // Rows are (token, k or v, head), one per D / 16 lanes.  A lane has two pieces of 8 elements, D / 16 pieces
 // apart so that neighbours read and write side by side; what a row costs beside its elements (its place,
@@ -59,12 +50,6 @@ __device__ __forceinline__ KvRow kv_row(const KvDev &c, int n_tokens, uint32_t h
     r.is_v = kh >= c.heads;
     r.h = r.is_v ? kh - c.heads : kh;
     return r;
-}
-
-// The row's number in the cache (they are below 2^31); first_page is the layer's.
-__device__ __forceinline__ uint32_t cache_row(const KvDev &c, uint32_t first_page, int page, int slot, int h)
-{
-    return ((first_page + page) * c.heads + h) * c.page + (slot & (c.page - 1));
 }
 
 template <int D>
@@ -109,7 +94,7 @@ __global__ void __launch_bounds__(KV_THREADS) kv_write_kernel(KvDev c, uint32_t 
             continue;
         }
         const uint32_t e = row_exp(a);
-        const float inv = __uint_as_float(e == 255u ? 0u : (254u - max(e, 1u)) << 23);
+        const float inv = row_inv(e);
         const uint32_t at = cache_row(c, first_page, page, slot[i], r[i].h);
         uint8_t *to = (r[i].is_v ? c.v : c.k) + (uint64_t)at * D + part * 8;
 #pragma unroll

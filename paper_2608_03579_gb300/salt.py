@@ -76,6 +76,11 @@ class _kv_config(ctypes.Structure):
                 + [(k, ctypes.c_void_p) for k in ("k", "v", "k_exp", "v_exp")])
 
 
+class _rope_config(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_int32) for k in ("head_dim", "rot_dim", "interleaved")] + [("inv_freq", ctypes.c_void_p)]
+                + [(k, ctypes.c_float) for k in ("scale", "eps", "norm_offset")])
+
+
 class _attn_config(ctypes.Structure):
     _fields_ = [(k, ctypes.c_int32) for k in ("n_heads", "max_seqs", "max_tokens", "max_pages", "max_groups")]
 
@@ -136,6 +141,11 @@ _SIGS = {
     "salt_kv_destroy": (None, [_vp]),
     "salt_kv_write": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp]),
     "salt_kv_read": (ctypes.c_int, [_vp, _i32, _i32, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "salt_rope_create": (ctypes.c_int, [_vp, ctypes.POINTER(_rope_config), ctypes.POINTER(_vp)]),
+    "salt_rope_destroy": (None, [_vp]),
+    "salt_rope_apply": (ctypes.c_int, [_vp, _i32, _vp, _i64, _i32, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _i64, _vp, _i64, _vp]),
+    "salt_rope_write": (ctypes.c_int, [_vp, _vp, _i32, _i32, _vp, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _vp,
+                                       _i64, _vp]),
     "salt_attn_create": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_config), ctypes.POINTER(_vp)]),
     "salt_attn_destroy": (None, [_vp]),
     "salt_attn_build": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_batch), _vp]),
@@ -583,6 +593,93 @@ def salt_kv_read(kv: KvCache, layer: int, slots, k, v, stream=None) -> None:
     if m != n:
         raise ValueError("k and v have different numbers of tokens")
     _check(_lib.salt_kv_read(kv.handle, layer, n, _int32s(slots, n), kp, ks, vp, vs, _stream(stream)), kv.ctx)
+
+
+class Rope:
+    """A salt_rope handle."""
+
+    def __init__(self, ctx, head_dim, rot_dim, inv_freq, interleaved, scale, eps, norm_offset):
+        freq = np.ascontiguousarray(inv_freq, dtype=np.float64)
+        if freq.shape != (max(rot_dim, 0) // 2,):
+            raise ValueError(f"{freq.size} frequencies for {rot_dim} rotated elements")
+        out = _vp()
+        cfg = _rope_config(head_dim, rot_dim, int(interleaved), freq.ctypes.data, scale, eps, norm_offset)
+        _check(_lib.salt_rope_create(ctx, ctypes.byref(cfg), ctypes.byref(out)), ctx)
+        self.ctx, self.handle, self.head_dim = ctx, out.value, head_dim
+
+    def close(self):
+        if self.handle:
+            _lib.salt_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def salt_rope_create(ctx, head_dim: int, rot_dim: int, inv_freq, interleaved: bool = False, scale: float = 1.0,
+                     eps: float = 1e-6, norm_offset: float = 0.0) -> Rope:
+    """Norms and rotation of heads; inv_freq: radians a position of each of
+    the rot_dim / 2 pairs."""
+    return Rope(ctx, int(head_dim), int(rot_dim), inv_freq, interleaved, scale, eps, norm_offset)
+
+
+def salt_rope_destroy(rope: Rope) -> None:
+    if rope is not None:
+        rope.close()
+
+
+def _norm_weights(w, dim: int):
+    if w is None:
+        return None
+    if _torch_bf16 is None:
+        _load_types()
+    if w.dtype is not _torch_bf16 or not w.is_cuda or w.numel() != dim or not w.is_contiguous():
+        raise ValueError(f"norm weights are not a contiguous CUDA bf16 tensor of {dim}")
+    return w.data_ptr()
+
+
+def _heads_of(t, dim: int, n: int | None = None):
+    """_head_rows of a tensor of any number of heads, and that number."""
+    if t.dim() != 3:
+        raise ValueError(f"not a CUDA bf16 tensor [tokens, heads, {dim}]")
+    m, p, s = _head_rows(t, t.shape[1], dim)
+    if n is not None and m != n:
+        raise ValueError(f"{m} tokens, {n} expected")
+    return m, p, s, t.shape[1]
+
+
+def salt_rope_apply(rope: Rope, q, k, positions, q_out, k_out, q_norm=None, k_norm=None, stream=None) -> None:
+    """Queries q and keys k (CUDA bf16 [tokens, heads, head dim], heads
+    contiguous within a row) normalised and rotated into q_out and k_out
+    (which may be q and k); positions CUDA int32 [tokens]."""
+    D = rope.head_dim
+    n, qp, qs, H = _heads_of(q, D)
+    _, kp, ks, KV = _heads_of(k, D, n)
+    _, qop, qos, Ho = _heads_of(q_out, D, n)
+    _, kop, kos, KVo = _heads_of(k_out, D, n)
+    if H != Ho or KV != KVo:
+        raise ValueError("the outputs have other numbers of heads")
+    _check(_lib.salt_rope_apply(rope.handle, n, qp, qs, H, kp, ks, KV, _norm_weights(q_norm, D), _norm_weights(k_norm, D),
+                                _int32s(positions, n), qop, qos, kop, kos, _stream(stream)), rope.ctx)
+
+
+def salt_rope_write(rope: Rope, kv: KvCache, layer: int, q, k, v, positions, slots, q_out, q_norm=None, k_norm=None,
+                    stream=None) -> None:
+    """The same for q, while k so treated and v as it is go into slots (CUDA
+    int32 [tokens], -1: skip) of a layer of the cache."""
+    D = rope.head_dim
+    n, qp, qs, H = _heads_of(q, D)
+    _, qop, qos, Ho = _heads_of(q_out, D, n)
+    _, kp, ks, KV = _heads_of(k, D, n)
+    _, vp, vs, KVv = _heads_of(v, D, n)
+    if H != Ho or KV != kv.n_kv_heads or KVv != KV:
+        raise ValueError("q_out, k or v has another number of heads")
+    _check(_lib.salt_rope_write(rope.handle, kv.handle, layer, n, qp, qs, H, kp, ks, vp, vs, _norm_weights(q_norm, D),
+                                _norm_weights(k_norm, D), _int32s(positions, n), _int32s(slots, n), qop, qos,
+                                _stream(stream)), rope.ctx)
 
 
 class AttnPlan:
