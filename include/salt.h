@@ -91,8 +91,9 @@ typedef enum salt_status {
 #define SALT_DEVERR_RANK 0x10u
 #define SALT_DEVERR_TIMEOUT 0x20u        /* a bounded in-kernel wait gave up (results of that call invalid) */
 #define SALT_DEVERR_GAMMA_RANGE 0x40u
-#define SALT_DEVERR_BATCH 0x80u          /* a captured call was replayed on a larger batch (salt_lora_apply_with_base, salt_attn_run) */
+#define SALT_DEVERR_BATCH 0x80u          /* a captured call was replayed on a larger batch (salt_lora_apply_with_base, salt_attn_run, salt_attn_weights, salt_attn_evict) */
 #define SALT_DEVERR_KV_SLOT 0x100u       /* a cache slot outside the cache (salt_kv_write, salt_kv_read, salt_rope_write) */
+#define SALT_DEVERR_KEEP 0x400u          /* a request was to keep fewer than no tokens, or more than its line of places holds (salt_attn_evict) */
 #define SALT_DEVERR_DRAFT 0x200u         /* draft pointers out of order or a drafted token outside the vocabulary */
 
 /*
@@ -753,6 +754,55 @@ salt_status salt_attn_get_shape(const salt_attn *plan, salt_attn_shape *shape);
  */
 salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, float scale,
                           void *out, int64_t out_stride, float *lse, salt_stream_t stream);
+
+/*
+ * From its next build on the plan serves salt_attn_weights and salt_attn_evict
+ * too (a build then copies a further table, of 16 words a request or group).
+ * Synchronous.
+ */
+salt_status salt_attn_track(salt_attn *plan);
+
+/*
+ * How much attention the built batch's cached tokens get, added to what they
+ * gathered before: for each token j of a request's own or of a group's prompt that
+ * some row sees, and each key/value head,
+ *     weights[j] = decay * weights[j] + sum_i exp(scale * q_i k_j - lse_i)
+ * over the rows (query token x query heads of the key/value head) that see j, as salt_attn_run says. Of
+ * a request's last q_len tokens, the step's own, and where decay is 0, what was there is not read
+ * and counts as 0.  weights is float [n_layers][n_pages][n_kv_heads][page_tokens], laid out as
+ * k_exp, 16-byte aligned; tokens that no row sees stay as they are.  q and scale are those
+ * that salt_attn_run was given for this layer, lse [tokens][n_heads] what it returned.  Scores and sums are
+ * fp32.  A token's weight is NaN if its key stands for NaN or if there is a NaN in the
+ * query or the log-sum of a row that sees it (salt_attn_run leaves a NaN log-sum for a query with an
+ * infinity); a row that sees nothing adds nothing, whatever it holds.  Results do not depend on timing.  A plan that was not built since
+ * salt_attn_track is refused (SALT_ERR_NOT_BUILT), and so is a batch that lists a page twice, for two requests or
+ * groups (SALT_ERR_INVALID_ARG).  Asynchronous on `stream`; ordered and captured as
+ * salt_attn_run's runs are.
+ */
+salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, const float *lse,
+                              float scale, float decay, float *weights, salt_stream_t stream);
+
+/*
+ * Leave each request b of the built batch keep[b] of its own cached tokens, in layers
+ * [layer, layer + n_layers), for each key/value head by itself: the last
+ * min(recent, keep[b]), the first min(first, what is left), and of the others those of
+ * the largest scores, ties to the earlier token (a NaN counts as less than minus
+ * infinity).  The kept tokens move, in their order, to the front of the request's
+ * pages: codes and exponents of k and v, and the weights unless NULL.  What
+ * lies behind them stays as it was, and so does all of a request of kv_len[b] <=
+ * keep[b] tokens; pages past the kept tokens are free to use.  kept[layer - first layer][b][head][i], i <
+ * keep[b], gets the place that token i had (nothing where nothing moved): int32
+ * [n_layers][n_seqs][n_kv_heads][kept_stride].  keep is device int32[n_seqs]; where it is below
+ * 0 or above kept_stride the request stays as it is and SALT_DEVERR_KEEP is
+ * raised.  scores is laid out as salt_attn_weights' weights, and may be
+ * those (it is not moved itself).  The plan keeps the old lengths: build it again before its next
+ * run.  A token's position is then no longer its place: see
+ * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Asynchronous on `stream`; ordered
+ * and captured as salt_attn_run's runs are (replayed on at most as many requests).
+ */
+salt_status salt_attn_evict(salt_attn *plan, int32_t layer, int32_t n_layers, const int32_t *keep, int32_t first,
+                            int32_t recent, const float *scores, float *weights, int32_t *kept,
+                            int64_t kept_stride, salt_stream_t stream);
 
 /*
  * Hold drafted tokens against the target model's probabilities (speculative

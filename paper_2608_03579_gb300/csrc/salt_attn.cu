@@ -35,6 +35,7 @@
 #include <cuda_fp16.h>
 
 #include "salt_async.cuh"
+#include "salt_attn.cuh"
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
 #include "salt_pipe.cuh"
@@ -43,10 +44,6 @@
 namespace salt {
 namespace {
 
-// The plan's device tables: int32 words of one block, written by the host
-// into a staging area and copied by a kernel.
-constexpr int HEAD_WORDS = 8;   // HD_* below
-constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // query tokens, records of either kind, whether rows need the combine
 constexpr int TOK_WORDS = 8;    // per query token: where its partial rows are, see TK_*
 constexpr int TK_OWN = 0, TK_OWN_ROWS = 1, TK_OWN_N = 2, TK_PRE = 3, TK_PRE_ROWS = 4, TK_PRE_N = 5, TK_DIRECT = 6;
 constexpr int REC_WORDS = 8;    // per item, shared by the key/value heads
@@ -150,78 +147,6 @@ struct Shape {
 constexpr int narrow_rows(int D) { return D == 128 ? Shape<128, false>::R_MAX : Shape<64, false>::R_MAX; }
 constexpr int WIDE_ROWS = Shape<128, true>::R_MAX;
 
-__device__ __forceinline__ float ex2(float x)
-{
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
-    return r;
-}
-// 2^k, 0 below the normal range (k <= 127)
-__device__ __forceinline__ float pow2(int k) { return __uint_as_float(k < -126 ? 0u : (uint32_t)(k + 127) << 23); }
-// 2^(e - 127) of an exponent byte; 0 for a row of zeros, NaN for a row that stands for NaN
-__device__ __forceinline__ float row_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
-
-__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y)
-{
-    asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(a), "r"(x), "r"(y) : "memory");
-}
-__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
-{
-    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t a)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
-    return v;
-}
-
-__device__ __forceinline__ float4 lds4f(uint32_t a)
-{
-    float4 v;
-    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ float ldsf(uint32_t a)
-{
-    float v;
-    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t a)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
-    return v;
-}
-__device__ __forceinline__ void stsf(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(a), "f"(v) : "memory"); }
-__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
-
-// two floats at a time
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    float2 r;
-    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}\n"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
-    return r;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    float2 r;
-    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
-        : "=f"(r.x), "=f"(r.y)
-        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return r;
-}
-
 struct Item {
     int flags, tok, ntok, pages, t0, t1, lim, part, kh;
     int tiles, rows, per;  // per: rows a warpgroup takes
@@ -252,16 +177,6 @@ __device__ __forceinline__ Item load_item(const AttnParams &p, int idx, int G)
     it.per = (it.rows + L::NWG - 1) / L::NWG;
     it.tiles = (it.t1 - it.t0 + TT - 1) / TT;
     return it;
-}
-
-// A bounded wait that also gives up when another role has.
-__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, const volatile int *dead)
-{
-    for (int i = 0; i < (1 << 20); ++i) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 255) == 255 && *dead) return false;
-    }
-    return false;
 }
 
 // Reduces each of N values over the warp's lanes (N a power of two up to
@@ -1235,31 +1150,6 @@ __global__ void __launch_bounds__(32 * (SPLIT > 1 ? SPLIT : COMBINE_WARPS)) attn
 
 using namespace salt;
 
-struct salt_attn {
-    salt_kv *kv = nullptr;
-    salt_attn_config cfg{};
-    int device = 0, n_sm = 1;
-    CUtensorMap kmap, vmap;
-    int32_t *plan = nullptr;                   // device tables
-    int tok_at = 0, order_at = 0, rec_at = 0, rec_cap = 0, pages_at = 0;
-    size_t plan_words = 0;
-    float *part_o = nullptr, *part_l = nullptr;
-    int64_t part_cap = 0;                      // partial rows
-    int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies of the tables
-    cudaEvent_t staging_ev[2] = {nullptr, nullptr};
-    bool staging_used[2] = {false, false};
-    int staging_next = 0;
-    bool built = false;
-    bool wide = false, narrow = false;         // there are items of this kind
-    bool partial = false;                      // some row needs the combine
-    int n_items[2] = {0, 0}, most_tiles[2] = {0, 0};  // narrow and wide items of all heads, tiles of the longest
-    int T = 0;
-    std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since, but for captured ones
-    unsigned long long capture = 0;            // the capture that the last captured run belongs to
-    std::vector<cudaStream_t> capture_streams; // and its runs' streams
-    cudaEvent_t tmp_ev = nullptr;
-};
-
 namespace {
 
 // The capture that the stream takes part in, 0 for none.
@@ -1301,6 +1191,22 @@ salt_status order_after_uses(salt_attn *a, cudaStream_t stream)
 void add_stream(std::vector<cudaStream_t> &v, cudaStream_t stream)
 {
     if (std::find(v.begin(), v.end(), stream) == v.end()) v.push_back(stream);
+}
+
+// Orders a run after the plan's other uses, in its capture if it is captured.
+salt_status order_use(salt_attn *a, cudaStream_t stream, unsigned long long capture)
+{
+    if (capture) {  // in the order of its capture's other runs; what its replays come after is the caller's to say
+        if (a->capture != capture) a->capture_streams.clear();
+        a->capture = capture;
+        SALT_CUDA_OR_FAIL(a->kv->ctx, order_after(a, a->capture_streams, stream));
+        add_stream(a->capture_streams, stream);
+    } else if (a->use_streams.size() != 1 || a->use_streams[0] != stream) {
+        const salt_status st = order_after_uses(a, stream);
+        if (st != SALT_OK) return st;
+        add_stream(a->use_streams, stream);
+    }
+    return SALT_OK;
 }
 
 salt_status check_batch(const salt_attn *a, const salt_attn_batch *b, int *tokens)
@@ -1607,6 +1513,60 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     return (size_t)a->pages_at + own_pages + grp_pages;
 }
 
+// The tracked table of a checked batch whose plan is at w; returns the words used.
+size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
+{
+    Track &tr = a->track;
+    const KvDev &kv = a->kv->dev;
+    std::memset(t, 0, TRACK_HEAD * 4);
+    const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
+    tr.page_seen.assign(kv.n_pages, 0);
+    tr.shared = false;
+    auto note = [&](const int32_t *pages, int len) {
+        for (int j = 0; j < (int)(((int64_t)len + kv.page - 1) >> kv.page_log2); ++j) {
+            tr.shared |= tr.page_seen[pages[j]] != 0;
+            tr.page_seen[pages[j]] = 1;
+        }
+    };
+    int32_t *list = t + tr.list_at;
+    int n = 0;
+    int64_t tiles = 0;
+    auto add = [&](int pages, int len, int tok, int ntok, int old, int lim, bool causal) {
+        if (len == 0 || ntok == 0) return;
+        int32_t *l = list + (size_t)n++ * LIST_WORDS;
+        l[LS_PAGES] = pages;
+        l[LS_LEN] = len;
+        l[LS_TOK] = tok;
+        l[LS_NTOK] = ntok;
+        l[LS_OLD] = old;
+        l[LS_LIM] = lim;
+        l[LS_CAUSAL] = causal;
+        l[LS_TILES] = (int)tiles;
+        tiles += (len + TRACK_TILE - 1) / TRACK_TILE;
+    };
+    std::vector<int> rows(b->n_groups, 0);  // query tokens of each group
+    int t0 = 0;
+    for (int i = 0; i < b->n_seqs; t0 += b->q_len[i], ++i) {
+        int32_t *s = t + tr.seq_at + (size_t)i * SEQ_WORDS;
+        s[0] = b->page_ptr[i];
+        s[1] = b->kv_len[i];
+        note(b->pages + b->page_ptr[i], b->kv_len[i]);
+        // (a request of more query than cached tokens: the first rows see nothing)
+        add(b->page_ptr[i], b->kv_len[i], t0, b->q_len[i], std::max(0, b->kv_len[i] - b->q_len[i]), b->kv_len[i] - b->q_len[i] + 1, true);
+        if (b->n_groups > 0 && b->group[i] >= 0) rows[b->group[i]] += b->q_len[i];
+    }
+    for (int g = 0, at = T; g < b->n_groups; at += rows[g], ++g) {
+        note(b->group_pages + b->group_page_ptr[g], b->group_len[g]);
+        add(own_pages + b->group_page_ptr[g], b->group_len[g], at, rows[g], b->group_len[g], b->group_len[g], false);
+    }
+    t[TH_TOKENS] = T;
+    t[TH_SEQS] = tr.n_seqs = b->n_seqs;
+    t[TH_LISTS] = tr.n_lists = n;
+    t[TH_SHARED] = tr.shared;
+    tr.tiles = tiles;
+    return (size_t)tr.list_at + (size_t)n * LIST_WORDS;
+}
+
 // A cache's codes as rows of D bytes, a box a page's rows of one head, swizzled over a row's width.
 cudaError_t encode_codes_map(CUtensorMap *out, uint8_t *codes, int dim, int64_t rows, int page)
 {
@@ -1666,6 +1626,21 @@ cudaError_t launch_attn(const AttnParams &p, int n_sm, bool wide, bool narrow, b
 }
 
 }  // namespace
+
+salt_status salt::track_enter(salt_attn *a, int32_t layer, int32_t n_layers, cudaStream_t stream, bool *captured)
+{
+    salt_ctx *ctx = a->kv->ctx;
+    if (!a->built) return ctx_fail(ctx, SALT_ERR_NOT_BUILT, "the attention plan was not built");
+    if (!a->track.built) return ctx_fail(ctx, SALT_ERR_NOT_BUILT, "the attention plan was not built since salt_attn_track");
+    if (n_layers < 0 || layer < 0 || layer > a->kv->n_layers || n_layers > a->kv->n_layers - layer)
+        return ctx_fail(ctx, SALT_ERR_LAYER_RANGE, "layers [%d, %lld) outside [0, %d)", layer, (long long)layer + n_layers, a->kv->n_layers);
+    if (a->track.shared) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "a page of the batch is listed twice");
+    if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
+    unsigned long long capture;
+    SALT_CUDA_OR_FAIL(ctx, capture_of(stream, &capture));
+    *captured = capture != 0;
+    return order_use(a, stream, capture);
+}
 
 extern "C" {
 
@@ -1734,7 +1709,9 @@ void salt_attn_destroy(salt_attn *a)
     cudaFree(a->plan);
     cudaFree(a->part_o);
     cudaFree(a->part_l);
+    cudaFree(a->track.table);
     for (int i = 0; i < 2; ++i) {
+        if (a->track.staging[i]) cudaFreeHost(a->track.staging[i]);
         if (a->staging[i]) cudaFreeHost(a->staging[i]);
         if (a->staging_ev[i]) cudaEventDestroy(a->staging_ev[i]);
     }
@@ -1754,7 +1731,7 @@ try {
     unsigned long long capture;
     SALT_CUDA_OR_FAIL(ctx, capture_of(stream, &capture));
     if (capture) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "a build cannot be captured");
-    a->built = false;
+    a->built = a->track.built = false;
     int T = 0;
     salt_status st = check_batch(a, b, &T);
     if (st != SALT_OK) return st;
@@ -1762,20 +1739,54 @@ try {
     if (a->staging_used[k]) SALT_CUDA_OR_FAIL(ctx, cudaEventSynchronize(a->staging_ev[k]));
     a->staging_next ^= 1;
     const size_t words = fill_plan(a, b, T, a->staging[k]);
+    const size_t track_words = a->track.on ? fill_track(a, b, T, a->track.staging[k]) : 0;
     st = order_after_uses(a, stream);
     if (st != SALT_OK) return st;
     const int n16 = (int)((words + 3) / 4);
     plan_copy_kernel<<<std::min(64, (n16 + 255) / 256), 256, 0, stream>>>(reinterpret_cast<const uint4 *>(a->staging[k]),
                                                                           reinterpret_cast<uint4 *>(a->plan), n16);
     SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+    if (a->track.on) {
+        const int t16 = (int)((track_words + 3) / 4);
+        plan_copy_kernel<<<std::min(64, (t16 + 255) / 256), 256, 0, stream>>>(reinterpret_cast<const uint4 *>(a->track.staging[k]),
+                                                                              reinterpret_cast<uint4 *>(a->track.table), t16);
+        SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+    }
     SALT_CUDA_OR_FAIL(ctx, cudaEventRecord(a->staging_ev[k], stream));
     a->staging_used[k] = true;
     a->T = T;
     a->use_streams.assign(1, stream);
     a->built = true;
+    a->track.built = a->track.on;
     return SALT_OK;
 } catch (const std::bad_alloc &) {
     return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
+}
+
+salt_status salt_attn_track(salt_attn *a)
+{
+    if (!a) return SALT_ERR_INVALID_ARG;
+    salt_ctx *ctx = a->kv->ctx;
+    Track &t = a->track;
+    if (t.on) return SALT_OK;
+    if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
+    t.seq_at = TRACK_HEAD;
+    t.list_at = (t.seq_at + a->cfg.max_seqs * SEQ_WORDS + 3) / 4 * 4;
+    t.words = (size_t)t.list_at + ((size_t)a->cfg.max_seqs + a->cfg.max_groups) * LIST_WORDS;
+    bool ok = cudaMalloc(&t.table, t.words * 4) == cudaSuccess;
+    for (int i = 0; i < 2 && ok; ++i) ok = cudaHostAlloc(reinterpret_cast<void **>(&t.staging[i]), t.words * 4, cudaHostAllocMapped) == cudaSuccess;
+    if (!ok) {
+        cudaGetLastError();
+        cudaFree(t.table);
+        t.table = nullptr;
+        for (int32_t *&s : t.staging) {
+            if (s) cudaFreeHost(s);
+            s = nullptr;
+        }
+        return ctx_fail(ctx, SALT_ERR_OOM, "no memory for the tracked tables");
+    }
+    t.on = true;
+    return SALT_OK;
 }
 
 salt_status salt_attn_get_shape(const salt_attn *a, salt_attn_shape *out)
@@ -1820,16 +1831,8 @@ try {
             (reinterpret_cast<uintptr_t>(lse) & 3))
             return ctx_fail(ctx, SALT_ERR_ALIGN, "rows of q or out not on 16-byte boundaries, or lse not on a 4-byte one");
     }
-    if (capture) {  // in the order of its capture's other runs; what its replays come after is the caller's to say
-        if (a->capture != capture) a->capture_streams.clear();
-        a->capture = capture;
-        SALT_CUDA_OR_FAIL(ctx, order_after(a, a->capture_streams, stream));
-        add_stream(a->capture_streams, stream);
-    } else if (a->use_streams.size() != 1 || a->use_streams[0] != stream) {
-        const salt_status st = order_after_uses(a, stream);
-        if (st != SALT_OK) return st;
-        add_stream(a->use_streams, stream);
-    }
+    const salt_status st = order_use(a, stream, capture);
+    if (st != SALT_OK) return st;
     AttnParams p;
     p.kmap = a->kmap;
     p.vmap = a->vmap;

@@ -1,0 +1,152 @@
+// The attention plan as its translation units see it: the attention itself
+// (salt_attn.cu), and what goes by its lists of cached tokens (salt_weights.cu,
+// salt_evict.cu).
+#pragma once
+
+#include <vector>
+
+#include "salt_internal.cuh"
+#include "salt_tcgen05.cuh"
+
+namespace salt {
+
+// The plan's device tables: int32 words of one block, written by the host
+// into a staging area and copied by a kernel.
+constexpr int HEAD_WORDS = 8;   // HD_* below
+constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // query tokens, records of either kind, whether rows need the combine
+
+// What a tracked plan's build writes besides: a table of its own, int32 words.
+constexpr int TRACK_HEAD = 8;   // TH_* below
+constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_LISTS = 2, TH_SHARED = 3;  // query tokens, requests, lists; whether a page is listed twice
+constexpr int SEQ_WORDS = 2;    // per request: first entry in the page lists, own cached tokens
+// per list of cached tokens that rows see, a request's own or a group's prompt: first entry in the page lists, tokens, first
+// entry in the token order, query tokens, tokens that were there before the step, tokens that the first query token sees,
+// whether the next ones each see one more, tiles of 128 tokens of the lists before
+constexpr int LIST_WORDS = 8;
+constexpr int LS_PAGES = 0, LS_LEN = 1, LS_TOK = 2, LS_NTOK = 3, LS_OLD = 4, LS_LIM = 5, LS_CAUSAL = 6, LS_TILES = 7;
+constexpr int TRACK_TILE = 128;
+
+struct Track {
+    int32_t *table = nullptr;                  // device
+    int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies, used with the plan's own
+    int seq_at = 0, list_at = 0;               // word offsets
+    size_t words = 0;
+    bool on = false, built = false, shared = false;
+    int n_seqs = 0, n_lists = 0;
+    int64_t tiles = 0;                         // of all lists
+    std::vector<uint8_t> page_seen;            // scratch of a build
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;\n" : "=f"(r) : "f"(x));
+    return r;
+}
+// 2^k, 0 below the normal range (k <= 127)
+__device__ __forceinline__ float pow2(int k) { return __uint_as_float(k < -126 ? 0u : (uint32_t)(k + 127) << 23); }
+// 2^(e - 127) of an exponent byte; 0 for a row of zeros, NaN for a row that stands for NaN
+__device__ __forceinline__ float row_scale(uint32_t e) { return __uint_as_float(e == 255u ? 0x7fc00000u : e << 23); }
+
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y)
+{
+    asm volatile("st.shared.v2.b32 [%0], {%1, %2};\n" ::"r"(a), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ float4 lds4f(uint32_t a)
+{
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ldsf(uint32_t a)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];\n" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];\n" : "=r"(v) : "r"(a) : "memory");
+    return v;
+}
+__device__ __forceinline__ void stsf(uint32_t a, float v) { asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(a), "f"(v) : "memory"); }
+__device__ __forceinline__ void sts32(uint32_t a, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(a), "r"(v) : "memory"); }
+
+// two floats at a time
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+// A bounded wait that also gives up when another role has.
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, const volatile int *dead)
+{
+    for (int i = 0; i < (1 << 20); ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 255) == 255 && *dead) return false;
+    }
+    return false;
+}
+
+// Checks that a call on the plan's tracked tables may go ahead on `stream` and orders it after the plan's other uses.
+// *captured: whether the stream is being captured.
+salt_status track_enter(salt_attn *a, int32_t layer, int32_t n_layers, cudaStream_t stream, bool *captured);
+
+}  // namespace salt
+
+struct salt_attn {
+    salt_kv *kv = nullptr;
+    salt_attn_config cfg{};
+    int device = 0, n_sm = 1;
+    CUtensorMap kmap, vmap;
+    int32_t *plan = nullptr;                   // device tables
+    int tok_at = 0, order_at = 0, rec_at = 0, rec_cap = 0, pages_at = 0;
+    size_t plan_words = 0;
+    float *part_o = nullptr, *part_l = nullptr;
+    int64_t part_cap = 0;                      // partial rows
+    int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies of the tables
+    cudaEvent_t staging_ev[2] = {nullptr, nullptr};
+    bool staging_used[2] = {false, false};
+    int staging_next = 0;
+    bool built = false;
+    bool wide = false, narrow = false;         // there are items of this kind
+    bool partial = false;                      // some row needs the combine
+    int n_items[2] = {0, 0}, most_tiles[2] = {0, 0};  // narrow and wide items of all heads, tiles of the longest
+    int T = 0;
+    std::vector<cudaStream_t> use_streams;     // the build's stream and the runs' since, but for captured ones
+    unsigned long long capture = 0;            // the capture that the last captured run belongs to
+    std::vector<cudaStream_t> capture_streams; // and its runs' streams
+    cudaEvent_t tmp_ev = nullptr;
+    salt::Track track;                         // what salt_attn_track adds
+};

@@ -151,6 +151,9 @@ _SIGS = {
     "salt_attn_build": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_batch), _vp]),
     "salt_attn_get_shape": (ctypes.c_int, [_vp, ctypes.POINTER(_attn_shape)]),
     "salt_attn_run": (ctypes.c_int, [_vp, _i32, _vp, _i64, _f32, _vp, _i64, _vp, _vp]),
+    "salt_attn_track": (ctypes.c_int, [_vp]),
+    "salt_attn_weights": (ctypes.c_int, [_vp, _i32, _vp, _i64, _vp, _f32, _f32, _vp, _vp]),
+    "salt_attn_evict": (ctypes.c_int, [_vp, _i32, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _i64, _vp]),
     "salt_verify_drafts": (ctypes.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp,
                                           _vp]),
 }
@@ -511,6 +514,7 @@ class KvCache:
         _check(_lib.salt_kv_create(ctx, ctypes.byref(cfg), ctypes.byref(out)), ctx)
         self.ctx, self.handle, self._tensors = ctx, out.value, (k, v, k_exp, v_exp)
         self.n_layers, self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = (int(n) for n in k.shape)
+        self.rows_shape = k.shape[:4]
 
     def close(self):
         if self.handle:
@@ -690,7 +694,7 @@ class AttnPlan:
         cfg = _attn_config(n_heads, max_seqs, max_tokens, max_pages, max_groups)
         _check(_lib.salt_attn_create(kv.handle, ctypes.byref(cfg), ctypes.byref(out)), kv.ctx)
         self.kv, self.ctx, self.handle, self.n_heads = kv, kv.ctx, out.value, n_heads
-        self.head_dim, self.n_tokens = kv.head_dim, 0
+        self.head_dim, self.n_tokens, self.n_seqs = kv.head_dim, 0, 0
 
     def close(self):
         if self.handle:
@@ -733,7 +737,7 @@ def salt_attn_batch(q_len, kv_len, page_ptr, pages, group=None, group_len=(), gr
 def salt_attn_build(plan: AttnPlan, batch, stream=None) -> None:
     """Plan a batch (salt_attn_batch)."""
     _check(_lib.salt_attn_build(plan.handle, ctypes.byref(batch), _stream(stream)), plan.ctx)
-    plan.n_tokens = batch._tokens
+    plan.n_tokens, plan.n_seqs = batch._tokens, batch.n_seqs
 
 
 def salt_attn_get_shape(plan: AttnPlan) -> dict:
@@ -753,6 +757,47 @@ def salt_attn_run(plan: AttnPlan, layer: int, q, out, scale: float, lse=None, st
     if lse is not None and (lse.numel() < plan.n_tokens * plan.n_heads or lse.dtype is not _torch_f32 or not lse.is_cuda):
         raise ValueError("lse is not a CUDA float32 tensor of the batch's rows")
     _check(_lib.salt_attn_run(plan.handle, layer, qp, qs, scale, op, os_, _ptr(lse), _stream(stream)), plan.ctx)
+
+
+def salt_attn_track(plan: AttnPlan) -> None:
+    """From its next build on the plan serves salt_attn_weights and salt_attn_evict."""
+    _check(_lib.salt_attn_track(plan.handle), plan.ctx)
+
+
+def _cache_floats(t, kv: KvCache, what: str) -> int:
+    """Pointer of a contiguous CUDA float32 tensor [layers, pages, kv heads, page tokens]."""
+    if _torch_f32 is None:
+        _load_types()
+    if t.dtype is not _torch_f32 or not t.is_cuda or not t.is_contiguous() or t.shape != kv.rows_shape:
+        raise ValueError(f"{what} is not a contiguous CUDA float32 tensor {list(kv.rows_shape)}")
+    return t.data_ptr()
+
+
+def salt_attn_weights(plan: AttnPlan, layer: int, q, lse, scale: float, weights, decay: float = 1.0, stream=None) -> None:
+    """Add the attention that the built batch's cached tokens of a layer get to
+    weights (CUDA float32 [layers, pages, kv heads, page tokens]), after
+    multiplying those by decay; q, lse and scale as in salt_attn_run."""
+    n, qp, qs = _head_rows(q, plan.n_heads, plan.head_dim)
+    if n < plan.n_tokens:
+        raise ValueError(f"q has fewer rows than the batch's {plan.n_tokens} query tokens")
+    if lse.numel() < plan.n_tokens * plan.n_heads or lse.dtype is not _torch_f32 or not lse.is_cuda or not lse.is_contiguous():
+        raise ValueError("lse is not a contiguous CUDA float32 tensor of the batch's rows")
+    _check(_lib.salt_attn_weights(plan.handle, layer, qp, qs, lse.data_ptr(), scale, decay, _cache_floats(weights, plan.kv, "weights"),
+                                  _stream(stream)), plan.ctx)
+
+
+def salt_attn_evict(plan: AttnPlan, layer: int, n_layers: int, keep, scores, kept, first: int = 0, recent: int = 0, weights=None,
+                    stream=None) -> None:
+    """Leave each request keep[b] (CUDA int32 [requests]) of its own tokens in
+    n_layers layers: the last `recent`, the first `first`, of the others those of
+    the largest scores (like weights, CUDA float32 [layers, pages, kv heads, page tokens]).  kept (CUDA int32
+    [n_layers, requests, kv heads, places]) gets the places they had; weights, if given, move along."""
+    n = plan.n_seqs
+    if kept.dim() != 4 or tuple(kept.shape[:3]) != (n_layers, n, plan.kv.n_kv_heads):
+        raise ValueError(f"kept is not [{n_layers}, {n}, {plan.kv.n_kv_heads}, places]")
+    _check(_lib.salt_attn_evict(plan.handle, layer, n_layers, _int32s(keep, n), first, recent, _cache_floats(scores, plan.kv, "scores"),
+                                None if weights is None else _cache_floats(weights, plan.kv, "weights"), _int32s(kept),
+                                kept.shape[3], _stream(stream)), plan.ctx)
 
 
 def _prob_rows(t, rows: int):
