@@ -30,7 +30,10 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <functional>
 #include <new>
+#include <queue>
+#include <utility>
 
 #include <cuda_fp16.h>
 
@@ -1289,6 +1292,10 @@ int items_of(const RowTile &x, double most, int *per_item)
     return (n + *per_item - 1) / *per_item;
 }
 
+// Of a unit of a tracked plan's lists of many rows, in steps of 128 rows: what it costs besides, and the least
+// that a part of one takes.
+constexpr int UNIT_COST = 2, LEAST_STEPS = 6;
+
 // Items of one cost.
 struct Same {
     float cost;
@@ -1513,11 +1520,79 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
     return (size_t)a->pages_at + own_pages + grp_pages;
 }
 
-// The tracked table of a checked batch whose plan is at w; returns the words used.
+// How the work on the lists of many rows is divided: units of 256 tokens of a head and a run of steps over their rows,
+// handed to the CTAs from the costliest down, each to the one that has least.  Where units are few or unequal, those of
+// many steps are split in parts, each a unit, that meet in a partial sum.  Where they are very many every CTA
+// takes each n_sm-th instead.
+void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
+{
+    Track &tr = a->track;
+    const int KV = a->kv->dev.heads, per = 128 / (a->cfg.n_heads / KV), n_sm = a->n_sm;
+    tr.split = false;
+    t[TH_LISTED] = 0;
+    if (n_many == 0 || tiles * KV > TRACK_UNITS / 2 || n_sm + 1 > TRACK_CTAS) return;
+    struct Tile {
+        int tile, from, to;
+    };
+    std::vector<Tile> all;
+    int64_t sum = 0;
+    for (int i = n_few; i < n_few + n_many; ++i) {
+        const int32_t *l = t + tr.list_at + (size_t)i * LIST_WORDS;
+        const int steps = (l[3] + per - 1) / per;
+        for (int j = 0; j < (l[1] + TRACK_MANY_TILE - 1) / TRACK_MANY_TILE; ++j) {
+            all.push_back({l[LS_TILES] + j, first_step(l[6], l[5], j * TRACK_MANY_TILE, per), steps});
+            sum += steps - all.back().from;
+        }
+    }
+    // a part takes at least what a unit costs besides its steps, a few times over
+    const int64_t share = sum * KV / n_sm, most = std::max<int64_t>(LEAST_STEPS, share / 3);
+    struct Piece {
+        int cost;
+        int32_t w[UNIT_WORDS];
+    };
+    std::vector<Piece> pieces;
+    int slots = 0;
+    for (const Tile &x : all) {
+        const int steps = x.to - x.from;
+        int parts = (int)std::min<int64_t>((steps + most - 1) / most, 64);
+        if (slots + (int64_t)parts * KV > TRACK_SLOTS || (int64_t)pieces.size() + (int64_t)(parts + (int64_t)all.size()) * KV > TRACK_UNITS) parts = 1;
+        for (int kh = 0; kh < KV; ++kh) {
+            for (int k = 0; k < parts; ++k) {
+                const int from = x.from + (int)((int64_t)steps * k / parts), to = x.from + (int)((int64_t)steps * (k + 1) / parts);
+                pieces.push_back({to - from + UNIT_COST, {x.tile * KV + kh, from, to, parts == 1 ? -1 : slots << 12 | k << 6 | (parts - 1)}});
+            }
+            if (parts > 1) slots += parts;
+        }
+    }
+    if ((int64_t)pieces.size() > TRACK_UNITS) return;
+    tr.split = slots > 0;
+    t[TH_LISTED] = 1;
+    std::stable_sort(pieces.begin(), pieces.end(), [](const Piece &x, const Piece &y) { return x.cost > y.cost; });
+    using Load = std::pair<int64_t, int>;
+    std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
+    for (int c = 0; c < n_sm; ++c) least.push({0, c});
+    std::vector<int> owner(pieces.size());
+    int32_t *ptr = t + tr.unit_at, *units = ptr + TRACK_CTAS;
+    std::fill(ptr, ptr + n_sm + 1, 0);
+    for (size_t i = 0; i < pieces.size(); ++i) {
+        Load l = least.top();
+        least.pop();
+        owner[i] = l.second;
+        ++ptr[l.second + 1];
+        l.first += pieces[i].cost;
+        least.push(l);
+    }
+    for (int c = 0; c < n_sm; ++c) ptr[c + 1] += ptr[c];
+    std::vector<int> next(ptr, ptr + n_sm);
+    for (size_t i = 0; i < pieces.size(); ++i) std::memcpy(units + (size_t)next[owner[i]]++ * UNIT_WORDS, pieces[i].w, UNIT_WORDS * 4);
+}
+
+// The tracked table of a checked batch; returns the words used.
 size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
 {
     Track &tr = a->track;
     const KvDev &kv = a->kv->dev;
+    const int G = a->cfg.n_heads / kv.heads;
     std::memset(t, 0, TRACK_HEAD * 4);
     const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
     tr.page_seen.assign(kv.n_pages, 0);
@@ -1528,21 +1603,16 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
             tr.page_seen[pages[j]] = 1;
         }
     };
-    int32_t *list = t + tr.list_at;
-    int n = 0;
-    int64_t tiles = 0;
+    struct Words {
+        int32_t w[LIST_WORDS];
+    };
+    std::vector<Words> lists[2];   // of few rows, of many
+    int64_t tiles[2] = {0, 0};
     auto add = [&](int pages, int len, int tok, int ntok, int old, int lim, bool causal) {
         if (len == 0 || ntok == 0) return;
-        int32_t *l = list + (size_t)n++ * LIST_WORDS;
-        l[LS_PAGES] = pages;
-        l[LS_LEN] = len;
-        l[LS_TOK] = tok;
-        l[LS_NTOK] = ntok;
-        l[LS_OLD] = old;
-        l[LS_LIM] = lim;
-        l[LS_CAUSAL] = causal;
-        l[LS_TILES] = (int)tiles;
-        tiles += (len + TRACK_TILE - 1) / TRACK_TILE;
+        const int kind = (int64_t)ntok * G > TRACK_FEW_ROWS, tile = kind ? TRACK_MANY_TILE : TRACK_TILE;
+        lists[kind].push_back({{pages, len, tok, ntok, old, lim, causal, (int)tiles[kind]}});
+        tiles[kind] += (len + tile - 1) / tile;
     };
     std::vector<int> rows(b->n_groups, 0);  // query tokens of each group
     int t0 = 0;
@@ -1559,12 +1629,22 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
         note(b->group_pages + b->group_page_ptr[g], b->group_len[g]);
         add(own_pages + b->group_page_ptr[g], b->group_len[g], at, rows[g], b->group_len[g], b->group_len[g], false);
     }
+    int32_t *list = t + tr.list_at;
+    for (const auto &kind : lists)
+        for (const Words &l : kind) {
+            std::memcpy(list, l.w, sizeof l.w);
+            list += LIST_WORDS;
+        }
     t[TH_TOKENS] = T;
     t[TH_SEQS] = tr.n_seqs = b->n_seqs;
-    t[TH_LISTS] = tr.n_lists = n;
+    t[TH_FEW] = tr.few = (int)lists[0].size();
+    t[TH_MANY] = tr.many = (int)lists[1].size();
+    t[TH_FEW_TILES] = (int)tiles[0];
+    t[TH_MANY_TILES] = (int)tiles[1];
     t[TH_SHARED] = tr.shared;
-    tr.tiles = tiles;
-    return (size_t)tr.list_at + (size_t)n * LIST_WORDS;
+    tr.few_tiles = tiles[0];
+    fill_units(a, tr.few, tr.many, tiles[1], t);
+    return t[TH_LISTED] ? tr.words : (size_t)(list - t);
 }
 
 // A cache's codes as rows of D bytes, a box a page's rows of one head, swizzled over a row's width.
@@ -1710,6 +1790,8 @@ void salt_attn_destroy(salt_attn *a)
     cudaFree(a->part_o);
     cudaFree(a->part_l);
     cudaFree(a->track.table);
+    cudaFree(a->track.part);
+    cudaFree(a->track.arrived);
     for (int i = 0; i < 2; ++i) {
         if (a->track.staging[i]) cudaFreeHost(a->track.staging[i]);
         if (a->staging[i]) cudaFreeHost(a->staging[i]);
@@ -1751,6 +1833,8 @@ try {
         plan_copy_kernel<<<std::min(64, (t16 + 255) / 256), 256, 0, stream>>>(reinterpret_cast<const uint4 *>(a->track.staging[k]),
                                                                               reinterpret_cast<uint4 *>(a->track.table), t16);
         SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+        // (a call whose waits gave up may have left some)
+        if (a->track.split) SALT_CUDA_OR_FAIL(ctx, cudaMemsetAsync(a->track.arrived, 0, TRACK_SLOTS * 8 * 4, stream));
     }
     SALT_CUDA_OR_FAIL(ctx, cudaEventRecord(a->staging_ev[k], stream));
     a->staging_used[k] = true;
@@ -1772,13 +1856,20 @@ salt_status salt_attn_track(salt_attn *a)
     if (!ctx_select_device(ctx)) return ctx_fail(ctx, SALT_ERR_CUDA, "cannot select the device");
     t.seq_at = TRACK_HEAD;
     t.list_at = (t.seq_at + a->cfg.max_seqs * SEQ_WORDS + 3) / 4 * 4;
-    t.words = (size_t)t.list_at + ((size_t)a->cfg.max_seqs + a->cfg.max_groups) * LIST_WORDS;
-    bool ok = cudaMalloc(&t.table, t.words * 4) == cudaSuccess;
+    t.unit_at = t.list_at + (a->cfg.max_seqs + a->cfg.max_groups) * LIST_WORDS;
+    t.words = (size_t)t.unit_at + TRACK_CTAS + TRACK_UNITS * UNIT_WORDS;
+    bool ok = cudaMalloc(&t.table, t.words * 4) == cudaSuccess &&
+              cudaMalloc(&t.part, (size_t)TRACK_SLOTS * TRACK_MANY_TILE * 4) == cudaSuccess &&
+              cudaMalloc(&t.arrived, TRACK_SLOTS * 8 * 4) == cudaSuccess && cudaMemset(t.arrived, 0, TRACK_SLOTS * 8 * 4) == cudaSuccess;
     for (int i = 0; i < 2 && ok; ++i) ok = cudaHostAlloc(reinterpret_cast<void **>(&t.staging[i]), t.words * 4, cudaHostAllocMapped) == cudaSuccess;
     if (!ok) {
         cudaGetLastError();
         cudaFree(t.table);
+        cudaFree(t.part);
+        cudaFree(t.arrived);
         t.table = nullptr;
+        t.part = nullptr;
+        t.arrived = nullptr;
         for (int32_t *&s : t.staging) {
             if (s) cudaFreeHost(s);
             s = nullptr;

@@ -17,23 +17,37 @@ constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // que
 
 // What a tracked plan's build writes besides: a table of its own, int32 words.
 constexpr int TRACK_HEAD = 8;   // TH_* below
-constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_LISTS = 2, TH_SHARED = 3;  // query tokens, requests, lists; whether a page is listed twice
+// query tokens, requests, lists of few rows, whether a page is listed twice, tiles of 128 tokens of those lists, lists of many rows (behind the others),
+// tiles of 256 tokens of those, whether the units of their work are listed
+constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_TILES = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7;
 constexpr int SEQ_WORDS = 2;    // per request: first entry in the page lists, own cached tokens
 // per list of cached tokens that rows see, a request's own or a group's prompt: first entry in the page lists, tokens, first
 // entry in the token order, query tokens, tokens that were there before the step, tokens that the first query token sees,
-// whether the next ones each see one more, tiles of 128 tokens of the lists before
+// whether the next ones each see one more, tiles of the lists of its kind before
 constexpr int LIST_WORDS = 8;
-constexpr int LS_PAGES = 0, LS_LEN = 1, LS_TOK = 2, LS_NTOK = 3, LS_OLD = 4, LS_LIM = 5, LS_CAUSAL = 6, LS_TILES = 7;
-constexpr int TRACK_TILE = 128;
+constexpr int LS_TILES = 7;
+constexpr int TRACK_TILE = 128, TRACK_MANY_TILE = 256;
+constexpr int TRACK_FEW_ROWS = 16;
+// units of the many rows' lists: each CTA's first one, then per unit: tile * heads + head, steps [from, to), (slot of its
+// first part << 12 | part << 6 | parts - 1) or -1
+constexpr int TRACK_CTAS = 512, UNIT_WORDS = 4, TRACK_UNITS = 8192;
+constexpr int TRACK_SLOTS = 2048;  // of partial sums, 256 tokens each
+// The first step of `per` query tokens that sees token t0.
+__host__ __device__ constexpr int first_step(bool causal, int lim, int t0, int per)
+{
+    return causal && t0 >= lim ? (t0 - lim + 1) / per : 0;
+}
 
 struct Track {
     int32_t *table = nullptr;                  // device
     int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies, used with the plan's own
-    int seq_at = 0, list_at = 0;               // word offsets
+    float *part = nullptr;                     // [TRACK_SLOTS][256]
+    uint32_t *arrived = nullptr;               // [TRACK_SLOTS][8], zero between calls
+    int seq_at = 0, list_at = 0, unit_at = 0;  // word offsets
     size_t words = 0;
-    bool on = false, built = false, shared = false;
-    int n_seqs = 0, n_lists = 0;
-    int64_t tiles = 0;                         // of all lists
+    bool on = false, built = false, shared = false, split = false;
+    int n_seqs = 0, few = 0, many = 0;
+    int64_t few_tiles = 0;
     std::vector<uint8_t> page_seen;            // scratch of a build
 };
 
@@ -104,6 +118,15 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
 {
     float2 r;
     asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mul.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    float2 r;
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
         : "=f"(r.x), "=f"(r.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;

@@ -3,8 +3,18 @@
 //     W[j] = decay * W[j] + sum_i exp(scale * q_i k_j - lse_i)
 // over the rows i (query token x query heads of the token's key/value head) that
 // see token j, W[j] counted as 0 for the step's own tokens.  The rows' log-sums come from
-// the attention itself, so that one pass over the keys is all there is to do, and a
-// token's weight is one thread's sum in a fixed order.
+// the attention itself, so that one pass over the keys is all there is to do.  The scores are made on the
+// tensor cores with the cached tokens as the 128-row operand, S[token][row] = K[token][:] . Q[row][:], so that a
+// token's weight is a sum over one thread's columns of tensor memory, in a fixed order.
+//
+// Lists of few rows (single query tokens, a few drafts) are bound by reading the keys: their e4m3 codes go to the
+// tensor cores as they are, one tile of 128 tokens after the other, and meet the query as two e4m3 terms, hi + 2^-5
+// lo: 4 and 4 bits, so a bf16 whole but for elements 2^-15 below the row's largest (2^-22 of
+// that).  The two terms have columns of their own, as lo would lose its small elements without its factor.
+//
+// Lists of many rows are bound by the products and exponentials: 256 tokens' keys are widened to bf16 once
+// (exact) and stay, the query's rows stream past them as they are.
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -23,15 +33,21 @@ namespace {
 constexpr float LOG2E = 1.4426950408889634f;
 
 struct WeightParams {
+    alignas(64) CUtensorMap kmap;   // the codes of every layer as rows of D bytes, box of one page
+    alignas(64) CUtensorMap qmap;   // wide: q as [tokens][heads][D], box of 64 elements of a group's heads of a step's tokens
+    alignas(64) CUtensorMap qmap1;  // the same of one token
     const int32_t *plan, *track;
-    int32_t order_at, pages_at, list_at;
+    int32_t order_at, pages_at, list_at, unit_at;
     KvDev kv;
     int64_t layer;
     const uint16_t *q;
     const float *lse;
     float *weights;
+    float *part;                    // partial sums of units whose rows are split
+    uint32_t *arrived;              // how many of a unit's parts are there
     int64_t q_stride;
     int32_t n_heads, max_tok;
+    int32_t behind;                 // whether the wide lists' kernel is the one before
     float scale, decay;
     uint32_t *err;
 };
@@ -46,87 +62,849 @@ __device__ __forceinline__ List load_list(const WeightParams &p, int i)
     const int4 a = __ldg(w), b = __ldg(w + 1);
     return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
-// The list that holds tile `tile` of all lists: the last one that begins at or before it.
-__device__ __forceinline__ int find_list(const WeightParams &p, int n, int tile)
+// Of the lists [lo, hi) the one that holds tile `tile` of them: the last that begins at or before it.
+__device__ __forceinline__ int find_list(const WeightParams &p, int lo, int hi, int tile)
 {
-    int lo = 0;
-    for (int hi = n; hi - lo > 1;) {
+    while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (__ldg(p.track + p.list_at + mid * LIST_WORDS + LS_TILES) <= tile) lo = mid;
         else hi = mid;
     }
     return lo;
 }
-
-constexpr int ROWS_AT_ONCE = 16;
-
-// A thread has a token's key in registers and walks the rows, which go through shared memory.
-template <int D>
-__global__ void __launch_bounds__(TRACK_TILE) weights_kernel(const WeightParams p)
+__device__ __forceinline__ int64_t first_row(const WeightParams &p, int page, int kh)
 {
-    __shared__ __align__(16) float s_q[ROWS_AT_ONCE][D];
-    __shared__ float s_lse[ROWS_AT_ONCE];
-    const int32_t *track = p.track;
-    if (track[TH_TOKENS] > p.max_tok || track[TH_SHARED]) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
-        return;
+    return ((p.layer * p.kv.n_pages + page) * p.kv.heads + kh) << p.kv.page_log2;
+}
+
+// ---------------------------------------------------------------- few rows
+template <int D_>
+struct Few {
+    static constexpr int D = D_;
+    static constexpr int R = TRACK_FEW_ROWS;                // rows of a list at most
+    static constexpr int N = 2 * R;                         // hi and lo
+    static constexpr int CTAS = 3;                          // an SM
+    static constexpr int THREADS = 256;
+    static constexpr int KST = D == 128 ? 3 : 6, EST = 8;   // stages of keys, and of what goes with a tile
+    static constexpr int SB = 4;                            // buffers of scores
+    static constexpr uint32_t TM_COLS = SB * N;
+    static constexpr uint32_t SIDE = TRACK_TILE * D;
+    static constexpr uint32_t K = 0;
+    static constexpr uint32_t Q_BUF = N * D;
+    static constexpr uint32_t Q = K + KST * SIDE;           // two segments' queries
+    static constexpr uint32_t INFO_BUF = R * 16;            // factors of the scores, log-sums, tokens seen
+    static constexpr uint32_t INFO = Q + 2 * Q_BUF;
+    // a tile's old weights, exponents, first rows of its pages
+    static constexpr uint32_t E_W = 0, E_EXP = TRACK_TILE * 4, E_ROW = E_EXP + TRACK_TILE, E_BUF = E_ROW + 64;
+    static constexpr uint32_t E = INFO + 2 * INFO_BUF;
+    static constexpr uint32_t K_FULL = E + EST * E_BUF;
+    static constexpr uint32_t K_FREE = K_FULL + 8 * KST;
+    static constexpr uint32_t E_FULL = K_FREE + 8 * KST;
+    static constexpr uint32_t E_FREE = E_FULL + 8 * EST;
+    static constexpr uint32_t S_FULL = E_FREE + 8 * EST;
+    static constexpr uint32_t S_FREE = S_FULL + 8 * SB;
+    static constexpr uint32_t Q_FULL = S_FREE + 8 * SB;
+    static constexpr uint32_t Q_FREE = Q_FULL + 16;         // by the products
+    static constexpr uint32_t I_FREE = Q_FREE + 16;         // by the sums
+    static constexpr uint32_t DRAIN = I_FREE + 16;
+    static constexpr uint32_t MISC = DRAIN + 8;             // TMEM address, failure flag
+    static constexpr uint32_t BYTES = MISC + 8 + 1024;      // slack for the 1024-byte alignment
+    static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
+    static_assert(TM_COLS * CTAS <= 512 && (TM_COLS & (TM_COLS - 1)) == 0, "tensor memory");
+};
+
+// A CTA's tiles [g, end) of the few rows' lists in the order list, key/value head, tile.  A segment is those of one list and head.
+struct Walk {
+    int64_t g, end;
+    int list, kh, j, tiles, segment;
+    List l;
+    __device__ __forceinline__ Walk(const WeightParams &p, int n_lists, int64_t all)
+    {
+        const int KV = p.kv.heads;
+        g = all * blockIdx.x / gridDim.x;
+        end = all * (blockIdx.x + 1) / gridDim.x;
+        segment = 0;
+        if (g >= end) return;
+        list = find_list(p, 0, n_lists, (int)(g / KV));  // (a list's first tile of all heads is its first tile times the heads)
+        l = load_list(p, list);
+        tiles = (l.len + TRACK_TILE - 1) / TRACK_TILE;
+        const int in = (int)(g - (int64_t)l.tiles * KV);
+        kh = in / tiles;
+        j = in - kh * tiles;
     }
-    const int KV = p.kv.heads, G = p.n_heads / KV, n_lists = track[TH_LISTS], tid = threadIdx.x;
-    if (n_lists == 0) return;
-    const List last = load_list(p, n_lists - 1);
-    const int64_t units = (int64_t)(last.tiles + (last.len + TRACK_TILE - 1) / TRACK_TILE) * KV;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int tile = (int)(u / KV), kh = (int)(u - (int64_t)tile * KV);
-        const List l = load_list(p, find_list(p, n_lists, tile));
-        const int j = (tile - l.tiles) * TRACK_TILE + tid;
-        const bool live = j < l.len;
-        const int page = live ? __ldg(p.plan + p.pages_at + l.pages + (j >> p.kv.page_log2)) : 0;
-        const int64_t at = (((p.layer * p.kv.n_pages + page) * KV + kh) << p.kv.page_log2) + (j & (p.kv.page - 1));
-        float k[D];
-        float kf = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 4; ++i) {
-            const uint32_t c = live ? __ldg(reinterpret_cast<const uint32_t *>(p.kv.k + at * D) + i) : 0;
-            const uint32_t lo = f16x2_of_e4m3x2((uint16_t)c), hi = f16x2_of_e4m3x2((uint16_t)(c >> 16));
-            const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&lo)), b = __half22float2(*reinterpret_cast<const __half2 *>(&hi));
-            k[4 * i] = a.x, k[4 * i + 1] = a.y, k[4 * i + 2] = b.x, k[4 * i + 3] = b.y;
-        }
-        if (live) kf = row_scale(p.kv.k_exp[at]);
-        float sum = 0.f;
-        const int rows = l.ntok * G;
-        for (int r0 = 0; r0 < rows; r0 += ROWS_AT_ONCE) {
-            __syncthreads();
-            for (int i = tid; i < ROWS_AT_ONCE * (D / 2); i += TRACK_TILE) {
-                const int r = r0 + i / (D / 2), d = i % (D / 2);
-                uint32_t x = 0;
-                if (r < rows) {
-                    const int t = __ldg(p.plan + p.order_at + l.tok + r / G);
-                    x = __ldg(reinterpret_cast<const uint32_t *>(p.q + t * p.q_stride + (kh * G + r % G) * D) + d);
-                    if (d == 0) s_lse[r - r0] = p.lse[(int64_t)t * p.n_heads + kh * G + r % G];
-                }
-                s_q[r - r0][2 * d] = __uint_as_float(x << 16);
-                s_q[r - r0][2 * d + 1] = __uint_as_float(x & 0xffff0000u);
+    __device__ __forceinline__ bool more() const { return g < end; }
+    __device__ __forceinline__ bool last_of_segment() const { return g + 1 == end || j + 1 == tiles; }
+    __device__ __forceinline__ void next_segment(const WeightParams &p)
+    {
+        j = 0;
+        ++segment;
+        if (++kh == p.kv.heads) {
+            kh = 0;
+            if (g < end) {
+                l = load_list(p, ++list);
+                tiles = (l.len + TRACK_TILE - 1) / TRACK_TILE;
             }
-            __syncthreads();
-            for (int i = 0; i < min(ROWS_AT_ONCE, rows - r0); ++i) {
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int d = 0; d < D; d += 4) {
-                    const float4 q = *reinterpret_cast<const float4 *>(&s_q[i][d]);
-                    s[0] = fmaf(q.x, k[d], s[0]);
-                    s[1] = fmaf(q.y, k[d + 1], s[1]);
-                    s[2] = fmaf(q.z, k[d + 2], s[2]);
-                    s[3] = fmaf(q.w, k[d + 3], s[3]);
-                }
-                const float x = fmaf((s[0] + s[1] + (s[2] + s[3])) * kf, p.scale, -s_lse[i]);
-                if (j < l.lim + (l.causal ? (r0 + i) / G : 0)) sum += ex2(x * LOG2E);
-            }
-        }
-        if (live) {
-            float *w = p.weights + at;
-            *w = p.decay != 0.f && j < l.old ? fmaf(p.decay, *w, sum) : sum;
         }
     }
+    __device__ __forceinline__ void next(const WeightParams &p)
+    {
+        ++g;
+        if (++j == tiles) next_segment(p);
+    }
+    // past the segment
+    __device__ __forceinline__ void skip(const WeightParams &p)
+    {
+        g += tiles - j;
+        next_segment(p);
+    }
+};
+
+// A segment's queries, each row scaled by a power of two, and the constants of its columns: two warps, this one the w-th.
+template <class L>
+__device__ __forceinline__ void stage_few(const WeightParams &p, uint32_t base, const Walk &k, int w)
+{
+    constexpr int LPR = L::D / 8, RPW = 32 / LPR;   // lanes a row, rows a warp deals with at a time
+    const int G = p.n_heads / p.kv.heads, lane = threadIdx.x & 31, part = lane % LPR, rows = k.l.ntok * G;
+    const uint32_t q_at = base + L::Q + (k.segment & 1) * L::Q_BUF, info = base + L::INFO + (k.segment & 1) * L::INFO_BUF;
+    constexpr int AT_ONCE = L::R / (2 * RPW);
+    uint4 q[AT_ONCE];
+    float lse[AT_ONCE];
+#pragma unroll
+    for (int n = 0; n < AT_ONCE; ++n) {
+        const int row = (2 * n + w) * RPW + lane / LPR, i = row / G, h = k.kh * G + row - i * G;
+        q[n] = make_uint4(0, 0, 0, 0);
+        lse[n] = 0.f;
+        if (row < rows) {
+            const int t = __ldg(p.plan + p.order_at + k.l.tok + i);
+            q[n] = __ldg(reinterpret_cast<const uint4 *>(p.q + t * p.q_stride + h * L::D) + part);
+            lse[n] = __ldg(p.lse + (int64_t)t * p.n_heads + h);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < AT_ONCE; ++n) {
+        const int row = (2 * n + w) * RPW + lane / LPR, i = row / G;
+        const uint4 u = q[n];
+        const uint32_t x[4] = {u.x, u.y, u.z, u.w};
+        uint32_t a = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a = max(a, max((x[e] << 16) & 0x7fffffffu, x[e] & 0x7fff0000u));
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
+        const int qe = max((int)(a >> 23) - 127 - 7, -120);  // the row's largest element to [2^7, 2^8)
+        const float inv = pow2(-qe);
+        uint32_t hi[2] = {0, 0}, lo[2] = {0, 0};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float v0 = __uint_as_float(x[e] << 16) * inv, v1 = __uint_as_float(x[e] & 0xffff0000u) * inv;
+            const uint16_t c = e4m3x2(v0, v1);
+            const uint32_t back = f16x2_of_e4m3x2(c);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&back));
+            hi[e / 2] |= (uint32_t)c << (16 * (e & 1));
+            lo[e / 2] |= (uint32_t)e4m3x2((v0 - f.x) * 32.f, (v1 - f.y) * 32.f) << (16 * (e & 1));  // (v - f at most 2^3)
+        }
+        if ((a >> 23) == 255) hi[0] = hi[1] = lo[0] = lo[1] = 0x7f7f7f7fu;
+        sts64(q_at + swz_rows<L::D>(row * L::D + part * 8), hi[0], hi[1]);
+        sts64(q_at + swz_rows<L::D>((L::R + row) * L::D + part * 8), lo[0], lo[1]);
+        if (part == 0) {  // (rows that fill up see nothing)
+            stsf(info + 4 * row, pow2(qe) * p.scale);
+            stsf(info + 4 * (L::R + row), -lse[n]);
+            sts32(info + 4 * (2 * L::R + row), row < rows ? k.l.lim + (k.l.causal ? i : 0) : 0);
+        }
+    }
+    fence_async_smem();
+}
+
+template <class L>
+__global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const __grid_constant__ WeightParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, KV = p.kv.heads;
+    volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
+    if (tid == 0) {
+        for (int i = 0; i < L::KST; ++i) {
+            mbar_init(base + L::K_FULL + 8 * i, 1);
+            mbar_init(base + L::K_FREE + 8 * i, 1);
+        }
+        for (int i = 0; i < L::EST; ++i) {
+            mbar_init(base + L::E_FULL + 8 * i, 1);
+            mbar_init(base + L::E_FREE + 8 * i, 4);
+        }
+        for (int i = 0; i < L::SB; ++i) {
+            mbar_init(base + L::S_FULL + 8 * i, 1);
+            mbar_init(base + L::S_FREE + 8 * i, 4);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(base + L::Q_FULL + 8 * i, 2);
+            mbar_init(base + L::Q_FREE + 8 * i, 1);
+            mbar_init(base + L::I_FREE + 8 * i, 4);
+        }
+        mbar_init(base + L::DRAIN, 1);
+        *dead = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(base + L::MISC, L::TM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<uint32_t *>(sm + L::MISC);
+    // (behind the wide lists' kernel nothing that it writes is needed, and it lets this one begin after its own wait)
+    if (!p.behind) pdl_wait();
+    pdl_launch_dependents();
+    const int32_t *track = after_pdl_wait(p.track);
+    const bool fits = track[TH_TOKENS] <= p.max_tok && !track[TH_SHARED];
+    if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
+    const int n_lists = fits ? track[TH_FEW] : 0;
+    Walk k(p, n_lists, n_lists ? (int64_t)track[TH_FEW_TILES] * KV : 0);
+    bool ok = true;
+    if (!k.more()) {
+    } else if (warp == 0) {
+        // ------------------------------------------------ loads: a lane per page of a tile
+        uint32_t ks = 0, kph = 0, es = 0, eph = 0, n = 0;
+        const int per = TRACK_TILE >> p.kv.page_log2;
+        for (; k.more() && ok; k.next(p), ++n) {
+            const int t = k.j * TRACK_TILE, first = t >> p.kv.page_log2;
+            const int pages = min(per, ((k.l.len - 1) >> p.kv.page_log2) - first + 1);
+            int page = 0;
+            if (lane < pages) page = __ldg(p.plan + p.pages_at + k.l.pages + first + lane);
+            const int64_t row = first_row(p, page, k.kh);
+            const bool old = p.decay != 0.f && t < k.l.old;
+            const uint32_t k_full = base + L::K_FULL + 8 * ks, e_full = base + L::E_FULL + 8 * es, e = base + L::E + es * L::E_BUF;
+            if (n >= (uint32_t)L::EST) ok = wait_bar(base + L::E_FREE + 8 * es, eph ^ 1, dead);
+            if (ok && n >= (uint32_t)L::KST) ok = wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (lane < pages) sts32(e + L::E_ROW + 4 * lane, (uint32_t)row);
+            __syncwarp();
+            if (lane == 0) {
+                mbar_expect_tx(k_full, pages * p.kv.page * L::D);
+                mbar_expect_tx(e_full, pages * p.kv.page * (old ? 5 : 1));
+            }
+            __syncwarp();
+            if (lane < pages) {
+                const uint32_t at = lane * p.kv.page;
+                tma_load_2d(base + L::K + ks * L::SIDE + at * L::D, &p.kmap, 0, (int)row, k_full);
+                bulk_load(e + L::E_EXP + at, p.kv.k_exp + row, p.kv.page, e_full);
+                if (old) bulk_load(e + L::E_W + 4 * at, p.weights + row, p.kv.page * 4, e_full);
+            }
+            if (++ks == (uint32_t)L::KST) ks = 0, kph ^= 1;
+            if (++es == (uint32_t)L::EST) es = 0, eph ^= 1;
+        }
+        if (!ok) {  // copies in flight land before the CTA ends
+            if (lane == 0) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+            }
+            for (uint32_t i = 0; i < min(n, (uint32_t)L::KST); ++i) mbar_wait(base + L::K_FULL + 8 * ((n - 1 - i) % L::KST), ((n - 1 - i) / L::KST) & 1);
+            for (uint32_t i = 0; i < min(n, (uint32_t)L::EST); ++i) mbar_wait(base + L::E_FULL + 8 * ((n - 1 - i) % L::EST), ((n - 1 - i) / L::EST) & 1);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issue
+        const bool lead = elect_one();
+        const uint32_t id = idesc_e4m3_f32(128, L::N);
+        uint32_t ks = 0, kph = 0, n = 0;
+        bool fresh = true;
+        for (; k.more(); k.next(p), ++n) {
+            const int b = n % L::SB, qb = k.segment & 1;
+            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * qb, (k.segment >> 1) & 1, dead);
+            fresh = k.last_of_segment();
+            ok = ok && wait_bar(base + L::K_FULL + 8 * ks, kph, dead);
+            if (n >= (uint32_t)L::SB) ok = ok && wait_bar(base + L::S_FREE + 8 * b, (n / L::SB - 1) & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            tc_fence_after();
+            const uint64_t kd = sdesc_rows(base + L::K + ks * L::SIDE, L::D, 0), qd = sdesc_rows(base + L::Q + qb * L::Q_BUF, L::D, 0);
+            if (lead) {
+#pragma unroll
+                for (int i = 0; i < L::D / 32; ++i) umma_e4m3(tmem + b * L::N, kd + 2 * i, qd + 2 * i, id, i > 0);
+                umma_commit(base + L::S_FULL + 8 * b);
+                umma_commit(base + L::K_FREE + 8 * ks);
+                if (fresh) umma_commit(base + L::Q_FREE + 8 * qb);
+            }
+            __syncwarp();
+            if (++ks == (uint32_t)L::KST) ks = 0, kph ^= 1;
+        }
+        if (!ok) {  // the products issued so far end before the CTA does
+            if (lead) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+                umma_commit(base + L::DRAIN);
+                mbar_wait(base + L::DRAIN, 0);
+            }
+            __syncwarp();
+        }
+    } else if (warp < 4) {
+        // ------------------------------------------------ queries, a segment ahead
+        for (; k.more(); k.skip(p)) {
+            const int s = k.segment, b = s & 1;
+            if (s > 1) ok = wait_bar(base + L::Q_FREE + 8 * b, ((s - 2) >> 1) & 1, dead) && wait_bar(base + L::I_FREE + 8 * b, ((s - 2) >> 1) & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            stage_few<L>(p, base, k, warp - 2);
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * b);
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    } else {
+        // ------------------------------------------------ a thread's token: its row of scores, its weight
+        const int me = tid - 128, G = p.n_heads / KV;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        uint32_t es = 0, eph = 0, n = 0;
+        bool fresh = true;
+        for (; k.more(); k.next(p), ++n) {
+            const int b = n % L::SB, qb = k.segment & 1, j = k.j * TRACK_TILE + me, rows = k.l.ntok * G;
+            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * qb, (k.segment >> 1) & 1, dead);
+            fresh = k.last_of_segment();
+            ok = ok && wait_bar(base + L::E_FULL + 8 * es, eph, dead);
+            const uint32_t e = base + L::E + es * L::E_BUF;
+            const float kf = row_scale(lds8(e + L::E_EXP + me));
+            const float was = p.decay != 0.f && j < k.l.old ? p.decay * ldsf(e + L::E_W + 4 * me) : 0.f;
+            const uint32_t at = lds32(e + L::E_ROW + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
+            ok = ok && wait_bar(base + L::S_FULL + 8 * b, (n / L::SB) & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive_release(base + L::E_FREE + 8 * es);
+            tc_fence_after();
+            const uint32_t info = base + L::INFO + qb * L::INFO_BUF, s_at = tmem + lanes + b * L::N;
+            float sum = 0.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < rows; c0 += 4) {
+                float hi[4], lo[4];
+                tmem_ld4(s_at + c0, reinterpret_cast<uint32_t *>(hi));
+                tmem_ld4(s_at + L::R + c0, reinterpret_cast<uint32_t *>(lo));
+                const float4 a = lds4f(info + 4 * c0), l = lds4f(info + 4 * (L::R + c0));
+                const uint4 lim = lds128(info + 4 * (2 * L::R + c0));
+                tmem_ld_wait();
+                const float f[4] = {a.x, a.y, a.z, a.w}, m[4] = {l.x, l.y, l.z, l.w};
+                const int see[4] = {(int)lim.x, (int)lim.y, (int)lim.z, (int)lim.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float x = fmaf(fmaf(lo[i], 0.03125f, hi[i]), f[i] * kf, m[i]) * LOG2E;
+                    if (j < see[i]) sum += ex2(x);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive_release(base + L::S_FREE + 8 * b);
+                if (fresh) mbar_arrive_release(base + L::I_FREE + 8 * qb);
+            }
+            if (j < k.l.len) p.weights[at] = was + sum;
+            if (++es == (uint32_t)L::EST) es = 0, eph ^= 1;
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
+    pdl_wait();  // so that what follows this kernel follows the one before it too
+}
+
+// ---------------------------------------------------------------- many rows
+// A unit is 256 tokens of a list and head, and a run of steps over the rows that see them, up to 128 at
+// a time.  Two warpgroups have 128 tokens each, all of the step's columns.
+template <int D_>
+struct Many {
+    static constexpr int D = D_;
+    static constexpr int THREADS = 128 + 2 * 128;
+    static constexpr int QST = D == 128 ? 3 : 6, MST = 4;   // stages of queries, and of what goes with a step
+    static constexpr uint32_t TM_COLS = 512;                // two buffers of 128 scores for either 128 tokens
+    static constexpr uint32_t A_TILE = 128 * 2 * D, RAW_TILE = 128 * D, Q_TILE = 128 * 2 * D;
+    static constexpr uint32_t A = 0;
+    static constexpr uint32_t RAW = A + 2 * A_TILE;
+    static constexpr uint32_t Q = RAW + 2 * RAW_TILE;
+    static constexpr uint32_t M_LSE = 0, M_LIM = 512, M_BUF = 1024;
+    static constexpr uint32_t META = Q + QST * Q_TILE;
+    static constexpr uint32_t EXPS = META + MST * M_BUF;    // 128 of either tile
+    static constexpr uint32_t ROWS = EXPS + 256;            // the first rows of either tile's pages
+    static constexpr uint32_t K_FULL = ROWS + 64;
+    static constexpr uint32_t K_FREE = K_FULL + 16;
+    static constexpr uint32_t A_FULL = K_FREE + 16;
+    static constexpr uint32_t Q_FULL = A_FULL + 16;
+    static constexpr uint32_t Q_FREE = Q_FULL + 8 * QST;
+    static constexpr uint32_t M_FULL = Q_FREE + 8 * QST;
+    static constexpr uint32_t M_FREE = M_FULL + 8 * MST;
+    static constexpr uint32_t S_FULL = M_FREE + 8 * MST;    // [warpgroup][buffer]
+    static constexpr uint32_t S_FREE = S_FULL + 32;
+    static constexpr uint32_t DRAIN = S_FREE + 32;
+    static constexpr uint32_t MISC = DRAIN + 8;
+    static constexpr uint32_t BYTES = MISC + 8 + 1024;
+    static_assert(BYTES + 1024 <= 228 * 1024, "shared memory of an SM");
+};
+
+struct Unit {
+    List l;
+    int kh, t0, r0, r1, split;  // head, first token, steps [r0, r1), where its parts meet
+    bool two;                   // more than 128 tokens
+};
+
+// A CTA's units: a list made by the build, or every gridDim-th one.
+struct Units {
+    int at, end, step;
+    bool listed;
+    __device__ __forceinline__ Units(const WeightParams &p, bool fits)
+    {
+        listed = p.track[TH_LISTED];
+        step = listed ? 1 : gridDim.x;
+        at = listed ? p.track[p.unit_at + blockIdx.x] : blockIdx.x;
+        end = !fits ? 0 : listed ? p.track[p.unit_at + blockIdx.x + 1] : p.track[TH_MANY_TILES] * p.kv.heads;
+    }
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ Unit get(const WeightParams &p, int per) const
+    {
+        int4 w = make_int4(at, -1, -1, -1);
+        if (listed) w = __ldg(reinterpret_cast<const int4 *>(p.track + p.unit_at + TRACK_CTAS) + at);
+        Unit u;
+        const int tile = w.x / p.kv.heads;
+        u.kh = w.x - tile * p.kv.heads;
+        u.l = load_list(p, find_list(p, p.track[TH_FEW], p.track[TH_FEW] + p.track[TH_MANY], tile));
+        u.t0 = (tile - u.l.tiles) * TRACK_MANY_TILE;
+        u.r0 = w.y >= 0 ? w.y : first_step(u.l.causal, u.l.lim, u.t0, per);
+        u.r1 = w.y >= 0 ? w.z : (u.l.ntok + per - 1) / per;
+        u.split = w.w;
+        u.two = u.l.len - u.t0 > 128;
+        return u;
+    }
+};
+
+// Widens a token's key: its row of codes to bf16, 128-byte swizzled halves of 64 elements.
+template <class L>
+__device__ __forceinline__ void widen_key(uint32_t base, int wg, int me)
+{
+    const uint32_t from = base + L::RAW + wg * L::RAW_TILE, to = base + L::A + wg * L::A_TILE;
+#pragma unroll
+    for (int c = 0; c < L::D / 16; ++c) {
+        const uint4 x = lds128(from + swz_rows<L::D>(me * L::D + c * 16));
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+        uint32_t y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t h = f16x2_of_e4m3x2((uint16_t)(w[i / 2] >> (16 * (i & 1))));
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&h));
+            const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
+            y[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        const uint32_t half = to + (c / 4) * (128 * 128);
+        sts128(half + swz128(me, (c % 4) * 2), y[0], y[1], y[2], y[3]);
+        sts128(half + swz128(me, (c % 4) * 2 + 1), y[4], y[5], y[6], y[7]);
+    }
+    fence_async_smem();
+}
+
+// The sum over columns [0, 16 n) of a thread's scores, none of which is masked.
+__device__ __forceinline__ float sum_columns(uint32_t s_at, uint32_t lse, float a, int n)
+{
+    const float2 a2 = make_float2(a, a), e2 = make_float2(LOG2E, LOG2E);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    float x[2][16];
+    tmem_ld16(s_at, *reinterpret_cast<uint32_t(*)[16]>(x[0]));
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        if (c >= n) break;
+        float (&y)[16] = x[c & 1];
+        float4 m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = lds4f(lse + 64 * c + 16 * i);
+        tmem_ld_wait();
+        if (c + 1 < 8) tmem_ld16(s_at + 16 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(x[(c + 1) & 1]));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 u = mul2(fma2(make_float2(y[4 * i], y[4 * i + 1]), a2, make_float2(m[i].x, m[i].y)), e2);
+            const float2 v = mul2(fma2(make_float2(y[4 * i + 2], y[4 * i + 3]), a2, make_float2(m[i].z, m[i].w)), e2);
+            sum[0] = add2(sum[0], make_float2(ex2(u.x), ex2(u.y)));
+            sum[1] = add2(sum[1], make_float2(ex2(v.x), ex2(v.y)));
+        }
+    }
+    tmem_ld_wait();
+    return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+}
+
+template <class L>
+__global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __grid_constant__ WeightParams p)
+{
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    const uint32_t base = smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, KV = p.kv.heads, G = p.n_heads / KV, per = 128 / G;
+    volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
+    if (tid == 0) {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(base + L::K_FULL + 8 * i, 1);
+            mbar_init(base + L::K_FREE + 8 * i, 4);
+            mbar_init(base + L::A_FULL + 8 * i, 4);
+        }
+        for (int i = 0; i < L::QST; ++i) {
+            mbar_init(base + L::Q_FULL + 8 * i, 1);
+            mbar_init(base + L::Q_FREE + 8 * i, 1);
+        }
+        for (int i = 0; i < L::MST; ++i) {
+            mbar_init(base + L::M_FULL + 8 * i, 1);
+            mbar_init(base + L::M_FREE + 8 * i, 8);
+        }
+        for (int i = 0; i < 4; ++i) {
+            mbar_init(base + L::S_FULL + 8 * i, 1);
+            mbar_init(base + L::S_FREE + 8 * i, 4);
+        }
+        mbar_init(base + L::DRAIN, 1);
+        *dead = 0;
+        mbar_fence_init();
+    }
+    if (warp == 1) {
+        tmem_alloc(base + L::MISC, L::TM_COLS);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *reinterpret_cast<uint32_t *>(sm + L::MISC);
+    pdl_wait();
+    pdl_launch_dependents();
+    const int32_t *track = after_pdl_wait(p.track);
+    const bool fits = track[TH_TOKENS] <= p.max_tok && !track[TH_SHARED];  // (the other kernel says so)
+    Units it(p, fits);
+    bool ok = true;
+    if (!it.more()) {
+    } else if (warp == 0) {
+        // ------------------------------------------------ loads: a unit's codes while the one before is under way, and its
+        // steps' queries, whole where their tokens follow each other, else token by token
+        uint32_t used[2] = {0, 0}, n = 0, st = 0, ph = 0;
+        const int page_per = 128 >> p.kv.page_log2;
+        const uint32_t q_bytes = G * 128 * (L::D / 64);
+        auto load_keys = [&](const Unit &u) {
+            for (int w = 0; w < (u.two ? 2 : 1) && ok; ++w) {
+                const int t = u.t0 + 128 * w, first = t >> p.kv.page_log2;
+                const int pages = min(page_per, ((u.l.len - 1) >> p.kv.page_log2) - first + 1);
+                int page = 0;
+                if (lane < pages) page = __ldg(p.plan + p.pages_at + u.l.pages + first + lane);
+                const int64_t row = first_row(p, page, u.kh);
+                const uint32_t full = base + L::K_FULL + 8 * w, at = lane * p.kv.page;
+                if (used[w] > 0) ok = wait_bar(base + L::K_FREE + 8 * w, (used[w] - 1) & 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) return;
+                if (lane < pages) sts32(base + L::ROWS + 32 * w + 4 * lane, (uint32_t)row);
+                __syncwarp();
+                if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * (L::D + 1));
+                __syncwarp();
+                if (lane < pages) {
+                    tma_load_2d(base + L::RAW + w * L::RAW_TILE + at * L::D, &p.kmap, 0, (int)row, full);
+                    bulk_load(base + L::EXPS + 128 * w + at, p.kv.k_exp + row, p.kv.page, full);
+                }
+                ++used[w];
+            }
+        };
+        Unit u = it.get(p, per);
+        load_keys(u);
+        while (ok && it.more()) {
+            it.at += it.step;
+            Unit v = u;
+            const bool next = it.more();
+            if (next) v = it.get(p, per);
+            for (int r = u.r0; r < u.r1; ++r, ++n) {
+                const int i0 = r * per, m = min(per, u.l.ntok - i0);
+                const int32_t *order = p.plan + p.order_at + u.l.tok + i0;
+                int tok[4];
+                bool run = true;
+                const int tok0 = __ldg(order);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int i = lane + 32 * k;
+                    tok[k] = i < m ? __ldg(order + i) : tok0 + i;
+                    run = run && tok[k] == tok0 + i;
+                }
+                run = __all_sync(0xffffffffu, run);
+                if (n >= (uint32_t)L::QST) ok = wait_bar(base + L::Q_FREE + 8 * st, ph ^ 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                const uint32_t full = base + L::Q_FULL + 8 * st, to = base + L::Q + st * L::Q_TILE;
+                if (lane == 0) mbar_expect_tx(full, (run ? per : m) * q_bytes);
+                __syncwarp();
+                if (run) {
+                    if (lane < L::D / 64) tma_load_3d(to + lane * (128 * 128), &p.qmap, 64 * lane, u.kh * G, tok0, full);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int i = lane + 32 * k;
+                        if (i < m)
+                            for (int h = 0; h < L::D / 64; ++h)
+                                tma_load_3d(to + h * (128 * 128) + i * G * 128, &p.qmap1, 64 * h, u.kh * G, tok[k], full);
+                    }
+                }
+                __syncwarp();
+                if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
+                if (r == u.r0 && next) {  // (this unit's codes are widened before its first products)
+                    load_keys(v);
+                    if (!ok) {
+                        ++n;
+                        break;
+                    }
+                }
+            }
+            u = v;
+        }
+        if (!ok) {  // copies in flight land before the CTA ends
+            if (lane == 0) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+            }
+            for (uint32_t i = 0; i < min(n, (uint32_t)L::QST); ++i) mbar_wait(base + L::Q_FULL + 8 * ((n - 1 - i) % L::QST), ((n - 1 - i) / L::QST) & 1);
+            for (int w = 0; w < 2; ++w)
+                if (used[w] > 0) mbar_wait(base + L::K_FULL + 8 * w, (used[w] - 1) & 1);
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------ MMA issue
+        const bool lead = elect_one();
+        const uint32_t id = idesc_bf16_f32(128, (per * G + 15) / 16 * 16);
+        uint32_t st = 0, ph = 0, units[2] = {0, 0}, steps[2] = {0, 0};
+        for (; it.more() && ok; it.at += it.step) {
+            const Unit u = it.get(p, per);
+            for (int r = u.r0; r < u.r1 && ok; ++r) {
+                ok = wait_bar(base + L::Q_FULL + 8 * st, ph, dead);
+                const uint64_t qd = sdesc_kmajor_sw128(base + L::Q + st * L::Q_TILE);
+#pragma unroll
+                for (int w = 0; w < 2; ++w) {
+                    if (w == 1 && !u.two) break;
+                    const uint32_t b = steps[w] & 1, s = 2 * w + b;
+                    if (r == u.r0) ok = ok && wait_bar(base + L::A_FULL + 8 * w, units[w] & 1, dead);
+                    if (steps[w] > 1) ok = ok && wait_bar(base + L::S_FREE + 8 * s, ((steps[w] >> 1) - 1) & 1, dead);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t ad = sdesc_kmajor_sw128(base + L::A + w * L::A_TILE);
+                    if (lead) {
+#pragma unroll
+                        for (int k = 0; k < L::D / 16; ++k)
+                            umma_bf16(tmem + s * 128, ad + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), qd + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), id, k > 0);
+                        umma_commit(base + L::S_FULL + 8 * s);
+                    }
+                    __syncwarp();
+                    ++steps[w];
+                }
+                if (!ok) break;
+                if (lead) umma_commit(base + L::Q_FREE + 8 * st);
+                __syncwarp();
+                if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
+            }
+            ++units[0];
+            units[1] += u.two;
+        }
+        if (!ok) {  // the products issued so far end before the CTA does
+            if (lead) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+                umma_commit(base + L::DRAIN);
+                mbar_wait(base + L::DRAIN, 0);
+            }
+            __syncwarp();
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------ the steps' log-sums, and how many tokens their rows see
+        uint32_t n = 0;
+        for (; it.more() && ok; it.at += it.step) {
+            const Unit u = it.get(p, per);
+            for (int r = u.r0; r < u.r1; ++r, ++n) {
+                const int i0 = r * per, m = min(per, u.l.ntok - i0);
+                float lse[4];
+                int lim[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int row = lane + 32 * k, i = row / G;
+                    lse[k] = 0.f;
+                    lim[k] = 0;
+                    if (i < m) {
+                        const int t = __ldg(p.plan + p.order_at + u.l.tok + i0 + i);
+                        lse[k] = -__ldg(p.lse + (int64_t)t * p.n_heads + u.kh * G + row - i * G);
+                        lim[k] = u.l.lim + (u.l.causal ? i0 + i : 0);
+                    }
+                }
+                const uint32_t s = n % L::MST, to = base + L::META + s * L::M_BUF + 4 * lane;
+                if (n >= (uint32_t)L::MST) ok = wait_bar(base + L::M_FREE + 8 * s, (n / L::MST - 1) & 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    stsf(to + L::M_LSE + 128 * k, lse[k]);
+                    sts32(to + L::M_LIM + 128 * k, (uint32_t)lim[k]);
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_release(base + L::M_FULL + 8 * s);
+            }
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------ a thread's token: its rows of scores, its weight
+        const int w = (warp - 4) >> 2, me = tid & 127;
+        const uint32_t s_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
+        uint32_t n = 0, steps = 0, units = 0;
+        float a = 0.f;
+        uint32_t at = 0;
+        // the unit's codes to bf16; its exponent and row
+        auto widen = [&]() {
+            ok = ok && wait_bar(base + L::K_FULL + 8 * w, units & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            widen_key<L>(base, w, me);
+            a = p.scale * row_scale(lds8(base + L::EXPS + 128 * w + me));
+            at = lds32(base + L::ROWS + 32 * w + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive_release(base + L::K_FREE + 8 * w);
+                mbar_arrive_release(base + L::A_FULL + 8 * w);
+            }
+            ++units;
+        };
+        Unit u = it.get(p, per);
+        if (w == 0 || u.two) widen();
+        while (ok && it.more()) {
+            it.at += it.step;
+            Unit v = u;
+            const bool next = it.more();
+            if (next) v = it.get(p, per);
+            const bool mine = w == 0 || u.two;
+            const int j = u.t0 + 128 * w + me, end = min(u.t0 + 128 * (w + 1), u.l.len);
+            const float a_now = a;
+            const uint32_t at_now = at;
+            const bool live = mine && j < u.l.len;
+            float was = 0.f, total = 0.f;
+            if (live && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
+            if (!mine && next && v.two) widen();
+            for (int r = u.r0; r < u.r1; ++r, ++n) {
+                const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF, b = steps & 1, s = 2 * w + b;
+                ok = ok && wait_bar(base + L::M_FULL + 8 * ms, (n / L::MST) & 1, dead);
+                if (mine) ok = ok && wait_bar(base + L::S_FULL + 8 * s, (steps >> 1) & 1, dead);
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
+                if (mine) {
+                    tc_fence_after();
+                    // (the unit's last products are done: the next unit's may begin beside this step's sums)
+                    if (r + 1 == u.r1 && next && (w == 0 || v.two)) {
+                        widen();
+                        if (!ok) break;
+                    }
+                    const int i0 = r * per, cols = min(per, u.l.ntok - i0) * G;
+                    const int full = u.l.causal && end > u.l.lim + i0 ? 0 : cols / 16;
+                    const uint32_t s_at = s_base + b * 128;
+                    float sum = full ? sum_columns(s_at, meta + L::M_LSE, a_now, full) : 0.f;
+#pragma unroll 1
+                    for (int c = 16 * full; c < cols; c += 4) {
+                        float x[4];
+                        tmem_ld4(s_at + c, reinterpret_cast<uint32_t *>(x));
+                        const float4 l = lds4f(meta + L::M_LSE + 4 * c);
+                        const uint4 lim = lds128(meta + L::M_LIM + 4 * c);
+                        tmem_ld_wait();
+                        const float m[4] = {l.x, l.y, l.z, l.w};
+                        const int see[4] = {(int)lim.x, (int)lim.y, (int)lim.z, (int)lim.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float e = ex2(fmaf(x[i], a_now, m[i]) * LOG2E);
+                            if (j < see[i]) sum += e;
+                        }
+                    }
+                    total += sum;
+                    tc_fence_before();
+                    ++steps;
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    if (mine) mbar_arrive_release(base + L::S_FREE + 8 * s);
+                    mbar_arrive_release(base + L::M_FREE + 8 * ms);
+                }
+            }
+            if (!ok) break;
+            if (mine && u.split < 0) {
+                if (live) p.weights[at_now] = was + total;
+            } else if (mine) {
+                // the warp that comes last adds up the parts, in their order
+                const int parts = (u.split & 63) + 1, part = (u.split >> 6) & 63, slot = u.split >> 12;
+                float *mine_at = p.part + (int64_t)slot * TRACK_MANY_TILE + w * 128 + me;
+                __stcg(mine_at + part * TRACK_MANY_TILE, total);
+                __threadfence();
+                __syncwarp();
+                uint32_t *count = p.arrived + slot * 8 + (warp - 4);
+                int before = 0;
+                if (lane == 0) before = (int)atomicAdd(count, 1u);
+                before = __shfl_sync(0xffffffffu, before, 0);
+                if (before + 1 == parts) {
+                    __threadfence();
+                    total = 0.f;
+                    for (int i = 0; i < parts; ++i) total += __ldcg(mine_at + i * TRACK_MANY_TILE);
+                    if (live) p.weights[at_now] = was + total;
+                    if (lane == 0) *count = 0;
+                }
+            }
+            u = v;
+        }
+        if (!ok && lane == 0) {
+            *dead = 1;
+            atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                 CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeTiled>(f) : nullptr;
+    }();
+    return fn;
+}
+
+// Queries as [tokens][heads][D] bf16, a box 64 elements of a group's heads of `box_tokens` tokens.
+cudaError_t encode_queries(CUtensorMap *out, const void *q, int64_t stride, int dim, int heads, int tokens, int G, int box_tokens)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return cudaErrorNotSupported;
+    const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens};
+    const cuuint64_t strides[2] = {(cuuint64_t)dim * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)G, (cuuint32_t)box_tokens}, es[3] = {1, 1, 1};
+    const CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box, es,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+template <int D>
+cudaError_t launch_weights(WeightParams &p, int n_sm, bool many, bool few, int64_t few_tiles, cudaStream_t stream)
+{
+    using F = Few<D>;
+    using M = Many<D>;
+    cudaError_t e = cudaSuccess;
+    if (many) {
+        e = cudaFuncSetAttribute(weights_many_kernel<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
+        if (e == cudaSuccess) e = launch_overlapped(weights_many_kernel<M>, n_sm, M::THREADS, M::BYTES, stream, p);
+        if (e != cudaSuccess) return e;
+    }
+    if (!few) return cudaSuccess;
+    p.behind = many;
+    e = cudaFuncSetAttribute(weights_few_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(weights_few_kernel<F>, (unsigned)std::min<int64_t>(n_sm * F::CTAS, few_tiles), F::THREADS, F::BYTES, stream, p);
 }
 
 }  // namespace
@@ -143,6 +921,7 @@ try {
     if (!a) return SALT_ERR_INVALID_ARG;
     salt_ctx *ctx = a->kv->ctx;
     const KvDev &kv = a->kv->dev;
+    const Track &tr = a->track;
     if (!std::isfinite(scale) || !std::isfinite(decay)) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "scale or decay is not finite");
     if (a->built && a->T > 0) {
         if (!q || !lse || !weights) return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "null q, lse or weights");
@@ -154,27 +933,40 @@ try {
     cudaStream_t stream = static_cast<cudaStream_t>(stream_);
     bool captured;
     const salt_status st = track_enter(a, layer, 1, stream, &captured);
-    if (st != SALT_OK || (a->track.n_lists == 0 && !captured)) return st;
+    if (st != SALT_OK) return st;
+    // a captured call may be replayed for a batch that needs the other kernel (none with more query tokens)
+    const bool many = a->T > 0 && (captured || tr.many > 0), few = captured || tr.few > 0;
+    if (!many && !few) return SALT_OK;
     WeightParams p;
+    p.kmap = a->kmap;
+    if (many) {
+        const int G = a->cfg.n_heads / kv.heads;
+        SALT_CUDA_OR_FAIL(ctx, encode_queries(&p.qmap, q, q_stride, kv.dim, a->cfg.n_heads, a->T, G, 128 / G));
+        SALT_CUDA_OR_FAIL(ctx, encode_queries(&p.qmap1, q, q_stride, kv.dim, a->cfg.n_heads, a->T, G, 1));
+    }
     p.plan = a->plan;
-    p.track = a->track.table;
+    p.track = tr.table;
     p.order_at = a->order_at;
     p.pages_at = a->pages_at;
-    p.list_at = a->track.list_at;
+    p.list_at = tr.list_at;
+    p.unit_at = tr.unit_at;
     p.kv = kv;
     p.layer = layer;
     p.q = static_cast<const uint16_t *>(q);
     p.lse = lse;
     p.weights = weights;
+    p.part = tr.part;
+    p.arrived = tr.arrived;
     p.q_stride = q_stride;
     p.n_heads = a->cfg.n_heads;
     p.max_tok = a->T;
+    p.behind = 0;
     p.scale = scale;
     p.decay = decay;
     p.err = ctx_error_word(ctx);
-    const auto kernel = kv.dim == 128 ? weights_kernel<128> : weights_kernel<64>;
-    kernel<<<a->n_sm * 3, TRACK_TILE, 0, stream>>>(p);
-    SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+    const int64_t tiles = captured ? 1 << 30 : tr.few_tiles * kv.heads;
+    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_weights<128>(p, a->n_sm, many, few, tiles, stream)
+                                         : launch_weights<64>(p, a->n_sm, many, few, tiles, stream));
     return SALT_OK;
 } catch (const std::bad_alloc &) {
     return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");

@@ -347,3 +347,51 @@ def test_refusals(salt_lib, ctx):
     salt_lib.salt_attn_weights(plan, 0, q[:0], lse[:0], 0.1, x)
     torch.cuda.synchronize()
     assert torch.equal(x, before) and salt_lib.salt_get_device_error(ctx) == 0
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("n,kv,prompt,heads,kv_heads", [(700, 900, 0, 8, 1), (1500, 1500, 300, 2, 2), (333, 5000, 64, 3, 1)])
+def test_rows_of_a_tile_split(salt_lib, ctx, n, kv, prompt, heads, kv_heads, dim):
+    """Few tiles of many rows: parts of a unit's rows meet, the same each time; on the GPU in 64 bits."""
+    page = 64
+    lens = [prompt, kv]
+    need = [-(-x // page) for x in lens]
+    order = torch.randperm(sum(need) + 1).tolist()
+    shape = (1, len(order), kv_heads, page, dim)
+    k = torch.randint(0, 0x70, shape, dtype=torch.uint8, device="cuda") | (torch.rand(shape, device="cuda") < 0.5).to(torch.uint8) * 128
+    e = torch.randint(117, 121, shape[:4], dtype=torch.uint8, device="cuda")
+    cache = salt_lib.salt_kv_create(ctx, k, k, e, e)
+    plan = salt_lib.salt_attn_create(cache, heads, 1, n, sum(need), 1)
+    salt_lib.salt_attn_track(plan)
+    salt_lib.salt_attn_build(plan, salt_lib.salt_attn_batch([n], [kv], [0, need[1]], order[need[0]:sum(need)], [0], [prompt], [0, need[0]], order[:need[0]]))
+    q = torch.randn((n, heads, dim), device="cuda").bfloat16()
+    out, lse = torch.empty_like(q), torch.empty((n, heads), device="cuda")
+    salt_lib.salt_attn_run(plan, 0, q, out, dim ** -0.5, lse)
+    w = torch.full(shape[:4], 0.5, device="cuda")
+    w[0, order[-1]] = math.nan   # not in the batch
+    first = w.clone()
+    salt_lib.salt_attn_weights(plan, 0, q, lse, dim ** -0.5, first, 0.5)
+    for _ in range(3):
+        again = w.clone()
+        salt_lib.salt_attn_weights(plan, 0, q, lse, dim ** -0.5, again, 0.5)
+        assert torch.equal(again[0, order[:-1]], first[0, order[:-1]])
+    assert salt_lib.salt_get_device_error(ctx) == 0 and bool(first[0, order[-1]].isnan().all())
+    K = k[0].view(torch.float8_e4m3fn).double() * torch.exp2(e[0].double() - 127)[..., None]
+    x = q.double().view(n, kv_heads, heads // kv_heads, dim)
+    ls = lse.double().view(n, kv_heads, -1).permute(1, 2, 0)[:, None]
+    for own in (False, True):
+        m, pages = (kv, order[need[0]:sum(need)]) if own else (prompt, order[:need[0]])
+        if m == 0:
+            continue
+        Kl = K[torch.tensor(pages, device="cuda")].transpose(1, 2).reshape(-1, kv_heads, dim)[:m]
+        s = torch.einsum("rkgd,nkd->kngr", x, Kl) * dim ** -0.5
+        j = torch.arange(m, device="cuda")
+        see = j[:, None] <= kv - n + torch.arange(n, device="cuda") if own else torch.ones((m, n), dtype=torch.bool, device="cuda")
+        p = torch.exp(s - ls) * see[None, :, None]
+        ds = (Kl.abs().sum(-1).T[:, :, None, None] * x.abs().amax(-1).permute(1, 2, 0)[:, None] * 2.0 ** -22
+              + torch.einsum("rkgd,nkd->kngr", x.abs(), Kl.abs()) * dim * 2.0 ** -23) * dim ** -0.5 + (s.abs() + ls.abs()) * 2.0 ** -21 + 2.0 ** -20
+        tol = (p * (torch.expm1(ds) + n * heads // kv_heads * 2.0 ** -24)).sum((2, 3)).T + 2.0 ** -22
+        want = p.sum((2, 3)).T + torch.where((j < kv - n)[:, None] if own else torch.ones((m, 1), dtype=torch.bool, device="cuda"), 0.25, 0.0)
+        got = first[0][torch.tensor(pages, device="cuda")].transpose(1, 2).reshape(-1, kv_heads)
+        assert bool(((got[:m].double() - want).abs() <= tol).all())
+        assert bool((got[m:] == 0.5).all())
