@@ -1597,6 +1597,7 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
     tr.page_seen.assign(kv.n_pages, 0);
     tr.shared = false;
+    tr.longest = tr.chunks = 0;
     auto note = [&](const int32_t *pages, int len) {
         for (int j = 0; j < (int)(((int64_t)len + kv.page - 1) >> kv.page_log2); ++j) {
             tr.shared |= tr.page_seen[pages[j]] != 0;
@@ -1620,6 +1621,10 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
         int32_t *s = t + tr.seq_at + (size_t)i * SEQ_WORDS;
         s[0] = b->page_ptr[i];
         s[1] = b->kv_len[i];
+        s[2] = tr.chunks;
+        s[3] = 0;
+        tr.longest = std::max(tr.longest, b->kv_len[i]);
+        tr.chunks += b->kv_len[i] / evict_rows(kv.dim) + 1;
         note(b->pages + b->page_ptr[i], b->kv_len[i]);
         // (a request of more query than cached tokens: the first rows see nothing)
         add(b->page_ptr[i], b->kv_len[i], t0, b->q_len[i], std::max(0, b->kv_len[i] - b->q_len[i]), b->kv_len[i] - b->q_len[i] + 1, true);
@@ -1789,9 +1794,7 @@ void salt_attn_destroy(salt_attn *a)
     cudaFree(a->plan);
     cudaFree(a->part_o);
     cudaFree(a->part_l);
-    cudaFree(a->track.table);
-    cudaFree(a->track.part);
-    cudaFree(a->track.arrived);
+    a->track.free_device();
     for (int i = 0; i < 2; ++i) {
         if (a->track.staging[i]) cudaFreeHost(a->track.staging[i]);
         if (a->staging[i]) cudaFreeHost(a->staging[i]);
@@ -1861,15 +1864,17 @@ salt_status salt_attn_track(salt_attn *a)
     bool ok = cudaMalloc(&t.table, t.words * 4) == cudaSuccess &&
               cudaMalloc(&t.part, (size_t)TRACK_SLOTS * TRACK_MANY_TILE * 4) == cudaSuccess &&
               cudaMalloc(&t.arrived, TRACK_SLOTS * 8 * 4) == cudaSuccess && cudaMemset(t.arrived, 0, TRACK_SLOTS * 8 * 4) == cudaSuccess;
+    // eviction's chunks of a layer; those of more layers at a time up to some memory
+    const KvDev &kv = a->kv->dev;
+    const int64_t chunks = std::min<int64_t>((int64_t)a->cfg.max_pages, kv.n_pages) * kv.page / evict_rows(kv.dim) + a->cfg.max_seqs, layer = chunks * kv.heads;
+    t.chunks_cap = (int)chunks;
+    t.layers_cap = (int)std::min<int64_t>(a->kv->n_layers, std::max<int64_t>(1, (1 << 22) / layer));
+    ok = ok && cudaMalloc(&t.chunk_ptr, ((size_t)a->cfg.max_seqs + 1) * 4) == cudaSuccess && cudaMalloc(&t.ticket, 4) == cudaSuccess &&
+         cudaMalloc(&t.bound, (size_t)layer * t.layers_cap * 4) == cudaSuccess && cudaMalloc(&t.read, (size_t)layer * t.layers_cap * 4) == cudaSuccess;
     for (int i = 0; i < 2 && ok; ++i) ok = cudaHostAlloc(reinterpret_cast<void **>(&t.staging[i]), t.words * 4, cudaHostAllocMapped) == cudaSuccess;
     if (!ok) {
         cudaGetLastError();
-        cudaFree(t.table);
-        cudaFree(t.part);
-        cudaFree(t.arrived);
-        t.table = nullptr;
-        t.part = nullptr;
-        t.arrived = nullptr;
+        t.free_device();
         for (int32_t *&s : t.staging) {
             if (s) cudaFreeHost(s);
             s = nullptr;

@@ -20,7 +20,8 @@ constexpr int TRACK_HEAD = 8;   // TH_* below
 // query tokens, requests, lists of few rows, whether a page is listed twice, tiles of 128 tokens of those lists, lists of many rows (behind the others),
 // tiles of 256 tokens of those, whether the units of their work are listed
 constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_TILES = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7;
-constexpr int SEQ_WORDS = 2;    // per request: first entry in the page lists, own cached tokens
+// per request: first entry in the page lists, own cached tokens, first entry in the tables of eviction's chunks, none
+constexpr int SEQ_WORDS = 4;
 // per list of cached tokens that rows see, a request's own or a group's prompt: first entry in the page lists, tokens, first
 // entry in the token order, query tokens, tokens that were there before the step, tokens that the first query token sees,
 // whether the next ones each see one more, tiles of the lists of its kind before
@@ -32,6 +33,8 @@ constexpr int TRACK_FEW_ROWS = 16;
 // first part << 12 | part << 6 | parts - 1) or -1
 constexpr int TRACK_CTAS = 512, UNIT_WORDS = 4, TRACK_UNITS = 8192;
 constexpr int TRACK_SLOTS = 2048;  // of partial sums, 256 tokens each
+// Rows that eviction moves at a time: 16 KB of keys and values.
+constexpr int evict_rows(int dim) { return 8192 / dim; }
 // The first step of `per` query tokens that sees token t0.
 __host__ __device__ constexpr int first_step(bool causal, int lim, int t0, int per)
 {
@@ -48,7 +51,19 @@ struct Track {
     bool on = false, built = false, shared = false, split = false;
     int n_seqs = 0, few = 0, many = 0;
     int64_t few_tiles = 0;
+    // eviction's: the longest request, chunks of all requests in the build; room for chunks and layers; tables
+    int longest = 0, chunks = 0, chunks_cap = 0, layers_cap = 0;
+    int32_t *chunk_ptr = nullptr, *bound = nullptr;
+    uint32_t *read = nullptr, *ticket = nullptr;
     std::vector<uint8_t> page_seen;            // scratch of a build
+
+    void free_device()
+    {
+        for (void *x : {(void *)table, (void *)part, (void *)arrived, (void *)chunk_ptr, (void *)bound, (void *)read, (void *)ticket}) cudaFree(x);
+        table = chunk_ptr = bound = nullptr;
+        part = nullptr;
+        arrived = read = ticket = nullptr;
+    }
 };
 
 __device__ __forceinline__ float ex2(float x)

@@ -4,10 +4,12 @@
 //
 // Kept are the last `recent` tokens, the first `first` ones, and of the others those of
 // the largest scores, ties to the earlier one.  Scores are ordered as unsigned
-// words; a search by digits from the top finds the last score that is kept and how many of its ties.
+// words; a search by digits from the top, 11, 11 and 10 bits, finds the last word that is kept and how many of its
+// ties are.
 //
-// A kept token's new place is never behind its old one, so rows move in place: place i is written once what lies
-// there was read, and that belongs to the i-th kept token or an earlier one.
+// A kept token's new place is never behind its old one, so rows move in place: a place may be written once what lies
+// there was read.  Rows move in chunks, each by a CTA that reads its chunk, says so, waits for the chunks that read what it will
+// write over (two of those before it at most: they have as many rows as it has places) and writes.
 #include <algorithm>
 #include <new>
 
@@ -20,7 +22,8 @@
 namespace salt {
 namespace {
 
-constexpr int SELECT_THREADS = 1024, MOVE_THREADS = 256;
+constexpr int DIGITS = 3, BINS = 2048;
+constexpr int digit_shift(int d) { return d == 0 ? 21 : d == 1 ? 10 : 0; }
 
 struct EvictParams {
     const int32_t *plan, *track;
@@ -33,8 +36,15 @@ struct EvictParams {
     int32_t *kept;              // [layers][requests][heads][kept_stride]
     int64_t kept_stride;
     int32_t n_seqs, first, recent;
+    // the plan's workspace: per request the chunks of those before it, per line and chunk how many kept tokens lie before the chunk's
+    // first place and whether its rows were read, the next chunk to move
+    int32_t *chunk_ptr, *bound;
+    uint32_t *read, *ticket;
+    int32_t chunks;             // entries of all requests, for one layer and head
+    int32_t key_cap;            // keys of a CTA that its shared memory holds
     uint32_t *err;
 };
+constexpr int EVICT_POLLS = 1 << 20;  // of a chunk for another's rows (a fraction of a second)
 
 // One layer's, request's and head's own tokens.
 struct Line {
@@ -42,28 +52,30 @@ struct Line {
     int64_t page0;              // number of the layer's first page
     int head, len, keep, first, recent;
     int32_t *kept;
+    int64_t chunk0;             // its first entry in the chunks' tables
 };
 
-// The line's b-th in the launch; keep is 0 where there is nothing to do.
-__device__ __forceinline__ Line load_line(const EvictParams &p, int b)
+// How many tokens of a request are kept where some go; 0 where none do, or none may stay (-1: not allowed).
+__device__ __forceinline__ int kept_of(const EvictParams &p, int seq, int len)
 {
-    const int KV = p.kv.heads;
-    const int head = b % KV, seq = b / KV % p.n_seqs, layer = b / KV / p.n_seqs;
-    const int2 s = __ldg(reinterpret_cast<const int2 *>(p.track + p.seq_at) + seq);
+    const int keep = __ldg(p.keep + seq);
+    return keep < 0 || keep > p.kept_stride ? -1 : keep < len ? keep : 0;
+}
+// lh: layer in the launch * heads + head
+__device__ __forceinline__ Line load_line(const EvictParams &p, int lh, int seq)
+{
+    const int layer = lh / p.kv.heads;
+    const int4 s = __ldg(reinterpret_cast<const int4 *>(p.track + p.seq_at) + seq);
     Line l;
+    l.head = lh - layer * p.kv.heads;
     l.pages = p.plan + p.pages_at + s.x;
     l.page0 = (p.layer + layer) * p.kv.n_pages;
-    l.head = head;
     l.len = s.y;
-    l.keep = __ldg(p.keep + seq);
-    l.kept = p.kept + (int64_t)b * p.kept_stride;
-    if (l.keep < 0 || l.keep > p.kept_stride) {
-        if (head == 0 && layer == 0 && threadIdx.x == 0) atomicOr(p.err, SALT_DEVERR_KEEP);
-        l.keep = 0;
-    }
-    if (l.keep >= l.len) l.keep = 0;
+    l.keep = max(kept_of(p, seq, l.len), 0);
+    l.kept = p.kept + (((int64_t)layer * p.n_seqs + seq) * p.kv.heads + l.head) * p.kept_stride;
     l.recent = min(p.recent, l.keep);
     l.first = min(p.first, l.keep - l.recent);
+    l.chunk0 = (int64_t)lh * p.chunks + s.z;
     return l;
 }
 __device__ __forceinline__ int64_t row_of(const EvictParams &p, const Line &l, int j)
@@ -107,94 +119,520 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t x, uint32_t *s_warp, uin
     return sum + (warp ? s_warp[warp - 1] : 0u);
 }
 
-__global__ void __launch_bounds__(SELECT_THREADS) evict_select_kernel(const EvictParams p)
+// A word of another CTA of the cluster.
+__device__ __forceinline__ uint32_t peer_word(uint32_t addr, uint32_t rank)
 {
-    __shared__ uint32_t s_hist[256], s_warp[32], s_found[2];
-    if (p.track[TH_SEQS] > p.n_seqs || p.track[TH_SHARED]) {
-        if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
+    uint32_t at, v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.u32 %0, [%1];\n" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync(uint32_t n)
+{
+    if (n == 1) {
+        __syncthreads();
         return;
     }
-    if (blockIdx.x / p.kv.heads % p.n_seqs >= p.track[TH_SEQS]) return;
-    const Line l = load_line(p, blockIdx.x);
-    if (l.keep == 0) return;
-    const int tid = threadIdx.x, from = l.first, to = l.len - l.recent;
-    uint32_t want = l.keep - l.first - l.recent, prefix = 0;
-    // the smallest key that is kept, and `want` of those that are equal to it
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        if (tid < 256) s_hist[tid] = 0;
-        __syncthreads();
-        for (int j = from + tid; j < to; j += SELECT_THREADS) {
-            const uint32_t key = key_of(__ldg(p.scores + row_of(p, l, j)));
-            if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&s_hist[(key >> shift) & 255], 1);
+    cluster_arrive();
+    cluster_wait();
+}
+
+// The places of a line's kept tokens, by a cluster, each CTA a run of the line's tokens, each warp a run of those.
+template <int THREADS, int ROWS>
+__global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_constant__ EvictParams p)
+{
+    constexpr int WARPS = THREADS / 32, PER = BINS / THREADS;
+    extern __shared__ __align__(16) uint32_t s_keys[];
+    __shared__ __align__(16) uint32_t s_hist[DIGITS][BINS], s_warp[32], s_found[2], s_held[WARPS], s_tied[WARPS], s_all[2];
+    pdl_wait();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_seqs = p.track[TH_SEQS];
+    uint32_t C, rank;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(C));
+    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    const bool fits = n_seqs <= p.n_seqs && !p.track[TH_SHARED];
+    if (blockIdx.x == 0) {  // the chunks of every request, once for all layers and heads
+        int before = 0;
+        for (int s0 = 0; fits && s0 < n_seqs; s0 += THREADS) {
+            const int s = s0 + tid, keep = s < n_seqs ? kept_of(p, s, __ldg(p.track + p.seq_at + s * SEQ_WORDS + 1)) : 0;
+            if (keep < 0) atomicOr(p.err, SALT_DEVERR_KEEP);
+            uint32_t all;
+            const uint32_t n = (max(keep, 0) + ROWS - 1) / ROWS, up_to = block_scan(n, s_warp, &all);
+            if (s < n_seqs) p.chunk_ptr[s + 1] = before + (int)up_to;
+            before += (int)all;
         }
-        __syncthreads();
-        // from the largest digit down
-        uint32_t total;
-        const uint32_t n = tid < 256 ? s_hist[255 - tid] : 0u, up_to = block_scan(n, s_warp, &total);
-        if (n > 0 && up_to >= want && up_to - n < want) {
-            s_found[0] = 255 - tid;
-            s_found[1] = want - (up_to - n);
+        if (tid == 0) {
+            p.chunk_ptr[0] = 0;
+            p.ticket[0] = 0;
+            if (!fits) atomicOr(p.err, SALT_DEVERR_BATCH);
         }
-        __syncthreads();
-        prefix = prefix << 8 | s_found[0];
-        want = s_found[1];
-        __syncthreads();
     }
-    const bool any = l.keep > l.first + l.recent;
-    uint32_t ties = 0, out = 0;  // so far
-    for (int j0 = 0; j0 < l.len; j0 += SELECT_THREADS) {
-        const int j = j0 + tid;
-        bool held = j < l.len && (j < from || j >= to), tie = false;
-        if (any && j >= from && j < to) {
-            const uint32_t key = key_of(__ldg(p.scores + row_of(p, l, j)));
-            held = key > prefix;
-            tie = key == prefix;
+    const int line = blockIdx.x / C, lh = line / p.n_seqs, seq = line - lh * p.n_seqs;
+    if (!fits || seq >= n_seqs) return;  // (the cluster together)
+    const Line l = load_line(p, lh, seq);
+    if (l.keep == 0) return;
+    const int from = l.first, to = l.len - l.recent;
+    const int warp_run = ((l.len + (int)C * WARPS - 1) / ((int)C * WARPS) + 31) & ~31, cta0 = (int)rank * WARPS * warp_run, warp0 = cta0 + warp * warp_run;
+    const int cta1 = min(l.len, cta0 + WARPS * warp_run), warp1 = min(l.len, warp0 + warp_run);
+    for (int i = tid; i < DIGITS * BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(s_hist[0])[i] = make_uint4(0, 0, 0, 0);
+    for (int c = (int)rank * THREADS + tid; c * ROWS < l.keep; c += (int)C * THREADS) p.read[l.chunk0 + c] = 0;
+    __syncthreads();
+    uint32_t want = l.keep - l.first - l.recent, prefix = 0;
+    const bool any = want > 0;
+    // A warp goes over its run 128 tokens at a time, four of a page a lane.
+    auto fetch = [&](int j) {
+        const float4 x = __ldg(reinterpret_cast<const float4 *>(p.scores + row_of(p, l, j)));
+        return make_uint4(key_of(x.x), key_of(x.y), key_of(x.z), key_of(x.w));
+    };
+    // (key_cap is a multiple of 4)
+    auto keys_at = [&](int j) { return j >= warp1 ? make_uint4(0, 0, 0, 0) : j - cta0 < p.key_cap ? *reinterpret_cast<const uint4 *>(s_keys + (j - cta0)) : fetch(j); };
+    // counts the keys whose digits above the d-th are `prefix`
+    auto count = [&](int d, int j, const uint4 &x) {
+        const uint32_t key[4] = {x.x, x.y, x.z, x.w};
+        const int above = digit_shift(d) + (d == 2 ? 10 : 11);
+        uint32_t bin[4], all = 0, same = 0;
+        bool in[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            in[i] = j + i >= from && j + i < to && j + i < warp1 && (d == 0 || key[i] >> above == prefix);
+            bin[i] = key[i] >> digit_shift(d) & (d == 2 ? 1023u : 2047u);
+            all += in[i];
         }
-        uint32_t total;
-        const uint32_t rank = block_scan(tie, s_warp, &total) - tie + ties;
-        ties += total;
-        held |= tie && rank < want;
-        const uint32_t at = block_scan(held, s_warp, &total) - held + out;
-        out += total;
-        if (held) l.kept[at] = j;
+        // (equal scores are common: a lane's, and a warp's, count as one)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) same += in[i] && bin[i] == bin[0] && in[0];
+        const uint32_t on = __ballot_sync(0xffffffffu, all > 0);
+        if (on == 0) return;
+        const uint32_t lead = __shfl_sync(0xffffffffu, bin[0], 0);
+        if (__all_sync(0xffffffffu, same == 4 && bin[0] == lead)) {
+            if (lane == 0) atomicAdd(&s_hist[d][bin[0]], 128u);
+        } else if (all > 0 && same == all) {
+            atomicAdd(&s_hist[d][bin[0]], all);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (in[i]) atomicAdd(&s_hist[d][bin[i]], 1u);
+        }
+    };
+    if (any) {
+        constexpr int AHEAD = 4;  // groups under way
+        for (int j0 = warp0; j0 < warp1; j0 += 128 * AHEAD) {
+            uint4 x[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int j = j0 + 128 * k + 4 * lane;
+                x[k] = make_uint4(0, 0, 0, 0);
+                if (j < warp1) x[k] = fetch(j);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int j = j0 + 128 * k + 4 * lane;
+                if (j0 + 128 * k >= warp1) break;
+                if (j < warp1 && j - cta0 < p.key_cap) *reinterpret_cast<uint4 *>(s_keys + (j - cta0)) = x[k];
+                count(0, j, x[k]);
+            }
+        }
+    }
+    for (int d = 0; d < DIGITS && any; ++d) {
+        if (d > 0)
+            for (int j0 = warp0; j0 < warp1; j0 += 128) count(d, j0 + 4 * lane, keys_at(j0 + 4 * lane));
+        cluster_sync(C);
+        // from the largest digit down: a thread has PER of them
+        uint32_t n[PER], sum = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int bin = BINS - 1 - (tid * PER + i);
+            n[i] = 0;
+            if (C == 1) {
+                n[i] = s_hist[d][bin];
+            } else {
+#pragma unroll
+                for (uint32_t r = 0; r < 8; ++r)
+                    if (r < C) n[i] += peer_word(smem_u32(&s_hist[d][bin]), r);
+            }
+            sum += n[i];
+        }
+        uint32_t all, before = block_scan(sum, s_warp, &all) - sum;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (before < want && before + n[i] >= want) {
+                s_found[0] = BINS - 1 - (tid * PER + i);
+                s_found[1] = want - before;
+            }
+            before += n[i];
+        }
+        __syncthreads();
+        prefix = prefix << (d == 2 ? 10 : 11) | s_found[0];
+        want = s_found[1];
+        // (s_found is written again behind the next barriers)
+    }
+    // a lane's tokens that are kept whatever the ties, and those that tie with the last one that is kept, a bit each
+    auto sort_out = [&](int j, uint32_t &h, uint32_t &t) {
+        const uint4 x = any ? keys_at(j) : make_uint4(0, 0, 0, 0);
+        const uint32_t key[4] = {x.x, x.y, x.z, x.w};
+        h = t = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = j + i >= from && j + i < to;
+            if (j + i < warp1) {
+                h |= (uint32_t)(!in || (any && key[i] > prefix)) << i;
+                t |= (uint32_t)(in && any && key[i] == prefix) << i;
+            }
+        }
+    };
+    uint32_t held = 0, tied = 0;
+    for (int j0 = warp0; j0 < warp1; j0 += 128) {
+        uint32_t h, t;
+        sort_out(j0 + 4 * lane, h, t);
+        held += __popc(h);
+        tied += __popc(t);
+    }
+    held = __reduce_add_sync(0xffffffffu, held);
+    tied = __reduce_add_sync(0xffffffffu, tied);
+    if (lane == 0) {
+        s_held[warp] = held;
+        s_tied[warp] = tied;
+    }
+    __syncthreads();
+    uint32_t held0 = lane < warp ? s_held[lane] : 0u, tied0 = lane < warp ? s_tied[lane] : 0u;
+    held0 = __reduce_add_sync(0xffffffffu, held0);
+    tied0 = __reduce_add_sync(0xffffffffu, tied0);
+    if (C > 1) {
+        if (warp == WARPS - 1 && lane == 0) {
+            s_all[0] = held0 + held;
+            s_all[1] = tied0 + tied;
+        }
+        cluster_sync(C);
+#pragma unroll
+        for (uint32_t r = 0; r < 8; ++r)
+            if (r < rank) {
+                held0 += peer_word(smem_u32(&s_all[0]), r);
+                tied0 += peer_word(smem_u32(&s_all[1]), r);
+            }
+        cluster_arrive();  // (nobody leaves while its words are read)
+    }
+    pdl_launch_dependents();
+    const uint32_t below = (1u << lane) - 1u;
+    uint32_t out0 = held0 + min(tied0, want);  // kept before the warp's run
+    for (int j0 = warp0; j0 < warp1; j0 += 128) {
+        const int j = j0 + 4 * lane;
+        uint32_t h, t;
+        sort_out(j, h, t);
+        uint32_t ties = 0, ties_here = 0, on = 0, on_here = 0;  // of the lanes before, of all
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __ballot_sync(0xffffffffu, t >> i & 1);
+            ties += __popc(x & below);
+            ties_here += __popc(x);
+        }
+        // the first `want` ties are kept
+        uint32_t rank_t = tied0 + ties;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t >> i & 1) h |= (uint32_t)(rank_t++ < want) << i;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __ballot_sync(0xffffffffu, h >> i & 1);
+            on += __popc(x & below);
+            on_here += __popc(x);
+        }
+        uint32_t out = out0 + on;
+        if (j % ROWS == 0 && j < l.keep + ROWS && j < warp1) p.bound[l.chunk0 + j / ROWS] = (int)out;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (h >> i & 1) l.kept[out++] = j + i;
+        out0 += on_here;
+        tied0 += ties_here;
+    }
+    if (C > 1) cluster_wait();
+}
+
+// Chunks are taken in their order, so that those that a chunk waits for are under way.  A CTA has some of them in slots of its shared
+// memory, and its warps deal with them in turn: one looks up the rows' places, some read the keys and values, one the exponents and weights,
+// one says when all are there, one waits for the chunks that read what this one will write over, some write.  Reading
+// runs ahead of writing by all the slots, whatever writing waits for.  (Where a chunk was read only once the one before it was written, chunks
+// waited for each other in long chains, 7 us each.)  The flags between CTAs carry no data and need no fence: a chunk's words
+// are in shared memory, not on their way, when its flag is written, and no store is made before the flag that allows it was read.
+constexpr int SLOTS = 5, LOAD_WARPS = 4, STORE_WARPS = 4, MOVE_THREADS = 32 * (LOAD_WARPS + STORE_WARPS + 4);
+
+template <int D_, int ROWS_>
+struct Move {
+    static constexpr int D = D_, ROWS = ROWS_;
+    static constexpr int LPR = D / 16;                                    // lanes a row
+    static constexpr uint32_t K = 0, V = ROWS * D, W = 2 * ROWS * D;      // a slot: keys, values, weights,
+    static constexpr uint32_t E = W + 4 * ROWS;                           // exponents of k and v,
+    static constexpr uint32_t SRC = E + 2 * ROWS, DST = SRC + 4 * ROWS;   // old and new rows (new -1: stays)
+    static constexpr uint32_t SLOT = DST + 4 * ROWS;
+    static constexpr uint32_t BYTES = SLOTS * SLOT;
+    static_assert(SLOT % 16 == 0 && 2 * (BYTES + 2048) <= 228 * 1024, "two CTAs an SM");
+};
+
+template <class M>
+__global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __grid_constant__ EvictParams p, int layers)
+{
+    constexpr int D = M::D, ROWS = M::ROWS;
+    extern __shared__ __align__(16) uint8_t s_slots[];
+    __shared__ __align__(8) uint64_t s_full[SLOTS], s_free[SLOTS], s_read[SLOTS], s_clear[SLOTS];
+    __shared__ int64_t s_chunk[SLOTS];     // the chunk's entry, -1: no more
+    __shared__ int32_t s_wait[SLOTS][2];   // the first and last chunk of the line that it waits for, from here
+    __shared__ int s_dead;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    volatile int *dead = &s_dead;
+    if (tid == 0) {
+        for (int i = 0; i < SLOTS; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_free[i]), STORE_WARPS + 2);
+            mbar_init(smem_u32(&s_read[i]), 32 * LOAD_WARPS + 1);
+            mbar_init(smem_u32(&s_clear[i]), 1);
+        }
+        s_dead = 0;
+        mbar_fence_init();
+    }
+    __syncthreads();
+    pdl_wait();
+    pdl_launch_dependents();
+    const int n_seqs = p.track[TH_SEQS];
+    if (n_seqs > p.n_seqs || p.track[TH_SHARED]) return;
+    bool ok = true;
+    auto wait = [&](uint64_t *bars, uint32_t n) {  // for the n-th use of its slot
+        ok = ok && wait_bar(smem_u32(&bars[n % SLOTS]), (n / SLOTS) & 1, dead);
+        ok = __all_sync(0xffffffffu, ok);
+        return ok;
+    };
+    auto arrive = [&](uint64_t *bars, uint32_t n) {
+        __syncwarp();
+        if (lane == 0) mbar_arrive_release(smem_u32(&bars[n % SLOTS]));
+    };
+    auto slot_of = [&](uint32_t n) { return s_slots + (n % SLOTS) * M::SLOT; };
+    if (warp == LOAD_WARPS + STORE_WARPS) {
+        // ------------------------------------------------ places
+        // (a chunk's line is found while the places of the one before are on their way: the waits for other chunks empty the L1)
+        const int per_lh = p.chunk_ptr[n_seqs];
+        const int64_t all = (int64_t)per_lh * p.kv.heads * layers;
+        struct Chunk {
+            Line l;
+            int c;
+            bool more;
+        };
+        auto find = [&](int64_t t) {
+            Chunk r;
+            r.more = t < all;
+            r.c = 0;
+            if (!r.more) return r;
+            const int lh = (int)(t / per_lh), x = (int)(t - (int64_t)lh * per_lh);
+            int lo = 0, n = n_seqs;  // the last request that begins at or before x is one of n
+            while (n > 1) {
+                const int step = (n + 31) / 32, at = lane * step;
+                const uint32_t on = __ballot_sync(0xffffffffu, at < n && p.chunk_ptr[lo + min(at, n - 1)] <= x);
+                const int last = 31 - __clz(on);  // (lane 0 is)
+                lo += last * step;
+                n = min(step, n - last * step);
+            }
+            r.c = x - p.chunk_ptr[lo];
+            r.l = load_line(p, lh, lo);
+            return r;
+        };
+        uint32_t ticket = 0;
+        auto draw = [&]() {
+            if (lane == 0) ticket = atomicAdd(p.ticket, 1u);
+        };
+        draw();
+        Chunk now = find(__shfl_sync(0xffffffffu, ticket, 0));
+        draw();
+        for (uint32_t n = 0;; ++n) {
+            const int slot = n % SLOTS;
+            if (!now.more) {
+                if (n >= SLOTS && !wait(s_free, n - SLOTS)) break;
+                if (lane == 0) s_chunk[slot] = -1;
+                arrive(s_full, n);
+                break;
+            }
+            const Line &l = now.l;
+            const int c = now.c;
+            int src[ROWS / 32], dst[ROWS / 32], from[ROWS / 32];
+#pragma unroll
+            for (int k = 0; k < ROWS / 32; ++k) {
+                const int i = c * ROWS + 32 * k + lane;
+                from[k] = i < l.keep ? l.kept[i] : i;
+            }
+            const int b0 = p.bound[l.chunk0 + c], b1 = (c + 1) * ROWS < l.len ? p.bound[l.chunk0 + c + 1] : l.keep;
+            const Chunk next = find(__shfl_sync(0xffffffffu, ticket, 0));
+            draw();
+#pragma unroll
+            for (int k = 0; k < ROWS / 32; ++k) {
+                const int i = c * ROWS + 32 * k + lane;
+                src[k] = 0;
+                dst[k] = -1;
+                if (from[k] != i) {
+                    src[k] = (int)row_of(p, l, from[k]);
+                    dst[k] = (int)row_of(p, l, i);
+                }
+            }
+            if (n >= SLOTS && !wait(s_free, n - SLOTS)) break;
+#pragma unroll
+            for (int k = 0; k < ROWS / 32; ++k) {
+                reinterpret_cast<int32_t *>(slot_of(n) + M::SRC)[32 * k + lane] = src[k];
+                reinterpret_cast<int32_t *>(slot_of(n) + M::DST)[32 * k + lane] = dst[k];
+            }
+            if (lane == 0) {
+                s_chunk[slot] = l.chunk0 + c;
+                // kept tokens [b0, b1) lie where this chunk will: chunks of the line up to this one
+                s_wait[slot][0] = b1 > b0 ? b0 / ROWS - c : 0;
+                s_wait[slot][1] = b1 > b0 ? (b1 - 1) / ROWS - c : 0;
+            }
+            arrive(s_full, n);
+            now = next;
+        }
+    } else if (warp == LOAD_WARPS + STORE_WARPS + 1) {
+        // ------------------------------------------------ chunks that were read
+        for (uint32_t n = 0; wait(s_full, n); ++n) {
+            const int64_t chunk = s_chunk[n % SLOTS];
+            if (chunk < 0 || !wait(s_read, n)) break;
+            if (lane == 0) {
+                asm volatile("st.relaxed.gpu.global.u32 [%0], %1;\n" ::"l"(p.read + chunk), "r"(1u) : "memory");
+            }
+            arrive(s_free, n);
+        }
+    } else if (warp == LOAD_WARPS + STORE_WARPS + 2) {
+        // ------------------------------------------------ chunks to wait for
+        for (uint32_t n = 0; wait(s_full, n); ++n) {
+            const int64_t chunk = s_chunk[n % SLOTS];
+            if (chunk < 0) break;
+            if (lane < 2 && s_wait[n % SLOTS][lane] < 0) {
+                const uint32_t *flag = p.read + chunk + s_wait[n % SLOTS][lane];
+                uint32_t x = 0;
+                for (int i = 0; i < EVICT_POLLS && !x && !*dead; ++i)
+                    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];\n" : "=r"(x) : "l"(flag) : "memory");
+                ok = x != 0;
+            }
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            arrive(s_clear, n);
+            arrive(s_free, n);
+        }
+    } else if (warp == LOAD_WARPS + STORE_WARPS + 3) {
+        // ------------------------------------------------ exponents and weights, the next chunk's on their way
+        uint32_t ke[2][ROWS / 32], ve[2][ROWS / 32];
+        float w[2][ROWS / 32];
+        auto load = [&](int b, uint32_t n) {
+            if (!wait(s_full, n) || s_chunk[n % SLOTS] < 0) return false;
+#pragma unroll
+            for (int k = 0; k < ROWS / 32; ++k) {
+                const int r = 32 * k + lane;
+                ke[b][k] = ve[b][k] = 0;
+                w[b][k] = 0.f;
+                if (reinterpret_cast<const int32_t *>(slot_of(n) + M::DST)[r] >= 0) {
+                    const int64_t at = reinterpret_cast<const int32_t *>(slot_of(n) + M::SRC)[r];
+                    ke[b][k] = p.kv.k_exp[at];
+                    ve[b][k] = p.kv.v_exp[at];
+                    if (p.weights) w[b][k] = p.weights[at];
+                }
+            }
+            return true;
+        };
+        auto put = [&](int b, uint32_t n) {
+#pragma unroll
+            for (int k = 0; k < ROWS / 32; ++k) {
+                const int r = 32 * k + lane;
+                (slot_of(n) + M::E)[r] = (uint8_t)ke[b][k];
+                (slot_of(n) + M::E)[ROWS + r] = (uint8_t)ve[b][k];
+                reinterpret_cast<float *>(slot_of(n) + M::W)[r] = w[b][k];
+            }
+            arrive(s_read, n);
+        };
+        bool more = load(0, 0);
+        for (uint32_t n = 0; more; n += 2) {
+            more = load(1, n + 1);
+            put(0, n);
+            if (!more) break;
+            more = load(0, n + 2);
+            put(1, n + 1);
+        }
+    } else if (warp < LOAD_WARPS) {
+        // ------------------------------------------------ keys and values into the slot
+        const int part = tid % M::LPR;
+        for (uint32_t n = 0; wait(s_full, n) && s_chunk[n % SLOTS] >= 0; ++n) {
+            uint8_t *slot = slot_of(n);
+            const int32_t *src = reinterpret_cast<const int32_t *>(slot + M::SRC), *dst = reinterpret_cast<const int32_t *>(slot + M::DST);
+#pragma unroll
+            for (int r = tid / M::LPR; r < ROWS; r += 32 * LOAD_WARPS / M::LPR) {
+                const bool moves = dst[r] >= 0;
+                const int64_t from = (int64_t)src[r] * D + part * 16;
+                cp_async16(smem_u32(slot + M::K + r * D + part * 16), p.kv.k + from, moves);
+                cp_async16(smem_u32(slot + M::V + r * D + part * 16), p.kv.v + from, moves);
+            }
+            cp_async_arrive_noinc(smem_u32(&s_read[n % SLOTS]));
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+    } else {
+        // ------------------------------------------------ out of it
+        const int me = tid - 32 * LOAD_WARPS, part = me % M::LPR;
+        for (uint32_t n = 0; wait(s_full, n) && s_chunk[n % SLOTS] >= 0; ++n) {
+            if (!wait(s_read, n) || !wait(s_clear, n)) break;
+            const uint8_t *slot = slot_of(n);
+            const int32_t *dst = reinterpret_cast<const int32_t *>(slot + M::DST);
+#pragma unroll
+            for (int r = me / M::LPR; r < ROWS; r += 32 * STORE_WARPS / M::LPR) {
+                const int64_t to = dst[r];
+                if (to < 0) continue;
+                reinterpret_cast<uint4 *>(p.kv.k + to * D)[part] = *reinterpret_cast<const uint4 *>(slot + M::K + r * D + part * 16);
+                reinterpret_cast<uint4 *>(p.kv.v + to * D)[part] = *reinterpret_cast<const uint4 *>(slot + M::V + r * D + part * 16);
+            }
+            if (me < ROWS && dst[me] >= 0) {
+                const int64_t to = dst[me];
+                p.kv.k_exp[to] = (slot + M::E)[me];
+                p.kv.v_exp[to] = (slot + M::E)[ROWS + me];
+                if (p.weights) p.weights[to] = reinterpret_cast<const float *>(slot + M::W)[me];
+            }
+            arrive(s_free, n);
+        }
+    }
+    if (!ok && lane == 0) {
+        s_dead = 1;
+        atomicOr(p.err, SALT_DEVERR_TIMEOUT);
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(MOVE_THREADS) evict_move_kernel(const EvictParams p)
+template <int THREADS, int ROWS>
+cudaError_t launch_select(const EvictParams &params, int64_t lines, int ctas, cudaStream_t stream, int len)
 {
-    constexpr int LPR = D / 16, ROWS = MOVE_THREADS / LPR;
-    if (p.track[TH_SEQS] > p.n_seqs || p.track[TH_SHARED] || blockIdx.x / p.kv.heads % p.n_seqs >= p.track[TH_SEQS]) return;
-    const Line l = load_line(p, blockIdx.x);
-    const int part = threadIdx.x % LPR;
-    for (int i0 = 0; i0 < l.keep; i0 += ROWS) {
-        const int i = i0 + threadIdx.x / LPR;
-        int64_t src = 0, dst = 0;
-        uint4 k, v;
-        uint8_t ke = 0, ve = 0;
-        float w = 0.f;
-        if (i < l.keep) {
-            src = row_of(p, l, l.kept[i]);
-            dst = row_of(p, l, i);
-            k = reinterpret_cast<const uint4 *>(p.kv.k + src * D)[part];
-            v = reinterpret_cast<const uint4 *>(p.kv.v + src * D)[part];
-            if (part == 0) {
-                ke = p.kv.k_exp[src];
-                ve = p.kv.v_exp[src];
-                if (p.weights) w = p.weights[src];
-            }
-        }
-        __syncthreads();
-        if (i < l.keep && src != dst) {
-            reinterpret_cast<uint4 *>(p.kv.k + dst * D)[part] = k;
-            reinterpret_cast<uint4 *>(p.kv.v + dst * D)[part] = v;
-            if (part == 0) {
-                p.kv.k_exp[dst] = ke;
-                p.kv.v_exp[dst] = ve;
-                if (p.weights) p.weights[dst] = w;
-            }
-        }
-    }
+    constexpr int CAP = THREADS == 256 ? 4096 : 20480;  // two CTAs an SM
+    EvictParams p = params;
+    p.key_cap = std::min<int64_t>(CAP, ((int64_t)len + ctas * THREADS - 1) / (ctas * THREADS) * THREADS + THREADS);
+    const size_t bytes = (size_t)p.key_cap * 4;
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(CAP * 4 + THREADS * 4));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)(lines * ctas), 1, 1);
+    cfg.blockDim = dim3(THREADS, 1, 1);
+    cfg.dynamicSmemBytes = bytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, evict_select_kernel<THREADS, ROWS>, p);
+}
+
+template <int D>
+cudaError_t launch_evict(const EvictParams &p, int n_sm, int layers, int longest, int64_t chunks, cudaStream_t stream)
+{
+    constexpr int ROWS = evict_rows(D);
+    const int64_t lines = (int64_t)layers * p.n_seqs * p.kv.heads;
+    // long lines go to several CTAs, as long as those of all lines fill the SMs no more than twice
+    int ctas = 1;
+    while (ctas < 8 && longest > 8192 * ctas && lines * ctas * 2 <= 2 * n_sm) ctas *= 2;
+    cudaError_t e = longest <= 4096 ? launch_select<256, ROWS>(p, lines, 1, stream, longest) : launch_select<512, ROWS>(p, lines, ctas, stream, longest);
+    if (e != cudaSuccess) return e;
+    const int64_t most = chunks * p.kv.heads * layers;
+    using M = Move<D, ROWS>;
+    e = cudaFuncSetAttribute(evict_move_kernel<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(evict_move_kernel<M>, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2 * n_sm)), MOVE_THREADS, M::BYTES, stream, p, layers);
 }
 
 }  // namespace
@@ -240,17 +678,20 @@ try {
     p.first = first;
     p.recent = recent;
     p.err = ctx_error_word(ctx);
-    // (a launch's lines are numbered in 32 bits; those of a layer are 2^24 at most)
-    const int64_t lines = (int64_t)p.n_seqs * kv.heads, most = std::max<int64_t>(1, (1ll << 30) / lines);
-    for (int64_t l = 0; l < n_layers; l += most) {
-        const unsigned n = (unsigned)(std::min<int64_t>(most, n_layers - l) * lines);
+    const Track &tr = a->track;
+    p.chunk_ptr = tr.chunk_ptr;
+    p.bound = tr.bound;
+    p.read = tr.read;
+    p.ticket = tr.ticket;
+    p.chunks = tr.chunks_cap;
+    p.key_cap = 0;
+    // as many layers at a time as the workspace has chunks for
+    for (int32_t l = 0; l < n_layers; l += tr.layers_cap) {
+        const int32_t n = std::min(tr.layers_cap, n_layers - l);
         p.layer = layer + l;
-        p.kept = kept + l * lines * kept_stride;
-        evict_select_kernel<<<n, SELECT_THREADS, 0, stream>>>(p);
-        SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
-        if (kv.dim == 128) evict_move_kernel<128><<<n, MOVE_THREADS, 0, stream>>>(p);
-        else evict_move_kernel<64><<<n, MOVE_THREADS, 0, stream>>>(p);
-        SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
+        p.kept = kept + (int64_t)l * p.n_seqs * kv.heads * kept_stride;
+        SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_evict<128>(p, a->n_sm, n, tr.longest, tr.chunks, stream)
+                                             : launch_evict<64>(p, a->n_sm, n, tr.longest, tr.chunks, stream));
     }
     return SALT_OK;
 } catch (const std::bad_alloc &) {
