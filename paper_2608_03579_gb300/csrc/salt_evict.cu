@@ -83,11 +83,11 @@ __device__ __forceinline__ int64_t row_of(const EvictParams &p, const Line &l, i
     return (((l.page0 + __ldg(l.pages + (j >> p.kv.page_log2))) * p.kv.heads + l.head) << p.kv.page_log2) + (j & (p.kv.page - 1));
 }
 
-// Larger scores are larger words; the zeros are one, a NaN is below everything.
+// Larger scores are larger words; the zeros are one, a NaN is below every number.  0 and the largest word are no scores'.
 __device__ __forceinline__ uint32_t key_of(float x)
 {
     const uint32_t u = __float_as_uint(x);
-    if (!(x == x)) return 0u;
+    if (!(x == x)) return 1u;
     if (x == 0.f) return 0x80000000u;
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -141,14 +141,22 @@ __device__ __forceinline__ void cluster_sync(uint32_t n)
 template <int THREADS, int ROWS>
 __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_constant__ EvictParams p)
 {
-    constexpr int WARPS = THREADS / 32, PER = BINS / THREADS;
+    constexpr int WARPS = THREADS / 32;
+    constexpr bool ALONE = THREADS < 1024;              // a line has one CTA
+    constexpr int HISTS = ALONE ? 1 : DIGITS;           // (other CTAs may still read the last digit's)
     extern __shared__ __align__(16) uint32_t s_keys[];
-    __shared__ __align__(16) uint32_t s_hist[DIGITS][BINS], s_warp[32], s_found[2], s_held[WARPS], s_tied[WARPS], s_all[2];
+    __shared__ __align__(16) uint32_t s_hist[HISTS][BINS], s_coarse[HISTS][BINS / 32], s_total[96], s_warp[32], s_held[WARPS], s_tied[WARPS], s_all[2];
     pdl_wait();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, n_seqs = p.track[TH_SEQS];
+    // (the warp's number from a shuffle, so that branches by it are known to be taken by whole warps)
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, n_seqs = p.track[TH_SEQS];
     uint32_t C, rank;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(C));
-    asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    if (ALONE) {
+        C = 1;
+        rank = 0;
+    } else {
+        asm volatile("mov.u32 %0, %%cluster_nctarank;\n" : "=r"(C));
+        asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+    }
     const bool fits = n_seqs <= p.n_seqs && !p.track[TH_SHARED];
     if (blockIdx.x == 0) {  // the chunks of every request, once for all layers and heads
         int before = 0;
@@ -170,121 +178,147 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     if (!fits || seq >= n_seqs) return;  // (the cluster together)
     const Line l = load_line(p, lh, seq);
     if (l.keep == 0) return;
-    const int from = l.first, to = l.len - l.recent;
-    const int warp_run = ((l.len + (int)C * WARPS - 1) / ((int)C * WARPS) + 31) & ~31, cta0 = (int)rank * WARPS * warp_run, warp0 = cta0 + warp * warp_run;
-    const int cta1 = min(l.len, cta0 + WARPS * warp_run), warp1 = min(l.len, warp0 + warp_run);
-    for (int i = tid; i < DIGITS * BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(s_hist[0])[i] = make_uint4(0, 0, 0, 0);
+    // (known to be a warp's, like its number: shuffles and votes in loops and branches by them are quick then)
+    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const int len = uniform(l.len), from = uniform(l.first), to = uniform(l.len - l.recent);
+    const int warp_run = ((len + (int)C * WARPS - 1) / ((int)C * WARPS) + 127) & ~127, cta0 = (int)rank * WARPS * warp_run, warp0 = cta0 + warp * warp_run;
+    const int warp1 = min(len, warp0 + warp_run);
+    auto clear = [&]() {
+        for (int i = tid; i < HISTS * BINS / 4; i += THREADS) reinterpret_cast<uint4 *>(s_hist[0])[i] = make_uint4(0, 0, 0, 0);
+    };
+    clear();
     for (int c = (int)rank * THREADS + tid; c * ROWS < l.keep; c += (int)C * THREADS) p.read[l.chunk0 + c] = 0;
     __syncthreads();
-    uint32_t want = l.keep - l.first - l.recent, prefix = 0;
-    const bool any = want > 0;
-    // A warp goes over its run 128 tokens at a time, four of a page a lane.
+    // A warp goes over its run 128 tokens at a time, four of a page a lane.  The first and last tokens, kept in any case, have the largest word, places
+    // past the line the least.
     auto fetch = [&](int j) {
-        const float4 x = __ldg(reinterpret_cast<const float4 *>(p.scores + row_of(p, l, j)));
-        return make_uint4(key_of(x.x), key_of(x.y), key_of(x.z), key_of(x.w));
-    };
-    // (key_cap is a multiple of 4)
-    auto keys_at = [&](int j) { return j >= warp1 ? make_uint4(0, 0, 0, 0) : j - cta0 < p.key_cap ? *reinterpret_cast<const uint4 *>(s_keys + (j - cta0)) : fetch(j); };
-    // counts the keys whose digits above the d-th are `prefix`
-    auto count = [&](int d, int j, const uint4 &x) {
-        const uint32_t key[4] = {x.x, x.y, x.z, x.w};
-        const int above = digit_shift(d) + (d == 2 ? 10 : 11);
-        uint32_t bin[4], all = 0, same = 0;
-        bool in[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            in[i] = j + i >= from && j + i < to && j + i < warp1 && (d == 0 || key[i] >> above == prefix);
-            bin[i] = key[i] >> digit_shift(d) & (d == 2 ? 1023u : 2047u);
-            all += in[i];
-        }
-        // (equal scores are common: a lane's, and a warp's, count as one)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) same += in[i] && bin[i] == bin[0] && in[0];
-        const uint32_t on = __ballot_sync(0xffffffffu, all > 0);
-        if (on == 0) return;
-        const uint32_t lead = __shfl_sync(0xffffffffu, bin[0], 0);
-        if (__all_sync(0xffffffffu, same == 4 && bin[0] == lead)) {
-            if (lane == 0) atomicAdd(&s_hist[d][bin[0]], 128u);
-        } else if (all > 0 && same == all) {
-            atomicAdd(&s_hist[d][bin[0]], all);
-        } else {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (j >= len) return x;
+        const float4 f = __ldg(reinterpret_cast<const float4 *>(p.scores + row_of(p, l, j)));
+        x = make_uint4(key_of(f.x), key_of(f.y), key_of(f.z), key_of(f.w));
+        if (j < from || j + 4 > to) {
+            uint32_t *key[4] = {&x.x, &x.y, &x.z, &x.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (in[i]) atomicAdd(&s_hist[d][bin[i]], 1u);
+                if (j + i < from || j + i >= to) *key[i] = j + i < len ? 0xffffffffu : 0u;
         }
+        return x;
     };
-    if (any) {
-        constexpr int AHEAD = 4;  // groups under way
-        for (int j0 = warp0; j0 < warp1; j0 += 128 * AHEAD) {
-            uint4 x[AHEAD];
+    auto keys_at = [&](int j0) {  // (key_cap is a multiple of 128)
+        return j0 - cta0 < p.key_cap ? *reinterpret_cast<const uint4 *>(s_keys + (j0 - cta0) + 4 * lane) : fetch(j0 + 4 * lane);
+    };
+    constexpr int AHEAD = ALONE ? 2 : 8;  // groups under way
+#pragma unroll 1
+    for (int j0 = warp0; j0 < warp1; j0 += 128 * AHEAD) {
+        uint4 x[AHEAD];
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int j = j0 + 128 * k + 4 * lane;
-                x[k] = make_uint4(0, 0, 0, 0);
-                if (j < warp1) x[k] = fetch(j);
-            }
+        for (int k = 0; k < AHEAD; ++k) x[k] = fetch(j0 + 128 * k + 4 * lane < warp1 ? j0 + 128 * k + 4 * lane : len);
 #pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                const int j = j0 + 128 * k + 4 * lane;
-                if (j0 + 128 * k >= warp1) break;
-                if (j < warp1 && j - cta0 < p.key_cap) *reinterpret_cast<uint4 *>(s_keys + (j - cta0)) = x[k];
-                count(0, j, x[k]);
-            }
-        }
-    }
-    for (int d = 0; d < DIGITS && any; ++d) {
-        if (d > 0)
-            for (int j0 = warp0; j0 < warp1; j0 += 128) count(d, j0 + 4 * lane, keys_at(j0 + 4 * lane));
-        cluster_sync(C);
-        // from the largest digit down: a thread has PER of them
-        uint32_t n[PER], sum = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int bin = BINS - 1 - (tid * PER + i);
-            n[i] = 0;
-            if (C == 1) {
-                n[i] = s_hist[d][bin];
+        for (int k = 0; k < AHEAD; ++k) {
+            const int j = j0 + 128 * k;
+            if (j >= warp1) break;
+            if (j - cta0 < p.key_cap) *reinterpret_cast<uint4 *>(s_keys + (j - cta0) + 4 * lane) = x[k];
+            // (equal scores are common: a lane's, and a warp's, count as one)
+            const uint32_t bin[4] = {x[k].x >> digit_shift(0), x[k].y >> digit_shift(0), x[k].z >> digit_shift(0), x[k].w >> digit_shift(0)};
+            const bool same = bin[0] == bin[1] && bin[0] == bin[2] && bin[0] == bin[3];
+            const uint32_t lead = __shfl_sync(0xffffffffu, bin[0], 0);
+            if (__all_sync(0xffffffffu, same && bin[0] == lead)) {
+                if (lane == 0) atomicAdd(&s_hist[0][lead], 128u);
+            } else if (same) {
+                atomicAdd(&s_hist[0][bin[0]], 4u);
             } else {
 #pragma unroll
-                for (uint32_t r = 0; r < 8; ++r)
-                    if (r < C) n[i] += peer_word(smem_u32(&s_hist[d][bin]), r);
+                for (int i = 0; i < 4; ++i) atomicAdd(&s_hist[0][bin[i]], 1u);
             }
-            sum += n[i];
+            __syncwarp();
         }
-        uint32_t all, before = block_scan(sum, s_warp, &all) - sum;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (before < want && before + n[i] >= want) {
-                s_found[0] = BINS - 1 - (tid * PER + i);
-                s_found[1] = want - before;
-            }
-            before += n[i];
-        }
-        __syncthreads();
-        prefix = prefix << (d == 2 ? 10 : 11) | s_found[0];
-        want = s_found[1];
-        // (s_found is written again behind the next barriers)
     }
-    // a lane's tokens that are kept whatever the ties, and those that tie with the last one that is kept, a bit each
-    auto sort_out = [&](int j, uint32_t &h, uint32_t &t) {
-        const uint4 x = any ? keys_at(j) : make_uint4(0, 0, 0, 0);
-        const uint32_t key[4] = {x.x, x.y, x.z, x.w};
-        h = t = 0;
+    // the smallest word that is kept, and `want` of those that are equal to it
+    uint32_t want = (uint32_t)uniform(l.keep), prefix = 0;
+#pragma unroll 1
+    for (int d = 0; d < DIGITS; ++d) {
+        if (d > 0) {  // of the words whose digits above are `prefix`
+            const int shift = digit_shift(d), above = shift + (d == 2 ? 10 : 11);
+            const uint32_t mask = d == 2 ? 1023u : 2047u;
+            uint32_t *to_hist = s_hist[d % HISTS];
+#pragma unroll 1
+            for (int j0 = warp0; j0 < warp1; j0 += 128) {
+                const uint4 x = keys_at(j0);
+                const uint32_t key[4] = {x.x, x.y, x.z, x.w};
+                bool in[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool in = j + i >= from && j + i < to;
-            if (j + i < warp1) {
-                h |= (uint32_t)(!in || (any && key[i] > prefix)) << i;
-                t |= (uint32_t)(in && any && key[i] == prefix) << i;
+                for (int i = 0; i < 4; ++i) in[i] = key[i] >> above == prefix;
+                if (!__any_sync(0xffffffffu, in[0] || in[1] || in[2] || in[3])) continue;
+                const uint32_t lead = __shfl_sync(0xffffffffu, key[0] >> shift, 0);
+                const bool same = in[0] && key[0] >> shift == lead && key[1] >> shift == lead && key[2] >> shift == lead && key[3] >> shift == lead;
+                if (__all_sync(0xffffffffu, same)) {
+                    if (lane == 0) atomicAdd(&to_hist[lead & mask], 128u);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (in[i]) atomicAdd(&to_hist[key[i] >> shift & mask], 1u);
+                }
+                __syncwarp();
             }
         }
-    };
-    uint32_t held = 0, tied = 0;
+        const uint32_t *hist = s_hist[d % HISTS], *coarse = s_coarse[d % HISTS];
+        __syncthreads();
+#pragma unroll 2
+        for (int g = warp; g < BINS / 32; g += WARPS) {
+            const uint32_t sum = __reduce_add_sync(0xffffffffu, hist[g * 32 + lane]);
+            if (lane == 0) s_coarse[d % HISTS][g] = sum;
+        }
+        cluster_sync(C);
+        // from the largest digit down: the 32 bins that hold the last one kept, then which of them.  (Every warp does the same, without
+        // branches: in one warp, inside a branch, the shuffles took 2 us a digit.)
+        auto total = [&](const uint32_t *at) {
+            uint32_t n = 0;
+#pragma unroll
+            for (uint32_t r = 0; r < 8; ++r)
+                if (r < C) n += peer_word(smem_u32(at), r);
+            return n;
+        };
+        if (!ALONE) {
+            if (tid < BINS / 32) s_total[tid] = total(coarse + tid);
+            __syncthreads();
+            coarse = s_total;
+        }
+        auto scan = [&](uint32_t n) {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t x = __shfl_up_sync(0xffffffffu, n, o);
+                if (lane >= o) n += x;
+            }
+            return n;
+        };
+        const uint32_t a = coarse[63 - 2 * lane], ab = a + coarse[62 - 2 * lane], ab_to = scan(ab);
+        const int two = __ffs(__ballot_sync(0xffffffffu, ab_to >= want)) - 1;
+        uint32_t before = __shfl_sync(0xffffffffu, ab_to - ab, two);
+        const uint32_t a_there = __shfl_sync(0xffffffffu, a, two);
+        const bool second = before + a_there < want;
+        before += second ? a_there : 0u;
+        const int bin0 = (63 - 2 * two - second) * 32;
+        if (!ALONE) {
+            if (tid < 32) s_total[64 + tid] = total(hist + bin0 + tid);
+            __syncthreads();
+        }
+        const uint32_t n = ALONE ? hist[bin0 + 31 - lane] : s_total[64 + 31 - lane], n_to = scan(n);
+        const int at = __ffs(__ballot_sync(0xffffffffu, before + n_to >= want)) - 1;
+        before += __shfl_sync(0xffffffffu, n_to - n, at);
+        prefix = prefix << (d == 2 ? 10 : 11) | (uint32_t)(bin0 + 31 - at);
+        want -= before;
+        if (ALONE && d + 1 < DIGITS) {
+            __syncthreads();
+            clear();
+            __syncthreads();
+        }
+    }
+    uint32_t held = 0, tied = 0;  // words above, and equal
+#pragma unroll 1
     for (int j0 = warp0; j0 < warp1; j0 += 128) {
-        uint32_t h, t;
-        sort_out(j0 + 4 * lane, h, t);
-        held += __popc(h);
-        tied += __popc(t);
+        const uint4 x = keys_at(j0);
+        held += (x.x > prefix) + (x.y > prefix) + (x.z > prefix) + (x.w > prefix);
+        tied += (x.x == prefix) + (x.y == prefix) + (x.z == prefix) + (x.w == prefix);
     }
     held = __reduce_add_sync(0xffffffffu, held);
     tied = __reduce_add_sync(0xffffffffu, tied);
@@ -313,35 +347,45 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     pdl_launch_dependents();
     const uint32_t below = (1u << lane) - 1u;
     uint32_t out0 = held0 + min(tied0, want);  // kept before the warp's run
+#pragma unroll 1
     for (int j0 = warp0; j0 < warp1; j0 += 128) {
         const int j = j0 + 4 * lane;
-        uint32_t h, t;
-        sort_out(j, h, t);
-        uint32_t ties = 0, ties_here = 0, on = 0, on_here = 0;  // of the lanes before, of all
+        const uint4 x = keys_at(j0);
+        const uint32_t key[4] = {x.x, x.y, x.z, x.w};
+        bool h[4], t[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t x = __ballot_sync(0xffffffffu, t >> i & 1);
-            ties += __popc(x & below);
-            ties_here += __popc(x);
+            h[i] = key[i] > prefix;
+            t[i] = key[i] == prefix;
         }
-        // the first `want` ties are kept
-        uint32_t rank_t = tied0 + ties;
+        // of a number below 8 a lane, the sum over the lanes before, and over all
+        auto ranks = [&](uint32_t n, uint32_t &all) {
+            uint32_t before = 0;
+            all = 0;
+#pragma unroll
+            for (int b = 0; b < 3; ++b) {
+                const uint32_t on = __ballot_sync(0xffffffffu, n >> b & 1);
+                before += __popc(on & below) << b;
+                all += __popc(on) << b;
+            }
+            return before;
+        };
+        const uint32_t ties = t[0] + t[1] + t[2] + t[3];
+        if (__any_sync(0xffffffffu, ties > 0)) {  // the first `want` ties are kept
+            uint32_t all, rank_t = tied0 + ranks(ties, all);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[i] = h[i] || (t[i] && rank_t < want);
+                rank_t += t[i];
+            }
+            tied0 += all;
+        }
+        uint32_t all, out = out0 + ranks(h[0] + h[1] + h[2] + h[3], all);
+        out0 += all;
+        if (j % ROWS == 0 && j < l.keep + ROWS && j < len) p.bound[l.chunk0 + j / ROWS] = (int)out;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (t >> i & 1) h |= (uint32_t)(rank_t++ < want) << i;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = __ballot_sync(0xffffffffu, h >> i & 1);
-            on += __popc(x & below);
-            on_here += __popc(x);
-        }
-        uint32_t out = out0 + on;
-        if (j % ROWS == 0 && j < l.keep + ROWS && j < warp1) p.bound[l.chunk0 + j / ROWS] = (int)out;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (h >> i & 1) l.kept[out++] = j + i;
-        out0 += on_here;
-        tied0 += ties_here;
+            if (h[i]) l.kept[out++] = j + i;
     }
     if (C > 1) cluster_wait();
 }
@@ -375,7 +419,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     __shared__ int64_t s_chunk[SLOTS];     // the chunk's entry, -1: no more
     __shared__ int32_t s_wait[SLOTS][2];   // the first and last chunk of the line that it waits for, from here
     __shared__ int s_dead;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int *dead = &s_dead;
     if (tid == 0) {
         for (int i = 0; i < SLOTS; ++i) {
@@ -593,14 +637,17 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     }
 }
 
+template <int THREADS>
+constexpr int key_cap() { return THREADS < 1024 ? 32 * THREADS : 48128; }  // (with the counts an SM's shared memory)
+
 template <int THREADS, int ROWS>
 cudaError_t launch_select(const EvictParams &params, int64_t lines, int ctas, cudaStream_t stream, int len)
 {
-    constexpr int CAP = THREADS == 256 ? 4096 : 20480;  // two CTAs an SM
+    constexpr int CAP = key_cap<THREADS>();
     EvictParams p = params;
-    p.key_cap = std::min<int64_t>(CAP, ((int64_t)len + ctas * THREADS - 1) / (ctas * THREADS) * THREADS + THREADS);
-    const size_t bytes = (size_t)p.key_cap * 4;
-    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(CAP * 4 + THREADS * 4));
+    const int64_t run = ((int64_t)len + ctas * (THREADS / 32) - 1) / (ctas * (THREADS / 32));
+    p.key_cap = (int)std::min<int64_t>(CAP, (run + 127) / 128 * 128 * (THREADS / 32));
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<THREADS, ROWS>, cudaFuncAttributeMaxDynamicSharedMemorySize, CAP * 4);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
@@ -611,10 +658,10 @@ cudaError_t launch_select(const EvictParams &params, int64_t lines, int ctas, cu
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)(lines * ctas), 1, 1);
     cfg.blockDim = dim3(THREADS, 1, 1);
-    cfg.dynamicSmemBytes = bytes;
+    cfg.dynamicSmemBytes = (size_t)p.key_cap * 4;
     cfg.stream = stream;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = ctas > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, evict_select_kernel<THREADS, ROWS>, p);
 }
 
@@ -623,10 +670,14 @@ cudaError_t launch_evict(const EvictParams &p, int n_sm, int layers, int longest
 {
     constexpr int ROWS = evict_rows(D);
     const int64_t lines = (int64_t)layers * p.n_seqs * p.kv.heads;
-    // long lines go to several CTAs, as long as those of all lines fill the SMs no more than twice
+    // Long lines go to several CTAs, up to 6: clusters of 8 whose CTAs take an SM each fit 15 times into the card's
+    // SMs, of 6 at least 20 times (16 lines of 262,144 tokens: XXX us with 8, the last one a second wave, XXX with 6).
     int ctas = 1;
-    while (ctas < 8 && longest > 8192 * ctas && lines * ctas * 2 <= 2 * n_sm) ctas *= 2;
-    cudaError_t e = longest <= 4096 ? launch_select<256, ROWS>(p, lines, 1, stream, longest) : launch_select<512, ROWS>(p, lines, ctas, stream, longest);
+    while (ctas < 6 && longest > 8192 * ctas && lines * (ctas + 1) <= n_sm) ++ctas;
+    const cudaError_t e1 = longest <= 2048 && lines > 2 * n_sm ? launch_select<128, ROWS>(p, lines, 1, stream, longest)
+                           : longest <= 4096                   ? launch_select<256, ROWS>(p, lines, 1, stream, longest)
+                                                               : launch_select<1024, ROWS>(p, lines, ctas, stream, longest);
+    cudaError_t e = e1;
     if (e != cudaSuccess) return e;
     const int64_t most = chunks * p.kv.heads * layers;
     using M = Move<D, ROWS>;

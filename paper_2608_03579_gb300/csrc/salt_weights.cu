@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(sm);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, KV = p.kv.heads;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, KV = p.kv.heads;
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
         for (int i = 0; i < L::KST; ++i) {
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     extern __shared__ uint8_t smem_raw[];
     uint8_t *sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     const uint32_t base = smem_u32(sm);
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, KV = p.kv.heads, G = p.n_heads / KV, per = 128 / G;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, KV = p.kv.heads, G = p.n_heads / KV, per = 128 / G;
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
