@@ -1532,7 +1532,8 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
     t[TH_LISTED] = 0;
     if (n_many == 0 || tiles * KV > TRACK_UNITS / 2 || n_sm + 1 > TRACK_CTAS) return;
     struct Tile {
-        int tile, from, to;
+        const int32_t *list;
+        int t0, from, to;
     };
     std::vector<Tile> all;
     int64_t sum = 0;
@@ -1540,15 +1541,15 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
         const int32_t *l = t + tr.list_at + (size_t)i * LIST_WORDS;
         const int steps = (l[3] + per - 1) / per;
         for (int j = 0; j < (l[1] + TRACK_MANY_TILE - 1) / TRACK_MANY_TILE; ++j) {
-            all.push_back({l[LS_TILES] + j, first_step(l[6], l[5], j * TRACK_MANY_TILE, per), steps});
+            all.push_back({l, j * TRACK_MANY_TILE, first_step(l[6], l[5], j * TRACK_MANY_TILE, per), steps});
             sum += steps - all.back().from;
         }
     }
     // a part takes at least what a unit costs besides its steps, a few times over
     const int64_t share = sum * KV / n_sm, most = std::max<int64_t>(LEAST_STEPS, share / 3);
     struct Piece {
-        int cost;
-        int32_t w[UNIT_WORDS];
+        int cost, kh, from, to, split;
+        const Tile *tile;
     };
     std::vector<Piece> pieces;
     int slots = 0;
@@ -1559,7 +1560,7 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
         for (int kh = 0; kh < KV; ++kh) {
             for (int k = 0; k < parts; ++k) {
                 const int from = x.from + (int)((int64_t)steps * k / parts), to = x.from + (int)((int64_t)steps * (k + 1) / parts);
-                pieces.push_back({to - from + UNIT_COST, {x.tile * KV + kh, from, to, parts == 1 ? -1 : slots << 12 | k << 6 | (parts - 1)}});
+                pieces.push_back({to - from + UNIT_COST, kh, from, to, parts == 1 ? -1 : slots << 12 | k << 6 | (parts - 1), &x});
             }
             if (parts > 1) slots += parts;
         }
@@ -1584,7 +1585,17 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
     }
     for (int c = 0; c < n_sm; ++c) ptr[c + 1] += ptr[c];
     std::vector<int> next(ptr, ptr + n_sm);
-    for (size_t i = 0; i < pieces.size(); ++i) std::memcpy(units + (size_t)next[owner[i]]++ * UNIT_WORDS, pieces[i].w, UNIT_WORDS * 4);
+    for (size_t i = 0; i < pieces.size(); ++i) {
+        const Piece &x = pieces[i];
+        int32_t *u = units + (size_t)next[owner[i]]++ * UNIT_WORDS;
+        std::memcpy(u, x.tile->list, LIST_WORDS * 4);
+        u[LS_TILES] = x.kh;
+        u[LIST_WORDS] = x.tile->t0;
+        u[LIST_WORDS + 1] = x.from;
+        u[LIST_WORDS + 2] = x.to;
+        u[LIST_WORDS + 3] = x.split;
+    }
+    tr.n_units = (int)pieces.size();
 }
 
 // The tracked table of a checked batch; returns the words used.
@@ -1649,7 +1660,7 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     t[TH_SHARED] = tr.shared;
     tr.few_tiles = tiles[0];
     fill_units(a, tr.few, tr.many, tiles[1], t);
-    return t[TH_LISTED] ? tr.words : (size_t)(list - t);
+    return t[TH_LISTED] ? (size_t)tr.unit_at + TRACK_CTAS + (size_t)tr.n_units * UNIT_WORDS : (size_t)(list - t);
 }
 
 // A cache's codes as rows of D bytes, a box a page's rows of one head, swizzled over a row's width.

@@ -29,9 +29,9 @@ constexpr int LIST_WORDS = 8;
 constexpr int LS_TILES = 7;
 constexpr int TRACK_TILE = 128, TRACK_MANY_TILE = 256;
 constexpr int TRACK_FEW_ROWS = 16;
-// units of the many rows' lists: each CTA's first one, then per unit: tile * heads + head, steps [from, to), (slot of its
-// first part << 12 | part << 6 | parts - 1) or -1
-constexpr int TRACK_CTAS = 512, UNIT_WORDS = 4, TRACK_UNITS = 8192;
+// units of the many rows' lists: each CTA's first one, then per unit its list's words, the last one the head instead of the tiles, and first token, steps
+// [from, to), (slot of its first part << 12 | part << 6 | parts - 1) or -1
+constexpr int TRACK_CTAS = 512, UNIT_WORDS = 12, TRACK_UNITS = 8192;
 constexpr int TRACK_SLOTS = 2048;  // of partial sums, 256 tokens each
 // Rows that eviction moves at a time: 16 KB of keys and values.
 constexpr int evict_rows(int dim) { return 8192 / dim; }
@@ -49,7 +49,7 @@ struct Track {
     int seq_at = 0, list_at = 0, unit_at = 0;  // word offsets
     size_t words = 0;
     bool on = false, built = false, shared = false, split = false;
-    int n_seqs = 0, few = 0, many = 0;
+    int n_seqs = 0, few = 0, many = 0, n_units = 0;
     int64_t few_tiles = 0;
     // eviction's: the longest request, chunks of all requests in the build; room for chunks and layers; tables
     int longest = 0, chunks = 0, chunks_cap = 0, layers_cap = 0;

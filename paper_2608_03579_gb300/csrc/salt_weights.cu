@@ -62,13 +62,15 @@ __device__ __forceinline__ List load_list(const WeightParams &p, int i)
     const int4 a = __ldg(w), b = __ldg(w + 1);
     return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
-// Of the lists [lo, hi) the one that holds tile `tile` of them: the last that begins at or before it.
+// Of the lists [lo, hi) the one that holds tile `tile` of them: the last that begins at or before it.  The whole warp, 32 guesses at a time.
 __device__ __forceinline__ int find_list(const WeightParams &p, int lo, int hi, int tile)
 {
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldg(p.track + p.list_at + mid * LIST_WORDS + LS_TILES) <= tile) lo = mid;
-        else hi = mid;
+    for (int n = hi - lo; n > 1;) {
+        const int step = (n + 31) / 32, at = (int)(threadIdx.x & 31) * step;
+        const uint32_t on = __ballot_sync(0xffffffffu, at < n && __ldg(p.track + p.list_at + (lo + min(at, n - 1)) * LIST_WORDS + LS_TILES) <= tile);
+        const int last = 31 - __clz(on);  // (lane 0 is)
+        lo += last * step;
+        n = min(step, n - last * step);
     }
     return lo;
 }
@@ -464,16 +466,25 @@ struct Units {
     __device__ __forceinline__ bool more() const { return at < end; }
     __device__ __forceinline__ Unit get(const WeightParams &p, int per) const
     {
-        int4 w = make_int4(at, -1, -1, -1);
-        if (listed) w = __ldg(reinterpret_cast<const int4 *>(p.track + p.unit_at + TRACK_CTAS) + at);
         Unit u;
-        const int tile = w.x / p.kv.heads;
-        u.kh = w.x - tile * p.kv.heads;
-        u.l = load_list(p, find_list(p, p.track[TH_FEW], p.track[TH_FEW] + p.track[TH_MANY], tile));
-        u.t0 = (tile - u.l.tiles) * TRACK_MANY_TILE;
-        u.r0 = w.y >= 0 ? w.y : first_step(u.l.causal, u.l.lim, u.t0, per);
-        u.r1 = w.y >= 0 ? w.z : (u.l.ntok + per - 1) / per;
-        u.split = w.w;
+        if (listed) {
+            const int4 *w = reinterpret_cast<const int4 *>(p.track + p.unit_at + TRACK_CTAS) + (int64_t)at * (UNIT_WORDS / 4);
+            const int4 a = __ldg(w), b = __ldg(w + 1), c = __ldg(w + 2);
+            u.l = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, 0};
+            u.kh = b.w;
+            u.t0 = c.x;
+            u.r0 = c.y;
+            u.r1 = c.z;
+            u.split = c.w;
+        } else {
+            const int tile = at / p.kv.heads;
+            u.kh = at - tile * p.kv.heads;
+            u.l = load_list(p, find_list(p, p.track[TH_FEW], p.track[TH_FEW] + p.track[TH_MANY], tile));
+            u.t0 = (tile - u.l.tiles) * TRACK_MANY_TILE;
+            u.r0 = first_step(u.l.causal, u.l.lim, u.t0, per);
+            u.r1 = (u.l.ntok + per - 1) / per;
+            u.split = -1;
+        }
         u.two = u.l.len - u.t0 > 128;
         return u;
     }
@@ -667,8 +678,11 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         const bool lead = elect_one();
         const uint32_t id = idesc_bf16_f32(128, (per * G + 15) / 16 * 16);
         uint32_t st = 0, ph = 0, units[2] = {0, 0}, steps[2] = {0, 0};
-        for (; it.more() && ok; it.at += it.step) {
-            const Unit u = it.get(p, per);
+        Unit u = it.get(p, per);
+        while (it.more() && ok) {
+            it.at += it.step;
+            Unit v = u;
+            if (it.more()) v = it.get(p, per);
             for (int r = u.r0; r < u.r1 && ok; ++r) {
                 ok = wait_bar(base + L::Q_FULL + 8 * st, ph, dead);
                 const uint64_t qd = sdesc_kmajor_sw128(base + L::Q + st * L::Q_TILE);
@@ -698,6 +712,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             }
             ++units[0];
             units[1] += u.two;
+            u = v;
         }
         if (!ok) {  // the products issued so far end before the CTA does
             if (lead) {
@@ -711,8 +726,11 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     } else if (warp == 2) {
         // ------------------------------------------------ the steps' log-sums, and how many tokens their rows see
         uint32_t n = 0;
-        for (; it.more() && ok; it.at += it.step) {
-            const Unit u = it.get(p, per);
+        Unit u = it.get(p, per);
+        while (it.more() && ok) {
+            it.at += it.step;
+            Unit v = u;
+            if (it.more()) v = it.get(p, per);
             for (int r = u.r0; r < u.r1; ++r, ++n) {
                 const int i0 = r * per, m = min(per, u.l.ntok - i0);
                 float lse[4];
@@ -740,6 +758,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 __syncwarp();
                 if (lane == 0) mbar_arrive_release(base + L::M_FULL + 8 * s);
             }
+            u = v;
         }
         if (!ok && lane == 0) {
             *dead = 1;

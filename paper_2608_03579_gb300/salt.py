@@ -638,21 +638,18 @@ def salt_rope_destroy(rope: Rope) -> None:
 def _norm_weights(w, dim: int):
     if w is None:
         return None
-    if _torch_bf16 is None:
-        _load_types()
     if w.dtype is not _torch_bf16 or not w.is_cuda or w.numel() != dim or not w.is_contiguous():
         raise ValueError(f"norm weights are not a contiguous CUDA bf16 tensor of {dim}")
     return w.data_ptr()
 
 
-def _heads_of(t, dim: int, n: int | None = None):
+def _heads_of(t, dim: int):
     """_head_rows of a tensor of any number of heads, and that number."""
-    if t.dim() != 3:
-        raise ValueError(f"not a CUDA bf16 tensor [tokens, heads, {dim}]")
-    m, p, s = _head_rows(t, t.shape[1], dim)
-    if n is not None and m != n:
-        raise ValueError(f"{m} tokens, {n} expected")
-    return m, p, s, t.shape[1]
+    n, heads, d = t.shape
+    s, h, e = t.stride()
+    if d != dim or e != 1 or (h != dim and heads > 1) or t.dtype is not _torch_bf16 or not t.is_cuda:
+        raise ValueError(f"not a CUDA bf16 tensor [tokens, heads, {dim}] whose heads are contiguous within a row")
+    return n, t.data_ptr(), s if n > 1 else max(s, heads * dim), heads
 
 
 def salt_rope_apply(rope: Rope, q, k, positions, q_out, k_out, q_norm=None, k_norm=None, stream=None) -> None:
@@ -660,14 +657,18 @@ def salt_rope_apply(rope: Rope, q, k, positions, q_out, k_out, q_norm=None, k_no
     contiguous within a row) normalised and rotated into q_out and k_out
     (which may be q and k); positions CUDA int32 [tokens]."""
     D = rope.head_dim
+    if _torch_bf16 is None:
+        _load_types()
     n, qp, qs, H = _heads_of(q, D)
-    _, kp, ks, KV = _heads_of(k, D, n)
-    _, qop, qos, Ho = _heads_of(q_out, D, n)
-    _, kop, kos, KVo = _heads_of(k_out, D, n)
-    if H != Ho or KV != KVo:
-        raise ValueError("the outputs have other numbers of heads")
-    _check(_lib.salt_rope_apply(rope.handle, n, qp, qs, H, kp, ks, KV, _norm_weights(q_norm, D), _norm_weights(k_norm, D),
-                                _int32s(positions, n), qop, qos, kop, kos, _stream(stream)), rope.ctx)
+    nk, kp, ks, KV = _heads_of(k, D)
+    no, qop, qos, Ho = _heads_of(q_out, D)
+    nko, kop, kos, KVo = _heads_of(k_out, D)
+    if not n == nk == no == nko or H != Ho or KV != KVo:
+        raise ValueError("q, k and the outputs have different numbers of tokens or heads")
+    st = _lib.salt_rope_apply(rope.handle, n, qp, qs, H, kp, ks, KV, _norm_weights(q_norm, D), _norm_weights(k_norm, D),
+                              _int32s(positions, n), qop, qos, kop, kos, _stream(stream))
+    if st:
+        _check(st, rope.ctx)
 
 
 def salt_rope_write(rope: Rope, kv: KvCache, layer: int, q, k, v, positions, slots, q_out, q_norm=None, k_norm=None,
@@ -675,15 +676,18 @@ def salt_rope_write(rope: Rope, kv: KvCache, layer: int, q, k, v, positions, slo
     """The same for q, while k so treated and v as it is go into slots (CUDA
     int32 [tokens], -1: skip) of a layer of the cache."""
     D = rope.head_dim
+    if _torch_bf16 is None:
+        _load_types()
     n, qp, qs, H = _heads_of(q, D)
-    _, qop, qos, Ho = _heads_of(q_out, D, n)
-    _, kp, ks, KV = _heads_of(k, D, n)
-    _, vp, vs, KVv = _heads_of(v, D, n)
-    if H != Ho or KV != kv.n_kv_heads or KVv != KV:
-        raise ValueError("q_out, k or v has another number of heads")
-    _check(_lib.salt_rope_write(rope.handle, kv.handle, layer, n, qp, qs, H, kp, ks, vp, vs, _norm_weights(q_norm, D),
-                                _norm_weights(k_norm, D), _int32s(positions, n), _int32s(slots, n), qop, qos,
-                                _stream(stream)), rope.ctx)
+    no, qop, qos, Ho = _heads_of(q_out, D)
+    nk, kp, ks, KV = _heads_of(k, D)
+    nv, vp, vs, KVv = _heads_of(v, D)
+    if not n == no == nk == nv or H != Ho or not KV == KVv == kv.n_kv_heads:
+        raise ValueError("q, k, v and q_out have different numbers of tokens, or other heads than the cache")
+    st = _lib.salt_rope_write(rope.handle, kv.handle, layer, n, qp, qs, H, kp, ks, vp, vs, _norm_weights(q_norm, D),
+                              _norm_weights(k_norm, D), _int32s(positions, n), _int32s(slots, n), qop, qos, _stream(stream))
+    if st:
+        _check(st, rope.ctx)
 
 
 class AttnPlan:
