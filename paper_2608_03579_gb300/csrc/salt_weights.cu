@@ -56,10 +56,18 @@ struct WeightParams {
 struct List {
     int pages, len, tok, ntok, old, lim, causal, tiles;
 };
+// The same word in every lane, and known to be: loops and branches by it are taken by whole warps then, and the votes in them are quick (by
+// words that might differ, a vote takes hundreds of cycles).
+__device__ __forceinline__ int one_word(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ int4 four_words(const int4 *at)
+{
+    const int4 x = __ldg(at);
+    return make_int4(one_word(x.x), one_word(x.y), one_word(x.z), one_word(x.w));
+}
 __device__ __forceinline__ List load_list(const WeightParams &p, int i)
 {
     const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + i * LIST_WORDS);
-    const int4 a = __ldg(w), b = __ldg(w + 1);
+    const int4 a = four_words(w), b = four_words(w + 1);
     return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 }
 // Of the lists [lo, hi) the one that holds tile `tile` of them: the last that begins at or before it.  The whole warp, 32 guesses at a time.
@@ -260,8 +268,8 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     const int32_t *track = after_pdl_wait(p.track);
     const bool fits = track[TH_TOKENS] <= p.max_tok && !track[TH_SHARED];
     if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
-    const int n_lists = fits ? track[TH_FEW] : 0;
-    Walk k(p, n_lists, n_lists ? (int64_t)track[TH_FEW_TILES] * KV : 0);
+    const int n_lists = one_word(fits ? track[TH_FEW] : 0);
+    Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_TILES]) * KV : 0);
     bool ok = true;
     if (!k.more()) {
     } else if (warp == 0) {
@@ -416,11 +424,11 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
 
 // ---------------------------------------------------------------- many rows
 // A unit is 256 tokens of a list and head, and a run of steps over the rows that see them, up to 128 at
-// a time.  Two warpgroups have 128 tokens each, all of the step's columns.
+// a time.  Two warpgroups have 128 tokens, each every other sixteen of the step's columns.
 template <int D_>
 struct Many {
     static constexpr int D = D_;
-    static constexpr int THREADS = 128 + 2 * 128;
+    static constexpr int THREADS = 128 + 4 * 128;
     static constexpr int QST = D == 128 ? 3 : 6, MST = 4;   // stages of queries, and of what goes with a step
     static constexpr uint32_t TM_COLS = 512;                // two buffers of 128 scores for either 128 tokens
     static constexpr uint32_t A_TILE = 128 * 2 * D, RAW_TILE = 128 * D, Q_TILE = 128 * 2 * D;
@@ -431,7 +439,10 @@ struct Many {
     static constexpr uint32_t META = Q + QST * Q_TILE;
     static constexpr uint32_t EXPS = META + MST * M_BUF;    // 128 of either tile
     static constexpr uint32_t ROWS = EXPS + 256;            // the first rows of either tile's pages
-    static constexpr uint32_t K_FULL = ROWS + 64;
+    static constexpr uint32_t HALF = ROWS + 64;             // the second warpgroup's sums of either tile
+    static constexpr uint32_t H_FULL = HALF + 1024;         // a warp's each
+    static constexpr uint32_t H_FREE = H_FULL + 64;
+    static constexpr uint32_t K_FULL = H_FREE + 64;
     static constexpr uint32_t K_FREE = K_FULL + 16;
     static constexpr uint32_t A_FULL = K_FREE + 16;
     static constexpr uint32_t Q_FULL = A_FULL + 16;
@@ -458,10 +469,10 @@ struct Units {
     bool listed;
     __device__ __forceinline__ Units(const WeightParams &p, bool fits)
     {
-        listed = p.track[TH_LISTED];
+        listed = one_word(p.track[TH_LISTED]);
         step = listed ? 1 : gridDim.x;
-        at = listed ? p.track[p.unit_at + blockIdx.x] : blockIdx.x;
-        end = !fits ? 0 : listed ? p.track[p.unit_at + blockIdx.x + 1] : p.track[TH_MANY_TILES] * p.kv.heads;
+        at = listed ? one_word(p.track[p.unit_at + blockIdx.x]) : blockIdx.x;
+        end = one_word(!fits ? 0 : listed ? p.track[p.unit_at + blockIdx.x + 1] : p.track[TH_MANY_TILES] * p.kv.heads);
     }
     __device__ __forceinline__ bool more() const { return at < end; }
     __device__ __forceinline__ Unit get(const WeightParams &p, int per) const
@@ -469,7 +480,7 @@ struct Units {
         Unit u;
         if (listed) {
             const int4 *w = reinterpret_cast<const int4 *>(p.track + p.unit_at + TRACK_CTAS) + (int64_t)at * (UNIT_WORDS / 4);
-            const int4 a = __ldg(w), b = __ldg(w + 1), c = __ldg(w + 2);
+            const int4 a = four_words(w), b = four_words(w + 1), c = four_words(w + 2);
             u.l = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, 0};
             u.kh = b.w;
             u.t0 = c.x;
@@ -490,13 +501,52 @@ struct Units {
     }
 };
 
-// Widens a token's key: its row of codes to bf16, 128-byte swizzled halves of 64 elements.
+// A CTA's steps, unit by unit, the next unit's words on their way.
+struct Steps {
+    Units it;
+    Unit u, v;
+    int r;
+    bool live, next;
+    __device__ __forceinline__ void ahead(const WeightParams &p, int per)
+    {
+        it.at += it.step;
+        next = it.more();
+        if (next) v = it.get(p, per);
+    }
+    __device__ __forceinline__ Steps(const WeightParams &p, const Units &units, int per) : it(units)
+    {
+        live = it.more();
+        if (!live) return;
+        u = it.get(p, per);
+        r = u.r0;
+        ahead(p, per);
+    }
+    __device__ __forceinline__ void advance(const WeightParams &p, int per)
+    {
+        if (++r < u.r1) return;
+        live = next;
+        if (!live) return;
+        u = v;
+        r = u.r0;
+        ahead(p, per);
+    }
+    // query tokens of the step; the i-th of them (a request's own follow each other in the order)
+    __device__ __forceinline__ int tokens(int per) const { return min(per, u.l.ntok - r * per); }
+    __device__ __forceinline__ int token(const WeightParams &p, int per, int i) const
+    {
+        const int at = u.l.tok + r * per + i;
+        return u.l.causal ? at : __ldg(p.plan + p.order_at + at);
+    }
+};
+
+// Widens half of a token's key: its row of codes to bf16, 128-byte swizzled halves of 64 elements.
 template <class L>
-__device__ __forceinline__ void widen_key(uint32_t base, int wg, int me)
+__device__ __forceinline__ void widen_key(uint32_t base, int wg, int me, int half)
 {
     const uint32_t from = base + L::RAW + wg * L::RAW_TILE, to = base + L::A + wg * L::A_TILE;
 #pragma unroll
-    for (int c = 0; c < L::D / 16; ++c) {
+    for (int k = 0; k < L::D / 32; ++k) {
+        const int c = half * (L::D / 32) + k;
         const uint4 x = lds128(from + swz_rows<L::D>(me * L::D + c * 16));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
         uint32_t y[8];
@@ -514,7 +564,7 @@ __device__ __forceinline__ void widen_key(uint32_t base, int wg, int me)
     fence_async_smem();
 }
 
-// The sum over columns [0, 16 n) of a thread's scores, none of which is masked.
+// The sum over every other sixteen of columns [0, 16 n) of a thread's scores, from the first or second on; none of them is masked.
 __device__ __forceinline__ float sum_columns(uint32_t s_at, uint32_t lse, float a, int n)
 {
     const float2 a2 = make_float2(a, a), e2 = make_float2(LOG2E, LOG2E);
@@ -522,14 +572,14 @@ __device__ __forceinline__ float sum_columns(uint32_t s_at, uint32_t lse, float 
     float x[2][16];
     tmem_ld16(s_at, *reinterpret_cast<uint32_t(*)[16]>(x[0]));
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        if (c >= n) break;
+    for (int c = 0; c < 4; ++c) {
+        if (2 * c >= n) break;
         float (&y)[16] = x[c & 1];
         float4 m[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = lds4f(lse + 64 * c + 16 * i);
+        for (int i = 0; i < 4; ++i) m[i] = lds4f(lse + 128 * c + 16 * i);
         tmem_ld_wait();
-        if (c + 1 < 8) tmem_ld16(s_at + 16 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(x[(c + 1) & 1]));
+        if (c + 1 < 4) tmem_ld16(s_at + 32 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(x[(c + 1) & 1]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 u = mul2(fma2(make_float2(y[4 * i], y[4 * i + 1]), a2, make_float2(m[i].x, m[i].y)), e2);
@@ -553,8 +603,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(base + L::K_FULL + 8 * i, 1);
-            mbar_init(base + L::K_FREE + 8 * i, 4);
-            mbar_init(base + L::A_FULL + 8 * i, 4);
+            mbar_init(base + L::K_FREE + 8 * i, 8);
+            mbar_init(base + L::A_FULL + 8 * i, 8);
         }
         for (int i = 0; i < L::QST; ++i) {
             mbar_init(base + L::Q_FULL + 8 * i, 1);
@@ -562,11 +612,15 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         }
         for (int i = 0; i < L::MST; ++i) {
             mbar_init(base + L::M_FULL + 8 * i, 1);
-            mbar_init(base + L::M_FREE + 8 * i, 8);
+            mbar_init(base + L::M_FREE + 8 * i, 16);
         }
         for (int i = 0; i < 4; ++i) {
             mbar_init(base + L::S_FULL + 8 * i, 1);
-            mbar_init(base + L::S_FREE + 8 * i, 4);
+            mbar_init(base + L::S_FREE + 8 * i, 8);
+        }
+        for (int i = 0; i < 8; ++i) {
+            mbar_init(base + L::H_FULL + 8 * i, 1);
+            mbar_init(base + L::H_FREE + 8 * i, 1);
         }
         mbar_init(base + L::DRAIN, 1);
         *dead = 0;
@@ -615,54 +669,49 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 ++used[w];
             }
         };
-        Unit u = it.get(p, per);
-        load_keys(u);
-        while (ok && it.more()) {
-            it.at += it.step;
-            Unit v = u;
-            const bool next = it.more();
-            if (next) v = it.get(p, per);
-            for (int r = u.r0; r < u.r1; ++r, ++n) {
-                const int i0 = r * per, m = min(per, u.l.ntok - i0);
-                const int32_t *order = p.plan + p.order_at + u.l.tok + i0;
-                int tok[4];
-                bool run = true;
-                const int tok0 = __ldg(order);
+        Steps s(p, it, per);
+        load_keys(s.u);
+        int tok[4];
+        auto look_up = [&](const Steps &x, int (&t)[4]) {
+            const int m = x.tokens(per);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) t[k] = lane + 32 * k < m ? x.token(p, per, lane + 32 * k) : -1;
+        };
+        look_up(s, tok);
+        while (ok && s.live) {
+            Steps t = s;
+            t.advance(p, per);
+            int ahead[4] = {0, 0, 0, 0};
+            if (t.live) look_up(t, ahead);
+            const int m = s.tokens(per), tok0 = __shfl_sync(0xffffffffu, tok[0], 0), kh = s.u.kh;
+            bool run = true;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) run = run && (lane + 32 * k >= m || tok[k] == tok0 + lane + 32 * k);
+            run = __all_sync(0xffffffffu, run);
+            if (n >= (uint32_t)L::QST) ok = wait_bar(base + L::Q_FREE + 8 * st, ph ^ 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const uint32_t full = base + L::Q_FULL + 8 * st, to = base + L::Q + st * L::Q_TILE;
+            if (lane == 0) mbar_expect_tx(full, (run ? per : m) * q_bytes);
+            __syncwarp();
+            if (run) {
+                if (lane < L::D / 64) tma_load_3d(to + lane * (128 * 128), &p.qmap, 64 * lane, kh * G, tok0, full);
+            } else {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int i = lane + 32 * k;
-                    tok[k] = i < m ? __ldg(order + i) : tok0 + i;
-                    run = run && tok[k] == tok0 + i;
-                }
-                run = __all_sync(0xffffffffu, run);
-                if (n >= (uint32_t)L::QST) ok = wait_bar(base + L::Q_FREE + 8 * st, ph ^ 1, dead);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                const uint32_t full = base + L::Q_FULL + 8 * st, to = base + L::Q + st * L::Q_TILE;
-                if (lane == 0) mbar_expect_tx(full, (run ? per : m) * q_bytes);
-                __syncwarp();
-                if (run) {
-                    if (lane < L::D / 64) tma_load_3d(to + lane * (128 * 128), &p.qmap, 64 * lane, u.kh * G, tok0, full);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int i = lane + 32 * k;
-                        if (i < m)
-                            for (int h = 0; h < L::D / 64; ++h)
-                                tma_load_3d(to + h * (128 * 128) + i * G * 128, &p.qmap1, 64 * h, u.kh * G, tok[k], full);
-                    }
-                }
-                __syncwarp();
-                if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
-                if (r == u.r0 && next) {  // (this unit's codes are widened before its first products)
-                    load_keys(v);
-                    if (!ok) {
-                        ++n;
-                        break;
-                    }
+                    if (i < m)
+                        for (int h = 0; h < L::D / 64; ++h)
+                            tma_load_3d(to + h * (128 * 128) + i * G * 128, &p.qmap1, 64 * h, kh * G, tok[k], full);
                 }
             }
-            u = v;
+            __syncwarp();
+            ++n;
+            if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
+            if (s.r == s.u.r0 && s.next) load_keys(s.v);  // (this unit's codes are widened before its first products)
+            s = t;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) tok[k] = ahead[k];
         }
         if (!ok) {  // copies in flight land before the CTA ends
             if (lane == 0) {
@@ -725,40 +774,57 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         }
     } else if (warp == 2) {
         // ------------------------------------------------ the steps' log-sums, and how many tokens their rows see
-        uint32_t n = 0;
-        Unit u = it.get(p, per);
-        while (it.more() && ok) {
-            it.at += it.step;
-            Unit v = u;
-            if (it.more()) v = it.get(p, per);
-            for (int r = u.r0; r < u.r1; ++r, ++n) {
-                const int i0 = r * per, m = min(per, u.l.ntok - i0);
-                float lse[4];
-                int lim[4];
+        // (a step's log-sums are fetched while the one's before are put, its tokens one step earlier still: one behind the other they took
+        // 1.3 us a step, as long as two steps' products)
+        int row_token[4], row_head[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = lane + 32 * k, i = row / G;
-                    lse[k] = 0.f;
-                    lim[k] = 0;
-                    if (i < m) {
-                        const int t = __ldg(p.plan + p.order_at + u.l.tok + i0 + i);
-                        lse[k] = -__ldg(p.lse + (int64_t)t * p.n_heads + u.kh * G + row - i * G);
-                        lim[k] = u.l.lim + (u.l.causal ? i0 + i : 0);
-                    }
-                }
-                const uint32_t s = n % L::MST, to = base + L::META + s * L::M_BUF + 4 * lane;
-                if (n >= (uint32_t)L::MST) ok = wait_bar(base + L::M_FREE + 8 * s, (n / L::MST - 1) & 1, dead);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
+        for (int k = 0; k < 4; ++k) {
+            row_token[k] = (lane + 32 * k) / G;
+            row_head[k] = lane + 32 * k - row_token[k] * G;
+        }
+        auto look_up = [&](const Steps &x, int (&t)[4]) {
+            const int m = x.tokens(per);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    stsf(to + L::M_LSE + 128 * k, lse[k]);
-                    sts32(to + L::M_LIM + 128 * k, (uint32_t)lim[k]);
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive_release(base + L::M_FULL + 8 * s);
+            for (int k = 0; k < 4; ++k) {
+                t[k] = row_token[k] < m ? x.token(p, per, row_token[k]) : -1;
             }
-            u = v;
+        };
+        auto fetch = [&](const Steps &x, const int (&t)[4], float (&lse)[4]) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) lse[k] = t[k] < 0 ? 0.f : -__ldg(p.lse + (int64_t)t[k] * p.n_heads + x.u.kh * G + row_head[k]);
+        };
+        Steps s(p, it, per);
+        int tok[4];
+        float lse[4];
+        look_up(s, tok);
+        fetch(s, tok, lse);
+        Steps t = s;
+        t.advance(p, per);
+        if (t.live) look_up(t, tok);
+        for (uint32_t n = 0; s.live; ++n) {
+            float lse_next[4] = {0.f, 0.f, 0.f, 0.f};
+            if (t.live) fetch(t, tok, lse_next);
+            Steps next = t;
+            if (t.live) {
+                next.advance(p, per);
+                if (next.live) look_up(next, tok);
+            }
+            const uint32_t slot = n % L::MST, to = base + L::META + slot * L::M_BUF + 4 * lane;
+            if (n >= (uint32_t)L::MST) ok = wait_bar(base + L::M_FREE + 8 * slot, (n / L::MST - 1) & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const int m = s.tokens(per);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int i = row_token[k];
+                stsf(to + L::M_LSE + 128 * k, lse[k]);
+                sts32(to + L::M_LIM + 128 * k, i < m ? (uint32_t)(s.u.l.lim + (s.u.l.causal ? s.r * per + i : 0)) : 0u);
+                lse[k] = lse_next[k];
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(base + L::M_FULL + 8 * slot);
+            s = t;
+            t = next;
         }
         if (!ok && lane == 0) {
             *dead = 1;
@@ -766,9 +832,9 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         }
     } else if (warp >= 4) {
         // ------------------------------------------------ a thread's token: its rows of scores, its weight
-        const int w = (warp - 4) >> 2, me = tid & 127;
+        const int w = (warp - 4) >> 2 & 1, half = (warp - 4) >> 3, me = tid & 127;
         const uint32_t s_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
-        uint32_t n = 0, steps = 0, units = 0;
+        uint32_t n = 0, steps = 0, units = 0, done = 0;
         float a = 0.f;
         uint32_t at = 0;
         // the unit's codes to bf16; its exponent and row
@@ -776,7 +842,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             ok = ok && wait_bar(base + L::K_FULL + 8 * w, units & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) return;
-            widen_key<L>(base, w, me);
+            widen_key<L>(base, w, me, half);
             a = p.scale * row_scale(lds8(base + L::EXPS + 128 * w + me));
             at = lds32(base + L::ROWS + 32 * w + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
             __syncwarp();
@@ -799,7 +865,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             const uint32_t at_now = at;
             const bool live = mine && j < u.l.len;
             float was = 0.f, total = 0.f;
-            if (live && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
+            if (live && !half && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
             if (!mine && next && v.two) widen();
             for (int r = u.r0; r < u.r1; ++r, ++n) {
                 const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF, b = steps & 1, s = 2 * w + b;
@@ -817,9 +883,9 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                     const int i0 = r * per, cols = min(per, u.l.ntok - i0) * G;
                     const int full = u.l.causal && end > u.l.lim + i0 ? 0 : cols / 16;
                     const uint32_t s_at = s_base + b * 128;
-                    float sum = full ? sum_columns(s_at, meta + L::M_LSE, a_now, full) : 0.f;
+                    float sum = full > half ? sum_columns(s_at + 16 * half, meta + L::M_LSE + 64 * half, a_now, full - half) : 0.f;
 #pragma unroll 1
-                    for (int c = 16 * full; c < cols; c += 4) {
+                    for (int c = 16 * full + 4 * half; c < cols; c += 8) {
                         float x[4];
                         tmem_ld4(s_at + c, reinterpret_cast<uint32_t *>(x));
                         const float4 l = lds4f(meta + L::M_LSE + 4 * c);
@@ -844,16 +910,36 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 }
             }
             if (!ok) break;
-            if (mine && u.split < 0) {
+            // the two warpgroups' sums
+            if (mine) {
+                const uint32_t at_h = base + L::HALF + 512 * w + 4 * me, pair = 4 * w + (warp & 3), full = base + L::H_FULL + 8 * pair, free = base + L::H_FREE + 8 * pair;
+                if (half) {
+                    if (done > 0) ok = wait_bar(free, (done - 1) & 1, dead);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    stsf(at_h, total);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release(full);
+                } else {
+                    ok = __all_sync(0xffffffffu, wait_bar(full, done & 1, dead));
+                    if (!ok) break;
+                    total += ldsf(at_h);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_release(free);
+                }
+                ++done;
+            }
+            if (!mine || half) {
+            } else if (u.split < 0) {
                 if (live) p.weights[at_now] = was + total;
-            } else if (mine) {
+            } else {
                 // the warp that comes last adds up the parts, in their order
                 const int parts = (u.split & 63) + 1, part = (u.split >> 6) & 63, slot = u.split >> 12;
                 float *mine_at = p.part + (int64_t)slot * TRACK_MANY_TILE + w * 128 + me;
                 __stcg(mine_at + part * TRACK_MANY_TILE, total);
                 __threadfence();
                 __syncwarp();
-                uint32_t *count = p.arrived + slot * 8 + (warp - 4);
+                uint32_t *count = p.arrived + slot * 8 + 4 * w + (warp & 3);
                 int before = 0;
                 if (lane == 0) before = (int)atomicAdd(count, 1u);
                 before = __shfl_sync(0xffffffffu, before, 0);
