@@ -429,11 +429,13 @@ template <int D_>
 struct Many {
     static constexpr int D = D_;
     static constexpr int THREADS = 128 + 4 * 128;
-    static constexpr int QST = D == 128 ? 3 : 6, MST = 4;   // stages of queries, and of what goes with a step
-    static constexpr uint32_t TM_COLS = 512;                // two buffers of 128 scores for either 128 tokens
-    static constexpr uint32_t A_TILE = 128 * 2 * D, RAW_TILE = 128 * D, Q_TILE = 128 * 2 * D;
-    static constexpr uint32_t A = 0;
-    static constexpr uint32_t RAW = A + 2 * A_TILE;
+    static constexpr int QST = D == 128 ? 4 : 6, MST = 4;   // stages of queries, and of what goes with a step
+    // Tensor memory: the keys of either 128 tokens as bf16, three buffers of 128 scores for both in turn.  (With the keys in shared
+    // memory a step's products read 128 KB from there, as long as they take themselves, besides all else: 277 us where this took 253.)
+    static constexpr int SB = 3;
+    static constexpr uint32_t TM_A = 0, TM_S = 128, TM_COLS = 512;
+    static constexpr uint32_t RAW_TILE = 128 * D, Q_TILE = 128 * 2 * D;
+    static constexpr uint32_t RAW = 0;
     static constexpr uint32_t Q = RAW + 2 * RAW_TILE;
     static constexpr uint32_t M_LSE = 0, M_LIM = 512, M_BUF = 1024;
     static constexpr uint32_t META = Q + QST * Q_TILE;
@@ -449,12 +451,13 @@ struct Many {
     static constexpr uint32_t Q_FREE = Q_FULL + 8 * QST;
     static constexpr uint32_t M_FULL = Q_FREE + 8 * QST;
     static constexpr uint32_t M_FREE = M_FULL + 8 * MST;
-    static constexpr uint32_t S_FULL = M_FREE + 8 * MST;    // [warpgroup][buffer]
-    static constexpr uint32_t S_FREE = S_FULL + 32;
-    static constexpr uint32_t DRAIN = S_FREE + 32;
+    static constexpr uint32_t S_FULL = M_FREE + 8 * MST;
+    static constexpr uint32_t S_FREE = S_FULL + 8 * SB;
+    static constexpr uint32_t DRAIN = S_FREE + 8 * SB;
     static constexpr uint32_t MISC = DRAIN + 8;
     static constexpr uint32_t BYTES = MISC + 8 + 1024;
     static_assert(BYTES + 1024 <= 228 * 1024, "shared memory of an SM");
+    static_assert(TM_S + SB * 128 <= TM_COLS && D <= 128, "tensor memory");
 };
 
 struct Unit {
@@ -539,11 +542,11 @@ struct Steps {
     }
 };
 
-// Widens half of a token's key: its row of codes to bf16, 128-byte swizzled halves of 64 elements.
+// Widens half of a token's key: its codes to bf16, two a column of the token's lane of tensor memory.
 template <class L>
-__device__ __forceinline__ void widen_key(uint32_t base, int wg, int me, int half)
+__device__ __forceinline__ void widen_key(uint32_t base, uint32_t to, int wg, int me, int half)
 {
-    const uint32_t from = base + L::RAW + wg * L::RAW_TILE, to = base + L::A + wg * L::A_TILE;
+    const uint32_t from = base + L::RAW + wg * L::RAW_TILE;
 #pragma unroll
     for (int k = 0; k < L::D / 32; ++k) {
         const int c = half * (L::D / 32) + k;
@@ -557,11 +560,9 @@ __device__ __forceinline__ void widen_key(uint32_t base, int wg, int me, int hal
             const __nv_bfloat162 b = __floats2bfloat162_rn(f.x, f.y);
             y[i] = *reinterpret_cast<const uint32_t *>(&b);
         }
-        const uint32_t half = to + (c / 4) * (128 * 128);
-        sts128(half + swz128(me, (c % 4) * 2), y[0], y[1], y[2], y[3]);
-        sts128(half + swz128(me, (c % 4) * 2 + 1), y[4], y[5], y[6], y[7]);
+        tmem_st8(to + 8 * c, y);
     }
-    fence_async_smem();
+    tmem_st_wait();
 }
 
 // The sum over every other sixteen of columns [0, 16 n) of a thread's scores, from the first or second on; none of them is masked.
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             mbar_init(base + L::M_FULL + 8 * i, 1);
             mbar_init(base + L::M_FREE + 8 * i, 16);
         }
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < L::SB; ++i) {
             mbar_init(base + L::S_FULL + 8 * i, 1);
             mbar_init(base + L::S_FREE + 8 * i, 8);
         }
@@ -726,7 +727,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         // ------------------------------------------------ MMA issue
         const bool lead = elect_one();
         const uint32_t id = idesc_bf16_f32(128, (per * G + 15) / 16 * 16);
-        uint32_t st = 0, ph = 0, units[2] = {0, 0}, steps[2] = {0, 0};
+        uint32_t st = 0, ph = 0, units[2] = {0, 0}, job = 0;  // (a job: a step's scores of 128 tokens)
         Unit u = it.get(p, per);
         while (it.more() && ok) {
             it.at += it.step;
@@ -738,21 +739,20 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
 #pragma unroll
                 for (int w = 0; w < 2; ++w) {
                     if (w == 1 && !u.two) break;
-                    const uint32_t b = steps[w] & 1, s = 2 * w + b;
+                    const uint32_t b = job % L::SB;
                     if (r == u.r0) ok = ok && wait_bar(base + L::A_FULL + 8 * w, units[w] & 1, dead);
-                    if (steps[w] > 1) ok = ok && wait_bar(base + L::S_FREE + 8 * s, ((steps[w] >> 1) - 1) & 1, dead);
+                    if (job >= (uint32_t)L::SB) ok = ok && wait_bar(base + L::S_FREE + 8 * b, (job / L::SB - 1) & 1, dead);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint64_t ad = sdesc_kmajor_sw128(base + L::A + w * L::A_TILE);
                     if (lead) {
 #pragma unroll
                         for (int k = 0; k < L::D / 16; ++k)
-                            umma_bf16(tmem + s * 128, ad + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), qd + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), id, k > 0);
-                        umma_commit(base + L::S_FULL + 8 * s);
+                            umma_bf16_ta(tmem + L::TM_S + b * 128, tmem + L::TM_A + w * 64 + 8 * k, qd + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), id, k > 0);
+                        umma_commit(base + L::S_FULL + 8 * b);
                     }
                     __syncwarp();
-                    ++steps[w];
+                    ++job;
                 }
                 if (!ok) break;
                 if (lead) umma_commit(base + L::Q_FREE + 8 * st);
@@ -833,8 +833,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     } else if (warp >= 4) {
         // ------------------------------------------------ a thread's token: its rows of scores, its weight
         const int w = (warp - 4) >> 2 & 1, half = (warp - 4) >> 3, me = tid & 127;
-        const uint32_t s_base = tmem + ((uint32_t)((warp & 3) * 32) << 16) + w * 256;
-        uint32_t n = 0, steps = 0, units = 0, done = 0;
+        const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t n = 0, job = w, units = 0, done = 0;  // (the next job of this tile)
         float a = 0.f;
         uint32_t at = 0;
         // the unit's codes to bf16; its exponent and row
@@ -842,7 +842,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             ok = ok && wait_bar(base + L::K_FULL + 8 * w, units & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) return;
-            widen_key<L>(base, w, me, half);
+            widen_key<L>(base, t_lane + L::TM_A + w * 64, w, me, half);
+            tc_fence_before();
             a = p.scale * row_scale(lds8(base + L::EXPS + 128 * w + me));
             at = lds32(base + L::ROWS + 32 * w + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
             __syncwarp();
@@ -868,9 +869,9 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             if (live && !half && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
             if (!mine && next && v.two) widen();
             for (int r = u.r0; r < u.r1; ++r, ++n) {
-                const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF, b = steps & 1, s = 2 * w + b;
+                const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF, b = job % L::SB;
                 ok = ok && wait_bar(base + L::M_FULL + 8 * ms, (n / L::MST) & 1, dead);
-                if (mine) ok = ok && wait_bar(base + L::S_FULL + 8 * s, (steps >> 1) & 1, dead);
+                if (mine) ok = ok && wait_bar(base + L::S_FULL + 8 * b, (job / L::SB) & 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (mine) {
@@ -882,7 +883,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                     }
                     const int i0 = r * per, cols = min(per, u.l.ntok - i0) * G;
                     const int full = u.l.causal && end > u.l.lim + i0 ? 0 : cols / 16;
-                    const uint32_t s_at = s_base + b * 128;
+                    const uint32_t s_at = t_lane + L::TM_S + b * 128;
                     float sum = full > half ? sum_columns(s_at + 16 * half, meta + L::M_LSE + 64 * half, a_now, full - half) : 0.f;
 #pragma unroll 1
                     for (int c = 16 * full + 4 * half; c < cols; c += 8) {
@@ -901,13 +902,13 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                     }
                     total += sum;
                     tc_fence_before();
-                    ++steps;
                 }
                 __syncwarp();
                 if (lane == 0) {
-                    if (mine) mbar_arrive_release(base + L::S_FREE + 8 * s);
+                    if (mine) mbar_arrive_release(base + L::S_FREE + 8 * b);
                     mbar_arrive_release(base + L::M_FREE + 8 * ms);
                 }
+                job += u.two ? 2 : 1;
             }
             if (!ok) break;
             // the two warpgroups' sums
