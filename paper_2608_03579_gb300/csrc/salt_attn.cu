@@ -1546,7 +1546,7 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
         }
     }
     // a part takes at least what a unit costs besides its steps, a few times over
-    const int64_t share = sum * KV / n_sm, most = std::max<int64_t>(LEAST_STEPS, share / 3);
+    const int64_t share = sum * KV / n_sm, most = std::max<int64_t>(LEAST_STEPS, share / 2);
     struct Piece {
         int cost, kh, from, to, split;
         const Tile *tile;

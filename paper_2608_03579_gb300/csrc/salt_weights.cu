@@ -424,11 +424,13 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
 
 // ---------------------------------------------------------------- many rows
 // A unit is 256 tokens of a list and head, and a run of steps over the rows that see them, up to 128 at
-// a time.  Two warpgroups have 128 tokens, each every other sixteen of the step's columns.
+// a time.  Either 128 tokens have two warpgroups, which take every other step each: what a step costs besides its sums (waiting, a vote, fetching scores; 600
+// cycles of 2,100) is spent beside the others' sums.  (With one warpgroup 268 us where these take 236; with two of half a step's columns each, which
+// meet at every barrier, 260.)
 template <int D_>
 struct Many {
     static constexpr int D = D_;
-    static constexpr int THREADS = 128 + 4 * 128;
+    static constexpr int THREADS = 96 + 4 * 128;            // (104 registers a thread; with a warp more 96, and scores spilled while they were fetched)
     static constexpr int QST = D == 128 ? 4 : 6, MST = 4;   // stages of queries, and of what goes with a step
     // Tensor memory: the keys of either 128 tokens as bf16, three buffers of 128 scores for both in turn.  (With the keys in shared
     // memory a step's products read 128 KB from there, as long as they take themselves, besides all else: 277 us where this took 253.)
@@ -451,8 +453,10 @@ struct Many {
     static constexpr uint32_t Q_FREE = Q_FULL + 8 * QST;
     static constexpr uint32_t M_FULL = Q_FREE + 8 * QST;
     static constexpr uint32_t M_FREE = M_FULL + 8 * MST;
+    // Of scores that are there two barriers for each warpgroup: of the three jobs at most that have a buffer it has two at most.  (By buffers, a
+    // warpgroup would wait for the second use to come of one that had its last while it was busy.)
     static constexpr uint32_t S_FULL = M_FREE + 8 * MST;
-    static constexpr uint32_t S_FREE = S_FULL + 8 * SB;
+    static constexpr uint32_t S_FREE = S_FULL + 64;
     static constexpr uint32_t DRAIN = S_FREE + 8 * SB;
     static constexpr uint32_t MISC = DRAIN + 8;
     static constexpr uint32_t BYTES = MISC + 8 + 1024;
@@ -542,14 +546,13 @@ struct Steps {
     }
 };
 
-// Widens half of a token's key: its codes to bf16, two a column of the token's lane of tensor memory.
+// Widens a token's key: its codes to bf16, two a column of the token's lane of tensor memory.
 template <class L>
-__device__ __forceinline__ void widen_key(uint32_t base, uint32_t to, int wg, int me, int half)
+__device__ __forceinline__ void widen_key(uint32_t base, uint32_t to, int wg, int me)
 {
     const uint32_t from = base + L::RAW + wg * L::RAW_TILE;
 #pragma unroll
-    for (int k = 0; k < L::D / 32; ++k) {
-        const int c = half * (L::D / 32) + k;
+    for (int c = 0; c < L::D / 16; ++c) {
         const uint4 x = lds128(from + swz_rows<L::D>(me * L::D + c * 16));
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
         uint32_t y[8];
@@ -565,32 +568,18 @@ __device__ __forceinline__ void widen_key(uint32_t base, uint32_t to, int wg, in
     tmem_st_wait();
 }
 
-// The sum over every other sixteen of columns [0, 16 n) of a thread's scores, from the first or second on; none of them is masked.
-__device__ __forceinline__ float sum_columns(uint32_t s_at, uint32_t lse, float a, int n)
+// Adds the terms of 16 columns' scores, none of them masked.
+__device__ __forceinline__ void add_columns(const float (&y)[16], uint32_t lse, float a, float2 (&sum)[2])
 {
     const float2 a2 = make_float2(a, a), e2 = make_float2(LOG2E, LOG2E);
-    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-    float x[2][16];
-    tmem_ld16(s_at, *reinterpret_cast<uint32_t(*)[16]>(x[0]));
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        if (2 * c >= n) break;
-        float (&y)[16] = x[c & 1];
-        float4 m[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = lds4f(lse + 128 * c + 16 * i);
-        tmem_ld_wait();
-        if (c + 1 < 4) tmem_ld16(s_at + 32 * (c + 1), *reinterpret_cast<uint32_t(*)[16]>(x[(c + 1) & 1]));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 u = mul2(fma2(make_float2(y[4 * i], y[4 * i + 1]), a2, make_float2(m[i].x, m[i].y)), e2);
-            const float2 v = mul2(fma2(make_float2(y[4 * i + 2], y[4 * i + 3]), a2, make_float2(m[i].z, m[i].w)), e2);
-            sum[0] = add2(sum[0], make_float2(ex2(u.x), ex2(u.y)));
-            sum[1] = add2(sum[1], make_float2(ex2(v.x), ex2(v.y)));
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float4 m = lds4f(lse + 16 * i);
+        const float2 u = mul2(fma2(make_float2(y[4 * i], y[4 * i + 1]), a2, make_float2(m.x, m.y)), e2);
+        const float2 v = mul2(fma2(make_float2(y[4 * i + 2], y[4 * i + 3]), a2, make_float2(m.z, m.w)), e2);
+        sum[0] = add2(sum[0], make_float2(ex2(u.x), ex2(u.y)));
+        sum[1] = add2(sum[1], make_float2(ex2(v.x), ex2(v.y)));
     }
-    tmem_ld_wait();
-    return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
 
 template <class L>
@@ -605,7 +594,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         for (int i = 0; i < 2; ++i) {
             mbar_init(base + L::K_FULL + 8 * i, 1);
             mbar_init(base + L::K_FREE + 8 * i, 8);
-            mbar_init(base + L::A_FULL + 8 * i, 8);
+            mbar_init(base + L::A_FULL + 8 * i, 4);
         }
         for (int i = 0; i < L::QST; ++i) {
             mbar_init(base + L::Q_FULL + 8 * i, 1);
@@ -613,12 +602,10 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         }
         for (int i = 0; i < L::MST; ++i) {
             mbar_init(base + L::M_FULL + 8 * i, 1);
-            mbar_init(base + L::M_FREE + 8 * i, 16);
+            mbar_init(base + L::M_FREE + 8 * i, 8);
         }
-        for (int i = 0; i < L::SB; ++i) {
-            mbar_init(base + L::S_FULL + 8 * i, 1);
-            mbar_init(base + L::S_FREE + 8 * i, 8);
-        }
+        for (int i = 0; i < 8; ++i) mbar_init(base + L::S_FULL + 8 * i, 1);
+        for (int i = 0; i < L::SB; ++i) mbar_init(base + L::S_FREE + 8 * i, 4);
         for (int i = 0; i < 8; ++i) {
             mbar_init(base + L::H_FULL + 8 * i, 1);
             mbar_init(base + L::H_FREE + 8 * i, 1);
@@ -727,7 +714,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         // ------------------------------------------------ MMA issue
         const bool lead = elect_one();
         const uint32_t id = idesc_bf16_f32(128, (per * G + 15) / 16 * 16);
-        uint32_t st = 0, ph = 0, units[2] = {0, 0}, job = 0;  // (a job: a step's scores of 128 tokens)
+        uint32_t st = 0, ph = 0, units[2] = {0, 0}, job = 0, n = 0, odd = 0;  // (odd: a bit a warpgroup; a job: a step's scores of 128 tokens)
         Unit u = it.get(p, per);
         while (it.more() && ok) {
             it.at += it.step;
@@ -749,14 +736,16 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
 #pragma unroll
                         for (int k = 0; k < L::D / 16; ++k)
                             umma_bf16_ta(tmem + L::TM_S + b * 128, tmem + L::TM_A + w * 64 + 8 * k, qd + (k / 4) * (128 * 128 / 16) + 2 * (k % 4), id, k > 0);
-                        umma_commit(base + L::S_FULL + 8 * b);
+                        umma_commit(base + L::S_FULL + 16 * (2 * w + (n & 1)) + 8 * (odd >> (2 * w + (n & 1)) & 1));
                     }
                     __syncwarp();
+                    odd ^= 1u << (2 * w + (n & 1));
                     ++job;
                 }
                 if (!ok) break;
                 if (lead) umma_commit(base + L::Q_FREE + 8 * st);
                 __syncwarp();
+                ++n;
                 if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
             }
             ++units[0];
@@ -830,66 +819,99 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             *dead = 1;
             atomicOr(p.err, SALT_DEVERR_TIMEOUT);
         }
-    } else if (warp >= 4) {
+    } else {
         // ------------------------------------------------ a thread's token: its rows of scores, its weight
-        const int w = (warp - 4) >> 2 & 1, half = (warp - 4) >> 3, me = tid & 127;
+        const int w = (warp - 3) >> 2 & 1, par = (warp - 3) >> 3, me = 32 * (warp & 3) + lane;  // the 128 tokens, the steps
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-        uint32_t n = 0, job = w, units = 0, done = 0;  // (the next job of this tile)
+        uint32_t n = 0, b = w, jobs = 0, units = 0, done = 0;  // (b: the buffer of the step's job)
         float a = 0.f;
         uint32_t at = 0;
-        // the unit's codes to bf16; its exponent and row
-        auto widen = [&]() {
+        // the next unit's exponent and row, and by one of the two warpgroups its codes to bf16
+        auto take_up = [&](bool widen) {
             ok = ok && wait_bar(base + L::K_FULL + 8 * w, units & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) return;
-            widen_key<L>(base, t_lane + L::TM_A + w * 64, w, me, half);
-            tc_fence_before();
+            if (widen) {
+                widen_key<L>(base, t_lane + L::TM_A + w * 64, w, me);
+                tc_fence_before();
+            }
             a = p.scale * row_scale(lds8(base + L::EXPS + 128 * w + me));
             at = lds32(base + L::ROWS + 32 * w + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive_release(base + L::K_FREE + 8 * w);
-                mbar_arrive_release(base + L::A_FULL + 8 * w);
+                if (widen) mbar_arrive_release(base + L::A_FULL + 8 * w);
             }
             ++units;
         };
         Unit u = it.get(p, per);
-        if (w == 0 || u.two) widen();
+        if (w == 0 || u.two) take_up(par == 0);
         while (ok && it.more()) {
             it.at += it.step;
-            Unit v = u;
-            const bool next = it.more();
-            if (next) v = it.get(p, per);
-            const bool mine = w == 0 || u.two;
+            // (all of the next unit's words are read when it begins, from the L1 then)
+            const bool next = it.more(), next_two = next && it.get(p, per).two, mine = w == 0 || u.two, theirs = next && (w == 0 || next_two);
+            // the unit's last step is this warpgroup's: when its products are done the next unit's keys take its keys' place
+            const bool last = ((n + (uint32_t)(u.r1 - u.r0) - 1) & 1) == (uint32_t)par;
             const int j = u.t0 + 128 * w + me, end = min(u.t0 + 128 * (w + 1), u.l.len);
             const float a_now = a;
             const uint32_t at_now = at;
             const bool live = mine && j < u.l.len;
-            float was = 0.f, total = 0.f;
-            if (live && !half && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
-            if (!mine && next && v.two) widen();
-            for (int r = u.r0; r < u.r1; ++r, ++n) {
-                const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF, b = job % L::SB;
+            float total = 0.f;
+            // (the first one knows of both that they are done with the unit before)
+            if (!mine && theirs) take_up(par == 0);
+            for (int r = u.r0; r < u.r1; ++r, ++n, b += u.two ? 2 : 1) {
+                if (b >= (uint32_t)L::SB) b -= L::SB;
+                if ((n & 1) != (uint32_t)par) continue;
+                const uint32_t ms = n % L::MST, meta = base + L::META + ms * L::M_BUF;
                 ok = ok && wait_bar(base + L::M_FULL + 8 * ms, (n / L::MST) & 1, dead);
-                if (mine) ok = ok && wait_bar(base + L::S_FULL + 8 * b, (job / L::SB) & 1, dead);
+                if (mine) ok = ok && wait_bar(base + L::S_FULL + 16 * (2 * w + par) + 8 * (jobs & 1), jobs >> 1 & 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 if (mine) {
+                    ++jobs;
                     tc_fence_after();
-                    // (the unit's last products are done: the next unit's may begin beside this step's sums)
-                    if (r + 1 == u.r1 && next && (w == 0 || v.two)) {
-                        widen();
+                    if (r + 1 == u.r1 && theirs) {
+                        take_up(true);
                         if (!ok) break;
                     }
                     const int i0 = r * per, cols = min(per, u.l.ntok - i0) * G;
                     const int full = u.l.causal && end > u.l.lim + i0 ? 0 : cols / 16;
-                    const uint32_t s_at = t_lane + L::TM_S + b * 128;
-                    float sum = full > half ? sum_columns(s_at + 16 * half, meta + L::M_LSE + 64 * half, a_now, full - half) : 0.f;
+                    const uint32_t s_at = t_lane + L::TM_S + b * 128, lse = meta + L::M_LSE;
+                    auto free = [&]() {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_release(base + L::S_FREE + 8 * b);
+                    };
+                    float2 sums[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+                    if (full == 8) {  // the scores' place is free once they are in registers
+                        float x[2][16];
+                        auto load = [&](int c) { tmem_ld16(s_at + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(x[c & 1])); };
+                        load(0);
+                        load(1);
+#pragma unroll
+                        for (int c = 0; c < 8; c += 2) {
+                            tmem_ld_wait();
+                            if (c == 6) free();
+                            add_columns(x[0], lse + 64 * c, a_now, sums);
+                            if (c < 6) load(c + 2);
+                            add_columns(x[1], lse + 64 * c + 64, a_now, sums);
+                            if (c < 6) load(c + 3);
+                        }
+                    } else {
 #pragma unroll 1
-                    for (int c = 16 * full + 4 * half; c < cols; c += 8) {
+                        for (int c = 0; c < full; ++c) {
+                            float x[16];
+                            tmem_ld16(s_at + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(x));
+                            tmem_ld_wait();
+                            add_columns(x, lse + 64 * c, a_now, sums);
+                        }
+                    }
+                    float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
+#pragma unroll 1
+                    for (int c = 16 * full; c < cols; c += 4) {
                         float x[4];
                         tmem_ld4(s_at + c, reinterpret_cast<uint32_t *>(x));
-                        const float4 l = lds4f(meta + L::M_LSE + 4 * c);
+                        const float4 l = lds4f(lse + 4 * c);
                         const uint4 lim = lds128(meta + L::M_LIM + 4 * c);
                         tmem_ld_wait();
                         const float m[4] = {l.x, l.y, l.z, l.w};
@@ -901,20 +923,19 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                         }
                     }
                     total += sum;
-                    tc_fence_before();
+                    if (full < 8) free();
                 }
                 __syncwarp();
-                if (lane == 0) {
-                    if (mine) mbar_arrive_release(base + L::S_FREE + 8 * b);
-                    mbar_arrive_release(base + L::M_FREE + 8 * ms);
-                }
-                job += u.two ? 2 : 1;
+                if (lane == 0) mbar_arrive_release(base + L::M_FREE + 8 * ms);
             }
             if (!ok) break;
-            // the two warpgroups' sums
-            if (mine) {
+            if (mine && theirs && !last) take_up(false);
+            if (!ok) break;
+            float was = 0.f;
+            if (live && par == 0 && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
+            if (mine) {  // the two warpgroups' sums
                 const uint32_t at_h = base + L::HALF + 512 * w + 4 * me, pair = 4 * w + (warp & 3), full = base + L::H_FULL + 8 * pair, free = base + L::H_FREE + 8 * pair;
-                if (half) {
+                if (par) {
                     if (done > 0) ok = wait_bar(free, (done - 1) & 1, dead);
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
@@ -930,7 +951,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 }
                 ++done;
             }
-            if (!mine || half) {
+            if (!mine || par) {
             } else if (u.split < 0) {
                 if (live) p.weights[at_now] = was + total;
             } else {
@@ -938,21 +959,19 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 const int parts = (u.split & 63) + 1, part = (u.split >> 6) & 63, slot = u.split >> 12;
                 float *mine_at = p.part + (int64_t)slot * TRACK_MANY_TILE + w * 128 + me;
                 __stcg(mine_at + part * TRACK_MANY_TILE, total);
-                __threadfence();
                 __syncwarp();
                 uint32_t *count = p.arrived + slot * 8 + 4 * w + (warp & 3);
-                int before = 0;
-                if (lane == 0) before = (int)atomicAdd(count, 1u);
+                uint32_t before = 0;
+                if (lane == 0) asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;\n" : "=r"(before) : "l"(count) : "memory");
                 before = __shfl_sync(0xffffffffu, before, 0);
-                if (before + 1 == parts) {
-                    __threadfence();
+                if ((int)before + 1 == parts) {
                     total = 0.f;
                     for (int i = 0; i < parts; ++i) total += __ldcg(mine_at + i * TRACK_MANY_TILE);
                     if (live) p.weights[at_now] = was + total;
                     if (lane == 0) *count = 0;
                 }
             }
-            u = v;
+            if (next) u = it.get(p, per);
         }
         if (!ok && lane == 0) {
             *dead = 1;
