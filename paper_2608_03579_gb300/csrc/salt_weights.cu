@@ -59,11 +59,8 @@ struct List {
 // The same word in every lane, and known to be: loops and branches by it are taken by whole warps then, and the votes in them are quick (by
 // words that might differ, a vote takes hundreds of cycles).
 __device__ __forceinline__ int one_word(int x) { return __shfl_sync(0xffffffffu, x, 0); }
-__device__ __forceinline__ int4 four_words(const int4 *at)
-{
-    const int4 x = __ldg(at);
-    return make_int4(one_word(x.x), one_word(x.y), one_word(x.z), one_word(x.w));
-}
+__device__ __forceinline__ int4 one_each(const int4 &x) { return make_int4(one_word(x.x), one_word(x.y), one_word(x.z), one_word(x.w)); }
+__device__ __forceinline__ int4 four_words(const int4 *at) { return one_each(__ldg(at)); }
 __device__ __forceinline__ List load_list(const WeightParams &p, int i)
 {
     const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + i * LIST_WORDS);
@@ -126,9 +123,17 @@ struct Few {
 // A CTA's tiles [g, end) of the few rows' lists in the order list, key/value head, tile.  A segment is those of one list and head.
 struct Walk {
     int64_t g, end;
-    int list, kh, j, tiles, segment;
+    int list, n_lists, kh, j, tiles, segment;
     List l;
-    __device__ __forceinline__ Walk(const WeightParams &p, int n_lists, int64_t all)
+    int4 a, b;  // the next list's words, on their way
+    __device__ __forceinline__ void ahead(const WeightParams &p)
+    {
+        if (list + 1 >= n_lists) return;
+        const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + (list + 1) * LIST_WORDS);
+        a = __ldg(w);
+        b = __ldg(w + 1);
+    }
+    __device__ __forceinline__ Walk(const WeightParams &p, int lists, int64_t all) : n_lists(lists)
     {
         const int KV = p.kv.heads;
         g = all * blockIdx.x / gridDim.x;
@@ -141,6 +146,7 @@ struct Walk {
         const int in = (int)(g - (int64_t)l.tiles * KV);
         kh = in / tiles;
         j = in - kh * tiles;
+        ahead(p);
     }
     __device__ __forceinline__ bool more() const { return g < end; }
     __device__ __forceinline__ bool last_of_segment() const { return g + 1 == end || j + 1 == tiles; }
@@ -151,8 +157,11 @@ struct Walk {
         if (++kh == p.kv.heads) {
             kh = 0;
             if (g < end) {
-                l = load_list(p, ++list);
+                ++list;
+                const int4 x = one_each(a), y = one_each(b);
+                l = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
                 tiles = (l.len + TRACK_TILE - 1) / TRACK_TILE;
+                ahead(p);
             }
         }
     }
@@ -276,13 +285,16 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
         // ------------------------------------------------ loads: a lane per page of a tile
         uint32_t ks = 0, kph = 0, es = 0, eph = 0, n = 0;
         const int per = TRACK_TILE >> p.kv.page_log2;
-        for (; k.more() && ok; k.next(p), ++n) {
-            const int t = k.j * TRACK_TILE, first = t >> p.kv.page_log2;
-            const int pages = min(per, ((k.l.len - 1) >> p.kv.page_log2) - first + 1);
-            int page = 0;
-            if (lane < pages) page = __ldg(p.plan + p.pages_at + k.l.pages + first + lane);
+        // (a tile's pages are looked up while the one's before are waited for)
+        auto pages_of = [&](const Walk &x) { return min(per, ((x.l.len - 1) >> p.kv.page_log2) - (x.j * TRACK_TILE >> p.kv.page_log2) + 1); };
+        auto look_up = [&](const Walk &x) { return lane < pages_of(x) ? __ldg(p.plan + p.pages_at + x.l.pages + (x.j * TRACK_TILE >> p.kv.page_log2) + lane) : 0; };
+        int page = look_up(k);
+        for (; k.more() && ok; ++n) {
+            const int t = k.j * TRACK_TILE, pages = pages_of(k);
             const int64_t row = first_row(p, page, k.kh);
             const bool old = p.decay != 0.f && t < k.l.old;
+            k.next(p);
+            if (k.more()) page = look_up(k);
             const uint32_t k_full = base + L::K_FULL + 8 * ks, e_full = base + L::E_FULL + 8 * es, e = base + L::E + es * L::E_BUF;
             if (n >= (uint32_t)L::EST) ok = wait_bar(base + L::E_FREE + 8 * es, eph ^ 1, dead);
             if (ok && n >= (uint32_t)L::KST) ok = wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead);
@@ -438,17 +450,17 @@ struct Many {
     static constexpr uint32_t TM_A = 0, TM_S = 128, TM_COLS = 512;
     static constexpr uint32_t RAW_TILE = 128 * D, Q_TILE = 128 * 2 * D;
     static constexpr uint32_t RAW = 0;
-    static constexpr uint32_t Q = RAW + 2 * RAW_TILE;
+    static constexpr uint32_t Q = RAW + 4 * RAW_TILE;       // (either tile's codes of this unit and the next)
     static constexpr uint32_t M_LSE = 0, M_LIM = 512, M_BUF = 1024;
     static constexpr uint32_t META = Q + QST * Q_TILE;
-    static constexpr uint32_t EXPS = META + MST * M_BUF;    // 128 of either tile
-    static constexpr uint32_t ROWS = EXPS + 256;            // the first rows of either tile's pages
-    static constexpr uint32_t HALF = ROWS + 64;             // the second warpgroup's sums of either tile
+    static constexpr uint32_t EXPS = META + MST * M_BUF;    // 128 of either tile, of two units
+    static constexpr uint32_t ROWS = EXPS + 512;            // the first rows of either tile's pages, of two units
+    static constexpr uint32_t HALF = ROWS + 128;            // the second warpgroup's sums of either tile
     static constexpr uint32_t H_FULL = HALF + 1024;         // a warp's each
     static constexpr uint32_t H_FREE = H_FULL + 64;
     static constexpr uint32_t K_FULL = H_FREE + 64;
-    static constexpr uint32_t K_FREE = K_FULL + 16;
-    static constexpr uint32_t A_FULL = K_FREE + 16;
+    static constexpr uint32_t K_FREE = K_FULL + 32;         // [tile][unit & 1]
+    static constexpr uint32_t A_FULL = K_FREE + 32;
     static constexpr uint32_t Q_FULL = A_FULL + 16;
     static constexpr uint32_t Q_FREE = Q_FULL + 8 * QST;
     static constexpr uint32_t M_FULL = Q_FREE + 8 * QST;
@@ -548,9 +560,8 @@ struct Steps {
 
 // Widens a token's key: its codes to bf16, two a column of the token's lane of tensor memory.
 template <class L>
-__device__ __forceinline__ void widen_key(uint32_t base, uint32_t to, int wg, int me)
+__device__ __forceinline__ void widen_key(uint32_t from, uint32_t to, int me)
 {
-    const uint32_t from = base + L::RAW + wg * L::RAW_TILE;
 #pragma unroll
     for (int c = 0; c < L::D / 16; ++c) {
         const uint4 x = lds128(from + swz_rows<L::D>(me * L::D + c * 16));
@@ -591,11 +602,11 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, KV = p.kv.heads, G = p.n_heads / KV, per = 128 / G;
     volatile int *dead = reinterpret_cast<volatile int *>(sm + L::MISC + 4);
     if (tid == 0) {
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < 4; ++i) {
             mbar_init(base + L::K_FULL + 8 * i, 1);
             mbar_init(base + L::K_FREE + 8 * i, 8);
-            mbar_init(base + L::A_FULL + 8 * i, 4);
         }
+        for (int i = 0; i < 2; ++i) mbar_init(base + L::A_FULL + 8 * i, 4);
         for (int i = 0; i < L::QST; ++i) {
             mbar_init(base + L::Q_FULL + 8 * i, 1);
             mbar_init(base + L::Q_FREE + 8 * i, 1);
@@ -642,23 +653,30 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 int page = 0;
                 if (lane < pages) page = __ldg(p.plan + p.pages_at + u.l.pages + first + lane);
                 const int64_t row = first_row(p, page, u.kh);
-                const uint32_t full = base + L::K_FULL + 8 * w, at = lane * p.kv.page;
-                if (used[w] > 0) ok = wait_bar(base + L::K_FREE + 8 * w, (used[w] - 1) & 1, dead);
+                const uint32_t buf = 2 * w + (used[w] & 1), full = base + L::K_FULL + 8 * buf, at = lane * p.kv.page;
+                if (used[w] > 1) ok = wait_bar(base + L::K_FREE + 8 * buf, ((used[w] >> 1) - 1) & 1, dead);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) return;
-                if (lane < pages) sts32(base + L::ROWS + 32 * w + 4 * lane, (uint32_t)row);
+                if (lane < pages) sts32(base + L::ROWS + 32 * buf + 4 * lane, (uint32_t)row);
                 __syncwarp();
                 if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * (L::D + 1));
                 __syncwarp();
                 if (lane < pages) {
-                    tma_load_2d(base + L::RAW + w * L::RAW_TILE + at * L::D, &p.kmap, 0, (int)row, full);
-                    bulk_load(base + L::EXPS + 128 * w + at, p.kv.k_exp + row, p.kv.page, full);
+                    tma_load_2d(base + L::RAW + buf * L::RAW_TILE + at * L::D, &p.kmap, 0, (int)row, full);
+                    bulk_load(base + L::EXPS + 128 * buf + at, p.kv.k_exp + row, p.kv.page, full);
                 }
                 ++used[w];
             }
         };
+        Units keys = it;  // (two units ahead)
+        auto next_keys = [&]() {
+            if (!ok || !keys.more()) return;
+            load_keys(keys.get(p, per));
+            keys.at += keys.step;
+        };
+        next_keys();
+        next_keys();
         Steps s(p, it, per);
-        load_keys(s.u);
         int tok[4];
         auto look_up = [&](const Steps &x, int (&t)[4]) {
             const int m = x.tokens(per);
@@ -696,7 +714,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             __syncwarp();
             ++n;
             if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
-            if (s.r == s.u.r0 && s.next) load_keys(s.v);  // (this unit's codes are widened before its first products)
+            if (s.r == s.u.r0) next_keys();  // (this unit's codes are widened before its first products)
             s = t;
 #pragma unroll
             for (int k = 0; k < 4; ++k) tok[k] = ahead[k];
@@ -708,7 +726,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             }
             for (uint32_t i = 0; i < min(n, (uint32_t)L::QST); ++i) mbar_wait(base + L::Q_FULL + 8 * ((n - 1 - i) % L::QST), ((n - 1 - i) / L::QST) & 1);
             for (int w = 0; w < 2; ++w)
-                if (used[w] > 0) mbar_wait(base + L::K_FULL + 8 * w, (used[w] - 1) & 1);
+                for (uint32_t i = 0; i < min(used[w], 2u); ++i) mbar_wait(base + L::K_FULL + 8 * (2 * w + ((used[w] - 1 - i) & 1)), ((used[w] - 1 - i) >> 1) & 1);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issue
@@ -828,18 +846,19 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         uint32_t at = 0;
         // the next unit's exponent and row, and by one of the two warpgroups its codes to bf16
         auto take_up = [&](bool widen) {
-            ok = ok && wait_bar(base + L::K_FULL + 8 * w, units & 1, dead);
+            const uint32_t buf = 2 * w + (units & 1);
+            ok = ok && wait_bar(base + L::K_FULL + 8 * buf, units >> 1 & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) return;
             if (widen) {
-                widen_key<L>(base, t_lane + L::TM_A + w * 64, w, me);
+                widen_key<L>(base + L::RAW + buf * L::RAW_TILE, t_lane + L::TM_A + w * 64, me);
                 tc_fence_before();
             }
-            a = p.scale * row_scale(lds8(base + L::EXPS + 128 * w + me));
-            at = lds32(base + L::ROWS + 32 * w + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
+            a = p.scale * row_scale(lds8(base + L::EXPS + 128 * buf + me));
+            at = lds32(base + L::ROWS + 32 * buf + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive_release(base + L::K_FREE + 8 * w);
+                mbar_arrive_release(base + L::K_FREE + 8 * buf);
                 if (widen) mbar_arrive_release(base + L::A_FULL + 8 * w);
             }
             ++units;
