@@ -1294,7 +1294,9 @@ int items_of(const RowTile &x, double most, int *per_item)
 
 // Of a unit of a tracked plan's lists of many rows, in steps of 128 rows: what it costs besides, and the least
 // that a part of one takes.
-constexpr int UNIT_COST = 2, LEAST_STEPS = 6;
+constexpr int UNIT_COST = 3, LEAST_STEPS = 6;
+// Measured: a step on an SM, and a unit of few_cost on one of its CTAs' SM.
+constexpr double STEP_US = 0.95, FEW_US = 0.07;
 
 // Items of one cost.
 struct Same {
@@ -1524,11 +1526,13 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
 // handed to the CTAs from the costliest down, each to the one that has least.  Where units are few or unequal, those of
 // many steps are split in parts, each a unit, that meet in a partial sum.  Where they are very many every CTA
 // takes each n_sm-th instead.
-void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
+void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int64_t few_cost, int32_t *t)
 {
     Track &tr = a->track;
-    const int KV = a->kv->dev.heads, per = 128 / (a->cfg.n_heads / KV), n_sm = a->n_sm;
+    const int KV = a->kv->dev.heads, per = 128 / (a->cfg.n_heads / KV);
+    int n_sm = a->n_sm;
     tr.split = false;
+    tr.many_sms = n_sm;
     t[TH_LISTED] = 0;
     if (n_many == 0 || tiles * KV > TRACK_UNITS / 2 || n_sm + 1 > TRACK_CTAS) return;
     struct Tile {
@@ -1541,10 +1545,16 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
         const int32_t *l = t + tr.list_at + (size_t)i * LIST_WORDS;
         const int steps = (l[3] + per - 1) / per;
         for (int j = 0; j < (l[1] + TRACK_MANY_TILE - 1) / TRACK_MANY_TILE; ++j) {
-            all.push_back({l, j * TRACK_MANY_TILE, first_step(l[6], l[5], j * TRACK_MANY_TILE, per), steps});
+            all.push_back({l, j * TRACK_MANY_TILE, first_step(l[6] & 1, l[5], j * TRACK_MANY_TILE, per), steps});
             sum += steps - all.back().from;
         }
     }
+    // the two kinds of lists run beside each other, on SMs by what they take
+    if (n_few > 0) {
+        const double many_us = STEP_US * (double)(sum + UNIT_COST * (int64_t)all.size()), few_us = FEW_US * (double)few_cost;
+        n_sm = (int)std::min<int64_t>(n_sm - 1, std::max<int64_t>(1, (int64_t)std::llround(n_sm * many_us / (many_us + few_us))));
+    }
+    n_sm = (int)std::min<int64_t>(n_sm, (int64_t)all.size() * KV * 64);
     // a part takes at least what a unit costs besides its steps, a few times over
     const int64_t share = sum * KV / n_sm, most = std::max<int64_t>(LEAST_STEPS, share / 2);
     struct Piece {
@@ -1567,7 +1577,7 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
     }
     if ((int64_t)pieces.size() > TRACK_UNITS) return;
     tr.split = slots > 0;
-    t[TH_LISTED] = 1;
+    t[TH_LISTED] = tr.many_sms = n_sm;
     std::stable_sort(pieces.begin(), pieces.end(), [](const Piece &x, const Piece &y) { return x.cost > y.cost; });
     using Load = std::pair<int64_t, int>;
     std::priority_queue<Load, std::vector<Load>, std::greater<Load>> least;
@@ -1589,7 +1599,7 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int32_t *t)
         const Piece &x = pieces[i];
         int32_t *u = units + (size_t)next[owner[i]]++ * UNIT_WORDS;
         std::memcpy(u, x.tile->list, LIST_WORDS * 4);
-        u[LS_TILES] = x.kh;
+        u[LS_BEFORE] = x.kh;
         u[LIST_WORDS] = x.tile->t0;
         u[LIST_WORDS + 1] = x.from;
         u[LIST_WORDS + 2] = x.to;
@@ -1608,7 +1618,7 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     const int own_pages = b->n_seqs > 0 ? b->page_ptr[b->n_seqs] : 0;
     tr.page_seen.assign(kv.n_pages, 0);
     tr.shared = false;
-    tr.longest = tr.chunks = 0;
+    tr.longest = tr.chunks = tr.few_rows = 0;
     auto note = [&](const int32_t *pages, int len) {
         for (int j = 0; j < (int)(((int64_t)len + kv.page - 1) >> kv.page_log2); ++j) {
             tr.shared |= tr.page_seen[pages[j]] != 0;
@@ -1619,12 +1629,15 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
         int32_t w[LIST_WORDS];
     };
     std::vector<Words> lists[2];   // of few rows, of many
-    int64_t tiles[2] = {0, 0};
+    int64_t tiles[2] = {0, 0}, cost_before[2] = {0, 0};
     auto add = [&](int pages, int len, int tok, int ntok, int old, int lim, bool causal) {
         if (len == 0 || ntok == 0) return;
         const int kind = (int64_t)ntok * G > TRACK_FEW_ROWS, tile = kind ? TRACK_MANY_TILE : TRACK_TILE;
-        lists[kind].push_back({{pages, len, tok, ntok, old, lim, causal, (int)tiles[kind]}});
-        tiles[kind] += (len + tile - 1) / tile;
+        if (!kind) tr.few_rows = std::max(tr.few_rows, ntok * G);
+        const int cost = kind ? 1 : few_cost(ntok * G), n = (len + tile - 1) / tile;
+        lists[kind].push_back({{pages, len, tok, ntok, old, lim, causal | cost << 1, (int)cost_before[kind]}});
+        cost_before[kind] += (int64_t)n * cost;
+        tiles[kind] += n;
     };
     std::vector<int> rows(b->n_groups, 0);  // query tokens of each group
     int t0 = 0;
@@ -1655,11 +1668,11 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     t[TH_SEQS] = tr.n_seqs = b->n_seqs;
     t[TH_FEW] = tr.few = (int)lists[0].size();
     t[TH_MANY] = tr.many = (int)lists[1].size();
-    t[TH_FEW_TILES] = (int)tiles[0];
+    t[TH_FEW_COST] = (int)cost_before[0];
     t[TH_MANY_TILES] = (int)tiles[1];
     t[TH_SHARED] = tr.shared;
     tr.few_tiles = tiles[0];
-    fill_units(a, tr.few, tr.many, tiles[1], t);
+    fill_units(a, tr.few, tr.many, tiles[1], cost_before[0], t);
     return t[TH_LISTED] ? (size_t)tr.unit_at + TRACK_CTAS + (size_t)tr.n_units * UNIT_WORDS : (size_t)(list - t);
 }
 

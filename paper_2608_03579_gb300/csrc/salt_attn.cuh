@@ -17,24 +17,27 @@ constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // que
 
 // What a tracked plan's build writes besides: a table of its own, int32 words.
 constexpr int TRACK_HEAD = 8;   // TH_* below
-// query tokens, requests, lists of few rows, whether a page is listed twice, tiles of 128 tokens of those lists, lists of many rows (behind the others),
-// tiles of 256 tokens of those, whether the units of their work are listed
-constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_TILES = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7;
+// query tokens, requests, lists of few rows, whether a page is listed twice, what the tiles of those lists cost, lists of many rows (behind the others),
+// tiles of 256 tokens of those, the CTAs that the units of their work are listed for (0: not listed)
+constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_COST = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7;
 // per request: first entry in the page lists, own cached tokens, first entry in the tables of eviction's chunks, none
 constexpr int SEQ_WORDS = 4;
 // per list of cached tokens that rows see, a request's own or a group's prompt: first entry in the page lists, tokens, first
 // entry in the token order, query tokens, tokens that were there before the step, tokens that the first query token sees,
-// whether the next ones each see one more, tiles of the lists of its kind before
+// whether the next ones each see one more (and twice what a tile costs), what the tiles of the lists of its kind before it cost
 constexpr int LIST_WORDS = 8;
-constexpr int LS_TILES = 7;
+constexpr int LS_BEFORE = 7;
 constexpr int TRACK_TILE = 128, TRACK_MANY_TILE = 256;
-constexpr int TRACK_FEW_ROWS = 16;
-// units of the many rows' lists: each CTA's first one, then per unit its list's words, the last one the head instead of the tiles, and first token, steps
+constexpr int TRACK_FEW_ROWS = 64;  // of a list whose keys stream past its rows
+// units of the many rows' lists: each CTA's first one, then per unit its list's words, the last one the head instead of the cost, and first token, steps
 // [from, to), (slot of its first part << 12 | part << 6 | parts - 1) or -1
 constexpr int TRACK_CTAS = 512, UNIT_WORDS = 12, TRACK_UNITS = 8192;
 constexpr int TRACK_SLOTS = 2048;  // of partial sums, 256 tokens each
 // Rows that eviction moves at a time: 16 KB of keys and values.
 constexpr int evict_rows(int dim) { return 8192 / dim; }
+// What a tile of a list of few rows costs, in quarters of one with a single row: of a tile of 128 tokens by its rows, 0.9 us with 4 and 2 with 80 (two CTAs an
+// SM).  Of many rows all count alike.
+constexpr int few_cost(int rows) { return 4 + rows / 12; }
 // The first step of `per` query tokens that sees token t0.
 __host__ __device__ constexpr int first_step(bool causal, int lim, int t0, int per)
 {
@@ -49,7 +52,7 @@ struct Track {
     int seq_at = 0, list_at = 0, unit_at = 0;  // word offsets
     size_t words = 0;
     bool on = false, built = false, shared = false, split = false;
-    int n_seqs = 0, few = 0, many = 0, n_units = 0;
+    int n_seqs = 0, few = 0, many = 0, n_units = 0, few_rows = 0, many_sms = 0;  // few_rows: of the lists of few, the most that one has; SMs for the lists of many
     int64_t few_tiles = 0;
     // eviction's: the longest request, chunks of all requests in the build; room for chunks and layers; tables
     int longest = 0, chunks = 0, chunks_cap = 0, layers_cap = 0;

@@ -54,8 +54,9 @@ struct WeightParams {
 
 // A list of cached tokens and the rows that see it.
 struct List {
-    int pages, len, tok, ntok, old, lim, causal, tiles;
+    int pages, len, tok, ntok, old, lim, causal, before, cost;
 };
+__device__ __forceinline__ List list_of(const int4 &a, const int4 &b) { return {a.x, a.y, a.z, a.w, b.x, b.y, b.z & 1, b.w, b.z >> 1}; }
 // The same word in every lane, and known to be: loops and branches by it are taken by whole warps then, and the votes in them are quick (by
 // words that might differ, a vote takes hundreds of cycles).
 __device__ __forceinline__ int one_word(int x) { return __shfl_sync(0xffffffffu, x, 0); }
@@ -64,15 +65,14 @@ __device__ __forceinline__ int4 four_words(const int4 *at) { return one_each(__l
 __device__ __forceinline__ List load_list(const WeightParams &p, int i)
 {
     const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + i * LIST_WORDS);
-    const int4 a = four_words(w), b = four_words(w + 1);
-    return {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    return list_of(four_words(w), four_words(w + 1));
 }
-// Of the lists [lo, hi) the one that holds tile `tile` of them: the last that begins at or before it.  The whole warp, 32 guesses at a time.
-__device__ __forceinline__ int find_list(const WeightParams &p, int lo, int hi, int tile)
+// Of the lists [lo, hi) the one that holds `at` of what their tiles count together: the last that begins at or before it.  The whole warp, 32 guesses at a time.
+__device__ __forceinline__ int find_list(const WeightParams &p, int lo, int hi, int at)
 {
     for (int n = hi - lo; n > 1;) {
-        const int step = (n + 31) / 32, at = (int)(threadIdx.x & 31) * step;
-        const uint32_t on = __ballot_sync(0xffffffffu, at < n && __ldg(p.track + p.list_at + (lo + min(at, n - 1)) * LIST_WORDS + LS_TILES) <= tile);
+        const int step = (n + 31) / 32, guess = (int)(threadIdx.x & 31) * step;
+        const uint32_t on = __ballot_sync(0xffffffffu, guess < n && __ldg(p.track + p.list_at + (lo + min(guess, n - 1)) * LIST_WORDS + LS_BEFORE) <= at);
         const int last = 31 - __clz(on);  // (lane 0 is)
         lo += last * step;
         n = min(step, n - last * step);
@@ -85,25 +85,28 @@ __device__ __forceinline__ int64_t first_row(const WeightParams &p, int page, in
 }
 
 // ---------------------------------------------------------------- few rows
-template <int D_>
+// Up to R rows a list.  With R = 16 three CTAs have an SM, which reading the keys needs; with 64, where one has more rows, two.
+template <int D_, int R_>
 struct Few {
     static constexpr int D = D_;
-    static constexpr int R = TRACK_FEW_ROWS;                // rows of a list at most
+    static constexpr int R = R_;
     static constexpr int N = 2 * R;                         // hi and lo
-    static constexpr int CTAS = 3;                          // an SM
-    static constexpr int THREADS = 256;
-    static constexpr int KST = D == 128 ? 3 : 6, EST = 8;   // stages of keys, and of what goes with a tile
-    static constexpr int SB = 4;                            // buffers of scores
+    static constexpr int CTAS = R == 16 ? 3 : 2;            // an SM
+    static constexpr int STAGERS = 4;                       // warps that stage queries
+    static constexpr int THREADS = 64 + 32 * STAGERS + 128;
+    static constexpr int KST = 3 * (128 / D), EST = 8;  // stages of keys, and of what goes with a tile
+    static constexpr int SLOTS = 2;                         // segments' queries
+    static constexpr int SB = R == 16 ? 4 : 2;              // buffers of scores
     static constexpr uint32_t TM_COLS = SB * N;
     static constexpr uint32_t SIDE = TRACK_TILE * D;
     static constexpr uint32_t K = 0;
     static constexpr uint32_t Q_BUF = N * D;
-    static constexpr uint32_t Q = K + KST * SIDE;           // two segments' queries
-    static constexpr uint32_t INFO_BUF = R * 16;            // factors of the scores, log-sums, tokens seen
-    static constexpr uint32_t INFO = Q + 2 * Q_BUF;
+    static constexpr uint32_t Q = K + KST * SIDE;
+    static constexpr uint32_t INFO_BUF = R * 12;            // factors of the scores, log-sums, tokens seen
+    static constexpr uint32_t INFO = Q + SLOTS * Q_BUF;
     // a tile's old weights, exponents, first rows of its pages
     static constexpr uint32_t E_W = 0, E_EXP = TRACK_TILE * 4, E_ROW = E_EXP + TRACK_TILE, E_BUF = E_ROW + 64;
-    static constexpr uint32_t E = INFO + 2 * INFO_BUF;
+    static constexpr uint32_t E = INFO + SLOTS * INFO_BUF;
     static constexpr uint32_t K_FULL = E + EST * E_BUF;
     static constexpr uint32_t K_FREE = K_FULL + 8 * KST;
     static constexpr uint32_t E_FULL = K_FREE + 8 * KST;
@@ -111,16 +114,18 @@ struct Few {
     static constexpr uint32_t S_FULL = E_FREE + 8 * EST;
     static constexpr uint32_t S_FREE = S_FULL + 8 * SB;
     static constexpr uint32_t Q_FULL = S_FREE + 8 * SB;
-    static constexpr uint32_t Q_FREE = Q_FULL + 16;         // by the products
-    static constexpr uint32_t I_FREE = Q_FREE + 16;         // by the sums
-    static constexpr uint32_t DRAIN = I_FREE + 16;
+    static constexpr uint32_t Q_FREE = Q_FULL + 8 * SLOTS;  // by the products
+    static constexpr uint32_t I_FREE = Q_FREE + 8 * SLOTS;  // by the sums
+    static constexpr uint32_t DRAIN = I_FREE + 8 * SLOTS;
     static constexpr uint32_t MISC = DRAIN + 8;             // TMEM address, failure flag
     static constexpr uint32_t BYTES = MISC + 8 + 1024;      // slack for the 1024-byte alignment
     static_assert(BYTES + 1024 <= 228 * 1024 / CTAS, "shared memory of an SM");
     static_assert(TM_COLS * CTAS <= 512 && (TM_COLS & (TM_COLS - 1)) == 0, "tensor memory");
+    static_assert(E % 16 == 0 && K_FULL % 8 == 0, "alignment");
 };
 
-// A CTA's tiles [g, end) of the few rows' lists in the order list, key/value head, tile.  A segment is those of one list and head.
+// A CTA's share [g, end) of what the few rows' lists' tiles cost, in the order list, key/value head, tile.  A segment is the tiles of one list and
+// head.
 struct Walk {
     int64_t g, end;
     int list, n_lists, kh, j, tiles, segment;
@@ -140,16 +145,24 @@ struct Walk {
         end = all * (blockIdx.x + 1) / gridDim.x;
         segment = 0;
         if (g >= end) return;
-        list = find_list(p, 0, n_lists, (int)(g / KV));  // (a list's first tile of all heads is its first tile times the heads)
+        list = find_list(p, 0, n_lists, (int)(g / KV));  // (what is before a list, for all heads, is that times the heads)
         l = load_list(p, list);
         tiles = (l.len + TRACK_TILE - 1) / TRACK_TILE;
-        const int in = (int)(g - (int64_t)l.tiles * KV);
-        kh = in / tiles;
-        j = in - kh * tiles;
+        // the first tile that begins in the share
+        const int64_t base = (int64_t)l.before * KV;
+        const int at = (int)((g - base + l.cost - 1) / l.cost);
+        g = base + (int64_t)at * l.cost;
+        kh = at / tiles;
+        j = at - kh * tiles;
         ahead(p);
+        if (kh == KV) {  // it is the next list's
+            --kh;
+            segment = -1;
+            next_segment(p);
+        }
     }
     __device__ __forceinline__ bool more() const { return g < end; }
-    __device__ __forceinline__ bool last_of_segment() const { return g + 1 == end || j + 1 == tiles; }
+    __device__ __forceinline__ bool last_of_segment() const { return g + l.cost >= end || j + 1 == tiles; }
     __device__ __forceinline__ void next_segment(const WeightParams &p)
     {
         j = 0;
@@ -158,8 +171,7 @@ struct Walk {
             kh = 0;
             if (g < end) {
                 ++list;
-                const int4 x = one_each(a), y = one_each(b);
-                l = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                l = list_of(one_each(a), one_each(b));
                 tiles = (l.len + TRACK_TILE - 1) / TRACK_TILE;
                 ahead(p);
             }
@@ -167,41 +179,45 @@ struct Walk {
     }
     __device__ __forceinline__ void next(const WeightParams &p)
     {
-        ++g;
+        g += l.cost;
         if (++j == tiles) next_segment(p);
     }
     // past the segment
     __device__ __forceinline__ void skip(const WeightParams &p)
     {
-        g += tiles - j;
+        g += (int64_t)(tiles - j) * l.cost;
         next_segment(p);
     }
 };
 
-// A segment's queries, each row scaled by a power of two, and the constants of its columns: two warps, this one the w-th.
+// A segment's queries, each row scaled by a power of two, and the constants of its columns: by STAGERS warps, this one the w-th.
 template <class L>
 __device__ __forceinline__ void stage_few(const WeightParams &p, uint32_t base, const Walk &k, int w)
 {
     constexpr int LPR = L::D / 8, RPW = 32 / LPR;   // lanes a row, rows a warp deals with at a time
-    const int G = p.n_heads / p.kv.heads, lane = threadIdx.x & 31, part = lane % LPR, rows = k.l.ntok * G;
-    const uint32_t q_at = base + L::Q + (k.segment & 1) * L::Q_BUF, info = base + L::INFO + (k.segment & 1) * L::INFO_BUF;
-    constexpr int AT_ONCE = L::R / (2 * RPW);
+    constexpr int AT_ONCE = (L::R + L::STAGERS * RPW - 1) / (L::STAGERS * RPW);  // loads of a lane under way together
+    const int G = p.n_heads / p.kv.heads, lane = threadIdx.x & 31, part = lane % LPR, rows = k.l.ntok * G, slot = k.segment % L::SLOTS;
+    const uint32_t q_at = base + L::Q + slot * L::Q_BUF, info = base + L::INFO + slot * L::INFO_BUF;
     uint4 q[AT_ONCE];
     float lse[AT_ONCE];
+    int see[AT_ONCE];
 #pragma unroll
     for (int n = 0; n < AT_ONCE; ++n) {
-        const int row = (2 * n + w) * RPW + lane / LPR, i = row / G, h = k.kh * G + row - i * G;
+        const int row = (L::STAGERS * n + w) * RPW + lane / LPR, i = row / G, h = k.kh * G + row - i * G;
         q[n] = make_uint4(0, 0, 0, 0);
         lse[n] = 0.f;
+        see[n] = 0;
         if (row < rows) {
-            const int t = __ldg(p.plan + p.order_at + k.l.tok + i);
+            const int t = k.l.causal ? k.l.tok + i : __ldg(p.plan + p.order_at + k.l.tok + i);  // (requests' own tokens are in order)
             q[n] = __ldg(reinterpret_cast<const uint4 *>(p.q + t * p.q_stride + h * L::D) + part);
             lse[n] = __ldg(p.lse + (int64_t)t * p.n_heads + h);
+            see[n] = k.l.lim + (k.l.causal ? i : 0);
         }
     }
 #pragma unroll
     for (int n = 0; n < AT_ONCE; ++n) {
-        const int row = (2 * n + w) * RPW + lane / LPR, i = row / G;
+        const int row = (L::STAGERS * n + w) * RPW + lane / LPR;
+        if ((L::STAGERS * n + w) * RPW >= ((rows + 3) & ~3)) break;  // (columns go by fours; rows that fill up see nothing)
         const uint4 u = q[n];
         const uint32_t x[4] = {u.x, u.y, u.z, u.w};
         uint32_t a = 0;
@@ -222,12 +238,14 @@ __device__ __forceinline__ void stage_few(const WeightParams &p, uint32_t base, 
             lo[e / 2] |= (uint32_t)e4m3x2((v0 - f.x) * 32.f, (v1 - f.y) * 32.f) << (16 * (e & 1));  // (v - f at most 2^3)
         }
         if ((a >> 23) == 255) hi[0] = hi[1] = lo[0] = lo[1] = 0x7f7f7f7fu;
-        sts64(q_at + swz_rows<L::D>(row * L::D + part * 8), hi[0], hi[1]);
-        sts64(q_at + swz_rows<L::D>((L::R + row) * L::D + part * 8), lo[0], lo[1]);
-        if (part == 0) {  // (rows that fill up see nothing)
-            stsf(info + 4 * row, pow2(qe) * p.scale);
-            stsf(info + 4 * (L::R + row), -lse[n]);
-            sts32(info + 4 * (2 * L::R + row), row < rows ? k.l.lim + (k.l.causal ? i : 0) : 0);
+        if (row < L::R) {
+            sts64(q_at + swz_rows<L::D>(row * L::D + part * 8), hi[0], hi[1]);
+            sts64(q_at + swz_rows<L::D>((L::R + row) * L::D + part * 8), lo[0], lo[1]);
+            if (part == 0) {
+                stsf(info + 4 * row, pow2(qe) * p.scale);
+                stsf(info + 4 * (L::R + row), -lse[n]);
+                sts32(info + 4 * (2 * L::R + row), (uint32_t)see[n]);
+            }
         }
     }
     fence_async_smem();
@@ -254,8 +272,8 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
             mbar_init(base + L::S_FULL + 8 * i, 1);
             mbar_init(base + L::S_FREE + 8 * i, 4);
         }
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(base + L::Q_FULL + 8 * i, 2);
+        for (int i = 0; i < L::SLOTS; ++i) {
+            mbar_init(base + L::Q_FULL + 8 * i, L::STAGERS);
             mbar_init(base + L::Q_FREE + 8 * i, 1);
             mbar_init(base + L::I_FREE + 8 * i, 4);
         }
@@ -278,7 +296,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     const bool fits = track[TH_TOKENS] <= p.max_tok && !track[TH_SHARED];
     if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
     const int n_lists = one_word(fits ? track[TH_FEW] : 0);
-    Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_TILES]) * KV : 0);
+    Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_COST]) * KV : 0);
     bool ok = true;
     if (!k.more()) {
     } else if (warp == 0) {
@@ -331,21 +349,21 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
         uint32_t ks = 0, kph = 0, n = 0;
         bool fresh = true;
         for (; k.more(); k.next(p), ++n) {
-            const int b = n % L::SB, qb = k.segment & 1;
-            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * qb, (k.segment >> 1) & 1, dead);
+            const int b = n % L::SB, slot = k.segment % L::SLOTS;
+            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * slot, (k.segment / L::SLOTS) & 1, dead);
             fresh = k.last_of_segment();
             ok = ok && wait_bar(base + L::K_FULL + 8 * ks, kph, dead);
             if (n >= (uint32_t)L::SB) ok = ok && wait_bar(base + L::S_FREE + 8 * b, (n / L::SB - 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            const uint64_t kd = sdesc_rows(base + L::K + ks * L::SIDE, L::D, 0), qd = sdesc_rows(base + L::Q + qb * L::Q_BUF, L::D, 0);
+            const uint64_t kd = sdesc_rows(base + L::K + ks * L::SIDE, L::D, 0), qd = sdesc_rows(base + L::Q + slot * L::Q_BUF, L::D, 0);
             if (lead) {
 #pragma unroll
                 for (int i = 0; i < L::D / 32; ++i) umma_e4m3(tmem + b * L::N, kd + 2 * i, qd + 2 * i, id, i > 0);
                 umma_commit(base + L::S_FULL + 8 * b);
                 umma_commit(base + L::K_FREE + 8 * ks);
-                if (fresh) umma_commit(base + L::Q_FREE + 8 * qb);
+                if (fresh) umma_commit(base + L::Q_FREE + 8 * slot);
             }
             __syncwarp();
             if (++ks == (uint32_t)L::KST) ks = 0, kph ^= 1;
@@ -359,16 +377,16 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
             }
             __syncwarp();
         }
-    } else if (warp < 4) {
+    } else if (warp < 2 + L::STAGERS) {
         // ------------------------------------------------ queries, a segment ahead
         for (; k.more(); k.skip(p)) {
-            const int s = k.segment, b = s & 1;
-            if (s > 1) ok = wait_bar(base + L::Q_FREE + 8 * b, ((s - 2) >> 1) & 1, dead) && wait_bar(base + L::I_FREE + 8 * b, ((s - 2) >> 1) & 1, dead);
+            const int slot = k.segment % L::SLOTS, use = k.segment / L::SLOTS;
+            if (use > 0) ok = wait_bar(base + L::Q_FREE + 8 * slot, (use - 1) & 1, dead) && wait_bar(base + L::I_FREE + 8 * slot, (use - 1) & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             stage_few<L>(p, base, k, warp - 2);
             __syncwarp();
-            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * b);
+            if (lane == 0) mbar_arrive_release(base + L::Q_FULL + 8 * slot);
         }
         if (!ok && lane == 0) {
             *dead = 1;
@@ -376,13 +394,13 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
         }
     } else {
         // ------------------------------------------------ a thread's token: its row of scores, its weight
-        const int me = tid - 128, G = p.n_heads / KV;
+        const int me = 32 * (warp & 3) + lane, G = p.n_heads / KV;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         uint32_t es = 0, eph = 0, n = 0;
         bool fresh = true;
         for (; k.more(); k.next(p), ++n) {
-            const int b = n % L::SB, qb = k.segment & 1, j = k.j * TRACK_TILE + me, rows = k.l.ntok * G;
-            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * qb, (k.segment >> 1) & 1, dead);
+            const int b = n % L::SB, slot = k.segment % L::SLOTS, j = k.j * TRACK_TILE + me, rows = k.l.ntok * G;
+            if (fresh) ok = wait_bar(base + L::Q_FULL + 8 * slot, (k.segment / L::SLOTS) & 1, dead);
             fresh = k.last_of_segment();
             ok = ok && wait_bar(base + L::E_FULL + 8 * es, eph, dead);
             const uint32_t e = base + L::E + es * L::E_BUF;
@@ -394,7 +412,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
             if (!ok) break;
             if (lane == 0) mbar_arrive_release(base + L::E_FREE + 8 * es);
             tc_fence_after();
-            const uint32_t info = base + L::INFO + qb * L::INFO_BUF, s_at = tmem + lanes + b * L::N;
+            const uint32_t info = base + L::INFO + slot * L::INFO_BUF, s_at = tmem + lanes + b * L::N;
             float sum = 0.f;
 #pragma unroll 1
             for (int c0 = 0; c0 < rows; c0 += 4) {
@@ -416,7 +434,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
             __syncwarp();
             if (lane == 0) {
                 mbar_arrive_release(base + L::S_FREE + 8 * b);
-                if (fresh) mbar_arrive_release(base + L::I_FREE + 8 * qb);
+                if (fresh) mbar_arrive_release(base + L::I_FREE + 8 * slot);
             }
             if (j < k.l.len) p.weights[at] = was + sum;
             if (++es == (uint32_t)L::EST) es = 0, eph ^= 1;
@@ -482,25 +500,40 @@ struct Unit {
     bool two;                   // more than 128 tokens
 };
 
-// A CTA's units: a list made by the build, or every gridDim-th one.
+// A CTA's units: the build's lists for CTAs blockIdx.x, blockIdx.x + gridDim.x, .. (a captured call may have another grid than the batch that it is replayed
+// for), or every gridDim-th one.
 struct Units {
-    int at, end, step;
-    bool listed;
+    int at, end, cta, ctas;
+    __device__ __forceinline__ void settle(const WeightParams &p)
+    {
+        while (ctas > 0 && at >= end && cta + (int)gridDim.x < ctas) {
+            cta += gridDim.x;
+            at = one_word(__ldg(p.track + p.unit_at + cta));
+            end = one_word(__ldg(p.track + p.unit_at + cta + 1));
+        }
+    }
     __device__ __forceinline__ Units(const WeightParams &p, bool fits)
     {
-        listed = one_word(p.track[TH_LISTED]);
-        step = listed ? 1 : gridDim.x;
-        at = listed ? one_word(p.track[p.unit_at + blockIdx.x]) : blockIdx.x;
-        end = one_word(!fits ? 0 : listed ? p.track[p.unit_at + blockIdx.x + 1] : p.track[TH_MANY_TILES] * p.kv.heads);
+        ctas = one_word(p.track[TH_LISTED]);
+        at = blockIdx.x;
+        end = ctas > 0 ? 0 : one_word(fits ? p.track[TH_MANY_TILES] * p.kv.heads : 0);
+        cta = (int)blockIdx.x - (int)gridDim.x;
+        if (!fits) ctas = end = 0;
+        else settle(p);
     }
     __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ void advance(const WeightParams &p)
+    {
+        at += ctas > 0 ? 1 : gridDim.x;
+        settle(p);
+    }
     __device__ __forceinline__ Unit get(const WeightParams &p, int per) const
     {
         Unit u;
-        if (listed) {
+        if (ctas > 0) {
             const int4 *w = reinterpret_cast<const int4 *>(p.track + p.unit_at + TRACK_CTAS) + (int64_t)at * (UNIT_WORDS / 4);
             const int4 a = four_words(w), b = four_words(w + 1), c = four_words(w + 2);
-            u.l = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, 0};
+            u.l = list_of(a, b);
             u.kh = b.w;
             u.t0 = c.x;
             u.r0 = c.y;
@@ -510,7 +543,7 @@ struct Units {
             const int tile = at / p.kv.heads;
             u.kh = at - tile * p.kv.heads;
             u.l = load_list(p, find_list(p, p.track[TH_FEW], p.track[TH_FEW] + p.track[TH_MANY], tile));
-            u.t0 = (tile - u.l.tiles) * TRACK_MANY_TILE;
+            u.t0 = (tile - u.l.before) * TRACK_MANY_TILE;
             u.r0 = first_step(u.l.causal, u.l.lim, u.t0, per);
             u.r1 = (u.l.ntok + per - 1) / per;
             u.split = -1;
@@ -528,7 +561,7 @@ struct Steps {
     bool live, next;
     __device__ __forceinline__ void ahead(const WeightParams &p, int per)
     {
-        it.at += it.step;
+        it.advance(p);
         next = it.more();
         if (next) v = it.get(p, per);
     }
@@ -672,7 +705,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         auto next_keys = [&]() {
             if (!ok || !keys.more()) return;
             load_keys(keys.get(p, per));
-            keys.at += keys.step;
+            keys.advance(p);
         };
         next_keys();
         next_keys();
@@ -735,7 +768,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         uint32_t st = 0, ph = 0, units[2] = {0, 0}, job = 0, n = 0, odd = 0;  // (odd: a bit a warpgroup; a job: a step's scores of 128 tokens)
         Unit u = it.get(p, per);
         while (it.more() && ok) {
-            it.at += it.step;
+            it.advance(p);
             Unit v = u;
             if (it.more()) v = it.get(p, per);
             for (int r = u.r0; r < u.r1 && ok; ++r) {
@@ -844,40 +877,40 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         uint32_t n = 0, b = w, jobs = 0, units = 0, done = 0;  // (b: the buffer of the step's job)
         float a = 0.f;
         uint32_t at = 0;
-        // the next unit's exponent and row, and by one of the two warpgroups its codes to bf16
-        auto take_up = [&](bool widen) {
+        // The next unit's codes to bf16, by one of the two warpgroups; its exponent and row, by both.
+        auto widen = [&]() {
             const uint32_t buf = 2 * w + (units & 1);
             ok = ok && wait_bar(base + L::K_FULL + 8 * buf, units >> 1 & 1, dead);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) return;
-            if (widen) {
-                widen_key<L>(base + L::RAW + buf * L::RAW_TILE, t_lane + L::TM_A + w * 64, me);
-                tc_fence_before();
-            }
+            widen_key<L>(base + L::RAW + buf * L::RAW_TILE, t_lane + L::TM_A + w * 64, me);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_release(base + L::A_FULL + 8 * w);
+        };
+        auto take_up = [&]() {
+            const uint32_t buf = 2 * w + (units & 1);
+            ok = ok && wait_bar(base + L::K_FULL + 8 * buf, units >> 1 & 1, dead);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
             a = p.scale * row_scale(lds8(base + L::EXPS + 128 * buf + me));
             at = lds32(base + L::ROWS + 32 * buf + 4 * (me >> p.kv.page_log2)) + (me & (p.kv.page - 1));
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive_release(base + L::K_FREE + 8 * buf);
-                if (widen) mbar_arrive_release(base + L::A_FULL + 8 * w);
-            }
+            if (lane == 0) mbar_arrive_release(base + L::K_FREE + 8 * buf);
             ++units;
         };
         Unit u = it.get(p, per);
-        if (w == 0 || u.two) take_up(par == 0);
+        if (par == 0 && (w == 0 || u.two)) widen();
+        if (w == 0 || u.two) take_up();
         while (ok && it.more()) {
-            it.at += it.step;
+            it.advance(p);
             // (all of the next unit's words are read when it begins, from the L1 then)
             const bool next = it.more(), next_two = next && it.get(p, per).two, mine = w == 0 || u.two, theirs = next && (w == 0 || next_two);
-            // the unit's last step is this warpgroup's: when its products are done the next unit's keys take its keys' place
-            const bool last = ((n + (uint32_t)(u.r1 - u.r0) - 1) & 1) == (uint32_t)par;
             const int j = u.t0 + 128 * w + me, end = min(u.t0 + 128 * (w + 1), u.l.len);
-            const float a_now = a;
-            const uint32_t at_now = at;
             const bool live = mine && j < u.l.len;
             float total = 0.f;
             // (the first one knows of both that they are done with the unit before)
-            if (!mine && theirs) take_up(par == 0);
+            if (!mine && theirs && par == 0) widen();
             for (int r = u.r0; r < u.r1; ++r, ++n, b += u.two ? 2 : 1) {
                 if (b >= (uint32_t)L::SB) b -= L::SB;
                 if ((n & 1) != (uint32_t)par) continue;
@@ -889,8 +922,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 if (mine) {
                     ++jobs;
                     tc_fence_after();
-                    if (r + 1 == u.r1 && theirs) {
-                        take_up(true);
+                    if (r + 1 == u.r1 && theirs) {  // (the unit's products are done: the next one's keys take its keys' place)
+                        widen();
                         if (!ok) break;
                     }
                     const int i0 = r * per, cols = min(per, u.l.ntok - i0) * G;
@@ -911,9 +944,9 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                         for (int c = 0; c < 8; c += 2) {
                             tmem_ld_wait();
                             if (c == 6) free();
-                            add_columns(x[0], lse + 64 * c, a_now, sums);
+                            add_columns(x[0], lse + 64 * c, a, sums);
                             if (c < 6) load(c + 2);
-                            add_columns(x[1], lse + 64 * c + 64, a_now, sums);
+                            add_columns(x[1], lse + 64 * c + 64, a, sums);
                             if (c < 6) load(c + 3);
                         }
                     } else {
@@ -922,7 +955,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                             float x[16];
                             tmem_ld16(s_at + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(x));
                             tmem_ld_wait();
-                            add_columns(x, lse + 64 * c, a_now, sums);
+                            add_columns(x, lse + 64 * c, a, sums);
                         }
                     }
                     float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
@@ -937,7 +970,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                         const int see[4] = {(int)lim.x, (int)lim.y, (int)lim.z, (int)lim.w};
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            const float e = ex2(fmaf(x[i], a_now, m[i]) * LOG2E);
+                            const float e = ex2(fmaf(x[i], a, m[i]) * LOG2E);
                             if (j < see[i]) sum += e;
                         }
                     }
@@ -948,10 +981,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 if (lane == 0) mbar_arrive_release(base + L::M_FREE + 8 * ms);
             }
             if (!ok) break;
-            if (mine && theirs && !last) take_up(false);
-            if (!ok) break;
             float was = 0.f;
-            if (live && par == 0 && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at_now];
+            if (live && par == 0 && p.decay != 0.f && j < u.l.old) was = p.decay * p.weights[at];
             if (mine) {  // the two warpgroups' sums
                 const uint32_t at_h = base + L::HALF + 512 * w + 4 * me, pair = 4 * w + (warp & 3), full = base + L::H_FULL + 8 * pair, free = base + L::H_FREE + 8 * pair;
                 if (par) {
@@ -972,7 +1003,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             }
             if (!mine || par) {
             } else if (u.split < 0) {
-                if (live) p.weights[at_now] = was + total;
+                if (live) p.weights[at] = was + total;
             } else {
                 // the warp that comes last adds up the parts, in their order
                 const int parts = (u.split & 63) + 1, part = (u.split >> 6) & 63, slot = u.split >> 12;
@@ -986,10 +1017,11 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 if ((int)before + 1 == parts) {
                     total = 0.f;
                     for (int i = 0; i < parts; ++i) total += __ldcg(mine_at + i * TRACK_MANY_TILE);
-                    if (live) p.weights[at_now] = was + total;
+                    if (live) p.weights[at] = was + total;
                     if (lane == 0) *count = 0;
                 }
             }
+            if (theirs) take_up();
             if (next) u = it.get(p, per);
         }
         if (!ok && lane == 0) {
@@ -1033,22 +1065,28 @@ cudaError_t encode_queries(CUtensorMap *out, const void *q, int64_t stride, int 
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-template <int D>
-cudaError_t launch_weights(WeightParams &p, int n_sm, bool many, bool few, int64_t few_tiles, cudaStream_t stream)
+template <class F>
+cudaError_t launch_few(const WeightParams &p, int n_sm, int64_t tiles, cudaStream_t stream)
 {
-    using F = Few<D>;
+    const cudaError_t e = cudaFuncSetAttribute(weights_few_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
+    if (e != cudaSuccess) return e;
+    return launch_overlapped(weights_few_kernel<F>, (unsigned)std::min<int64_t>(n_sm * F::CTAS, tiles), F::THREADS, F::BYTES, stream, p);
+}
+
+// The lists of many rows on many_sms of the SMs (a CTA has one to itself), beside them those of few, of up to few_rows, on the others.
+template <int D>
+cudaError_t launch_weights(WeightParams &p, int n_sm, int many_sms, bool few, int few_rows, int64_t few_tiles, cudaStream_t stream)
+{
     using M = Many<D>;
-    cudaError_t e = cudaSuccess;
-    if (many) {
-        e = cudaFuncSetAttribute(weights_many_kernel<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
-        if (e == cudaSuccess) e = launch_overlapped(weights_many_kernel<M>, n_sm, M::THREADS, M::BYTES, stream, p);
+    if (many_sms > 0) {
+        cudaError_t e = cudaFuncSetAttribute(weights_many_kernel<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
+        if (e == cudaSuccess) e = launch_overlapped(weights_many_kernel<M>, many_sms, M::THREADS, M::BYTES, stream, p);
         if (e != cudaSuccess) return e;
     }
     if (!few) return cudaSuccess;
-    p.behind = many;
-    e = cudaFuncSetAttribute(weights_few_kernel<F>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::BYTES);
-    if (e != cudaSuccess) return e;
-    return launch_overlapped(weights_few_kernel<F>, (unsigned)std::min<int64_t>(n_sm * F::CTAS, few_tiles), F::THREADS, F::BYTES, stream, p);
+    p.behind = many_sms > 0;
+    const int sms = many_sms < n_sm ? n_sm - many_sms : n_sm;
+    return few_rows <= 16 ? launch_few<Few<D, 16>>(p, sms, few_tiles, stream) : launch_few<Few<D, 64>>(p, sms, few_tiles, stream);
 }
 
 }  // namespace
@@ -1109,8 +1147,9 @@ try {
     p.decay = decay;
     p.err = ctx_error_word(ctx);
     const int64_t tiles = captured ? 1 << 30 : tr.few_tiles * kv.heads;
-    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_weights<128>(p, a->n_sm, many, few, tiles, stream)
-                                         : launch_weights<64>(p, a->n_sm, many, few, tiles, stream));
+    const int rows = captured ? TRACK_FEW_ROWS : tr.few_rows, sms = many ? tr.many_sms : 0;
+    SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_weights<128>(p, a->n_sm, sms, few, rows, tiles, stream)
+                                         : launch_weights<64>(p, a->n_sm, sms, few, rows, tiles, stream));
     return SALT_OK;
 } catch (const std::bad_alloc &) {
     return ctx_fail(a->kv->ctx, SALT_ERR_OOM, "no host memory");
