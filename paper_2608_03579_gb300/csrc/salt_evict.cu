@@ -434,7 +434,9 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     __syncthreads();
     pdl_wait();
     pdl_launch_dependents();
-    const int n_seqs = p.track[TH_SEQS];
+    // (known to be a warp's words: what goes by them, votes and shuffles too, is quick then)
+    auto uniform = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+    const int n_seqs = uniform(p.track[TH_SEQS]);
     if (n_seqs > p.n_seqs || p.track[TH_SHARED]) return;
     bool ok = true;
     auto wait = [&](uint64_t *bars, uint32_t n) {  // for the n-th use of its slot
@@ -446,11 +448,13 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
         __syncwarp();
         if (lane == 0) mbar_arrive_release(smem_u32(&bars[n % SLOTS]));
     };
+    // the chunk in a slot, -1 behind the last
+    auto chunk_of = [&](uint32_t n) { return (int64_t)uniform((int)(s_chunk[n % SLOTS] >> 32)) << 32 | (uint32_t)uniform((int)s_chunk[n % SLOTS]); };
     auto slot_of = [&](uint32_t n) { return s_slots + (n % SLOTS) * M::SLOT; };
     if (warp == LOAD_WARPS + STORE_WARPS) {
         // ------------------------------------------------ places
         // (a chunk's line is found while the places of the one before are on their way: the waits for other chunks empty the L1)
-        const int per_lh = p.chunk_ptr[n_seqs];
+        const int per_lh = uniform(p.chunk_ptr[n_seqs]);
         const int64_t all = (int64_t)per_lh * p.kv.heads * layers;
         struct Chunk {
             Line l;
@@ -471,7 +475,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
                 lo += last * step;
                 n = min(step, n - last * step);
             }
-            r.c = x - p.chunk_ptr[lo];
+            r.c = x - uniform(p.chunk_ptr[lo]);
             r.l = load_line(p, lh, lo);
             return r;
         };
@@ -529,7 +533,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     } else if (warp == LOAD_WARPS + STORE_WARPS + 1) {
         // ------------------------------------------------ chunks that were read
         for (uint32_t n = 0; wait(s_full, n); ++n) {
-            const int64_t chunk = s_chunk[n % SLOTS];
+            const int64_t chunk = chunk_of(n);
             if (chunk < 0 || !wait(s_read, n)) break;
             if (lane == 0) {
                 asm volatile("st.relaxed.gpu.global.u32 [%0], %1;\n" ::"l"(p.read + chunk), "r"(1u) : "memory");
@@ -539,7 +543,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     } else if (warp == LOAD_WARPS + STORE_WARPS + 2) {
         // ------------------------------------------------ chunks to wait for
         for (uint32_t n = 0; wait(s_full, n); ++n) {
-            const int64_t chunk = s_chunk[n % SLOTS];
+            const int64_t chunk = chunk_of(n);
             if (chunk < 0) break;
             if (lane < 2 && s_wait[n % SLOTS][lane] < 0) {
                 const uint32_t *flag = p.read + chunk + s_wait[n % SLOTS][lane];
@@ -558,7 +562,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
         uint32_t ke[2][ROWS / 32], ve[2][ROWS / 32];
         float w[2][ROWS / 32];
         auto load = [&](int b, uint32_t n) {
-            if (!wait(s_full, n) || s_chunk[n % SLOTS] < 0) return false;
+            if (!wait(s_full, n) || chunk_of(n) < 0) return false;
 #pragma unroll
             for (int k = 0; k < ROWS / 32; ++k) {
                 const int r = 32 * k + lane;
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     } else if (warp < LOAD_WARPS) {
         // ------------------------------------------------ keys and values into the slot
         const int part = tid % M::LPR;
-        for (uint32_t n = 0; wait(s_full, n) && s_chunk[n % SLOTS] >= 0; ++n) {
+        for (uint32_t n = 0; wait(s_full, n) && chunk_of(n) >= 0; ++n) {
             uint8_t *slot = slot_of(n);
             const int32_t *src = reinterpret_cast<const int32_t *>(slot + M::SRC), *dst = reinterpret_cast<const int32_t *>(slot + M::DST);
 #pragma unroll
@@ -611,7 +615,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     } else {
         // ------------------------------------------------ out of it
         const int me = tid - 32 * LOAD_WARPS, part = me % M::LPR;
-        for (uint32_t n = 0; wait(s_full, n) && s_chunk[n % SLOTS] >= 0; ++n) {
+        for (uint32_t n = 0; wait(s_full, n) && chunk_of(n) >= 0; ++n) {
             if (!wait(s_read, n) || !wait(s_clear, n)) break;
             const uint8_t *slot = slot_of(n);
             const int32_t *dst = reinterpret_cast<const int32_t *>(slot + M::DST);

@@ -18,6 +18,7 @@
 #include <new>
 
 #include "salt_async.cuh"
+#include "salt_attn.cuh"
 #include "salt_host.cuh"
 #include "salt_internal.cuh"
 #include "salt_kvrow.cuh"
@@ -51,21 +52,18 @@ struct RopeParams {
     uint64_t freq[64];
 };
 
-__device__ __forceinline__ void unpack8(const uint4 &x, float *y)
+__device__ __forceinline__ void unpack8(const uint4 &x, float2 *y)
 {
     const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        y[2 * i] = __uint_as_float(w[i] << 16);
-        y[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
+    for (int i = 0; i < 4; ++i) y[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
 }
-__device__ __forceinline__ uint4 pack8(const float *y)
+__device__ __forceinline__ uint4 pack8(const float2 *y)
 {
     uint32_t w[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 b = __floats2bfloat162_rn(y[2 * i], y[2 * i + 1]);
+        const __nv_bfloat162 b = __floats2bfloat162_rn(y[i].x, y[i].y);
         w[i] = *reinterpret_cast<const uint32_t *>(&b);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -80,11 +78,12 @@ __device__ __forceinline__ float sum_lanes(float x)
 }
 
 template <int D, bool WRITE, bool MIXED>
-__global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constant__ RopeParams p)
+__global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_constant__ RopeParams p)
 {
     constexpr int LPR = D / 16, RPW = 32 / LPR;  // lanes a row, rows a warp deals with at a time
     __shared__ __align__(16) float2 s_turn[ROPE_WARPS][64];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = lane % LPR;
+    // (the warp's number from a shuffle: loops by it are known to be a warp's then, and the shuffles in them are quick)
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, part = lane % LPR;
     const uint32_t task = blockIdx.x * ROPE_WARPS + warp;
     const int t = (int)(task / (uint32_t)p.splits), split = (int)(task - (uint32_t)t * p.splits);
     // the lane's pieces of a row, in units of 8 elements, and whether they are rotated
@@ -104,7 +103,8 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
     const int slot = WRITE ? __ldg(slots + t) : -1, page = WRITE ? slot >> p.kv.page_log2 : 0;
     const bool stored = WRITE && slot >= 0 && page < p.kv.n_pages;
     if (WRITE && split == 0 && lane == 0 && !stored && slot != -1) atomicOr(p.err, SALT_DEVERR_KV_SLOT);
-    float c[8], s[8];
+    // sines and cosines of the lane's pairs, and of the kind of head at hand its weights, two at a time
+    float2 c[4], s[4];
     {
         const int64_t at = __ldg(positions + t);
 #pragma unroll
@@ -116,11 +116,11 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
         }
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 8; e += 2) {
             const int pair = MIXED ? 4 * (e < 4 ? c0 : c1) + (e & 3) : part * 8 + e;
-            const float2 x = s_turn[warp][pair & 63];
-            c[e] = x.x;
-            s[e] = x.y;
+            const float4 x = *reinterpret_cast<const float4 *>(&s_turn[warp][pair & 63]);
+            c[e / 2] = make_float2(x.x, x.z);
+            s[e / 2] = make_float2(x.y, x.w);
         }
     }
     for (int pass = split * p.passes; pass < pass1; pass += ROPE_ROWS) {
@@ -141,46 +141,55 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
 #pragma unroll
         for (int i = 0; i < ROPE_ROWS; ++i) {
             const bool is_q = row[i] < H, is_v = row[i] >= H + KV;
-            float y[16];
+            float2 y[8];
             unpack8(x[i][0], y);
-            unpack8(x[i][1], y + 8);
+            unpack8(x[i][1], y + 4);
             const uint16_t *norm = is_q ? p.q_norm : p.k_norm;
             if (p.q_norm || p.k_norm) {
-                float ss = 0.f;
+                float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) ss = fmaf(y[e], y[e], ss);
-                ss = sum_lanes<LPR>(ss);
+                for (int e = 0; e < 8; ++e) s2[e & 1] = fma2(y[e], y[e], s2[e & 1]);
+                const float ss = sum_lanes<LPR>((s2[0].x + s2[0].y) + (s2[1].x + s2[1].y));
                 float r = rsqrtf(ss * (1.f / D) + p.eps);
                 if (__any_sync(0xffffffffu, !(ss <= FLT_MAX))) {  // squares past fp32's range: the row scaled down
                     const float down = 0x1p-70f;
-                    float s2 = 0.f;
+                    float s1 = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) s2 = fmaf(y[e] * down, y[e] * down, s2);
-                    s2 = sum_lanes<LPR>(s2);
-                    if (!(ss <= FLT_MAX)) r = rsqrtf(s2 * (1.f / D)) * down;
+                    for (int e = 0; e < 8; ++e) s1 = fmaf(y[e].x * down, y[e].x * down, fmaf(y[e].y * down, y[e].y * down, s1));
+                    s1 = sum_lanes<LPR>(s1);
+                    if (!(ss <= FLT_MAX)) r = rsqrtf(s1 * (1.f / D)) * down;
                 }
                 if (norm && !is_v && row[i] >= 0) {
-                    float w[16];
-                    unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c0), w);
-                    unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c1), w + 8);
+                    float2 w[8];
+                    {
+                        unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c0), w);
+                        unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c1), w + 4);
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) y[e] = y[e] * r * (w[e] + p.offset);
+                        for (int e = 0; e < 8; ++e) w[e] = add2(w[e], make_float2(p.offset, p.offset));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = mul2(mul2(y[e], make_float2(r, r)), w[e]);
                 }
             }
-            if (!is_v) {
+            if (!is_v) {  // (what is not rotated stays as it is, zeros' signs and all)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int i0 = MIXED ? 2 * e : e, i1 = MIXED ? 2 * e + 1 : 8 + e;
-                    const float a = y[i0], b = y[i1];
-                    const bool turned = MIXED ? (e < 4 ? turned0 : turned1) : turned0;
-                    y[i0] = turned ? fmaf(a, c[e], -(b * s[e])) : a;
-                    y[i1] = turned ? fmaf(b, c[e], a * s[e]) : b;
+                for (int e = 0; e < 4; ++e) {
+                    if (MIXED) {
+                        if (!(e < 2 ? turned0 : turned1)) continue;
+                        const float2 a = y[2 * e], b = y[2 * e + 1];
+                        y[2 * e] = make_float2(fmaf(a.x, c[e].x, -(a.y * s[e].x)), fmaf(a.y, c[e].x, a.x * s[e].x));
+                        y[2 * e + 1] = make_float2(fmaf(b.x, c[e].y, -(b.y * s[e].y)), fmaf(b.y, c[e].y, b.x * s[e].y));
+                    } else if (turned0) {
+                        const float2 a = y[e], b = y[4 + e], n = make_float2(-s[e].x, -s[e].y);
+                        y[e] = fma2(a, c[e], mul2(b, n));
+                        y[4 + e] = fma2(b, c[e], mul2(a, s[e]));
+                    }
                 }
             }
             if (WRITE) {
                 uint32_t a = 0;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) a = max(a, __float_as_uint(y[e]) & 0x7fffffffu);
+                for (int e = 0; e < 8; ++e) a = max(a, max(__float_as_uint(y[e].x) & 0x7fffffffu, __float_as_uint(y[e].y) & 0x7fffffffu));
 #pragma unroll
                 for (int o = LPR / 2; o > 0; o >>= 1) a = max(a, __shfl_xor_sync(0xffffffffu, a, o));
                 if (!is_q && stored) {
@@ -190,10 +199,10 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
                     uint8_t *to = (is_v ? p.kv.v : p.kv.k) + (uint64_t)at * D;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float *z = y + 8 * h;
+                        const float2 *z = y + 4 * h;
                         uint2 codes;
-                        codes.x = (uint32_t)e4m3x2(z[0] * inv, z[1] * inv) | (uint32_t)e4m3x2(z[2] * inv, z[3] * inv) << 16;
-                        codes.y = (uint32_t)e4m3x2(z[4] * inv, z[5] * inv) | (uint32_t)e4m3x2(z[6] * inv, z[7] * inv) << 16;
+                        codes.x = (uint32_t)e4m3x2(z[0].x * inv, z[0].y * inv) | (uint32_t)e4m3x2(z[1].x * inv, z[1].y * inv) << 16;
+                        codes.y = (uint32_t)e4m3x2(z[2].x * inv, z[2].y * inv) | (uint32_t)e4m3x2(z[3].x * inv, z[3].y * inv) << 16;
                         *(reinterpret_cast<uint2 *>(to) + (h ? c1 : c0)) = e == 255u ? make_uint2(0, 0) : codes;
                     }
                     if (part == 0) (is_v ? p.kv.v_exp : p.kv.k_exp)[at] = (uint8_t)e;
@@ -202,7 +211,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
             if (row[i] >= 0 && (is_q || !WRITE)) {
                 uint16_t *dst = is_q ? p.q_out + t * p.q_out_stride + row[i] * D : p.k_out + t * p.k_out_stride + (row[i] - H) * D;
                 __stcs(reinterpret_cast<uint4 *>(dst) + c0, pack8(y));
-                __stcs(reinterpret_cast<uint4 *>(dst) + c1, pack8(y + 8));
+                __stcs(reinterpret_cast<uint4 *>(dst) + c1, pack8(y + 4));
             }
         }
     }

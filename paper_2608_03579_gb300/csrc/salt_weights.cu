@@ -92,8 +92,8 @@ struct Few {
     static constexpr int R = R_;
     static constexpr int N = 2 * R;                         // hi and lo
     static constexpr int CTAS = R == 16 ? 3 : 2;            // an SM
-    static constexpr int STAGERS = 4;                       // warps that stage queries
-    static constexpr int THREADS = 64 + 32 * STAGERS + 128;
+    static constexpr int STAGERS = R == 16 ? 2 : 4;         // warps that stage queries
+    static constexpr int THREADS = 96 + 32 * STAGERS + 128;
     static constexpr int KST = 3 * (128 / D), EST = 8;  // stages of keys, and of what goes with a tile
     static constexpr int SLOTS = 2;                         // segments' queries
     static constexpr int SB = R == 16 ? 4 : 2;              // buffers of scores
@@ -298,41 +298,27 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     const int n_lists = one_word(fits ? track[TH_FEW] : 0);
     Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_COST]) * KV : 0);
     bool ok = true;
+    // A tile's pages, a lane each, are looked up while the one's before are waited for.  Its codes are one warp's to fetch, its exponents and old weights
+    // another's (one for all took 800 cycles a tile, the longest of the roles).
+    auto pages_of = [&](const Walk &x) { return min(TRACK_TILE >> p.kv.page_log2, ((x.l.len - 1) >> p.kv.page_log2) - (x.j * TRACK_TILE >> p.kv.page_log2) + 1); };
+    auto look_up = [&](const Walk &x) { return lane < pages_of(x) ? __ldg(p.plan + p.pages_at + x.l.pages + (x.j * TRACK_TILE >> p.kv.page_log2) + lane) : 0; };
     if (!k.more()) {
     } else if (warp == 0) {
-        // ------------------------------------------------ loads: a lane per page of a tile
-        uint32_t ks = 0, kph = 0, es = 0, eph = 0, n = 0;
-        const int per = TRACK_TILE >> p.kv.page_log2;
-        // (a tile's pages are looked up while the one's before are waited for)
-        auto pages_of = [&](const Walk &x) { return min(per, ((x.l.len - 1) >> p.kv.page_log2) - (x.j * TRACK_TILE >> p.kv.page_log2) + 1); };
-        auto look_up = [&](const Walk &x) { return lane < pages_of(x) ? __ldg(p.plan + p.pages_at + x.l.pages + (x.j * TRACK_TILE >> p.kv.page_log2) + lane) : 0; };
+        // ------------------------------------------------ codes
+        uint32_t ks = 0, kph = 0, n = 0;
         int page = look_up(k);
-        for (; k.more() && ok; ++n) {
-            const int t = k.j * TRACK_TILE, pages = pages_of(k);
+        for (; k.more(); ++n) {
+            const int pages = pages_of(k);
             const int64_t row = first_row(p, page, k.kh);
-            const bool old = p.decay != 0.f && t < k.l.old;
+            const uint32_t full = base + L::K_FULL + 8 * ks;
             k.next(p);
             if (k.more()) page = look_up(k);
-            const uint32_t k_full = base + L::K_FULL + 8 * ks, e_full = base + L::E_FULL + 8 * es, e = base + L::E + es * L::E_BUF;
-            if (n >= (uint32_t)L::EST) ok = wait_bar(base + L::E_FREE + 8 * es, eph ^ 1, dead);
-            if (ok && n >= (uint32_t)L::KST) ok = wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead);
-            ok = __all_sync(0xffffffffu, ok);
+            if (n >= (uint32_t)L::KST) ok = __all_sync(0xffffffffu, wait_bar(base + L::K_FREE + 8 * ks, kph ^ 1, dead));
             if (!ok) break;
-            if (lane < pages) sts32(e + L::E_ROW + 4 * lane, (uint32_t)row);
+            if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * L::D);
             __syncwarp();
-            if (lane == 0) {
-                mbar_expect_tx(k_full, pages * p.kv.page * L::D);
-                mbar_expect_tx(e_full, pages * p.kv.page * (old ? 5 : 1));
-            }
-            __syncwarp();
-            if (lane < pages) {
-                const uint32_t at = lane * p.kv.page;
-                tma_load_2d(base + L::K + ks * L::SIDE + at * L::D, &p.kmap, 0, (int)row, k_full);
-                bulk_load(e + L::E_EXP + at, p.kv.k_exp + row, p.kv.page, e_full);
-                if (old) bulk_load(e + L::E_W + 4 * at, p.weights + row, p.kv.page * 4, e_full);
-            }
+            if (lane < pages) tma_load_2d(base + L::K + ks * L::SIDE + lane * p.kv.page * L::D, &p.kmap, 0, (int)row, full);
             if (++ks == (uint32_t)L::KST) ks = 0, kph ^= 1;
-            if (++es == (uint32_t)L::EST) es = 0, eph ^= 1;
         }
         if (!ok) {  // copies in flight land before the CTA ends
             if (lane == 0) {
@@ -340,6 +326,35 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
             }
             for (uint32_t i = 0; i < min(n, (uint32_t)L::KST); ++i) mbar_wait(base + L::K_FULL + 8 * ((n - 1 - i) % L::KST), ((n - 1 - i) / L::KST) & 1);
+        }
+    } else if (warp == 2 + L::STAGERS) {
+        // ------------------------------------------------ exponents, old weights, where they lie
+        uint32_t es = 0, eph = 0, n = 0;
+        int page = look_up(k);
+        for (; k.more(); ++n) {
+            const int pages = pages_of(k);
+            const int64_t row = first_row(p, page, k.kh);
+            const bool old = p.decay != 0.f && k.j * TRACK_TILE < k.l.old;
+            const uint32_t full = base + L::E_FULL + 8 * es, e = base + L::E + es * L::E_BUF, at = lane * p.kv.page;
+            k.next(p);
+            if (k.more()) page = look_up(k);
+            if (n >= (uint32_t)L::EST) ok = __all_sync(0xffffffffu, wait_bar(base + L::E_FREE + 8 * es, eph ^ 1, dead));
+            if (!ok) break;
+            if (lane < pages) sts32(e + L::E_ROW + 4 * lane, (uint32_t)row);
+            __syncwarp();
+            if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * (old ? 5 : 1));
+            __syncwarp();
+            if (lane < pages) {
+                bulk_load(e + L::E_EXP + at, p.kv.k_exp + row, p.kv.page, full);
+                if (old) bulk_load(e + L::E_W + 4 * at, p.weights + row, p.kv.page * 4, full);
+            }
+            if (++es == (uint32_t)L::EST) es = 0, eph ^= 1;
+        }
+        if (!ok) {  // as above
+            if (lane == 0) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+            }
             for (uint32_t i = 0; i < min(n, (uint32_t)L::EST); ++i) mbar_wait(base + L::E_FULL + 8 * ((n - 1 - i) % L::EST), ((n - 1 - i) / L::EST) & 1);
         }
     } else if (warp == 1) {
