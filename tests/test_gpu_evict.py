@@ -137,6 +137,12 @@ def test_long_lines(salt_lib, ctx, n, keep, first, recent, kind, dim, page, kv_h
     c.check([keep, 50], scores_of(c, kind), first, recent)
 
 
+def test_lines_longer_than_shared_memory(salt_lib, ctx):
+    """Scores that no cluster's shared memory holds are read again."""
+    c = Cache(salt_lib, ctx, [400003, 17], dim=64, page=128, kv_heads=1, layers=1)
+    c.check([123456, 17], scores_of(c, "close"), 3, 1000)
+
+
 def test_many_lines(salt_lib, ctx):
     lens = [int(n) for n in np.random.RandomState(1).randint(1, 200, 300)]
     c = Cache(salt_lib, ctx, lens, kv_heads=4, layers=2)
@@ -202,6 +208,23 @@ def test_captured_and_replayed(salt_lib, ctx):
     torch.cuda.synchronize()
     assert salt_lib.salt_get_device_error(ctx) == 0x80
     assert all(np.array_equal(a.view(np.uint8), b.view(np.uint8)) for a, b in zip(before, c.host()))
+
+
+def test_captured_for_short_lines_and_replayed_on_long_ones(salt_lib, ctx):
+    c = Cache(salt_lib, ctx, [9001, 300], layers=1, kv_heads=3, page=64)
+    scores, keep = scores_of(c, "normal"), torch.tensor([5000, 100], dtype=torch.int32, device="cuda")
+    kept = torch.full((1, 2, 3, 5000), -7, dtype=torch.int32, device="cuda")
+    c.build(kv_len=[40, 300])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        salt_lib.salt_attn_evict(c.plan, 0, 1, keep, scores, kept, 1, 9, c.t["weights"])
+    c.build()
+    before = c.host()
+    graph.replay()
+    torch.cuda.synchronize()
+    arrays, want = evict(before, c.batch, 64, [0], [5000, 100], scores.cpu().numpy(), np.full((1, 2, 3, 5000), -7), 1, 9)
+    assert np.array_equal(kept.cpu().numpy(), want) and salt_lib.salt_get_device_error(ctx) == 0
+    assert all(np.array_equal(a.view(np.uint8), b.view(np.uint8)) for a, b in zip(c.host(), arrays))
 
 
 def test_refusals(salt_lib, ctx):

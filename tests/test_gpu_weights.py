@@ -290,6 +290,39 @@ def test_captured_and_replayed(salt_lib, ctx):
     assert salt_lib.salt_get_device_error(ctx) == 0
 
 
+def test_captured_for_one_kind_of_lists_and_replayed_on_others(salt_lib, ctx):
+    """Single tokens, long chunks and both, each captured and replayed on the others."""
+    big = Weights(salt_lib, ctx, [120, 1, 3], [300, 70, 5], [0, -1, 0], [200], heads=4, kv_heads=2, dim=64)
+    batches = [big.batch, dict(big.batch, q_len=[1, 1, 3], kv_len=[200, 70, 5]), dict(big.batch, q_len=[120, 0, 0])]
+    w, q, lse = big.w.cuda(), big.q.cuda(), big.lse.cuda()
+    graphs = []
+
+    def build(b):
+        salt_lib.salt_attn_build(big.plan, salt_lib.salt_attn_batch(b["q_len"], b["kv_len"], b["page_ptr"], b["pages"], b["group"], b["group_len"],
+                                                                    b["group_page_ptr"], b["group_pages"]))
+    for b in batches:
+        build(b)
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            salt_lib.salt_attn_weights(big.plan, 0, q, lse, big.scale, w, 0.5)
+    for i, g in enumerate(graphs):
+        for b in batches:
+            build(b)
+            w.copy_(big.w)
+            g.replay()
+            torch.cuda.synchronize()
+            if sum(b["q_len"]) > sum(batches[i]["q_len"]):
+                assert salt_lib.salt_get_device_error(ctx) == 0x80 and torch.equal(w.cpu(), big.w)
+                continue
+            assert salt_lib.salt_get_device_error(ctx) == 0
+            T = sum(b["q_len"])
+            want, tol = add_weights(big.w[0], big.k_values, big.q[:T], big.lse[:T], b, 16, big.scale, 0.5)
+            # (log-sums of another batch: their exponentials may pass fp32's range)
+            fine = want.abs() < 1e30
+            got = w[0].cpu().double()
+            assert bool(((got - want).abs() <= tol)[fine].all())
+
+
 def test_refusals(salt_lib, ctx):
     w = Weights(salt_lib, ctx, [1, 2], [20, 30], dim=64)
     q, lse, x = w.q.cuda(), w.lse.cuda(), w.w.cuda()
@@ -350,9 +383,9 @@ def test_refusals(salt_lib, ctx):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
-@pytest.mark.parametrize("n,kv,prompt,heads,kv_heads", [(700, 900, 0, 8, 1), (1500, 1500, 300, 2, 2), (333, 5000, 64, 3, 1)])
+@pytest.mark.parametrize("n,kv,prompt,heads,kv_heads", [(700, 900, 0, 8, 1), (1500, 1500, 300, 2, 2), (333, 5000, 64, 3, 1), (80, 300, 140000, 8, 8)])
 def test_rows_of_a_tile_split(salt_lib, ctx, n, kv, prompt, heads, kv_heads, dim):
-    """Few tiles of many rows: parts of a unit's rows meet, the same each time; on the GPU in 64 bits."""
+    """Few tiles of many rows: parts of a unit's rows meet, the same each time; and more tiles than a build lists. On the GPU in 64 bits."""
     page = 64
     lens = [prompt, kv]
     need = [-(-x // page) for x in lens]

@@ -4,6 +4,7 @@ import ctypes
 import math
 
 import numpy as np
+import pytest
 import torch
 
 from keeping_reference import add_weights, evict, kept_places
@@ -14,6 +15,21 @@ def test_null_handles(salt_lib):
     assert lib.salt_attn_track(None) == 1
     assert lib.salt_attn_weights(None, 0, None, 0, None, 1.0, 1.0, None, None) == 1
     assert lib.salt_attn_evict(None, 0, 1, None, 0, 0, None, None, None, ctypes.c_int64(0), None) == 1
+
+
+def test_tensors_are_checked_before_the_call(salt_lib):
+    salt_lib._load_types()
+    kv, plan = object.__new__(salt_lib.KvCache), object.__new__(salt_lib.AttnPlan)
+    kv.handle = plan.handle = plan.ctx = None
+    kv.rows_shape, kv.n_kv_heads = torch.Size((1, 2, 2, 16)), 2
+    plan.kv, plan.n_heads, plan.head_dim, plan.n_tokens, plan.n_seqs = kv, 4, 64, 3, 1
+    q, lse, w = torch.zeros((3, 4, 64), dtype=torch.bfloat16), torch.zeros((3, 4)), torch.zeros((1, 2, 2, 16))
+    with pytest.raises(ValueError):
+        salt_lib.salt_attn_weights(plan, 0, q, lse, 1.0, w)                                         # host tensors
+    keep, kept = torch.zeros(1, dtype=torch.int32), torch.zeros((1, 1, 2, 5), dtype=torch.int32)
+    for args in ((keep, w, kept), (keep, w, kept[:, :, :1]), (keep, w, kept[0])):
+        with pytest.raises(ValueError):
+            salt_lib.salt_attn_evict(plan, 0, 1, *args)
 
 
 def test_kept_places():
