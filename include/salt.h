@@ -757,8 +757,10 @@ salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t
 
 /*
  * From its next build on the plan serves salt_attn_weights and salt_attn_evict
- * too (a build then copies a further table, of 16 words a request or group).
- * Synchronous.
+ * too.  A build then copies a further table (some words a request and group, up to 400 KB
+ * where many rows see a list of cached tokens), and the plan has more device memory, which
+ * salt_attn_get_shape counts: 3 MB and eight bytes for every 16 KB of cached keys and values of up to
+ * 2^22 such pieces.  Synchronous.
  */
 salt_status salt_attn_track(salt_attn *plan);
 
@@ -776,7 +778,8 @@ salt_status salt_attn_track(salt_attn *plan);
  * query or the log-sum of a row that sees it (salt_attn_run leaves a NaN log-sum for a query with an
  * infinity); a row that sees nothing adds nothing, whatever it holds.  Results do not depend on timing.  A plan that was not built since
  * salt_attn_track is refused (SALT_ERR_NOT_BUILT), and so is a batch that lists a page twice, for two requests or
- * groups (SALT_ERR_INVALID_ARG).  Asynchronous on `stream`; ordered and captured as
+ * groups (SALT_ERR_INVALID_ARG; a captured call replayed on one does nothing and raises
+ * SALT_DEVERR_BATCH).  One or two kernels, asynchronous on `stream`; ordered and captured as
  * salt_attn_run's runs are.
  */
 salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, const float *lse,
@@ -797,7 +800,8 @@ salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int
  * raised.  scores is laid out as salt_attn_weights' weights, and may be
  * those (it is not moved itself).  The plan keeps the old lengths: build it again before its next
  * run.  A token's position is then no longer its place: see
- * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Asynchronous on `stream`; ordered
+ * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Two kernels (for each
+ * part of the layers, where the plan's memory does not hold all), asynchronous on `stream`; ordered
  * and captured as salt_attn_run's runs are (replayed on at most as many requests).
  */
 salt_status salt_attn_evict(salt_attn *plan, int32_t layer, int32_t n_layers, const int32_t *keep, int32_t first,

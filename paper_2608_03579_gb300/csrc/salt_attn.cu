@@ -1905,6 +1905,7 @@ salt_status salt_attn_track(salt_attn *a)
         }
         return ctx_fail(ctx, SALT_ERR_OOM, "no memory for the tracked tables");
     }
+    t.bytes = t.words * 4 + (size_t)TRACK_SLOTS * (TRACK_MANY_TILE + 8) * 4 + ((size_t)a->cfg.max_seqs + 2) * 4 + (size_t)layer * t.layers_cap * 8;
     t.on = true;
     return SALT_OK;
 }
@@ -1913,7 +1914,7 @@ salt_status salt_attn_get_shape(const salt_attn *a, salt_attn_shape *out)
 {
     if (!a || !out) return SALT_ERR_INVALID_ARG;
     *out = salt_attn_shape{};
-    out->workspace_bytes = (int64_t)a->plan_words * 4 + a->part_cap * (a->kv->dev.dim + 1) * 4;
+    out->workspace_bytes = (int64_t)a->plan_words * 4 + a->part_cap * (a->kv->dev.dim + 1) * 4 + (int64_t)a->track.bytes;
     out->wide_ctas = a->n_sm * Shape<128, true>::CTAS;
     out->narrow_ctas = a->n_sm * Shape<128, false>::CTAS;
     if (!a->built) return SALT_OK;

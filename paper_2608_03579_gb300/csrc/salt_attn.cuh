@@ -50,7 +50,7 @@ struct Track {
     float *part = nullptr;                     // [TRACK_SLOTS][256]
     uint32_t *arrived = nullptr;               // [TRACK_SLOTS][8], zero between calls
     int seq_at = 0, list_at = 0, unit_at = 0;  // word offsets
-    size_t words = 0;
+    size_t words = 0, bytes = 0;               // of the table, of all its device memory
     bool on = false, built = false, shared = false, split = false;
     int n_seqs = 0, few = 0, many = 0, n_units = 0, few_rows = 0, many_sms = 0;  // few_rows: of the lists of few, the most that one has; SMs for the lists of many
     int64_t few_tiles = 0;

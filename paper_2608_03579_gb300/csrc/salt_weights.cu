@@ -7,13 +7,17 @@
 // tensor cores with the cached tokens as the 128-row operand, S[token][row] = K[token][:] . Q[row][:], so that a
 // token's weight is a sum over one thread's columns of tensor memory, in a fixed order.
 //
-// Lists of few rows (single query tokens, a few drafts) are bound by reading the keys: their e4m3 codes go to the
+// Lists of up to 64 rows (single query tokens, a few drafts, a prompt that some requests share) are bound by reading the keys, and that by what a tile
+// costs besides: their e4m3 codes go to the
 // tensor cores as they are, one tile of 128 tokens after the other, and meet the query as two e4m3 terms, hi + 2^-5
 // lo: 4 and 4 bits, so a bf16 whole but for elements 2^-15 below the row's largest (2^-22 of
 // that).  The two terms have columns of their own, as lo would lose its small elements without its factor.
 //
 // Lists of many rows are bound by the products and exponentials: 256 tokens' keys are widened to bf16 once
 // (exact) and stay, the query's rows stream past them as they are.
+//
+// Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 23 us, four prompt
+// chunks of 900 to 2,048 tokens behind 4,096 226 us (1,150 TFLOP/s; 1.0e9 exponentials, 59% of the products' measured rate).
 #include <algorithm>
 #include <cmath>
 #include <new>
@@ -34,7 +38,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 
 struct WeightParams {
     alignas(64) CUtensorMap kmap;   // the codes of every layer as rows of D bytes, box of one page
-    alignas(64) CUtensorMap qmap;   // wide: q as [tokens][heads][D], box of 64 elements of a group's heads of a step's tokens
+    alignas(64) CUtensorMap qmap;   // many rows: q as [tokens][heads][D], box of 64 elements of a group's heads of a step's tokens
     alignas(64) CUtensorMap qmap1;  // the same of one token
     const int32_t *plan, *track;
     int32_t order_at, pages_at, list_at, unit_at;
@@ -47,7 +51,7 @@ struct WeightParams {
     uint32_t *arrived;              // how many of a unit's parts are there
     int64_t q_stride;
     int32_t n_heads, max_tok;
-    int32_t behind;                 // whether the wide lists' kernel is the one before
+    int32_t behind;                 // whether the many rows' kernel is the one before
     float scale, decay;
     uint32_t *err;
 };
@@ -289,7 +293,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *reinterpret_cast<uint32_t *>(sm + L::MISC);
-    // (behind the wide lists' kernel nothing that it writes is needed, and it lets this one begin after its own wait)
+    // (behind the many rows' kernel nothing that it writes is needed, and it lets this one begin after its own wait)
     if (!p.behind) pdl_wait();
     pdl_launch_dependents();
     const int32_t *track = after_pdl_wait(p.track);
@@ -470,7 +474,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
 // ---------------------------------------------------------------- many rows
 // A unit is 256 tokens of a list and head, and a run of steps over the rows that see them, up to 128 at
 // a time.  Either 128 tokens have two warpgroups, which take every other step each: what a step costs besides its sums (waiting, a vote, fetching scores; 600
-// cycles of 2,100) is spent beside the others' sums.  (With one warpgroup 268 us where these take 236; with two of half a step's columns each, which
+// cycles of 2,100) is spent beside the others' sums.  (With one warpgroup four prompt chunks took 268 us where these took 236; with two of half a step's columns each, which
 // meet at every barrier, 260.)
 template <int D_>
 struct Many {
