@@ -1295,8 +1295,9 @@ int items_of(const RowTile &x, double most, int *per_item)
 // Of a unit of a tracked plan's lists of many rows, in steps of 128 rows: what it costs besides, and the least
 // that a part of one takes.
 constexpr int UNIT_COST = 3, LEAST_STEPS = 6;
-// Measured: a step on an SM, and a unit of few_cost on one of its CTAs' SM.
-constexpr double STEP_US = 0.95, FEW_US = 0.07;
+// A step on an SM, and a unit of few_cost there, as they balance the two kernels (the second one starts later; 64 decoding requests of four
+// prompts took 23.3 us with 0.07 for the latter, 19.0 with 0.12 and 0.16, 20.5 with 0.22; 48 with drafts 16.5, 13.6, 13.2 and 14.8).
+constexpr double STEP_US = 0.95, FEW_US = 0.15;
 
 // Items of one cost.
 struct Same {

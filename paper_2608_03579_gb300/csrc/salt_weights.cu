@@ -16,7 +16,7 @@
 // Lists of many rows are bound by the products and exponentials: 256 tokens' keys are widened to bf16 once
 // (exact) and stay, the query's rows stream past them as they are.
 //
-// Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 23 us, four prompt
+// Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 19 us, four prompt
 // chunks of 900 to 2,048 tokens behind 4,096 226 us (1,150 TFLOP/s; 1.0e9 exponentials, 59% of the products' measured rate).
 #include <algorithm>
 #include <cmath>
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
 template <int D_>
 struct Many {
     static constexpr int D = D_;
-    static constexpr int THREADS = 96 + 4 * 128;            // (104 registers a thread; with a warp more 96, and scores spilled while they were fetched)
+    static constexpr int THREADS = 128 + 4 * 128;           // (96 registers a thread: a score that is spilled is one that may not have come yet)
     static constexpr int QST = D == 128 ? 4 : 6, MST = 4;   // stages of queries, and of what goes with a step
     // Tensor memory: the keys of either 128 tokens as bf16, three buffers of 128 scores for both in turn.  (With the keys in shared
     // memory a step's products read 128 KB from there, as long as they take themselves, besides all else: 277 us where this took 253.)
@@ -693,41 +693,10 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     bool ok = true;
     if (!it.more()) {
     } else if (warp == 0) {
-        // ------------------------------------------------ loads: a unit's codes while the one before is under way, and its
-        // steps' queries, whole where their tokens follow each other, else token by token
-        uint32_t used[2] = {0, 0}, n = 0, st = 0, ph = 0;
-        const int page_per = 128 >> p.kv.page_log2;
+        // ------------------------------------------------ a step's queries, whole where their tokens follow each other, else token by
+        // token
+        uint32_t n = 0, st = 0, ph = 0;
         const uint32_t q_bytes = G * 128 * (L::D / 64);
-        auto load_keys = [&](const Unit &u) {
-            for (int w = 0; w < (u.two ? 2 : 1) && ok; ++w) {
-                const int t = u.t0 + 128 * w, first = t >> p.kv.page_log2;
-                const int pages = min(page_per, ((u.l.len - 1) >> p.kv.page_log2) - first + 1);
-                int page = 0;
-                if (lane < pages) page = __ldg(p.plan + p.pages_at + u.l.pages + first + lane);
-                const int64_t row = first_row(p, page, u.kh);
-                const uint32_t buf = 2 * w + (used[w] & 1), full = base + L::K_FULL + 8 * buf, at = lane * p.kv.page;
-                if (used[w] > 1) ok = wait_bar(base + L::K_FREE + 8 * buf, ((used[w] >> 1) - 1) & 1, dead);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) return;
-                if (lane < pages) sts32(base + L::ROWS + 32 * buf + 4 * lane, (uint32_t)row);
-                __syncwarp();
-                if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * (L::D + 1));
-                __syncwarp();
-                if (lane < pages) {
-                    tma_load_2d(base + L::RAW + buf * L::RAW_TILE + at * L::D, &p.kmap, 0, (int)row, full);
-                    bulk_load(base + L::EXPS + 128 * buf + at, p.kv.k_exp + row, p.kv.page, full);
-                }
-                ++used[w];
-            }
-        };
-        Units keys = it;  // (two units ahead)
-        auto next_keys = [&]() {
-            if (!ok || !keys.more()) return;
-            load_keys(keys.get(p, per));
-            keys.advance(p);
-        };
-        next_keys();
-        next_keys();
         Steps s(p, it, per);
         int tok[4];
         auto look_up = [&](const Steps &x, int (&t)[4]) {
@@ -737,10 +706,6 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
         };
         look_up(s, tok);
         while (ok && s.live) {
-            Steps t = s;
-            t.advance(p, per);
-            int ahead[4] = {0, 0, 0, 0};
-            if (t.live) look_up(t, ahead);
             const int m = s.tokens(per), tok0 = __shfl_sync(0xffffffffu, tok[0], 0), kh = s.u.kh;
             bool run = true;
 #pragma unroll
@@ -766,10 +731,8 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             __syncwarp();
             ++n;
             if (++st == (uint32_t)L::QST) st = 0, ph ^= 1;
-            if (s.r == s.u.r0) next_keys();  // (this unit's codes are widened before its first products)
-            s = t;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) tok[k] = ahead[k];
+            s.advance(p, per);
+            if (s.live) look_up(s, tok);
         }
         if (!ok) {  // copies in flight land before the CTA ends
             if (lane == 0) {
@@ -777,8 +740,6 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 atomicOr(p.err, SALT_DEVERR_TIMEOUT);
             }
             for (uint32_t i = 0; i < min(n, (uint32_t)L::QST); ++i) mbar_wait(base + L::Q_FULL + 8 * ((n - 1 - i) % L::QST), ((n - 1 - i) / L::QST) & 1);
-            for (int w = 0; w < 2; ++w)
-                for (uint32_t i = 0; i < min(used[w], 2u); ++i) mbar_wait(base + L::K_FULL + 8 * (2 * w + ((used[w] - 1 - i) & 1)), ((used[w] - 1 - i) >> 1) & 1);
         }
     } else if (warp == 1) {
         // ------------------------------------------------ MMA issue
@@ -889,9 +850,43 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
             *dead = 1;
             atomicOr(p.err, SALT_DEVERR_TIMEOUT);
         }
+    } else if (warp == 3) {
+        // ------------------------------------------------ the units' codes, up to two units ahead
+        uint32_t used[2] = {0, 0};
+        const int page_per = 128 >> p.kv.page_log2;
+        for (; it.more() && ok; it.advance(p)) {
+            const Unit u = it.get(p, per);
+            for (int w = 0; w < (u.two ? 2 : 1); ++w) {
+                const int t = u.t0 + 128 * w, first = t >> p.kv.page_log2;
+                const int pages = min(page_per, ((u.l.len - 1) >> p.kv.page_log2) - first + 1);
+                int page = 0;
+                if (lane < pages) page = __ldg(p.plan + p.pages_at + u.l.pages + first + lane);
+                const int64_t row = first_row(p, page, u.kh);
+                const uint32_t buf = 2 * w + (used[w] & 1), full = base + L::K_FULL + 8 * buf, at = lane * p.kv.page;
+                if (used[w] > 1) ok = __all_sync(0xffffffffu, wait_bar(base + L::K_FREE + 8 * buf, ((used[w] >> 1) - 1) & 1, dead));
+                if (!ok) break;
+                if (lane < pages) sts32(base + L::ROWS + 32 * buf + 4 * lane, (uint32_t)row);
+                __syncwarp();
+                if (lane == 0) mbar_expect_tx(full, pages * p.kv.page * (L::D + 1));
+                __syncwarp();
+                if (lane < pages) {
+                    tma_load_2d(base + L::RAW + buf * L::RAW_TILE + at * L::D, &p.kmap, 0, (int)row, full);
+                    bulk_load(base + L::EXPS + 128 * buf + at, p.kv.k_exp + row, p.kv.page, full);
+                }
+                ++used[w];
+            }
+        }
+        if (!ok) {  // copies in flight land before the CTA ends
+            if (lane == 0) {
+                *dead = 1;
+                atomicOr(p.err, SALT_DEVERR_TIMEOUT);
+            }
+            for (int w = 0; w < 2; ++w)
+                for (uint32_t i = 0; i < min(used[w], 2u); ++i) mbar_wait(base + L::K_FULL + 8 * (2 * w + ((used[w] - 1 - i) & 1)), ((used[w] - 1 - i) >> 1) & 1);
+        }
     } else {
         // ------------------------------------------------ a thread's token: its rows of scores, its weight
-        const int w = (warp - 3) >> 2 & 1, par = (warp - 3) >> 3, me = 32 * (warp & 3) + lane;  // the 128 tokens, the steps
+        const int w = (warp - 4) >> 2 & 1, par = (warp - 4) >> 3, me = tid & 127;  // the 128 tokens, the steps
         const uint32_t t_lane = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         uint32_t n = 0, b = w, jobs = 0, units = 0, done = 0;  // (b: the buffer of the step's job)
         float a = 0.f;
