@@ -12,6 +12,12 @@
 // A row (token, head) goes to D / 16 lanes, 16 elements each in two pieces of 8: where pairs are (i, i + rot / 2)
 // the pieces are rot / 2 elements apart, so that a lane has both elements of its pairs.  A warp deals with rows of one token,
 // whose sines and cosines it computes once, two pairs a lane, and hands round through shared memory.
+//
+// 16,384 tokens with 32 and 8 heads of 128, norms, the keys and values into the cache: 60 us, 6.1 TB/s (90% of a copy's rate).  Rows
+// come by copies of 16 bytes a lane into shared memory, two passes ahead of those at hand (loaded into registers, 64 of them for four
+// CTAs an SM: 73 us), and issue slots are the rest: weights widened once a CTA and codes' maxima for keys and values alone
+// gave 6 of those us.  Warps that go on from token to token took 62, deeper copies 5 to 9 more, three passes no less.
+// 64 decoding tokens: 3.2 us, a launch and a row's chain of loads and sums.
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
@@ -37,7 +43,7 @@ namespace {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_WARPS = ROPE_THREADS / 32;
-constexpr int ROPE_ROWS = 2;  // rows a lane has under way
+constexpr int ROPE_ROWS = 2;  // rows a lane deals with side by side
 
 struct RopeParams {
     const uint16_t *q, *k, *v, *q_norm, *k_norm;
@@ -82,6 +88,8 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
 {
     constexpr int LPR = D / 16, RPW = 32 / LPR;  // lanes a row, rows a warp deals with at a time
     __shared__ __align__(16) float2 s_turn[ROPE_WARPS][64];
+    __shared__ uint4 s_rows[2][ROPE_ROWS][2][ROPE_THREADS];  // a lane's pieces of the rows at hand and of the next ones
+    __shared__ float4 s_norm[2][2][D / 8];  // weights of query and key heads, offset added: of 8 elements the first and the last 4
     // (the warp's number from a shuffle: loops by it are known to be a warp's then, and the shuffles in them are quick)
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, part = lane % LPR;
     const uint32_t task = blockIdx.x * ROPE_WARPS + warp;
@@ -95,15 +103,42 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
     const uint64_t f0 = p.freq[lane], f1 = p.freq[lane + 32];
     pdl_wait();  // (launched beside the end of what came before)
     pdl_launch_dependents();
+    if (p.q_norm || p.k_norm) {
+        for (int i = threadIdx.x; i < 2 * D / 4; i += ROPE_THREADS) {
+            const uint16_t *norm = after_pdl_wait(i < D / 4 ? p.q_norm : p.k_norm);
+            if (!norm) continue;
+            const int e = i % (D / 4);
+            const uint2 x = __ldg(reinterpret_cast<const uint2 *>(norm) + e);
+            s_norm[i / (D / 4)][e & 1][e / 2] = make_float4(__uint_as_float(x.x << 16) + p.offset, __uint_as_float(x.x & 0xffff0000u) + p.offset,
+                                                            __uint_as_float(x.y << 16) + p.offset, __uint_as_float(x.y & 0xffff0000u) + p.offset);
+        }
+        __syncthreads();
+    }
     if (t >= p.n_tokens) return;
     const int32_t *positions = after_pdl_wait(p.positions), *slots = WRITE ? after_pdl_wait(p.slots) : nullptr;
     const uint16_t *q = after_pdl_wait(p.q), *k = after_pdl_wait(p.k), *v = WRITE ? after_pdl_wait(p.v) : nullptr;
     const int H = p.n_heads, KV = p.n_kv_heads;
     const int pass1 = min((p.rows + RPW - 1) / RPW, (split + 1) * p.passes);
+    // Copies the lane's pieces of a pass's rows to shared memory, while the rows before them are dealt with.  (Rows past the
+    // token's are zeros: every lane stays for the shuffles.)
+    auto fetch = [&](int pass, int buf) {
+#pragma unroll
+        for (int i = 0; i < ROPE_ROWS; ++i) {
+            const int r = (pass + i) * RPW + lane / LPR, row = min(r, p.rows - 1);
+            const bool there = pass + i < pass1 && r < p.rows;
+            const uint16_t *src = row < H ? q + t * p.q_stride + row * D
+                                  : row < H + KV ? k + t * p.k_stride + (row - H) * D
+                                                 : v + t * p.v_stride + (row - H - KV) * D;
+            cp_async16(smem_u32(&s_rows[buf][i][0][threadIdx.x]), reinterpret_cast<const uint4 *>(src) + c0, there);
+            cp_async16(smem_u32(&s_rows[buf][i][1][threadIdx.x]), reinterpret_cast<const uint4 *>(src) + c1, there);
+        }
+        cp_async_commit();
+    };
+    fetch(split * p.passes, 0);
     const int slot = WRITE ? __ldg(slots + t) : -1, page = WRITE ? slot >> p.kv.page_log2 : 0;
     const bool stored = WRITE && slot >= 0 && page < p.kv.n_pages;
     if (WRITE && split == 0 && lane == 0 && !stored && slot != -1) atomicOr(p.err, SALT_DEVERR_KV_SLOT);
-    // sines and cosines of the lane's pairs, and of the kind of head at hand its weights, two at a time
+    // sines and cosines of the lane's pairs, two at a time
     float2 c[4], s[4];
     {
         const int64_t at = __ldg(positions + t);
@@ -123,27 +158,18 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
             s[e / 2] = make_float2(x.y, x.w);
         }
     }
-    for (int pass = split * p.passes; pass < pass1; pass += ROPE_ROWS) {
-        uint4 x[ROPE_ROWS][2];
-        int row[ROPE_ROWS];
+    int buf = 0;
+    for (int pass = split * p.passes; pass < pass1; pass += ROPE_ROWS, buf ^= 1) {
+        asm volatile("" ::: "memory");  // (what is fetched takes the place of rows that were read)
+        fetch(pass + ROPE_ROWS, buf ^ 1);
+        cp_async_wait<1>();
 #pragma unroll
         for (int i = 0; i < ROPE_ROWS; ++i) {
-            row[i] = (pass + i) * RPW + lane / LPR;
-            x[i][0] = x[i][1] = make_uint4(0, 0, 0, 0);
-            if (pass + i >= pass1 || row[i] >= p.rows) row[i] = -1;  // every lane stays for the shuffles
-            if (row[i] < 0) continue;
-            const uint16_t *src = row[i] < H ? q + t * p.q_stride + row[i] * D
-                                  : row[i] < H + KV ? k + t * p.k_stride + (row[i] - H) * D
-                                                    : v + t * p.v_stride + (row[i] - H - KV) * D;
-            x[i][0] = __ldcs(reinterpret_cast<const uint4 *>(src) + c0);
-            x[i][1] = __ldcs(reinterpret_cast<const uint4 *>(src) + c1);
-        }
-#pragma unroll
-        for (int i = 0; i < ROPE_ROWS; ++i) {
-            const bool is_q = row[i] < H, is_v = row[i] >= H + KV;
+            const int r = (pass + i) * RPW + lane / LPR, row = pass + i < pass1 && r < p.rows ? r : -1;
+            const bool is_q = row < H, is_v = row >= H + KV;
             float2 y[8];
-            unpack8(x[i][0], y);
-            unpack8(x[i][1], y + 4);
+            unpack8(s_rows[buf][i][0][threadIdx.x], y);
+            unpack8(s_rows[buf][i][1][threadIdx.x], y + 4);
             const uint16_t *norm = is_q ? p.q_norm : p.k_norm;
             if (p.q_norm || p.k_norm) {
                 float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -159,13 +185,13 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
                     s1 = sum_lanes<LPR>(s1);
                     if (!(ss <= FLT_MAX)) r = rsqrtf(s1 * (1.f / D)) * down;
                 }
-                if (norm && !is_v && row[i] >= 0) {
+                if (norm && !is_v && row >= 0) {
                     float2 w[8];
-                    {
-                        unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c0), w);
-                        unpack8(__ldg(reinterpret_cast<const uint4 *>(norm) + c1), w + 4);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) w[e] = add2(w[e], make_float2(p.offset, p.offset));
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 x = s_norm[is_q ? 0 : 1][e & 1][e < 2 ? c0 : c1];
+                        w[2 * e] = make_float2(x.x, x.y);
+                        w[2 * e + 1] = make_float2(x.z, x.w);
                     }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] = mul2(mul2(y[e], make_float2(r, r)), w[e]);
@@ -186,7 +212,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
                     }
                 }
             }
-            if (WRITE) {
+            if (WRITE && (pass + i) * RPW + RPW > H) {  // (any of the warp's rows)
                 uint32_t a = 0;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) a = max(a, max(__float_as_uint(y[e].x) & 0x7fffffffu, __float_as_uint(y[e].y) & 0x7fffffffu));
@@ -195,7 +221,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
                 if (!is_q && stored) {
                     const uint32_t e = row_exp(a > 0x7f800000u ? 0x7f800000u : a);
                     const float inv = row_inv(e);
-                    const uint32_t at = cache_row(p.kv, p.first_page, page, slot, is_v ? row[i] - H - KV : row[i] - H);
+                    const uint32_t at = cache_row(p.kv, p.first_page, page, slot, is_v ? row - H - KV : row - H);
                     uint8_t *to = (is_v ? p.kv.v : p.kv.k) + (uint64_t)at * D;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -208,13 +234,14 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
                     if (part == 0) (is_v ? p.kv.v_exp : p.kv.k_exp)[at] = (uint8_t)e;
                 }
             }
-            if (row[i] >= 0 && (is_q || !WRITE)) {
-                uint16_t *dst = is_q ? p.q_out + t * p.q_out_stride + row[i] * D : p.k_out + t * p.k_out_stride + (row[i] - H) * D;
+            if (row >= 0 && (is_q || !WRITE)) {
+                uint16_t *dst = is_q ? p.q_out + t * p.q_out_stride + row * D : p.k_out + t * p.k_out_stride + (row - H) * D;
                 __stcs(reinterpret_cast<uint4 *>(dst) + c0, pack8(y));
                 __stcs(reinterpret_cast<uint4 *>(dst) + c1, pack8(y + 4));
             }
         }
     }
+    cp_async_wait<0>();
 }
 
 salt_status check_heads(salt_rope *r, const char *what, const void *x, int64_t stride, int heads)
@@ -254,9 +281,10 @@ salt_status launch_rope(salt_rope *r, RopeParams &p, cudaStream_t stream)
     std::copy(r->freq, r->freq + 64, p.freq);
     const int per = 32 / (r->dim / 16), all = (p.rows + per - 1) / per;  // passes of a token
     // A warp takes all of a token's passes where there are tokens enough to fill the SMs (its sines are
-    // computed once), fewer where not.
+    // computed once), fewer where not, two by two.
     const int64_t fill = 152 * 32;
-    p.passes = (int)std::min<int64_t>(all, std::max<int64_t>(1, (int64_t)p.n_tokens * all / fill));
+    const int64_t few = std::max<int64_t>(1, (int64_t)p.n_tokens * all / fill);
+    p.passes = (int)std::min<int64_t>(all, (few + ROPE_ROWS - 1) / ROPE_ROWS * ROPE_ROWS);
     p.splits = (all + p.passes - 1) / p.passes;
     const auto kernel = r->dim == 128 ? (r->mixed ? rope_kernel<128, WRITE, true> : rope_kernel<128, WRITE, false>)
                                       : (r->mixed ? rope_kernel<64, WRITE, true> : rope_kernel<64, WRITE, false>);

@@ -17,7 +17,8 @@
 // (exact) and stay, the query's rows stream past them as they are.
 //
 // Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 19 us, four prompt
-// chunks of 900 to 2,048 tokens behind 4,096 226 us (1,150 TFLOP/s; 1.0e9 exponentials, 59% of the products' measured rate).
+// chunks of 900 to 2,048 tokens behind 4,096 221 us (1,170 TFLOP/s, 61% of the products' measured rate; 1.0e9 exponentials, whose pipe
+// is 53% busy as the tensor cores are).
 #include <algorithm>
 #include <cmath>
 #include <new>
