@@ -148,7 +148,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
             // in half turns, [-1, 1); what fp32 leaves of them turns the pair of sine and cosine (rounded to fp32 alone an angle is
             // up to 9e-8 off, more than any of a row's other roundings)
             const float at32 = (float)(int32_t)(turns >> 32);
-            const float rest = (float)((int64_t)turns - ((int64_t)at32 << 32)) * (0x1p-63f * 3.14159265f);
+            const float rest = (float)(int64_t)(turns - ((uint64_t)(int64_t)at32 << 32)) * (0x1p-63f * 3.14159265f);
             float sn, cs;
             sincospif(at32 * 0x1p-31f, &sn, &cs);
             s_turn[warp][lane + 32 * i] = make_float2(fmaf(-rest, sn, cs) * p.scale, fmaf(rest, cs, sn) * p.scale);
