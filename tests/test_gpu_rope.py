@@ -187,6 +187,35 @@ def test_many_tokens_and_heads(salt_lib, ctx):
     check_bf16(y, want, tol)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dim,heads,kv_heads", [(128, 17, 4), (128, 4, 1), (64, 33, 3), (64, 40, 8)])
+def test_warps_that_take_many_rows(salt_lib, ctx, dim, heads, kv_heads, interleaved):
+    """Tokens enough that a warp goes over all rows of one, with an odd or even number of passes: rows as in calls of a few tokens, where each pass
+    has a warp; into the cache, and in place."""
+    n, few, page = 5001, 120, 64
+    q, k, v, pos, freq = heads_of(n, heads, dim, 1), heads_of(n, kv_heads, dim, 2), heads_of(n, kv_heads, dim, 3), places(n, 10 ** 6, 4), frequencies(dim)
+    wq, wk = weights_of(dim, 5).cuda(), weights_of(dim, 6).cuda()
+    rope = salt_lib.salt_rope_create(ctx, dim, dim, freq, interleaved)
+    a, b = (make_cache(salt_lib, ctx, 1, n // page + 2, kv_heads, page, dim) for _ in range(2))
+    qkv, at = torch.cat([q, k, v], 1).cuda(), pos.cuda()
+    slots = torch.randperm(n, generator=torch.Generator().manual_seed(7)).int().cuda()
+    split = lambda x: (x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:])  # noqa: E731
+    q1, q2, k2 = torch.zeros((n, heads, dim), dtype=torch.bfloat16, device="cuda"), torch.zeros((n, heads, dim), dtype=torch.bfloat16, device="cuda"), k.cuda()
+    salt_lib.salt_rope_write(rope, a["kv"], 0, *split(qkv), at, slots, q1, wq, wk)
+    for i in range(0, n, few):
+        part = slice(i, i + few)
+        salt_lib.salt_rope_write(rope, b["kv"], 0, *split(qkv[part]), at[part], slots[part], q2[part], wq, wk)
+        salt_lib.salt_rope_apply(rope, qkv[part, :0], k2[part], at[part], qkv[part, :0], k2[part], wq, wk)
+    salt_lib.salt_rope_apply(rope, *split(qkv)[:2], at, *split(qkv)[:2], wq, wk)
+    torch.cuda.synchronize()
+    assert salt_lib.salt_get_device_error(ctx) == 0 and guards_ok(a) and guards_ok(b)
+    assert torch.equal(q1, q2) and all(torch.equal(a[x], b[x]) for x in ("k", "v", "k_exp", "v_exp"))
+    assert torch.equal(qkv[:, :heads], q1) and torch.equal(qkv[:, heads:heads + kv_heads], k2) and torch.equal(qkv[:, heads + kv_heads:].cpu(), v)
+    some = torch.arange(0, n, 97)
+    check_bf16(q1.cpu()[some], *rotate(q[some], pos[some], freq, interleaved, wq.cpu()))
+    check_bf16(k2.cpu()[some], *rotate(k[some], pos[some], freq, interleaved, wk.cpu()))
+
+
 def test_captured_and_on_another_stream(salt_lib, ctx):
     n, dim = 40, 128
     x, pos, freq = heads_of(n, 4, dim, 1).cuda(), places(n, 1000, 2).cuda(), frequencies(dim)
