@@ -612,7 +612,7 @@ salt_status salt_kv_read(salt_kv *kv, int32_t layer, int32_t n_tokens, const int
  * (y = x without norm weights w), and of its first rot_dim elements each pair
  * (a, b) becomes scale * (a cos t - b sin t, b cos t + a sin t), t = position *
  * inv_freq[pair]; the others stay y.  Pair i is elements (i, i + rot_dim / 2), or
- * (2i, 2i + 1) where interleaved.  Angles are exact to 2^-24 of a half turn at
+ * (2i, 2i + 1) where interleaved.  Angles are exact to 2^-32 of a half turn at
  * any position (int32, below zero too); everything else is fp32, rounded once.  An infinity
  * or a NaN among a head's elements spoils that head alone.
  */

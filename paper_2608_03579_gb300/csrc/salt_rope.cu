@@ -346,10 +346,14 @@ salt_status salt_rope_create(salt_ctx *ctx, const salt_rope_config *c, salt_rope
     r->eps = c->eps;
     r->offset = c->norm_offset;
     for (int i = 0; i < 64; ++i) {
-        const double turns = i < c->rot_dim / 2 ? c->inv_freq[i] / 6.283185307179586476925 : 0.0;
-        const double part = turns - std::floor(turns);  // [0, 1]
-        const double hi = std::floor(part * 4294967296.0);
-        r->freq[i] = ((uint64_t)hi << 32) + (uint64_t)((part * 4294967296.0 - hi) * 4294967296.0);
+        // turns = inv_freq / (2 pi) as a sum of two doubles (one alone is 2^-25 of a turn off at position 2^31)
+        const double inv_2pi = 0.15915494309189535, inv_2pi_low = -9.839338337591243e-18;
+        const double given = i < c->rot_dim / 2 ? c->inv_freq[i] : 0.0, f = std::fabs(given), turns = f * inv_2pi;
+        const double low = std::fma(f, inv_2pi, -turns) + f * inv_2pi_low;
+        const double part = (turns - std::floor(turns)) * 4294967296.0;  // [0, 2^32)
+        const double hi = std::floor(part);
+        const uint64_t bits = ((uint64_t)hi << 32) + (uint64_t)std::llrint((part - hi) * 4294967296.0 + low * 0x1p64);
+        r->freq[i] = given < 0 ? 0 - bits : bits;
     }
     *out = r;
     return SALT_OK;
