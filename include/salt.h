@@ -779,7 +779,8 @@ salt_status salt_attn_track(salt_attn *plan);
  * infinity); a row that sees nothing adds nothing, whatever it holds.  Results do not depend on timing.  A plan that was not built since
  * salt_attn_track is refused (SALT_ERR_NOT_BUILT), and so is a batch that lists a page twice, for two requests or
  * groups (SALT_ERR_INVALID_ARG; a captured call replayed on one does nothing and raises
- * SALT_DEVERR_BATCH).  One or two kernels, asynchronous on `stream`; ordered and captured as
+ * SALT_DEVERR_BATCH).  Where it raises SALT_DEVERR_TIMEOUT the weights of that layer's listed tokens are of no more use; later calls
+ * give what they should.  One or two kernels, asynchronous on `stream`; ordered and captured as
  * salt_attn_run's runs are.
  */
 salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int64_t q_stride, const float *lse,
@@ -800,7 +801,8 @@ salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int
  * raised.  scores is laid out as salt_attn_weights' weights, and may be
  * those (it is not moved itself).  The plan keeps the old lengths: build it again before its next
  * run.  A token's position is then no longer its place: see
- * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Two kernels (for each
+ * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Where it raises
+ * SALT_DEVERR_TIMEOUT, requests that were to lose tokens may be partly moved and are of no more use; others are as they should be.  Two kernels (for each
  * part of the layers, where the plan's memory does not hold all), asynchronous on `stream`; ordered
  * and captured as salt_attn_run's runs are (replayed on at most as many requests).
  */

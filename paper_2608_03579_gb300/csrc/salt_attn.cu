@@ -1861,7 +1861,7 @@ try {
         plan_copy_kernel<<<std::min(64, (t16 + 255) / 256), 256, 0, stream>>>(reinterpret_cast<const uint4 *>(a->track.staging[k]),
                                                                               reinterpret_cast<uint4 *>(a->track.table), t16);
         SALT_CUDA_OR_FAIL(ctx, cudaGetLastError());
-        // (a call whose waits gave up may have left some)
+        // (see TH_FAILED)
         if (a->track.split) SALT_CUDA_OR_FAIL(ctx, cudaMemsetAsync(a->track.arrived, 0, TRACK_SLOTS * 8 * 4, stream));
     }
     SALT_CUDA_OR_FAIL(ctx, cudaEventRecord(a->staging_ev[k], stream));

@@ -16,10 +16,11 @@ constexpr int HEAD_WORDS = 8;   // HD_* below
 constexpr int HD_TOKENS = 0, HD_WIDE = 1, HD_NARROW = 2, HD_PARTIAL = 3;  // query tokens, records of either kind, whether rows need the combine
 
 // What a tracked plan's build writes besides: a table of its own, int32 words.
-constexpr int TRACK_HEAD = 8;   // TH_* below
+constexpr int TRACK_HEAD = 12;  // TH_* below
 // query tokens, requests, lists of few rows, whether a page is listed twice, what the tiles of those lists cost, lists of many rows (behind the others),
-// tiles of 256 tokens of those, the CTAs that the units of their work are listed for (0: not listed)
-constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_COST = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7;
+// tiles of 256 tokens of those, the CTAs that the units of their work are listed for (0: not listed), whether a wait of a call since the build gave up (written
+// by that call: the parts' counts may be anything then, and later ones go by whole tiles, which need none)
+constexpr int TH_TOKENS = 0, TH_SEQS = 1, TH_FEW = 2, TH_SHARED = 3, TH_FEW_COST = 4, TH_MANY = 5, TH_MANY_TILES = 6, TH_LISTED = 7, TH_FAILED = 8;
 // per request: first entry in the page lists, own cached tokens, first entry in the tables of eviction's chunks, none
 constexpr int SEQ_WORDS = 4;
 // per list of cached tokens that rows see, a request's own or a group's prompt: first entry in the page lists, tokens, first
@@ -48,7 +49,7 @@ struct Track {
     int32_t *table = nullptr;                  // device
     int32_t *staging[2] = {nullptr, nullptr};  // page-locked host copies, used with the plan's own
     float *part = nullptr;                     // [TRACK_SLOTS][256]
-    uint32_t *arrived = nullptr;               // [TRACK_SLOTS][8], zero between calls
+    uint32_t *arrived = nullptr;               // [TRACK_SLOTS][8], zero between calls, but see TH_FAILED
     int seq_at = 0, list_at = 0, unit_at = 0;  // word offsets
     size_t words = 0, bytes = 0;               // of the table, of all its device memory
     bool on = false, built = false, shared = false, split = false;

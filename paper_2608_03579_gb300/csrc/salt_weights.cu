@@ -50,6 +50,7 @@ struct WeightParams {
     float *weights;
     float *part;                    // partial sums of units whose rows are split
     uint32_t *arrived;              // how many of a unit's parts are there
+    int32_t *failed;                // the table's TH_FAILED
     int64_t q_stride;
     int32_t n_heads, max_tok;
     int32_t behind;                 // whether the many rows' kernel is the one before
@@ -521,7 +522,7 @@ struct Unit {
 };
 
 // A CTA's units: the build's lists for CTAs blockIdx.x, blockIdx.x + gridDim.x, .. (a captured call may have another grid than the batch that it is replayed
-// for), or every gridDim-th one.
+// for), or every gridDim-th one, whole tiles all.
 struct Units {
     int at, end, cta, ctas;
     __device__ __forceinline__ void settle(const WeightParams &p)
@@ -534,7 +535,7 @@ struct Units {
     }
     __device__ __forceinline__ Units(const WeightParams &p, bool fits)
     {
-        ctas = one_word(p.track[TH_LISTED]);
+        ctas = one_word(p.track[TH_FAILED] ? 0 : p.track[TH_LISTED]);
         at = blockIdx.x;
         end = ctas > 0 ? 0 : one_word(fits ? p.track[TH_MANY_TILES] * p.kv.heads : 0);
         cta = (int)blockIdx.x - (int)gridDim.x;
@@ -1049,6 +1050,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
     __syncthreads();
     tc_fence_after();
     if (warp == 1) tmem_dealloc(tmem, L::TM_COLS);
+    if (tid == 0 && *dead) *p.failed = 1;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
@@ -1154,6 +1156,7 @@ try {
     p.weights = weights;
     p.part = tr.part;
     p.arrived = tr.arrived;
+    p.failed = tr.table + TH_FAILED;
     p.q_stride = q_stride;
     p.n_heads = a->cfg.n_heads;
     p.max_tok = a->T;
