@@ -1894,7 +1894,8 @@ salt_status salt_attn_track(salt_attn *a)
     const int64_t chunks = std::min<int64_t>((int64_t)a->cfg.max_pages, kv.n_pages) * kv.page / evict_rows(kv.dim) + a->cfg.max_seqs, layer = chunks * kv.heads;
     t.chunks_cap = (int)chunks;
     t.layers_cap = (int)std::min<int64_t>(a->kv->n_layers, std::max<int64_t>(1, (1 << 22) / layer));
-    ok = ok && cudaMalloc(&t.chunk_ptr, ((size_t)a->cfg.max_seqs + 1) * 4) == cudaSuccess && cudaMalloc(&t.ticket, 4) == cudaSuccess &&
+    ok = ok && cudaMalloc(&t.chunk_ptr, ((size_t)a->cfg.max_seqs + 1) * 4) == cudaSuccess &&
+         cudaMalloc(&t.losing, ((size_t)a->cfg.max_seqs + 1) * 4) == cudaSuccess && cudaMalloc(&t.ticket, 4) == cudaSuccess &&
          cudaMalloc(&t.bound, (size_t)layer * t.layers_cap * 4) == cudaSuccess && cudaMalloc(&t.read, (size_t)layer * t.layers_cap * 4) == cudaSuccess;
     for (int i = 0; i < 2 && ok; ++i) ok = cudaHostAlloc(reinterpret_cast<void **>(&t.staging[i]), t.words * 4, cudaHostAllocMapped) == cudaSuccess;
     if (!ok) {
@@ -1906,7 +1907,7 @@ salt_status salt_attn_track(salt_attn *a)
         }
         return ctx_fail(ctx, SALT_ERR_OOM, "no memory for the tracked tables");
     }
-    t.bytes = t.words * 4 + (size_t)TRACK_SLOTS * (TRACK_MANY_TILE + 8) * 4 + ((size_t)a->cfg.max_seqs + 2) * 4 + (size_t)layer * t.layers_cap * 8;
+    t.bytes = t.words * 4 + (size_t)TRACK_SLOTS * (TRACK_MANY_TILE + 8) * 4 + ((size_t)a->cfg.max_seqs * 2 + 3) * 4 + (size_t)layer * t.layers_cap * 8;
     t.on = true;
     return SALT_OK;
 }

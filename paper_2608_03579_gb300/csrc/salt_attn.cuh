@@ -57,14 +57,14 @@ struct Track {
     int64_t few_tiles = 0;
     // eviction's: the longest request, chunks of all requests in the build; room for chunks and layers; tables
     int longest = 0, chunks = 0, chunks_cap = 0, layers_cap = 0;
-    int32_t *chunk_ptr = nullptr, *bound = nullptr;
+    int32_t *chunk_ptr = nullptr, *losing = nullptr, *bound = nullptr;
     uint32_t *read = nullptr, *ticket = nullptr;
     std::vector<uint8_t> page_seen;            // scratch of a build
 
     void free_device()
     {
-        for (void *x : {(void *)table, (void *)part, (void *)arrived, (void *)chunk_ptr, (void *)bound, (void *)read, (void *)ticket}) cudaFree(x);
-        table = chunk_ptr = bound = nullptr;
+        for (void *x : {(void *)table, (void *)part, (void *)arrived, (void *)chunk_ptr, (void *)losing, (void *)bound, (void *)read, (void *)ticket}) cudaFree(x);
+        table = chunk_ptr = losing = bound = nullptr;
         part = nullptr;
         arrived = read = ticket = nullptr;
     }

@@ -8,12 +8,12 @@
 // ties are.
 //
 // A kept token's new place is never behind its old one, so rows move in place: a place may be written once what lies
-// there was read.  Rows move in chunks, each by a CTA that reads its chunk, says so, waits for the chunks that read what it will
-// write over (two of those before it at most: they have as many rows as it has places) and writes.
+// there was read.  Rows move in chunks. A CTA that moves a whole line has only to take its chunks in order. Where CTAs share a line, each reads a chunk, says
+// so, waits for the chunks that read what it will write over (two of those before it at most: they have as many rows as it has places) and writes.
 //
-// 8 layers of 32 requests of up to 4,096 tokens with 8 heads of 128: 184 us, 23 for the search (the scores lie in the L2 after the first
-// digit; shuffles and shared atomics, issue slots at 59%) and 161 for the move (5.2 TB/s of rows, those of a line's first kept
-// tokens that stay where they are neither read nor written).  Two requests of 200,000 tokens and more with heads of 64: 107 us, 37 and 70.
+// 8 layers of 32 requests of 1,200 to 2,048 tokens with 8 heads of 128: 166 us, 23 for the search (the scores lie in the L2 after the first
+// digit; shuffles and shared atomics, issue slots at 59%) and 143 for the move (6.1 TB/s of rows, those of a line's first kept
+// tokens that stay where they are neither read nor written).  Two requests of 200,000 tokens and more with heads of 64: 113 us, 37 and 76.
 #include <algorithm>
 #include <new>
 
@@ -41,10 +41,12 @@ struct EvictParams {
     int64_t kept_stride;
     int32_t n_seqs, first, recent;
     // the plan's workspace: per request the chunks of those before it, per line and chunk how many kept tokens lie before the chunk's
-    // first place and whether its rows were read, the next chunk to move
+    // first place and whether its rows were read, the next piece of work to move, the requests that lose tokens and how many they are
     int32_t *chunk_ptr, *bound;
     uint32_t *read, *ticket;
+    int32_t *losing;            // (the number first)
     int32_t chunks;             // entries of all requests, for one layer and head
+    int32_t whole;              // whether there are lines enough that CTAs of the move take some whole
     int32_t key_cap;            // keys of a CTA that its shared memory holds
     uint32_t *err;
 };
@@ -164,6 +166,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     const bool fits = n_seqs <= p.n_seqs && !p.track[TH_SHARED];
     if (blockIdx.x == 0) {  // the chunks of every request, once for all layers and heads
         int before = 0;
+        uint32_t losing = 0;
         for (int s0 = 0; fits && s0 < n_seqs; s0 += THREADS) {
             const int s = s0 + tid, keep = s < n_seqs ? kept_of(p, s, __ldg(p.track + p.seq_at + s * SEQ_WORDS + 1)) : 0;
             if (keep < 0) atomicOr(p.err, SALT_DEVERR_KEEP);
@@ -171,10 +174,15 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
             const uint32_t n = (max(keep, 0) + ROWS - 1) / ROWS, up_to = block_scan(n, s_warp, &all);
             if (s < n_seqs) p.chunk_ptr[s + 1] = before + (int)up_to;
             before += (int)all;
+            if (!p.whole) continue;
+            const uint32_t at = block_scan(n > 0, s_warp, &all);
+            if (n > 0) p.losing[losing + at] = s;
+            losing += all;
         }
         if (tid == 0) {
             p.chunk_ptr[0] = 0;
             p.ticket[0] = 0;
+            p.losing[0] = (int)losing;
             if (!fits) atomicOr(p.err, SALT_DEVERR_BATCH);
         }
     }
@@ -394,13 +402,16 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     if (C > 1) cluster_wait();
 }
 
-// Chunks are taken in their order, so that those that a chunk waits for are under way.  A CTA has some of them in slots of its shared
-// memory, and its warps deal with them in turn: one looks up the rows' places, some read the keys and values, one the exponents and weights,
-// one says when all are there, one waits for the chunks that read what this one will write over, some write.  Reading
-// runs ahead of writing by all the slots, whatever writing waits for.  (Where a chunk was read only once the one before it was written, chunks
-// waited for each other in long chains, 7 us each.)  The flags between CTAs carry no data and need no fence: a chunk's words
-// are in shared memory, not on their way, when its flag is written, and no store is made before the flag that allows it was read.
-constexpr int SLOTS = 5, LOAD_WARPS = 4, STORE_WARPS = 4, MOVE_THREADS = 32 * (LOAD_WARPS + STORE_WARPS + 4);
+// The CTAs draw whole lines first, as many as go evenly into them, and then the others' chunks one by one, in their order, so that those that a chunk waits for
+// are under way.  A CTA has some chunks in slots of its shared memory, and its warps deal with them in turn: one looks up the rows' places, some read the keys
+// and values, one the exponents and weights, two say in turn when all are there, one waits for the chunks that read what this one will write over, some write.
+// Reading runs ahead of writing by all the slots, whatever writing waits for.  (Where a chunk was read only once the one before it was written, chunks
+// waited for each other in long chains, 7 us each.)  Within a line of its own a CTA's slots order reading and writing: a chunk that was read tells that those
+// before it were.  Between CTAs a chunk's flag is a release behind its reads, and the wait for it an acquire before the stores that write over them.  These cost: the
+// release takes as long as the stores under way, and the acquire empties the L1.  8 layers of 32 requests take 208 us by chunks (232 with one warp that says so and
+// has its slot meanwhile; 187 if nothing ordered them) and 166 by lines; 16 lines of 200,000 tokens and more 113 (121, 109).  Several chunks of a line
+// a CTA are worse than either (up to 560 us: a run's first chunk waits for the last one of the run before).
+constexpr int SLOTS = 5, LOAD_WARPS = 4, STORE_WARPS = 4, SAY_WARPS = 2, MOVE_THREADS = 32 * (LOAD_WARPS + STORE_WARPS + 3 + SAY_WARPS);
 
 template <int D_, int ROWS_>
 struct Move {
@@ -414,7 +425,7 @@ struct Move {
     static_assert(SLOT % 16 == 0 && 2 * (BYTES + 2048) <= 228 * 1024, "two CTAs an SM");
 };
 
-template <class M>
+template <class M, bool WHOLE>
 __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __grid_constant__ EvictParams p, int layers)
 {
     constexpr int D = M::D, ROWS = M::ROWS;
@@ -422,13 +433,14 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     __shared__ __align__(8) uint64_t s_full[SLOTS], s_free[SLOTS], s_read[SLOTS], s_clear[SLOTS];
     __shared__ int64_t s_chunk[SLOTS];     // the chunk's entry, -1: no more
     __shared__ int32_t s_wait[SLOTS][2];   // the first and last chunk of the line that it waits for, from here
+    __shared__ int32_t s_alone[SLOTS];     // whether it is of a whole line: none waits for it
     __shared__ int s_dead;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     volatile int *dead = &s_dead;
     if (tid == 0) {
         for (int i = 0; i < SLOTS; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
-            mbar_init(smem_u32(&s_free[i]), STORE_WARPS + 2);
+            mbar_init(smem_u32(&s_free[i]), STORE_WARPS + 1 + SAY_WARPS);
             mbar_init(smem_u32(&s_read[i]), 32 * LOAD_WARPS + 1);
             mbar_init(smem_u32(&s_clear[i]), 1);
         }
@@ -458,19 +470,37 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
     if (warp == LOAD_WARPS + STORE_WARPS) {
         // ------------------------------------------------ places
         // (a chunk's line is found while the places of the one before are on their way: the waits for other chunks empty the L1)
-        const int per_lh = uniform(p.chunk_ptr[n_seqs]);
-        const int64_t all = (int64_t)per_lh * p.kv.heads * layers;
-        struct Chunk {
+        const int per_lh = uniform(p.chunk_ptr[n_seqs]), losing = WHOLE ? uniform(p.losing[0]) : 0;
+        const uint32_t all = (uint32_t)per_lh * p.kv.heads * layers;  // (below 2^27, as a layer's rows are below 2^31)
+        // Lines that are taken whole: full rounds of one a CTA, and all where the last round is half full.  (200 lines, two thirds of a round, take 86 us so
+        // and 95 by chunks; 160 lines 50 and 51.)
+        const int ctas = gridDim.x, lines = losing * p.kv.heads * layers;
+        const uint32_t whole = min(lines, (lines + ctas / 2) / ctas * ctas);
+        uint32_t chunk_at = 0;  // the first chunk of the other lines
+        if (WHOLE && whole > 0) {
+            const int lh = (int)whole / losing, at = (int)whole - lh * losing;
+            chunk_at = (uint32_t)lh * per_lh + (at > 0 ? uniform(p.chunk_ptr[p.losing[1 + at]]) : 0);  // (before the first of these there are none)
+        }
+        struct Work {
             Line l;
-            int c;
-            bool more;
+            int c, end;   // chunks [c, end) of the line
+            bool more, alone;
         };
-        auto find = [&](int64_t t) {
-            Chunk r;
-            r.more = t < all;
-            r.c = 0;
+        auto find = [&](uint32_t t) {
+            Work r;
+            r.alone = WHOLE && uniform(t < whole);
+            r.c = r.end = 0;
+            if (r.alone) {
+                const int lh = (int)t / losing;
+                r.more = true;
+                r.l = load_line(p, lh, uniform(p.losing[1 + (int)t - lh * losing]));
+                r.end = (uniform(r.l.keep) + ROWS - 1) / ROWS;
+                return r;
+            }
+            t += chunk_at - whole;
+            r.more = uniform(t < all);
             if (!r.more) return r;
-            const int lh = (int)(t / per_lh), x = (int)(t - (int64_t)lh * per_lh);
+            const int lh = t / (uint32_t)per_lh, x = t - (uint32_t)lh * per_lh;
             int lo = 0, n = n_seqs;  // the last request that begins at or before x is one of n
             while (n > 1) {
                 const int step = (n + 31) / 32, at = lane * step;
@@ -480,6 +510,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
                 n = min(step, n - last * step);
             }
             r.c = x - uniform(p.chunk_ptr[lo]);
+            r.end = r.c + 1;
             r.l = load_line(p, lh, lo);
             return r;
         };
@@ -488,8 +519,9 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
             if (lane == 0) ticket = atomicAdd(p.ticket, 1u);
         };
         draw();
-        Chunk now = find(__shfl_sync(0xffffffffu, ticket, 0));
-        draw();
+        // (drawn a chunk ahead, not sooner: others may wait for a chunk that is drawn)
+        Work now = find(__shfl_sync(0xffffffffu, ticket, 0));
+        if (!WHOLE || uniform(now.end - now.c) <= 1) draw();
         for (uint32_t n = 0;; ++n) {
             const int slot = n % SLOTS;
             if (!now.more) {
@@ -507,8 +539,10 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
                 from[k] = i < l.keep ? l.kept[i] : i;
             }
             const int b0 = p.bound[l.chunk0 + c], b1 = (c + 1) * ROWS < l.len ? p.bound[l.chunk0 + c + 1] : l.keep;
-            const Chunk next = find(__shfl_sync(0xffffffffu, ticket, 0));
-            draw();
+            Work next = now;
+            const int left = WHOLE ? uniform(now.end - ++next.c) : 0;
+            if (left == 0) next = find(__shfl_sync(0xffffffffu, ticket, 0));
+            if (!WHOLE || (left == 0 ? uniform(next.end - next.c) <= 1 : left == 1)) draw();
 #pragma unroll
             for (int k = 0; k < ROWS / 32; ++k) {
                 const int i = c * ROWS + 32 * k + lane;
@@ -528,23 +562,25 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
             if (lane == 0) {
                 s_chunk[slot] = l.chunk0 + c;
                 // kept tokens [b0, b1) lie where this chunk will: chunks of the line up to this one
-                s_wait[slot][0] = b1 > b0 ? b0 / ROWS - c : 0;
-                s_wait[slot][1] = b1 > b0 ? (b1 - 1) / ROWS - c : 0;
+                s_wait[slot][0] = b1 > b0 && !now.alone ? b0 / ROWS - c : 0;
+                s_wait[slot][1] = b1 > b0 && !now.alone ? (b1 - 1) / ROWS - c : 0;
+                if (WHOLE) s_alone[slot] = now.alone;
             }
             arrive(s_full, n);
             now = next;
         }
-    } else if (warp == LOAD_WARPS + STORE_WARPS + 1) {
+    } else if (warp >= LOAD_WARPS + STORE_WARPS + 3) {
         // ------------------------------------------------ chunks that were read
         for (uint32_t n = 0; wait(s_full, n); ++n) {
             const int64_t chunk = chunk_of(n);
-            if (chunk < 0 || !wait(s_read, n)) break;
-            if (lane == 0) {
-                asm volatile("st.relaxed.gpu.global.u32 [%0], %1;\n" ::"l"(p.read + chunk), "r"(1u) : "memory");
-            }
-            arrive(s_free, n);
+            if (chunk < 0) break;
+            const bool mine = n % SAY_WARPS == (uint32_t)(warp - (LOAD_WARPS + STORE_WARPS + 3));
+            if (mine && !wait(s_read, n)) break;
+            const bool alone = WHOLE && s_alone[n % SLOTS];
+            arrive(s_free, n);  // (before the release, which takes as long as the stores under way)
+            if (lane == 0 && mine && !alone) asm volatile("st.release.gpu.global.u32 [%0], %1;\n" ::"l"(p.read + chunk), "r"(1u) : "memory");
         }
-    } else if (warp == LOAD_WARPS + STORE_WARPS + 2) {
+    } else if (warp == LOAD_WARPS + STORE_WARPS + 1) {
         // ------------------------------------------------ chunks to wait for
         for (uint32_t n = 0; wait(s_full, n); ++n) {
             const int64_t chunk = chunk_of(n);
@@ -553,7 +589,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
                 const uint32_t *flag = p.read + chunk + s_wait[n % SLOTS][lane];
                 uint32_t x = 0;
                 for (int i = 0; i < EVICT_POLLS && !x && !*dead; ++i)
-                    asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];\n" : "=r"(x) : "l"(flag) : "memory");
+                    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];\n" : "=r"(x) : "l"(flag) : "memory");
                 ok = x != 0;
             }
             ok = __all_sync(0xffffffffu, ok);
@@ -561,7 +597,7 @@ __global__ void __launch_bounds__(MOVE_THREADS, 2) evict_move_kernel(const __gri
             arrive(s_clear, n);
             arrive(s_free, n);
         }
-    } else if (warp == LOAD_WARPS + STORE_WARPS + 3) {
+    } else if (warp == LOAD_WARPS + STORE_WARPS + 2) {
         // ------------------------------------------------ exponents and weights, the next chunk's on their way
         uint32_t ke[2][ROWS / 32], ve[2][ROWS / 32];
         float w[2][ROWS / 32];
@@ -674,10 +710,11 @@ cudaError_t launch_select(const EvictParams &params, int64_t lines, int ctas, cu
 }
 
 template <int D>
-cudaError_t launch_evict(const EvictParams &p, int n_sm, int layers, int longest, int64_t chunks, cudaStream_t stream)
+cudaError_t launch_evict(EvictParams &p, int n_sm, int layers, int longest, int64_t chunks, cudaStream_t stream)
 {
     constexpr int ROWS = evict_rows(D);
     const int64_t lines = (int64_t)layers * p.n_seqs * p.kv.heads;
+    p.whole = lines >= n_sm;  // (the move has two CTAs an SM; 100 lines by chunks take 35 us without looking for whole ones, 37 with)
     // Long lines go to several CTAs, up to 6: clusters of 8 whose CTAs take an SM each fit 15 times into the card's
     // SMs, of 6 at least 20 times (16 lines of 262,144 tokens: 151 us with 8, one of them in a second wave, 108 with 6, all else alike but for some shorter code).
     int ctas = 1;
@@ -689,9 +726,10 @@ cudaError_t launch_evict(const EvictParams &p, int n_sm, int layers, int longest
     if (e != cudaSuccess) return e;
     const int64_t most = chunks * p.kv.heads * layers;
     using M = Move<D, ROWS>;
-    e = cudaFuncSetAttribute(evict_move_kernel<M>, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
+    const auto move = p.whole ? evict_move_kernel<M, true> : evict_move_kernel<M, false>;
+    e = cudaFuncSetAttribute(move, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(evict_move_kernel<M>, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2 * n_sm)), MOVE_THREADS, M::BYTES, stream, p, layers);
+    return launch_overlapped(move, (unsigned)std::max<int64_t>(1, std::min<int64_t>(most, 2 * n_sm)), MOVE_THREADS, M::BYTES, stream, p, layers);
 }
 
 }  // namespace
@@ -742,8 +780,9 @@ try {
     p.bound = tr.bound;
     p.read = tr.read;
     p.ticket = tr.ticket;
+    p.losing = tr.losing;
     p.chunks = tr.chunks_cap;
-    p.key_cap = 0;
+    p.whole = p.key_cap = 0;
     // as many layers at a time as the workspace has chunks for
     for (int32_t l = 0; l < n_layers; l += tr.layers_cap) {
         const int32_t n = std::min(tr.layers_cap, n_layers - l);

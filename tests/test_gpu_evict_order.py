@@ -1,0 +1,54 @@
+"""Evictions whose chunks of rows all write over what others read: every row moves by little, again and again, bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from test_gpu_evict import ARRAYS, Cache
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx(salt_lib):
+    c = salt_lib.salt_ctx_create([64], [64], 1, 1, 1, 1, 1)
+    yield c
+    salt_lib.salt_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("dim,page,lens,kv_heads,layers", [(64, 16, [4097, 3001], 8, 2), (128, 64, [20001], 4, 1), (128, 16, [700] * 24, 4, 3)])
+@pytest.mark.parametrize("by", [1, 63, 65, 129])
+def test_every_chunk_waits(salt_lib, ctx, dim, page, lens, kv_heads, layers, by):
+    """The last tokens are kept, so that a row moves `by` places and each chunk's place is where one or two others still lie."""
+    c = Cache(salt_lib, ctx, lens, kv_heads=kv_heads, dim=dim, page=page, layers=layers, seed=by)
+    scores = torch.zeros_like(c.t["weights"])
+    left = [x.reshape(x.shape[:4] + (-1,)).view(np.uint8) for x in c.host()]
+    for _ in range(5):
+        keep = [n - by for n in lens]
+        kept = torch.full((layers, len(lens), kv_heads, max(keep)), -7, dtype=torch.int32, device="cuda")
+        salt_lib.salt_attn_evict(c.plan, 0, layers, torch.tensor(keep, dtype=torch.int32, device="cuda"), scores, kept, 0, 1 << 30, c.t["weights"])
+        torch.cuda.synchronize()
+        assert salt_lib.salt_get_device_error(ctx) == 0
+        for b, n in enumerate(lens):
+            pages = np.array(c.batch["pages"][c.batch["page_ptr"][b]:c.batch["page_ptr"][b + 1]])
+            j = np.arange(n)
+            P, O = pages[j // page], j % page
+            for x in left:
+                x[:, P[:n - by], :, O[:n - by]] = x[:, P[by:], :, O[by:]]
+            assert bool((kept[:, b, :, :n - by] == torch.arange(by, n, device="cuda")).all())
+        for name, a, b in zip(ARRAYS, c.host(), left):
+            assert np.array_equal(a.reshape(a.shape[:4] + (-1,)).view(np.uint8), b), name
+        lens = keep
+        c.build(kv_len=lens)
+
+
+@pytest.mark.parametrize("dim,page", [(128, 32), (64, 16)])
+@pytest.mark.parametrize("requests,part", [(40, 1.0), (40, 0.6), (20, 0.9), (31, 0.02)])
+def test_whole_lines_and_shared_ones(salt_lib, ctx, dim, page, requests, part):
+    """Lines of many chunks, more and fewer than a round of them a CTA, among requests that lose nothing."""
+    r = np.random.RandomState(requests)
+    lens = [int(n) for n in r.randint(300, 1800, requests)]
+    keep = [int(n * r.uniform(0.3, 0.99)) if r.rand() < part else n for n in lens]
+    keep[-1] = lens[-1] - 1
+    c = Cache(salt_lib, ctx, lens, kv_heads=4, dim=dim, page=page, layers=4, seed=3)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    c.check(keep, torch.randn(c.t["weights"].shape, device="cuda", generator=g), 4, 100)
