@@ -1030,6 +1030,7 @@ __global__ void __launch_bounds__(L::THREADS, 1) weights_many_kernel(const __gri
                 uint32_t before = 0;
                 if (lane == 0) asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;\n" : "=r"(before) : "l"(count) : "memory");
                 before = __shfl_sync(0xffffffffu, before, 0);
+                __syncwarp();  // (a shuffle orders no memory: what lane 0 acquired is the other lanes' by this)
                 if ((int)before + 1 == parts) {
                     total = 0.f;
                     for (int i = 0; i < parts; ++i) total += __ldcg(mine_at + i * TRACK_MANY_TILE);
