@@ -61,17 +61,18 @@ struct Line {
     int64_t chunk0;             // its first entry in the chunks' tables
 };
 
+// (Tables at places that do not hang on words read before, here and below: plain loads, as those of constants, __ldg, might be moved before the pdl_wait.)
 // How many tokens of a request are kept where some go; 0 where none do, or none may stay (-1: not allowed).
 __device__ __forceinline__ int kept_of(const EvictParams &p, int seq, int len)
 {
-    const int keep = __ldg(p.keep + seq);
+    const int keep = p.keep[seq];
     return keep < 0 || keep > p.kept_stride ? -1 : keep < len ? keep : 0;
 }
 // lh: layer in the launch * heads + head
 __device__ __forceinline__ Line load_line(const EvictParams &p, int lh, int seq)
 {
     const int layer = lh / p.kv.heads;
-    const int4 s = __ldg(reinterpret_cast<const int4 *>(p.track + p.seq_at) + seq);
+    const int4 s = reinterpret_cast<const int4 *>(p.track + p.seq_at)[seq];
     Line l;
     l.head = lh - layer * p.kv.heads;
     l.pages = p.plan + p.pages_at + s.x;
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
         int before = 0;
         uint32_t losing = 0;
         for (int s0 = 0; fits && s0 < n_seqs; s0 += THREADS) {
-            const int s = s0 + tid, keep = s < n_seqs ? kept_of(p, s, __ldg(p.track + p.seq_at + s * SEQ_WORDS + 1)) : 0;
+            const int s = s0 + tid, keep = s < n_seqs ? kept_of(p, s, p.track[p.seq_at + s * SEQ_WORDS + 1]) : 0;
             if (keep < 0) atomicOr(p.err, SALT_DEVERR_KEEP);
             uint32_t all;
             const uint32_t n = (max(keep, 0) + ROWS - 1) / ROWS, up_to = block_scan(n, s_warp, &all);

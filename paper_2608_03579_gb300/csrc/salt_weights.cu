@@ -67,7 +67,9 @@ __device__ __forceinline__ List list_of(const int4 &a, const int4 &b) { return {
 // words that might differ, a vote takes hundreds of cycles).
 __device__ __forceinline__ int one_word(int x) { return __shfl_sync(0xffffffffu, x, 0); }
 __device__ __forceinline__ int4 one_each(const int4 &x) { return make_int4(one_word(x.x), one_word(x.y), one_word(x.z), one_word(x.w)); }
-__device__ __forceinline__ int4 four_words(const int4 *at) { return one_each(__ldg(at)); }
+// (Of the table, as all of its words by plain loads: its first ones are at places that do not hang on words read before, and loads of constants, __ldg, of those might
+// be moved before the pdl_wait.)
+__device__ __forceinline__ int4 four_words(const int4 *at) { return one_each(*at); }
 __device__ __forceinline__ List load_list(const WeightParams &p, int i)
 {
     const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + i * LIST_WORDS);
@@ -78,7 +80,7 @@ __device__ __forceinline__ int find_list(const WeightParams &p, int lo, int hi, 
 {
     for (int n = hi - lo; n > 1;) {
         const int step = (n + 31) / 32, guess = (int)(threadIdx.x & 31) * step;
-        const uint32_t on = __ballot_sync(0xffffffffu, guess < n && __ldg(p.track + p.list_at + (lo + min(guess, n - 1)) * LIST_WORDS + LS_BEFORE) <= at);
+        const uint32_t on = __ballot_sync(0xffffffffu, guess < n && p.track[p.list_at + (lo + min(guess, n - 1)) * LIST_WORDS + LS_BEFORE] <= at);
         const int last = 31 - __clz(on);  // (lane 0 is)
         lo += last * step;
         n = min(step, n - last * step);
@@ -141,8 +143,8 @@ struct Walk {
     {
         if (list + 1 >= n_lists) return;
         const int4 *w = reinterpret_cast<const int4 *>(p.track + p.list_at + (list + 1) * LIST_WORDS);
-        a = __ldg(w);
-        b = __ldg(w + 1);
+        a = w[0];
+        b = w[1];
     }
     __device__ __forceinline__ Walk(const WeightParams &p, int lists, int64_t all) : n_lists(lists)
     {
@@ -529,8 +531,8 @@ struct Units {
     {
         while (ctas > 0 && at >= end && cta + (int)gridDim.x < ctas) {
             cta += gridDim.x;
-            at = one_word(__ldg(p.track + p.unit_at + cta));
-            end = one_word(__ldg(p.track + p.unit_at + cta + 1));
+            at = one_word(p.track[p.unit_at + cta]);
+            end = one_word(p.track[p.unit_at + cta + 1]);
         }
     }
     __device__ __forceinline__ Units(const WeightParams &p, bool fits)
