@@ -54,6 +54,7 @@ struct WeightParams {
     int64_t q_stride;
     int32_t n_heads, max_tok;
     int32_t behind;                 // whether the many rows' kernel is the one before
+    int32_t n_sm;
     float scale, decay;
     uint32_t *err;
 };
@@ -132,7 +133,7 @@ struct Few {
     static_assert(E % 16 == 0 && K_FULL % 8 == 0, "alignment");
 };
 
-// A CTA's share [g, end) of what the few rows' lists' tiles cost, in the order list, key/value head, tile.  A segment is the tiles of one list and
+// A CTA's share [g, end), one of `ctas`, of what the few rows' lists' tiles cost, in the order list, key/value head, tile.  A segment is the tiles of one list and
 // head.
 struct Walk {
     int64_t g, end;
@@ -146,12 +147,13 @@ struct Walk {
         a = w[0];
         b = w[1];
     }
-    __device__ __forceinline__ Walk(const WeightParams &p, int lists, int64_t all) : n_lists(lists)
+    __device__ __forceinline__ Walk(const WeightParams &p, int lists, int64_t all, int ctas) : n_lists(lists)
     {
         const int KV = p.kv.heads;
-        g = all * blockIdx.x / gridDim.x;
-        end = all * (blockIdx.x + 1) / gridDim.x;
+        g = all * blockIdx.x / ctas;
+        end = all * (blockIdx.x + 1) / ctas;
         segment = 0;
+        if ((int)blockIdx.x >= ctas) g = end;
         if (g >= end) return;
         list = find_list(p, 0, n_lists, (int)(g / KV));  // (what is before a list, for all heads, is that times the heads)
         l = load_list(p, list);
@@ -304,7 +306,9 @@ __global__ void __launch_bounds__(L::THREADS, L::CTAS) weights_few_kernel(const 
     const bool fits = track[TH_TOKENS] <= p.max_tok && !track[TH_SHARED];
     if (!fits && blockIdx.x == 0 && tid == 0) atomicOr(p.err, SALT_DEVERR_BATCH);
     const int n_lists = one_word(fits ? track[TH_FEW] : 0);
-    Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_COST]) * KV : 0);
+    // The CTAs of the SMs that the lists of many rows leave: all of a direct call's; one that was captured is launched on every SM, for whatever batch it is replayed on.
+    const int listed = one_word(track[TH_LISTED]), sms = listed > 0 && listed < p.n_sm ? p.n_sm - listed : p.n_sm;
+    Walk k(p, n_lists, n_lists ? (int64_t)one_word(track[TH_FEW_COST]) * KV : 0, min((int)gridDim.x, sms * L::CTAS));
     bool ok = true;
     // A tile's pages, a lane each, are looked up while the one's before are waited for.  Its codes are one warp's to fetch, its exponents and old weights
     // another's (one for all took 800 cycles a tile, the longest of the roles).
@@ -523,8 +527,8 @@ struct Unit {
     bool two;                   // more than 128 tokens
 };
 
-// A CTA's units: the build's lists for CTAs blockIdx.x, blockIdx.x + gridDim.x, .. (a captured call may have another grid than the batch that it is replayed
-// for), or every gridDim-th one, whole tiles all.
+// A CTA's units: the build's lists for CTAs blockIdx.x, blockIdx.x + gridDim.x, .. (a call has as many CTAs as there are lists, a captured one as there are
+// SMs), or every gridDim-th one, whole tiles all.
 struct Units {
     int at, end, cta, ctas;
     __device__ __forceinline__ void settle(const WeightParams &p)
@@ -1164,11 +1168,12 @@ try {
     p.n_heads = a->cfg.n_heads;
     p.max_tok = a->T;
     p.behind = 0;
+    p.n_sm = a->n_sm;
     p.scale = scale;
     p.decay = decay;
     p.err = ctx_error_word(ctx);
     const int64_t tiles = captured ? 1 << 30 : tr.few_tiles * kv.heads;
-    const int rows = captured ? TRACK_FEW_ROWS : tr.few_rows, sms = many ? tr.many_sms : 0;
+    const int rows = captured ? TRACK_FEW_ROWS : tr.few_rows, sms = !many ? 0 : captured ? a->n_sm : tr.many_sms;
     SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_weights<128>(p, a->n_sm, sms, few, rows, tiles, stream)
                                          : launch_weights<64>(p, a->n_sm, sms, few, rows, tiles, stream));
     return SALT_OK;
