@@ -804,7 +804,8 @@ salt_status salt_attn_weights(salt_attn *plan, int32_t layer, const void *q, int
  * salt_rope_write.  Groups' prompts are not touched.  Refused as salt_attn_weights.  Where it raises
  * SALT_DEVERR_TIMEOUT, requests that were to lose tokens may be partly moved and are of no more use; others are as they should be.  Two kernels (for each
  * part of the layers, where the plan's memory does not hold all), asynchronous on `stream`; ordered
- * and captured as salt_attn_run's runs are (replayed on at most as many requests).
+ * and captured as salt_attn_run's runs are (replayed on at most as many requests; the search for what is kept stays divided as the
+ * longest request at the capture called for, so that one captured on short requests is slow on long ones).
  */
 salt_status salt_attn_evict(salt_attn *plan, int32_t layer, int32_t n_layers, const int32_t *keep, int32_t first,
                             int32_t recent, const float *scores, float *weights, int32_t *kept,

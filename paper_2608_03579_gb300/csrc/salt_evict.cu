@@ -711,7 +711,7 @@ cudaError_t launch_select(const EvictParams &params, int64_t lines, int ctas, cu
 }
 
 template <int D>
-cudaError_t launch_evict(EvictParams &p, int n_sm, int layers, int longest, int64_t chunks, cudaStream_t stream)
+cudaError_t launch_evict(EvictParams &p, int n_sm, int layers, int longest, int64_t chunks, bool captured, cudaStream_t stream)
 {
     constexpr int ROWS = evict_rows(D);
     const int64_t lines = (int64_t)layers * p.n_seqs * p.kv.heads;
@@ -725,7 +725,7 @@ cudaError_t launch_evict(EvictParams &p, int n_sm, int layers, int longest, int6
                                                                : launch_select<1024, ROWS>(p, lines, ctas, stream, longest);
     cudaError_t e = e1;
     if (e != cudaSuccess) return e;
-    const int64_t most = chunks * p.kv.heads * layers;
+    const int64_t most = captured ? 2 * n_sm : chunks * p.kv.heads * layers;  // (a captured call may be replayed on more)
     using M = Move<D, ROWS>;
     const auto move = p.whole ? evict_move_kernel<M, true> : evict_move_kernel<M, false>;
     e = cudaFuncSetAttribute(move, cudaFuncAttributeMaxDynamicSharedMemorySize, M::BYTES);
@@ -789,8 +789,8 @@ try {
         const int32_t n = std::min(tr.layers_cap, n_layers - l);
         p.layer = layer + l;
         p.kept = kept + (int64_t)l * p.n_seqs * kv.heads * kept_stride;
-        SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_evict<128>(p, a->n_sm, n, tr.longest, tr.chunks, stream)
-                                             : launch_evict<64>(p, a->n_sm, n, tr.longest, tr.chunks, stream));
+        SALT_CUDA_OR_FAIL(ctx, kv.dim == 128 ? launch_evict<128>(p, a->n_sm, n, tr.longest, tr.chunks, captured, stream)
+                                             : launch_evict<64>(p, a->n_sm, n, tr.longest, tr.chunks, captured, stream));
     }
     return SALT_OK;
 } catch (const std::bad_alloc &) {
