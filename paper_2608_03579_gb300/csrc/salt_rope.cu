@@ -93,7 +93,8 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
     // (the warp's number from a shuffle: loops by it are known to be a warp's then, and the shuffles in them are quick)
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31, part = lane % LPR;
     const uint32_t task = blockIdx.x * ROPE_WARPS + warp;
-    const int t = (int)(task / (uint32_t)p.splits), split = (int)(task - (uint32_t)t * p.splits);
+    const uint32_t token = task / (uint32_t)p.splits;
+    const int t = (int)token, split = (int)(task - token * p.splits);
     // the lane's pieces of a row, in units of 8 elements, and whether they are rotated
     const int n_rot = p.rot / 16;
     const bool turned0 = MIXED ? part < 2 * n_rot : part < n_rot;
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(ROPE_THREADS, 4) rope_kernel(const __grid_cons
         }
         __syncthreads();
     }
-    if (t >= p.n_tokens) return;
+    if (token >= (uint32_t)p.n_tokens) return;
     const int32_t *positions = after_pdl_wait(p.positions), *slots = WRITE ? after_pdl_wait(p.slots) : nullptr;
     const uint16_t *q = after_pdl_wait(p.q), *k = after_pdl_wait(p.k), *v = WRITE ? after_pdl_wait(p.v) : nullptr;
     const int H = p.n_heads, KV = p.n_kv_heads;
@@ -292,24 +293,9 @@ salt_status launch_rope(salt_rope *r, RopeParams &p, cudaStream_t stream)
     p.splits = (all + p.passes - 1) / p.passes;
     const auto kernel = r->dim == 128 ? (r->mixed ? rope_kernel<128, WRITE, true> : rope_kernel<128, WRITE, false>)
                                       : (r->mixed ? rope_kernel<64, WRITE, true> : rope_kernel<64, WRITE, false>);
-    const int n = p.n_tokens;
-    const int32_t most = (int32_t)std::max<int64_t>(1, ((1ll << 31) - ROPE_WARPS) / p.splits);  // warps are numbered in 32 bits
-    for (int64_t t = 0; t < n; t += most) {
-        RopeParams a = p;
-        a.n_tokens = (int32_t)std::min<int64_t>(most, n - t);
-        a.q += t * p.q_stride;
-        a.k += t * p.k_stride;
-        a.q_out += t * p.q_out_stride;
-        a.positions += t;
-        if (WRITE) {
-            a.v += t * p.v_stride;
-            a.slots += t;
-        } else {
-            a.k_out += t * p.k_out_stride;
-        }
-        SALT_CUDA_OR_FAIL(ctx, launch_overlapped(kernel, (unsigned)(((int64_t)a.n_tokens * p.splits + ROPE_WARPS - 1) / ROPE_WARPS), ROPE_THREADS,
-                                                 0, stream, a));
-    }
+    // (a token has one warp unless there are few: the warps' numbers fit 32 bits, those of the last CTA past the tokens too)
+    SALT_CUDA_OR_FAIL(ctx, launch_overlapped(kernel, (unsigned)(((int64_t)p.n_tokens * p.splits + ROPE_WARPS - 1) / ROPE_WARPS), ROPE_THREADS, 0,
+                                             stream, p));
     return SALT_OK;
 }
 
