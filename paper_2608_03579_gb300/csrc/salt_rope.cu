@@ -32,7 +32,7 @@
 
 struct salt_rope {
     salt_ctx *ctx;
-    int dim, rot;
+    int dim, rot, n_sm;
     bool mixed;
     float scale, eps, offset;
     uint64_t freq[64];  // turns a position, in units of 2^-64
@@ -287,7 +287,7 @@ salt_status launch_rope(salt_rope *r, RopeParams &p, cudaStream_t stream)
     const int per = 32 / (r->dim / 16), all = (p.rows + per - 1) / per;  // passes of a token
     // A warp takes all of a token's passes where there are tokens enough to fill the SMs (its sines are
     // computed once), fewer where not, two by two.
-    const int64_t fill = 152 * 32;
+    const int64_t fill = r->n_sm * 32;
     const int64_t few = std::max<int64_t>(1, (int64_t)p.n_tokens * all / fill);
     p.passes = (int)std::min<int64_t>(all, (few + ROPE_ROWS - 1) / ROPE_ROWS * ROPE_ROWS);
     p.splits = (all + p.passes - 1) / p.passes;
@@ -322,9 +322,12 @@ salt_status salt_rope_create(salt_ctx *ctx, const salt_rope_config *c, salt_rope
     for (int i = 0; i < c->rot_dim / 2; ++i)
         if (!(std::fabs(c->inv_freq[i]) <= 6.2831853071795864))
             return ctx_fail(ctx, SALT_ERR_INVALID_ARG, "inv_freq[%d] is more than a turn a position", i);
+    int n_sm = 0;
+    SALT_CUDA_OR_FAIL(ctx, cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, ctx_device(ctx)));
     salt_rope *r = new (std::nothrow) salt_rope;
     if (!r) return ctx_fail(ctx, SALT_ERR_OOM, "no host memory");
     r->ctx = ctx;
+    r->n_sm = n_sm;
     r->dim = c->head_dim;
     r->rot = c->rot_dim;
     r->mixed = c->interleaved != 0;
