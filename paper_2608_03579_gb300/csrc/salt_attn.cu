@@ -1295,9 +1295,14 @@ int items_of(const RowTile &x, double most, int *per_item)
 // Of a unit of a tracked plan's lists of many rows, in steps of 128 rows: what it costs besides, and the least
 // that a part of one takes.
 constexpr int UNIT_COST = 3, LEAST_STEPS = 6;
-// A step on an SM, and a unit of few_cost there, as they balance the two kernels (the second one starts later; 64 decoding requests of four
-// prompts took 23.3 us with 0.07 for the latter, 19.0 with 0.12 and 0.16, 20.5 with 0.22; 48 with drafts 16.5, 13.6, 13.2 and 14.8).
-constexpr double STEP_US = 0.95, FEW_US = 0.15;
+// How the two kinds of lists share the SMs, by what either takes on some of them.  On one SM a step takes STEP_US and COPY_US for each copy that brings its queries (one
+// for 64 elements of all its tokens where they follow each other, else of each), a unit UNIT_US besides, a list's head of few rows LIST_US and a unit of its few_cost FEW_US
+// in the kernel for up to 16 rows a list, FEW64_US in the one for up to 64; either begins LATE_US later.  From 18 batches of 20 to 256 requests with heads of 64 and 128,
+// groups of 3 to 8 heads, prompts of 0 to 8,192 tokens and own tokens up to 8,000, each with 4 to 140 SMs for the many rows: their times on few SMs are such sums to
+// about 15%, and what these constants choose takes 4% more than the best share on average, 11% at most.  (A share of the SMs like that of STEP_US = 0.95 a step
+// and 0.15 a unit of few_cost, which suits 64 requests of 50 to 1,000 tokens, takes up to 93% more: 200 requests of 500 to 3,000 tokens 118 us where the best
+// is 65.)
+constexpr double STEP_US = 1.0, COPY_US = 0.014, UNIT_US = 0.5, LIST_US = 0.14, FEW_US = 0.044, FEW64_US = 0.068, LATE_US = 2.0;
 
 // Items of one cost.
 struct Same {
@@ -1527,10 +1532,11 @@ size_t fill_plan(salt_attn *a, const salt_attn_batch *b, int T, int32_t *w)
 // handed to the CTAs from the costliest down, each to the one that has least.  Where units are few or unequal, those of
 // many steps are split in parts, each a unit, that meet in a partial sum.  Where they are very many every CTA
 // takes each n_sm-th instead.
-void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int64_t few_cost, int32_t *t)
+// `runs`: whether the query tokens of each follow each other.
+void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int64_t few_cost, const std::vector<bool> &runs, int32_t *t)
 {
     Track &tr = a->track;
-    const int KV = a->kv->dev.heads, per = 128 / (a->cfg.n_heads / KV);
+    const int KV = a->kv->dev.heads, per = 128 / (a->cfg.n_heads / KV), parts_of_row = a->kv->dev.dim / 64;
     int n_sm = a->n_sm;
     tr.split = false;
     tr.many_sms = n_sm;
@@ -1542,18 +1548,31 @@ void fill_units(salt_attn *a, int n_few, int n_many, int64_t tiles, int64_t few_
     };
     std::vector<Tile> all;
     int64_t sum = 0;
+    double many_us = 0;
     for (int i = n_few; i < n_few + n_many; ++i) {
         const int32_t *l = t + tr.list_at + (size_t)i * LIST_WORDS;
         const int steps = (l[3] + per - 1) / per;
+        const double step_us = STEP_US + COPY_US * parts_of_row * (runs[i - n_few] ? 1 : std::min(per, l[3]));
         for (int j = 0; j < (l[1] + TRACK_MANY_TILE - 1) / TRACK_MANY_TILE; ++j) {
             all.push_back({l, j * TRACK_MANY_TILE, first_step(l[6] & 1, l[5], j * TRACK_MANY_TILE, per), steps});
             sum += steps - all.back().from;
+            many_us += KV * (UNIT_US + step_us * (steps - all.back().from));
         }
     }
-    // the two kinds of lists run beside each other, on SMs by what they take
+    // the two kinds of lists run beside each other, on SMs by what they take (units of few steps are not split: some SMs may get one more than others)
     if (n_few > 0) {
-        const double many_us = STEP_US * (double)(sum + UNIT_COST * (int64_t)all.size()), few_us = FEW_US * (double)few_cost;
-        n_sm = (int)std::min<int64_t>(n_sm - 1, std::max<int64_t>(1, (int64_t)std::llround(n_sm * many_us / (many_us + few_us))));
+        const double units = (double)all.size() * KV, few_us = KV * (LIST_US * n_few + (tr.few_rows <= 16 ? FEW_US : FEW64_US) * (double)few_cost);
+        const bool whole = sum < 2 * LEAST_STEPS * (int64_t)all.size();
+        double best = 1e300;
+        int share = 1;
+        for (int k = 1; k < n_sm; ++k) {
+            const double us = std::max(many_us * (whole ? std::ceil(units / k) / units : 1.0 / k), LATE_US + few_us / (n_sm - k));
+            if (us < best) {
+                best = us;
+                share = k;
+            }
+        }
+        n_sm = std::min(n_sm, share);
     }
     n_sm = (int)std::min<int64_t>(n_sm, (int64_t)all.size() * KV * 64);
     // a part takes at least what a unit costs besides its steps, a few times over
@@ -1631,16 +1650,18 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     };
     std::vector<Words> lists[2];   // of few rows, of many
     int64_t tiles[2] = {0, 0}, cost_before[2] = {0, 0};
-    auto add = [&](int pages, int len, int tok, int ntok, int old, int lim, bool causal) {
+    std::vector<bool> runs;        // of those of many
+    auto add = [&](int pages, int len, int tok, int ntok, int old, int lim, bool causal, bool run) {
         if (len == 0 || ntok == 0) return;
         const int kind = (int64_t)ntok * G > TRACK_FEW_ROWS, tile = kind ? TRACK_MANY_TILE : TRACK_TILE;
         if (!kind) tr.few_rows = std::max(tr.few_rows, ntok * G);
+        else runs.push_back(run);
         const int cost = kind ? 1 : few_cost(ntok * G), n = (len + tile - 1) / tile;
         lists[kind].push_back({{pages, len, tok, ntok, old, lim, causal | cost << 1, (int)cost_before[kind]}});
         cost_before[kind] += (int64_t)n * cost;
         tiles[kind] += n;
     };
-    std::vector<int> rows(b->n_groups, 0);  // query tokens of each group
+    std::vector<int> rows(b->n_groups, 0), begin(b->n_groups, 0), end(b->n_groups, 0);  // query tokens of each group, where its first and last ones are
     int t0 = 0;
     for (int i = 0; i < b->n_seqs; t0 += b->q_len[i], ++i) {
         int32_t *s = t + tr.seq_at + (size_t)i * SEQ_WORDS;
@@ -1652,12 +1673,17 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
         tr.chunks += b->kv_len[i] / evict_rows(kv.dim) + 1;
         note(b->pages + b->page_ptr[i], b->kv_len[i]);
         // (a request of more query than cached tokens: the first rows see nothing)
-        add(b->page_ptr[i], b->kv_len[i], t0, b->q_len[i], std::max(0, b->kv_len[i] - b->q_len[i]), b->kv_len[i] - b->q_len[i] + 1, true);
-        if (b->n_groups > 0 && b->group[i] >= 0) rows[b->group[i]] += b->q_len[i];
+        add(b->page_ptr[i], b->kv_len[i], t0, b->q_len[i], std::max(0, b->kv_len[i] - b->q_len[i]), b->kv_len[i] - b->q_len[i] + 1, true, true);
+        if (b->n_groups > 0 && b->group[i] >= 0 && b->q_len[i] > 0) {
+            const int g = b->group[i];
+            if (rows[g] == 0) begin[g] = t0;
+            end[g] = t0 + b->q_len[i];
+            rows[g] += b->q_len[i];
+        }
     }
     for (int g = 0, at = T; g < b->n_groups; at += rows[g], ++g) {
         note(b->group_pages + b->group_page_ptr[g], b->group_len[g]);
-        add(own_pages + b->group_page_ptr[g], b->group_len[g], at, rows[g], b->group_len[g], b->group_len[g], false);
+        add(own_pages + b->group_page_ptr[g], b->group_len[g], at, rows[g], b->group_len[g], b->group_len[g], false, end[g] - begin[g] == rows[g]);
     }
     int32_t *list = t + tr.list_at;
     for (const auto &kind : lists)
@@ -1673,7 +1699,7 @@ size_t fill_track(salt_attn *a, const salt_attn_batch *b, int T, int32_t *t)
     t[TH_MANY_TILES] = (int)tiles[1];
     t[TH_SHARED] = tr.shared;
     tr.few_tiles = tiles[0];
-    fill_units(a, tr.few, tr.many, tiles[1], cost_before[0], t);
+    fill_units(a, tr.few, tr.many, tiles[1], cost_before[0], runs, t);
     return t[TH_LISTED] ? (size_t)tr.unit_at + TRACK_CTAS + (size_t)tr.n_units * UNIT_WORDS : (size_t)(list - t);
 }
 

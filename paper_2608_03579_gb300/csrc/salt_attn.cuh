@@ -36,8 +36,9 @@ constexpr int TRACK_CTAS = 512, UNIT_WORDS = 12, TRACK_UNITS = 8192;
 constexpr int TRACK_SLOTS = 2048;  // of partial sums, 256 tokens each
 // Rows that eviction moves at a time: 16 KB of keys and values.
 constexpr int evict_rows(int dim) { return 8192 / dim; }
-// What a tile of a list of few rows costs, in quarters of one with a single row: of a tile of 128 tokens by its rows, 0.9 us with 4 and 2 with 80 (two CTAs an
-// SM).  Of many rows all count alike.
+// What a tile of 128 tokens of a list of few rows costs, in quarters of one with a single row.  (64 lists of 8,192 tokens with 8 heads of 64, of which an SM's two CTAs take
+// a tile in 0.37 us with 20 rows, 0.48 with 32, 0.61 with 48 and 0.75 with 64, where this says 5, 6, 8 and 9; three CTAs an SM, 0.26 with 1 and 8 rows, 0.28 with 16, where it
+// says 4, 4 and 5.)
 constexpr int few_cost(int rows) { return 4 + rows / 12; }
 // The first step of `per` query tokens that sees token t0.
 __host__ __device__ constexpr int first_step(bool causal, int lim, int t0, int per)
