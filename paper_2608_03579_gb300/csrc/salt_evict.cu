@@ -720,7 +720,10 @@ cudaError_t launch_evict(EvictParams &p, int n_sm, int layers, int longest, int6
     // SMs, of 6 at least 20 times (16 lines of 262,144 tokens: 151 us with 8, one of them in a second wave, 108 with 6, all else alike but for some shorter code).
     int ctas = 1;
     while (ctas < 6 && longest > 8192 * ctas && lines * (ctas + 1) <= n_sm) ++ctas;
-    const cudaError_t e1 = longest <= 2048 && lines > 2 * n_sm ? launch_select<128, ROWS>(p, lines, 1, stream, longest)
+    // Short lines that are more than a wave of CTAs of 256 threads, 8 an SM, go by CTAs of 128.  (All of an eviction that keeps 8 tokens: 2,432 lines of 500, 1,000,
+    // 2,040 and 4,000 tokens 29, 32, 39 and 51 us with 128 threads, 33, 37, 41 and 52 with 256; 1,824 lines 27, 29, 31 and 43, 27, 29, 33 and 41; 1,216 lines
+    // 24, 27, 29 and 29, 21, 22, 25 and 30; 304 lines 19, 22, 24 and 24, 16, 18, 20 and 26.)
+    const cudaError_t e1 = longest <= 2048 && lines > 8 * n_sm ? launch_select<128, ROWS>(p, lines, 1, stream, longest)
                            : longest <= 4096                   ? launch_select<256, ROWS>(p, lines, 1, stream, longest)
                                                                : launch_select<1024, ROWS>(p, lines, ctas, stream, longest);
     cudaError_t e = e1;

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_evict import ARRAYS, Cache
+from test_gpu_evict import ARRAYS, Cache, scores_of
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,12 @@ def test_whole_lines_and_shared_ones(salt_lib, ctx, dim, page, requests, part):
     c = Cache(salt_lib, ctx, lens, kv_heads=4, dim=dim, page=page, layers=4, seed=3)
     g = torch.Generator(device="cuda").manual_seed(4)
     c.check(keep, torch.randn(c.t["weights"].shape, device="cuda", generator=g), 4, 100)
+
+
+@pytest.mark.parametrize("kind", ["ties", "close", "strange"])
+def test_more_lines_than_a_wave(salt_lib, ctx, kind):
+    """Lines up to the longest that the smallest CTAs search."""
+    r = np.random.RandomState(7)
+    lens = [2048, 1, 2047] + [int(n) for n in r.randint(1, 900, 157)]
+    c = Cache(salt_lib, ctx, lens, kv_heads=8, dim=64, page=64, layers=1, seed=8)
+    c.check([int(n * r.uniform(0.0, 1.0)) for n in lens], scores_of(c, kind), 2, 5)
