@@ -760,7 +760,7 @@ salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t
  * too.  A build then copies a further table (some words a request and group, up to 400 KB
  * where many rows see a list of cached tokens), and the plan has more device memory, which
  * salt_attn_get_shape counts: 3 MB and eight bytes for every 16 KB of cached keys and values of up to
- * 2^22 such pieces.  Synchronous.
+ * 2^22 such pieces.  On the host it takes 2 to 24 us longer (one byte a page of the cache is cleared, and work is dealt out).  Synchronous.
  */
 salt_status salt_attn_track(salt_attn *plan);
 
@@ -774,7 +774,9 @@ salt_status salt_attn_track(salt_attn *plan);
  * and counts as 0.  weights is float [n_layers][n_pages][n_kv_heads][page_tokens], laid out as
  * k_exp, 16-byte aligned; tokens that no row sees stay as they are.  q and scale are those
  * that salt_attn_run was given for this layer, lse [tokens][n_heads] what it returned.  Scores and sums are
- * fp32.  A token's weight is NaN if its key stands for NaN or if there is a NaN in the
+ * fp32.  For tokens that at most 64 rows see (their list's, query tokens times query heads of a key/value head) the query meets
+ * the keys as the sum of two e4m3 terms, whole but for elements below 2^-14 of their row's largest, which are off by up to 2^-22 of that; for others as it
+ * is.  A token's weight is NaN if its key stands for NaN or if there is a NaN in the
  * query or the log-sum of a row that sees it (salt_attn_run leaves a NaN log-sum for a query with an
  * infinity); a row that sees nothing adds nothing, whatever it holds.  Results do not depend on timing.  A plan that was not built since
  * salt_attn_track is refused (SALT_ERR_NOT_BUILT), and so is a batch that lists a page twice, for two requests or

@@ -10,15 +10,15 @@
 // Lists of up to 64 rows (single query tokens, a few drafts, a prompt that some requests share) are bound by reading the keys, and that by what a tile
 // costs besides: their e4m3 codes go to the
 // tensor cores as they are, one tile of 128 tokens after the other, and meet the query as two e4m3 terms, hi + 2^-5
-// lo: 4 and 4 bits, so a bf16 whole but for elements 2^-15 below the row's largest (2^-22 of
+// lo: 4 and 4 bits, so a bf16 whole but for elements below 2^-14 of the row's largest (off by up to 2^-22 of
 // that).  The two terms have columns of their own, as lo would lose its small elements without its factor.
 //
 // Lists of many rows are bound by the products and exponentials: 256 tokens' keys are widened to bf16 once
 // (exact) and stay, the query's rows stream past them as they are.
 //
-// Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 19 us, four prompt
-// chunks of 900 to 2,048 tokens behind 4,096 221 us (1,170 TFLOP/s, 61% of the products' measured rate; 1.0e9 exponentials, whose pipe
-// is 53% busy as the tensor cores are).
+// Two requests of 200,000 tokens and more with heads of 64 take 47 us (5.4 TB/s), 64 decoding requests with four prompts of 4,096 20 us, four prompt
+// chunks of 900 to 2,048 tokens behind 4,096 215 us (1,210 TFLOP/s, 63% of the products' measured rate; 1.0e9 exponentials, whose pipe
+// is 54% busy as the tensor cores are).
 #include <algorithm>
 #include <cmath>
 #include <new>
