@@ -760,7 +760,7 @@ salt_status salt_attn_run(salt_attn *plan, int32_t layer, const void *q, int64_t
  * too.  A build then copies a further table (some words a request and group, up to 400 KB
  * where many rows see a list of cached tokens), and the plan has more device memory, which
  * salt_attn_get_shape counts: 3 MB and eight bytes for every 16 KB of cached keys and values of up to
- * 2^22 such pieces.  On the host it takes 2 to 24 us longer (one byte a page of the cache is cleared, and work is dealt out).  Synchronous.
+ * 2^22 such pieces.  On the host it takes 1 to 25 us longer (work is dealt out), and 25 more for a million pages of the cache.  Synchronous.
  */
 salt_status salt_attn_track(salt_attn *plan);
 

@@ -13,7 +13,7 @@
 //
 // 8 layers of 32 requests of 1,200 to 2,048 tokens with 8 heads of 128: 166 us, 23 for the search (the scores lie in the L2 after the first
 // digit; shuffles and shared atomics, issue slots at 59%) and 143 for the move (6.1 TB/s of rows, those of a line's first kept
-// tokens that stay where they are neither read nor written).  Two requests of 200,000 tokens and more with heads of 64: 115 us, 38 and 77.
+// tokens that stay where they are neither read nor written).  Two requests of 200,000 tokens and more with heads of 64: 113 us, 37 and 76.
 #include <algorithm>
 #include <new>
 
