@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     constexpr bool ALONE = THREADS < 1024;              // a line has one CTA
     constexpr int HISTS = ALONE ? 1 : DIGITS;           // (other CTAs may still read the last digit's)
     extern __shared__ __align__(16) uint32_t s_keys[];
-    __shared__ __align__(16) uint32_t s_hist[HISTS][BINS], s_coarse[HISTS][BINS / 32], s_total[96], s_warp[32], s_held[WARPS], s_tied[WARPS], s_all[2];
+    __shared__ __align__(16) uint32_t s_hist[HISTS][BINS], s_coarse[HISTS][BINS / 32], s_total[96], s_warp[32], s_held[WARPS], s_tied[WARPS], s_all[2], s_most;
     pdl_wait();
     // (the warp's number from a shuffle, so that branches by it are known to be taken by whole warps)
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, n_seqs = p.track[TH_SEQS];
@@ -168,6 +168,7 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
     if (blockIdx.x == 0) {  // the chunks of every request, once for all layers and heads
         int before = 0;
         uint32_t losing = 0;
+        if (tid == 0) s_most = 0;
         for (int s0 = 0; fits && s0 < n_seqs; s0 += THREADS) {
             const int s = s0 + tid, keep = s < n_seqs ? kept_of(p, s, p.track[p.seq_at + s * SEQ_WORDS + 1]) : 0;
             if (keep < 0) atomicOr(p.err, SALT_DEVERR_KEEP);
@@ -177,8 +178,16 @@ __global__ void __launch_bounds__(THREADS) evict_select_kernel(const __grid_cons
             before += (int)all;
             if (!p.whole) continue;
             const uint32_t at = block_scan(n > 0, s_warp, &all);
-            if (n > 0) p.losing[losing + at] = s;
+            if (n > 0) {
+                p.losing[losing + at] = s;
+                atomicMax(&s_most, n);
+            }
             losing += all;
+        }
+        if (p.whole) {  // lines of very different lengths are all shared: a CTA with a long one would be at it when the others are done
+                        // (8 lines of 60,000 tokens among 240 of 1,500: 415 us whole, 122 shared)
+            __syncthreads();
+            if (4ll * s_most * losing > 5ll * before) losing = 0;
         }
         if (tid == 0) {
             p.chunk_ptr[0] = 0;
